@@ -788,6 +788,156 @@ int32_t rk_schedule_round_nodes(rk_ctx *ctx, const rk_jobs *jobs, const rk_plan_
                                 rk_assign *assign, rk_assign *placed, uint32_t *place_off, rk_place_entry *entries,
                                 uint64_t cap_entries, float *total, uint32_t *stats_or_null);
 
+/* ---- operators of a training step ------------------------------------------
+ *
+ * The descriptors above hold what was measured of a job: the forward seconds
+ * of a sample, the backward's share, the activation bytes (Sec. 4.1, Sec. 4.3).
+ * These are the operators that such a job runs between its matrix products, for
+ * steps to be measured on this GPU: the norms around a block, the router of a
+ * mixture of experts, the loss of a student.
+ *
+ * Matrices (rk_matrix) have rows of consecutive elements; row i begins
+ * i * stride elements behind data.  Unlike the other [device] pointers of this
+ * header, those of the operators need only their element's alignment.  Strides are
+ * not smaller than the width; outputs may not overlap inputs except where
+ * stated, nor each other.  Every sum, statistic and softmax is held in 32 bits,
+ * sums over all rows or tokens in fixed order, so that equal calls return equal
+ * bits.  A matrix without rows is no error: sums over its rows are zero.  With
+ * the same shapes a call allocates nothing after the first, waits for nothing
+ * and can be captured into a graph. */
+#define RK_F32   0u
+#define RK_BF16  1u
+#define RK_F16   2u
+
+typedef struct {
+    void *data;                 /* [device] */
+    uint64_t stride;            /* elements from row to row */
+    uint32_t type;              /* RK_F32, RK_BF16 or RK_F16 */
+} rk_matrix;
+
+#define RK_NORM_NONE   0u
+#define RK_NORM_RMS    1u   /* v / sqrt(mean(v^2) + eps) */
+#define RK_NORM_LAYER  2u   /* (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) */
+#define RK_NORM_MAX_WIDTH 32768u
+
+/* The join of a block's output y and the residual stream x, up to the input u
+ * of the next block:
+ *     n = post(y) * post_weight + post_bias        x_out = res_scale * x + gate * n
+ *     u = pre(x_out) * pre_weight + pre_bias       (of x_out before it is rounded)
+ * Vectors are width elements of param_type [device]; a null weight or gate
+ * stands for ones, a null bias for zeros.  A side whose kind is RK_NORM_NONE has
+ * neither weight nor bias (post: n = y; pre: no u).  gate_rows = 0: one gate for all rows; otherwise
+ * row i has gate i / gate_rows, gates lying gate_stride elements apart. */
+typedef struct {
+    uint32_t post_kind, pre_kind;
+    float post_eps, pre_eps;
+    float res_scale;
+    uint32_t param_type;
+    const void *post_weight, *post_bias, *pre_weight, *pre_bias, *gate;
+    uint64_t gate_rows, gate_stride;
+} rk_norm_block;
+
+/* Gradients of a block's vectors, float32 [device]; those not wanted, or whose
+ * vector is null, are null.  Gates' gradients lie gate_stride elements apart. */
+typedef struct {
+    float *post_weight, *post_bias, *pre_weight, *pre_bias, *gate;
+    uint64_t gate_stride;
+} rk_norm_grads;
+
+/* x, x_out share a type: that of y and u, or RK_F32.  y null: x_out = res_scale * x (the
+ * stream's first norm; post_kind RK_NORM_NONE, no gate).  x_out null: not kept.  u null
+ * exactly if pre_kind is RK_NORM_NONE.  x_out may be x, u may be y (same data and stride).
+ *   stats  [device] n_rows x 4 floats: mean and 1/sqrt(..) of y, the same of
+ *          x_out (mean 0 for RK_NORM_RMS; 0 and 1 for RK_NORM_NONE); for the backward pass
+ * Rows of 1 to RK_NORM_MAX_WIDTH elements. */
+int32_t rk_norm_forward(rk_ctx *ctx, const rk_norm_block *block, uint64_t n_rows, uint32_t width,
+                        const rk_matrix *x, const rk_matrix *y_or_null, const rk_matrix *x_out_or_null,
+                        const rk_matrix *u_or_null, float *stats);
+
+/* From the gradients of x_out (dx_out, null: zero) and u (du; null exactly if
+ * there is no u), and the x_out, y and stats of the forward pass, the gradients
+ * of x and y (dy null exactly if y is) and of the vectors (grads or null).
+ * dx and dx_out have x_out's type, dy and du have y's. */
+int32_t rk_norm_backward(rk_ctx *ctx, const rk_norm_block *block, uint64_t n_rows, uint32_t width,
+                         const rk_matrix *x_out, const rk_matrix *y_or_null, const float *stats,
+                         const rk_matrix *dx_out_or_null, const rk_matrix *du_or_null, const rk_matrix *dx,
+                         const rk_matrix *dy_or_null, const rk_norm_grads *grads_or_null);
+
+#define RK_MAX_EXPERTS  1024u
+#define RK_MAX_TOP_K    32u
+
+/* A router over n_experts logits a token.  group_tokens: the tokens that one
+ * balance is taken over (a sequence), 0: all; the last group may have fewer. */
+typedef struct {
+    uint32_t n_experts, top_k;
+    uint32_t renormalise;       /* 1: a token's weights sum to one */
+    uint64_t group_tokens;
+} rk_router;
+
+/* p = softmax of a token's logits; its top_k largest logits, the largest first, equal
+ * ones by index; weight = p of these, or p over their sum.  Logits of -inf or
+ * NaN are never chosen: what is left of expert is then -1, of weight 0.  A
+ * token whose mask byte is 0, or without a logit above -inf, is left out:
+ * expert -1, weight and lse 0, counted nowhere, whatever its logits hold.  Over the n_g tokens that count of
+ * each group, G' of the G groups having any, and the n tokens of all:
+ *     counts[g][e]   tokens that chose e          prob_sum[g][e]  sum of p[e]
+ *     balance = 1/G' sum_g n_experts / (top_k n_g^2) sum_e counts[g][e] prob_sum[g][e]
+ *     z       = 1/n sum of lse^2,                 lse = log sum exp of a token's logits
+ *   mask      [device] n_tokens bytes or NULL
+ *   expert    [device] n_tokens * top_k;  weight [device] likewise;  lse [device] n_tokens
+ *   counts, prob_sum  [device] G * n_experts;  tokens  [device] G: the n_g
+ *   loss      [device] two floats: balance, z (0 if no token counts) */
+int32_t rk_route_forward(rk_ctx *ctx, const rk_router *router, uint64_t n_tokens, const rk_matrix *logits,
+                         const uint8_t *mask_or_null, int32_t *expert, float *weight, float *lse,
+                         uint32_t *counts, float *prob_sum, uint32_t *tokens, float *loss);
+
+/* The gradient of the logits from those of loss (d_loss [device] two floats)
+ * and weight (d_weight [device] n_tokens * top_k, or NULL: zero); counts are constants. expert, lse, counts and
+ * tokens are the forward pass's.  d_logits has the logits' type and may be
+ * the logits; 0 for tokens that are left out. */
+int32_t rk_route_backward(rk_ctx *ctx, const rk_router *router, uint64_t n_tokens, const rk_matrix *logits,
+                          const int32_t *expert, const float *lse, const uint32_t *counts, const uint32_t *tokens,
+                          const float *d_loss, const float *d_weight_or_null, const rk_matrix *d_logits);
+
+#define RK_MAX_TEACHER_LOGITS 1024u
+
+/* A student's loss against a teacher of whom the largest logits are kept:
+ *     loss = kd_weight T^2 sum_k q_k (log q_k - log p_T[index_k]) + ce_weight (-log p_1[label])
+ * q = softmax(teacher / T) over a row's kept logits, p_T = softmax(student / T). */
+typedef struct {
+    float temperature;          /* T > 0 */
+    float kd_weight, ce_weight; /* >= 0 and finite, not both 0 */
+} rk_distill;
+
+/* What the rows are compared with.  An index outside the vocabulary is no kept
+ * logit (nor is a logit of -inf), a label outside it no label; indices that repeat add up.  A
+ * row without a kept logit has no first term, one without a label no second. */
+typedef struct {
+    const rk_matrix *logits;    /* n_rows x top_k, any type; null exactly if kd_weight is 0 */
+    const int32_t *index;       /* [device] n_rows * top_k */
+    uint32_t top_k;
+    const int32_t *label;       /* [device] n_rows; null exactly if ce_weight is 0 */
+    const float *row_weight;    /* [device] n_rows or NULL: ones */
+} rk_teacher;
+
+/* loss [device] n_rows (unweighted); lse [device] n_rows x 2: log sum exp of student / T and of student, 0
+ * where its term's weight is 0; total [device] one float: sum of row_weight * loss.
+ * Rows whose weight is 0 are not read: loss and lse 0.  Rows without a logit
+ * above -inf have loss 0 and lse -inf. */
+int32_t rk_distill_loss(rk_ctx *ctx, const rk_distill *distill, uint64_t n_rows, uint32_t vocab,
+                        const rk_matrix *student, const rk_teacher *teacher, float *loss, float *lse, float *total);
+
+/* The gradient of the student's logits from that of total (d_total [device] one
+ * float, NULL: one) and the forward pass's lse; 0 for rows that are left out. d_student has the student's type. */
+int32_t rk_distill_backward(rk_ctx *ctx, const rk_distill *distill, uint64_t n_rows, uint32_t vocab,
+                            const rk_matrix *student, const rk_teacher *teacher, const float *lse,
+                            const float *d_total_or_null, const rk_matrix *d_student);
+
+/* Both at once, where the gradient of total is known beforehand. */
+int32_t rk_distill_loss_backward(rk_ctx *ctx, const rk_distill *distill, uint64_t n_rows, uint32_t vocab,
+                                 const rk_matrix *student, const rk_teacher *teacher, const float *d_total_or_null,
+                                 float *loss, float *lse, float *total, const rk_matrix *d_student);
+
 /* ---- measurement helper (no part of the method) --------------------------- */
 
 /* Streams a buffer and nothing else, for the benchmark's roofline context:

@@ -26,7 +26,9 @@ FIT_FIELDS = ("k_bwd", "k_sync", "k_opt", "k_opt_off", "k_off", "k_swap", "k_con
 EXPORTS = ("rk_create", "rk_destroy", "rk_sync", "rk_last_error", "rk_enumerate_plans", "rk_eval_candidates",
            "rk_best_plan", "rk_curves", "rk_job_curves", "rk_allocate", "rk_schedule_round", "rk_schedule_rounds",
            "rk_eval_points", "rk_min_res", "rk_allocate_sla", "rk_schedule_round_sla", "rk_fit_models", "rk_simulate", "rk_schedule_rounds_shared", "rk_place", "rk_allocate_static", "rk_place_plans",
-           "rk_schedule_round_placed", "rk_reschedule", "rk_probe_stream", "rk_eval_best_plan", "rk_reschedule_nodes", "rk_best_plan_placed", "rk_reschedule_rounds", "rk_schedule_round_nodes", "rk_privileged", "rk_curve_slopes")
+           "rk_schedule_round_placed", "rk_reschedule", "rk_probe_stream", "rk_eval_best_plan", "rk_reschedule_nodes", "rk_best_plan_placed", "rk_reschedule_rounds", "rk_schedule_round_nodes", "rk_privileged", "rk_curve_slopes",
+           "rk_norm_forward", "rk_norm_backward", "rk_route_forward", "rk_route_backward", "rk_distill_loss",
+           "rk_distill_backward", "rk_distill_loss_backward")
 
 _JOB_F32 = ("P_bytes", "seq", "hidden", "elem_bytes", "t_fwd_sample", "k_bwd", "k_sync", "k_opt", "k_opt_off",
             "k_off", "k_swap", "k_const", "mem_state", "mem_act", "mem_act_gc", "mem_const", "ref_thr")
@@ -604,3 +606,246 @@ def assign_to_numpy(t) -> np.ndarray:
 def u32(t) -> np.ndarray:
     """Host copy of an int32 device tensor reinterpreted as uint32."""
     return t.cpu().numpy().view(np.uint32)
+
+
+# ------------------------------------------------------------------ operators of a training step
+RK_F32, RK_BF16, RK_F16 = 0, 1, 2
+RK_NORM_KINDS = {"none": 0, "rms": 1, "layer": 2}
+RK_NORM_MAX_WIDTH, RK_MAX_EXPERTS, RK_MAX_TOP_K, RK_MAX_TEACHER_LOGITS = 32768, 1024, 32, 1024
+
+
+class rk_matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_uint64), ("type", C.c_uint32)]
+
+
+class rk_norm_block(C.Structure):
+    _fields_ = [("post_kind", C.c_uint32), ("pre_kind", C.c_uint32), ("post_eps", C.c_float), ("pre_eps", C.c_float),
+                ("res_scale", C.c_float), ("param_type", C.c_uint32)] + \
+               [(n, C.c_void_p) for n in ("post_weight", "post_bias", "pre_weight", "pre_bias", "gate")] + \
+               [("gate_rows", C.c_uint64), ("gate_stride", C.c_uint64)]
+
+
+class rk_norm_grads(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("post_weight", "post_bias", "pre_weight", "pre_bias", "gate")] + [("gate_stride", C.c_uint64)]
+
+
+class rk_router(C.Structure):
+    _fields_ = [("n_experts", C.c_uint32), ("top_k", C.c_uint32), ("renormalise", C.c_uint32), ("group_tokens", C.c_uint64)]
+
+
+class rk_distill(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("kd_weight", C.c_float), ("ce_weight", C.c_float)]
+
+
+class rk_teacher(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("index", C.c_void_p), ("top_k", C.c_uint32), ("label", C.c_void_p),
+                ("row_weight", C.c_void_p)]
+
+
+def _refuse(what):
+    raise RkError(RK_ERR_INVALID_ARG, what)
+
+
+def _type_of(t):
+    import torch
+    types = {torch.float32: RK_F32, torch.bfloat16: RK_BF16, torch.float16: RK_F16}
+    if t.dtype not in types:
+        _refuse(f"{t.dtype} is none of float32, bfloat16, float16")
+    return types[t.dtype]
+
+
+def _matrix(t, name, shape=None):
+    """A [rows, width] tensor, its rows of consecutive elements, as an rk_matrix; the tensor has to outlive the call."""
+    if t is None:
+        return None
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        _refuse(f"{name} is no matrix of consecutive row elements")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        _refuse(f"{name} is {tuple(t.shape)}, not {tuple(shape)}")
+    stride = t.stride(0)
+    if t.shape[0] > 1 and stride < t.shape[1]:
+        _refuse(f"the rows of {name} overlap")
+    return rk_matrix(t.data_ptr(), max(stride, t.shape[1]), _type_of(t))
+
+
+def _plain(t, name, shape, dtypes):
+    """A contiguous tensor of that shape and of one of these types, or None."""
+    if t is not None and (tuple(t.shape) != tuple(shape) or not t.is_contiguous() or str(t.dtype)[6:] not in dtypes):
+        _refuse(f"{name} is no contiguous {' or '.join(dtypes)} tensor of shape {tuple(shape)}")
+    return _ptr(t)
+
+
+def _same_device(*tensors):
+    devices = {t.device for t in tensors if t is not None}
+    if len(devices) > 1 or any(d.type != "cuda" for d in devices):
+        _refuse("the tensors are not on one GPU")
+
+
+def _ref(s):
+    return None if s is None else C.byref(s)
+
+
+class NormBlock:
+    """The norms around a block with its gate and residual scale (rk_norm_block).  post and pre: "none", "rms" or "layer";
+    vectors are [width] tensors of one type, gate is [1, width] for all rows (gate_rows 0) or [gates, width], one for every
+    gate_rows rows."""
+
+    def __init__(self, post="rms", pre="rms", post_weight=None, post_bias=None, pre_weight=None, pre_bias=None, gate=None,
+                 gate_rows=0, res_scale=1.0, post_eps=1e-6, pre_eps=1e-6):
+        if post not in RK_NORM_KINDS or pre not in RK_NORM_KINDS:
+            _refuse(f"norms are one of {tuple(RK_NORM_KINDS)}")
+        self.vectors = {"post_weight": post_weight, "post_bias": post_bias, "pre_weight": pre_weight, "pre_bias": pre_bias}
+        self.gate = gate
+        given = [t for t in (*self.vectors.values(), gate) if t is not None]
+        self.width = int(given[0].shape[-1]) if given else None
+        _same_device(*given)
+        if len({t.dtype for t in given}) > 1:
+            _refuse("weights, biases and gate are of one type")
+        for name, t in self.vectors.items():
+            if t is not None and (tuple(t.shape) != (self.width,) or not t.is_contiguous()):
+                _refuse(f"{name} is no contiguous vector of {self.width} elements")
+        c_gate = _matrix(gate, "gate")
+        if gate is not None and (gate.shape[1] != self.width or (gate_rows == 0 and gate.shape[0] != 1)):
+            _refuse("gate is [1, width], or [gates, width] with gate_rows")
+        self.c = rk_norm_block(RK_NORM_KINDS[post], RK_NORM_KINDS[pre], post_eps, pre_eps, res_scale,
+                               _type_of(given[0]) if given else RK_F32,
+                               *[None if t is None else t.data_ptr() for t in self.vectors.values()],
+                               None if gate is None else gate.data_ptr(), int(gate_rows),
+                               c_gate.stride if c_gate is not None else 0)
+
+    def _rows(self, t, name):
+        if t.dim() != 2 or (self.width is not None and t.shape[1] != self.width):
+            _refuse(f"{name} has no rows of {self.width} elements")
+        rows = int(t.shape[0])
+        if self.gate is not None and self.c.gate_rows and self.gate.shape[0] * self.c.gate_rows < rows:
+            _refuse(f"{self.gate.shape[0]} gates of {self.c.gate_rows} rows for {rows} rows")
+        return rows, int(t.shape[1])
+
+
+class NormGrads:
+    """Room for the gradients of a block's vectors, float32; `tensors` by name (all that the block has, or those named)."""
+
+    def __init__(self, block: NormBlock, names=None):
+        import torch
+        have = dict(block.vectors, gate=block.gate)
+        self.tensors = {n: torch.empty(t.shape, dtype=torch.float32, device=t.device) for n, t in have.items()
+                        if t is not None and (names is None or n in names)}
+        ptr = {n: t.data_ptr() for n, t in self.tensors.items()}
+        self.c = rk_norm_grads(*[ptr.get(n) for n in ("post_weight", "post_bias", "pre_weight", "pre_bias", "gate")],
+                               block.width or 0)
+
+
+def _block_tensors(block):
+    return (*block.vectors.values(), block.gate)
+
+
+def rk_norm_forward(ctx, block: NormBlock, x, y, x_out, u, stats):
+    """y, x_out and u may be None as the header says; stats is [rows, 4] float32."""
+    rows, width = block._rows(x, "x")
+    _same_device(x, y, x_out, u, stats, *_block_tensors(block))
+    m = [_matrix(t, n, (rows, width)) for t, n in ((x, "x"), (y, "y"), (x_out, "x_out"), (u, "u"))]
+    _check(ctx, load_library().rk_norm_forward(ctx, C.byref(block.c), C.c_uint64(rows), C.c_uint32(width), *[_ref(a) for a in m],
+                                               _plain(stats, "stats", (rows, 4), ("float32",))))
+
+
+def rk_norm_backward(ctx, block: NormBlock, x_out, y, stats, dx_out, du, dx, dy, grads: NormGrads = None):
+    rows, width = block._rows(x_out, "x_out")
+    _same_device(x_out, y, stats, dx_out, du, dx, dy, *_block_tensors(block), *(grads.tensors.values() if grads else ()))
+    for n, t in (grads.tensors if grads else {}).items():
+        have = block.gate if n == "gate" else block.vectors[n]
+        if have is None or have.shape != t.shape:
+            _refuse(f"the gradient of {n} is another block's")
+    m = [_matrix(t, n, (rows, width)) for t, n in ((x_out, "x_out"), (y, "y"), (dx_out, "dx_out"), (du, "du"), (dx, "dx"), (dy, "dy"))]
+    _check(ctx, load_library().rk_norm_backward(ctx, C.byref(block.c), C.c_uint64(rows), C.c_uint32(width), _ref(m[0]), _ref(m[1]),
+                                                _plain(stats, "stats", (rows, 4), ("float32",)), *[_ref(a) for a in m[2:]],
+                                                _ref(grads.c if grads else None)))
+
+
+def make_router(n_experts, top_k, renormalise=True, group_tokens=0) -> rk_router:
+    return rk_router(int(n_experts), int(top_k), int(bool(renormalise)), int(group_tokens))
+
+
+def _router_sizes(router, logits):
+    if logits.dim() != 2 or logits.shape[1] != router.n_experts:
+        _refuse(f"logits are not [tokens, {router.n_experts}]")
+    n = int(logits.shape[0])
+    per = router.group_tokens if 0 < router.group_tokens else max(n, 1)
+    return n, (n + per - 1) // per if router.group_tokens else 1
+
+
+def rk_route_forward(ctx, router: rk_router, logits, mask, expert, weight, lse, counts, prob_sum, tokens, loss):
+    """mask uint8 [tokens] or None; expert int32 and weight float32 [tokens, top_k]; lse [tokens]; counts int32 and prob_sum
+    [groups, experts]; tokens int32 [groups]; loss [2]: balance, z."""
+    n, groups = _router_sizes(router, logits)
+    _same_device(logits, mask, expert, weight, lse, counts, prob_sum, tokens, loss)
+    k, e = router.top_k, router.n_experts
+    _check(ctx, load_library().rk_route_forward(
+        ctx, C.byref(router), C.c_uint64(n), _ref(_matrix(logits, "logits")), _plain(mask, "mask", (n,), ("uint8", "bool")),
+        _plain(expert, "expert", (n, k), ("int32",)), _plain(weight, "weight", (n, k), ("float32",)),
+        _plain(lse, "lse", (n,), ("float32",)), _plain(counts, "counts", (groups, e), ("int32",)),
+        _plain(prob_sum, "prob_sum", (groups, e), ("float32",)), _plain(tokens, "tokens", (groups,), ("int32",)),
+        _plain(loss, "loss", (2,), ("float32",))))
+
+
+def rk_route_backward(ctx, router: rk_router, logits, expert, lse, counts, tokens, d_loss, d_weight, d_logits):
+    n, groups = _router_sizes(router, logits)
+    _same_device(logits, expert, lse, counts, tokens, d_loss, d_weight, d_logits)
+    k, e = router.top_k, router.n_experts
+    _check(ctx, load_library().rk_route_backward(
+        ctx, C.byref(router), C.c_uint64(n), _ref(_matrix(logits, "logits")), _plain(expert, "expert", (n, k), ("int32",)),
+        _plain(lse, "lse", (n,), ("float32",)), _plain(counts, "counts", (groups, e), ("int32",)),
+        _plain(tokens, "tokens", (groups,), ("int32",)), _plain(d_loss, "d_loss", (2,), ("float32",)),
+        _plain(d_weight, "d_weight", (n, k), ("float32",)), _ref(_matrix(d_logits, "d_logits", (n, e)))))
+
+
+def make_distill(temperature=1.0, kd_weight=1.0, ce_weight=0.0) -> rk_distill:
+    return rk_distill(float(temperature), float(kd_weight), float(ce_weight))
+
+
+class _Teacher:
+    """rk_teacher of a call's tensors, checked against the student's rows."""
+
+    def __init__(self, student, logits, index, label, row_weight):
+        if student.dim() != 2:
+            _refuse("student is not [rows, vocab]")
+        self.rows, self.vocab = int(student.shape[0]), int(student.shape[1])
+        _same_device(student, logits, index, label, row_weight)
+        self.student = _matrix(student, "student")
+        if (logits is None) != (index is None):
+            _refuse("the teacher's logits and their indices go together")
+        k = 0 if logits is None else int(logits.shape[-1])
+        self.logits = _matrix(logits, "teacher_logits", (self.rows, k)) if logits is not None else None
+        self.c = rk_teacher(C.cast(C.byref(self.logits), C.c_void_p) if self.logits is not None else None,
+                            _plain(index, "teacher_index", (self.rows, k), ("int32",)), k,
+                            _plain(label, "label", (self.rows,), ("int32",)),
+                            _plain(row_weight, "row_weight", (self.rows,), ("float32",)))
+        self.sizes = (C.c_uint64(self.rows), C.c_uint32(self.vocab), C.byref(self.student), C.byref(self.c))
+
+    def results(self, loss, lse, total):
+        _same_device(loss, lse, total)
+        return (_plain(loss, "loss", (self.rows,), ("float32",)), _plain(lse, "lse", (self.rows, 2), ("float32",)),
+                _plain(total, "total", (1,), ("float32",)))
+
+
+def rk_distill_loss(ctx, distill: rk_distill, student, teacher_logits, teacher_index, label, row_weight, loss, lse, total):
+    """teacher_logits [rows, k] with teacher_index int32 (None if kd_weight is 0); label int32 [rows] (None if ce_weight is 0);
+    row_weight float32 [rows] or None; loss [rows], lse [rows, 2], total [1], all float32."""
+    t = _Teacher(student, teacher_logits, teacher_index, label, row_weight)
+    _check(ctx, load_library().rk_distill_loss(ctx, C.byref(distill), *t.sizes, *t.results(loss, lse, total)))
+
+
+def rk_distill_backward(ctx, distill: rk_distill, student, teacher_logits, teacher_index, label, row_weight, lse, d_total, d_student):
+    t = _Teacher(student, teacher_logits, teacher_index, label, row_weight)
+    _same_device(student, lse, d_total, d_student)
+    _check(ctx, load_library().rk_distill_backward(
+        ctx, C.byref(distill), *t.sizes, _plain(lse, "lse", (t.rows, 2), ("float32",)), _plain(d_total, "d_total", (1,), ("float32",)),
+        _ref(_matrix(d_student, "d_student", (t.rows, t.vocab)))))
+
+
+def rk_distill_loss_backward(ctx, distill: rk_distill, student, teacher_logits, teacher_index, label, row_weight, d_total, loss, lse,
+                             total, d_student):
+    t = _Teacher(student, teacher_logits, teacher_index, label, row_weight)
+    _same_device(student, d_total, loss, d_student)
+    _check(ctx, load_library().rk_distill_loss_backward(
+        ctx, C.byref(distill), *t.sizes, _plain(d_total, "d_total", (1,), ("float32",)), *t.results(loss, lse, total),
+        _ref(_matrix(d_student, "d_student", (t.rows, t.vocab)))))

@@ -9,7 +9,7 @@
 
 #include "rubick.h"
 
-enum { RK_SCRATCH_SLOTS = 64 };
+enum { RK_SCRATCH_SLOTS = 72 };
 
 // How often a context's calls went which way: for tests of the rules that choose (rk_ctx_ways and, for those behind
 // WAY_COUNT, rk_ctx_ways_eval; not in rubick.h).
@@ -73,6 +73,8 @@ enum {
     SL_ND_STATES,                                        // ... in a simulation: what is kept of every job in every state
     SL_FEW_STATES,                                       // simulation from scratch: the walks of all jobs
     SL_FIT_NEXT,                                         // model fitting: the next model to take
+    SL_NORM_PARTS, SL_NORM_ROWS,                         // norms around a block: sums of the chunks of rows; per row, what its gradient takes off
+    SL_ROUTE_COUNTS, SL_ROUTE_PROBS, SL_ROUTE_Z, SL_ROUTE_GROUPS,   // router: its workgroups' counts and sums, its groups'
     SL_COUNT
 };
 static_assert(SL_COUNT <= RK_SCRATCH_SLOTS, "more scratch slots than the context holds");

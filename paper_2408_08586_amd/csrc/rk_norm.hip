@@ -1,0 +1,572 @@
+// The join of a block and its residual stream: norm of the block's output, gate, scaled residual, norm before the next
+// block, forward and backward (rk_norm_forward, rk_norm_backward).
+#include <cmath>
+
+#include "rk_vec.h"
+
+namespace {
+
+enum { G_POST_W, G_POST_B, G_PRE_W, G_PRE_B, G_GATE, G_VECTORS };
+
+struct NormArgs {
+    const void *x, *y, *dxo, *du;       // forward: x; backward: x_out
+    void *xo, *u;                       // forward: x_out, u; backward: dx, dy
+    uint64_t x_st, y_st, dxo_st, du_st, xo_st, u_st;
+    float *stats;
+    const void *vec[G_VECTORS];
+    uint64_t gate_rows, gate_st;
+    uint64_t n_rows;
+    uint32_t width;
+    uint32_t post, pre, p32;            // p32: the vectors are float32
+    float post_eps, pre_eps, scale;
+    float4 *row_sums;                   // backward: per row, what its norms' gradients subtract
+};
+
+// ---- sums over a row, which `nw` wavefronts hold together
+struct RowGroup {
+    float *lds;                         // 3 x 16 floats for every exchange that may be under way
+    uint32_t nw, wave, lane;
+    uint32_t turn;                      // exchanges alternate between two places: one barrier each is enough
+    __device__ __forceinline__ float *place() { return lds + 48 * (turn++ & 1u); }
+    __device__ __forceinline__ void two(float &a, float &b) {
+        a = wave_sum(a); b = wave_sum(b);
+        if (nw == 1) return;
+        float *const s = place();
+        if (lane == 0) { s[wave] = a; s[16 + wave] = b; }
+        __syncthreads();
+        const uint32_t w = lane & 15u;
+        a = row_sum(w < nw ? s[w] : 0.f);
+        b = row_sum(w < nw ? s[16 + w] : 0.f);
+    }
+};
+
+__device__ __forceinline__ int32_t valid_of(uint32_t width, uint32_t c0) { return (int32_t)width - (int32_t)c0; }
+
+template <typename T, int CH> __device__ __forceinline__ void load_param(const void *p, uint32_t p32, uint64_t at, int32_t valid, float none, float (&v)[CH]) {
+    if (!p) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) v[i] = none;
+    } else if (p32) {
+        load_row<float, CH>((const float *)p + at, valid, v);
+    } else {
+        load_row<T, CH>((const T *)p + at, valid, v);
+    }
+}
+
+// Mean and sum of squares about it of the elements in v.  Each wavefront takes its squares about its own mean, and the parts
+// are joined by what the means differ: nothing is cancelled, and one exchange is enough.
+template <int CH, int NC>
+__device__ __forceinline__ void row_stats(RowGroup &G, const float (&v)[NC][CH], uint32_t width, uint32_t tid, uint32_t threads, uint32_t how,
+                                          float eps, float &mean, float &r) {
+    mean = 0.f; r = 1.f;
+    if (how == RK_NORM_NONE) return;
+    if (how == RK_NORM_RMS) {
+        float q = 0.f, none = 0.f;
+#pragma unroll
+        for (int k = 0; k < NC; ++k)
+#pragma unroll
+            for (int i = 0; i < CH; ++i) q += v[k][i] * v[k][i];
+        G.two(q, none);
+        r = 1.0f / sqrtf(q / (float)width + eps);
+        return;
+    }
+    float s = 0.f, n = 0.f;
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+        const int32_t valid = valid_of(width, (tid + k * threads) * CH);
+        n += (float)(valid < 0 ? 0 : valid < CH ? valid : CH);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) s += v[k][i];          // those behind the row's end are zero
+    }
+    s = wave_sum(s); n = wave_sum(n);
+    const float own = n > 0.f ? s / n : 0.f;
+    float q = 0.f;
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+        const int32_t valid = valid_of(width, (tid + k * threads) * CH);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) { const float d = i < valid ? v[k][i] - own : 0.f; q += d * d; }
+    }
+    q = wave_sum(q);
+    if (G.nw > 1) {
+        float *const p = G.place();
+        if (G.lane == 0) { p[G.wave] = s; p[16 + G.wave] = n; p[32 + G.wave] = q; }
+        __syncthreads();
+        const uint32_t w = G.lane & 15u;
+        const float sw = w < G.nw ? p[w] : 0.f, nn = w < G.nw ? p[16 + w] : 0.f, qw = w < G.nw ? p[32 + w] : 0.f;
+        mean = row_sum(sw) / (float)width;
+        const float d = nn > 0.f ? sw / nn - mean : 0.f;
+        q = row_sum(qw + nn * d * d);
+    } else {
+        mean = own;
+    }
+    r = 1.0f / sqrtf(q / (float)width + eps);
+}
+
+// The rows of a workgroup: one (its wavefronts share it), or one per wavefront for rows that a wavefront holds.
+struct RowOf { uint64_t row; uint32_t tid, threads; bool there; };
+__device__ __forceinline__ RowOf row_of(uint64_t n_rows, bool per_wave, RowGroup &G, float *lds) {
+    const uint32_t t = threadIdx.x, waves = blockDim.x >> 6;
+    G.lane = t & 63u; G.wave = t >> 6; G.turn = 0; G.lds = lds;
+    G.nw = per_wave ? 1u : waves;
+    const uint64_t row = per_wave ? (uint64_t)blockIdx.x * waves + G.wave : blockIdx.x;
+    return RowOf{row, per_wave ? G.lane : t, per_wave ? 64u : blockDim.x, row < n_rows};
+}
+
+template <typename T, typename R, int CH, int NC, int MAXT>
+__global__ __launch_bounds__(MAXT) void k_norm_forward(NormArgs A, bool per_wave) {
+    __shared__ float lds[96];
+    RowGroup G;
+    const RowOf P = row_of(A.n_rows, per_wave, G, lds);
+    if (!P.there) return;                                   // (per_wave only: whole wavefronts, no barrier follows)
+    float x[NC][CH], v[NC][CH];
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+        const uint32_t c0 = (P.tid + k * P.threads) * CH;
+        const int32_t valid = valid_of(A.width, c0);
+        load_row<R, CH>((const R *)A.x + P.row * A.x_st + c0, valid, x[k]);
+        if (A.y) load_row<T, CH>((const T *)A.y + P.row * A.y_st + c0, valid, v[k]);
+    }
+    float my = 0.f, ry = 1.f, mx, rx;
+    if (A.y) row_stats<CH, NC>(G, v, A.width, P.tid, P.threads, A.post, A.post_eps, my, ry);
+    const uint64_t gate_at = A.gate_rows ? P.row / A.gate_rows * A.gate_st : 0;
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+        const uint32_t c0 = (P.tid + k * P.threads) * CH;
+        const int32_t valid = valid_of(A.width, c0);
+        if (A.y) {
+            float w[CH], b[CH], g[CH];
+            load_param<T, CH>(A.vec[G_POST_W], A.p32, c0, valid, 1.f, w);
+            load_param<T, CH>(A.vec[G_POST_B], A.p32, c0, valid, 0.f, b);
+            load_param<T, CH>(A.vec[G_GATE], A.p32, gate_at + c0, valid, 1.f, g);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const float n = (v[k][i] - my) * ry * w[i] + b[i];
+                x[k][i] = i < valid ? A.scale * x[k][i] + g[i] * n : 0.f;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < CH; ++i) x[k][i] *= A.scale;
+        }
+        if (A.xo) store_row<R, CH>((R *)A.xo + P.row * A.xo_st + c0, valid, x[k]);
+    }
+    row_stats<CH, NC>(G, x, A.width, P.tid, P.threads, A.pre, A.pre_eps, mx, rx);
+    if (P.tid == 0) reinterpret_cast<float4 *>(A.stats)[P.row] = make_float4(my, ry, mx, rx);
+    if (A.pre == RK_NORM_NONE) return;
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+        const uint32_t c0 = (P.tid + k * P.threads) * CH;
+        const int32_t valid = valid_of(A.width, c0);
+        float w[CH], b[CH];
+        load_param<T, CH>(A.vec[G_PRE_W], A.p32, c0, valid, 1.f, w);
+        load_param<T, CH>(A.vec[G_PRE_B], A.p32, c0, valid, 0.f, b);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) x[k][i] = (x[k][i] - mx) * rx * w[i] + b[i];
+        store_row<T, CH>((T *)A.u + P.row * A.u_st + c0, valid, x[k]);
+    }
+}
+
+// One row back: D = dx_out + (what comes through the norm before the next block), dx = scale * D, and dy through gate and the
+// block's own norm.  row_sums keeps what D takes off, for the sums over rows.
+template <typename T, typename R, int CH, int NC, int MAXT>
+__global__ __launch_bounds__(MAXT) void k_norm_backward(NormArgs A, bool per_wave) {
+    __shared__ float lds[96];
+    RowGroup G;
+    const RowOf P = row_of(A.n_rows, per_wave, G, lds);
+    if (!P.there) return;
+    const float4 st = reinterpret_cast<const float4 *>(A.stats)[P.row];
+    float d[NC][CH], e[NC][CH];
+    float c = 0.f, m = 0.f;
+    if (A.pre != RK_NORM_NONE) {
+        float hat[NC][CH];
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+            const uint32_t c0 = (P.tid + k * P.threads) * CH;
+            const int32_t valid = valid_of(A.width, c0);
+            float w[CH];
+            load_row<R, CH>((const R *)A.x + P.row * A.x_st + c0, valid, hat[k]);
+            load_row<T, CH>((const T *)A.du + P.row * A.du_st + c0, valid, e[k]);
+            load_param<T, CH>(A.vec[G_PRE_W], A.p32, c0, valid, 1.f, w);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                hat[k][i] = (hat[k][i] - st.z) * st.w;
+                e[k][i] *= w[i];                            // zero behind the row's end
+                c += e[k][i] * hat[k][i]; m += e[k][i];
+            }
+        }
+        G.two(c, m);
+        c /= (float)A.width;
+        m = A.pre == RK_NORM_LAYER ? m / (float)A.width : 0.f;
+#pragma unroll
+        for (int k = 0; k < NC; ++k)
+#pragma unroll
+            for (int i = 0; i < CH; ++i) d[k][i] = st.w * (e[k][i] - m - hat[k][i] * c);
+    } else {
+#pragma unroll
+        for (int k = 0; k < NC; ++k)
+#pragma unroll
+            for (int i = 0; i < CH; ++i) d[k][i] = 0.f;
+    }
+    if (A.row_sums && P.tid == 0) A.row_sums[P.row] = make_float4(c, m, 0.f, 0.f);
+    const uint64_t gate_at = A.gate_rows ? P.row / A.gate_rows * A.gate_st : 0;
+    c = 0.f; m = 0.f;
+    float hat[NC][CH];
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+        const uint32_t c0 = (P.tid + k * P.threads) * CH;
+        const int32_t valid = valid_of(A.width, c0);
+        if (A.dxo) {
+            float t[CH];
+            load_row<R, CH>((const R *)A.dxo + P.row * A.dxo_st + c0, valid, t);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) d[k][i] += t[i];
+        }
+        float t[CH];
+#pragma unroll
+        for (int i = 0; i < CH; ++i) t[i] = A.scale * d[k][i];
+        store_row<R, CH>((R *)A.xo + P.row * A.xo_st + c0, valid, t);
+        if (!A.y) continue;
+        float w[CH], g[CH];
+        load_param<T, CH>(A.vec[G_GATE], A.p32, gate_at + c0, valid, 1.f, g);
+        load_param<T, CH>(A.vec[G_POST_W], A.p32, c0, valid, 1.f, w);
+        load_row<T, CH>((const T *)A.y + P.row * A.y_st + c0, valid, hat[k]);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            d[k][i] = i < valid ? d[k][i] * g[i] * w[i] : 0.f;
+            hat[k][i] = (hat[k][i] - st.x) * st.y;
+            c += d[k][i] * hat[k][i]; m += d[k][i];
+        }
+    }
+    if (!A.y) return;
+    if (A.post != RK_NORM_NONE) {
+        G.two(c, m);
+        c /= (float)A.width;
+        m = A.post == RK_NORM_LAYER ? m / (float)A.width : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+        const uint32_t c0 = (P.tid + k * P.threads) * CH;
+        const int32_t valid = valid_of(A.width, c0);
+        if (A.post != RK_NORM_NONE)
+#pragma unroll
+            for (int i = 0; i < CH; ++i) d[k][i] = st.y * (d[k][i] - m - hat[k][i] * c);
+        store_row<T, CH>((T *)A.u + P.row * A.u_st + c0, valid, d[k]);
+    }
+}
+
+// ---- gradients of the vectors: sums over rows
+// The rows are cut into chunks, and no chunk holds parts of two gates' rows unless it holds all of each of them.
+struct Chunks {
+    uint64_t rows;              // of a chunk
+    uint64_t per_gate;          // chunks of a gate's rows; 0: chunks hold whole gates, or the gate is one for all
+    uint64_t n;
+};
+struct NormSums {
+    NormArgs A;
+    Chunks C;
+    float *part[G_VECTORS];     // null: not wanted; [chunk][width], or, of the gates, where `gate_direct`, [gate][stride]
+    uint64_t gate_out_st;
+    bool gate_direct;
+};
+__device__ __forceinline__ void chunk_rows(const NormArgs &A, const Chunks &C, uint64_t c, uint64_t &r0, uint64_t &r1) {
+    uint64_t end = A.n_rows;
+    if (C.per_gate) {
+        const uint64_t g = c / C.per_gate;
+        r0 = g * A.gate_rows + (c - g * C.per_gate) * C.rows;
+        const uint64_t last = (g + 1) * A.gate_rows;
+        end = last < end ? last : end;
+    } else {
+        r0 = c * C.rows;
+    }
+    r1 = r0 + C.rows < end ? r0 + C.rows : end;
+    if (r0 > r1) r0 = r1;
+}
+
+constexpr int SUM_THREADS = 256;
+template <typename T, typename R, int CH>
+__global__ __launch_bounds__(SUM_THREADS) void k_norm_sums(NormSums S, uint32_t tiles) {
+    const NormArgs &A = S.A;
+    const uint64_t chunk = blockIdx.x / tiles;
+    const uint32_t c0 = (blockIdx.x % tiles * SUM_THREADS + threadIdx.x) * CH;
+    const int32_t valid = valid_of(A.width, c0);
+    if (valid <= 0) return;
+    uint64_t r0, r1;
+    chunk_rows(A, S.C, chunk, r0, r1);
+    float acc[G_VECTORS][CH] = {};
+    float w1[CH], b1[CH], w2[CH];
+    load_param<T, CH>(A.vec[G_POST_W], A.p32, c0, valid, 1.f, w1);
+    load_param<T, CH>(A.vec[G_POST_B], A.p32, c0, valid, 0.f, b1);
+    load_param<T, CH>(A.vec[G_PRE_W], A.p32, c0, valid, 1.f, w2);
+    for (uint64_t r = r0; r < r1; ++r) {
+        const float4 st = reinterpret_cast<const float4 *>(A.stats)[r];
+        float d[CH] = {};
+        if (A.dxo) load_row<R, CH>((const R *)A.dxo + r * A.dxo_st + c0, valid, d);
+        if (A.pre != RK_NORM_NONE) {
+            const float4 off = A.row_sums[r];
+            float hat[CH], e[CH];
+            load_row<R, CH>((const R *)A.x + r * A.x_st + c0, valid, hat);
+            load_row<T, CH>((const T *)A.du + r * A.du_st + c0, valid, e);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                hat[i] = (hat[i] - st.z) * st.w;
+                acc[G_PRE_W][i] += e[i] * hat[i];
+                acc[G_PRE_B][i] += e[i];
+                d[i] += st.w * (e[i] * w2[i] - off.y - hat[i] * off.x);
+            }
+        }
+        if (!A.y) continue;
+        float g[CH], y[CH];
+        const uint64_t gate = A.gate_rows ? r / A.gate_rows : 0;
+        load_param<T, CH>(A.vec[G_GATE], A.p32, gate * A.gate_st + c0, valid, 1.f, g);
+        load_row<T, CH>((const T *)A.y + r * A.y_st + c0, valid, y);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            y[i] = (y[i] - st.x) * st.y;
+            acc[G_GATE][i] += d[i] * (y[i] * w1[i] + b1[i]);
+            d[i] *= g[i];
+            acc[G_POST_W][i] += d[i] * y[i];
+            acc[G_POST_B][i] += d[i];
+        }
+        if (S.gate_direct && (r + 1 == r1 || (r + 1) % A.gate_rows == 0)) {
+            store_row<float, CH>(S.part[G_GATE] + gate * S.gate_out_st + c0, valid, acc[G_GATE]);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) acc[G_GATE][i] = 0.f;
+        }
+    }
+#pragma unroll
+    for (int s = 0; s < G_VECTORS; ++s)
+        if (S.part[s] && !(s == G_GATE && S.gate_direct)) store_row<float, CH>(S.part[s] + chunk * A.width + c0, valid, acc[s]);
+}
+
+// the chunks' sums added up, always in the same order: 64 columns a workgroup, its 16 wavefronts take every 16th chunk
+struct Joined { const float *from[G_VECTORS]; float *to[G_VECTORS]; uint64_t count[G_VECTORS]; uint32_t n; uint64_t gate_chunks, gate_out_st; };
+__global__ __launch_bounds__(1024) void k_norm_join(Joined J, uint32_t width, uint32_t tiles) {
+    __shared__ float lds[16][64];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const uint64_t job = blockIdx.x / tiles;
+    const uint32_t col = blockIdx.x % tiles * 64u + lane;
+    // the vectors first, then the gates one by one (J.gate_chunks each)
+    const uint32_t v = job < J.n ? (uint32_t)job : J.n;
+    const float *from = J.from[v];
+    float *to = J.to[v];
+    uint64_t count = J.count[v];
+    if (job >= J.n) { from += (job - J.n) * J.gate_chunks * width; to += (job - J.n) * J.gate_out_st; count = J.gate_chunks; }
+    float s = 0.f;
+    if (col < width)
+        for (uint64_t c = wave; c < count; c += 16) s += from[c * width + col];
+    lds[wave][lane] = s;
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int w = 1; w < 16; ++w) s += lds[w][lane];
+    if (col < width) to[col] = s;
+}
+
+// ---- host
+struct Shape { int nc; uint32_t threads, rows_per_wg; bool per_wave; };
+
+template <typename T, typename R> constexpr int chunk_of() { return sizeof(T) == 2 ? 8 : 4; }
+
+// A lane holds nc vectors of a row, a row as few wavefronts as that allows; rows that one wavefront holds go four to a workgroup.
+Shape shape_of(uint32_t width, int ch) {
+    for (int nc = 1; nc <= 2; ++nc)
+        if (width <= 64u * ch * nc) return Shape{nc, 256, 4, true};
+    int nc = 2;
+    while (nc < 8 && width > 1024u * ch * nc) nc *= 2;
+    const uint32_t threads = (width + ch * nc * 64 - 1) / (ch * nc * 64) * 64;
+    return Shape{nc, threads, 1, false};
+}
+
+template <typename T, typename R, int NC, int MAXT>
+void launch_nc(hipStream_t st, const NormArgs &A, const Shape &S, bool back) {
+    constexpr int CH = chunk_of<T, R>();
+    const uint32_t blocks = (uint32_t)((A.n_rows + S.rows_per_wg - 1) / S.rows_per_wg);
+    if (back) k_norm_backward<T, R, CH, NC, MAXT><<<blocks, S.threads, 0, st>>>(A, S.per_wave);
+    else k_norm_forward<T, R, CH, NC, MAXT><<<blocks, S.threads, 0, st>>>(A, S.per_wave);
+}
+template <typename T, typename R> void launch_rows(hipStream_t st, const NormArgs &A, bool back) {
+    const Shape S = shape_of(A.width, chunk_of<T, R>());
+    if (S.nc == 1) launch_nc<T, R, 1, 256>(st, A, S, back);
+    else if (S.nc == 2 && S.threads <= 512) launch_nc<T, R, 2, 512>(st, A, S, back);
+    else if (S.nc == 2) launch_nc<T, R, 2, 1024>(st, A, S, back);
+    else if (S.nc == 4) launch_nc<T, R, 4, 1024>(st, A, S, back);
+    else if constexpr (chunk_of<T, R>() == 4) launch_nc<T, R, 8, 1024>(st, A, S, back);
+}
+template <typename T, typename R> void launch_sums(hipStream_t st, const NormSums &S) {
+    constexpr int CH = chunk_of<T, R>();
+    const uint32_t tiles = (S.A.width + SUM_THREADS * CH - 1) / (SUM_THREADS * CH);
+    k_norm_sums<T, R, CH><<<(uint32_t)(S.C.n * tiles), SUM_THREADS, 0, st>>>(S, tiles);
+}
+// f(T(), R()) for the types of y and of the stream
+template <typename F> void with_types(uint32_t type, uint32_t res, F f) {
+    if (type == RK_F32) f(float(), float());
+    else if (type == RK_BF16 && res == RK_F32) f(__bf16(), float());
+    else if (type == RK_BF16) f(__bf16(), __bf16());
+    else if (res == RK_F32) f(_Float16(), float());
+    else f(_Float16(), _Float16());
+}
+
+bool aligned(const void *p, uint32_t type) { return ((uintptr_t)p & (type == RK_F32 ? 3u : 1u)) == 0; }
+
+// what both directions ask of a block; mats: the matrices that have to be there
+int32_t check_block(rk_ctx *ctx, const rk_norm_block *b, uint64_t n_rows, uint32_t width, const rk_matrix *x, const rk_matrix *y, const float *stats) {
+    if (!b) return rk_fail(ctx, RK_ERR_INVALID_ARG, "block is null");
+    if (b->post_kind > RK_NORM_LAYER || b->pre_kind > RK_NORM_LAYER) return rk_fail(ctx, RK_ERR_INVALID_ARG, "unknown kind of norm");
+    if (b->param_type > RK_F16) return rk_fail(ctx, RK_ERR_INVALID_ARG, "unknown param_type");
+    if (!(b->post_eps >= 0.f) || !(b->pre_eps >= 0.f) || !std::isfinite(b->post_eps) || !std::isfinite(b->pre_eps) || !std::isfinite(b->res_scale))
+        return rk_fail(ctx, RK_ERR_INVALID_ARG, "eps negative, or eps or res_scale not finite");
+    if ((b->post_kind == RK_NORM_NONE && (b->post_weight || b->post_bias)) || (b->pre_kind == RK_NORM_NONE && (b->pre_weight || b->pre_bias)))
+        return rk_fail(ctx, RK_ERR_INVALID_ARG, "weight or bias of a norm that is not there");
+    if (!y && (b->post_kind != RK_NORM_NONE || b->gate)) return rk_fail(ctx, RK_ERR_INVALID_ARG, "norm or gate of a block's output that is not there");
+    if (!b->gate && b->gate_rows) return rk_fail(ctx, RK_ERR_INVALID_ARG, "gate_rows without a gate");
+    if (b->gate_rows && n_rows > b->gate_rows && b->gate_stride < width) return rk_fail(ctx, RK_ERR_INVALID_ARG, "gate_stride below the width");
+    for (const void *p : {b->post_weight, b->post_bias, b->pre_weight, b->pre_bias, b->gate})
+        if (!aligned(p, b->param_type)) return rk_fail(ctx, RK_ERR_INVALID_ARG, "misaligned weight, bias or gate");
+    if (width < 1) return rk_fail(ctx, RK_ERR_INVALID_ARG, "width below 1");
+    if (width > RK_NORM_MAX_WIDTH) return rk_fail(ctx, RK_ERR_UNSUPPORTED, "rows of %u elements, %u at most", width, RK_NORM_MAX_WIDTH);
+    if (n_rows > 0x7FFFFFFFull) return rk_fail(ctx, RK_ERR_UNSUPPORTED, "more than 2^31 - 1 rows");
+    if (!rk_matrix_ok(x, n_rows, width) || (y && !rk_matrix_ok(y, n_rows, width)) || (n_rows && (!stats || ((uintptr_t)stats & 15u))))
+        return rk_fail(ctx, RK_ERR_INVALID_ARG, "x, y or stats null, misaligned or of a stride below the width");
+    return RK_OK;
+}
+// the types go together: the stream's is y's and u's, or float32; the vectors' is y's and u's, or float32
+int32_t check_types(rk_ctx *ctx, const rk_norm_block *b, uint32_t type, uint32_t res) {
+    if (res != type && res != RK_F32) return rk_fail(ctx, RK_ERR_INVALID_ARG, "the stream's type is neither the block's nor RK_F32");
+    const bool any = b->post_weight || b->post_bias || b->pre_weight || b->pre_bias || b->gate;
+    if (any && b->param_type != type && b->param_type != RK_F32) return rk_fail(ctx, RK_ERR_INVALID_ARG, "param_type is neither the block's nor RK_F32");
+    return RK_OK;
+}
+void fill_block(NormArgs &A, const rk_norm_block *b, uint64_t n_rows, uint32_t width) {
+    A.vec[G_POST_W] = b->post_weight; A.vec[G_POST_B] = b->post_bias;
+    A.vec[G_PRE_W] = b->pre_weight; A.vec[G_PRE_B] = b->pre_bias; A.vec[G_GATE] = b->gate;
+    A.gate_rows = b->gate_rows < n_rows ? b->gate_rows : 0; A.gate_st = b->gate_stride;     // (a gate for all rows is one for all)
+    A.n_rows = n_rows; A.width = width;
+    A.post = b->post_kind; A.pre = b->pre_kind; A.p32 = b->param_type == RK_F32;
+    A.post_eps = b->post_eps; A.pre_eps = b->pre_eps; A.scale = b->res_scale;
+}
+
+}  // namespace
+
+extern "C" int32_t rk_norm_forward(rk_ctx *ctx, const rk_norm_block *block, uint64_t n_rows, uint32_t width, const rk_matrix *x,
+                                   const rk_matrix *y, const rk_matrix *x_out, const rk_matrix *u, float *stats) {
+    if (!ctx) return RK_ERR_INVALID_ARG;
+    int32_t rc = check_block(ctx, block, n_rows, width, x, y, stats);
+    if (rc != RK_OK) return rc;
+    if ((u == nullptr) != (block->pre_kind == RK_NORM_NONE)) return rk_fail(ctx, RK_ERR_INVALID_ARG, "u goes with the norm before the next block");
+    if (!u && !x_out) return rk_fail(ctx, RK_ERR_INVALID_ARG, "neither x_out nor u");
+    if ((x_out && !rk_matrix_ok(x_out, n_rows, width)) || (u && !rk_matrix_ok(u, n_rows, width)))
+        return rk_fail(ctx, RK_ERR_INVALID_ARG, "x_out or u null, misaligned or of a stride below the width");
+    const uint32_t type = u ? u->type : y ? y->type : x->type;
+    if ((y && y->type != type) || (x_out && x_out->type != x->type)) return rk_fail(ctx, RK_ERR_INVALID_ARG, "y and u, or x and x_out, are of different types");
+    if ((rc = check_types(ctx, block, type, x->type)) != RK_OK) return rc;
+    if (n_rows == 0) return RK_OK;
+    RK_HIP(ctx, hipSetDevice(ctx->device));
+    NormArgs A{};
+    fill_block(A, block, n_rows, width);
+    A.x = x->data; A.x_st = x->stride;
+    if (y) { A.y = y->data; A.y_st = y->stride; }
+    if (x_out) { A.xo = x_out->data; A.xo_st = x_out->stride; }
+    if (u) { A.u = u->data; A.u_st = u->stride; }
+    A.stats = stats;
+    with_types(type, x->type, [&](auto t, auto r) { launch_rows<decltype(t), decltype(r)>(ctx->stream, A, false); });
+    RK_CHECK_LAUNCH(ctx, "k_norm_forward");
+    return RK_OK;
+}
+
+extern "C" int32_t rk_norm_backward(rk_ctx *ctx, const rk_norm_block *block, uint64_t n_rows, uint32_t width, const rk_matrix *x_out,
+                                    const rk_matrix *y, const float *stats, const rk_matrix *dx_out, const rk_matrix *du,
+                                    const rk_matrix *dx, const rk_matrix *dy, const rk_norm_grads *grads) {
+    if (!ctx) return RK_ERR_INVALID_ARG;
+    int32_t rc = check_block(ctx, block, n_rows, width, x_out, y, stats);
+    if (rc != RK_OK) return rc;
+    if ((du == nullptr) != (block->pre_kind == RK_NORM_NONE)) return rk_fail(ctx, RK_ERR_INVALID_ARG, "du goes with the norm before the next block");
+    if ((dy == nullptr) != (y == nullptr)) return rk_fail(ctx, RK_ERR_INVALID_ARG, "dy goes with y");
+    if (!du && !dx_out) return rk_fail(ctx, RK_ERR_INVALID_ARG, "neither dx_out nor du");
+    if (!rk_matrix_ok(dx, n_rows, width) || (dy && !rk_matrix_ok(dy, n_rows, width)) || (dx_out && !rk_matrix_ok(dx_out, n_rows, width)) ||
+        (du && !rk_matrix_ok(du, n_rows, width)))
+        return rk_fail(ctx, RK_ERR_INVALID_ARG, "a gradient null, misaligned or of a stride below the width");
+    const uint32_t type = du ? du->type : y ? y->type : x_out->type;
+    if ((y && (y->type != type || dy->type != type)) || dx->type != x_out->type || (dx_out && dx_out->type != x_out->type))
+        return rk_fail(ctx, RK_ERR_INVALID_ARG, "a gradient's type differs from its tensor's");
+    if ((rc = check_types(ctx, block, type, x_out->type)) != RK_OK) return rc;
+    float *out[G_VECTORS] = {};
+    if (grads) {
+        out[G_POST_W] = grads->post_weight; out[G_POST_B] = grads->post_bias;
+        out[G_PRE_W] = grads->pre_weight; out[G_PRE_B] = grads->pre_bias; out[G_GATE] = grads->gate;
+    }
+    const void *const have[G_VECTORS] = {block->post_weight, block->post_bias, block->pre_weight, block->pre_bias, block->gate};
+    bool any = false;
+    for (int s = 0; s < G_VECTORS; ++s) {
+        if (out[s] && (!have[s] || ((uintptr_t)out[s] & 3u))) return rk_fail(ctx, RK_ERR_INVALID_ARG, "gradient of a vector that is not there, or misaligned");
+    }
+    if (n_rows == 0 && block->gate_rows) out[G_GATE] = nullptr;         // no row, no gate
+    for (float *o : out) any = any || o;
+    if (out[G_GATE] && block->gate_rows && n_rows > block->gate_rows && grads->gate_stride < width)
+        return rk_fail(ctx, RK_ERR_INVALID_ARG, "gate_stride of the gradients below the width");
+    if (n_rows == 0 && !any) return RK_OK;
+    RK_HIP(ctx, hipSetDevice(ctx->device));
+    NormArgs A{};
+    fill_block(A, block, n_rows, width);
+    A.x = x_out->data; A.x_st = x_out->stride;
+    if (y) { A.y = y->data; A.y_st = y->stride; A.u = dy->data; A.u_st = dy->stride; }
+    if (dx_out) { A.dxo = dx_out->data; A.dxo_st = dx_out->stride; }
+    if (du) { A.du = du->data; A.du_st = du->stride; }
+    A.xo = dx->data; A.xo_st = dx->stride;
+    A.stats = const_cast<float *>(stats);
+    NormSums S{};
+    Joined J{};
+    uint64_t join_jobs = 0;
+    if (any) {
+        // about two chunks a compute unit, of eight rows at least
+        uint64_t rows = (n_rows + 511) / 512;
+        if (rows < 8) rows = 8;
+        const bool gates = A.gate_rows != 0;
+        if (!gates) {
+            S.C = Chunks{rows, 0, (n_rows + rows - 1) / rows};
+        } else if (A.gate_rows <= rows) {
+            rows = rows / A.gate_rows * A.gate_rows;
+            S.C = Chunks{rows, 0, (n_rows + rows - 1) / rows};
+        } else {
+            const uint64_t per = (A.gate_rows + rows - 1) / rows, n_gates = (n_rows + A.gate_rows - 1) / A.gate_rows;
+            S.C = Chunks{(A.gate_rows + per - 1) / per, per, per * n_gates};
+        }
+        S.gate_direct = gates && S.C.per_gate == 0 && out[G_GATE];
+        S.gate_out_st = gates ? grads->gate_stride : 0;
+        int n_part = 0;
+        for (int s = 0; s < G_VECTORS; ++s) n_part += out[s] && !(s == G_GATE && S.gate_direct);
+        float *part = nullptr;
+        rc = rk_scratch(ctx, SL_NORM_PARTS, (size_t)(n_part * S.C.n * width) * 4, (void **)&part);
+        if (rc != RK_OK) return rc;
+        rc = rk_scratch(ctx, SL_NORM_ROWS, (size_t)n_rows * 16, (void **)&A.row_sums);
+        if (rc != RK_OK) return rc;
+        for (int s = 0; s < G_VECTORS; ++s) {
+            if (!out[s]) continue;
+            if (s == G_GATE && S.gate_direct) { S.part[s] = out[s]; continue; }
+            S.part[s] = part; part += S.C.n * width;
+            if (s == G_GATE && S.C.per_gate) {
+                J.from[J.n] = S.part[s]; J.to[J.n] = out[s]; J.gate_chunks = S.C.per_gate; J.gate_out_st = S.gate_out_st;
+                join_jobs = S.C.n / S.C.per_gate;
+            } else {
+                J.from[J.n] = S.part[s]; J.to[J.n] = out[s]; J.count[J.n] = S.C.n;
+                ++J.n;
+            }
+        }
+        join_jobs += J.n;
+        if (S.C.n * ((width + 1023) / 1024) > 0x7FFFFFFFull) return rk_fail(ctx, RK_ERR_UNSUPPORTED, "too many rows");
+    }
+    if (n_rows) {
+        with_types(type, x_out->type, [&](auto t, auto r) { launch_rows<decltype(t), decltype(r)>(ctx->stream, A, true); });
+        RK_CHECK_LAUNCH(ctx, "k_norm_backward");
+        if (any) {
+            S.A = A;
+            with_types(type, x_out->type, [&](auto t, auto r) { launch_sums<decltype(t), decltype(r)>(ctx->stream, S); });
+            RK_CHECK_LAUNCH(ctx, "k_norm_sums");
+        }
+    }
+    if (join_jobs) {
+        const uint32_t tiles = (width + 63) / 64;
+        k_norm_join<<<(uint32_t)(join_jobs * tiles), 1024, 0, ctx->stream>>>(J, width, tiles);
+        RK_CHECK_LAUNCH(ctx, "k_norm_join");
+    }
+    return RK_OK;
+}
