@@ -1,6 +1,7 @@
 // A student's loss against a teacher's largest logits and the labels, and its gradient (rk_distill_loss,
 // rk_distill_backward, rk_distill_loss_backward).
 #include <cmath>
+#include <type_traits>
 
 #include "rk_vec.h"
 
@@ -41,7 +42,7 @@ __device__ __forceinline__ float teacher_at(const DistillArgs &A, uint64_t r, ui
 }
 
 // A workgroup a row.  LOSS: the sums of the softmax over the row, then the loss; GRAD: the gradient, from these or from lse.
-template <typename T, int CH, bool LOSS, bool GRAD>
+template <bool CUTS, typename T, int CH, bool LOSS, bool GRAD>
 __global__ __launch_bounds__(DS_THREADS) void k_distill(DistillArgs A) {
     __shared__ float q[RK_MAX_TEACHER_LOGITS], sv[RK_MAX_TEACHER_LOGITS], red[16];
     __shared__ int32_t at[RK_MAX_TEACHER_LOGITS];
@@ -49,6 +50,7 @@ __global__ __launch_bounds__(DS_THREADS) void k_distill(DistillArgs A) {
     const uint64_t r = blockIdx.x;
     const T *const row = (const T *)A.student + r * A.st;
     T *const out = (T *)A.d_student + r * A.d_st;
+    const Row<T> from(A.student, r, A.st, V), to(A.d_student, r, A.d_st, V);
     const float weight = A.row_weight ? A.row_weight[r] : 1.f;
     const float inv_t = 1.f / A.temperature;
     float lse_t = 0.f, lse_1 = 0.f;
@@ -56,9 +58,10 @@ __global__ __launch_bounds__(DS_THREADS) void k_distill(DistillArgs A) {
     if (there && LOSS) {
         float m = -INFINITY, st = 0.f, s1 = 0.f;
         for (uint32_t c0 = tid * CH; c0 < V; c0 += DS_THREADS * CH) {
-            const int32_t valid = (int32_t)(V - c0);
+            const Place at(c0, V, CH);
+            const int32_t valid = at.valid;
             float v[CH], top = m;
-            load_row<T, CH>(row + c0, valid, v);
+            load_row<CUTS, T, CH>(from, at, v);
 #pragma unroll
             for (int i = 0; i < CH; ++i) if (i < valid) top = fmaxf(top, v[i]);
             const float ref = top == -INFINITY ? 0.f : top;
@@ -136,10 +139,10 @@ __global__ __launch_bounds__(DS_THREADS) void k_distill(DistillArgs A) {
     const float label_v = labelled ? (float)row[label] : 0.f;
     __syncthreads();                            // d_student may be student: what the rest needs of the row is held
     for (uint32_t c0 = tid * CH; c0 < V; c0 += DS_THREADS * CH) {
-        const int32_t valid = (int32_t)(V - c0);
+        const Place place(c0, V, CH);
         float v[CH] = {};
         if (there) {
-            load_row<T, CH>(row + c0, valid, v);
+            load_row<CUTS, T, CH>(from, place, v);
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
                 float d = 0.f;
@@ -148,7 +151,7 @@ __global__ __launch_bounds__(DS_THREADS) void k_distill(DistillArgs A) {
                 v[i] = d;
             }
         }
-        store_row<T, CH>(out + c0, valid, v);
+        store_row<CUTS, T, CH>(to, place, v);
     }
     if (!there) return;
     __syncthreads();
@@ -191,7 +194,7 @@ int32_t check_distill(rk_ctx *ctx, const rk_distill *d, uint64_t n_rows, uint32_
         !std::isfinite(d->kd_weight) || !std::isfinite(d->ce_weight) || (d->kd_weight == 0.f && d->ce_weight == 0.f))
         return rk_fail(ctx, RK_ERR_INVALID_ARG, "temperature not positive, or weights negative, not finite or both 0");
     if (vocab < 1) return rk_fail(ctx, RK_ERR_INVALID_ARG, "vocab below 1");
-    if (vocab > 0x7FFFFFFFu - 65536u || n_rows > 0x7FFFFFFFull) return rk_fail(ctx, RK_ERR_UNSUPPORTED, "vocab or n_rows beyond 2^31");
+    if (vocab > ROW_MAX || n_rows > 0x7FFFFFFFull) return rk_fail(ctx, RK_ERR_UNSUPPORTED, "vocab beyond 2^28, or n_rows beyond 2^31 - 1");
     if (!rk_matrix_ok(student, n_rows, vocab)) return rk_fail(ctx, RK_ERR_INVALID_ARG, "student null, misaligned or of a stride below vocab");
     if ((t->logits != nullptr) != (d->kd_weight > 0.f)) return rk_fail(ctx, RK_ERR_INVALID_ARG, "the teacher's logits go with kd_weight");
     if ((t->label != nullptr) != (d->ce_weight > 0.f) && n_rows) return rk_fail(ctx, RK_ERR_INVALID_ARG, "labels go with ce_weight");
@@ -209,9 +212,13 @@ int32_t check_distill(rk_ctx *ctx, const rk_distill *d, uint64_t n_rows, uint32_
 }
 template <bool LOSS, bool GRAD> void launch_type(hipStream_t st, uint32_t type, const DistillArgs &A) {
     const uint32_t n = (uint32_t)A.n_rows;
-    if (type == RK_F32) k_distill<float, 4, LOSS, GRAD><<<n, DS_THREADS, 0, st>>>(A);
-    else if (type == RK_BF16) k_distill<__bf16, 8, LOSS, GRAD><<<n, DS_THREADS, 0, st>>>(A);
-    else k_distill<_Float16, 8, LOSS, GRAD><<<n, DS_THREADS, 0, st>>>(A);
+    auto go = [&](auto cuts) {
+        constexpr bool CUTS = decltype(cuts)::value;
+        if (type == RK_F32) k_distill<CUTS, float, 4, LOSS, GRAD><<<n, DS_THREADS, 0, st>>>(A);
+        else if (type == RK_BF16) k_distill<CUTS, __bf16, 8, LOSS, GRAD><<<n, DS_THREADS, 0, st>>>(A);
+        else k_distill<CUTS, _Float16, 8, LOSS, GRAD><<<n, DS_THREADS, 0, st>>>(A);
+    };
+    if (A.vocab % (type == RK_F32 ? 4 : 8)) go(std::true_type()); else go(std::false_type());
 }
 int32_t run(rk_ctx *ctx, uint32_t type, DistillArgs &A, bool want_loss, bool want_grad) {
     RK_HIP(ctx, hipSetDevice(ctx->device));

@@ -1,6 +1,7 @@
 // The join of a block and its residual stream: norm of the block's output, gate, scaled residual, norm before the next
 // block, forward and backward (rk_norm_forward, rk_norm_backward).
 #include <cmath>
+#include <type_traits>
 
 #include "rk_vec.h"
 
@@ -40,24 +41,25 @@ struct RowGroup {
     }
 };
 
-__device__ __forceinline__ int32_t valid_of(uint32_t width, uint32_t c0) { return (int32_t)width - (int32_t)c0; }
-
-template <typename T, int CH> __device__ __forceinline__ void load_param(const void *p, uint32_t p32, uint64_t at, int32_t valid, float none, float (&v)[CH]) {
-    if (!p) {
+// a lane's part of a weight, bias or gate; `none` in each place if there is none
+template <bool CUTS, typename T, int CH>
+__device__ __forceinline__ void load_param(const NormArgs &A, int which, uint64_t row, uint64_t stride, const Place &p, float none, float (&v)[CH]) {
+    const void *const base = A.vec[which];
+    if (!base) {
 #pragma unroll
         for (int i = 0; i < CH; ++i) v[i] = none;
-    } else if (p32) {
-        load_row<float, CH>((const float *)p + at, valid, v);
+    } else if (A.p32) {
+        load_row<CUTS, float, CH>(Row<float>(base, row, stride, A.width), p, v);
     } else {
-        load_row<T, CH>((const T *)p + at, valid, v);
+        load_row<CUTS, T, CH>(Row<T>(base, row, stride, A.width), p, v);
     }
 }
 
 // Mean and sum of squares about it of the elements in v.  Each wavefront takes its squares about its own mean, and the parts
 // are joined by what the means differ: nothing is cancelled, and one exchange is enough.
 template <int CH, int NC>
-__device__ __forceinline__ void row_stats(RowGroup &G, const float (&v)[NC][CH], uint32_t width, uint32_t tid, uint32_t threads, uint32_t how,
-                                          float eps, float &mean, float &r) {
+__device__ __forceinline__ void row_stats(RowGroup &G, const float (&v)[NC][CH], uint32_t width, const Place (&at)[NC], uint32_t how, float eps,
+                                          float &mean, float &r) {
     mean = 0.f; r = 1.f;
     if (how == RK_NORM_NONE) return;
     if (how == RK_NORM_RMS) {
@@ -73,7 +75,7 @@ __device__ __forceinline__ void row_stats(RowGroup &G, const float (&v)[NC][CH],
     float s = 0.f, n = 0.f;
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
-        const int32_t valid = valid_of(width, (tid + k * threads) * CH);
+        const int32_t valid = at[k].valid;
         n += (float)(valid < 0 ? 0 : valid < CH ? valid : CH);
 #pragma unroll
         for (int i = 0; i < CH; ++i) s += v[k][i];          // those behind the row's end are zero
@@ -83,9 +85,8 @@ __device__ __forceinline__ void row_stats(RowGroup &G, const float (&v)[NC][CH],
     float q = 0.f;
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
-        const int32_t valid = valid_of(width, (tid + k * threads) * CH);
 #pragma unroll
-        for (int i = 0; i < CH; ++i) { const float d = i < valid ? v[k][i] - own : 0.f; q += d * d; }
+        for (int i = 0; i < CH; ++i) { const float d = i < at[k].valid ? v[k][i] - own : 0.f; q += d * d; }
     }
     q = wave_sum(q);
     if (G.nw > 1) {
@@ -103,95 +104,98 @@ __device__ __forceinline__ void row_stats(RowGroup &G, const float (&v)[NC][CH],
     r = 1.0f / sqrtf(q / (float)width + eps);
 }
 
+template <int CH, int NC> __device__ __forceinline__ void places(Place (&at)[NC], uint32_t tid, uint32_t threads, uint32_t width) {
+#pragma unroll
+    for (int k = 0; k < NC; ++k) at[k] = Place((tid + k * threads) * CH, width, CH);
+}
+
 // The rows of a workgroup: one (its wavefronts share it), or one per wavefront for rows that a wavefront holds.
 struct RowOf { uint64_t row; uint32_t tid, threads; bool there; };
 __device__ __forceinline__ RowOf row_of(uint64_t n_rows, bool per_wave, RowGroup &G, float *lds) {
     const uint32_t t = threadIdx.x, waves = blockDim.x >> 6;
-    G.lane = t & 63u; G.wave = t >> 6; G.turn = 0; G.lds = lds;
+    G.lane = t & 63u; G.wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(t >> 6)); G.turn = 0; G.lds = lds;
     G.nw = per_wave ? 1u : waves;
     const uint64_t row = per_wave ? (uint64_t)blockIdx.x * waves + G.wave : blockIdx.x;
     return RowOf{row, per_wave ? G.lane : t, per_wave ? 64u : blockDim.x, row < n_rows};
 }
 
-template <typename T, typename R, int CH, int NC, int MAXT>
+template <bool CUTS, typename T, typename R, int CH, int NC, int MAXT>
 __global__ __launch_bounds__(MAXT) void k_norm_forward(NormArgs A, bool per_wave) {
     __shared__ float lds[96];
     RowGroup G;
     const RowOf P = row_of(A.n_rows, per_wave, G, lds);
     if (!P.there) return;                                   // (per_wave only: whole wavefronts, no barrier follows)
+    Place at[NC];
+    places<CH, NC>(at, P.tid, P.threads, A.width);
     float x[NC][CH], v[NC][CH];
+    {
+        const Row<R> rx(A.x, P.row, A.x_st, A.width);
+        const Row<T> ry(A.y, P.row, A.y_st, A.width);
 #pragma unroll
-    for (int k = 0; k < NC; ++k) {
-        const uint32_t c0 = (P.tid + k * P.threads) * CH;
-        const int32_t valid = valid_of(A.width, c0);
-        load_row<R, CH>((const R *)A.x + P.row * A.x_st + c0, valid, x[k]);
-        if (A.y) load_row<T, CH>((const T *)A.y + P.row * A.y_st + c0, valid, v[k]);
+        for (int k = 0; k < NC; ++k) {
+            load_row<CUTS, R, CH>(rx, at[k], x[k]);
+            load_row<CUTS, T, CH>(ry, at[k], v[k]);
+        }
     }
     float my = 0.f, ry = 1.f, mx, rx;
-    if (A.y) row_stats<CH, NC>(G, v, A.width, P.tid, P.threads, A.post, A.post_eps, my, ry);
-    const uint64_t gate_at = A.gate_rows ? P.row / A.gate_rows * A.gate_st : 0;
+    row_stats<CH, NC>(G, v, A.width, at, A.post, A.post_eps, my, ry);
+    const uint64_t gate = A.gate_rows ? P.row / A.gate_rows : 0;
+    const Row<R> xo(A.xo, P.row, A.xo_st, A.width);
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
-        const uint32_t c0 = (P.tid + k * P.threads) * CH;
-        const int32_t valid = valid_of(A.width, c0);
-        if (A.y) {
-            float w[CH], b[CH], g[CH];
-            load_param<T, CH>(A.vec[G_POST_W], A.p32, c0, valid, 1.f, w);
-            load_param<T, CH>(A.vec[G_POST_B], A.p32, c0, valid, 0.f, b);
-            load_param<T, CH>(A.vec[G_GATE], A.p32, gate_at + c0, valid, 1.f, g);
+        float w[CH], b[CH], g[CH];
+        load_param<CUTS, T, CH>(A, G_POST_W, 0, 0, at[k], 1.f, w);
+        load_param<CUTS, T, CH>(A, G_POST_B, 0, 0, at[k], 0.f, b);
+        load_param<CUTS, T, CH>(A, G_GATE, gate, A.gate_st, at[k], 1.f, g);
 #pragma unroll
-            for (int i = 0; i < CH; ++i) {
-                const float n = (v[k][i] - my) * ry * w[i] + b[i];
-                x[k][i] = i < valid ? A.scale * x[k][i] + g[i] * n : 0.f;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < CH; ++i) x[k][i] *= A.scale;
+        for (int i = 0; i < CH; ++i) {
+            const float n = (v[k][i] - my) * ry * w[i] + b[i];
+            x[k][i] = i < at[k].valid ? A.scale * x[k][i] + g[i] * n : 0.f;
         }
-        if (A.xo) store_row<R, CH>((R *)A.xo + P.row * A.xo_st + c0, valid, x[k]);
+        store_row<CUTS, R, CH>(xo, at[k], x[k]);
     }
-    row_stats<CH, NC>(G, x, A.width, P.tid, P.threads, A.pre, A.pre_eps, mx, rx);
+    row_stats<CH, NC>(G, x, A.width, at, A.pre, A.pre_eps, mx, rx);
     if (P.tid == 0) reinterpret_cast<float4 *>(A.stats)[P.row] = make_float4(my, ry, mx, rx);
     if (A.pre == RK_NORM_NONE) return;
+    const Row<T> u(A.u, P.row, A.u_st, A.width);
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
-        const uint32_t c0 = (P.tid + k * P.threads) * CH;
-        const int32_t valid = valid_of(A.width, c0);
         float w[CH], b[CH];
-        load_param<T, CH>(A.vec[G_PRE_W], A.p32, c0, valid, 1.f, w);
-        load_param<T, CH>(A.vec[G_PRE_B], A.p32, c0, valid, 0.f, b);
+        load_param<CUTS, T, CH>(A, G_PRE_W, 0, 0, at[k], 1.f, w);
+        load_param<CUTS, T, CH>(A, G_PRE_B, 0, 0, at[k], 0.f, b);
 #pragma unroll
         for (int i = 0; i < CH; ++i) x[k][i] = (x[k][i] - mx) * rx * w[i] + b[i];
-        store_row<T, CH>((T *)A.u + P.row * A.u_st + c0, valid, x[k]);
+        store_row<CUTS, T, CH>(u, at[k], x[k]);
     }
 }
 
 // One row back: D = dx_out + (what comes through the norm before the next block), dx = scale * D, and dy through gate and the
 // block's own norm.  row_sums keeps what D takes off, for the sums over rows.
-template <typename T, typename R, int CH, int NC, int MAXT>
+template <bool CUTS, typename T, typename R, int CH, int NC, int MAXT>
 __global__ __launch_bounds__(MAXT) void k_norm_backward(NormArgs A, bool per_wave) {
     __shared__ float lds[96];
     RowGroup G;
     const RowOf P = row_of(A.n_rows, per_wave, G, lds);
     if (!P.there) return;
+    Place at[NC];
+    places<CH, NC>(at, P.tid, P.threads, A.width);
     const float4 st = reinterpret_cast<const float4 *>(A.stats)[P.row];
-    float d[NC][CH], e[NC][CH];
+    float d[NC][CH], hat[NC][CH];
     float c = 0.f, m = 0.f;
     if (A.pre != RK_NORM_NONE) {
-        float hat[NC][CH];
+        const Row<R> rx(A.x, P.row, A.x_st, A.width);
+        const Row<T> ru(A.du, P.row, A.du_st, A.width);
 #pragma unroll
         for (int k = 0; k < NC; ++k) {
-            const uint32_t c0 = (P.tid + k * P.threads) * CH;
-            const int32_t valid = valid_of(A.width, c0);
             float w[CH];
-            load_row<R, CH>((const R *)A.x + P.row * A.x_st + c0, valid, hat[k]);
-            load_row<T, CH>((const T *)A.du + P.row * A.du_st + c0, valid, e[k]);
-            load_param<T, CH>(A.vec[G_PRE_W], A.p32, c0, valid, 1.f, w);
+            load_row<CUTS, R, CH>(rx, at[k], hat[k]);
+            load_row<CUTS, T, CH>(ru, at[k], d[k]);
+            load_param<CUTS, T, CH>(A, G_PRE_W, 0, 0, at[k], 1.f, w);
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
                 hat[k][i] = (hat[k][i] - st.z) * st.w;
-                e[k][i] *= w[i];                            // zero behind the row's end
-                c += e[k][i] * hat[k][i]; m += e[k][i];
+                d[k][i] *= w[i];                            // zero behind the row's end
+                c += d[k][i] * hat[k][i]; m += d[k][i];
             }
         }
         G.two(c, m);
@@ -200,7 +204,7 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward(NormArgs A, bool per_wav
 #pragma unroll
         for (int k = 0; k < NC; ++k)
 #pragma unroll
-            for (int i = 0; i < CH; ++i) d[k][i] = st.w * (e[k][i] - m - hat[k][i] * c);
+            for (int i = 0; i < CH; ++i) d[k][i] = st.w * (d[k][i] - m - hat[k][i] * c);
     } else {
 #pragma unroll
         for (int k = 0; k < NC; ++k)
@@ -208,31 +212,29 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward(NormArgs A, bool per_wav
             for (int i = 0; i < CH; ++i) d[k][i] = 0.f;
     }
     if (A.row_sums && P.tid == 0) A.row_sums[P.row] = make_float4(c, m, 0.f, 0.f);
-    const uint64_t gate_at = A.gate_rows ? P.row / A.gate_rows * A.gate_st : 0;
+    const uint64_t gate = A.gate_rows ? P.row / A.gate_rows : 0;
+    const Row<R> rd(A.dxo, P.row, A.dxo_st, A.width), dx(A.xo, P.row, A.xo_st, A.width);
+    const Row<T> ry(A.y, P.row, A.y_st, A.width), dy(A.u, P.row, A.u_st, A.width);
     c = 0.f; m = 0.f;
-    float hat[NC][CH];
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
-        const uint32_t c0 = (P.tid + k * P.threads) * CH;
-        const int32_t valid = valid_of(A.width, c0);
+        float t[CH];
         if (A.dxo) {
-            float t[CH];
-            load_row<R, CH>((const R *)A.dxo + P.row * A.dxo_st + c0, valid, t);
+            load_row<CUTS, R, CH>(rd, at[k], t);
 #pragma unroll
             for (int i = 0; i < CH; ++i) d[k][i] += t[i];
         }
-        float t[CH];
 #pragma unroll
         for (int i = 0; i < CH; ++i) t[i] = A.scale * d[k][i];
-        store_row<R, CH>((R *)A.xo + P.row * A.xo_st + c0, valid, t);
+        store_row<CUTS, R, CH>(dx, at[k], t);
         if (!A.y) continue;
         float w[CH], g[CH];
-        load_param<T, CH>(A.vec[G_GATE], A.p32, gate_at + c0, valid, 1.f, g);
-        load_param<T, CH>(A.vec[G_POST_W], A.p32, c0, valid, 1.f, w);
-        load_row<T, CH>((const T *)A.y + P.row * A.y_st + c0, valid, hat[k]);
+        load_param<CUTS, T, CH>(A, G_GATE, gate, A.gate_st, at[k], 1.f, g);
+        load_param<CUTS, T, CH>(A, G_POST_W, 0, 0, at[k], 1.f, w);
+        load_row<CUTS, T, CH>(ry, at[k], hat[k]);
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            d[k][i] = i < valid ? d[k][i] * g[i] * w[i] : 0.f;
+            d[k][i] = i < at[k].valid ? d[k][i] * g[i] * w[i] : 0.f;
             hat[k][i] = (hat[k][i] - st.x) * st.y;
             c += d[k][i] * hat[k][i]; m += d[k][i];
         }
@@ -245,12 +247,10 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward(NormArgs A, bool per_wav
     }
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
-        const uint32_t c0 = (P.tid + k * P.threads) * CH;
-        const int32_t valid = valid_of(A.width, c0);
         if (A.post != RK_NORM_NONE)
 #pragma unroll
             for (int i = 0; i < CH; ++i) d[k][i] = st.y * (d[k][i] - m - hat[k][i] * c);
-        store_row<T, CH>((T *)A.u + P.row * A.u_st + c0, valid, d[k]);
+        store_row<CUTS, T, CH>(dy, at[k], d[k]);
     }
 }
 
@@ -283,29 +283,28 @@ __device__ __forceinline__ void chunk_rows(const NormArgs &A, const Chunks &C, u
 }
 
 constexpr int SUM_THREADS = 256;
-template <typename T, typename R, int CH>
+template <bool CUTS, typename T, typename R, int CH>
 __global__ __launch_bounds__(SUM_THREADS) void k_norm_sums(NormSums S, uint32_t tiles) {
     const NormArgs &A = S.A;
     const uint64_t chunk = blockIdx.x / tiles;
-    const uint32_t c0 = (blockIdx.x % tiles * SUM_THREADS + threadIdx.x) * CH;
-    const int32_t valid = valid_of(A.width, c0);
-    if (valid <= 0) return;
+    const Place at((blockIdx.x % tiles * SUM_THREADS + threadIdx.x) * CH, A.width, CH);
+    if (at.valid <= 0) return;
     uint64_t r0, r1;
     chunk_rows(A, S.C, chunk, r0, r1);
     float acc[G_VECTORS][CH] = {};
     float w1[CH], b1[CH], w2[CH];
-    load_param<T, CH>(A.vec[G_POST_W], A.p32, c0, valid, 1.f, w1);
-    load_param<T, CH>(A.vec[G_POST_B], A.p32, c0, valid, 0.f, b1);
-    load_param<T, CH>(A.vec[G_PRE_W], A.p32, c0, valid, 1.f, w2);
+    load_param<CUTS, T, CH>(A, G_POST_W, 0, 0, at, 1.f, w1);
+    load_param<CUTS, T, CH>(A, G_POST_B, 0, 0, at, 0.f, b1);
+    load_param<CUTS, T, CH>(A, G_PRE_W, 0, 0, at, 1.f, w2);
     for (uint64_t r = r0; r < r1; ++r) {
         const float4 st = reinterpret_cast<const float4 *>(A.stats)[r];
         float d[CH] = {};
-        if (A.dxo) load_row<R, CH>((const R *)A.dxo + r * A.dxo_st + c0, valid, d);
+        if (A.dxo) load_row<CUTS, R, CH>(Row<R>(A.dxo, r, A.dxo_st, A.width), at, d);
         if (A.pre != RK_NORM_NONE) {
             const float4 off = A.row_sums[r];
             float hat[CH], e[CH];
-            load_row<R, CH>((const R *)A.x + r * A.x_st + c0, valid, hat);
-            load_row<T, CH>((const T *)A.du + r * A.du_st + c0, valid, e);
+            load_row<CUTS, R, CH>(Row<R>(A.x, r, A.x_st, A.width), at, hat);
+            load_row<CUTS, T, CH>(Row<T>(A.du, r, A.du_st, A.width), at, e);
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
                 hat[i] = (hat[i] - st.z) * st.w;
@@ -317,8 +316,8 @@ __global__ __launch_bounds__(SUM_THREADS) void k_norm_sums(NormSums S, uint32_t 
         if (!A.y) continue;
         float g[CH], y[CH];
         const uint64_t gate = A.gate_rows ? r / A.gate_rows : 0;
-        load_param<T, CH>(A.vec[G_GATE], A.p32, gate * A.gate_st + c0, valid, 1.f, g);
-        load_row<T, CH>((const T *)A.y + r * A.y_st + c0, valid, y);
+        load_param<CUTS, T, CH>(A, G_GATE, gate, A.gate_st, at, 1.f, g);
+        load_row<CUTS, T, CH>(Row<T>(A.y, r, A.y_st, A.width), at, y);
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             y[i] = (y[i] - st.x) * st.y;
@@ -328,14 +327,218 @@ __global__ __launch_bounds__(SUM_THREADS) void k_norm_sums(NormSums S, uint32_t 
             acc[G_POST_B][i] += d[i];
         }
         if (S.gate_direct && (r + 1 == r1 || (r + 1) % A.gate_rows == 0)) {
-            store_row<float, CH>(S.part[G_GATE] + gate * S.gate_out_st + c0, valid, acc[G_GATE]);
+            store_row<CUTS, float, CH>(Row<float>(S.part[G_GATE], gate, S.gate_out_st, A.width), at, acc[G_GATE]);
 #pragma unroll
             for (int i = 0; i < CH; ++i) acc[G_GATE][i] = 0.f;
         }
     }
 #pragma unroll
     for (int s = 0; s < G_VECTORS; ++s)
-        if (S.part[s] && !(s == G_GATE && S.gate_direct)) store_row<float, CH>(S.part[s] + chunk * A.width + c0, valid, acc[s]);
+        if (S.part[s] && !(s == G_GATE && S.gate_direct)) store_row<CUTS, float, CH>(Row<float>(S.part[s], chunk, A.width, A.width), at, acc[s]);
+}
+
+// what a lane keeps in LDS of two weights, gate and (with biases) the block's bias, in 16 bytes: an odd number of them, so that
+// the lanes' reads spread over the banks
+constexpr uint32_t sums_lds_of(int ch, int nc, bool bias) { return (uint32_t)((bias ? 4 : 3) * nc * ch / 4) | 1u; }
+
+// Rows back and the sums over them in one pass: a workgroup (or, of rows that a wavefront holds, a wavefront) takes a chunk of
+// rows, and every lane keeps the sums of its columns in registers.  The next row's x_out and du are on their way while this row's
+// first norm is summed, its dx_out and y while the second is.  Weights and gate, which every row needs, lie in LDS: each lane reads only
+// what it wrote itself, and registers are left for the sums.  Of the vectors behind the gate only sum D y^ and sum D are kept:
+//     d post_weight = gate sum D y^,  d post_bias = gate sum D,  d gate = post_weight sum D y^ + post_bias sum D
+// for rows of one gate.  A chunk with several gates' rows adds its first two up in its place in memory, gate by gate.
+template <bool CUTS, typename T, typename R, int CH, int NC, int MAXT, bool BIAS>
+__global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool per_wave) {
+    extern __shared__ float4 param_lds[];
+    __shared__ float lds[96];
+    const NormArgs &A = S.A;
+    RowGroup G;
+    const RowOf P = row_of(S.C.n, per_wave, G, lds);            // (its "row" is the chunk)
+    if (!P.there) return;
+    const uint64_t chunk = P.row;
+    uint64_t r0, r1;
+    chunk_rows(A, S.C, chunk, r0, r1);
+    Place at[NC];
+    places<CH, NC>(at, P.tid, P.threads, A.width);
+    float sum_dy[NC][CH] = {}, acc_w2[NC][CH] = {}, sum_d[BIAS ? NC : 1][CH] = {}, acc_b2[BIAS ? NC : 1][CH] = {};
+    constexpr int Q = CH / 4;
+    float4 *const mine = param_lds + threadIdx.x * sums_lds_of(CH, NC, BIAS);
+    auto put = [&](int v, int k, const float (&x)[CH]) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q) mine[(v * NC + k) * Q + q] = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+    };
+    auto get = [&](int v, int k, float (&x)[CH]) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            const float4 f = mine[(v * NC + k) * Q + q];
+            x[4 * q] = f.x; x[4 * q + 1] = f.y; x[4 * q + 2] = f.z; x[4 * q + 3] = f.w;
+        }
+    };
+    enum { L_W1, L_W2, L_GATE, L_B1 };
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+        float x[CH];
+        load_param<CUTS, T, CH>(A, G_POST_W, 0, 0, at[k], 1.f, x);
+        put(L_W1, k, x);
+        load_param<CUTS, T, CH>(A, G_PRE_W, 0, 0, at[k], 1.f, x);
+        put(L_W2, k, x);
+        if constexpr (BIAS) { load_param<CUTS, T, CH>(A, G_POST_B, 0, 0, at[k], 0.f, x); put(L_B1, k, x); }
+    }
+    Words<R, CH> rx[NC], rd[NC];
+    Words<T, CH> ru[NC], ry[NC];
+    float4 st_next = make_float4(0.f, 1.f, 0.f, 1.f);
+    auto fetch_first = [&](uint64_t r) {
+        const bool there = r < r1;                              // (behind the chunk: a row of no elements)
+        st_next = reinterpret_cast<const float4 *>(A.stats)[there ? r : r0];
+        const Row<R> x(there ? A.x : nullptr, r, A.x_st, A.width);
+        const Row<T> u(there ? A.du : nullptr, r, A.du_st, A.width);
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+            rx[k] = fetch_row<CUTS, R, CH>(x, at[k]);
+            ru[k] = fetch_row<CUTS, T, CH>(u, at[k]);
+        }
+    };
+    auto fetch_second = [&](uint64_t r) {
+        const bool there = r < r1;
+        const Row<R> dxo(there ? A.dxo : nullptr, r, A.dxo_st, A.width);
+        const Row<T> y(there ? A.y : nullptr, r, A.y_st, A.width);
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+            rd[k] = fetch_row<CUTS, R, CH>(dxo, at[k]);
+            ry[k] = fetch_row<CUTS, T, CH>(y, at[k]);
+        }
+    };
+    if (r0 < r1) { fetch_first(r0); fetch_second(r0); }
+    uint64_t gate = ~0ull, gate_end = 0;
+    const float inv = 1.f / (float)A.width;
+    for (uint64_t r = r0; r < r1; ++r) {
+        const float4 st = st_next;
+        if (gate == ~0ull || (A.gate_rows && r == gate_end)) {
+            gate = A.gate_rows ? r / A.gate_rows : 0;
+            gate_end = (gate + 1) * A.gate_rows;
+#pragma unroll
+            for (int k = 0; k < NC; ++k) {
+                float x[CH];
+                load_param<CUTS, T, CH>(A, G_GATE, gate, A.gate_st, at[k], 1.f, x);
+                put(L_GATE, k, x);
+            }
+        }
+        float d[NC][CH], hat[NC][CH];
+        float c = 0.f, m = 0.f;
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+            float w2[CH];
+            get(L_W2, k, w2);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const float u = element<T>(ru[k], i);
+                hat[k][i] = (element<R>(rx[k], i) - st.z) * st.w;
+                acc_w2[k][i] += u * hat[k][i];
+                if constexpr (BIAS) acc_b2[k][i] += u;
+                d[k][i] = u * w2[i];
+                c += d[k][i] * hat[k][i]; m += d[k][i];
+            }
+            __builtin_amdgcn_sched_barrier(0);                  // vector by vector: fewer registers at once
+        }
+        fetch_first(r + 1);
+        G.two(c, m);
+        c *= inv;
+        m = A.pre == RK_NORM_LAYER ? m * inv : 0.f;
+#pragma unroll
+        for (int k = 0; k < NC; ++k)
+#pragma unroll
+            for (int i = 0; i < CH; ++i) d[k][i] = st.w * (d[k][i] - m - hat[k][i] * c) + element<R>(rd[k], i);
+        c = 0.f; m = 0.f;
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+            float t[CH], w1[CH], g[CH];
+            get(L_W1, k, w1);
+            get(L_GATE, k, g);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                t[i] = A.scale * d[k][i];
+            }
+            store_row<CUTS, R, CH>(Row<R>(A.xo, r, A.xo_st, A.width), at[k], t);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const float y = (element<T>(ry[k], i) - st.x) * st.y;
+                sum_dy[k][i] += d[k][i] * y;
+                if constexpr (BIAS) sum_d[k][i] += d[k][i];
+                hat[k][i] = y;
+                d[k][i] = i < at[k].valid ? d[k][i] * g[i] * w1[i] : 0.f;
+                c += d[k][i] * y; m += d[k][i];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        fetch_second(r + 1);
+        if (A.post != RK_NORM_NONE) {
+            G.two(c, m);
+            c *= inv;
+            m = A.post == RK_NORM_LAYER ? m * inv : 0.f;
+#pragma unroll
+            for (int k = 0; k < NC; ++k)
+#pragma unroll
+                for (int i = 0; i < CH; ++i) d[k][i] = st.y * (d[k][i] - m - hat[k][i] * c);
+        }
+        {
+            const Row<T> dy(A.u, r, A.u_st, A.width);
+#pragma unroll
+            for (int k = 0; k < NC; ++k) store_row<CUTS, T, CH>(dy, at[k], d[k]);
+        }
+        if (r + 1 == r1 || r + 1 == gate_end) {
+            const bool first = gate_end <= r0 + A.gate_rows || !A.gate_rows;        // (of the chunk's gates)
+            const Row<float> pw(S.part[G_POST_W], chunk, A.width, A.width), pb(S.part[G_POST_B], chunk, A.width, A.width);
+            const Row<float> pg(S.part[G_GATE], S.gate_direct ? gate : chunk, S.gate_direct ? S.gate_out_st : A.width, A.width);
+#pragma unroll
+            for (int k = 0; k < NC; ++k) {
+                float g[CH], w1[CH], x[CH], old[CH];
+                get(L_GATE, k, g);
+                get(L_W1, k, w1);
+#pragma unroll
+                for (int i = 0; i < CH; ++i) x[i] = g[i] * sum_dy[k][i];
+                if (!first) {
+                    load_row<CUTS, float, CH>(pw, at[k], old);
+#pragma unroll
+                    for (int i = 0; i < CH; ++i) x[i] += old[i];
+                }
+                store_row<CUTS, float, CH>(pw, at[k], x);
+#pragma unroll
+                for (int i = 0; i < CH; ++i) x[i] = w1[i] * sum_dy[k][i];
+                if constexpr (BIAS) {
+                    get(L_B1, k, w1);
+#pragma unroll
+                    for (int i = 0; i < CH; ++i) { x[i] += w1[i] * sum_d[k][i]; g[i] *= sum_d[k][i]; sum_d[k][i] = 0.f; }
+                    if (!first) {
+                        load_row<CUTS, float, CH>(pb, at[k], old);
+#pragma unroll
+                        for (int i = 0; i < CH; ++i) g[i] += old[i];
+                    }
+                    store_row<CUTS, float, CH>(pb, at[k], g);
+                }
+                store_row<CUTS, float, CH>(pg, at[k], x);
+#pragma unroll
+                for (int i = 0; i < CH; ++i) sum_dy[k][i] = 0.f;
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    }
+    const Row<float> pw(S.part[G_PRE_W], chunk, A.width, A.width), pb(S.part[G_PRE_B], chunk, A.width, A.width);
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+        store_row<CUTS, float, CH>(pw, at[k], acc_w2[k]);
+        if constexpr (BIAS) store_row<CUTS, float, CH>(pb, at[k], acc_b2[k]);
+    }
+    if (r0 == r1) {                                             // (a chunk behind the last row of the last gate)
+        const float zero[CH] = {};
+        const Row<float> p0(S.part[G_POST_W], chunk, A.width, A.width), p1(S.part[G_POST_B], chunk, A.width, A.width);
+        const Row<float> p2(S.gate_direct ? nullptr : S.part[G_GATE], chunk, A.width, A.width);
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+            store_row<CUTS, float, CH>(p0, at[k], zero);
+            store_row<CUTS, float, CH>(p1, at[k], zero);
+            store_row<CUTS, float, CH>(p2, at[k], zero);
+        }
+    }
 }
 
 // the chunks' sums added up, always in the same order: 64 columns a workgroup, its 16 wavefronts take every 16th chunk
@@ -363,6 +566,9 @@ __global__ __launch_bounds__(1024) void k_norm_join(Joined J, uint32_t width, ui
 }
 
 // ---- host
+#ifndef NORM_ONE_MAX
+#define NORM_ONE_MAX 8192u
+#endif
 struct Shape { int nc; uint32_t threads, rows_per_wg; bool per_wave; };
 
 template <typename T, typename R> constexpr int chunk_of() { return sizeof(T) == 2 ? 8 : 4; }
@@ -381,8 +587,12 @@ template <typename T, typename R, int NC, int MAXT>
 void launch_nc(hipStream_t st, const NormArgs &A, const Shape &S, bool back) {
     constexpr int CH = chunk_of<T, R>();
     const uint32_t blocks = (uint32_t)((A.n_rows + S.rows_per_wg - 1) / S.rows_per_wg);
-    if (back) k_norm_backward<T, R, CH, NC, MAXT><<<blocks, S.threads, 0, st>>>(A, S.per_wave);
-    else k_norm_forward<T, R, CH, NC, MAXT><<<blocks, S.threads, 0, st>>>(A, S.per_wave);
+    auto go = [&](auto cuts) {
+        constexpr bool CUTS = decltype(cuts)::value;
+        if (back) k_norm_backward<CUTS, T, R, CH, NC, MAXT><<<blocks, S.threads, 0, st>>>(A, S.per_wave);
+        else k_norm_forward<CUTS, T, R, CH, NC, MAXT><<<blocks, S.threads, 0, st>>>(A, S.per_wave);
+    };
+    if (A.width % CH) go(std::true_type()); else go(std::false_type());
 }
 template <typename T, typename R> void launch_rows(hipStream_t st, const NormArgs &A, bool back) {
     const Shape S = shape_of(A.width, chunk_of<T, R>());
@@ -392,10 +602,43 @@ template <typename T, typename R> void launch_rows(hipStream_t st, const NormArg
     else if (S.nc == 4) launch_nc<T, R, 4, 1024>(st, A, S, back);
     else if constexpr (chunk_of<T, R>() == 4) launch_nc<T, R, 8, 1024>(st, A, S, back);
 }
+// How the rows are held where their sums are taken along; nc 0: too wide for a lane's registers or a compute unit's LDS, rows and sums
+// are two passes.
+Shape sums_shape_of(uint32_t width, int ch, bool bias) {
+    const int per = 8 / ch;                                     // vectors of eight elements
+    for (int n8 = 1; n8 <= 2; ++n8)
+        if (width <= 512u * n8) return Shape{n8 * per, 256, 4, true};
+    const int n8 = width <= NORM_ONE_MAX ? 1 : 2;
+    const uint32_t threads = (width + 8 * n8 * 64 - 1) / (8 * n8 * 64) * 64;
+    if (threads > (n8 == 1 ? 1024u : 768u) || threads * sums_lds_of(8, n8, bias) * 16 > 163840u - 1024u) return Shape{0, 0, 0, false};
+    return Shape{n8 * per, threads, 1, false};
+}
+template <typename T, typename R, int NC, int MAXT> int32_t launch_fused_nc(rk_ctx *ctx, const NormSums &S, const Shape &H, bool bias) {
+    constexpr int CH = chunk_of<T, R>();
+    const uint32_t blocks = (uint32_t)((S.C.n + H.rows_per_wg - 1) / H.rows_per_wg);
+    const uint32_t lds = H.threads * sums_lds_of(CH, NC, bias) * 16;
+    auto go = [&](auto cuts, auto with_bias) -> int32_t {
+        const auto kernel = k_norm_backward_sums<decltype(cuts)::value, T, R, CH, NC, MAXT, decltype(with_bias)::value>;
+        if (lds > 65536u - 1024u) RK_HIP(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+        kernel<<<blocks, H.threads, lds, ctx->stream>>>(S, H.per_wave);
+        return RK_OK;
+    };
+    const bool cuts = S.A.width % CH != 0;
+    if (bias) return cuts ? go(std::true_type(), std::true_type()) : go(std::false_type(), std::true_type());
+    return cuts ? go(std::true_type(), std::false_type()) : go(std::false_type(), std::false_type());
+}
+template <typename T, typename R> int32_t launch_fused(rk_ctx *ctx, const NormSums &S, const Shape &H, bool bias) {
+    constexpr int PER = 8 / chunk_of<T, R>();
+    if (H.nc == PER && H.threads <= 512) return launch_fused_nc<T, R, PER, 512>(ctx, S, H, bias);
+    if (H.nc == PER) return launch_fused_nc<T, R, PER, 1024>(ctx, S, H, bias);
+    if (H.threads <= 512) return launch_fused_nc<T, R, 2 * PER, 512>(ctx, S, H, bias);
+    return launch_fused_nc<T, R, 2 * PER, 768>(ctx, S, H, bias);
+}
 template <typename T, typename R> void launch_sums(hipStream_t st, const NormSums &S) {
     constexpr int CH = chunk_of<T, R>();
     const uint32_t tiles = (S.A.width + SUM_THREADS * CH - 1) / (SUM_THREADS * CH);
-    k_norm_sums<T, R, CH><<<(uint32_t)(S.C.n * tiles), SUM_THREADS, 0, st>>>(S, tiles);
+    if (S.A.width % CH) k_norm_sums<true, T, R, CH><<<(uint32_t)(S.C.n * tiles), SUM_THREADS, 0, st>>>(S, tiles);
+    else k_norm_sums<false, T, R, CH><<<(uint32_t)(S.C.n * tiles), SUM_THREADS, 0, st>>>(S, tiles);
 }
 // f(T(), R()) for the types of y and of the stream
 template <typename F> void with_types(uint32_t type, uint32_t res, F f) {
@@ -507,7 +750,7 @@ extern "C" int32_t rk_norm_backward(rk_ctx *ctx, const rk_norm_block *block, uin
     RK_HIP(ctx, hipSetDevice(ctx->device));
     NormArgs A{};
     fill_block(A, block, n_rows, width);
-    A.x = x_out->data; A.x_st = x_out->stride;
+    if (du) { A.x = x_out->data; A.x_st = x_out->stride; }
     if (y) { A.y = y->data; A.y_st = y->stride; A.u = dy->data; A.u_st = dy->stride; }
     if (dx_out) { A.dxo = dx_out->data; A.dxo_st = dx_out->stride; }
     if (du) { A.du = du->data; A.du_st = du->stride; }
@@ -516,10 +759,13 @@ extern "C" int32_t rk_norm_backward(rk_ctx *ctx, const rk_norm_block *block, uin
     NormSums S{};
     Joined J{};
     uint64_t join_jobs = 0;
+    const bool bias = block->post_bias || out[G_PRE_B];
+    const Shape H = sums_shape_of(width, type == RK_F32 ? 4 : 8, bias);
     if (any) {
-        // about two chunks a compute unit, of eight rows at least
-        uint64_t rows = (n_rows + 511) / 512;
-        if (rows < 8) rows = 8;
+        // a chunk for every workgroup (wavefront) that fits the chip at once, of four rows at least
+        const uint64_t at_once = H.per_wave ? 4096 : H.nc && H.threads <= 512 ? 512 : 256;
+        uint64_t rows = (n_rows + at_once - 1) / at_once;
+        if (rows < 4) rows = 4;
         const bool gates = A.gate_rows != 0;
         if (!gates) {
             S.C = Chunks{rows, 0, (n_rows + rows - 1) / rows};
@@ -537,8 +783,7 @@ extern "C" int32_t rk_norm_backward(rk_ctx *ctx, const rk_norm_block *block, uin
         float *part = nullptr;
         rc = rk_scratch(ctx, SL_NORM_PARTS, (size_t)(n_part * S.C.n * width) * 4, (void **)&part);
         if (rc != RK_OK) return rc;
-        rc = rk_scratch(ctx, SL_NORM_ROWS, (size_t)n_rows * 16, (void **)&A.row_sums);
-        if (rc != RK_OK) return rc;
+        if (!H.nc && (rc = rk_scratch(ctx, SL_NORM_ROWS, (size_t)n_rows * 16, (void **)&A.row_sums)) != RK_OK) return rc;
         for (int s = 0; s < G_VECTORS; ++s) {
             if (!out[s]) continue;
             if (s == G_GATE && S.gate_direct) { S.part[s] = out[s]; continue; }
@@ -554,11 +799,15 @@ extern "C" int32_t rk_norm_backward(rk_ctx *ctx, const rk_norm_block *block, uin
         join_jobs += J.n;
         if (S.C.n * ((width + 1023) / 1024) > 0x7FFFFFFFull) return rk_fail(ctx, RK_ERR_UNSUPPORTED, "too many rows");
     }
-    if (n_rows) {
+    S.A = A;
+    if (n_rows && any && H.nc) {
+        with_types(type, x_out->type, [&](auto t, auto r) { rc = launch_fused<decltype(t), decltype(r)>(ctx, S, H, bias); });
+        if (rc != RK_OK) return rc;
+        RK_CHECK_LAUNCH(ctx, "k_norm_backward_sums");
+    } else if (n_rows) {
         with_types(type, x_out->type, [&](auto t, auto r) { launch_rows<decltype(t), decltype(r)>(ctx->stream, A, true); });
         RK_CHECK_LAUNCH(ctx, "k_norm_backward");
         if (any) {
-            S.A = A;
             with_types(type, x_out->type, [&](auto t, auto r) { launch_sums<decltype(t), decltype(r)>(ctx->stream, S); });
             RK_CHECK_LAUNCH(ctx, "k_norm_sums");
         }

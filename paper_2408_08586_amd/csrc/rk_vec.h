@@ -6,32 +6,82 @@
 #pragma clang fp contract(fast)
 
 template <typename T, int N> using Vec = T __attribute__((ext_vector_type(N)));
+// N elements of a row as they lie in memory: whole 32-bit words, two narrow elements each (vectors of narrow elements themselves are
+// taken apart where paths meet, a register an element)
+template <typename T, int N> using Words = Vec<uint32_t, N * (int)sizeof(T) / 4>;
 
-// N consecutive elements of a row from `p` on, those from `valid` on being zero.  Whole vectors are loaded and stored as
-// one whatever their alignment: rows of odd strides stay on the same path, and the memory system takes accesses that are not
-// aligned apart by itself.
-template <typename T, int N> __device__ __forceinline__ void load_row(const T *__restrict__ p, int32_t valid, float (&v)[N]) {
-    typedef Vec<T, N> Any __attribute__((aligned(sizeof(T))));
-    if (valid >= N) {
-        const Vec<T, N> x = *reinterpret_cast<const Any *>(p);
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = (float)x[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = i < valid ? (float)p[i] : 0.f;
+// A row as a buffer that ends with it: what is loaded from behind its end is zero and what is stored there is dropped, by the memory
+// system, so that rows of any width take the same instructions; a matrix that is not there is one whose rows have no elements; and a
+// lane's place in a row is one register, whatever the matrix.
+template <typename T> struct Row {
+    __amdgpu_buffer_rsrc_t buf;
+    __device__ __forceinline__ Row(const void *base, uint64_t row, uint64_t stride, uint32_t width)
+        : buf(__builtin_amdgcn_make_buffer_rsrc(const_cast<T *>((const T *)base + row * stride), 0, (int)(base ? width * (uint32_t)sizeof(T) : 0u), 0x00027000)) {}
+};
+// A lane's N elements of a row, from element `first` on.  Those that are all inside go as whole vectors, whatever their alignment;
+// the ones that the row's end cuts go one by one (CUTS: the width is no multiple of N, there is such a vector).
+constexpr uint32_t ROW_NOWHERE = 1u << 29, ROW_MAX = 1u << 28;      // elements: behind every row; the widest row
+struct Place {
+    uint32_t whole, cut;            // where the vector begins, or ROW_NOWHERE
+    int32_t valid;
+    __device__ __forceinline__ Place() {}
+    __device__ __forceinline__ Place(uint32_t first, uint32_t width, int n) {
+        valid = (int32_t)width - (int32_t)first;
+        whole = valid >= n ? first : ROW_NOWHERE;
+        cut = valid > 0 && valid < n ? first : ROW_NOWHERE;
     }
+};
+template <bool CUTS, typename T, int N> __device__ __forceinline__ Words<T, N> fetch_row(const Row<T> &row, const Place &p) {
+    Words<T, N> w;
+    constexpr int PARTS = N * (int)sizeof(T) / 16;
+    const uint32_t at = p.whole * (uint32_t)sizeof(T);
+#pragma unroll
+    for (int h = 0; h < PARTS; ++h) {
+        const Vec<uint32_t, 4> x = __builtin_amdgcn_raw_buffer_load_b128(row.buf, at + 16u * h, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[4 * h + i] = x[i];
+    }
+    if constexpr (CUTS) {
+        const uint32_t from = p.cut * (uint32_t)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if constexpr (sizeof(T) == 4) w[i] |= __builtin_amdgcn_raw_buffer_load_b32(row.buf, from + 4u * i, 0, 0);
+            else w[i / 2] |= (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(row.buf, from + 2u * i, 0, 0) << (i & 1 ? 16 : 0);
+        }
+    }
+    return w;
 }
-template <typename T, int N> __device__ __forceinline__ void store_row(T *__restrict__ p, int32_t valid, const float (&v)[N]) {
-    typedef Vec<T, N> Any __attribute__((aligned(sizeof(T))));
-    if (valid >= N) {
-        Vec<T, N> x;
+template <typename T, int W> __device__ __forceinline__ float element(const Vec<uint32_t, W> &w, int i) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else if constexpr (__is_same(T, __bf16)) return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+    else return (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? w[i / 2] >> 16 : w[i / 2]));
+}
+template <bool CUTS, typename T, int N> __device__ __forceinline__ void load_row(const Row<T> &row, const Place &p, float (&v)[N]) {
+    const Words<T, N> w = fetch_row<CUTS, T, N>(row, p);
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = (T)v[i];         // to nearest, ties to even
-        *reinterpret_cast<Any *>(p) = x;
-    } else {
+    for (int i = 0; i < N; ++i) v[i] = element<T>(w, i);
+}
+template <bool CUTS, typename T, int N> __device__ __forceinline__ void store_row(const Row<T> &row, const Place &p, const float (&v)[N]) {
+    Vec<T, N> x;
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (i < valid) p[i] = (T)v[i];
+    for (int i = 0; i < N; ++i) x[i] = (T)v[i];             // to nearest, ties to even
+    const Words<T, N> w = __builtin_bit_cast(Words<T, N>, x);
+    constexpr int PARTS = N * (int)sizeof(T) / 16;
+    const uint32_t at = p.whole * (uint32_t)sizeof(T);
+#pragma unroll
+    for (int h = 0; h < PARTS; ++h) {
+        Vec<uint32_t, 4> y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = w[4 * h + i];
+        __builtin_amdgcn_raw_buffer_store_b128(y, row.buf, at + 16u * h, 0, 0);
+    }
+    if constexpr (CUTS) {
+        const uint32_t from = p.cut * (uint32_t)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(w[i], row.buf, from + 4u * i, 0, 0);
+            else __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(i & 1 ? w[i / 2] >> 16 : w[i / 2]), row.buf, from + 2u * i, 0, 0);
+        }
     }
 }
 
