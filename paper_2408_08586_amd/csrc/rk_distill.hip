@@ -7,8 +7,6 @@
 
 namespace {
 
-constexpr int DS_THREADS = 512, DS_WAVES = 8;
-
 struct DistillArgs {
     const void *student;
     void *d_student;
@@ -20,155 +18,361 @@ struct DistillArgs {
     const float *row_weight, *d_total;
     float *loss, *lse, *total;
     float temperature, kd, ce;
+    uint32_t slices, slice;             // of a row, where several workgroups share it, and their elements
+    float4 *part;                       // [row][slice]: largest logit, sums of the exponentials relative to it
+    float4 *cross;                      // [row]: what teacher and label add to the loss
 };
 
-__device__ __forceinline__ float block_sum(float v, float *lds, uint32_t lane, uint32_t wave) {
-    v = wave_sum(v);
-    __syncthreads();
-    if (lane == 0) lds[wave] = v;
-    __syncthreads();
-    return row_sum((lane & 15u) < DS_WAVES ? lds[lane & 15u] : 0.f);
-}
-__device__ __forceinline__ float block_max(float v, float *lds, uint32_t lane, uint32_t wave) {
-    v = wave_max(v);
-    __syncthreads();
-    if (lane == 0) lds[wave] = v;
-    __syncthreads();
-    return row_max((lane & 15u) < DS_WAVES ? lds[lane & 15u] : -INFINITY);
-}
-__device__ __forceinline__ float teacher_at(const DistillArgs &A, uint64_t r, uint32_t k) {
-    const uint64_t at = r * A.t_st + k;
-    return A.t_type == RK_F32 ? ((const float *)A.teacher)[at] : A.t_type == RK_BF16 ? (float)((const __bf16 *)A.teacher)[at] : (float)((const _Float16 *)A.teacher)[at];
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));        // (no quieting before: NaN come out of the sums)
+    return r;
 }
 
-// A workgroup a row.  LOSS: the sums of the softmax over the row, then the loss; GRAD: the gradient, from these or from lse.
-template <bool CUTS, typename T, int CH, bool LOSS, bool GRAD>
-__global__ __launch_bounds__(DS_THREADS) void k_distill(DistillArgs A) {
-    __shared__ float q[RK_MAX_TEACHER_LOGITS], sv[RK_MAX_TEACHER_LOGITS], red[16];
-    __shared__ int32_t at[RK_MAX_TEACHER_LOGITS];
-    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, V = A.vocab, K = A.kd > 0.f ? A.top_k : 0u;
-    const uint64_t r = blockIdx.x;
-    const T *const row = (const T *)A.student + r * A.st;
-    T *const out = (T *)A.d_student + r * A.d_st;
-    const Row<T> from(A.student, r, A.st, V), to(A.d_student, r, A.d_st, V);
-    const float weight = A.row_weight ? A.row_weight[r] : 1.f;
-    const float inv_t = 1.f / A.temperature;
-    float lse_t = 0.f, lse_1 = 0.f;
-    bool there = weight != 0.f;
-    if (there && LOSS) {
-        float m = -INFINITY, st = 0.f, s1 = 0.f;
-        for (uint32_t c0 = tid * CH; c0 < V; c0 += DS_THREADS * CH) {
-            const Place at(c0, V, CH);
-            const int32_t valid = at.valid;
-            float v[CH], top = m;
-            load_row<CUTS, T, CH>(from, at, v);
+// The exponentials of a row: one stream where the two terms of the loss share it (T = 1) or one of them is all there is, two
+// streams otherwise, of which the second is the first's square if T = 2.
+enum { ONE, TWO, SQUARE };
+
+// What is not positive is taken off first, in the logits' own units: masks of the type's lowest value stay finite.  A 16-bit student's
+// exponentials are then one product and one instruction to base 2: the exponent's rounding, 2^-24 of it, is far below a step of the
+// logits.  A 32-bit student's have the argument's lower part (exp_f32).
+template <typename T> struct Exp {
+    static constexpr bool EXACT = sizeof(T) == 4;
+    static __device__ __forceinline__ float of(float x) { return EXACT ? exp_f32(x) : __builtin_amdgcn_exp2f(x); }
+    static __device__ __forceinline__ float log(float x) { return EXACT ? logf(x) : __builtin_amdgcn_logf(x); }
+    static __device__ __forceinline__ float unit() { return EXACT ? 1.f : 1.4426950408889634f; }
+    static __device__ __forceinline__ float natural(float x) { return EXACT ? x : x * 0.6931471805599453f; }
+};
+struct Streams { float ka, kb, inv_a; };        // what a difference of logits is multiplied by; the first without the base
+template <typename T> __device__ __forceinline__ Streams streams_of(const DistillArgs &A) {
+    const float inv = A.kd > 0.f ? 1.f / A.temperature : 1.f;
+    return Streams{inv * Exp<T>::unit(), Exp<T>::unit(), inv};
+}
+
+// the sums of a stretch of logits, relative to the largest of them seen so far
+template <typename T, int SUMS> struct Running {
+    float m = -INFINITY, ref = 0.f, sa = 0.f, sb = 0.f;         // (nothing above -inf yet: relative to 0)
+    __device__ __forceinline__ void to(const Streams &S, float by) {
+        const float f = Exp<T>::of(by * S.ka);
+        sa *= f;
+        if constexpr (SUMS == TWO) sb *= Exp<T>::of(by * S.kb);
+        if constexpr (SUMS == SQUARE) sb *= f * f;
+    }
+    template <int CH> __device__ __forceinline__ void take(const Streams &S, const float (&v)[CH]) {
+        float top = v[0];
 #pragma unroll
-            for (int i = 0; i < CH; ++i) if (i < valid) top = fmaxf(top, v[i]);
-            const float ref = top == -INFINITY ? 0.f : top;
-            if (top > m) { st *= exp_f32((m - ref) * inv_t); s1 *= exp_f32(m - ref); m = top; }
+        for (int i = 1; i + 1 < CH; i += 2) top = max3(top, v[i], v[i + 1]);
+        top = max3(top, v[CH - 1], m);
+        if (top > m) { to(S, m - top); m = top; ref = top; }
 #pragma unroll
-            for (int i = 0; i < CH; ++i) {
-                if (i >= valid) continue;
-                if (A.kd > 0.f) st += exp_f32((v[i] - ref) * inv_t);
-                if (A.ce > 0.f) s1 += exp_f32(v[i] - ref);
+        for (int i = 0; i < CH; ++i) {
+            const float d = v[i] - ref, e = Exp<T>::of(d * S.ka);
+            sa += e;
+            if constexpr (SUMS == TWO) sb += Exp<T>::of(d * S.kb);
+            if constexpr (SUMS == SQUARE) sb += e * e;
+        }
+    }
+    // relative to another largest one
+    __device__ __forceinline__ void move(const Streams &S, float top) {
+        if (m != -INFINITY) to(S, m - top);
+    }
+};
+
+// Calls f(first, words) for a thread's vectors of [begin, end), four of which are under way at once, and then tail(place) for those
+// behind the last whole round; end is the row's end or a multiple of CH.
+template <int THREADS, typename T, int CH, typename F, typename G>
+__device__ __forceinline__ void stream_row(const Row<T> &row, uint32_t begin, uint32_t end, uint32_t vocab, F f, G tail) {
+    constexpr uint32_t U = 4, STEP = THREADS * CH;
+    uint32_t base = begin + threadIdx.x * CH;
+    for (uint32_t round = begin; round + U * STEP <= end; round += U * STEP, base += U * STEP) {
+        Words<T, CH> w[U];
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) w[u] = fetch_at<T, CH>(row, base + u * STEP);
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) f(base + u * STEP, w[u]);
+    }
+    for (; base < end; base += STEP) tail(Place(base, vocab, CH));
+}
+template <bool CUTS, int THREADS, typename T, int CH, int SUMS>
+__device__ __forceinline__ void sum_row(const Row<T> &row, uint32_t begin, uint32_t end, uint32_t vocab, const Streams &S, Running<T, SUMS> &R) {
+    stream_row<THREADS, T, CH>(row, begin, end, vocab,
+        [&](uint32_t, const Words<T, CH> &w) {
+            float v[CH];
+#pragma unroll
+            for (int i = 0; i < CH; ++i) v[i] = element<T>(w, i);
+            R.take(S, v);
+        },
+        [&](const Place &p) {
+            float v[CH];
+            load_row<CUTS, T, CH>(row, p, v);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) v[i] = i < p.valid ? v[i] : -INFINITY;
+            R.take(S, v);
+        });
+}
+
+// What a row's teacher and label say: a thread holds kept logits tid, tid + THREADS, ..., fetched before the row's logits.
+template <int THREADS> struct Wanted {
+    static constexpr int N = (int)RK_MAX_TEACHER_LOGITS / THREADS;
+    int32_t at[N], label;
+    float t[N], s[N], label_s;
+    template <typename T> __device__ __forceinline__ void fetch(const DistillArgs &A, uint64_t r) {
+        const T *const row = (const T *)A.student + r * A.st;
+        label = A.ce > 0.f ? A.label[r] : -1;
+        if ((uint32_t)label >= A.vocab) label = -1;
+        label_s = label >= 0 ? (float)row[label] : 0.f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const uint32_t k = threadIdx.x + n * THREADS;
+            at[n] = -1; t[n] = -INFINITY; s[n] = 0.f;
+            if (A.kd > 0.f && k < A.top_k) {
+                const int32_t i = A.index[r * A.top_k + k];
+                const uint64_t p = r * A.t_st + k;
+                t[n] = A.t_type == RK_F32 ? ((const float *)A.teacher)[p] : A.t_type == RK_BF16 ? (float)((const __bf16 *)A.teacher)[p] : (float)((const _Float16 *)A.teacher)[p];
+                at[n] = (uint32_t)i < A.vocab && t[n] != -INFINITY ? i : -1;
+                if (at[n] >= 0) s[n] = (float)row[i];
+                else t[n] = -INFINITY;
             }
         }
-        const float top = block_max(m, red, lane, wave);
-        if (top == -INFINITY) {
-            there = false;
-            lse_t = A.kd > 0.f ? -INFINITY : 0.f; lse_1 = A.ce > 0.f ? -INFINITY : 0.f;
-        } else {
-            // a thread that saw nothing above -inf has sums of zero (or NaN), taken about zero
-            const float own = m == -INFINITY ? 0.f : (m - top);
-            st = block_sum(st * exp_f32(own * inv_t), red, lane, wave);
-            s1 = block_sum(s1 * exp_f32(own), red, lane, wave);
-            if (A.kd > 0.f) lse_t = top * inv_t + logf(st);
-            if (A.ce > 0.f) lse_1 = top + logf(s1);
-        }
     }
-    if (there && !LOSS) {
-        lse_t = A.lse[2 * r]; lse_1 = A.lse[2 * r + 1];
-        there = (A.kd > 0.f ? lse_t : lse_1) != -INFINITY;
-    }
-    const int32_t label = A.ce > 0.f && there ? A.label[r] : -1;
-    const bool labelled = label >= 0 && (uint32_t)label < V;
-    float ce = labelled ? A.ce : 0.f, big_q = 0.f, log_sum = 0.f, tmax = -INFINITY;
-    if (there && K) {
-        for (uint32_t k = tid; k < K; k += DS_THREADS) {
-            const int32_t i = A.index[r * K + k];
-            const float t = teacher_at(A, r, k);
-            const bool kept = i >= 0 && (uint32_t)i < V && t != -INFINITY;
-            at[k] = kept ? i : -1;
-            q[k] = t;
-            sv[k] = kept ? (float)row[i] : 0.f;
-            if (kept) tmax = fmaxf(tmax, t);
-        }
-        tmax = block_max(tmax, red, lane, wave);
-        float s = 0.f, some = 0.f;
-        for (uint32_t k = tid; k < K; k += DS_THREADS) {
-            if (at[k] < 0) continue;
-            some = 1.f;
-            s += exp_f32((q[k] - tmax) * inv_t);
-        }
-        s = block_sum(s, red, lane, wave);
-        big_q = block_max(some, red, lane, wave);
-        log_sum = logf(s);
-    }
-    const float kd = big_q > 0.f ? A.kd : 0.f;
-    if (there && K) {
-        float part = 0.f;
-        for (uint32_t k = tid; k < K; k += DS_THREADS) {
-            if (at[k] < 0) continue;
-            const float log_q = (q[k] - tmax) * inv_t - log_sum, v = exp_f32(log_q);
-            q[k] = v;
-            if (v != 0.f) part += v * (log_q - (sv[k] * inv_t - lse_t));
-        }
-        if (LOSS) part = block_sum(part, red, lane, wave);
-        if (LOSS && tid == 0) {
-            float l = kd * A.temperature * A.temperature * part;
-            if (labelled) l += ce * (lse_1 - (float)row[label]);
-            A.loss[r] = l;
-        }
-    } else if (LOSS && tid == 0) {
-        A.loss[r] = there && labelled ? ce * (lse_1 - (float)row[label]) : 0.f;
-    }
-    if (LOSS && tid == 0) { A.lse[2 * r] = lse_t; A.lse[2 * r + 1] = lse_1; }
-    if (!GRAD) return;
-    const float scale = there ? weight * (A.d_total ? A.d_total[0] : 1.f) : 0.f;
-    const float ft = scale * kd * A.temperature, f1 = scale * ce;
-    const float label_v = labelled ? (float)row[label] : 0.f;
-    __syncthreads();                            // d_student may be student: what the rest needs of the row is held
-    for (uint32_t c0 = tid * CH; c0 < V; c0 += DS_THREADS * CH) {
-        const Place place(c0, V, CH);
-        float v[CH] = {};
-        if (there) {
-            load_row<CUTS, T, CH>(from, place, v);
+    __device__ __forceinline__ float top() const {
+        float m = t[0];
 #pragma unroll
-            for (int i = 0; i < CH; ++i) {
-                float d = 0.f;
-                if (kd > 0.f) d += ft * exp_f32(v[i] * inv_t - lse_t);
-                if (ce > 0.f) d += f1 * exp_f32(v[i] - lse_1);
-                v[i] = d;
-            }
-        }
-        store_row<CUTS, T, CH>(to, place, v);
+        for (int n = 1; n < N; ++n) m = fmaxf(m, t[n]);
+        return m;
     }
-    if (!there) return;
+    // t becomes e^((t - top) / T); sum and cross are the thread's parts of sum e and sum e ((t - s - top) / T)
+    __device__ __forceinline__ void weigh(const DistillArgs &A, float top, float &sum, float &cross) {
+        const float inv = 1.f / A.temperature;
+        sum = 0.f; cross = 0.f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const float x = (t[n] - top) * inv, e = at[n] >= 0 ? exp_f32(x) : 0.f;
+            t[n] = e;
+            sum += e;
+            if (e != 0.f) cross += e * (x - s[n] * inv);
+        }
+    }
+};
+
+// sums (or maxima) over a workgroup, two barriers
+template <int WAVES, bool MAX> __device__ __forceinline__ void block_all(float4 &v, float4 *lds) {
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    auto one = [](float x) { return MAX ? wave_max(x) : wave_sum(x); };
+    v = make_float4(one(v.x), one(v.y), one(v.z), one(v.w));
+    __syncthreads();
+    if (lane == 0) lds[wave] = v;
+    __syncthreads();
+    const float none = MAX ? -INFINITY : 0.f;
+    const float4 o = (lane & 15u) < (uint32_t)WAVES ? lds[lane & 15u] : make_float4(none, none, none, none);
+    auto row = [](float x) { return MAX ? row_max(x) : row_sum(x); };
+    v = make_float4(row(o.x), row(o.y), row(o.z), row(o.w));
+}
+
+// d s of [begin, end) of a row: its streams' exponentials are e^(k (s - top) - l), in the streams' units
+template <bool CUTS, int THREADS, typename T, int CH, int SUMS>
+__device__ __forceinline__ void write_gradient(const DistillArgs &A, const Row<T> &from, const Row<T> &to, T *out, uint32_t begin, uint32_t end, const Streams &S,
+                                               float top, float la, float lb, float weight, bool kept, Wanted<THREADS> &W, float t_sum, float *q, int32_t *at) {
+    const float scale = weight * (A.d_total ? A.d_total[0] : 1.f);
+    const float ft = kept ? scale * A.kd * A.temperature : 0.f, f1 = W.label >= 0 ? scale * A.ce : 0.f;
+    // (a stream that both terms share, or that is the only term's)
+    const float ca = SUMS == ONE ? ft + f1 : ft, cb = SUMS == SQUARE ? f1 * Exp<T>::of(la + la - lb) : f1;
+    const uint32_t K = A.kd > 0.f ? A.top_k : 0u;
+    const float inv_sum = kept ? 1.f / t_sum : 0.f;
+#pragma unroll
+    for (int n = 0; n < Wanted<THREADS>::N; ++n) {
+        const uint32_t k = threadIdx.x + n * THREADS;
+        if (k < K) { q[k] = W.t[n] * inv_sum; at[k] = W.at[n]; }
+    }
+    __syncthreads();                    // d_student may be student: what is needed of other places has been read
+    auto slope = [&](float x) {
+        const float v = x - top, e = Exp<T>::of(__builtin_fmaf(v, S.ka, -la));
+        if constexpr (SUMS == ONE) return ca * e;
+        if constexpr (SUMS == TWO) return ca * e + cb * Exp<T>::of(__builtin_fmaf(v, S.kb, -lb));
+        return e * (ca + cb * e);
+    };
+    stream_row<THREADS, T, CH>(from, begin, end, A.vocab,
+        [&](uint32_t first, const Words<T, CH> &w) {
+            float v[CH];
+#pragma unroll
+            for (int i = 0; i < CH; ++i) v[i] = slope(element<T>(w, i));
+            store_at<T, CH>(to, first, words_of<T, CH>(v));
+        },
+        [&](const Place &p) {
+            float v[CH];
+            load_row<CUTS, T, CH>(from, p, v);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) v[i] = slope(v[i]);
+            store_row<CUTS, T, CH>(to, p, v);
+        });
     __syncthreads();
     // where teacher or label have something: the whole value, once more (equal indices get equal values)
-    auto fix = [&](int32_t i, float s) {
-        float d = 0.f;
-        if (kd > 0.f) {
-            float mass = 0.f;
-            for (uint32_t k = 0; k < K; ++k) mass += at[k] == i ? q[k] : 0.f;
-            d += ft * (exp_f32(s * inv_t - lse_t) - mass);
-        }
-        if (ce > 0.f) d += f1 * (exp_f32(s - lse_1) - (i == label ? 1.f : 0.f));
-        out[i] = (T)d;
+    auto again = [&](int32_t i, float s) {
+        if ((uint32_t)i < begin || (uint32_t)i >= end) return;
+        float mass = 0.f;
+        for (uint32_t k = 0; k < K; ++k) mass += at[k] == i ? q[k] : 0.f;
+        out[i] = (T)(slope(s) - ft * mass - (i == W.label ? f1 : 0.f));
     };
-    for (uint32_t k = tid; k < K; k += DS_THREADS)
-        if (at[k] >= 0) fix(at[k], sv[k]);
-    if (tid == 0 && labelled) fix(label, label_v);
+#pragma unroll
+    for (int n = 0; n < Wanted<THREADS>::N; ++n)
+        if (W.at[n] >= 0) again(W.at[n], W.s[n]);
+    if (threadIdx.x == 0 && W.label >= 0) again(W.label, W.label_s);
+}
+template <bool CUTS, int THREADS, typename T, int CH> __device__ __forceinline__ void write_zeros(const Row<T> &to, uint32_t begin, uint32_t end, uint32_t vocab) {
+    const float zero[CH] = {};
+    for (uint32_t c = begin + threadIdx.x * CH; c < end; c += THREADS * CH) store_row<CUTS, T, CH>(to, Place(c, vocab, CH), zero);
+}
+
+// a row's loss and log sums from the joined sums; cross: teacher's cross term and sum, the label's logit and whether there is one
+struct RowLoss { float loss, lse_a, lse_b, la, lb; bool left; };
+template <typename T, int SUMS> __device__ __forceinline__ RowLoss row_loss(const DistillArgs &A, const Streams &S, float top, float sa, float sb, float4 cross) {
+    if (top == -INFINITY) return RowLoss{0.f, -INFINITY, -INFINITY, 0.f, 0.f, true};
+    RowLoss L;
+    L.left = false;
+    L.la = Exp<T>::log(sa);
+    L.lb = SUMS == ONE ? L.la : Exp<T>::log(sb);
+    L.lse_a = top * S.inv_a + Exp<T>::natural(L.la);
+    L.lse_b = SUMS == ONE ? L.lse_a : top + Exp<T>::natural(L.lb);
+    L.loss = 0.f;
+    if (A.kd > 0.f && cross.y != 0.f) L.loss = A.kd * A.temperature * A.temperature * (cross.x / cross.y - logf(cross.y) + L.lse_a);
+    if (A.ce > 0.f && cross.w != 0.f) L.loss += A.ce * (L.lse_b - cross.z);
+    return L;
+}
+__device__ __forceinline__ void keep_row(const DistillArgs &A, uint64_t r, const RowLoss &L) {
+    A.loss[r] = L.loss;
+    A.lse[2 * r] = A.kd > 0.f ? L.lse_a : 0.f;
+    A.lse[2 * r + 1] = A.ce > 0.f ? L.lse_b : 0.f;
+}
+
+// A workgroup a row: its sums, its loss and (GRAD) its gradient, for which the row is read again, from the caches.
+template <bool CUTS, int THREADS, typename T, int CH, int SUMS, bool GRAD>
+__global__ __launch_bounds__(THREADS) void k_distill_rows(DistillArgs A) {
+    __shared__ float4 red[16];
+    __shared__ float q[GRAD ? RK_MAX_TEACHER_LOGITS : 1];
+    __shared__ int32_t at[GRAD ? RK_MAX_TEACHER_LOGITS : 1];
+    const uint64_t r = blockIdx.x;
+    const Row<T> from(A.student, r, A.st, A.vocab), to(A.d_student, r, A.d_st, A.vocab);
+    const float weight = A.row_weight ? A.row_weight[r] : 1.f;
+    if (weight == 0.f) {
+        if (threadIdx.x == 0) { A.loss[r] = 0.f; A.lse[2 * r] = 0.f; A.lse[2 * r + 1] = 0.f; }
+        if constexpr (GRAD) write_zeros<CUTS, THREADS, T, CH>(to, 0, A.vocab, A.vocab);
+        return;
+    }
+    Wanted<THREADS> W;
+    W.template fetch<T>(A, r);
+    const Streams S = streams_of<T>(A);
+    Running<T, SUMS> R;
+    sum_row<CUTS, THREADS, T, CH, SUMS>(from, 0, A.vocab, A.vocab, S, R);
+    float4 v = make_float4(R.m, W.top(), -INFINITY, -INFINITY);
+    block_all<THREADS / 64, true>(v, red);
+    const float top = v.x;
+    R.move(S, top);
+    float sum, cross;
+    W.weigh(A, v.y, sum, cross);
+    v = make_float4(R.sa, R.sb, sum, cross);
+    block_all<THREADS / 64, false>(v, red);
+    const RowLoss L = row_loss<T, SUMS>(A, S, top, v.x, v.y, make_float4(v.w, v.z, W.label_s, W.label >= 0 ? 1.f : 0.f));
+    if (threadIdx.x == 0) keep_row(A, r, L);
+    if constexpr (GRAD) {
+        // (without a kept logit and a label there is no term, whatever the logits hold)
+        if (L.left || (v.z == 0.f && W.label < 0)) write_zeros<CUTS, THREADS, T, CH>(to, 0, A.vocab, A.vocab);
+        else write_gradient<CUTS, THREADS, T, CH, SUMS>(A, from, to, (T *)A.d_student + r * A.d_st, 0, A.vocab, S, top, L.la, L.lb, weight, v.z != 0.f, W, v.z, q, at);
+    }
+}
+
+// The sums of a slice of a row, for k_distill_join; the first slice's workgroup also looks up what teacher and label want.
+template <bool CUTS, int THREADS, typename T, int CH, int SUMS>
+__global__ __launch_bounds__(THREADS) void k_distill_part(DistillArgs A) {
+    __shared__ float4 red[16];
+    const uint64_t r = blockIdx.x / A.slices;
+    const uint32_t slice = blockIdx.x - (uint32_t)r * A.slices, begin = slice * A.slice;
+    const uint32_t end = slice + 1 == A.slices ? A.vocab : begin + A.slice;
+    if (A.row_weight && A.row_weight[r] == 0.f) return;
+    const Row<T> from(A.student, r, A.st, A.vocab);
+    Wanted<THREADS> W;
+    W.at[0] = -1; W.t[0] = -INFINITY;
+    if (slice == 0) W.template fetch<T>(A, r);
+    const Streams S = streams_of<T>(A);
+    Running<T, SUMS> R;
+    sum_row<CUTS, THREADS, T, CH, SUMS>(from, begin, end, A.vocab, S, R);
+    float4 v = make_float4(R.m, slice == 0 ? W.top() : -INFINITY, -INFINITY, -INFINITY);
+    block_all<THREADS / 64, true>(v, red);
+    const float top = v.x;
+    R.move(S, top);
+    float sum = 0.f, cross = 0.f;
+    if (slice == 0) W.weigh(A, v.y, sum, cross);
+    v = make_float4(R.sa, R.sb, sum, cross);
+    block_all<THREADS / 64, false>(v, red);
+    if (threadIdx.x) return;
+    A.part[r * A.slices + slice] = make_float4(top, v.x, v.y, 0.f);
+    if (slice == 0) A.cross[r] = make_float4(v.w, v.z, W.label_s, W.label >= 0 ? 1.f : 0.f);
+}
+
+// The slices of the rows joined, a wavefront a row (at most 64 slices), and the rows' losses added up, in one order.
+constexpr int JOIN_WAVES = 16;
+template <typename T, int SUMS> __global__ __launch_bounds__(64 * JOIN_WAVES) void k_distill_join(DistillArgs A) {
+    __shared__ double lds[JOIN_WAVES];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const Streams S = streams_of<T>(A);
+    double total = 0.0;
+    for (uint64_t r = wave; r < A.n_rows; r += JOIN_WAVES) {
+        const float weight = A.row_weight ? A.row_weight[r] : 1.f;
+        if (weight == 0.f) {
+            if (lane == 0) { A.loss[r] = 0.f; A.lse[2 * r] = 0.f; A.lse[2 * r + 1] = 0.f; }
+            continue;
+        }
+        const float4 p = lane < A.slices ? A.part[r * A.slices + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+        const float top = wave_max(p.x);
+        Running<T, SUMS> R;
+        R.m = p.x; R.sa = p.y; R.sb = p.z;
+        R.move(S, top);
+        const RowLoss L = row_loss<T, SUMS>(A, S, top, wave_sum(R.sa), wave_sum(R.sb), A.cross[r]);
+        if (lane == 0) keep_row(A, r, L);
+        total += (double)weight * (double)L.loss;
+    }
+    if (lane == 0) lds[wave] = total;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < JOIN_WAVES; ++w) total += lds[w];
+    A.total[0] = (float)total;
+}
+
+// The gradient of a slice of a row (or of all of it) from the row's log sums.
+template <bool CUTS, int THREADS, typename T, int CH, int SUMS>
+__global__ __launch_bounds__(THREADS) void k_distill_gradient(DistillArgs A) {
+    __shared__ float4 red[16];
+    __shared__ float q[RK_MAX_TEACHER_LOGITS];
+    __shared__ int32_t at[RK_MAX_TEACHER_LOGITS];
+    const uint64_t r = blockIdx.x / A.slices;
+    const uint32_t slice = blockIdx.x - (uint32_t)r * A.slices, begin = slice * A.slice;
+    const uint32_t end = slice + 1 == A.slices ? A.vocab : begin + A.slice;
+    const Row<T> from(A.student, r, A.st, A.vocab), to(A.d_student, r, A.d_st, A.vocab);
+    const float weight = A.row_weight ? A.row_weight[r] : 1.f;
+    const float la = A.lse[2 * r + (A.kd > 0.f ? 0 : 1)], lb = A.lse[2 * r + 1];
+    if (weight == 0.f || la == -INFINITY) {
+        write_zeros<CUTS, THREADS, T, CH>(to, begin, end, A.vocab);
+        return;
+    }
+    Wanted<THREADS> W;
+    W.template fetch<T>(A, r);
+    float4 v = make_float4(W.top(), -INFINITY, -INFINITY, -INFINITY);
+    float sum = 0.f, cross = 0.f;
+    if (A.kd > 0.f) {
+        block_all<THREADS / 64, true>(v, red);
+        W.weigh(A, v.x, sum, cross);
+        v = make_float4(sum, 0.f, 0.f, 0.f);
+        block_all<THREADS / 64, false>(v, red);
+        sum = v.x;
+    }
+    if (sum == 0.f && W.label < 0) {
+        write_zeros<CUTS, THREADS, T, CH>(to, begin, end, A.vocab);
+        return;
+    }
+    // relative to where the first stream's exponential is one
+    const Streams S = streams_of<T>(A);
+    const float top = SUMS == ONE && A.kd == 0.f ? la : la * A.temperature;
+    write_gradient<CUTS, THREADS, T, CH, SUMS>(A, from, to, (T *)A.d_student + r * A.d_st, begin, end, S, top, 0.f, (lb - top) * S.kb, weight, sum != 0.f, W, sum, q,
+                                               at);
 }
 
 // the rows' losses added up, in one order
@@ -188,6 +392,8 @@ __global__ __launch_bounds__(1024) void k_distill_total(DistillArgs A) {
 }
 
 // ---- host
+constexpr uint32_t DS_SMALL = 8192;           // elements up to which 256 threads take a row or slice
+
 int32_t check_distill(rk_ctx *ctx, const rk_distill *d, uint64_t n_rows, uint32_t vocab, const rk_matrix *student, const rk_teacher *t, DistillArgs &A) {
     if (!d || !t) return rk_fail(ctx, RK_ERR_INVALID_ARG, "distill or teacher is null");
     if (!(d->temperature > 0.f) || !std::isfinite(d->temperature) || !(d->kd_weight >= 0.f) || !(d->ce_weight >= 0.f) ||
@@ -210,23 +416,75 @@ int32_t check_distill(rk_ctx *ctx, const rk_distill *d, uint64_t n_rows, uint32_
     A.temperature = d->temperature; A.kd = d->kd_weight; A.ce = d->ce_weight;
     return RK_OK;
 }
-template <bool LOSS, bool GRAD> void launch_type(hipStream_t st, uint32_t type, const DistillArgs &A) {
-    const uint32_t n = (uint32_t)A.n_rows;
-    auto go = [&](auto cuts) {
+enum Step { STEP_LOSS, STEP_BOTH, STEP_PART, STEP_JOIN, STEP_GRADIENT };
+template <typename T, int SUMS> void launch(hipStream_t st, const DistillArgs &A, Step step) {
+    constexpr int CH = sizeof(T) == 4 ? 4 : 8;
+    if (step == STEP_JOIN) {
+        k_distill_join<T, SUMS><<<1, 64 * JOIN_WAVES, 0, st>>>(A);
+        return;
+    }
+    auto go = [&](auto cuts, auto threads) {
         constexpr bool CUTS = decltype(cuts)::value;
-        if (type == RK_F32) k_distill<CUTS, float, 4, LOSS, GRAD><<<n, DS_THREADS, 0, st>>>(A);
-        else if (type == RK_BF16) k_distill<CUTS, __bf16, 8, LOSS, GRAD><<<n, DS_THREADS, 0, st>>>(A);
-        else k_distill<CUTS, _Float16, 8, LOSS, GRAD><<<n, DS_THREADS, 0, st>>>(A);
+        constexpr int N = decltype(threads)::value;
+        const uint32_t blocks = (uint32_t)(A.n_rows * A.slices);
+        if (step == STEP_LOSS) k_distill_rows<CUTS, N, T, CH, SUMS, false><<<blocks, N, 0, st>>>(A);
+        else if (step == STEP_BOTH) k_distill_rows<CUTS, N, T, CH, SUMS, true><<<blocks, N, 0, st>>>(A);
+        else if (step == STEP_PART) k_distill_part<CUTS, N, T, CH, SUMS><<<blocks, N, 0, st>>>(A);
+        else k_distill_gradient<CUTS, N, T, CH, SUMS><<<blocks, N, 0, st>>>(A);
     };
-    if (A.vocab % (type == RK_F32 ? 4 : 8)) go(std::true_type()); else go(std::false_type());
+    auto sized = [&](auto cuts) {
+        if (A.slice <= DS_SMALL) go(cuts, std::integral_constant<int, 256>());
+        else go(cuts, std::integral_constant<int, 1024>());
+    };
+    if (A.vocab % CH) sized(std::true_type()); else sized(std::false_type());
+}
+int32_t send(rk_ctx *ctx, uint32_t type, const DistillArgs &A, Step step) {
+    const int sums = A.kd == 0.f || A.ce == 0.f || A.temperature == 1.f ? ONE : A.temperature == 2.f && type != RK_F32 ? SQUARE : TWO;
+    if (type == RK_F32) { if (sums == ONE) launch<float, ONE>(ctx->stream, A, step); else launch<float, TWO>(ctx->stream, A, step); }
+    else if (type == RK_BF16) {
+        if (sums == ONE) launch<__bf16, ONE>(ctx->stream, A, step);
+        else if (sums == TWO) launch<__bf16, TWO>(ctx->stream, A, step);
+        else launch<__bf16, SQUARE>(ctx->stream, A, step);
+    } else {
+        if (sums == ONE) launch<_Float16, ONE>(ctx->stream, A, step);
+        else if (sums == TWO) launch<_Float16, TWO>(ctx->stream, A, step);
+        else launch<_Float16, SQUARE>(ctx->stream, A, step);
+    }
+    RK_CHECK_LAUNCH(ctx, step == STEP_JOIN ? "k_distill_join" : step == STEP_PART ? "k_distill_part" : step == STEP_GRADIENT ? "k_distill_gradient" : "k_distill_rows");
+    return RK_OK;
+}
+// rows in as many slices as bring `want` workgroups together, of `least` elements at least
+void cut_rows(DistillArgs &A, uint64_t want, uint32_t least) {
+    uint64_t n = A.n_rows ? want / A.n_rows : 1;
+    if (n > A.vocab / least) n = A.vocab / least;
+    if (n > 64) n = 64;                                         // k_distill_join: a lane a slice
+    if (n < 1) n = 1;
+    A.slice = (uint32_t)(((A.vocab + n - 1) / n + 7) / 8 * 8);
+    A.slices = (A.vocab + A.slice - 1) / A.slice;
 }
 int32_t run(rk_ctx *ctx, uint32_t type, DistillArgs &A, bool want_loss, bool want_grad) {
     RK_HIP(ctx, hipSetDevice(ctx->device));
-    if (A.n_rows) {
-        if (want_loss && want_grad) launch_type<true, true>(ctx->stream, type, A);
-        else if (want_loss) launch_type<true, false>(ctx->stream, type, A);
-        else launch_type<false, true>(ctx->stream, type, A);
-        RK_CHECK_LAUNCH(ctx, "k_distill");
+    int32_t rc;
+    A.slices = 1; A.slice = A.vocab;
+    bool gradient = want_grad && !want_loss;
+    if (want_loss && A.n_rows) {
+        cut_rows(A, 512, 4096);
+        if (A.n_rows < 256 && A.slices > 1) {
+            const size_t parts = (size_t)(A.n_rows * A.slices);
+            float4 *room;
+            if ((rc = rk_scratch(ctx, SL_DISTILL_PARTS, (parts + A.n_rows) * 16, (void **)&room)) != RK_OK) return rc;
+            A.part = room; A.cross = room + parts;
+            if ((rc = send(ctx, type, A, STEP_PART)) != RK_OK || (rc = send(ctx, type, A, STEP_JOIN)) != RK_OK) return rc;
+            gradient = want_grad;
+            want_loss = false;
+        } else {
+            A.slices = 1; A.slice = A.vocab;
+            if ((rc = send(ctx, type, A, want_grad ? STEP_BOTH : STEP_LOSS)) != RK_OK) return rc;
+        }
+    }
+    if (gradient && A.n_rows) {
+        cut_rows(A, 1024, 8192);
+        if ((rc = send(ctx, type, A, STEP_GRADIENT)) != RK_OK) return rc;
     }
     if (want_loss) {
         k_distill_total<<<1, 1024, 0, ctx->stream>>>(A);

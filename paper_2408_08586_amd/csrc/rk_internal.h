@@ -75,6 +75,7 @@ enum {
     SL_FIT_NEXT,                                         // model fitting: the next model to take
     SL_NORM_PARTS, SL_NORM_ROWS,                         // norms around a block: sums of the chunks of rows; per row, what its gradient takes off
     SL_ROUTE_COUNTS, SL_ROUTE_PROBS, SL_ROUTE_Z, SL_ROUTE_GROUPS,   // router: its workgroups' counts and sums, its groups'
+    SL_DISTILL_PARTS,                                    // distillation: the sums of the rows' slices
     SL_COUNT
 };
 static_assert(SL_COUNT <= RK_SCRATCH_SLOTS, "more scratch slots than the context holds");

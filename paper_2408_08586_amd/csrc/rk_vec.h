@@ -24,24 +24,30 @@ constexpr uint32_t ROW_NOWHERE = 1u << 29, ROW_MAX = 1u << 28;      // elements:
 struct Place {
     uint32_t whole, cut;            // where the vector begins, or ROW_NOWHERE
     int32_t valid;
+    bool cut_here;                  // some lane of the wavefront has one that is cut: only these take the long way
     __device__ __forceinline__ Place() {}
     __device__ __forceinline__ Place(uint32_t first, uint32_t width, int n) {
         valid = (int32_t)width - (int32_t)first;
         whole = valid >= n ? first : ROW_NOWHERE;
         cut = valid > 0 && valid < n ? first : ROW_NOWHERE;
+        cut_here = __builtin_amdgcn_ballot_w64(cut != ROW_NOWHERE) != 0;
     }
 };
-template <bool CUTS, typename T, int N> __device__ __forceinline__ Words<T, N> fetch_row(const Row<T> &row, const Place &p) {
+template <typename T, int N> __device__ __forceinline__ Words<T, N> fetch_at(const Row<T> &row, uint32_t first) {
     Words<T, N> w;
     constexpr int PARTS = N * (int)sizeof(T) / 16;
-    const uint32_t at = p.whole * (uint32_t)sizeof(T);
+    const uint32_t at = first * (uint32_t)sizeof(T);
 #pragma unroll
     for (int h = 0; h < PARTS; ++h) {
         const Vec<uint32_t, 4> x = __builtin_amdgcn_raw_buffer_load_b128(row.buf, at + 16u * h, 0, 0);
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[4 * h + i] = x[i];
     }
-    if constexpr (CUTS) {
+    return w;
+}
+template <bool CUTS, typename T, int N> __device__ __forceinline__ Words<T, N> fetch_row(const Row<T> &row, const Place &p) {
+    Words<T, N> w = fetch_at<T, N>(row, p.whole);
+    if (CUTS && p.cut_here) {
         const uint32_t from = p.cut * (uint32_t)sizeof(T);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -61,13 +67,15 @@ template <bool CUTS, typename T, int N> __device__ __forceinline__ void load_row
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = element<T>(w, i);
 }
-template <bool CUTS, typename T, int N> __device__ __forceinline__ void store_row(const Row<T> &row, const Place &p, const float (&v)[N]) {
+template <typename T, int N> __device__ __forceinline__ Words<T, N> words_of(const float (&v)[N]) {
     Vec<T, N> x;
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = (T)v[i];             // to nearest, ties to even
-    const Words<T, N> w = __builtin_bit_cast(Words<T, N>, x);
+    return __builtin_bit_cast(Words<T, N>, x);
+}
+template <typename T, int N> __device__ __forceinline__ void store_at(const Row<T> &row, uint32_t first, const Words<T, N> &w) {
     constexpr int PARTS = N * (int)sizeof(T) / 16;
-    const uint32_t at = p.whole * (uint32_t)sizeof(T);
+    const uint32_t at = first * (uint32_t)sizeof(T);
 #pragma unroll
     for (int h = 0; h < PARTS; ++h) {
         Vec<uint32_t, 4> y;
@@ -75,7 +83,11 @@ template <bool CUTS, typename T, int N> __device__ __forceinline__ void store_ro
         for (int i = 0; i < 4; ++i) y[i] = w[4 * h + i];
         __builtin_amdgcn_raw_buffer_store_b128(y, row.buf, at + 16u * h, 0, 0);
     }
-    if constexpr (CUTS) {
+}
+template <bool CUTS, typename T, int N> __device__ __forceinline__ void store_row(const Row<T> &row, const Place &p, const float (&v)[N]) {
+    const Words<T, N> w = words_of<T, N>(v);
+    store_at<T, N>(row, p.whole, w);
+    if (CUTS && p.cut_here) {
         const uint32_t from = p.cut * (uint32_t)sizeof(T);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
