@@ -646,43 +646,80 @@ def _refuse(what):
     raise RkError(RK_ERR_INVALID_ARG, what)
 
 
+_TYPES = {}                 # element types by torch dtype, and the dtypes by name; filled with the first tensor
+
+
+def _types():
+    if not _TYPES:
+        import torch
+        _TYPES.update({torch.float32: RK_F32, torch.bfloat16: RK_BF16, torch.float16: RK_F16, "float32": torch.float32,
+                       "int32": torch.int32, "uint8": torch.uint8, "bool": torch.bool})
+    return _TYPES
+
+
 def _type_of(t):
-    import torch
-    types = {torch.float32: RK_F32, torch.bfloat16: RK_BF16, torch.float16: RK_F16}
-    if t.dtype not in types:
-        _refuse(f"{t.dtype} is none of float32, bfloat16, float16")
-    return types[t.dtype]
+    kind = _types().get(t.dtype)
+    return _refuse(f"{t.dtype} is none of float32, bfloat16, float16") if kind is None else kind
 
 
 def _matrix(t, name, shape=None):
     """A [rows, width] tensor, its rows of consecutive elements, as an rk_matrix; the tensor has to outlive the call."""
     if t is None:
         return None
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    size, strides = t.shape, t.stride()
+    if len(size) != 2 or (strides[1] != 1 and size[1] > 1):
         _refuse(f"{name} is no matrix of consecutive row elements")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        _refuse(f"{name} is {tuple(t.shape)}, not {tuple(shape)}")
-    stride = t.stride(0)
-    if t.shape[0] > 1 and stride < t.shape[1]:
-        _refuse(f"the rows of {name} overlap")
-    return rk_matrix(t.data_ptr(), max(stride, t.shape[1]), _type_of(t))
+    if shape is not None and size != shape:
+        _refuse(f"{name} is {tuple(size)}, not {tuple(shape)}")
+    stride, width = strides[0], size[1]
+    if stride < width:
+        if size[0] > 1:
+            _refuse(f"the rows of {name} overlap")
+        stride = width
+    return rk_matrix(t.data_ptr(), stride, _TYPES.get(t.dtype) if t.dtype in _TYPES else _type_of(t))
+
+
+_F32, _I32 = ("float32",), ("int32",)
 
 
 def _plain(t, name, shape, dtypes):
-    """A contiguous tensor of that shape and of one of these types, or None."""
-    if t is not None and (tuple(t.shape) != tuple(shape) or not t.is_contiguous() or str(t.dtype)[6:] not in dtypes):
+    """The address of a contiguous tensor of that shape and of one of these types, or None."""
+    if t is None:
+        return None
+    known = _TYPES or _types()
+    if t.shape != shape or not t.is_contiguous() or (t.dtype != known[dtypes[0]] and t.dtype != known[dtypes[-1]]):
         _refuse(f"{name} is no contiguous {' or '.join(dtypes)} tensor of shape {tuple(shape)}")
-    return _ptr(t)
+    return t.data_ptr()
 
 
-def _same_device(*tensors):
-    devices = {t.device for t in tensors if t is not None}
-    if len(devices) > 1 or any(d.type != "cuda" for d in devices):
-        _refuse("the tensors are not on one GPU")
+def _same_device(first, *others):
+    device = first.get_device()
+    if device < 0:
+        _refuse("the tensors are not on a GPU")
+    for t in others:
+        if t is not None and t.get_device() != device:
+            _refuse("the tensors are not on one GPU")
 
 
 def _ref(s):
     return None if s is None else C.byref(s)
+
+
+_OPERATORS = {
+    "rk_norm_forward": "cbqu" + "m" * 4 + "p", "rk_norm_backward": "cbqu" + "mmp" + "m" * 4 + "g",
+    "rk_route_forward": "crqm" + "p" * 8, "rk_route_backward": "crqm" + "p" * 6 + "m",
+    "rk_distill_loss": "cdqumt" + "ppp", "rk_distill_backward": "cdqumt" + "ppm", "rk_distill_loss_backward": "cdqumt" + "ppppm",
+}
+
+
+def _operator(name):
+    """The library's function, its argument types known (which spares wrapping every number of every call)."""
+    f = getattr(load_library(), name)
+    if f.argtypes is None:
+        kinds = {"c": C.c_void_p, "q": C.c_uint64, "u": C.c_uint32, "p": C.c_void_p, "b": C.POINTER(rk_norm_block), "g": C.POINTER(rk_norm_grads),
+                 "m": C.POINTER(rk_matrix), "r": C.POINTER(rk_router), "d": C.POINTER(rk_distill), "t": C.POINTER(rk_teacher)}
+        f.argtypes = [kinds[k] for k in _OPERATORS[name]]
+    return f
 
 
 class NormBlock:
@@ -696,30 +733,31 @@ class NormBlock:
             _refuse(f"norms are one of {tuple(RK_NORM_KINDS)}")
         self.vectors = {"post_weight": post_weight, "post_bias": post_bias, "pre_weight": pre_weight, "pre_bias": pre_bias}
         self.gate = gate
-        given = [t for t in (*self.vectors.values(), gate) if t is not None]
-        self.width = int(given[0].shape[-1]) if given else None
-        _same_device(*given)
-        if len({t.dtype for t in given}) > 1:
-            _refuse("weights, biases and gate are of one type")
+        self.given = [t for t in (*self.vectors.values(), gate) if t is not None]
+        self.width = int(self.given[0].shape[-1]) if self.given else None
+        if len({(t.dtype, t.device) for t in self.given}) > 1:
+            _refuse("weights, biases and gate are of one type, on one GPU")
         for name, t in self.vectors.items():
             if t is not None and (tuple(t.shape) != (self.width,) or not t.is_contiguous()):
                 _refuse(f"{name} is no contiguous vector of {self.width} elements")
         c_gate = _matrix(gate, "gate")
         if gate is not None and (gate.shape[1] != self.width or (gate_rows == 0 and gate.shape[0] != 1)):
             _refuse("gate is [1, width], or [gates, width] with gate_rows")
+        self.gate_capacity = gate.shape[0] * int(gate_rows) if gate is not None and gate_rows else None
         self.c = rk_norm_block(RK_NORM_KINDS[post], RK_NORM_KINDS[pre], post_eps, pre_eps, res_scale,
-                               _type_of(given[0]) if given else RK_F32,
+                               _type_of(self.given[0]) if self.given else RK_F32,
                                *[None if t is None else t.data_ptr() for t in self.vectors.values()],
                                None if gate is None else gate.data_ptr(), int(gate_rows),
                                c_gate.stride if c_gate is not None else 0)
 
     def _rows(self, t, name):
-        if t.dim() != 2 or (self.width is not None and t.shape[1] != self.width):
+        """The shape of the rows that a call is about."""
+        size = t.shape
+        if len(size) != 2 or (self.width is not None and size[1] != self.width):
             _refuse(f"{name} has no rows of {self.width} elements")
-        rows = int(t.shape[0])
-        if self.gate is not None and self.c.gate_rows and self.gate.shape[0] * self.c.gate_rows < rows:
-            _refuse(f"{self.gate.shape[0]} gates of {self.c.gate_rows} rows for {rows} rows")
-        return rows, int(t.shape[1])
+        if self.gate_capacity is not None and self.gate_capacity < size[0]:
+            _refuse(f"{self.gate.shape[0]} gates of {self.c.gate_rows} rows for {size[0]} rows")
+        return size
 
 
 class NormGrads:
@@ -727,6 +765,7 @@ class NormGrads:
 
     def __init__(self, block: NormBlock, names=None):
         import torch
+        self.block = block
         have = dict(block.vectors, gate=block.gate)
         self.tensors = {n: torch.empty(t.shape, dtype=torch.float32, device=t.device) for n, t in have.items()
                         if t is not None and (names is None or n in names)}
@@ -735,30 +774,24 @@ class NormGrads:
                                block.width or 0)
 
 
-def _block_tensors(block):
-    return (*block.vectors.values(), block.gate)
-
-
 def rk_norm_forward(ctx, block: NormBlock, x, y, x_out, u, stats):
     """y, x_out and u may be None as the header says; stats is [rows, 4] float32."""
-    rows, width = block._rows(x, "x")
-    _same_device(x, y, x_out, u, stats, *_block_tensors(block))
-    m = [_matrix(t, n, (rows, width)) for t, n in ((x, "x"), (y, "y"), (x_out, "x_out"), (u, "u"))]
-    _check(ctx, load_library().rk_norm_forward(ctx, C.byref(block.c), C.c_uint64(rows), C.c_uint32(width), *[_ref(a) for a in m],
-                                               _plain(stats, "stats", (rows, 4), ("float32",))))
+    size = block._rows(x, "x")
+    _same_device(x, y, x_out, u, stats, *block.given[:1])
+    _check(ctx, _operator("rk_norm_forward")(
+        ctx, C.byref(block.c), size[0], size[1], C.byref(_matrix(x, "x")), _ref(_matrix(y, "y", size)), _ref(_matrix(x_out, "x_out", size)),
+        _ref(_matrix(u, "u", size)), _plain(stats, "stats", (size[0], 4), _F32)))
 
 
 def rk_norm_backward(ctx, block: NormBlock, x_out, y, stats, dx_out, du, dx, dy, grads: NormGrads = None):
-    rows, width = block._rows(x_out, "x_out")
-    _same_device(x_out, y, stats, dx_out, du, dx, dy, *_block_tensors(block), *(grads.tensors.values() if grads else ()))
-    for n, t in (grads.tensors if grads else {}).items():
-        have = block.gate if n == "gate" else block.vectors[n]
-        if have is None or have.shape != t.shape:
-            _refuse(f"the gradient of {n} is another block's")
-    m = [_matrix(t, n, (rows, width)) for t, n in ((x_out, "x_out"), (y, "y"), (dx_out, "dx_out"), (du, "du"), (dx, "dx"), (dy, "dy"))]
-    _check(ctx, load_library().rk_norm_backward(ctx, C.byref(block.c), C.c_uint64(rows), C.c_uint32(width), _ref(m[0]), _ref(m[1]),
-                                                _plain(stats, "stats", (rows, 4), ("float32",)), *[_ref(a) for a in m[2:]],
-                                                _ref(grads.c if grads else None)))
+    size = block._rows(x_out, "x_out")
+    _same_device(x_out, y, stats, dx_out, du, dx, dy, *block.given[:1])
+    if grads is not None and grads.block is not block:
+        _refuse("the gradients are another block's")
+    _check(ctx, _operator("rk_norm_backward")(
+        ctx, C.byref(block.c), size[0], size[1], C.byref(_matrix(x_out, "x_out")), _ref(_matrix(y, "y", size)),
+        _plain(stats, "stats", (size[0], 4), _F32), _ref(_matrix(dx_out, "dx_out", size)), _ref(_matrix(du, "du", size)),
+        C.byref(_matrix(dx, "dx", size)), _ref(_matrix(dy, "dy", size)), None if grads is None else C.byref(grads.c)))
 
 
 def make_router(n_experts, top_k, renormalise=True, group_tokens=0) -> rk_router:
@@ -766,86 +799,76 @@ def make_router(n_experts, top_k, renormalise=True, group_tokens=0) -> rk_router
 
 
 def _router_sizes(router, logits):
-    if logits.dim() != 2 or logits.shape[1] != router.n_experts:
+    size = logits.shape
+    if len(size) != 2 or size[1] != router.n_experts:
         _refuse(f"logits are not [tokens, {router.n_experts}]")
-    n = int(logits.shape[0])
-    per = router.group_tokens if 0 < router.group_tokens else max(n, 1)
-    return n, (n + per - 1) // per if router.group_tokens else 1
+    n, per = size[0], router.group_tokens
+    return n, router.top_k, size[1], (n + per - 1) // per if per else 1
 
 
 def rk_route_forward(ctx, router: rk_router, logits, mask, expert, weight, lse, counts, prob_sum, tokens, loss):
     """mask uint8 [tokens] or None; expert int32 and weight float32 [tokens, top_k]; lse [tokens]; counts int32 and prob_sum
     [groups, experts]; tokens int32 [groups]; loss [2]: balance, z."""
-    n, groups = _router_sizes(router, logits)
+    n, k, e, groups = _router_sizes(router, logits)
     _same_device(logits, mask, expert, weight, lse, counts, prob_sum, tokens, loss)
-    k, e = router.top_k, router.n_experts
-    _check(ctx, load_library().rk_route_forward(
-        ctx, C.byref(router), C.c_uint64(n), _ref(_matrix(logits, "logits")), _plain(mask, "mask", (n,), ("uint8", "bool")),
-        _plain(expert, "expert", (n, k), ("int32",)), _plain(weight, "weight", (n, k), ("float32",)),
-        _plain(lse, "lse", (n,), ("float32",)), _plain(counts, "counts", (groups, e), ("int32",)),
-        _plain(prob_sum, "prob_sum", (groups, e), ("float32",)), _plain(tokens, "tokens", (groups,), ("int32",)),
-        _plain(loss, "loss", (2,), ("float32",))))
+    _check(ctx, _operator("rk_route_forward")(
+        ctx, C.byref(router), n, C.byref(_matrix(logits, "logits")), _plain(mask, "mask", (n,), ("uint8", "bool")),
+        _plain(expert, "expert", (n, k), _I32), _plain(weight, "weight", (n, k), _F32), _plain(lse, "lse", (n,), _F32),
+        _plain(counts, "counts", (groups, e), _I32), _plain(prob_sum, "prob_sum", (groups, e), _F32),
+        _plain(tokens, "tokens", (groups,), _I32), _plain(loss, "loss", (2,), _F32)))
 
 
 def rk_route_backward(ctx, router: rk_router, logits, expert, lse, counts, tokens, d_loss, d_weight, d_logits):
-    n, groups = _router_sizes(router, logits)
+    n, k, e, groups = _router_sizes(router, logits)
     _same_device(logits, expert, lse, counts, tokens, d_loss, d_weight, d_logits)
-    k, e = router.top_k, router.n_experts
-    _check(ctx, load_library().rk_route_backward(
-        ctx, C.byref(router), C.c_uint64(n), _ref(_matrix(logits, "logits")), _plain(expert, "expert", (n, k), ("int32",)),
-        _plain(lse, "lse", (n,), ("float32",)), _plain(counts, "counts", (groups, e), ("int32",)),
-        _plain(tokens, "tokens", (groups,), ("int32",)), _plain(d_loss, "d_loss", (2,), ("float32",)),
-        _plain(d_weight, "d_weight", (n, k), ("float32",)), _ref(_matrix(d_logits, "d_logits", (n, e)))))
+    _check(ctx, _operator("rk_route_backward")(
+        ctx, C.byref(router), n, C.byref(_matrix(logits, "logits")), _plain(expert, "expert", (n, k), _I32),
+        _plain(lse, "lse", (n,), _F32), _plain(counts, "counts", (groups, e), _I32), _plain(tokens, "tokens", (groups,), _I32),
+        _plain(d_loss, "d_loss", (2,), _F32), _plain(d_weight, "d_weight", (n, k), _F32),
+        _ref(_matrix(d_logits, "d_logits", (n, e)))))
 
 
 def make_distill(temperature=1.0, kd_weight=1.0, ce_weight=0.0) -> rk_distill:
     return rk_distill(float(temperature), float(kd_weight), float(ce_weight))
 
 
-class _Teacher:
-    """rk_teacher of a call's tensors, checked against the student's rows."""
-
-    def __init__(self, student, logits, index, label, row_weight):
-        if student.dim() != 2:
-            _refuse("student is not [rows, vocab]")
-        self.rows, self.vocab = int(student.shape[0]), int(student.shape[1])
-        _same_device(student, logits, index, label, row_weight)
-        self.student = _matrix(student, "student")
-        if (logits is None) != (index is None):
-            _refuse("the teacher's logits and their indices go together")
-        k = 0 if logits is None else int(logits.shape[-1])
-        self.logits = _matrix(logits, "teacher_logits", (self.rows, k)) if logits is not None else None
-        self.c = rk_teacher(C.cast(C.byref(self.logits), C.c_void_p) if self.logits is not None else None,
-                            _plain(index, "teacher_index", (self.rows, k), ("int32",)), k,
-                            _plain(label, "label", (self.rows,), ("int32",)),
-                            _plain(row_weight, "row_weight", (self.rows,), ("float32",)))
-        self.sizes = (C.c_uint64(self.rows), C.c_uint32(self.vocab), C.byref(self.student), C.byref(self.c))
-
-    def results(self, loss, lse, total):
-        _same_device(loss, lse, total)
-        return (_plain(loss, "loss", (self.rows,), ("float32",)), _plain(lse, "lse", (self.rows, 2), ("float32",)),
-                _plain(total, "total", (1,), ("float32",)))
+def _distill_call(ctx, name, distill, student, teacher_logits, teacher_index, label, row_weight, *rest):
+    size = student.shape
+    if len(size) != 2:
+        _refuse("student is not [rows, vocab]")
+    rows = size[0]
+    if (teacher_logits is None) != (teacher_index is None):
+        _refuse("the teacher's logits and their indices go together")
+    logits, k = None, 0
+    if teacher_logits is not None:
+        k = teacher_logits.shape[-1]
+        logits = _matrix(teacher_logits, "teacher_logits", (rows, k))
+    teacher = rk_teacher(None if logits is None else C.addressof(logits), _plain(teacher_index, "teacher_index", (rows, k), _I32), k,
+                         _plain(label, "label", (rows,), _I32), _plain(row_weight, "row_weight", (rows,), _F32))
+    _check(ctx, _operator(name)(ctx, C.byref(distill), rows, size[1], C.byref(_matrix(student, "student")), C.byref(teacher), *rest))
 
 
 def rk_distill_loss(ctx, distill: rk_distill, student, teacher_logits, teacher_index, label, row_weight, loss, lse, total):
     """teacher_logits [rows, k] with teacher_index int32 (None if kd_weight is 0); label int32 [rows] (None if ce_weight is 0);
     row_weight float32 [rows] or None; loss [rows], lse [rows, 2], total [1], all float32."""
-    t = _Teacher(student, teacher_logits, teacher_index, label, row_weight)
-    _check(ctx, load_library().rk_distill_loss(ctx, C.byref(distill), *t.sizes, *t.results(loss, lse, total)))
+    _same_device(student, teacher_logits, teacher_index, label, row_weight, loss, lse, total)
+    rows = student.shape[0]
+    _distill_call(ctx, "rk_distill_loss", distill, student, teacher_logits, teacher_index, label, row_weight,
+                  _plain(loss, "loss", (rows,), _F32), _plain(lse, "lse", (rows, 2), _F32), _plain(total, "total", (1,), _F32))
 
 
 def rk_distill_backward(ctx, distill: rk_distill, student, teacher_logits, teacher_index, label, row_weight, lse, d_total, d_student):
-    t = _Teacher(student, teacher_logits, teacher_index, label, row_weight)
-    _same_device(student, lse, d_total, d_student)
-    _check(ctx, load_library().rk_distill_backward(
-        ctx, C.byref(distill), *t.sizes, _plain(lse, "lse", (t.rows, 2), ("float32",)), _plain(d_total, "d_total", (1,), ("float32",)),
-        _ref(_matrix(d_student, "d_student", (t.rows, t.vocab)))))
+    _same_device(student, teacher_logits, teacher_index, label, row_weight, lse, d_total, d_student)
+    _distill_call(ctx, "rk_distill_backward", distill, student, teacher_logits, teacher_index, label, row_weight,
+                  _plain(lse, "lse", (student.shape[0], 2), _F32), _plain(d_total, "d_total", (1,), _F32),
+                  _ref(_matrix(d_student, "d_student", student.shape)))
 
 
 def rk_distill_loss_backward(ctx, distill: rk_distill, student, teacher_logits, teacher_index, label, row_weight, d_total, loss, lse,
                              total, d_student):
-    t = _Teacher(student, teacher_logits, teacher_index, label, row_weight)
-    _same_device(student, d_total, loss, d_student)
-    _check(ctx, load_library().rk_distill_loss_backward(
-        ctx, C.byref(distill), *t.sizes, _plain(d_total, "d_total", (1,), ("float32",)), *t.results(loss, lse, total),
-        _ref(_matrix(d_student, "d_student", (t.rows, t.vocab)))))
+    _same_device(student, teacher_logits, teacher_index, label, row_weight, d_total, loss, lse, total, d_student)
+    rows = student.shape[0]
+    _distill_call(ctx, "rk_distill_loss_backward", distill, student, teacher_logits, teacher_index, label, row_weight,
+                  _plain(d_total, "d_total", (1,), _F32), _plain(loss, "loss", (rows,), _F32),
+                  _plain(lse, "lse", (rows, 2), _F32), _plain(total, "total", (1,), _F32),
+                  _ref(_matrix(d_student, "d_student", student.shape)))

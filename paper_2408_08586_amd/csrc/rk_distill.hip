@@ -78,35 +78,44 @@ template <typename T, int SUMS> struct Running {
     }
 };
 
-// Calls f(first, words) for a thread's vectors of [begin, end), four of which are under way at once, and then tail(place) for those
-// behind the last whole round; end is the row's end or a multiple of CH.
-template <int THREADS, typename T, int CH, typename F, typename G>
-__device__ __forceinline__ void stream_row(const Row<T> &row, uint32_t begin, uint32_t end, uint32_t vocab, F f, G tail) {
+// Calls f(first, words) for a thread's vectors of [begin, end), four of which are under way at once, and tail(place, words) for those of
+// the last round; end is the row's end or a multiple of CH.
+template <bool CUTS, int THREADS, typename T, int CH, typename F, typename G>
+__device__ __forceinline__ void stream_row(const Row<T> &row, uint32_t begin, uint32_t end, F f, G tail) {
     constexpr uint32_t U = 4, STEP = THREADS * CH;
-    uint32_t base = begin + threadIdx.x * CH;
-    for (uint32_t round = begin; round + U * STEP <= end; round += U * STEP, base += U * STEP) {
+    uint32_t base = begin + threadIdx.x * CH, round = begin;
+    for (; round + U * STEP <= end; round += U * STEP, base += U * STEP) {
         Words<T, CH> w[U];
 #pragma unroll
         for (uint32_t u = 0; u < U; ++u) w[u] = fetch_at<T, CH>(row, base + u * STEP);
 #pragma unroll
         for (uint32_t u = 0; u < U; ++u) f(base + u * STEP, w[u]);
     }
-    for (; base < end; base += STEP) tail(Place(base, vocab, CH));
+    if (round >= end) return;
+    Words<T, CH> w[U];
+    Place p[U];
+#pragma unroll
+    for (uint32_t u = 0; u < U; ++u) {
+        p[u] = Place(base + u * STEP, end, CH);
+        w[u] = fetch_row<CUTS, T, CH>(row, p[u]);
+    }
+#pragma unroll
+    for (uint32_t u = 0; u < U; ++u)
+        if (round + u * STEP < end) tail(p[u], w[u]);
 }
 template <bool CUTS, int THREADS, typename T, int CH, int SUMS>
-__device__ __forceinline__ void sum_row(const Row<T> &row, uint32_t begin, uint32_t end, uint32_t vocab, const Streams &S, Running<T, SUMS> &R) {
-    stream_row<THREADS, T, CH>(row, begin, end, vocab,
+__device__ __forceinline__ void sum_row(const Row<T> &row, uint32_t begin, uint32_t end, const Streams &S, Running<T, SUMS> &R) {
+    stream_row<CUTS, THREADS, T, CH>(row, begin, end,
         [&](uint32_t, const Words<T, CH> &w) {
             float v[CH];
 #pragma unroll
             for (int i = 0; i < CH; ++i) v[i] = element<T>(w, i);
             R.take(S, v);
         },
-        [&](const Place &p) {
+        [&](const Place &p, const Words<T, CH> &w) {
             float v[CH];
-            load_row<CUTS, T, CH>(row, p, v);
 #pragma unroll
-            for (int i = 0; i < CH; ++i) v[i] = i < p.valid ? v[i] : -INFINITY;
+            for (int i = 0; i < CH; ++i) v[i] = i < p.valid ? element<T>(w, i) : -INFINITY;
             R.take(S, v);
         });
 }
@@ -191,18 +200,17 @@ __device__ __forceinline__ void write_gradient(const DistillArgs &A, const Row<T
         if constexpr (SUMS == TWO) return ca * e + cb * Exp<T>::of(__builtin_fmaf(v, S.kb, -lb));
         return e * (ca + cb * e);
     };
-    stream_row<THREADS, T, CH>(from, begin, end, A.vocab,
+    stream_row<CUTS, THREADS, T, CH>(from, begin, end,
         [&](uint32_t first, const Words<T, CH> &w) {
             float v[CH];
 #pragma unroll
             for (int i = 0; i < CH; ++i) v[i] = slope(element<T>(w, i));
             store_at<T, CH>(to, first, words_of<T, CH>(v));
         },
-        [&](const Place &p) {
+        [&](const Place &p, const Words<T, CH> &w) {
             float v[CH];
-            load_row<CUTS, T, CH>(from, p, v);
 #pragma unroll
-            for (int i = 0; i < CH; ++i) v[i] = slope(v[i]);
+            for (int i = 0; i < CH; ++i) v[i] = slope(element<T>(w, i));
             store_row<CUTS, T, CH>(to, p, v);
         });
     __syncthreads();
@@ -218,9 +226,9 @@ __device__ __forceinline__ void write_gradient(const DistillArgs &A, const Row<T
         if (W.at[n] >= 0) again(W.at[n], W.s[n]);
     if (threadIdx.x == 0 && W.label >= 0) again(W.label, W.label_s);
 }
-template <bool CUTS, int THREADS, typename T, int CH> __device__ __forceinline__ void write_zeros(const Row<T> &to, uint32_t begin, uint32_t end, uint32_t vocab) {
+template <bool CUTS, int THREADS, typename T, int CH> __device__ __forceinline__ void write_zeros(const Row<T> &to, uint32_t begin, uint32_t end) {
     const float zero[CH] = {};
-    for (uint32_t c = begin + threadIdx.x * CH; c < end; c += THREADS * CH) store_row<CUTS, T, CH>(to, Place(c, vocab, CH), zero);
+    for (uint32_t c = begin + threadIdx.x * CH; c < end; c += THREADS * CH) store_row<CUTS, T, CH>(to, Place(c, end, CH), zero);
 }
 
 // a row's loss and log sums from the joined sums; cross: teacher's cross term and sum, the label's logit and whether there is one
@@ -255,14 +263,14 @@ __global__ __launch_bounds__(THREADS) void k_distill_rows(DistillArgs A) {
     const float weight = A.row_weight ? A.row_weight[r] : 1.f;
     if (weight == 0.f) {
         if (threadIdx.x == 0) { A.loss[r] = 0.f; A.lse[2 * r] = 0.f; A.lse[2 * r + 1] = 0.f; }
-        if constexpr (GRAD) write_zeros<CUTS, THREADS, T, CH>(to, 0, A.vocab, A.vocab);
+        if constexpr (GRAD) write_zeros<CUTS, THREADS, T, CH>(to, 0, A.vocab);
         return;
     }
     Wanted<THREADS> W;
     W.template fetch<T>(A, r);
     const Streams S = streams_of<T>(A);
     Running<T, SUMS> R;
-    sum_row<CUTS, THREADS, T, CH, SUMS>(from, 0, A.vocab, A.vocab, S, R);
+    sum_row<CUTS, THREADS, T, CH, SUMS>(from, 0, A.vocab, S, R);
     float4 v = make_float4(R.m, W.top(), -INFINITY, -INFINITY);
     block_all<THREADS / 64, true>(v, red);
     const float top = v.x;
@@ -275,7 +283,7 @@ __global__ __launch_bounds__(THREADS) void k_distill_rows(DistillArgs A) {
     if (threadIdx.x == 0) keep_row(A, r, L);
     if constexpr (GRAD) {
         // (without a kept logit and a label there is no term, whatever the logits hold)
-        if (L.left || (v.z == 0.f && W.label < 0)) write_zeros<CUTS, THREADS, T, CH>(to, 0, A.vocab, A.vocab);
+        if (L.left || (v.z == 0.f && W.label < 0)) write_zeros<CUTS, THREADS, T, CH>(to, 0, A.vocab);
         else write_gradient<CUTS, THREADS, T, CH, SUMS>(A, from, to, (T *)A.d_student + r * A.d_st, 0, A.vocab, S, top, L.la, L.lb, weight, v.z != 0.f, W, v.z, q, at);
     }
 }
@@ -294,7 +302,7 @@ __global__ __launch_bounds__(THREADS) void k_distill_part(DistillArgs A) {
     if (slice == 0) W.template fetch<T>(A, r);
     const Streams S = streams_of<T>(A);
     Running<T, SUMS> R;
-    sum_row<CUTS, THREADS, T, CH, SUMS>(from, begin, end, A.vocab, S, R);
+    sum_row<CUTS, THREADS, T, CH, SUMS>(from, begin, end, S, R);
     float4 v = make_float4(R.m, slice == 0 ? W.top() : -INFINITY, -INFINITY, -INFINITY);
     block_all<THREADS / 64, true>(v, red);
     const float top = v.x;
@@ -350,7 +358,7 @@ __global__ __launch_bounds__(THREADS) void k_distill_gradient(DistillArgs A) {
     const float weight = A.row_weight ? A.row_weight[r] : 1.f;
     const float la = A.lse[2 * r + (A.kd > 0.f ? 0 : 1)], lb = A.lse[2 * r + 1];
     if (weight == 0.f || la == -INFINITY) {
-        write_zeros<CUTS, THREADS, T, CH>(to, begin, end, A.vocab);
+        write_zeros<CUTS, THREADS, T, CH>(to, begin, end);
         return;
     }
     Wanted<THREADS> W;
@@ -365,7 +373,7 @@ __global__ __launch_bounds__(THREADS) void k_distill_gradient(DistillArgs A) {
         sum = v.x;
     }
     if (sum == 0.f && W.label < 0) {
-        write_zeros<CUTS, THREADS, T, CH>(to, begin, end, A.vocab);
+        write_zeros<CUTS, THREADS, T, CH>(to, begin, end);
         return;
     }
     // relative to where the first stream's exponential is one

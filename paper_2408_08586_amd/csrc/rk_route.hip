@@ -1,12 +1,14 @@
 // The router of a mixture of experts: top-k choice and weights, counts per expert, balance and z loss, and the gradient of the
 // logits (rk_route_forward, rk_route_backward).
 #include <cmath>
+#include <initializer_list>
+#include <type_traits>
 
 #include "rk_vec.h"
 
 namespace {
 
-constexpr int RT_THREADS = 256, RT_WAVES = 4;
+constexpr int RT_THREADS = 512, RT_WAVES = RT_THREADS / 64;
 
 struct RouteArgs {
     const void *logits;
@@ -23,21 +25,144 @@ struct RouteArgs {
     uint32_t *part_counts;              // [workgroup][expert]
     float *part_probs;
     float2 *part_z;                     // [workgroup]: tokens, sum of lse^2
-    float4 *group_z;                    // [group]: its balance, sum of lse^2, tokens, 1 if any
+    float4 *tile_z;                     // [group][tile of experts]: sum of counts * prob_sum, sum of lse^2, tokens
+    uint32_t tiles;
     // backward
     void *d_logits;
     uint64_t d_st;
     const float *d_loss, *d_weight;
 };
 
-// A wavefront holds a token's logits, expert e in lane e & 63; a workgroup's tokens belong to one group.
-template <typename T, int VPL>
+// ---- A token's logits lie in L lanes next to each other (8, or the 16 of a DPP row), in vectors of four: vector j + L i is the i-th
+// of lane j.  A wavefront works on 64 / L tokens at once, and what is summed over a token never leaves its row.
+template <int CTRL> __device__ __forceinline__ uint32_t dpp_u(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false);
+}
+// quad_perm 1,0,3,2 and 2,3,0,1; row_half_mirror; row_mirror: after each, twice as many lanes have the same
+template <int L> __device__ __forceinline__ float lanes_sum(float v) {
+    v += dpp_of<0xB1>(v); v += dpp_of<0x4E>(v); v += dpp_of<0x141>(v);
+    if constexpr (L == 16) v += dpp_of<0x140>(v);
+    return v;
+}
+template <int L> __device__ __forceinline__ float lanes_max(float v) {
+    v = fmaxf(v, dpp_of<0xB1>(v)); v = fmaxf(v, dpp_of<0x4E>(v)); v = fmaxf(v, dpp_of<0x141>(v));
+    if constexpr (L == 16) v = fmaxf(v, dpp_of<0x140>(v));
+    return v;
+}
+__device__ __forceinline__ uint32_t max_u(uint32_t a, uint32_t b) { return a > b ? a : b; }
+__device__ __forceinline__ double max_d(double a, double b) {
+    double r;
+    asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));                 // (keys are never NaN)
+    return r;
+}
+template <int CTRL> __device__ __forceinline__ double dpp_d(double v) {
+    const unsigned long long u = (unsigned long long)__double_as_longlong(v);
+    return __longlong_as_double((long long)((unsigned long long)dpp_u<CTRL>((uint32_t)(u >> 32)) << 32 | dpp_u<CTRL>((uint32_t)u)));
+}
+
+// four logits from `first` on; behind the last expert -inf
+template <typename T, bool CUTS> __device__ __forceinline__ void load4(const T *row, uint32_t first, uint32_t n, bool live, float (&v)[4]) {
+    typedef Words<T, 4> Any __attribute__((aligned(sizeof(T))));
+    if (live && first + 4 <= n) {
+        const Words<T, 4> w = *reinterpret_cast<const Any *>(row + first);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = element<T>(w, i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = -INFINITY;
+        if constexpr (CUTS)
+            if (live)
+#pragma unroll
+                for (int i = 0; i < 3; ++i) if (first + i < n) v[i] = (float)row[first + i];
+    }
+}
+template <typename T, bool CUTS> __device__ __forceinline__ void store4(T *row, uint32_t first, uint32_t n, const float (&v)[4]) {
+    typedef Words<T, 4> Any __attribute__((aligned(sizeof(T))));
+    if (first + 4 <= n) {
+        *reinterpret_cast<Any *>(row + first) = words_of<T, 4>(v);
+    } else if constexpr (CUTS) {
+#pragma unroll
+        for (int i = 0; i < 3; ++i) if (first + i < n) row[first + i] = (T)v[i];
+    }
+}
+
+// Logits as keys that differ for every expert, larger for larger logits and, among equal ones, for lower indices: the largest key
+// names the expert.  A 16-bit logit and ten bits of index go into a word; the next key below the last is found by one subtraction
+// each, what lies below it becoming large by wrapping.  A 32-bit logit is a double whose last bits hold the index.
+template <typename T> struct Keys {
+    typedef uint32_t Key;
+    static __device__ __forceinline__ Key of(float l, uint32_t e) {
+        const float v = l + 0.f;                                            // (zeros of both signs are equal)
+        uint32_t u;
+        if constexpr (__is_same(T, __bf16)) u = __float_as_uint(v) >> 16;
+        else u = __builtin_bit_cast(uint16_t, (_Float16)v);
+        u = u & 0x8000u ? ~u & 0xFFFFu : u | 0x8000u;
+        return v > -INFINITY ? u << 10 | (1023u - e) : 0u;
+    }
+    static __device__ __forceinline__ float value(Key k) {
+        uint32_t u = k >> 10;
+        u = u & 0x8000u ? u & 0x7FFFu : ~u & 0xFFFFu;
+        if constexpr (__is_same(T, __bf16)) return __uint_as_float(u << 16);
+        else return (float)__builtin_bit_cast(_Float16, (uint16_t)u);
+    }
+    static __device__ __forceinline__ int32_t expert(Key k) { return k ? (int32_t)(1023u - (k & 1023u)) : -1; }
+    static __device__ __forceinline__ Key none() { return 0u; }
+    static __device__ __forceinline__ Key before() { return 0x7FFFFFFFu; }
+    template <int L, int N> static __device__ __forceinline__ Key next(Key (&key)[N], Key last) {
+        uint32_t c = 0u;
+#pragma unroll
+        for (int i = 0; i < N; ++i) c = max_u(c, key[i] - last);
+        c = max_u(c, dpp_u<0xB1>(c)); c = max_u(c, dpp_u<0x4E>(c)); c = max_u(c, dpp_u<0x141>(c));
+        if constexpr (L == 16) c = max_u(c, dpp_u<0x140>(c));
+        return c >= 0x80000000u ? c + last : 0u;
+    }
+};
+template <> struct Keys<float> {
+    typedef double Key;
+    static __device__ __forceinline__ Key none() { return -1.7e308; }
+    static __device__ __forceinline__ Key before() { return 1.7e308; }
+    static __device__ __forceinline__ Key of(float l, uint32_t e) {
+        const double d = (double)(l + 0.f);
+        unsigned long long u = (unsigned long long)__double_as_longlong(d);
+        if (l == INFINITY) u = 0x7FE0000000000000ull;                       // (above every finite float)
+        u |= l < 0.f ? e : 1023u - e;
+        return l > -INFINITY ? __longlong_as_double((long long)u) : none();
+    }
+    static __device__ __forceinline__ float value(Key k) {
+        const unsigned long long u = (unsigned long long)__double_as_longlong(k);
+        return (u >> 32) == 0x7FE00000ull ? INFINITY : (float)__longlong_as_double((long long)(u & ~1023ull));
+    }
+    static __device__ __forceinline__ int32_t expert(Key k) {
+        const uint32_t low = (uint32_t)__double_as_longlong(k) & 1023u;
+        return k == none() ? -1 : (int32_t)(k < 0.0 ? low : 1023u - low);
+    }
+    template <int L, int N> static __device__ __forceinline__ Key next(Key (&key)[N], Key last) {
+        double c = none();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (key[i] == last) key[i] = none();
+            c = max_d(c, key[i]);
+        }
+        c = max_d(c, dpp_d<0xB1>(c)); c = max_d(c, dpp_d<0x4E>(c)); c = max_d(c, dpp_d<0x141>(c));
+        if constexpr (L == 16) c = max_d(c, dpp_d<0x140>(c));
+        return c;
+    }
+};
+
+// balance of a group from sum counts * prob_sum
+__device__ __forceinline__ float balance_of(uint32_t n_experts, uint32_t top_k, float cp, float n) {
+    return n > 0.f ? (float)n_experts / ((float)top_k * n) * (cp / n) : 0.f;
+}
+
+// A workgroup's tokens belong to one group.  The only workgroup of a call ends it; otherwise k_route_join follows.
+template <typename T, int L, int NV, bool CUTS>
 __global__ __launch_bounds__(RT_THREADS) void k_route_forward(RouteArgs A) {
+    constexpr int SLOTS = 64 / L, V = 4 * NV, KEPT = (int)RK_MAX_TOP_K / L;
     extern __shared__ uint32_t lds[];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, E = A.n_experts, K = A.top_k, j = lane & (L - 1), slot = lane / L;
     uint32_t *const hist = lds;                                 // [n_experts]
-    float *const probs = (float *)(lds + A.n_experts);          // [waves][n_experts]
-    float *const zs = probs + RT_WAVES * A.n_experts;           // [waves][2]
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, E = A.n_experts, K = A.top_k;
+    float *const probs = (float *)(lds + E);                    // [waves * slots][n_experts]
+    float *const zs = probs + RT_WAVES * SLOTS * E;             // [waves][3]
     for (uint32_t e = threadIdx.x; e < E; e += RT_THREADS) hist[e] = 0u;
     __syncthreads();
     const uint64_t g = blockIdx.x / A.per_group;
@@ -45,105 +170,142 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_forward(RouteArgs A) {
     uint64_t t1 = t0 + A.chunk, end = (g + 1) * A.group_tokens;
     end = end < A.n_tokens ? end : A.n_tokens;
     t1 = t1 < end ? t1 : end;
-    float sum[VPL] = {};
+    float sum[V] = {};
     float z = 0.f, n = 0.f;
-    for (uint64_t t = t0 + wave; t < t1; t += RT_WAVES) {
+    for (uint64_t base = t0 + wave * SLOTS; base < t1; base += RT_WAVES * SLOTS) {
+        const uint64_t t = base + slot;
+        const bool live = t < t1;
         const T *const row = (const T *)A.logits + t * A.st;
-        float l[VPL], m = -INFINITY;
+        float l[V], m = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) {
-            const uint32_t e = lane + 64u * i;
-            l[i] = e < E ? (float)row[e] : -INFINITY;
-            m = fmaxf(m, l[i]);
+        for (int i = 0; i < NV; ++i) {
+            float x[4];
+            load4<T, CUTS>(row, (j + L * i) * 4, E, live, x);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) { l[4 * i + q] = x[q]; m = fmaxf(m, x[q]); }
         }
-        m = wave_max(m);
-        const bool there = (!A.mask || A.mask[t]) && m > -INFINITY;
-        float lse = 0.f, mine = 0.f;
-        int32_t chosen = -1;
-        if (there) {
-            float s = 0.f;
+        bool there = live;
+        if (A.mask && live) there = A.mask[t] != 0;
+        m = lanes_max<L>(m);
+        there = there && m > -INFINITY;
+        const float ref = there ? m : 0.f;
+        typename Keys<T>::Key key[V];
+        float s = 0.f;
 #pragma unroll
-            for (int i = 0; i < VPL; ++i) s += exp_f32(l[i] - m);
-            lse = m + logf(wave_sum(s));
+        for (int i = 0; i < V; ++i) {
+            const uint32_t e = (j + L * (i / 4)) * 4 + i % 4;
+            key[i] = there ? Keys<T>::of(l[i], e) : Keys<T>::none();
+            l[i] = there ? exp_f32(l[i] - ref) : 0.f;
+            s += l[i];
+        }
+        s = lanes_sum<L>(s);
+        const float lse = there ? ref + logf(s) : 0.f, inv = there ? 1.f / s : 0.f;
 #pragma unroll
-            for (int i = 0; i < VPL; ++i) sum[i] += exp_f32(l[i] - lse);
-            z += lse * lse; n += 1.f;
-            for (uint32_t k = 0; k < K; ++k) {
-                float best = -INFINITY;
-                uint32_t at = 0xFFFFFFFFu;
+        for (int i = 0; i < V; ++i) sum[i] += l[i] * inv;
+        z += lse * lse; n += there ? 1.f : 0.f;
+        typename Keys<T>::Key last = Keys<T>::before(), mine[KEPT];
 #pragma unroll
-                for (int i = 0; i < VPL; ++i)
-                    if (l[i] > best) { best = l[i]; at = lane + 64u * i; }
-                const float top = wave_max(best);
-                if (!(top > -INFINITY)) break;
-                uint32_t who = best == top ? at : 0xFFFFFFFFu;
-#pragma unroll
-                for (int off = 1; off < 64; off <<= 1) { const uint32_t o = (uint32_t)__shfl_xor((int)who, off, 64); who = o < who ? o : who; }
-#pragma unroll
-                for (int i = 0; i < VPL; ++i)
-                    if (lane + 64u * i == who) l[i] = -INFINITY;
-                if (lane == k) { chosen = (int32_t)who; mine = exp_f32(top - lse); }
-                if (lane == 0) atomicAdd(&hist[who], 1u);
+        for (int h = 0; h < KEPT; ++h) {
+            mine[h] = Keys<T>::none();
+            for (uint32_t k = 0; k < (uint32_t)L && h * L + k < K; ++k) {
+                last = Keys<T>::template next<L, V>(key, last);
+                if (j == k) mine[h] = last;
             }
-            if (A.renorm) mine /= wave_sum(mine);
         }
-        if (lane < K) {
-            A.expert[t * K + lane] = chosen;
-            A.weight[t * K + lane] = chosen < 0 ? 0.f : mine;
+        float w[KEPT], ws = 0.f;
+#pragma unroll
+        for (int h = 0; h < KEPT; ++h) {
+            w[h] = Keys<T>::expert(mine[h]) >= 0 ? exp_f32(Keys<T>::value(mine[h]) - lse) : 0.f;
+            ws += w[h];
         }
-        if (lane == 0) A.lse[t] = lse;
+        const float scale = A.renorm && there ? 1.f / lanes_sum<L>(ws) : 1.f;
+#pragma unroll
+        for (int h = 0; h < KEPT; ++h) {
+            const uint32_t k = h * L + j;
+            const int32_t e = Keys<T>::expert(mine[h]);
+            if (live && k < K) {
+                A.expert[t * K + k] = e;
+                A.weight[t * K + k] = w[h] * scale;
+                if (e >= 0) atomicAdd(&hist[e], 1u);
+            }
+        }
+        if (live && j == 0) A.lse[t] = lse;
     }
 #pragma unroll
-    for (int i = 0; i < VPL; ++i)
-        if (lane + 64u * i < E) probs[wave * E + lane + 64u * i] = sum[i];
-    if (lane == 0) { zs[2 * wave] = n; zs[2 * wave + 1] = z; }
-    __syncthreads();
-    for (uint32_t e = threadIdx.x; e < E; e += RT_THREADS) {
-        A.part_counts[(uint64_t)blockIdx.x * E + e] = hist[e];
-        A.part_probs[(uint64_t)blockIdx.x * E + e] = (probs[e] + probs[E + e]) + (probs[2 * E + e] + probs[3 * E + e]);
+    for (int i = 0; i < V; ++i) {
+        const uint32_t e = (j + L * (i / 4)) * 4 + i % 4;
+        if (e < E) probs[(wave * SLOTS + slot) * E + e] = sum[i];
     }
-    if (threadIdx.x == 0)
-        A.part_z[blockIdx.x] = make_float2((zs[0] + zs[2]) + (zs[4] + zs[6]), (zs[1] + zs[3]) + (zs[5] + zs[7]));
+    z = wave_sum(j == 0 ? z : 0.f); n = wave_sum(j == 0 ? n : 0.f);
+    if (lane == 0) { zs[wave] = n; zs[RT_WAVES + wave] = z; }
+    __syncthreads();
+    const bool only = gridDim.x == 1;
+    float cp = 0.f;
+    for (uint32_t e = threadIdx.x; e < E; e += RT_THREADS) {
+        float p = 0.f;
+        for (int r = 0; r < RT_WAVES * SLOTS; ++r) p += probs[r * E + e];
+        const uint64_t at = only ? e : (uint64_t)blockIdx.x * E + e;
+        (only ? A.counts : A.part_counts)[at] = hist[e];
+        (only ? A.prob_sum : A.part_probs)[at] = p;
+        cp += (float)hist[e] * p;
+    }
+    n = 0.f; z = 0.f;
+#pragma unroll
+    for (int w = 0; w < RT_WAVES; ++w) { n += zs[w]; z += zs[RT_WAVES + w]; }
+    if (!only) {
+        if (threadIdx.x == 0) A.part_z[blockIdx.x] = make_float2(n, z);
+        return;
+    }
+    cp = wave_sum(cp);
+    if (lane == 0) zs[2 * RT_WAVES + wave] = cp;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < RT_WAVES; ++w) cp += zs[2 * RT_WAVES + w];
+    A.tokens[0] = (uint32_t)n;
+    A.loss[0] = balance_of(E, K, cp, n);
+    A.loss[1] = n > 0.f ? z / n : 0.f;
 }
 
-// the workgroups' parts of a group added up in their order, and the group's balance
-__global__ __launch_bounds__(RT_THREADS) void k_route_join(RouteArgs A) {
-    __shared__ float lds[RT_WAVES][3];
-    const uint64_t g = blockIdx.x, first = g * A.per_group;
-    const uint32_t E = A.n_experts, lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    float n = 0.f, z = 0.f, cp = 0.f;
-    for (uint64_t c = threadIdx.x; c < A.per_group; c += RT_THREADS) { n += A.part_z[first + c].x; z += A.part_z[first + c].y; }
-    for (uint32_t e = threadIdx.x; e < E; e += RT_THREADS) {
-        uint32_t count = 0;
-        float p = 0.f;
-        for (uint64_t c = 0; c < A.per_group; ++c) {
+// The workgroups' parts of a group added up in their order: a workgroup has 64 experts, its wavefronts every 16th part.
+constexpr int RT_JOIN = 16;
+__global__ __launch_bounds__(64 * RT_JOIN) void k_route_join(RouteArgs A) {
+    __shared__ float lds_p[RT_JOIN][64], lds_n[RT_JOIN], lds_z[RT_JOIN];
+    __shared__ uint32_t lds_c[RT_JOIN][64];
+    const uint64_t g = blockIdx.x / A.tiles, first = g * A.per_group;
+    const uint32_t E = A.n_experts, lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, e = (blockIdx.x - (uint32_t)g * A.tiles) * 64u + lane;
+    float n = 0.f, z = 0.f, p = 0.f;
+    uint32_t count = 0;
+    for (uint64_t c = threadIdx.x; c < A.per_group; c += 64 * RT_JOIN) { n += A.part_z[first + c].x; z += A.part_z[first + c].y; }
+    if (e < E)
+#pragma unroll 4
+        for (uint64_t c = wave; c < A.per_group; c += RT_JOIN) {
             count += A.part_counts[(first + c) * E + e];
             p += A.part_probs[(first + c) * E + e];
         }
-        A.counts[g * E + e] = count;
-        A.prob_sum[g * E + e] = p;
-        cp += (float)count * p;
-    }
-    n = wave_sum(n); z = wave_sum(z); cp = wave_sum(cp);
-    if (lane == 0) { lds[wave][0] = n; lds[wave][1] = z; lds[wave][2] = cp; }
+    n = wave_sum(n); z = wave_sum(z);
+    if (lane == 0) { lds_n[wave] = n; lds_z[wave] = z; }
+    lds_p[wave][lane] = p; lds_c[wave][lane] = count;
     __syncthreads();
-    if (threadIdx.x) return;
-    n = (lds[0][0] + lds[1][0]) + (lds[2][0] + lds[3][0]);
-    z = (lds[0][1] + lds[1][1]) + (lds[2][1] + lds[3][1]);
-    cp = (lds[0][2] + lds[1][2]) + (lds[2][2] + lds[3][2]);
-    A.tokens[g] = (uint32_t)n;
-    A.group_z[g] = make_float4(n > 0.f ? (float)E / ((float)A.top_k * n) * (cp / n) : 0.f, z, n, n > 0.f ? 1.f : 0.f);
+    if (wave) return;
+    for (int w = 1; w < RT_JOIN; ++w) { n += lds_n[w]; z += lds_z[w]; p += lds_p[w][lane]; count += lds_c[w][lane]; }
+    if (e < E) { A.counts[g * E + e] = count; A.prob_sum[g * E + e] = p; }
+    const float cp = wave_sum(e < E ? (float)count * p : 0.f);
+    if (lane) return;
+    A.tile_z[blockIdx.x] = make_float4(cp, z, n, 0.f);
+    if (e == 0) A.tokens[g] = (uint32_t)n;
 }
 
-__global__ __launch_bounds__(RT_THREADS) void k_route_loss(RouteArgs A) {
-    __shared__ double lds[RT_THREADS][4];
+__global__ __launch_bounds__(256) void k_route_loss(RouteArgs A) {
+    __shared__ double lds[256][4];
     double s[4] = {0.0, 0.0, 0.0, 0.0};
-    for (uint64_t g = threadIdx.x; g < A.n_groups; g += RT_THREADS) {
-        const float4 v = A.group_z[g];
-        s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
+    for (uint64_t g = threadIdx.x; g < A.n_groups; g += 256) {
+        float cp = 0.f;
+        for (uint32_t i = 0; i < A.tiles; ++i) cp += A.tile_z[g * A.tiles + i].x;
+        const float4 v = A.tile_z[g * A.tiles];
+        s[0] += balance_of(A.n_experts, A.top_k, cp, v.z); s[1] += v.y; s[2] += v.z; s[3] += v.z > 0.f ? 1.0 : 0.0;
     }
     for (int i = 0; i < 4; ++i) lds[threadIdx.x][i] = s[i];
-    for (uint32_t off = RT_THREADS / 2; off; off >>= 1) {
+    for (uint32_t off = 128; off; off >>= 1) {
         __syncthreads();
         if (threadIdx.x < off)
             for (int i = 0; i < 4; ++i) lds[threadIdx.x][i] += lds[threadIdx.x + off][i];
@@ -153,94 +315,138 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_loss(RouteArgs A) {
     A.loss[1] = lds[0][2] > 0.0 ? (float)(lds[0][1] / lds[0][2]) : 0.f;
 }
 
-// d l = p (A - sum A p + d_z 2 lse / n) (+ what comes through renormalised weights), a wavefront a token
-template <typename T, int VPL>
+// d l = p (A - sum A p - sum y + d_z 2 lse / n) + y at the chosen experts, where y = p d weight, or, of renormalised weights,
+// w (d weight - sum w d weight), and then not in the sum.  y reaches its experts' lanes over LDS: zeros but for what a
+// token's lanes put there and take away again; the tokens of a wavefront use places of their own, in program order.
+template <typename T, int L, int NV, bool CUTS>
 __global__ __launch_bounds__(RT_THREADS) void k_route_backward(RouteArgs A) {
-    __shared__ float lds[RT_WAVES][2];
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, E = A.n_experts, K = A.top_k;
+    constexpr int SLOTS = 64 / L, KEPT = (int)RK_MAX_TOP_K / L;
+    extern __shared__ float4 lds4[];
+    __shared__ float red[RT_WAVES][2];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, E = A.n_experts, K = A.top_k, j = lane & (L - 1), slot = lane / L;
+    float *const y = (float *)lds4 + (wave * SLOTS + slot) * (L * NV * 4);
+    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) ((float4 *)y)[j + L * i] = zero;
     float n = 0.f, some = 0.f;
     for (uint64_t g = threadIdx.x; g < A.n_groups; g += RT_THREADS) {
         const uint32_t c = A.tokens[g];
         n += (float)c; some += c ? 1.f : 0.f;
     }
     n = wave_sum(n); some = wave_sum(some);
-    if (lane == 0) { lds[wave][0] = n; lds[wave][1] = some; }
+    if (lane == 0) { red[wave][0] = n; red[wave][1] = some; }
     __syncthreads();
-    n = (lds[0][0] + lds[1][0]) + (lds[2][0] + lds[3][0]);
-    some = (lds[0][1] + lds[1][1]) + (lds[2][1] + lds[3][1]);
+    n = 0.f; some = 0.f;
+#pragma unroll
+    for (int w = 0; w < RT_WAVES; ++w) { n += red[w][0]; some += red[w][1]; }
     const float bal = some > 0.f ? A.d_loss[0] * (float)E / ((float)K * some) : 0.f;
     const float dz = n > 0.f ? A.d_loss[1] * 2.f / n : 0.f;
-    uint64_t t0 = ((uint64_t)blockIdx.x * RT_WAVES + wave) * A.chunk, t1 = t0 + A.chunk, of = ~0ull;
-    t1 = t1 < A.n_tokens ? t1 : A.n_tokens;
-    float a[VPL] = {};
-    for (uint64_t t = t0; t < t1; ++t) {
-        const uint64_t g = t / A.group_tokens;
-        if (g != of) {
-            of = g;
-            const float c = (float)A.tokens[g];
-            const float s = c > 0.f ? bal / c / c : 0.f;
+    const uint64_t t0 = (uint64_t)blockIdx.x * A.chunk;
+    const uint64_t t1 = t0 + A.chunk < A.n_tokens ? t0 + A.chunk : A.n_tokens;
+    uint64_t g_end = 0;                                     // first token behind the group that `a` is of
+    float a[4 * NV] = {};
+    for (uint64_t base = t0 + wave * SLOTS; base < t1; base += RT_WAVES * SLOTS) {
+        const uint64_t t = base + slot;
+        const bool live = t < t1;
+        if (live && t >= g_end) {
+            const uint64_t g = t / A.group_tokens;
+            g_end = (g + 1) * A.group_tokens;
+            const float c = (float)A.tokens[g], s = c > 0.f ? bal / c / c : 0.f;
 #pragma unroll
-            for (int i = 0; i < VPL; ++i)
-                if (lane + 64u * i < E) a[i] = s * (float)A.counts[g * E + lane + 64u * i];
+            for (int i = 0; i < 4 * NV; ++i) {
+                const uint32_t e = (j + L * (i / 4)) * 4 + i % 4;
+                a[i] = e < E ? s * (float)A.counts[g * E + e] : 0.f;
+            }
         }
-        const int32_t mine = lane < K ? A.expert[t * K + lane] : -1;
-        const bool there = __builtin_amdgcn_readfirstlane(mine) >= 0;
+        const T *const row = (const T *)A.logits + t * A.st;
         T *const out = (T *)A.d_logits + t * A.d_st;
-        float d[VPL];
-        if (there) {
-            const T *const row = (const T *)A.logits + t * A.st;
-            const float lse = A.lse[t];
-            float p[VPL], x[VPL] = {}, w[VPL] = {};
+        int32_t e[KEPT];
+        float dw[KEPT];
 #pragma unroll
-            for (int i = 0; i < VPL; ++i) p[i] = lane + 64u * i < E ? exp_f32((float)row[lane + 64u * i] - lse) : 0.f;
-            if (A.d_weight) {
-                const float dw = lane < K && mine >= 0 ? A.d_weight[t * K + lane] : 0.f;
-                for (uint32_t k = 0; k < K; ++k) {
-                    const int32_t e = __builtin_amdgcn_readlane(mine, k);
-                    const float v = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(dw), k));
-#pragma unroll
-                    for (int i = 0; i < VPL; ++i)
-                        if ((int32_t)(lane + 64u * i) == e) { x[i] = v; w[i] = p[i]; }
-                }
-            }
-            float s = 0.f, ws = 0.f, wx = 0.f;
-#pragma unroll
-            for (int i = 0; i < VPL; ++i) {
-                s += (A.renorm ? a[i] : a[i] + x[i]) * p[i];
-                ws += w[i]; wx += w[i] * x[i];
-            }
-            s = wave_sum(s);
-            if (A.renorm && A.d_weight) {
-                ws = wave_sum(ws); wx = wave_sum(wx) / ws;
-            }
-#pragma unroll
-            for (int i = 0; i < VPL; ++i) {
-                d[i] = p[i] * ((A.renorm ? a[i] : a[i] + x[i]) - s + dz * lse);
-                if (A.renorm && A.d_weight && w[i] != 0.f) d[i] += w[i] / ws * (x[i] - wx);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < VPL; ++i) d[i] = 0.f;
+        for (int h = 0; h < KEPT; ++h) {
+            const uint32_t k = h * L + j;
+            const bool on = live && k < K;
+            e[h] = on ? A.expert[t * K + k] : -1;
+            e[h] = (uint32_t)e[h] < E ? e[h] : -1;
+            dw[h] = on && A.d_weight ? A.d_weight[t * K + k] : 0.f;
         }
+        float p[4 * NV];
 #pragma unroll
-        for (int i = 0; i < VPL; ++i)
-            if (lane + 64u * i < E) out[lane + 64u * i] = (T)d[i];
+        for (int i = 0; i < NV; ++i) {
+            float x[4];
+            load4<T, CUTS>(row, (j + L * i) * 4, E, live, x);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) p[4 * i + q] = x[q];
+        }
+        const float lse = live ? A.lse[t] : 0.f;
+        // a token that counts has its first choice
+        const bool there = __shfl(e[0], lane & ~(L - 1), 64) >= 0;
+        float yk[KEPT], ws = 0.f, wd = 0.f;
+        if (A.d_weight) {
+#pragma unroll
+            for (int h = 0; h < KEPT; ++h) {
+                yk[h] = e[h] >= 0 ? exp_f32((float)row[e[h]] - lse) : 0.f;
+                ws += yk[h]; wd += e[h] >= 0 ? yk[h] * dw[h] : 0.f;
+            }
+            ws = lanes_sum<L>(ws); wd = lanes_sum<L>(wd);
+#pragma unroll
+            for (int h = 0; h < KEPT; ++h) {
+                yk[h] = A.renorm ? yk[h] / ws * (dw[h] - wd / ws) : yk[h] * dw[h];
+                if (e[h] >= 0) y[e[h]] = yk[h];
+            }
+        }
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4 * NV; ++i) {
+            p[i] = there ? exp_f32(p[i] - lse) : 0.f;
+            s += a[i] * p[i];
+        }
+        s = lanes_sum<L>(s) + (A.renorm ? 0.f : wd) - dz * lse;
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float4 add = zero;
+            if (A.d_weight) add = ((const float4 *)y)[j + L * i];
+            float d[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float v = q == 0 ? add.x : q == 1 ? add.y : q == 2 ? add.z : add.w;
+                d[q] = there ? p[4 * i + q] * (a[4 * i + q] - s) + v : 0.f;
+            }
+            if (live) store4<T, CUTS>(out, (j + L * i) * 4, E, d);
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (A.d_weight)
+#pragma unroll
+            for (int h = 0; h < KEPT; ++h) if (e[h] >= 0) y[e[h]] = 0.f;
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
 // ---- host
+// f(type, lanes of a token, vectors of a lane, whether four divide the experts)
 template <typename F> void with_lanes(uint32_t type, uint32_t n_experts, F f) {
+    auto cut = [&](auto t, auto l, auto v) {
+        if (n_experts % 4) f(t, l, v, std::true_type()); else f(t, l, v, std::false_type());
+    };
     auto sized = [&](auto t) {
-        if (n_experts <= 64) f(t, std::integral_constant<int, 1>());
-        else if (n_experts <= 128) f(t, std::integral_constant<int, 2>());
-        else if (n_experts <= 256) f(t, std::integral_constant<int, 4>());
-        else if (n_experts <= 512) f(t, std::integral_constant<int, 8>());
-        else f(t, std::integral_constant<int, 16>());
+        const auto L8 = std::integral_constant<int, 8>();
+        const auto L16 = std::integral_constant<int, 16>();
+        if (n_experts <= 32) cut(t, L8, std::integral_constant<int, 1>());
+        else if (n_experts <= 64) cut(t, L8, std::integral_constant<int, 2>());
+        else if (n_experts <= 128) cut(t, L16, std::integral_constant<int, 2>());
+        else if (n_experts <= 192) cut(t, L16, std::integral_constant<int, 3>());
+        else if (n_experts <= 256) cut(t, L16, std::integral_constant<int, 4>());
+        else if (n_experts <= 512) cut(t, L16, std::integral_constant<int, 8>());
+        else cut(t, L16, std::integral_constant<int, 16>());
     };
     if (type == RK_F32) sized(float());
     else if (type == RK_BF16) sized(__bf16());
     else sized(_Float16());
 }
+uint32_t lanes_of(uint32_t n_experts) { return n_experts <= 64 ? 8 : 16; }
 
 int32_t check_router(rk_ctx *ctx, const rk_router *r, uint64_t n_tokens, const rk_matrix *logits) {
     if (!r) return rk_fail(ctx, RK_ERR_INVALID_ARG, "router is null");
@@ -279,28 +485,37 @@ extern "C" int32_t rk_route_forward(rk_ctx *ctx, const rk_router *router, uint64
         return rk_fail(ctx, RK_ERR_INVALID_ARG, "an output is null or misaligned");
     RK_HIP(ctx, hipSetDevice(ctx->device));
     A.mask = mask; A.expert = expert; A.weight = weight; A.lse = lse; A.counts = counts; A.prob_sum = prob_sum; A.tokens = tokens; A.loss = loss;
-    // four workgroups a compute unit share the tokens, eight tokens each at least
-    uint64_t chunk = (n_tokens + 1023) / 1024;
-    if (chunk < 8) chunk = 8;
+    // two workgroups a compute unit share the tokens, each at least as many as its wavefronts hold at once; few tokens are one's
+    const uint64_t at_once = RT_WAVES * 64 / lanes_of(A.n_experts);
+    uint64_t chunk = (n_tokens + 511) / 512;
+    if (chunk < at_once) chunk = at_once;
     A.per_group = n_tokens ? (A.group_tokens + chunk - 1) / chunk : 0;
     A.chunk = A.per_group ? (A.group_tokens + A.per_group - 1) / A.per_group : 0;
+    A.tiles = (A.n_experts + 63) / 64;
     const uint64_t blocks = A.per_group * (n_tokens ? A.n_groups : 0);
-    if ((rc = rk_scratch(ctx, SL_ROUTE_COUNTS, blocks * A.n_experts * 4, (void **)&A.part_counts)) != RK_OK) return rc;
-    if ((rc = rk_scratch(ctx, SL_ROUTE_PROBS, blocks * A.n_experts * 4, (void **)&A.part_probs)) != RK_OK) return rc;
-    if ((rc = rk_scratch(ctx, SL_ROUTE_Z, blocks * 8, (void **)&A.part_z)) != RK_OK) return rc;
-    if ((rc = rk_scratch(ctx, SL_ROUTE_GROUPS, A.n_groups * 16, (void **)&A.group_z)) != RK_OK) return rc;
+    if (blocks != 1) {
+        if ((rc = rk_scratch(ctx, SL_ROUTE_COUNTS, blocks * A.n_experts * 4, (void **)&A.part_counts)) != RK_OK) return rc;
+        if ((rc = rk_scratch(ctx, SL_ROUTE_PROBS, blocks * A.n_experts * 4, (void **)&A.part_probs)) != RK_OK) return rc;
+        if ((rc = rk_scratch(ctx, SL_ROUTE_Z, blocks * 8, (void **)&A.part_z)) != RK_OK) return rc;
+        if ((rc = rk_scratch(ctx, SL_ROUTE_GROUPS, A.n_groups * A.tiles * 16, (void **)&A.tile_z)) != RK_OK) return rc;
+    }
     if (blocks) {
-        const size_t lds = (size_t)A.n_experts * 4 * (1 + RT_WAVES) + RT_WAVES * 8;
-        with_lanes(logits->type, A.n_experts, [&](auto t, auto v) {
-            k_route_forward<decltype(t), decltype(v)::value><<<(uint32_t)blocks, RT_THREADS, lds, ctx->stream>>>(A);
+        const size_t lds = (size_t)A.n_experts * 4 * (1 + at_once) + RT_WAVES * 12;
+        with_lanes(logits->type, A.n_experts, [&](auto t, auto l, auto v, auto c) {
+            const auto kernel = k_route_forward<decltype(t), decltype(l)::value, decltype(v)::value, decltype(c)::value>;
+            if (lds > 65536)
+                rc = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess ? RK_OK : RK_ERR_DEVICE;
+            if (rc == RK_OK) kernel<<<(uint32_t)blocks, RT_THREADS, lds, ctx->stream>>>(A);
         });
+        if (rc != RK_OK) return rk_fail(ctx, rc, "k_route_forward: no room in LDS");
         RK_CHECK_LAUNCH(ctx, "k_route_forward");
+        if (blocks == 1) return RK_OK;
     }
     if (A.n_groups) {
-        k_route_join<<<(uint32_t)A.n_groups, RT_THREADS, 0, ctx->stream>>>(A);
+        k_route_join<<<(uint32_t)(A.n_groups * A.tiles), 64 * RT_JOIN, 0, ctx->stream>>>(A);
         RK_CHECK_LAUNCH(ctx, "k_route_join");
     }
-    k_route_loss<<<1, RT_THREADS, 0, ctx->stream>>>(A);
+    k_route_loss<<<1, 256, 0, ctx->stream>>>(A);
     RK_CHECK_LAUNCH(ctx, "k_route_loss");
     return RK_OK;
 }
@@ -322,11 +537,20 @@ extern "C" int32_t rk_route_backward(rk_ctx *ctx, const rk_router *router, uint6
     A.expert = const_cast<int32_t *>(expert); A.lse = const_cast<float *>(lse); A.counts = const_cast<uint32_t *>(counts);
     A.tokens = const_cast<uint32_t *>(tokens);
     A.d_loss = d_loss; A.d_weight = d_weight; A.d_logits = d_logits->data; A.d_st = d_logits->stride;
-    A.chunk = (n_tokens + 8191) / 8192;                     // tokens of a wavefront
-    const uint64_t blocks = (n_tokens + A.chunk * RT_WAVES - 1) / (A.chunk * RT_WAVES);
-    with_lanes(logits->type, A.n_experts, [&](auto t, auto v) {
-        k_route_backward<decltype(t), decltype(v)::value><<<(uint32_t)blocks, RT_THREADS, 0, ctx->stream>>>(A);
+    // four workgroups a compute unit, each at least as many tokens as its wavefronts hold at once
+    const uint64_t at_once = RT_WAVES * 64 / lanes_of(A.n_experts);
+    A.chunk = (n_tokens + 1023) / 1024;
+    A.chunk = (A.chunk + at_once - 1) / at_once * at_once;
+    const uint64_t blocks = (n_tokens + A.chunk - 1) / A.chunk;
+    with_lanes(logits->type, A.n_experts, [&](auto t, auto l, auto v, auto c) {
+        constexpr int L = decltype(l)::value, NV = decltype(v)::value;
+        const size_t lds = (size_t)RT_WAVES * 64 * NV * 16;
+        const auto kernel = k_route_backward<decltype(t), L, NV, decltype(c)::value>;
+        if (lds > 65536 - 1024)
+            rc = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess ? RK_OK : RK_ERR_DEVICE;
+        if (rc == RK_OK) kernel<<<(uint32_t)blocks, RT_THREADS, lds, ctx->stream>>>(A);
     });
+    if (rc != RK_OK) return rk_fail(ctx, rc, "k_route_backward: no room in LDS");
     RK_CHECK_LAUNCH(ctx, "k_route_backward");
     return RK_OK;
 }
