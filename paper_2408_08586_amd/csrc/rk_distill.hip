@@ -33,9 +33,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // streams otherwise, of which the second is the first's square if T = 2.
 enum { ONE, TWO, SQUARE };
 
-// What is not positive is taken off first, in the logits' own units: masks of the type's lowest value stay finite.  A 16-bit student's
-// exponentials are then one product and one instruction to base 2: the exponent's rounding, 2^-24 of it, is far below a step of the
-// logits.  A 32-bit student's have the argument's lower part (exp_f32).
+// A 16-bit student's are taken to base 2, e^(x/T - r) = 2^(x log2(e)/T - r'): one fused product and one instruction, whose exponent's
+// rounding, 2^-24 of it, is far below a step of the logits.  Rows whose largest logit is beyond HUGE_LOGIT (all of them masked by the
+// type's lowest value) would overflow there, and a 32-bit student wants its exponents closer: these take differences of logits first.
+constexpr float HUGE_LOGIT = 1e30f;
 template <typename T> struct Exp {
     static constexpr bool EXACT = sizeof(T) == 4;
     static __device__ __forceinline__ float of(float x) { return EXACT ? exp_f32(x) : __builtin_amdgcn_exp2f(x); }
@@ -43,51 +44,58 @@ template <typename T> struct Exp {
     static __device__ __forceinline__ float unit() { return EXACT ? 1.f : 1.4426950408889634f; }
     static __device__ __forceinline__ float natural(float x) { return EXACT ? x : x * 0.6931471805599453f; }
 };
-struct Streams { float ka, kb, inv_a; };        // what a difference of logits is multiplied by; the first without the base
+struct Streams { float ka, kb, inv_a; };        // what a logit is multiplied by; the first without the base
 template <typename T> __device__ __forceinline__ Streams streams_of(const DistillArgs &A) {
     const float inv = A.kd > 0.f ? 1.f / A.temperature : 1.f;
     return Streams{inv * Exp<T>::unit(), Exp<T>::unit(), inv};
 }
+__device__ __forceinline__ bool is_huge(float top) { return fabsf(top) > HUGE_LOGIT && top != -INFINITY; }
 
 // the sums of a stretch of logits, relative to the largest of them seen so far
 template <typename T, int SUMS> struct Running {
-    float m = -INFINITY, ref = 0.f, sa = 0.f, sb = 0.f;         // (nothing above -inf yet: relative to 0)
-    __device__ __forceinline__ void to(const Streams &S, float by) {
-        const float f = Exp<T>::of(by * S.ka);
-        sa *= f;
-        if constexpr (SUMS == TWO) sb *= Exp<T>::of(by * S.kb);
-        if constexpr (SUMS == SQUARE) sb *= f * f;
+    float m = -INFINITY, ref = 0.f, ra = 0.f, rb = 0.f, sa = 0.f, sb = 0.f;     // (nothing above -inf yet: relative to 0)
+    __device__ __forceinline__ void rebase(const Streams &S, float top) {
+        const float r = fminf(fmaxf(top, -HUGE_LOGIT), HUGE_LOGIT);             // (of a row that is not huge, one of its huge parts: its sums are zero)
+        if (m != -INFINITY) {
+            const float f = Exp<T>::of((ref - r) * S.ka);
+            sa *= f;
+            if constexpr (SUMS == TWO) sb *= Exp<T>::of((ref - r) * S.kb);
+            if constexpr (SUMS == SQUARE) sb *= f * f;
+        }
+        ref = r; ra = r * S.ka; rb = r * S.kb;
+    }
+    __device__ __forceinline__ void add(const Streams &S, float x) {
+        const float d = x - ref;
+        const float e = Exp<T>::of(Exp<T>::EXACT ? d * S.ka : __builtin_fmaf(x, S.ka, -ra));
+        sa += e;
+        if constexpr (SUMS == TWO) sb += Exp<T>::of(Exp<T>::EXACT ? d * S.kb : __builtin_fmaf(x, S.kb, -rb));
+        if constexpr (SUMS == SQUARE) sb += e * e;
     }
     template <int CH> __device__ __forceinline__ void take(const Streams &S, const float (&v)[CH]) {
         float top = v[0];
 #pragma unroll
         for (int i = 1; i + 1 < CH; i += 2) top = max3(top, v[i], v[i + 1]);
         top = max3(top, v[CH - 1], m);
-        if (top > m) { to(S, m - top); m = top; ref = top; }
+        if (top > m) { rebase(S, top); m = top; }
 #pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            const float d = v[i] - ref, e = Exp<T>::of(d * S.ka);
-            sa += e;
-            if constexpr (SUMS == TWO) sb += Exp<T>::of(d * S.kb);
-            if constexpr (SUMS == SQUARE) sb += e * e;
-        }
+        for (int i = 0; i < CH; ++i) add(S, v[i]);
     }
-    // relative to another largest one
+    // relative to the largest of all; a thread that saw nothing has zeros
     __device__ __forceinline__ void move(const Streams &S, float top) {
-        if (m != -INFINITY) to(S, m - top);
+        if (m != -INFINITY) rebase(S, top);
     }
 };
 
 // Calls f(first, words) for a thread's vectors of [begin, end), four of which are under way at once, and tail(place, words) for those of
 // the last round; end is the row's end or a multiple of CH.
-template <bool CUTS, int THREADS, typename T, int CH, typename F, typename G>
+template <bool CUTS, int THREADS, typename T, int CH, int HINT, typename F, typename G>
 __device__ __forceinline__ void stream_row(const Row<T> &row, uint32_t begin, uint32_t end, F f, G tail) {
     constexpr uint32_t U = 4, STEP = THREADS * CH;
     uint32_t base = begin + threadIdx.x * CH, round = begin;
     for (; round + U * STEP <= end; round += U * STEP, base += U * STEP) {
         Words<T, CH> w[U];
 #pragma unroll
-        for (uint32_t u = 0; u < U; ++u) w[u] = fetch_at<T, CH>(row, base + u * STEP);
+        for (uint32_t u = 0; u < U; ++u) w[u] = fetch_at<T, CH, HINT>(row, base + u * STEP);
 #pragma unroll
         for (uint32_t u = 0; u < U; ++u) f(base + u * STEP, w[u]);
     }
@@ -97,7 +105,7 @@ __device__ __forceinline__ void stream_row(const Row<T> &row, uint32_t begin, ui
 #pragma unroll
     for (uint32_t u = 0; u < U; ++u) {
         p[u] = Place(base + u * STEP, end, CH);
-        w[u] = fetch_row<CUTS, T, CH>(row, p[u]);
+        w[u] = fetch_row<CUTS, T, CH, HINT>(row, p[u]);
     }
 #pragma unroll
     for (uint32_t u = 0; u < U; ++u)
@@ -105,7 +113,7 @@ __device__ __forceinline__ void stream_row(const Row<T> &row, uint32_t begin, ui
 }
 template <bool CUTS, int THREADS, typename T, int CH, int SUMS>
 __device__ __forceinline__ void sum_row(const Row<T> &row, uint32_t begin, uint32_t end, const Streams &S, Running<T, SUMS> &R) {
-    stream_row<CUTS, THREADS, T, CH>(row, begin, end,
+    stream_row<CUTS, THREADS, T, CH, KEEP>(row, begin, end,
         [&](uint32_t, const Words<T, CH> &w) {
             float v[CH];
 #pragma unroll
@@ -120,28 +128,53 @@ __device__ __forceinline__ void sum_row(const Row<T> &row, uint32_t begin, uint3
         });
 }
 
-// What a row's teacher and label say: a thread holds kept logits tid, tid + THREADS, ..., fetched before the row's logits.
+// the same of a stretch whose largest logit is huge, in differences from it
+template <bool CUTS, int THREADS, typename T, int CH, int SUMS>
+__device__ __forceinline__ void sum_huge(const Row<T> &row, uint32_t begin, uint32_t end, const Streams &S, float top, Running<T, SUMS> &R) {
+    R.sa = 0.f; R.sb = 0.f;
+    for (uint32_t c = begin + threadIdx.x * CH; c < end; c += THREADS * CH) {
+        const Place p(c, end, CH);
+        float v[CH];
+        load_row<CUTS, T, CH>(row, p, v);
+        for (int i = 0; i < CH; ++i) {
+            if (i >= p.valid) continue;
+            const float d = v[i] - top, e = Exp<T>::of(d * S.ka);
+            R.sa += e;
+            if constexpr (SUMS == TWO) R.sb += Exp<T>::of(d * S.kb);
+            if constexpr (SUMS == SQUARE) R.sb += e * e;
+        }
+    }
+}
+
+// What a row's teacher and label say: a thread holds kept logits tid, tid + THREADS, ...
 template <int THREADS> struct Wanted {
     static constexpr int N = (int)RK_MAX_TEACHER_LOGITS / THREADS;
     int32_t at[N], label;
     float t[N], s[N], label_s;
-    template <typename T> __device__ __forceinline__ void fetch(const DistillArgs &A, uint64_t r) {
-        const T *const row = (const T *)A.student + r * A.st;
+    // what teacher and label name; then, when that is there, the student's logits at their places.  Loads return in their order: what is
+    // asked for between the two calls does not wait for the first, nor the second's answers hold it up.
+    __device__ __forceinline__ void ask(const DistillArgs &A, uint64_t r) {
         label = A.ce > 0.f ? A.label[r] : -1;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const uint32_t k = threadIdx.x + n * THREADS;
+            at[n] = -1; t[n] = -INFINITY;
+            if (A.kd > 0.f && k < A.top_k) {
+                const uint64_t p = r * A.t_st + k;
+                at[n] = A.index[r * A.top_k + k];
+                t[n] = A.t_type == RK_F32 ? ((const float *)A.teacher)[p] : A.t_type == RK_BF16 ? (float)((const __bf16 *)A.teacher)[p] : (float)((const _Float16 *)A.teacher)[p];
+            }
+        }
+    }
+    template <typename T> __device__ __forceinline__ void look(const DistillArgs &A, uint64_t r) {
+        const T *const row = (const T *)A.student + r * A.st;
         if ((uint32_t)label >= A.vocab) label = -1;
         label_s = label >= 0 ? (float)row[label] : 0.f;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const uint32_t k = threadIdx.x + n * THREADS;
-            at[n] = -1; t[n] = -INFINITY; s[n] = 0.f;
-            if (A.kd > 0.f && k < A.top_k) {
-                const int32_t i = A.index[r * A.top_k + k];
-                const uint64_t p = r * A.t_st + k;
-                t[n] = A.t_type == RK_F32 ? ((const float *)A.teacher)[p] : A.t_type == RK_BF16 ? (float)((const __bf16 *)A.teacher)[p] : (float)((const _Float16 *)A.teacher)[p];
-                at[n] = (uint32_t)i < A.vocab && t[n] != -INFINITY ? i : -1;
-                if (at[n] >= 0) s[n] = (float)row[i];
-                else t[n] = -INFINITY;
-            }
+            at[n] = (uint32_t)at[n] < A.vocab && t[n] != -INFINITY ? at[n] : -1;
+            if (at[n] < 0) t[n] = -INFINITY;
+            s[n] = at[n] >= 0 ? (float)row[at[n]] : 0.f;
         }
     }
     __device__ __forceinline__ float top() const {
@@ -150,7 +183,7 @@ template <int THREADS> struct Wanted {
         for (int n = 1; n < N; ++n) m = fmaxf(m, t[n]);
         return m;
     }
-    // t becomes e^((t - top) / T); sum and cross are the thread's parts of sum e and sum e ((t - s - top) / T)
+    // t becomes e^((t - top) / T) (0 where nothing is kept); sum and cross are the thread's parts of sum e and sum e ((t - s - top) / T)
     __device__ __forceinline__ void weigh(const DistillArgs &A, float top, float &sum, float &cross) {
         const float inv = 1.f / A.temperature;
         sum = 0.f; cross = 0.f;
@@ -178,57 +211,105 @@ template <int WAVES, bool MAX> __device__ __forceinline__ void block_all(float4 
     v = make_float4(row(o.x), row(o.y), row(o.z), row(o.w));
 }
 
-// d s of [begin, end) of a row: its streams' exponentials are e^(k (s - top) - l), in the streams' units
-template <bool CUTS, int THREADS, typename T, int CH, int SUMS>
-__device__ __forceinline__ void write_gradient(const DistillArgs &A, const Row<T> &from, const Row<T> &to, T *out, uint32_t begin, uint32_t end, const Streams &S,
-                                               float top, float la, float lb, float weight, bool kept, Wanted<THREADS> &W, float t_sum, float *q, int32_t *at) {
-    const float scale = weight * (A.d_total ? A.d_total[0] : 1.f);
-    const float ft = kept ? scale * A.kd * A.temperature : 0.f, f1 = W.label >= 0 ? scale * A.ce : 0.f;
-    // (a stream that both terms share, or that is the only term's)
-    const float ca = SUMS == ONE ? ft + f1 : ft, cb = SUMS == SQUARE ? f1 * Exp<T>::of(la + la - lb) : f1;
+// d s of a logit: the streams' exponentials are e^(k (s - top) - l), in the streams' units
+template <typename T, int SUMS> struct Slope {
+    float ka, kb, top, la, lb, ba, bb, ca, cb;
+    float ft, f1;                       // of a kept logit's share, of the label
+    __device__ __forceinline__ Slope(const DistillArgs &A, const Streams &S, float top_, float la_, float lb_, float weight, bool kept, bool labelled)
+        : ka(S.ka), kb(S.kb), top(top_), la(la_), lb(lb_), ba(top_ * S.ka + la_), bb(top_ * S.kb + lb_) {
+        const float scale = weight * (A.d_total ? A.d_total[0] : 1.f);
+        ft = kept ? scale * A.kd * A.temperature : 0.f;
+        f1 = labelled ? scale * A.ce : 0.f;
+        // (a stream that both terms share, or that is the only term's)
+        ca = SUMS == ONE ? ft + f1 : ft;
+        cb = SUMS == SQUARE ? f1 * Exp<T>::of(la + la - lb) : f1;
+    }
+    template <bool APART> __device__ __forceinline__ float of(float x) const {
+        const float v = x - top;
+        const float e = Exp<T>::of(APART ? __builtin_fmaf(v, ka, -la) : __builtin_fmaf(x, ka, -ba));
+        if constexpr (SUMS == ONE) return ca * e;
+        if constexpr (SUMS == TWO) return ca * e + cb * Exp<T>::of(APART ? __builtin_fmaf(v, kb, -lb) : __builtin_fmaf(x, kb, -bb));
+        return e * (ca + cb * e);
+    }
+    __device__ __forceinline__ float operator()(float x) const { return of<Exp<T>::EXACT>(x); }
+};
+// The teacher's shares q of the kept logits, by their places, for all threads; then t becomes what those of the same place have
+// together (indices may repeat), and label_q what those at the label have, in its thread.
+struct Shares { float4 q[RK_MAX_TEACHER_LOGITS / 4]; int4 at[RK_MAX_TEACHER_LOGITS / 4]; };
+template <int THREADS> __device__ __forceinline__ float share_wanted(const DistillArgs &A, Wanted<THREADS> &W, float t_sum, Shares &lds) {
+    const float inv_sum = t_sum != 0.f ? 1.f / t_sum : 0.f;
     const uint32_t K = A.kd > 0.f ? A.top_k : 0u;
-    const float inv_sum = kept ? 1.f / t_sum : 0.f;
 #pragma unroll
     for (int n = 0; n < Wanted<THREADS>::N; ++n) {
         const uint32_t k = threadIdx.x + n * THREADS;
-        if (k < K) { q[k] = W.t[n] * inv_sum; at[k] = W.at[n]; }
+        if (k < ((K + 3u) & ~3u)) {                     // (behind the last one there is none: at is -1)
+            ((float *)lds.q)[k] = W.t[n] * inv_sum;
+            ((int32_t *)lds.at)[k] = W.at[n];
+        }
     }
     __syncthreads();                    // d_student may be student: what is needed of other places has been read
-    auto slope = [&](float x) {
-        const float v = x - top, e = Exp<T>::of(__builtin_fmaf(v, S.ka, -la));
-        if constexpr (SUMS == ONE) return ca * e;
-        if constexpr (SUMS == TWO) return ca * e + cb * Exp<T>::of(__builtin_fmaf(v, S.kb, -lb));
-        return e * (ca + cb * e);
+    auto together = [&](int32_t i) {
+        float mass = 0.f;
+#pragma unroll 4
+        for (uint32_t k = 0; k < (K + 3u) / 4u; ++k) {
+            const float4 q = lds.q[k];
+            const int4 at = lds.at[k];
+            mass += (at.x == i ? q.x : 0.f) + (at.y == i ? q.y : 0.f) + (at.z == i ? q.z : 0.f) + (at.w == i ? q.w : 0.f);
+        }
+        return mass;
     };
-    stream_row<CUTS, THREADS, T, CH>(from, begin, end,
+#pragma unroll
+    for (int n = 0; n < Wanted<THREADS>::N; ++n)
+        if (W.at[n] >= 0) W.t[n] = together(W.at[n]);
+    return threadIdx.x == THREADS - 1 && W.label >= 0 ? together(W.label) : 0.f;
+}
+// where teacher or label have something in [begin, end): the whole value, once more (equal indices get equal values)
+template <int THREADS, typename T, int SUMS>
+__device__ __forceinline__ void write_wanted(const Wanted<THREADS> &W, const Slope<T, SUMS> &slope, T *out, uint32_t begin, uint32_t end, float label_q) {
+    auto again = [&](int32_t i, float s, float mass) {
+        if ((uint32_t)i < begin || (uint32_t)i >= end) return;
+        out[i] = (T)((is_huge(slope.top) ? slope.template of<true>(s) : slope(s)) - slope.ft * mass - (i == W.label ? slope.f1 : 0.f));
+    };
+#pragma unroll
+    for (int n = 0; n < Wanted<THREADS>::N; ++n)
+        if (W.at[n] >= 0) again(W.at[n], W.s[n], W.t[n]);
+    if (threadIdx.x == THREADS - 1 && W.label >= 0) again(W.label, W.label_s, label_q);
+}
+template <bool CUTS, int THREADS, typename T, int CH, int SUMS>
+__device__ __forceinline__ void write_huge(const Row<T> &from, const Row<T> &to, uint32_t begin, uint32_t end, const Slope<T, SUMS> &slope) {
+    for (uint32_t c = begin + threadIdx.x * CH; c < end; c += THREADS * CH) {
+        const Place p(c, end, CH);
+        float v[CH];
+        load_row<CUTS, T, CH>(from, p, v);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) v[i] = slope.template of<true>(v[i]);
+        store_row<CUTS, T, CH>(to, p, v);
+    }
+}
+template <bool CUTS, int THREADS, typename T, int CH, int SUMS>
+__device__ __forceinline__ void write_gradient(const DistillArgs &A, const Row<T> &from, const Row<T> &to, T *out, uint32_t begin, uint32_t end, const Slope<T, SUMS> &slope,
+                                               Wanted<THREADS> &W, float t_sum, Shares &lds) {
+    const float label_q = share_wanted(A, W, t_sum, lds);
+    if (is_huge(slope.top)) write_huge<CUTS, THREADS, T, CH, SUMS>(from, to, begin, end, slope);
+    else stream_row<CUTS, THREADS, T, CH, STREAM>(from, begin, end,
         [&](uint32_t first, const Words<T, CH> &w) {
             float v[CH];
 #pragma unroll
             for (int i = 0; i < CH; ++i) v[i] = slope(element<T>(w, i));
-            store_at<T, CH>(to, first, words_of<T, CH>(v));
+            store_at<T, CH, STREAM>(to, first, words_of<T, CH>(v));
         },
         [&](const Place &p, const Words<T, CH> &w) {
             float v[CH];
 #pragma unroll
             for (int i = 0; i < CH; ++i) v[i] = slope(element<T>(w, i));
-            store_row<CUTS, T, CH>(to, p, v);
+            store_row<CUTS, T, CH, STREAM>(to, p, v);
         });
     __syncthreads();
-    // where teacher or label have something: the whole value, once more (equal indices get equal values)
-    auto again = [&](int32_t i, float s) {
-        if ((uint32_t)i < begin || (uint32_t)i >= end) return;
-        float mass = 0.f;
-        for (uint32_t k = 0; k < K; ++k) mass += at[k] == i ? q[k] : 0.f;
-        out[i] = (T)(slope(s) - ft * mass - (i == W.label ? f1 : 0.f));
-    };
-#pragma unroll
-    for (int n = 0; n < Wanted<THREADS>::N; ++n)
-        if (W.at[n] >= 0) again(W.at[n], W.s[n]);
-    if (threadIdx.x == 0 && W.label >= 0) again(W.label, W.label_s);
+    write_wanted(W, slope, out, begin, end, label_q);
 }
 template <bool CUTS, int THREADS, typename T, int CH> __device__ __forceinline__ void write_zeros(const Row<T> &to, uint32_t begin, uint32_t end) {
     const float zero[CH] = {};
-    for (uint32_t c = begin + threadIdx.x * CH; c < end; c += THREADS * CH) store_row<CUTS, T, CH>(to, Place(c, end, CH), zero);
+    for (uint32_t c = begin + threadIdx.x * CH; c < end; c += THREADS * CH) store_row<CUTS, T, CH, STREAM>(to, Place(c, end, CH), zero);
 }
 
 // a row's loss and log sums from the joined sums; cross: teacher's cross term and sum, the label's logit and whether there is one
@@ -252,40 +333,126 @@ __device__ __forceinline__ void keep_row(const DistillArgs &A, uint64_t r, const
     A.lse[2 * r + 1] = A.ce > 0.f ? L.lse_b : 0.f;
 }
 
-// A workgroup a row: its sums, its loss and (GRAD) its gradient, for which the row is read again, from the caches.
-template <bool CUTS, int THREADS, typename T, int CH, int SUMS, bool GRAD>
-__global__ __launch_bounds__(THREADS) void k_distill_rows(DistillArgs A) {
+// A workgroup a row: its sums, its loss and, if there is a d_student, its gradient.  Of what a thread reads, its first NR vectors stay in
+// registers and its next NL in LDS until then; only what is beyond them is read again.
+template <bool CUTS, int THREADS, int NR, int NL, typename T, int CH, int SUMS>
+__global__ __launch_bounds__(THREADS, 8) void k_distill_rows(DistillArgs A) {
+    extern __shared__ float4 kept_lds[];
     __shared__ float4 red[16];
-    __shared__ float q[GRAD ? RK_MAX_TEACHER_LOGITS : 1];
-    __shared__ int32_t at[GRAD ? RK_MAX_TEACHER_LOGITS : 1];
+    __shared__ Shares lds;
+    constexpr uint32_t STEP = THREADS * CH;
     const uint64_t r = blockIdx.x;
     const Row<T> from(A.student, r, A.st, A.vocab), to(A.d_student, r, A.d_st, A.vocab);
     const float weight = A.row_weight ? A.row_weight[r] : 1.f;
     if (weight == 0.f) {
         if (threadIdx.x == 0) { A.loss[r] = 0.f; A.lse[2 * r] = 0.f; A.lse[2 * r + 1] = 0.f; }
-        if constexpr (GRAD) write_zeros<CUTS, THREADS, T, CH>(to, 0, A.vocab);
+        write_zeros<CUTS, THREADS, T, CH>(to, 0, A.vocab);          // (nothing, if there is no d_student)
         return;
     }
     Wanted<THREADS> W;
-    W.template fetch<T>(A, r);
+    W.ask(A, r);
+    // whole rounds of vectors, and one that the row's end cuts off
+    const uint32_t whole = A.vocab / STEP, first = threadIdx.x * CH;
+    const Place last(first + whole * STEP, A.vocab, CH);
+    auto fetch = [&](uint32_t k, auto hint) {
+        constexpr int HINT = decltype(hint)::value;
+        return k < whole ? fetch_at<T, CH, HINT>(from, first + k * STEP) : fetch_row<CUTS, T, CH, HINT>(from, last);
+    };
+    const auto keep = std::integral_constant<int, KEEP>();
+    const auto stream = std::integral_constant<int, STREAM>();
+    Words<T, CH> w[NR];
+#pragma unroll
+    for (int k = 0; k < NR; ++k)
+        if ((uint32_t)k <= whole) w[k] = fetch(k, stream);
+    W.template look<T>(A, r);
     const Streams S = streams_of<T>(A);
     Running<T, SUMS> R;
-    sum_row<CUTS, THREADS, T, CH, SUMS>(from, 0, A.vocab, S, R);
+    auto take = [&](uint32_t k, const Words<T, CH> &x) {
+        float v[CH];
+        if (k < whole) {
+#pragma unroll
+            for (int i = 0; i < CH; ++i) v[i] = element<T>(x, i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < CH; ++i) v[i] = i < last.valid ? element<T>(x, i) : -INFINITY;
+        }
+        R.take(S, v);
+    };
+    constexpr uint32_t W4 = CH * (int)sizeof(T) / 16;
+    static_assert(W4 == 1, "a vector is 16 bytes");
+#pragma unroll
+    for (int k = 0; k < NR; ++k)
+        if ((uint32_t)k <= whole) take(k, w[k]);
+    if constexpr (NL > 0) {
+        Words<T, CH> x[NL];
+#pragma unroll
+        for (int k = 0; k < NL; ++k)
+            if (NR + (uint32_t)k <= whole) x[k] = fetch(NR + k, stream);
+#pragma unroll
+        for (int k = 0; k < NL; ++k) {
+            if (NR + (uint32_t)k > whole) continue;
+            if (A.d_student) kept_lds[k * THREADS + threadIdx.x] = __builtin_bit_cast(float4, x[k]);
+            take(NR + k, x[k]);
+        }
+        for (uint32_t k = NR + NL; k <= whole; k += 4) {
+            Words<T, CH> y[4];
+#pragma unroll
+            for (uint32_t u = 0; u < 4; ++u)
+                if (k + u <= whole) y[u] = fetch(k + u, keep);
+#pragma unroll
+            for (uint32_t u = 0; u < 4; ++u)
+                if (k + u <= whole) take(k + u, y[u]);
+        }
+    }
     float4 v = make_float4(R.m, W.top(), -INFINITY, -INFINITY);
     block_all<THREADS / 64, true>(v, red);
     const float top = v.x;
     R.move(S, top);
+    if (is_huge(top)) sum_huge<CUTS, THREADS, T, CH, SUMS>(from, 0, A.vocab, S, top, R);
     float sum, cross;
     W.weigh(A, v.y, sum, cross);
     v = make_float4(R.sa, R.sb, sum, cross);
     block_all<THREADS / 64, false>(v, red);
     const RowLoss L = row_loss<T, SUMS>(A, S, top, v.x, v.y, make_float4(v.w, v.z, W.label_s, W.label >= 0 ? 1.f : 0.f));
     if (threadIdx.x == 0) keep_row(A, r, L);
-    if constexpr (GRAD) {
-        // (without a kept logit and a label there is no term, whatever the logits hold)
-        if (L.left || (v.z == 0.f && W.label < 0)) write_zeros<CUTS, THREADS, T, CH>(to, 0, A.vocab);
-        else write_gradient<CUTS, THREADS, T, CH, SUMS>(A, from, to, (T *)A.d_student + r * A.d_st, 0, A.vocab, S, top, L.la, L.lb, weight, v.z != 0.f, W, v.z, q, at);
+    if (!A.d_student) return;
+    // (without a kept logit and a label there is no term, whatever the logits hold)
+    if (L.left || (v.z == 0.f && W.label < 0)) {
+        write_zeros<CUTS, THREADS, T, CH>(to, 0, A.vocab);
+        return;
     }
+    const Slope<T, SUMS> slope(A, S, top, L.la, L.lb, weight, v.z != 0.f, W.label >= 0);
+    const float label_q = share_wanted(A, W, v.z, lds);
+    if (is_huge(top)) {
+        write_huge<CUTS, THREADS, T, CH, SUMS>(from, to, 0, A.vocab, slope);
+    } else {
+        auto give = [&](uint32_t k, const Words<T, CH> &x) {
+            float g[CH];
+#pragma unroll
+            for (int i = 0; i < CH; ++i) g[i] = slope(element<T>(x, i));
+            if (k < whole) store_at<T, CH, STREAM>(to, first + k * STEP, words_of<T, CH>(g));
+            else store_row<CUTS, T, CH, STREAM>(to, last, g);
+        };
+        if constexpr (NL > 0)
+            for (uint32_t k = NR + NL; k <= whole; k += 4) {
+                Words<T, CH> y[4];
+#pragma unroll
+                for (uint32_t u = 0; u < 4; ++u)
+                    if (k + u <= whole) y[u] = fetch(k + u, stream);
+#pragma unroll
+                for (uint32_t u = 0; u < 4; ++u)
+                    if (k + u <= whole) give(k + u, y[u]);
+            }
+#pragma unroll
+        for (int k = 0; k < NR; ++k)
+            if ((uint32_t)k <= whole) give(k, w[k]);
+        if constexpr (NL > 0)
+#pragma unroll
+            for (int k = 0; k < NL; ++k)
+                if (NR + (uint32_t)k <= whole) give(NR + k, __builtin_bit_cast(Vec<uint32_t, 4>, kept_lds[k * THREADS + threadIdx.x]));
+    }
+    __syncthreads();
+    write_wanted(W, slope, (T *)A.d_student + r * A.d_st, 0, A.vocab, label_q);
 }
 
 // The sums of a slice of a row, for k_distill_join; the first slice's workgroup also looks up what teacher and label want.
@@ -299,7 +466,7 @@ __global__ __launch_bounds__(THREADS) void k_distill_part(DistillArgs A) {
     const Row<T> from(A.student, r, A.st, A.vocab);
     Wanted<THREADS> W;
     W.at[0] = -1; W.t[0] = -INFINITY;
-    if (slice == 0) W.template fetch<T>(A, r);
+    if (slice == 0) { W.ask(A, r); W.template look<T>(A, r); }
     const Streams S = streams_of<T>(A);
     Running<T, SUMS> R;
     sum_row<CUTS, THREADS, T, CH, SUMS>(from, begin, end, S, R);
@@ -307,6 +474,7 @@ __global__ __launch_bounds__(THREADS) void k_distill_part(DistillArgs A) {
     block_all<THREADS / 64, true>(v, red);
     const float top = v.x;
     R.move(S, top);
+    if (is_huge(top)) sum_huge<CUTS, THREADS, T, CH, SUMS>(from, begin, end, S, top, R);
     float sum = 0.f, cross = 0.f;
     if (slice == 0) W.weigh(A, v.y, sum, cross);
     v = make_float4(R.sa, R.sb, sum, cross);
@@ -331,10 +499,10 @@ template <typename T, int SUMS> __global__ __launch_bounds__(64 * JOIN_WAVES) vo
         }
         const float4 p = lane < A.slices ? A.part[r * A.slices + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
         const float top = wave_max(p.x);
-        Running<T, SUMS> R;
-        R.m = p.x; R.sa = p.y; R.sb = p.z;
-        R.move(S, top);
-        const RowLoss L = row_loss<T, SUMS>(A, S, top, wave_sum(R.sa), wave_sum(R.sb), A.cross[r]);
+        const bool some = p.x != -INFINITY;
+        const float d = p.x - top, f = Exp<T>::of(d * S.ka);
+        const float sa = some ? p.y * f : p.y, sb = some ? p.z * (SUMS == SQUARE ? f * f : Exp<T>::of(d * S.kb)) : p.z;
+        const RowLoss L = row_loss<T, SUMS>(A, S, top, wave_sum(sa), wave_sum(sb), A.cross[r]);
         if (lane == 0) keep_row(A, r, L);
         total += (double)weight * (double)L.loss;
     }
@@ -349,8 +517,7 @@ template <typename T, int SUMS> __global__ __launch_bounds__(64 * JOIN_WAVES) vo
 template <bool CUTS, int THREADS, typename T, int CH, int SUMS>
 __global__ __launch_bounds__(THREADS) void k_distill_gradient(DistillArgs A) {
     __shared__ float4 red[16];
-    __shared__ float q[RK_MAX_TEACHER_LOGITS];
-    __shared__ int32_t at[RK_MAX_TEACHER_LOGITS];
+    __shared__ Shares lds;
     const uint64_t r = blockIdx.x / A.slices;
     const uint32_t slice = blockIdx.x - (uint32_t)r * A.slices, begin = slice * A.slice;
     const uint32_t end = slice + 1 == A.slices ? A.vocab : begin + A.slice;
@@ -362,7 +529,8 @@ __global__ __launch_bounds__(THREADS) void k_distill_gradient(DistillArgs A) {
         return;
     }
     Wanted<THREADS> W;
-    W.template fetch<T>(A, r);
+    W.ask(A, r);
+    W.template look<T>(A, r);
     float4 v = make_float4(W.top(), -INFINITY, -INFINITY, -INFINITY);
     float sum = 0.f, cross = 0.f;
     if (A.kd > 0.f) {
@@ -379,28 +547,31 @@ __global__ __launch_bounds__(THREADS) void k_distill_gradient(DistillArgs A) {
     // relative to where the first stream's exponential is one
     const Streams S = streams_of<T>(A);
     const float top = SUMS == ONE && A.kd == 0.f ? la : la * A.temperature;
-    write_gradient<CUTS, THREADS, T, CH, SUMS>(A, from, to, (T *)A.d_student + r * A.d_st, begin, end, S, top, 0.f, (lb - top) * S.kb, weight, sum != 0.f, W, sum, q,
-                                               at);
+    write_gradient<CUTS, THREADS, T, CH, SUMS>(A, from, to, (T *)A.d_student + r * A.d_st, begin, end,
+                                               Slope<T, SUMS>(A, S, top, 0.f, (lb - top) * S.kb, weight, sum != 0.f, W.label >= 0), W, sum, lds);
 }
 
 // the rows' losses added up, in one order
 __global__ __launch_bounds__(1024) void k_distill_total(DistillArgs A) {
-    __shared__ double lds[1024];
+    __shared__ double lds[16];
     double s = 0.0;
     for (uint64_t r = threadIdx.x; r < A.n_rows; r += 1024) {
         const float w = A.row_weight ? A.row_weight[r] : 1.f;
-        if (w != 0.f) s += (double)w * (double)A.loss[r];
+        const float l = A.loss[r];
+        s += w != 0.f ? (double)w * (double)l : 0.0;
     }
-    lds[threadIdx.x] = s;
-    for (uint32_t off = 512; off; off >>= 1) {
-        __syncthreads();
-        if (threadIdx.x < off) lds[threadIdx.x] += lds[threadIdx.x + off];
-    }
-    if (threadIdx.x == 0) A.total[0] = (float)lds[0];
+#pragma unroll
+    for (int off = 32; off; off >>= 1) s += __shfl_xor(s, off, 64);
+    if ((threadIdx.x & 63u) == 0) lds[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < 16; ++w) s += lds[w];
+    A.total[0] = (float)s;
 }
 
 // ---- host
-constexpr uint32_t DS_SMALL = 8192;           // elements up to which 256 threads take a row or slice
+constexpr int DS_REGISTERS = 4, DS_LDS = 4;                     // vectors a thread of a long row keeps in LDS: 64 KB a workgroup, two of which fit a compute unit
+constexpr uint32_t DS_SMALL = 16384;           // elements up to which 256 threads take a row or slice
 
 int32_t check_distill(rk_ctx *ctx, const rk_distill *d, uint64_t n_rows, uint32_t vocab, const rk_matrix *student, const rk_teacher *t, DistillArgs &A) {
     if (!d || !t) return rk_fail(ctx, RK_ERR_INVALID_ARG, "distill or teacher is null");
@@ -424,40 +595,52 @@ int32_t check_distill(rk_ctx *ctx, const rk_distill *d, uint64_t n_rows, uint32_
     A.temperature = d->temperature; A.kd = d->kd_weight; A.ce = d->ce_weight;
     return RK_OK;
 }
-enum Step { STEP_LOSS, STEP_BOTH, STEP_PART, STEP_JOIN, STEP_GRADIENT };
-template <typename T, int SUMS> void launch(hipStream_t st, const DistillArgs &A, Step step) {
+enum Step { STEP_ROWS, STEP_PART, STEP_JOIN, STEP_GRADIENT };
+template <typename T, int SUMS> hipError_t launch(hipStream_t st, const DistillArgs &A, Step step) {
     constexpr int CH = sizeof(T) == 4 ? 4 : 8;
     if (step == STEP_JOIN) {
         k_distill_join<T, SUMS><<<1, 64 * JOIN_WAVES, 0, st>>>(A);
-        return;
+        return hipSuccess;
     }
     auto go = [&](auto cuts, auto threads) {
         constexpr bool CUTS = decltype(cuts)::value;
         constexpr int N = decltype(threads)::value;
         const uint32_t blocks = (uint32_t)(A.n_rows * A.slices);
-        if (step == STEP_LOSS) k_distill_rows<CUTS, N, T, CH, SUMS, false><<<blocks, N, 0, st>>>(A);
-        else if (step == STEP_BOTH) k_distill_rows<CUTS, N, T, CH, SUMS, true><<<blocks, N, 0, st>>>(A);
-        else if (step == STEP_PART) k_distill_part<CUTS, N, T, CH, SUMS><<<blocks, N, 0, st>>>(A);
+        if (step == STEP_PART) k_distill_part<CUTS, N, T, CH, SUMS><<<blocks, N, 0, st>>>(A);
         else k_distill_gradient<CUTS, N, T, CH, SUMS><<<blocks, N, 0, st>>>(A);
     };
+    auto rows = [&](auto cuts) {
+        constexpr bool CUTS = decltype(cuts)::value;
+        const uint32_t vectors = (A.vocab + CH - 1) / CH, n = (uint32_t)A.n_rows;
+        if (vectors <= 256 * 8) k_distill_rows<CUTS, 256, 8, 0, T, CH, SUMS><<<n, 256, 0, st>>>(A);
+        else if (vectors <= 512 * 8) k_distill_rows<CUTS, 512, 8, 0, T, CH, SUMS><<<n, 512, 0, st>>>(A);
+        else {
+            const auto kernel = k_distill_rows<CUTS, 1024, DS_REGISTERS, DS_LDS, T, CH, SUMS>;
+            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, DS_LDS * 1024 * 16);
+            if (e != hipSuccess) return e;
+            kernel<<<n, 1024, DS_LDS * 1024 * 16, st>>>(A);
+        }
+        return hipSuccess;
+    };
+    if (step == STEP_ROWS) return A.vocab % CH ? rows(std::true_type()) : rows(std::false_type());
     auto sized = [&](auto cuts) {
         if (A.slice <= DS_SMALL) go(cuts, std::integral_constant<int, 256>());
         else go(cuts, std::integral_constant<int, 1024>());
     };
     if (A.vocab % CH) sized(std::true_type()); else sized(std::false_type());
+    return hipSuccess;
 }
 int32_t send(rk_ctx *ctx, uint32_t type, const DistillArgs &A, Step step) {
     const int sums = A.kd == 0.f || A.ce == 0.f || A.temperature == 1.f ? ONE : A.temperature == 2.f && type != RK_F32 ? SQUARE : TWO;
-    if (type == RK_F32) { if (sums == ONE) launch<float, ONE>(ctx->stream, A, step); else launch<float, TWO>(ctx->stream, A, step); }
-    else if (type == RK_BF16) {
-        if (sums == ONE) launch<__bf16, ONE>(ctx->stream, A, step);
-        else if (sums == TWO) launch<__bf16, TWO>(ctx->stream, A, step);
-        else launch<__bf16, SQUARE>(ctx->stream, A, step);
-    } else {
-        if (sums == ONE) launch<_Float16, ONE>(ctx->stream, A, step);
-        else if (sums == TWO) launch<_Float16, TWO>(ctx->stream, A, step);
-        else launch<_Float16, SQUARE>(ctx->stream, A, step);
-    }
+    auto go = [&](auto t) {
+        typedef decltype(t) T;
+        if (sums == ONE) return launch<T, ONE>(ctx->stream, A, step);
+        if constexpr (sizeof(T) == 2)
+            if (sums == SQUARE) return launch<T, SQUARE>(ctx->stream, A, step);
+        return launch<T, TWO>(ctx->stream, A, step);
+    };
+    const hipError_t e = type == RK_F32 ? go(float()) : type == RK_BF16 ? go(__bf16()) : go(_Float16());
+    if (e != hipSuccess) return rk_fail(ctx, RK_ERR_DEVICE, "k_distill_rows: %s", hipGetErrorString(e));
     RK_CHECK_LAUNCH(ctx, step == STEP_JOIN ? "k_distill_join" : step == STEP_PART ? "k_distill_part" : step == STEP_GRADIENT ? "k_distill_gradient" : "k_distill_rows");
     return RK_OK;
 }
@@ -487,11 +670,11 @@ int32_t run(rk_ctx *ctx, uint32_t type, DistillArgs &A, bool want_loss, bool wan
             want_loss = false;
         } else {
             A.slices = 1; A.slice = A.vocab;
-            if ((rc = send(ctx, type, A, want_grad ? STEP_BOTH : STEP_LOSS)) != RK_OK) return rc;
+            if ((rc = send(ctx, type, A, STEP_ROWS)) != RK_OK) return rc;
         }
     }
     if (gradient && A.n_rows) {
-        cut_rows(A, 1024, 8192);
+        cut_rows(A, 4096, 8192);
         if ((rc = send(ctx, type, A, STEP_GRADIENT)) != RK_OK) return rc;
     }
     if (want_loss) {

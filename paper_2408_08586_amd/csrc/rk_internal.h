@@ -44,6 +44,7 @@ struct rk_ctx {
     bool loop_lds_raised;                   // the Schedule loop over totals: likewise
     bool nodes_lds_raised;                  // the Schedule loop over nodes: likewise
     unsigned char *static_scratch;          // this device's copy of the static scratch array (rk_allocate_static)
+    bool route_clear;                       // routing: the counter of ended workgroups is known to be zero
     bool place_lds_raised;                  // placement kernel: its dynamic LDS limit has been raised for this context
 };
 
@@ -74,7 +75,7 @@ enum {
     SL_FEW_STATES,                                       // simulation from scratch: the walks of all jobs
     SL_FIT_NEXT,                                         // model fitting: the next model to take
     SL_NORM_PARTS, SL_NORM_ROWS,                         // norms around a block: sums of the chunks of rows; per row, what its gradient takes off
-    SL_ROUTE_COUNTS, SL_ROUTE_PROBS, SL_ROUTE_Z, SL_ROUTE_GROUPS,   // router: its workgroups' counts and sums, its groups'
+    SL_ROUTE_COUNTS, SL_ROUTE_PROBS, SL_ROUTE_Z, SL_ROUTE_GROUPS, SL_ROUTE_DONE,   // router: its workgroups' counts and sums, its groups'
     SL_DISTILL_PARTS,                                    // distillation: the sums of the rows' slices
     SL_COUNT
 };

@@ -152,7 +152,7 @@ __global__ __launch_bounds__(MAXT) void k_norm_forward(NormArgs A, bool per_wave
             const float n = (v[k][i] - my) * ry * w[i] + b[i];
             x[k][i] = i < at[k].valid ? A.scale * x[k][i] + g[i] * n : 0.f;
         }
-        store_row<CUTS, R, CH>(xo, at[k], x[k]);
+        store_row<CUTS, R, CH, STREAM>(xo, at[k], x[k]);
     }
     row_stats<CH, NC>(G, x, A.width, at, A.pre, A.pre_eps, mx, rx);
     if (P.tid == 0) reinterpret_cast<float4 *>(A.stats)[P.row] = make_float4(my, ry, mx, rx);
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(MAXT) void k_norm_forward(NormArgs A, bool per_wave
         load_param<CUTS, T, CH>(A, G_PRE_B, 0, 0, at[k], 0.f, b);
 #pragma unroll
         for (int i = 0; i < CH; ++i) x[k][i] = (x[k][i] - mx) * rx * w[i] + b[i];
-        store_row<CUTS, T, CH>(u, at[k], x[k]);
+        store_row<CUTS, T, CH, STREAM>(u, at[k], x[k]);
     }
 }
 
@@ -394,8 +394,8 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
         const Row<T> u(there ? A.du : nullptr, r, A.du_st, A.width);
 #pragma unroll
         for (int k = 0; k < NC; ++k) {
-            rx[k] = fetch_row<CUTS, R, CH>(x, at[k]);
-            ru[k] = fetch_row<CUTS, T, CH>(u, at[k]);
+            rx[k] = fetch_row<CUTS, R, CH, STREAM>(x, at[k]);
+            ru[k] = fetch_row<CUTS, T, CH, STREAM>(u, at[k]);
         }
     };
     auto fetch_second = [&](uint64_t r) {
@@ -404,8 +404,8 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
         const Row<T> y(there ? A.y : nullptr, r, A.y_st, A.width);
 #pragma unroll
         for (int k = 0; k < NC; ++k) {
-            rd[k] = fetch_row<CUTS, R, CH>(dxo, at[k]);
-            ry[k] = fetch_row<CUTS, T, CH>(y, at[k]);
+            rd[k] = fetch_row<CUTS, R, CH, STREAM>(dxo, at[k]);
+            ry[k] = fetch_row<CUTS, T, CH, STREAM>(y, at[k]);
         }
     };
     if (r0 < r1) { fetch_first(r0); fetch_second(r0); }
@@ -458,7 +458,7 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
             for (int i = 0; i < CH; ++i) {
                 t[i] = A.scale * d[k][i];
             }
-            store_row<CUTS, R, CH>(Row<R>(A.xo, r, A.xo_st, A.width), at[k], t);
+            store_row<CUTS, R, CH, STREAM>(Row<R>(A.xo, r, A.xo_st, A.width), at[k], t);
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
                 const float y = (element<T>(ry[k], i) - st.x) * st.y;
@@ -483,7 +483,7 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
         {
             const Row<T> dy(A.u, r, A.u_st, A.width);
 #pragma unroll
-            for (int k = 0; k < NC; ++k) store_row<CUTS, T, CH>(dy, at[k], d[k]);
+            for (int k = 0; k < NC; ++k) store_row<CUTS, T, CH, STREAM>(dy, at[k], d[k]);
         }
         if (r + 1 == r1 || r + 1 == gate_end) {
             const bool first = gate_end <= r0 + A.gate_rows || !A.gate_rows;        // (of the chunk's gates)
@@ -555,8 +555,17 @@ __global__ __launch_bounds__(1024) void k_norm_join(Joined J, uint32_t width, ui
     uint64_t count = J.count[v];
     if (job >= J.n) { from += (job - J.n) * J.gate_chunks * width; to += (job - J.n) * J.gate_out_st; count = J.gate_chunks; }
     float s = 0.f;
-    if (col < width)
-        for (uint64_t c = wave; c < count; c += 16) s += from[c * width + col];
+    if (col < width) {
+        uint64_t c = wave;
+        for (; c + 112 < count; c += 128) {                     // eight under way at once
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = from[(c + 16 * i) * width + col];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += v[i];
+        }
+        for (; c < count; c += 16) s += from[c * width + col];
+    }
     lds[wave][lane] = s;
     __syncthreads();
     if (wave) return;
@@ -566,9 +575,6 @@ __global__ __launch_bounds__(1024) void k_norm_join(Joined J, uint32_t width, ui
 }
 
 // ---- host
-#ifndef NORM_ONE_MAX
-#define NORM_ONE_MAX 8192u
-#endif
 struct Shape { int nc; uint32_t threads, rows_per_wg; bool per_wave; };
 
 template <typename T, typename R> constexpr int chunk_of() { return sizeof(T) == 2 ? 8 : 4; }
@@ -608,7 +614,7 @@ Shape sums_shape_of(uint32_t width, int ch, bool bias) {
     const int per = 8 / ch;                                     // vectors of eight elements
     for (int n8 = 1; n8 <= 2; ++n8)
         if (width <= 512u * n8) return Shape{n8 * per, 256, 4, true};
-    const int n8 = width <= NORM_ONE_MAX ? 1 : 2;
+    const int n8 = width <= 8192u ? 1 : 2;
     const uint32_t threads = (width + 8 * n8 * 64 - 1) / (8 * n8 * 64) * 64;
     if (threads > (n8 == 1 ? 1024u : 768u) || threads * sums_lds_of(8, n8, bias) * 16 > 163840u - 1024u) return Shape{0, 0, 0, false};
     return Shape{n8 * per, threads, 1, false};

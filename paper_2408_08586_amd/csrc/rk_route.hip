@@ -26,6 +26,7 @@ struct RouteArgs {
     float *part_probs;
     float2 *part_z;                     // [workgroup]: tokens, sum of lse^2
     float4 *tile_z;                     // [group][tile of experts]: sum of counts * prob_sum, sum of lse^2, tokens
+    uint32_t *done;                     // workgroups that have ended; 0 between calls
     uint32_t tiles;
     // backward
     void *d_logits;
@@ -290,29 +291,45 @@ __global__ __launch_bounds__(64 * RT_JOIN) void k_route_join(RouteArgs A) {
     for (int w = 1; w < RT_JOIN; ++w) { n += lds_n[w]; z += lds_z[w]; p += lds_p[w][lane]; count += lds_c[w][lane]; }
     if (e < E) { A.counts[g * E + e] = count; A.prob_sum[g * E + e] = p; }
     const float cp = wave_sum(e < E ? (float)count * p : 0.f);
+    // The workgroup that ends last adds the groups up, in their order.  What it needs of the others goes through stores and loads at the
+    // device's scope (the workgroups sit on several L2 caches), which are written through and read where all of the device sees
+    // them; when the wait before the counter is over they have arrived, and no cache has to be written back.
+    uint32_t ends = 0;
+    if (lane == 0) {
+        if (e == 0) A.tokens[g] = (uint32_t)n;
+        float *const mine = (float *)&A.tile_z[blockIdx.x];
+        __hip_atomic_store(mine, cp, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(mine + 1, z, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(mine + 2, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        ends = __hip_atomic_fetch_add(A.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if ((uint32_t)__builtin_amdgcn_readfirstlane((int)ends) != gridDim.x - 1u) return;
+    asm volatile("" ::: "memory");
+    if (lane == 0) __hip_atomic_store(A.done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);     // (for the next call)
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
+    for (uint64_t q = lane; q < A.n_groups; q += 64) {
+        const float *const of = (const float *)&A.tile_z[q * A.tiles];
+        float sum = 0.f;
+        for (uint32_t i = 0; i < A.tiles; ++i) sum += __hip_atomic_load(of + 4 * i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const float zq = __hip_atomic_load(of + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const float nq = __hip_atomic_load(of + 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        s[0] += balance_of(E, A.top_k, sum, nq); s[1] += zq; s[2] += nq; s[3] += nq > 0.f ? 1.0 : 0.0;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int off = 32; off; off >>= 1) s[i] += __shfl_xor(s[i], off, 64);
     if (lane) return;
-    A.tile_z[blockIdx.x] = make_float4(cp, z, n, 0.f);
-    if (e == 0) A.tokens[g] = (uint32_t)n;
+    A.loss[0] = s[3] > 0.0 ? (float)(s[0] / s[3]) : 0.f;
+    A.loss[1] = s[2] > 0.0 ? (float)(s[1] / s[2]) : 0.f;
 }
 
-__global__ __launch_bounds__(256) void k_route_loss(RouteArgs A) {
-    __shared__ double lds[256][4];
-    double s[4] = {0.0, 0.0, 0.0, 0.0};
-    for (uint64_t g = threadIdx.x; g < A.n_groups; g += 256) {
-        float cp = 0.f;
-        for (uint32_t i = 0; i < A.tiles; ++i) cp += A.tile_z[g * A.tiles + i].x;
-        const float4 v = A.tile_z[g * A.tiles];
-        s[0] += balance_of(A.n_experts, A.top_k, cp, v.z); s[1] += v.y; s[2] += v.z; s[3] += v.z > 0.f ? 1.0 : 0.0;
-    }
-    for (int i = 0; i < 4; ++i) lds[threadIdx.x][i] = s[i];
-    for (uint32_t off = 128; off; off >>= 1) {
-        __syncthreads();
-        if (threadIdx.x < off)
-            for (int i = 0; i < 4; ++i) lds[threadIdx.x][i] += lds[threadIdx.x + off][i];
-    }
-    if (threadIdx.x) return;
-    A.loss[0] = lds[0][3] > 0.0 ? (float)(lds[0][0] / lds[0][3]) : 0.f;
-    A.loss[1] = lds[0][2] > 0.0 ? (float)(lds[0][1] / lds[0][2]) : 0.f;
+// no token: nothing but zeros (of the one group, if the tokens are not in groups)
+__global__ __launch_bounds__(256) void k_route_nothing(RouteArgs A) {
+    for (uint64_t e = threadIdx.x; e < A.n_groups * A.n_experts; e += 256) { A.counts[e] = 0u; A.prob_sum[e] = 0.f; }
+    if (threadIdx.x < A.n_groups) A.tokens[threadIdx.x] = 0u;
+    if (threadIdx.x < 2) A.loss[threadIdx.x] = 0.f;
 }
 
 // d l = p (A - sum A p - sum y + d_z 2 lse / n) + y at the chosen experts, where y = p d weight, or, of renormalised weights,
@@ -493,30 +510,36 @@ extern "C" int32_t rk_route_forward(rk_ctx *ctx, const rk_router *router, uint64
     A.chunk = A.per_group ? (A.group_tokens + A.per_group - 1) / A.per_group : 0;
     A.tiles = (A.n_experts + 63) / 64;
     const uint64_t blocks = A.per_group * (n_tokens ? A.n_groups : 0);
-    if (blocks != 1) {
+    if (blocks == 0) {
+        k_route_nothing<<<1, 256, 0, ctx->stream>>>(A);
+        RK_CHECK_LAUNCH(ctx, "k_route_nothing");
+        return RK_OK;
+    }
+    if (blocks > 1) {
         if ((rc = rk_scratch(ctx, SL_ROUTE_COUNTS, blocks * A.n_experts * 4, (void **)&A.part_counts)) != RK_OK) return rc;
         if ((rc = rk_scratch(ctx, SL_ROUTE_PROBS, blocks * A.n_experts * 4, (void **)&A.part_probs)) != RK_OK) return rc;
         if ((rc = rk_scratch(ctx, SL_ROUTE_Z, blocks * 8, (void **)&A.part_z)) != RK_OK) return rc;
         if ((rc = rk_scratch(ctx, SL_ROUTE_GROUPS, A.n_groups * A.tiles * 16, (void **)&A.tile_z)) != RK_OK) return rc;
+        if ((rc = rk_scratch(ctx, SL_ROUTE_DONE, 4, (void **)&A.done)) != RK_OK) return rc;
+        if (!ctx->route_clear) {                                // (once, and never in a graph: the wait would fail there)
+            RK_HIP(ctx, hipMemsetAsync(A.done, 0, 4, ctx->stream));
+            RK_HIP(ctx, hipStreamSynchronize(ctx->stream));
+            ctx->route_clear = true;
+        }
     }
-    if (blocks) {
-        const size_t lds = (size_t)A.n_experts * 4 * (1 + at_once) + RT_WAVES * 12;
-        with_lanes(logits->type, A.n_experts, [&](auto t, auto l, auto v, auto c) {
-            const auto kernel = k_route_forward<decltype(t), decltype(l)::value, decltype(v)::value, decltype(c)::value>;
-            if (lds > 65536)
-                rc = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess ? RK_OK : RK_ERR_DEVICE;
-            if (rc == RK_OK) kernel<<<(uint32_t)blocks, RT_THREADS, lds, ctx->stream>>>(A);
-        });
-        if (rc != RK_OK) return rk_fail(ctx, rc, "k_route_forward: no room in LDS");
-        RK_CHECK_LAUNCH(ctx, "k_route_forward");
-        if (blocks == 1) return RK_OK;
-    }
-    if (A.n_groups) {
+    const size_t lds = (size_t)A.n_experts * 4 * (1 + at_once) + RT_WAVES * 12;
+    with_lanes(logits->type, A.n_experts, [&](auto t, auto l, auto v, auto c) {
+        const auto kernel = k_route_forward<decltype(t), decltype(l)::value, decltype(v)::value, decltype(c)::value>;
+        if (lds > 65536)
+            rc = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess ? RK_OK : RK_ERR_DEVICE;
+        if (rc == RK_OK) kernel<<<(uint32_t)blocks, RT_THREADS, lds, ctx->stream>>>(A);
+    });
+    if (rc != RK_OK) return rk_fail(ctx, rc, "k_route_forward: no room in LDS");
+    RK_CHECK_LAUNCH(ctx, "k_route_forward");
+    if (blocks > 1) {
         k_route_join<<<(uint32_t)(A.n_groups * A.tiles), 64 * RT_JOIN, 0, ctx->stream>>>(A);
         RK_CHECK_LAUNCH(ctx, "k_route_join");
     }
-    k_route_loss<<<1, 256, 0, ctx->stream>>>(A);
-    RK_CHECK_LAUNCH(ctx, "k_route_loss");
     return RK_OK;
 }
 

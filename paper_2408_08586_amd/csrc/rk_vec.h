@@ -33,20 +33,22 @@ struct Place {
         cut_here = __builtin_amdgcn_ballot_w64(cut != ROW_NOWHERE) != 0;
     }
 };
-template <typename T, int N> __device__ __forceinline__ Words<T, N> fetch_at(const Row<T> &row, uint32_t first) {
+// How long the caches are to keep what passes: STREAM is for what is read or written once (the instructions' non-temporal bit).
+enum { KEEP = 0, STREAM = 2 };
+template <typename T, int N, int HINT = KEEP> __device__ __forceinline__ Words<T, N> fetch_at(const Row<T> &row, uint32_t first) {
     Words<T, N> w;
     constexpr int PARTS = N * (int)sizeof(T) / 16;
     const uint32_t at = first * (uint32_t)sizeof(T);
 #pragma unroll
     for (int h = 0; h < PARTS; ++h) {
-        const Vec<uint32_t, 4> x = __builtin_amdgcn_raw_buffer_load_b128(row.buf, at + 16u * h, 0, 0);
+        const Vec<uint32_t, 4> x = __builtin_amdgcn_raw_buffer_load_b128(row.buf, at + 16u * h, 0, HINT);
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[4 * h + i] = x[i];
     }
     return w;
 }
-template <bool CUTS, typename T, int N> __device__ __forceinline__ Words<T, N> fetch_row(const Row<T> &row, const Place &p) {
-    Words<T, N> w = fetch_at<T, N>(row, p.whole);
+template <bool CUTS, typename T, int N, int HINT = KEEP> __device__ __forceinline__ Words<T, N> fetch_row(const Row<T> &row, const Place &p) {
+    Words<T, N> w = fetch_at<T, N, HINT>(row, p.whole);
     if (CUTS && p.cut_here) {
         const uint32_t from = p.cut * (uint32_t)sizeof(T);
 #pragma unroll
@@ -62,8 +64,8 @@ template <typename T, int W> __device__ __forceinline__ float element(const Vec<
     else if constexpr (__is_same(T, __bf16)) return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
     else return (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? w[i / 2] >> 16 : w[i / 2]));
 }
-template <bool CUTS, typename T, int N> __device__ __forceinline__ void load_row(const Row<T> &row, const Place &p, float (&v)[N]) {
-    const Words<T, N> w = fetch_row<CUTS, T, N>(row, p);
+template <bool CUTS, typename T, int N, int HINT = KEEP> __device__ __forceinline__ void load_row(const Row<T> &row, const Place &p, float (&v)[N]) {
+    const Words<T, N> w = fetch_row<CUTS, T, N, HINT>(row, p);
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = element<T>(w, i);
 }
@@ -73,7 +75,7 @@ template <typename T, int N> __device__ __forceinline__ Words<T, N> words_of(con
     for (int i = 0; i < N; ++i) x[i] = (T)v[i];             // to nearest, ties to even
     return __builtin_bit_cast(Words<T, N>, x);
 }
-template <typename T, int N> __device__ __forceinline__ void store_at(const Row<T> &row, uint32_t first, const Words<T, N> &w) {
+template <typename T, int N, int HINT = KEEP> __device__ __forceinline__ void store_at(const Row<T> &row, uint32_t first, const Words<T, N> &w) {
     constexpr int PARTS = N * (int)sizeof(T) / 16;
     const uint32_t at = first * (uint32_t)sizeof(T);
 #pragma unroll
@@ -81,12 +83,12 @@ template <typename T, int N> __device__ __forceinline__ void store_at(const Row<
         Vec<uint32_t, 4> y;
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[i] = w[4 * h + i];
-        __builtin_amdgcn_raw_buffer_store_b128(y, row.buf, at + 16u * h, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(y, row.buf, at + 16u * h, 0, HINT);
     }
 }
-template <bool CUTS, typename T, int N> __device__ __forceinline__ void store_row(const Row<T> &row, const Place &p, const float (&v)[N]) {
+template <bool CUTS, typename T, int N, int HINT = KEEP> __device__ __forceinline__ void store_row(const Row<T> &row, const Place &p, const float (&v)[N]) {
     const Words<T, N> w = words_of<T, N>(v);
-    store_at<T, N>(row, p.whole, w);
+    store_at<T, N, HINT>(row, p.whole, w);
     if (CUTS && p.cut_here) {
         const uint32_t from = p.cut * (uint32_t)sizeof(T);
 #pragma unroll
