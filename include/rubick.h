@@ -922,7 +922,7 @@ typedef struct {
 
 /* loss [device] n_rows (unweighted); lse [device] n_rows x 2: log sum exp of student / T and of student, 0
  * where its term's weight is 0; total [device] one float: sum of row_weight * loss.
- * Rows whose weight is 0 are not read: loss and lse 0.  Rows without a logit
+ * Rows whose weight is 0 are left out, whatever they hold: loss and lse 0.  Rows without a logit
  * above -inf have loss 0 and lse -inf. */
 int32_t rk_distill_loss(rk_ctx *ctx, const rk_distill *distill, uint64_t n_rows, uint32_t vocab,
                         const rk_matrix *student, const rk_teacher *teacher, float *loss, float *lse, float *total);

@@ -344,13 +344,7 @@ __global__ __launch_bounds__(THREADS, 8) void k_distill_rows(DistillArgs A) {
     const uint64_t r = blockIdx.x;
     const Row<T> from(A.student, r, A.st, A.vocab), to(A.d_student, r, A.d_st, A.vocab);
     const float weight = A.row_weight ? A.row_weight[r] : 1.f;
-    if (weight == 0.f) {
-        if (threadIdx.x == 0) { A.loss[r] = 0.f; A.lse[2 * r] = 0.f; A.lse[2 * r + 1] = 0.f; }
-        write_zeros<CUTS, THREADS, T, CH>(to, 0, A.vocab);          // (nothing, if there is no d_student)
-        return;
-    }
     Wanted<THREADS> W;
-    W.ask(A, r);
     // whole rounds of vectors, and one that the row's end cuts off
     const uint32_t whole = A.vocab / STEP, first = threadIdx.x * CH;
     const Place last(first + whole * STEP, A.vocab, CH);
@@ -361,9 +355,19 @@ __global__ __launch_bounds__(THREADS, 8) void k_distill_rows(DistillArgs A) {
     const auto keep = std::integral_constant<int, KEEP>();
     const auto stream = std::integral_constant<int, STREAM>();
     Words<T, CH> w[NR];
+    auto begin = [&] {
+        W.ask(A, r);
 #pragma unroll
-    for (int k = 0; k < NR; ++k)
-        if ((uint32_t)k <= whole) w[k] = fetch(k, stream);
+        for (int k = 0; k < NR; ++k)
+            if ((uint32_t)k <= whole) w[k] = fetch(k, stream);
+    };
+    if (NL == 0) begin();                   // (a short row is fetched before its weight is there)
+    if (weight == 0.f) {
+        if (threadIdx.x == 0) { A.loss[r] = 0.f; A.lse[2 * r] = 0.f; A.lse[2 * r + 1] = 0.f; }
+        write_zeros<CUTS, THREADS, T, CH>(to, 0, A.vocab);          // (nothing, if there is no d_student)
+        return;
+    }
+    if (NL > 0) begin();
     W.template look<T>(A, r);
     const Streams S = streams_of<T>(A);
     Running<T, SUMS> R;
@@ -484,28 +488,30 @@ __global__ __launch_bounds__(THREADS) void k_distill_part(DistillArgs A) {
     if (slice == 0) A.cross[r] = make_float4(v.w, v.z, W.label_s, W.label >= 0 ? 1.f : 0.f);
 }
 
-// The slices of the rows joined, a wavefront a row (at most 64 slices), and the rows' losses added up, in one order.
+// The slices of the rows joined, a wavefront a row (at most 64 slices); one workgroup also adds the rows' losses up, in one order.
 constexpr int JOIN_WAVES = 16;
 template <typename T, int SUMS> __global__ __launch_bounds__(64 * JOIN_WAVES) void k_distill_join(DistillArgs A) {
     __shared__ double lds[JOIN_WAVES];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     const Streams S = streams_of<T>(A);
     double total = 0.0;
-    for (uint64_t r = wave; r < A.n_rows; r += JOIN_WAVES) {
+    for (uint64_t r = (uint64_t)blockIdx.x * JOIN_WAVES + wave; r < A.n_rows; r += (uint64_t)gridDim.x * JOIN_WAVES) {
         const float weight = A.row_weight ? A.row_weight[r] : 1.f;
+        const float4 p = lane < A.slices ? A.part[r * A.slices + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+        const float4 cross = A.cross[r];
         if (weight == 0.f) {
             if (lane == 0) { A.loss[r] = 0.f; A.lse[2 * r] = 0.f; A.lse[2 * r + 1] = 0.f; }
             continue;
         }
-        const float4 p = lane < A.slices ? A.part[r * A.slices + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
         const float top = wave_max(p.x);
         const bool some = p.x != -INFINITY;
         const float d = p.x - top, f = Exp<T>::of(d * S.ka);
         const float sa = some ? p.y * f : p.y, sb = some ? p.z * (SUMS == SQUARE ? f * f : Exp<T>::of(d * S.kb)) : p.z;
-        const RowLoss L = row_loss<T, SUMS>(A, S, top, wave_sum(sa), wave_sum(sb), A.cross[r]);
+        const RowLoss L = row_loss<T, SUMS>(A, S, top, wave_sum(sa), wave_sum(sb), cross);
         if (lane == 0) keep_row(A, r, L);
         total += (double)weight * (double)L.loss;
     }
+    if (gridDim.x > 1) return;
     if (lane == 0) lds[wave] = total;
     __syncthreads();
     if (threadIdx.x) return;
@@ -552,25 +558,30 @@ __global__ __launch_bounds__(THREADS) void k_distill_gradient(DistillArgs A) {
 }
 
 // the rows' losses added up, in one order
-__global__ __launch_bounds__(1024) void k_distill_total(DistillArgs A) {
-    __shared__ double lds[16];
+__global__ __launch_bounds__(256) void k_distill_total(DistillArgs A) {
+    __shared__ double lds[4];
     double s = 0.0;
     for (uint64_t r = threadIdx.x; r < A.n_rows; r += 1024) {
-        const float w = A.row_weight ? A.row_weight[r] : 1.f;
-        const float l = A.loss[r];
-        s += w != 0.f ? (double)w * (double)l : 0.0;
+        float w[4], l[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {                           // four under way at once
+            const uint64_t q = r + 256 * i < A.n_rows ? r + 256 * i : r;
+            w[i] = A.row_weight ? A.row_weight[q] : 1.f;
+            l[i] = A.loss[q];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s += r + 256 * i < A.n_rows && w[i] != 0.f ? (double)w[i] * (double)l[i] : 0.0;
     }
 #pragma unroll
     for (int off = 32; off; off >>= 1) s += __shfl_xor(s, off, 64);
     if ((threadIdx.x & 63u) == 0) lds[threadIdx.x >> 6] = s;
     __syncthreads();
-    if (threadIdx.x) return;
-    for (int w = 1; w < 16; ++w) s += lds[w];
-    A.total[0] = (float)s;
+    if (threadIdx.x == 0) A.total[0] = (float)((lds[0] + lds[1]) + (lds[2] + lds[3]));
 }
 
 // ---- host
 constexpr int DS_REGISTERS = 4, DS_LDS = 4;                     // vectors a thread of a long row keeps in LDS: 64 KB a workgroup, two of which fit a compute unit
+constexpr uint64_t DS_FEW = 256;                // rows
 constexpr uint32_t DS_SMALL = 16384;           // elements up to which 256 threads take a row or slice
 
 int32_t check_distill(rk_ctx *ctx, const rk_distill *d, uint64_t n_rows, uint32_t vocab, const rk_matrix *student, const rk_teacher *t, DistillArgs &A) {
@@ -599,7 +610,7 @@ enum Step { STEP_ROWS, STEP_PART, STEP_JOIN, STEP_GRADIENT };
 template <typename T, int SUMS> hipError_t launch(hipStream_t st, const DistillArgs &A, Step step) {
     constexpr int CH = sizeof(T) == 4 ? 4 : 8;
     if (step == STEP_JOIN) {
-        k_distill_join<T, SUMS><<<1, 64 * JOIN_WAVES, 0, st>>>(A);
+        k_distill_join<T, SUMS><<<A.n_rows < DS_FEW ? 1 : (uint32_t)((A.n_rows + JOIN_WAVES - 1) / JOIN_WAVES), 64 * JOIN_WAVES, 0, st>>>(A);
         return hipSuccess;
     }
     auto go = [&](auto cuts, auto threads) {
@@ -659,15 +670,17 @@ int32_t run(rk_ctx *ctx, uint32_t type, DistillArgs &A, bool want_loss, bool wan
     A.slices = 1; A.slice = A.vocab;
     bool gradient = want_grad && !want_loss;
     if (want_loss && A.n_rows) {
-        cut_rows(A, 512, 4096);
-        if (A.n_rows < 256 && A.slices > 1) {
+        // Rows that would leave compute units without one are cut into slices: fewer than DS_FEW of them, or, where the loss is all and
+        // the slices need no second reading, up to four times as many.
+        cut_rows(A, want_grad ? 512 : 2048, want_grad ? 4096 : 8192);
+        if (A.slices > 1 && A.n_rows < (want_grad ? DS_FEW : 4 * DS_FEW)) {
             const size_t parts = (size_t)(A.n_rows * A.slices);
             float4 *room;
             if ((rc = rk_scratch(ctx, SL_DISTILL_PARTS, (parts + A.n_rows) * 16, (void **)&room)) != RK_OK) return rc;
             A.part = room; A.cross = room + parts;
             if ((rc = send(ctx, type, A, STEP_PART)) != RK_OK || (rc = send(ctx, type, A, STEP_JOIN)) != RK_OK) return rc;
             gradient = want_grad;
-            want_loss = false;
+            want_loss = A.n_rows >= DS_FEW;                     // (otherwise the join has the total)
         } else {
             A.slices = 1; A.slice = A.vocab;
             if ((rc = send(ctx, type, A, STEP_ROWS)) != RK_OK) return rc;
@@ -678,7 +691,7 @@ int32_t run(rk_ctx *ctx, uint32_t type, DistillArgs &A, bool want_loss, bool wan
         if ((rc = send(ctx, type, A, STEP_GRADIENT)) != RK_OK) return rc;
     }
     if (want_loss) {
-        k_distill_total<<<1, 1024, 0, ctx->stream>>>(A);
+        k_distill_total<<<1, 256, 0, ctx->stream>>>(A);
         RK_CHECK_LAUNCH(ctx, "k_distill_total");
     }
     return RK_OK;

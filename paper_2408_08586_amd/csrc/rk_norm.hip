@@ -337,9 +337,9 @@ __global__ __launch_bounds__(SUM_THREADS) void k_norm_sums(NormSums S, uint32_t 
         if (S.part[s] && !(s == G_GATE && S.gate_direct)) store_row<CUTS, float, CH>(Row<float>(S.part[s], chunk, A.width, A.width), at, acc[s]);
 }
 
-// what a lane keeps in LDS of two weights, gate and (with biases) the block's bias, in 16 bytes: an odd number of them, so that
-// the lanes' reads spread over the banks
-constexpr uint32_t sums_lds_of(int ch, int nc, bool bias) { return (uint32_t)((bias ? 4 : 3) * nc * ch / 4) | 1u; }
+// what a lane keeps in LDS of two weights and the gate, in 16 bytes: an odd number of them, so that the lanes' reads spread over the
+// banks
+constexpr uint32_t sums_lds_of(int ch, int nc) { return (uint32_t)(3 * nc * ch / 4) | 1u; }
 
 // Rows back and the sums over them in one pass: a workgroup (or, of rows that a wavefront holds, a wavefront) takes a chunk of
 // rows, and every lane keeps the sums of its columns in registers.  The next row's x_out and du are on their way while this row's
@@ -362,7 +362,7 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
     places<CH, NC>(at, P.tid, P.threads, A.width);
     float sum_dy[NC][CH] = {}, acc_w2[NC][CH] = {}, sum_d[BIAS ? NC : 1][CH] = {}, acc_b2[BIAS ? NC : 1][CH] = {};
     constexpr int Q = CH / 4;
-    float4 *const mine = param_lds + threadIdx.x * sums_lds_of(CH, NC, BIAS);
+    float4 *const mine = param_lds + threadIdx.x * sums_lds_of(CH, NC);
     auto put = [&](int v, int k, const float (&x)[CH]) {
 #pragma unroll
         for (int q = 0; q < Q; ++q) mine[(v * NC + k) * Q + q] = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
@@ -374,7 +374,7 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
             x[4 * q] = f.x; x[4 * q + 1] = f.y; x[4 * q + 2] = f.z; x[4 * q + 3] = f.w;
         }
     };
-    enum { L_W1, L_W2, L_GATE, L_B1 };
+    enum { L_W1, L_W2, L_GATE };
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
         float x[CH];
@@ -382,7 +382,6 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
         put(L_W1, k, x);
         load_param<CUTS, T, CH>(A, G_PRE_W, 0, 0, at[k], 1.f, x);
         put(L_W2, k, x);
-        if constexpr (BIAS) { load_param<CUTS, T, CH>(A, G_POST_B, 0, 0, at[k], 0.f, x); put(L_B1, k, x); }
     }
     Words<R, CH> rx[NC], rd[NC];
     Words<T, CH> ru[NC], ry[NC];
@@ -505,7 +504,7 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
 #pragma unroll
                 for (int i = 0; i < CH; ++i) x[i] = w1[i] * sum_dy[k][i];
                 if constexpr (BIAS) {
-                    get(L_B1, k, w1);
+                    load_param<CUTS, T, CH>(A, G_POST_B, 0, 0, at[k], 0.f, w1);
 #pragma unroll
                     for (int i = 0; i < CH; ++i) { x[i] += w1[i] * sum_d[k][i]; g[i] *= sum_d[k][i]; sum_d[k][i] = 0.f; }
                     if (!first) {
@@ -541,13 +540,14 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
     }
 }
 
-// the chunks' sums added up, always in the same order: 64 columns a workgroup, its 16 wavefronts take every 16th chunk
+// the chunks' sums added up, always in the same order: a workgroup has COLS columns, and 1,024 / COLS threads of it share a column's chunks
 struct Joined { const float *from[G_VECTORS]; float *to[G_VECTORS]; uint64_t count[G_VECTORS]; uint32_t n; uint64_t gate_chunks, gate_out_st; };
-__global__ __launch_bounds__(1024) void k_norm_join(Joined J, uint32_t width, uint32_t tiles) {
-    __shared__ float lds[16][64];
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+template <int COLS> __global__ __launch_bounds__(1024) void k_norm_join(Joined J, uint32_t width, uint32_t tiles) {
+    constexpr uint32_t SHARE = 1024 / COLS;
+    __shared__ float lds[SHARE][COLS];
+    const uint32_t lane = threadIdx.x % COLS, part = threadIdx.x / COLS;
     const uint64_t job = blockIdx.x / tiles;
-    const uint32_t col = blockIdx.x % tiles * 64u + lane;
+    const uint32_t col = blockIdx.x % tiles * COLS + lane;
     // the vectors first, then the gates one by one (J.gate_chunks each)
     const uint32_t v = job < J.n ? (uint32_t)job : J.n;
     const float *from = J.from[v];
@@ -556,21 +556,21 @@ __global__ __launch_bounds__(1024) void k_norm_join(Joined J, uint32_t width, ui
     if (job >= J.n) { from += (job - J.n) * J.gate_chunks * width; to += (job - J.n) * J.gate_out_st; count = J.gate_chunks; }
     float s = 0.f;
     if (col < width) {
-        uint64_t c = wave;
-        for (; c + 112 < count; c += 128) {                     // eight under way at once
-            float v[8];
+        uint64_t c = part;
+        for (; c + 7 * SHARE < count; c += 8 * SHARE) {         // eight under way at once
+            float x[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = from[(c + 16 * i) * width + col];
+            for (int i = 0; i < 8; ++i) x[i] = from[(c + SHARE * i) * width + col];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s += v[i];
+            for (int i = 0; i < 8; ++i) s += x[i];
         }
-        for (; c < count; c += 16) s += from[c * width + col];
+        for (; c < count; c += SHARE) s += from[c * width + col];
     }
-    lds[wave][lane] = s;
+    lds[part][lane] = s;
     __syncthreads();
-    if (wave) return;
-#pragma unroll
-    for (int w = 1; w < 16; ++w) s += lds[w][lane];
+    if (threadIdx.x >= COLS) return;
+#pragma unroll 16
+    for (uint32_t w = 1; w < SHARE; ++w) s += lds[w][lane];
     if (col < width) to[col] = s;
 }
 
@@ -610,19 +610,19 @@ template <typename T, typename R> void launch_rows(hipStream_t st, const NormArg
 }
 // How the rows are held where their sums are taken along; nc 0: too wide for a lane's registers or a compute unit's LDS, rows and sums
 // are two passes.
-Shape sums_shape_of(uint32_t width, int ch, bool bias) {
+Shape sums_shape_of(uint32_t width, int ch) {
     const int per = 8 / ch;                                     // vectors of eight elements
     for (int n8 = 1; n8 <= 2; ++n8)
         if (width <= 512u * n8) return Shape{n8 * per, 256, 4, true};
     const int n8 = width <= 8192u ? 1 : 2;
     const uint32_t threads = (width + 8 * n8 * 64 - 1) / (8 * n8 * 64) * 64;
-    if (threads > (n8 == 1 ? 1024u : 768u) || threads * sums_lds_of(8, n8, bias) * 16 > 163840u - 1024u) return Shape{0, 0, 0, false};
+    if (threads > (n8 == 1 ? 1024u : 768u) || threads * sums_lds_of(8, n8) * 16 > 163840u - 1024u) return Shape{0, 0, 0, false};
     return Shape{n8 * per, threads, 1, false};
 }
 template <typename T, typename R, int NC, int MAXT> int32_t launch_fused_nc(rk_ctx *ctx, const NormSums &S, const Shape &H, bool bias) {
     constexpr int CH = chunk_of<T, R>();
     const uint32_t blocks = (uint32_t)((S.C.n + H.rows_per_wg - 1) / H.rows_per_wg);
-    const uint32_t lds = H.threads * sums_lds_of(CH, NC, bias) * 16;
+    const uint32_t lds = H.threads * sums_lds_of(CH, NC) * 16;
     auto go = [&](auto cuts, auto with_bias) -> int32_t {
         const auto kernel = k_norm_backward_sums<decltype(cuts)::value, T, R, CH, NC, MAXT, decltype(with_bias)::value>;
         if (lds > 65536u - 1024u) RK_HIP(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
@@ -766,12 +766,12 @@ extern "C" int32_t rk_norm_backward(rk_ctx *ctx, const rk_norm_block *block, uin
     Joined J{};
     uint64_t join_jobs = 0;
     const bool bias = block->post_bias || out[G_PRE_B];
-    const Shape H = sums_shape_of(width, type == RK_F32 ? 4 : 8, bias);
+    const Shape H = sums_shape_of(width, type == RK_F32 ? 4 : 8);
     if (any) {
-        // a chunk for every workgroup (wavefront) that fits the chip at once, of four rows at least
-        const uint64_t at_once = H.per_wave ? 4096 : H.nc && H.threads <= 512 ? 512 : 256;
+        // a chunk for every workgroup (wavefront) that fits the chip at once
+        const uint64_t at_once = H.per_wave ? 2048 : H.nc && H.threads <= 512 ? 512 : 256;
         uint64_t rows = (n_rows + at_once - 1) / at_once;
-        if (rows < 4) rows = 4;
+        if (rows < 1) rows = 1;
         const bool gates = A.gate_rows != 0;
         if (!gates) {
             S.C = Chunks{rows, 0, (n_rows + rows - 1) / rows};
@@ -819,8 +819,11 @@ extern "C" int32_t rk_norm_backward(rk_ctx *ctx, const rk_norm_block *block, uin
         }
     }
     if (join_jobs) {
-        const uint32_t tiles = (width + 63) / 64;
-        k_norm_join<<<(uint32_t)(join_jobs * tiles), 1024, 0, ctx->stream>>>(J, width, tiles);
+        // 64 columns a workgroup, or 16 where that would leave compute units without one
+        const bool narrow = join_jobs * ((width + 63) / 64) < 256;
+        const uint32_t tiles = narrow ? (width + 15) / 16 : (width + 63) / 64;
+        if (narrow) k_norm_join<16><<<(uint32_t)(join_jobs * tiles), 1024, 0, ctx->stream>>>(J, width, tiles);
+        else k_norm_join<64><<<(uint32_t)(join_jobs * tiles), 1024, 0, ctx->stream>>>(J, width, tiles);
         RK_CHECK_LAUNCH(ctx, "k_norm_join");
     }
     return RK_OK;

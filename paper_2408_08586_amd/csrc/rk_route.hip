@@ -502,12 +502,10 @@ extern "C" int32_t rk_route_forward(rk_ctx *ctx, const rk_router *router, uint64
         return rk_fail(ctx, RK_ERR_INVALID_ARG, "an output is null or misaligned");
     RK_HIP(ctx, hipSetDevice(ctx->device));
     A.mask = mask; A.expert = expert; A.weight = weight; A.lse = lse; A.counts = counts; A.prob_sum = prob_sum; A.tokens = tokens; A.loss = loss;
-    // two workgroups a compute unit share the tokens, each at least as many as its wavefronts hold at once; few tokens are one's
+    // up to four workgroups a compute unit share the tokens, each in rounds of as many as its wavefronts hold; few tokens are one's
     const uint64_t at_once = RT_WAVES * 64 / lanes_of(A.n_experts);
-    uint64_t chunk = (n_tokens + 511) / 512;
-    if (chunk < at_once) chunk = at_once;
-    A.per_group = n_tokens ? (A.group_tokens + chunk - 1) / chunk : 0;
-    A.chunk = A.per_group ? (A.group_tokens + A.per_group - 1) / A.per_group : 0;
+    A.chunk = (n_tokens + 1024 * at_once - 1) / (1024 * at_once) * at_once;
+    A.per_group = n_tokens ? (A.group_tokens + A.chunk - 1) / A.chunk : 0;
     A.tiles = (A.n_experts + 63) / 64;
     const uint64_t blocks = A.per_group * (n_tokens ? A.n_groups : 0);
     if (blocks == 0) {

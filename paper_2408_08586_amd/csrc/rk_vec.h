@@ -19,15 +19,18 @@ template <typename T> struct Row {
         : buf(__builtin_amdgcn_make_buffer_rsrc(const_cast<T *>((const T *)base + row * stride), 0, (int)(base ? width * (uint32_t)sizeof(T) : 0u), 0x00027000)) {}
 };
 // A lane's N elements of a row, from element `first` on.  Those that are all inside go as whole vectors, whatever their alignment;
-// the ones that the row's end cuts go one by one (CUTS: the width is no multiple of N, there is such a vector).
+// the one that the row's end cuts goes in the pieces that its length has in base 2 (CUTS: the width is no multiple of N, there is such
+// a vector, and it has width % N elements: the same for all rows, so that the pieces' places are known to the scalar unit).
 constexpr uint32_t ROW_NOWHERE = 1u << 29, ROW_MAX = 1u << 28;      // elements: behind every row; the widest row
 struct Place {
     uint32_t whole, cut;            // where the vector begins, or ROW_NOWHERE
     int32_t valid;
+    uint32_t tail;                  // width % n
     bool cut_here;                  // some lane of the wavefront has one that is cut: only these take the long way
     __device__ __forceinline__ Place() {}
     __device__ __forceinline__ Place(uint32_t first, uint32_t width, int n) {
         valid = (int32_t)width - (int32_t)first;
+        tail = width % (uint32_t)n;
         whole = valid >= n ? first : ROW_NOWHERE;
         cut = valid > 0 && valid < n ? first : ROW_NOWHERE;
         cut_here = __builtin_amdgcn_ballot_w64(cut != ROW_NOWHERE) != 0;
@@ -51,10 +54,41 @@ template <bool CUTS, typename T, int N, int HINT = KEEP> __device__ __forceinlin
     Words<T, N> w = fetch_at<T, N, HINT>(row, p.whole);
     if (CUTS && p.cut_here) {
         const uint32_t from = p.cut * (uint32_t)sizeof(T);
+        if constexpr (sizeof(T) == 4) {
+            static_assert(N == 4 || N == 8, "");
+            constexpr uint32_t HALF = N / 2;
+            uint32_t at = 0;
+            if (N == 8 && (p.tail & 4u)) {
+                const Vec<uint32_t, 4> x = __builtin_amdgcn_raw_buffer_load_b128(row.buf, from, 0, 0);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if constexpr (sizeof(T) == 4) w[i] |= __builtin_amdgcn_raw_buffer_load_b32(row.buf, from + 4u * i, 0, 0);
-            else w[i / 2] |= (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(row.buf, from + 2u * i, 0, 0) << (i & 1 ? 16 : 0);
+                for (int i = 0; i < 4; ++i) w[i] |= x[i];
+                at = HALF;
+            }
+            if (p.tail & 2u) {
+                const Vec<uint32_t, 2> x = __builtin_amdgcn_raw_buffer_load_b64(row.buf, from + 4u * at, 0, 0);
+#pragma unroll
+                for (uint32_t i = 0; i < 2; ++i) { if (at) w[(HALF + i) % N] |= x[i]; else w[i] |= x[i]; }
+            }
+            if (p.tail & 1u) {
+                const uint32_t x = __builtin_amdgcn_raw_buffer_load_b32(row.buf, from + 4u * (p.tail & 6u), 0, 0);
+#pragma unroll
+                for (uint32_t i = 0; i < N; i += 2) w[i] |= (p.tail & 6u) == i ? x : 0u;
+            }
+        } else {
+            static_assert(N == 8, "");
+            if (p.tail & 4u) {
+                const Vec<uint32_t, 2> x = __builtin_amdgcn_raw_buffer_load_b64(row.buf, from, 0, 0);
+                w[0] |= x[0]; w[1] |= x[1];
+            }
+            if (p.tail & 2u) {
+                const uint32_t x = __builtin_amdgcn_raw_buffer_load_b32(row.buf, from + 2u * (p.tail & 4u), 0, 0);
+                w[0] |= p.tail & 4u ? 0u : x; w[2] |= p.tail & 4u ? x : 0u;
+            }
+            if (p.tail & 1u) {
+                const uint32_t x = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(row.buf, from + 2u * (p.tail & 6u), 0, 0);
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) w[i] |= (p.tail & 6u) == 2u * i ? x : 0u;
+            }
         }
     }
     return w;
@@ -91,10 +125,41 @@ template <bool CUTS, typename T, int N, int HINT = KEEP> __device__ __forceinlin
     store_at<T, N, HINT>(row, p.whole, w);
     if (CUTS && p.cut_here) {
         const uint32_t from = p.cut * (uint32_t)sizeof(T);
+        if constexpr (sizeof(T) == 4) {
+            constexpr uint32_t HALF = N / 2;
+            uint32_t at = 0;
+            if (N == 8 && (p.tail & 4u)) {
+                Vec<uint32_t, 4> x;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(w[i], row.buf, from + 4u * i, 0, 0);
-            else __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(i & 1 ? w[i / 2] >> 16 : w[i / 2]), row.buf, from + 2u * i, 0, 0);
+                for (int i = 0; i < 4; ++i) x[i] = w[i];
+                __builtin_amdgcn_raw_buffer_store_b128(x, row.buf, from, 0, 0);
+                at = HALF;
+            }
+            if (p.tail & 2u) {
+                Vec<uint32_t, 2> x;
+#pragma unroll
+                for (uint32_t i = 0; i < 2; ++i) x[i] = at ? w[(HALF + i) % N] : w[i];
+                __builtin_amdgcn_raw_buffer_store_b64(x, row.buf, from + 4u * at, 0, 0);
+            }
+            if (p.tail & 1u) {
+                uint32_t x = w[0];
+#pragma unroll
+                for (uint32_t i = 2; i < N; i += 2) x = (p.tail & 6u) == i ? w[i] : x;
+                __builtin_amdgcn_raw_buffer_store_b32(x, row.buf, from + 4u * (p.tail & 6u), 0, 0);
+            }
+        } else {
+            if (p.tail & 4u) {
+                Vec<uint32_t, 2> x;
+                x[0] = w[0]; x[1] = w[1];
+                __builtin_amdgcn_raw_buffer_store_b64(x, row.buf, from, 0, 0);
+            }
+            if (p.tail & 2u) __builtin_amdgcn_raw_buffer_store_b32(p.tail & 4u ? w[2] : w[0], row.buf, from + 2u * (p.tail & 4u), 0, 0);
+            if (p.tail & 1u) {
+                uint32_t x = w[0];
+#pragma unroll
+                for (uint32_t i = 1; i < 4; ++i) x = (p.tail & 6u) == 2u * i ? w[i] : x;
+                __builtin_amdgcn_raw_buffer_store_b16((uint16_t)x, row.buf, from + 2u * (p.tail & 6u), 0, 0);
+            }
         }
     }
 }
