@@ -147,8 +147,8 @@ __device__ __forceinline__ void sum_huge(const Row<T> &row, uint32_t begin, uint
 }
 
 // What a row's teacher and label say: a thread holds kept logits tid, tid + THREADS, ...
-template <int THREADS> struct Wanted {
-    static constexpr int N = (int)RK_MAX_TEACHER_LOGITS / THREADS;
+template <int THREADS, int MOST = (int)RK_MAX_TEACHER_LOGITS> struct Wanted {
+    static constexpr int N = MOST / THREADS;
     int32_t at[N], label;
     float t[N], s[N], label_s;
     // what teacher and label name; then, when that is there, the student's logits at their places.  Loads return in their order: what is
@@ -235,12 +235,12 @@ template <typename T, int SUMS> struct Slope {
 };
 // The teacher's shares q of the kept logits, by their places, for all threads; then t becomes what those of the same place have
 // together (indices may repeat), and label_q what those at the label have, in its thread.
-struct Shares { float4 q[RK_MAX_TEACHER_LOGITS / 4]; int4 at[RK_MAX_TEACHER_LOGITS / 4]; };
-template <int THREADS> __device__ __forceinline__ float share_wanted(const DistillArgs &A, Wanted<THREADS> &W, float t_sum, Shares &lds) {
+template <int MOST> struct Shares { float4 q[MOST / 4]; int4 at[MOST / 4]; };
+template <int THREADS, int MOST> __device__ __forceinline__ float share_wanted(const DistillArgs &A, Wanted<THREADS, MOST> &W, float t_sum, Shares<MOST> &lds) {
     const float inv_sum = t_sum != 0.f ? 1.f / t_sum : 0.f;
     const uint32_t K = A.kd > 0.f ? A.top_k : 0u;
 #pragma unroll
-    for (int n = 0; n < Wanted<THREADS>::N; ++n) {
+    for (int n = 0; n < Wanted<THREADS, MOST>::N; ++n) {
         const uint32_t k = threadIdx.x + n * THREADS;
         if (k < ((K + 3u) & ~3u)) {                     // (behind the last one there is none: at is -1)
             ((float *)lds.q)[k] = W.t[n] * inv_sum;
@@ -259,19 +259,19 @@ template <int THREADS> __device__ __forceinline__ float share_wanted(const Disti
         return mass;
     };
 #pragma unroll
-    for (int n = 0; n < Wanted<THREADS>::N; ++n)
+    for (int n = 0; n < Wanted<THREADS, MOST>::N; ++n)
         if (W.at[n] >= 0) W.t[n] = together(W.at[n]);
     return threadIdx.x == THREADS - 1 && W.label >= 0 ? together(W.label) : 0.f;
 }
 // where teacher or label have something in [begin, end): the whole value, once more (equal indices get equal values)
-template <int THREADS, typename T, int SUMS>
-__device__ __forceinline__ void write_wanted(const Wanted<THREADS> &W, const Slope<T, SUMS> &slope, T *out, uint32_t begin, uint32_t end, float label_q) {
+template <int THREADS, int MOST, typename T, int SUMS>
+__device__ __forceinline__ void write_wanted(const Wanted<THREADS, MOST> &W, const Slope<T, SUMS> &slope, T *out, uint32_t begin, uint32_t end, float label_q) {
     auto again = [&](int32_t i, float s, float mass) {
         if ((uint32_t)i < begin || (uint32_t)i >= end) return;
         out[i] = (T)((is_huge(slope.top) ? slope.template of<true>(s) : slope(s)) - slope.ft * mass - (i == W.label ? slope.f1 : 0.f));
     };
 #pragma unroll
-    for (int n = 0; n < Wanted<THREADS>::N; ++n)
+    for (int n = 0; n < Wanted<THREADS, MOST>::N; ++n)
         if (W.at[n] >= 0) again(W.at[n], W.s[n], W.t[n]);
     if (threadIdx.x == THREADS - 1 && W.label >= 0) again(W.label, W.label_s, label_q);
 }
@@ -288,7 +288,7 @@ __device__ __forceinline__ void write_huge(const Row<T> &from, const Row<T> &to,
 }
 template <bool CUTS, int THREADS, typename T, int CH, int SUMS>
 __device__ __forceinline__ void write_gradient(const DistillArgs &A, const Row<T> &from, const Row<T> &to, T *out, uint32_t begin, uint32_t end, const Slope<T, SUMS> &slope,
-                                               Wanted<THREADS> &W, float t_sum, Shares &lds) {
+                                               Wanted<THREADS> &W, float t_sum, Shares<(int)RK_MAX_TEACHER_LOGITS> &lds) {
     const float label_q = share_wanted(A, W, t_sum, lds);
     if (is_huge(slope.top)) write_huge<CUTS, THREADS, T, CH, SUMS>(from, to, begin, end, slope);
     else stream_row<CUTS, THREADS, T, CH, STREAM>(from, begin, end,
@@ -335,16 +335,16 @@ __device__ __forceinline__ void keep_row(const DistillArgs &A, uint64_t r, const
 
 // A workgroup a row: its sums, its loss and, if there is a d_student, its gradient.  Of what a thread reads, its first NR vectors stay in
 // registers and its next NL in LDS until then; only what is beyond them is read again.
-template <bool CUTS, int THREADS, int NR, int NL, typename T, int CH, int SUMS>
+template <bool CUTS, int THREADS, int NR, int NL, int MOST, typename T, int CH, int SUMS>
 __global__ __launch_bounds__(THREADS, 8) void k_distill_rows(DistillArgs A) {
     extern __shared__ float4 kept_lds[];
     __shared__ float4 red[16];
-    __shared__ Shares lds;
+    __shared__ Shares<MOST> lds;
     constexpr uint32_t STEP = THREADS * CH;
     const uint64_t r = blockIdx.x;
     const Row<T> from(A.student, r, A.st, A.vocab), to(A.d_student, r, A.d_st, A.vocab);
     const float weight = A.row_weight ? A.row_weight[r] : 1.f;
-    Wanted<THREADS> W;
+    Wanted<THREADS, MOST> W;
     // whole rounds of vectors, and one that the row's end cuts off
     const uint32_t whole = A.vocab / STEP, first = threadIdx.x * CH;
     const Place last(first + whole * STEP, A.vocab, CH);
@@ -523,7 +523,7 @@ template <typename T, int SUMS> __global__ __launch_bounds__(64 * JOIN_WAVES) vo
 template <bool CUTS, int THREADS, typename T, int CH, int SUMS>
 __global__ __launch_bounds__(THREADS) void k_distill_gradient(DistillArgs A) {
     __shared__ float4 red[16];
-    __shared__ Shares lds;
+    __shared__ Shares<(int)RK_MAX_TEACHER_LOGITS> lds;
     const uint64_t r = blockIdx.x / A.slices;
     const uint32_t slice = blockIdx.x - (uint32_t)r * A.slices, begin = slice * A.slice;
     const uint32_t end = slice + 1 == A.slices ? A.vocab : begin + A.slice;
@@ -623,10 +623,12 @@ template <typename T, int SUMS> hipError_t launch(hipStream_t st, const DistillA
     auto rows = [&](auto cuts) {
         constexpr bool CUTS = decltype(cuts)::value;
         const uint32_t vectors = (A.vocab + CH - 1) / CH, n = (uint32_t)A.n_rows;
-        if (vectors <= 256 * 8) k_distill_rows<CUTS, 256, 8, 0, T, CH, SUMS><<<n, 256, 0, st>>>(A);
-        else if (vectors <= 512 * 8) k_distill_rows<CUTS, 512, 8, 0, T, CH, SUMS><<<n, 512, 0, st>>>(A);
+        constexpr int MOST = (int)RK_MAX_TEACHER_LOGITS;
+        if (vectors <= 128 * 4 && A.top_k <= 256) k_distill_rows<CUTS, 128, 4, 0, 256, T, CH, SUMS><<<n, 128, 0, st>>>(A);
+        else if (vectors <= 256 * 8) k_distill_rows<CUTS, 256, 8, 0, MOST, T, CH, SUMS><<<n, 256, 0, st>>>(A);
+        else if (vectors <= 512 * 8) k_distill_rows<CUTS, 512, 8, 0, MOST, T, CH, SUMS><<<n, 512, 0, st>>>(A);
         else {
-            const auto kernel = k_distill_rows<CUTS, 1024, DS_REGISTERS, DS_LDS, T, CH, SUMS>;
+            const auto kernel = k_distill_rows<CUTS, 1024, DS_REGISTERS, DS_LDS, MOST, T, CH, SUMS>;
             const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, DS_LDS * 1024 * 16);
             if (e != hipSuccess) return e;
             kernel<<<n, 1024, DS_LDS * 1024 * 16, st>>>(A);
@@ -672,7 +674,7 @@ int32_t run(rk_ctx *ctx, uint32_t type, DistillArgs &A, bool want_loss, bool wan
     if (want_loss && A.n_rows) {
         // Rows that would leave compute units without one are cut into slices: fewer than DS_FEW of them, or, where the loss is all and
         // the slices need no second reading, up to four times as many.
-        cut_rows(A, want_grad ? 512 : 2048, want_grad ? 4096 : 8192);
+        cut_rows(A, want_grad ? 512 : 4096, want_grad ? 4096 : 8192);
         if (A.slices > 1 && A.n_rows < (want_grad ? DS_FEW : 4 * DS_FEW)) {
             const size_t parts = (size_t)(A.n_rows * A.slices);
             float4 *room;

@@ -55,10 +55,10 @@ __device__ __forceinline__ void load_param(const NormArgs &A, int which, uint64_
     }
 }
 
-// Mean and sum of squares about it of the elements in v.  Each wavefront takes its squares about its own mean, and the parts
+// Mean and sum of squares about it of a lane's elements v(k, i).  Each wavefront takes its squares about its own mean, and the parts
 // are joined by what the means differ: nothing is cancelled, and one exchange is enough.
-template <int CH, int NC>
-__device__ __forceinline__ void row_stats(RowGroup &G, const float (&v)[NC][CH], uint32_t width, const Place (&at)[NC], uint32_t how, float eps,
+template <int CH, int NC, typename V>
+__device__ __forceinline__ void row_stats(RowGroup &G, V v, uint32_t width, const Place (&at)[NC], uint32_t how, float eps,
                                           float &mean, float &r) {
     mean = 0.f; r = 1.f;
     if (how == RK_NORM_NONE) return;
@@ -67,7 +67,7 @@ __device__ __forceinline__ void row_stats(RowGroup &G, const float (&v)[NC][CH],
 #pragma unroll
         for (int k = 0; k < NC; ++k)
 #pragma unroll
-            for (int i = 0; i < CH; ++i) q += v[k][i] * v[k][i];
+            for (int i = 0; i < CH; ++i) q += v(k, i) * v(k, i);
         G.two(q, none);
         r = 1.0f / sqrtf(q / (float)width + eps);
         return;
@@ -78,7 +78,7 @@ __device__ __forceinline__ void row_stats(RowGroup &G, const float (&v)[NC][CH],
         const int32_t valid = at[k].valid;
         n += (float)(valid < 0 ? 0 : valid < CH ? valid : CH);
 #pragma unroll
-        for (int i = 0; i < CH; ++i) s += v[k][i];          // those behind the row's end are zero
+        for (int i = 0; i < CH; ++i) s += v(k, i);          // those behind the row's end are zero
     }
     s = wave_sum(s); n = wave_sum(n);
     const float own = n > 0.f ? s / n : 0.f;
@@ -86,7 +86,7 @@ __device__ __forceinline__ void row_stats(RowGroup &G, const float (&v)[NC][CH],
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
 #pragma unroll
-        for (int i = 0; i < CH; ++i) { const float d = i < at[k].valid ? v[k][i] - own : 0.f; q += d * d; }
+        for (int i = 0; i < CH; ++i) { const float d = i < at[k].valid ? v(k, i) - own : 0.f; q += d * d; }
     }
     q = wave_sum(q);
     if (G.nw > 1) {
@@ -104,9 +104,14 @@ __device__ __forceinline__ void row_stats(RowGroup &G, const float (&v)[NC][CH],
     r = 1.0f / sqrtf(q / (float)width + eps);
 }
 
+// A lane's vectors are its thread's number and those a stride further.  Only the last of them can be the one that the row's end cuts, since a
+// row takes as few threads as hold it (in 32 bits, where vectors are taken in pairs, or the last but one, of narrow rows the first).
 template <int CH, int NC> __device__ __forceinline__ void places(Place (&at)[NC], uint32_t tid, uint32_t threads, uint32_t width) {
 #pragma unroll
-    for (int k = 0; k < NC; ++k) at[k] = Place((tid + k * threads) * CH, width, CH);
+    for (int k = 0; k < NC; ++k) {
+        at[k] = Place((tid + k * threads) * CH, width, CH);
+        if (k + 1 < NC && !(CH == 4 && (NC == 2 || (NC == 4 && k == 2)))) at[k].cut_here = false;
+    }
 }
 
 // The rows of a workgroup: one (its wavefronts share it), or one per wavefront for rows that a wavefront holds.
@@ -127,18 +132,19 @@ __global__ __launch_bounds__(MAXT) void k_norm_forward(NormArgs A, bool per_wave
     if (!P.there) return;                                   // (per_wave only: whole wavefronts, no barrier follows)
     Place at[NC];
     places<CH, NC>(at, P.tid, P.threads, A.width);
-    float x[NC][CH], v[NC][CH];
+    Words<R, CH> wx[NC];
+    Words<T, CH> wy[NC];
     {
-        const Row<R> rx(A.x, P.row, A.x_st, A.width);
         const Row<T> ry(A.y, P.row, A.y_st, A.width);
+        const Row<R> rx(A.x, P.row, A.x_st, A.width);
 #pragma unroll
-        for (int k = 0; k < NC; ++k) {
-            load_row<CUTS, R, CH>(rx, at[k], x[k]);
-            load_row<CUTS, T, CH>(ry, at[k], v[k]);
-        }
+        for (int k = 0; k < NC; ++k) wy[k] = fetch_row<CUTS, T, CH>(ry, at[k]);
+#pragma unroll
+        for (int k = 0; k < NC; ++k) wx[k] = fetch_row<CUTS, R, CH>(rx, at[k]);
     }
-    float my = 0.f, ry = 1.f, mx, rx;
-    row_stats<CH, NC>(G, v, A.width, at, A.post, A.post_eps, my, ry);
+    float my, ry, mx, rx;
+    row_stats<CH, NC>(G, [&](int k, int i) { return element<T>(wy[k], i); }, A.width, at, A.post, A.post_eps, my, ry);
+    float x[NC][CH];
     const uint64_t gate = A.gate_rows ? P.row / A.gate_rows : 0;
     const Row<R> xo(A.xo, P.row, A.xo_st, A.width);
 #pragma unroll
@@ -149,12 +155,12 @@ __global__ __launch_bounds__(MAXT) void k_norm_forward(NormArgs A, bool per_wave
         load_param<CUTS, T, CH>(A, G_GATE, gate, A.gate_st, at[k], 1.f, g);
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            const float n = (v[k][i] - my) * ry * w[i] + b[i];
-            x[k][i] = i < at[k].valid ? A.scale * x[k][i] + g[i] * n : 0.f;
+            const float n = (element<T>(wy[k], i) - my) * ry * w[i] + b[i];
+            x[k][i] = i < at[k].valid ? A.scale * element<R>(wx[k], i) + g[i] * n : 0.f;
         }
         store_row<CUTS, R, CH, STREAM>(xo, at[k], x[k]);
     }
-    row_stats<CH, NC>(G, x, A.width, at, A.pre, A.pre_eps, mx, rx);
+    row_stats<CH, NC>(G, [&](int k, int i) { return x[k][i]; }, A.width, at, A.pre, A.pre_eps, mx, rx);
     if (P.tid == 0) reinterpret_cast<float4 *>(A.stats)[P.row] = make_float4(my, ry, mx, rx);
     if (A.pre == RK_NORM_NONE) return;
     const Row<T> u(A.u, P.row, A.u_st, A.width);
@@ -341,54 +347,35 @@ __global__ __launch_bounds__(SUM_THREADS) void k_norm_sums(NormSums S, uint32_t 
 // banks
 constexpr uint32_t sums_lds_of(int ch, int nc) { return (uint32_t)(3 * nc * ch / 4) | 1u; }
 
-// Rows back and the sums over them in one pass: a workgroup (or, of rows that a wavefront holds, a wavefront) takes a chunk of
-// rows, and every lane keeps the sums of its columns in registers.  The next row's x_out and du are on their way while this row's
-// first norm is summed, its dx_out and y while the second is.  Weights and gate, which every row needs, lie in LDS: each lane reads only
-// what it wrote itself, and registers are left for the sums.  Of the vectors behind the gate only sum D y^ and sum D are kept:
+// Rows back and the sums over them in one pass: a workgroup takes a chunk of rows and every lane keeps the sums of its columns in
+// registers.  Rows that a wavefront holds are shared out to the workgroup's four, which add their sums up at the end, or (`alone`: with
+// gates of rows) are a chunk to each of them.  The next row's x_out and du are on their way while this row's first norm is summed,
+// its dx_out and y while the second is; LEAN has half of that under way, for rows that take all registers.  Weights and gate,
+// which every row needs, lie in LDS: each lane reads only what it wrote itself.  Of the vectors behind the gate only sum D y^ and sum D are kept:
 //     d post_weight = gate sum D y^,  d post_bias = gate sum D,  d gate = post_weight sum D y^ + post_bias sum D
 // for rows of one gate.  A chunk with several gates' rows adds its first two up in its place in memory, gate by gate.
 template <bool CUTS, typename T, typename R, int CH, int NC, int MAXT, bool BIAS>
-__global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool per_wave) {
+__global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool per_wave, bool alone) {
+    constexpr bool LEAN = MAXT == 768 && (BIAS || CUTS || sizeof(R) == 4);
     extern __shared__ float4 param_lds[];
     __shared__ float lds[96];
     const NormArgs &A = S.A;
     RowGroup G;
-    const RowOf P = row_of(S.C.n, per_wave, G, lds);            // (its "row" is the chunk)
-    if (!P.there) return;
-    const uint64_t chunk = P.row;
+    const RowOf P = row_of(S.C.n, per_wave, G, lds);            // (its "row" is the chunk of one that is alone)
+    if (!P.there && alone) return;
+    const bool shared = per_wave && !alone;
+    const uint64_t chunk = shared ? blockIdx.x : P.row;
     uint64_t r0, r1;
     chunk_rows(A, S.C, chunk, r0, r1);
+    const uint64_t stride = shared ? blockDim.x >> 6 : 1, begin = r0 + (shared ? G.wave : 0u);
     Place at[NC];
     places<CH, NC>(at, P.tid, P.threads, A.width);
-    float sum_dy[NC][CH] = {}, acc_w2[NC][CH] = {}, sum_d[BIAS ? NC : 1][CH] = {}, acc_b2[BIAS ? NC : 1][CH] = {};
-    constexpr int Q = CH / 4;
-    float4 *const mine = param_lds + threadIdx.x * sums_lds_of(CH, NC);
-    auto put = [&](int v, int k, const float (&x)[CH]) {
-#pragma unroll
-        for (int q = 0; q < Q; ++q) mine[(v * NC + k) * Q + q] = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
-    };
-    auto get = [&](int v, int k, float (&x)[CH]) {
-#pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            const float4 f = mine[(v * NC + k) * Q + q];
-            x[4 * q] = f.x; x[4 * q + 1] = f.y; x[4 * q + 2] = f.z; x[4 * q + 3] = f.w;
-        }
-    };
-    enum { L_W1, L_W2, L_GATE };
-#pragma unroll
-    for (int k = 0; k < NC; ++k) {
-        float x[CH];
-        load_param<CUTS, T, CH>(A, G_POST_W, 0, 0, at[k], 1.f, x);
-        put(L_W1, k, x);
-        load_param<CUTS, T, CH>(A, G_PRE_W, 0, 0, at[k], 1.f, x);
-        put(L_W2, k, x);
-    }
     Words<R, CH> rx[NC], rd[NC];
     Words<T, CH> ru[NC], ry[NC];
     float4 st_next = make_float4(0.f, 1.f, 0.f, 1.f);
     auto fetch_first = [&](uint64_t r) {
         const bool there = r < r1;                              // (behind the chunk: a row of no elements)
-        st_next = reinterpret_cast<const float4 *>(A.stats)[there ? r : r0];
+        if (there) st_next = reinterpret_cast<const float4 *>(A.stats)[r];
         const Row<R> x(there ? A.x : nullptr, r, A.x_st, A.width);
         const Row<T> u(there ? A.du : nullptr, r, A.du_st, A.width);
 #pragma unroll
@@ -407,13 +394,67 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
             ry[k] = fetch_row<CUTS, T, CH, STREAM>(y, at[k]);
         }
     };
-    if (r0 < r1) { fetch_first(r0); fetch_second(r0); }
-    uint64_t gate = ~0ull, gate_end = 0;
+    fetch_first(begin);
+    if (!LEAN) fetch_second(begin);
+    constexpr int Q = CH / 4;
+    float4 *const mine = param_lds + threadIdx.x * sums_lds_of(CH, NC);
+    auto put = [&](int v, int k, const float (&x)[CH]) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q) mine[(v * NC + k) * Q + q] = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+    };
+    auto get = [&](int v, int k, float (&x)[CH]) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            const float4 f = mine[(v * NC + k) * Q + q];
+            x[4 * q] = f.x; x[4 * q + 1] = f.y; x[4 * q + 2] = f.z; x[4 * q + 3] = f.w;
+        }
+    };
+    enum { L_W1, L_W2, L_GATE };
+    uint64_t gate = A.gate_rows ? begin / A.gate_rows : 0, gate_end = A.gate_rows ? (gate + 1) * A.gate_rows : ~0ull;
+    // the vectors' parts, all under way before the first is waited for
+    auto vectors = [&](auto p) {
+        typedef decltype(p) V;
+        Words<V, CH> w[3][NC];
+        const Row<V> w1(A.vec[G_POST_W], 0, 0, A.width), w2(A.vec[G_PRE_W], 0, 0, A.width), g(begin < r1 ? A.vec[G_GATE] : nullptr, gate, A.gate_st, A.width);
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+            w[L_W1][k] = fetch_row<CUTS, V, CH>(w1, at[k]);
+            w[L_W2][k] = fetch_row<CUTS, V, CH>(w2, at[k]);
+            w[L_GATE][k] = fetch_row<CUTS, V, CH>(g, at[k]);
+        }
+        const bool have[3] = {A.vec[G_POST_W] != nullptr, A.vec[G_PRE_W] != nullptr, A.vec[G_GATE] != nullptr};
+#pragma unroll
+        for (int v = 0; v < 3; ++v)
+#pragma unroll
+            for (int k = 0; k < NC; ++k) {
+                float x[CH];
+#pragma unroll
+                for (int i = 0; i < CH; ++i) x[i] = have[v] ? element<V>(w[v][k], i) : 1.f;
+                put(v, k, x);
+            }
+    };
+    if (A.p32) vectors(float()); else vectors(T());
+    float sum_dy[NC][CH] = {}, acc_w2[NC][CH] = {}, sum_d[BIAS ? NC : 1][CH] = {}, acc_b2[BIAS ? NC : 1][CH] = {};
+    // what the sums since the last gate give
+    auto of_gate = [&](int k, float (&w)[CH], float (&b)[CH], float (&g)[CH]) {
+        float v[CH];
+        get(L_GATE, k, v);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) { w[i] = v[i] * sum_dy[k][i]; if constexpr (BIAS) b[i] = v[i] * sum_d[k][i]; }
+        get(L_W1, k, v);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) { g[i] = v[i] * sum_dy[k][i]; sum_dy[k][i] = 0.f; }
+        if constexpr (BIAS) {
+            load_param<CUTS, T, CH>(A, G_POST_B, 0, 0, at[k], 0.f, v);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) { g[i] += v[i] * sum_d[k][i]; sum_d[k][i] = 0.f; }
+        }
+    };
     const float inv = 1.f / (float)A.width;
-    for (uint64_t r = r0; r < r1; ++r) {
+    for (uint64_t r = begin; r < r1; r += stride) {
         const float4 st = st_next;
-        if (gate == ~0ull || (A.gate_rows && r == gate_end)) {
-            gate = A.gate_rows ? r / A.gate_rows : 0;
+        if (r >= gate_end) {
+            gate = r / A.gate_rows;
             gate_end = (gate + 1) * A.gate_rows;
 #pragma unroll
             for (int k = 0; k < NC; ++k) {
@@ -439,7 +480,7 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
             }
             __builtin_amdgcn_sched_barrier(0);                  // vector by vector: fewer registers at once
         }
-        fetch_first(r + 1);
+        if (LEAN) fetch_second(r); else fetch_first(r + stride);
         G.two(c, m);
         c *= inv;
         m = A.pre == RK_NORM_LAYER ? m * inv : 0.f;
@@ -448,6 +489,7 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
 #pragma unroll
             for (int i = 0; i < CH; ++i) d[k][i] = st.w * (d[k][i] - m - hat[k][i] * c) + element<R>(rd[k], i);
         c = 0.f; m = 0.f;
+        const Row<R> dx(A.xo, r, A.xo_st, A.width);
 #pragma unroll
         for (int k = 0; k < NC; ++k) {
             float t[CH], w1[CH], g[CH];
@@ -457,7 +499,7 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
             for (int i = 0; i < CH; ++i) {
                 t[i] = A.scale * d[k][i];
             }
-            store_row<CUTS, R, CH, STREAM>(Row<R>(A.xo, r, A.xo_st, A.width), at[k], t);
+            store_row<CUTS, R, CH, STREAM>(dx, at[k], t);
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
                 const float y = (element<T>(ry[k], i) - st.x) * st.y;
@@ -469,7 +511,7 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        fetch_second(r + 1);
+        if (LEAN) fetch_first(r + stride); else fetch_second(r + stride);
         if (A.post != RK_NORM_NONE) {
             G.two(c, m);
             c *= inv;
@@ -479,63 +521,76 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
 #pragma unroll
                 for (int i = 0; i < CH; ++i) d[k][i] = st.y * (d[k][i] - m - hat[k][i] * c);
         }
-        {
-            const Row<T> dy(A.u, r, A.u_st, A.width);
+        const Row<T> dy(A.u, r, A.u_st, A.width);
 #pragma unroll
-            for (int k = 0; k < NC; ++k) store_row<CUTS, T, CH, STREAM>(dy, at[k], d[k]);
-        }
-        if (r + 1 == r1 || r + 1 == gate_end) {
-            const bool first = gate_end <= r0 + A.gate_rows || !A.gate_rows;        // (of the chunk's gates)
+        for (int k = 0; k < NC; ++k) store_row<CUTS, T, CH, STREAM>(dy, at[k], d[k]);
+        if (A.gate_rows && (r + 1 == r1 || r + 1 == gate_end)) {
+            const bool first = gate_end <= r0 + A.gate_rows;    // (of the chunk's gates)
             const Row<float> pw(S.part[G_POST_W], chunk, A.width, A.width), pb(S.part[G_POST_B], chunk, A.width, A.width);
             const Row<float> pg(S.part[G_GATE], S.gate_direct ? gate : chunk, S.gate_direct ? S.gate_out_st : A.width, A.width);
 #pragma unroll
             for (int k = 0; k < NC; ++k) {
-                float g[CH], w1[CH], x[CH], old[CH];
-                get(L_GATE, k, g);
-                get(L_W1, k, w1);
-#pragma unroll
-                for (int i = 0; i < CH; ++i) x[i] = g[i] * sum_dy[k][i];
+                float w[CH], b[CH], g[CH], old[CH];
+                of_gate(k, w, b, g);
+                store_row<CUTS, float, CH>(pg, at[k], g);
                 if (!first) {
                     load_row<CUTS, float, CH>(pw, at[k], old);
 #pragma unroll
-                    for (int i = 0; i < CH; ++i) x[i] += old[i];
+                    for (int i = 0; i < CH; ++i) w[i] += old[i];
                 }
-                store_row<CUTS, float, CH>(pw, at[k], x);
-#pragma unroll
-                for (int i = 0; i < CH; ++i) x[i] = w1[i] * sum_dy[k][i];
+                store_row<CUTS, float, CH>(pw, at[k], w);
                 if constexpr (BIAS) {
-                    load_param<CUTS, T, CH>(A, G_POST_B, 0, 0, at[k], 0.f, w1);
-#pragma unroll
-                    for (int i = 0; i < CH; ++i) { x[i] += w1[i] * sum_d[k][i]; g[i] *= sum_d[k][i]; sum_d[k][i] = 0.f; }
                     if (!first) {
                         load_row<CUTS, float, CH>(pb, at[k], old);
 #pragma unroll
-                        for (int i = 0; i < CH; ++i) g[i] += old[i];
+                        for (int i = 0; i < CH; ++i) b[i] += old[i];
                     }
-                    store_row<CUTS, float, CH>(pb, at[k], g);
+                    store_row<CUTS, float, CH>(pb, at[k], b);
                 }
-                store_row<CUTS, float, CH>(pg, at[k], x);
-#pragma unroll
-                for (int i = 0; i < CH; ++i) sum_dy[k][i] = 0.f;
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
     }
-    const Row<float> pw(S.part[G_PRE_W], chunk, A.width, A.width), pb(S.part[G_PRE_B], chunk, A.width, A.width);
+    // the chunk's sums; a shared chunk's wavefronts add them up over LDS, in their order, a vector of each lane at a time
+    auto keep = [&](int which, int k, float (&v)[CH]) {
+        const Row<float> part(S.part[which], chunk, A.width, A.width);
+        if (!shared) {
+            store_row<CUTS, float, CH>(part, at[k], v);
+            return;
+        }
+        if (!S.part[which]) return;
+        __syncthreads();                                        // (weights and gate are not needed any more)
+        if (G.wave) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) param_lds[((G.wave - 1) * Q + q) * 64 + G.lane] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+        }
+        __syncthreads();
+        if (G.wave) return;
+        for (uint32_t w = 0; w + 1 < stride; ++w)
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                const float4 f = param_lds[(w * Q + q) * 64 + G.lane];
+                v[4 * q] += f.x; v[4 * q + 1] += f.y; v[4 * q + 2] += f.z; v[4 * q + 3] += f.w;
+            }
+        store_row<CUTS, float, CH>(part, at[k], v);
+    };
+    float w[NC][CH], b[NC][CH], g[NC][CH];
+    if (!A.gate_rows)
+#pragma unroll
+        for (int k = 0; k < NC; ++k) of_gate(k, w[k], b[k], g[k]);
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
-        store_row<CUTS, float, CH>(pw, at[k], acc_w2[k]);
-        if constexpr (BIAS) store_row<CUTS, float, CH>(pb, at[k], acc_b2[k]);
-    }
-    if (r0 == r1) {                                             // (a chunk behind the last row of the last gate)
-        const float zero[CH] = {};
-        const Row<float> p0(S.part[G_POST_W], chunk, A.width, A.width), p1(S.part[G_POST_B], chunk, A.width, A.width);
-        const Row<float> p2(S.gate_direct ? nullptr : S.part[G_GATE], chunk, A.width, A.width);
-#pragma unroll
-        for (int k = 0; k < NC; ++k) {
-            store_row<CUTS, float, CH>(p0, at[k], zero);
-            store_row<CUTS, float, CH>(p1, at[k], zero);
-            store_row<CUTS, float, CH>(p2, at[k], zero);
+        keep(G_PRE_W, k, acc_w2[k]);
+        if constexpr (BIAS) keep(G_PRE_B, k, acc_b2[k]);
+        if (!A.gate_rows) {
+            keep(G_POST_W, k, w[k]);
+            if constexpr (BIAS) keep(G_POST_B, k, b[k]);
+            keep(G_GATE, k, g[k]);
+        } else if (r0 == r1) {                                  // (a chunk behind the last row of the last gate)
+            float zero[CH] = {};
+            keep(G_POST_W, k, zero);
+            keep(G_POST_B, k, zero);
+            if (!S.gate_direct) keep(G_GATE, k, zero);
         }
     }
 }
@@ -621,12 +676,13 @@ Shape sums_shape_of(uint32_t width, int ch) {
 }
 template <typename T, typename R, int NC, int MAXT> int32_t launch_fused_nc(rk_ctx *ctx, const NormSums &S, const Shape &H, bool bias) {
     constexpr int CH = chunk_of<T, R>();
-    const uint32_t blocks = (uint32_t)((S.C.n + H.rows_per_wg - 1) / H.rows_per_wg);
+    const bool alone = !H.per_wave || S.A.gate_rows;
+    const uint32_t blocks = (uint32_t)(alone ? (S.C.n + H.rows_per_wg - 1) / H.rows_per_wg : S.C.n);
     const uint32_t lds = H.threads * sums_lds_of(CH, NC) * 16;
     auto go = [&](auto cuts, auto with_bias) -> int32_t {
         const auto kernel = k_norm_backward_sums<decltype(cuts)::value, T, R, CH, NC, MAXT, decltype(with_bias)::value>;
         if (lds > 65536u - 1024u) RK_HIP(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-        kernel<<<blocks, H.threads, lds, ctx->stream>>>(S, H.per_wave);
+        kernel<<<blocks, H.threads, lds, ctx->stream>>>(S, H.per_wave, alone);
         return RK_OK;
     };
     const bool cuts = S.A.width % CH != 0;
@@ -768,10 +824,12 @@ extern "C" int32_t rk_norm_backward(rk_ctx *ctx, const rk_norm_block *block, uin
     const bool bias = block->post_bias || out[G_PRE_B];
     const Shape H = sums_shape_of(width, type == RK_F32 ? 4 : 8);
     if (any) {
-        // a chunk for every workgroup (wavefront) that fits the chip at once
-        const uint64_t at_once = H.per_wave ? 2048 : H.nc && H.threads <= 512 ? 512 : 256;
+        // a chunk for every workgroup (of rows with gates that a wavefront holds: every wavefront) that fits the chip at once, but of
+        // several rows, where there are enough: chunks cost a start and sums that have to be joined
+        const uint64_t at_once = H.per_wave && A.gate_rows ? 2048 : H.nc && H.threads <= 512 ? 512 : 256;
+        const uint64_t least = n_rows <= 256 ? (H.per_wave && !A.gate_rows ? 4 : 1) : H.per_wave && !A.gate_rows ? 8 : 2;
         uint64_t rows = (n_rows + at_once - 1) / at_once;
-        if (rows < 1) rows = 1;
+        if (rows < least) rows = least;
         const bool gates = A.gate_rows != 0;
         if (!gates) {
             S.C = Chunks{rows, 0, (n_rows + rows - 1) / rows};

@@ -267,28 +267,37 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_forward(RouteArgs A) {
     A.loss[1] = n > 0.f ? z / n : 0.f;
 }
 
-// The workgroups' parts of a group added up in their order: a workgroup has 64 experts, its wavefronts every 16th part.
-constexpr int RT_JOIN = 16;
-__global__ __launch_bounds__(64 * RT_JOIN) void k_route_join(RouteArgs A) {
-    __shared__ float lds_p[RT_JOIN][64], lds_n[RT_JOIN], lds_z[RT_JOIN];
-    __shared__ uint32_t lds_c[RT_JOIN][64];
+// The workgroups' parts of a group added up in their order: a workgroup has 16 experts, and 64 threads of it share an expert's parts.
+constexpr uint32_t RT_COLS = 16, RT_SHARE = 64;
+__global__ __launch_bounds__(RT_COLS * RT_SHARE) void k_route_join(RouteArgs A) {
+    __shared__ float lds_p[RT_SHARE][RT_COLS], lds_n[16], lds_z[16];
+    __shared__ uint32_t lds_c[RT_SHARE][RT_COLS];
     const uint64_t g = blockIdx.x / A.tiles, first = g * A.per_group;
-    const uint32_t E = A.n_experts, lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, e = (blockIdx.x - (uint32_t)g * A.tiles) * 64u + lane;
+    const uint32_t E = A.n_experts, lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, part = threadIdx.x / RT_COLS;
+    uint32_t e = (blockIdx.x - (uint32_t)g * A.tiles) * RT_COLS + threadIdx.x % RT_COLS;
     float n = 0.f, z = 0.f, p = 0.f;
     uint32_t count = 0;
-    for (uint64_t c = threadIdx.x; c < A.per_group; c += 64 * RT_JOIN) { n += A.part_z[first + c].x; z += A.part_z[first + c].y; }
+    for (uint64_t c = threadIdx.x; c < A.per_group; c += RT_COLS * RT_SHARE) { n += A.part_z[first + c].x; z += A.part_z[first + c].y; }
     if (e < E)
 #pragma unroll 4
-        for (uint64_t c = wave; c < A.per_group; c += RT_JOIN) {
+        for (uint64_t c = part; c < A.per_group; c += RT_SHARE) {
             count += A.part_counts[(first + c) * E + e];
             p += A.part_probs[(first + c) * E + e];
         }
     n = wave_sum(n); z = wave_sum(z);
     if (lane == 0) { lds_n[wave] = n; lds_z[wave] = z; }
-    lds_p[wave][lane] = p; lds_c[wave][lane] = count;
+    lds_p[part][threadIdx.x % RT_COLS] = p; lds_c[part][threadIdx.x % RT_COLS] = count;
     __syncthreads();
     if (wave) return;
-    for (int w = 1; w < RT_JOIN; ++w) { n += lds_n[w]; z += lds_z[w]; p += lds_p[w][lane]; count += lds_c[w][lane]; }
+    // the first wavefront: lane l has the parts l / 16, l / 16 + 4, ... of expert l % 16
+    n = 0.f; z = 0.f; p = 0.f; count = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) { n += lds_n[w]; z += lds_z[w]; }
+#pragma unroll
+    for (uint32_t s = 0; s < RT_SHARE; s += 4) { p += lds_p[s + lane / RT_COLS][lane % RT_COLS]; count += lds_c[s + lane / RT_COLS][lane % RT_COLS]; }
+    p += __shfl_xor(p, 16, 64); count += (uint32_t)__shfl_xor((int)count, 16, 64);
+    p += __shfl_xor(p, 32, 64); count += (uint32_t)__shfl_xor((int)count, 32, 64);
+    if (lane >= RT_COLS) e = E;                             // (the others have the same)
     if (e < E) { A.counts[g * E + e] = count; A.prob_sum[g * E + e] = p; }
     const float cp = wave_sum(e < E ? (float)count * p : 0.f);
     // The workgroup that ends last adds the groups up, in their order.  What it needs of the others goes through stores and loads at the
@@ -505,8 +514,9 @@ extern "C" int32_t rk_route_forward(rk_ctx *ctx, const rk_router *router, uint64
     // up to four workgroups a compute unit share the tokens, each in rounds of as many as its wavefronts hold; few tokens are one's
     const uint64_t at_once = RT_WAVES * 64 / lanes_of(A.n_experts);
     A.chunk = (n_tokens + 1024 * at_once - 1) / (1024 * at_once) * at_once;
+    if (A.n_groups == 1 && n_tokens <= 4 * at_once) A.chunk = 4 * at_once;      // (then there is nothing to join)
     A.per_group = n_tokens ? (A.group_tokens + A.chunk - 1) / A.chunk : 0;
-    A.tiles = (A.n_experts + 63) / 64;
+    A.tiles = (A.n_experts + RT_COLS - 1) / RT_COLS;
     const uint64_t blocks = A.per_group * (n_tokens ? A.n_groups : 0);
     if (blocks == 0) {
         k_route_nothing<<<1, 256, 0, ctx->stream>>>(A);
@@ -535,7 +545,7 @@ extern "C" int32_t rk_route_forward(rk_ctx *ctx, const rk_router *router, uint64
     if (rc != RK_OK) return rk_fail(ctx, rc, "k_route_forward: no room in LDS");
     RK_CHECK_LAUNCH(ctx, "k_route_forward");
     if (blocks > 1) {
-        k_route_join<<<(uint32_t)(A.n_groups * A.tiles), 64 * RT_JOIN, 0, ctx->stream>>>(A);
+        k_route_join<<<(uint32_t)(A.n_groups * A.tiles), RT_COLS * RT_SHARE, 0, ctx->stream>>>(A);
         RK_CHECK_LAUNCH(ctx, "k_route_join");
     }
     return RK_OK;
