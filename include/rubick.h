@@ -877,8 +877,8 @@ typedef struct {
 /* p = softmax of a token's logits; its top_k largest logits, the largest first, equal
  * ones by index; weight = p of these, or p over their sum.  Logits of -inf or
  * NaN are never chosen: what is left of expert is then -1, of weight 0.  A
- * token whose mask byte is 0, or without a logit above -inf, is left out:
- * expert -1, weight and lse 0, counted nowhere, whatever its logits hold.  Over the n_g tokens that count of
+ * token whose mask byte is 0, whatever its logits hold, or whose logits are all -inf, is left out:
+ * expert -1, weight and lse 0, counted nowhere.  A NaN makes its token's lse and with it the losses NaN.  Over the n_g tokens that count of
  * each group, G' of the G groups having any, and the n tokens of all:
  *     counts[g][e]   tokens that chose e          prob_sum[g][e]  sum of p[e]
  *     balance = 1/G' sum_g n_experts / (top_k n_g^2) sum_e counts[g][e] prob_sum[g][e]
@@ -922,8 +922,8 @@ typedef struct {
 
 /* loss [device] n_rows (unweighted); lse [device] n_rows x 2: log sum exp of student / T and of student, 0
  * where its term's weight is 0; total [device] one float: sum of row_weight * loss.
- * Rows whose weight is 0 are left out, whatever they hold: loss and lse 0.  Rows without a logit
- * above -inf have loss 0 and lse -inf. */
+ * Rows whose weight is 0 are left out, whatever they hold: loss and lse 0.  Rows of nothing but
+ * -inf have loss 0 and lse -inf; a NaN makes its row's loss and gradient NaN. */
 int32_t rk_distill_loss(rk_ctx *ctx, const rk_distill *distill, uint64_t n_rows, uint32_t vocab,
                         const rk_matrix *student, const rk_teacher *teacher, float *loss, float *lse, float *total);
 

@@ -98,7 +98,7 @@ def route(logits, mask, top_k, renormalise, group_tokens, d_loss=None, d_weight=
     n_tok, n_exp = logits.shape
     per = group_tokens or max(n_tok, 1)
     groups = (n_tok + per - 1) // per if group_tokens else 1
-    there = (logits > -INF).any(1) if n_tok else torch.zeros(0, dtype=torch.bool)
+    there = ~(logits == -INF).all(1) if n_tok else torch.zeros(0, dtype=torch.bool)
     if mask is not None:
         there = there & (mask != 0)
     p = torch.zeros_like(logits)
@@ -111,7 +111,7 @@ def route(logits, mask, top_k, renormalise, group_tokens, d_loss=None, d_weight=
         if not there[t]:
             continue
         l = logits[t]
-        top = l[l == l].max()
+        top = l.nan_to_num(nan=-INF, posinf=INF, neginf=-INF).max()
         lse[t] = top + torch.log(torch.exp(l - top).sum())
         p[t] = torch.exp(l - lse[t])
         order = sorted((e for e in range(n_exp) if float(l[e]) > -INF), key=lambda e: (-float(l[e]), e))[:top_k]
@@ -161,11 +161,10 @@ def distill(student, t_logits, index, label, row_weight, tau, kd, ce, d_total=1.
         if w == 0.0:
             continue
         s = student[r]
-        if not bool((s > -INF).any()):
+        if bool((s == -INF).all()):
             lse[r] = torch.tensor([-INF if kd else 0.0, -INF if ce else 0.0])
             continue
-        top = s[s == s].max()
-        parts = []
+        top = s.nan_to_num(nan=-INF, posinf=INF, neginf=-INF).max()
         if kd:
             lse[r, 0] = top / tau + torch.log(torch.exp((s - top) / tau).sum())
             kept = [k for k in range(index.shape[1]) if 0 <= int(index[r, k]) < vocab and float(t_logits[r, k]) != -INF]

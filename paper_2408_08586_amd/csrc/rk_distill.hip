@@ -315,7 +315,7 @@ template <bool CUTS, int THREADS, typename T, int CH> __device__ __forceinline__
 // a row's loss and log sums from the joined sums; cross: teacher's cross term and sum, the label's logit and whether there is one
 struct RowLoss { float loss, lse_a, lse_b, la, lb; bool left; };
 template <typename T, int SUMS> __device__ __forceinline__ RowLoss row_loss(const DistillArgs &A, const Streams &S, float top, float sa, float sb, float4 cross) {
-    if (top == -INFINITY) return RowLoss{0.f, -INFINITY, -INFINITY, 0.f, 0.f, true};
+    if (top == -INFINITY && sa == 0.f) return RowLoss{0.f, -INFINITY, -INFINITY, 0.f, 0.f, true};
     RowLoss L;
     L.left = false;
     L.la = Exp<T>::log(sa);

@@ -188,8 +188,7 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_forward(RouteArgs A) {
         bool there = live;
         if (A.mask && live) there = A.mask[t] != 0;
         m = lanes_max<L>(m);
-        there = there && m > -INFINITY;
-        const float ref = there ? m : 0.f;
+        const float ref = there && m > -INFINITY ? m : 0.f;
         typename Keys<T>::Key key[V];
         float s = 0.f;
 #pragma unroll
@@ -200,6 +199,7 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_forward(RouteArgs A) {
             s += l[i];
         }
         s = lanes_sum<L>(s);
+        there = there && s != 0.f;                          // (nothing but -inf: no exponential; a NaN stays one)
         const float lse = there ? ref + logf(s) : 0.f, inv = there ? 1.f / s : 0.f;
 #pragma unroll
         for (int i = 0; i < V; ++i) sum[i] += l[i] * inv;
@@ -405,8 +405,8 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_backward(RouteArgs A) {
             for (int q = 0; q < 4; ++q) p[4 * i + q] = x[q];
         }
         const float lse = live ? A.lse[t] : 0.f;
-        // a token that counts has its first choice
-        const bool there = __shfl(e[0], lane & ~(L - 1), 64) >= 0;
+        // a token that counts has its first choice, unless all its logits are -inf and NaN
+        const bool there = __shfl(e[0], lane & ~(L - 1), 64) >= 0 || lse != lse;
         float yk[KEPT], ws = 0.f, wd = 0.f;
         if (A.d_weight) {
 #pragma unroll
@@ -428,7 +428,7 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_backward(RouteArgs A) {
             s += a[i] * p[i];
         }
         s = lanes_sum<L>(s) + (A.renorm ? 0.f : wd) - dz * lse;
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -446,7 +446,7 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_backward(RouteArgs A) {
         if (A.d_weight)
 #pragma unroll
             for (int h = 0; h < KEPT; ++h) if (e[h] >= 0) y[e[h]] = 0.f;
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
 }
