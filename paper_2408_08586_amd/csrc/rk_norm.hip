@@ -595,38 +595,53 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
     }
 }
 
-// the chunks' sums added up, always in the same order: a workgroup has COLS columns, and 1,024 / COLS threads of it share a column's chunks
+// The chunks' sums added up, always in the same order: LANES lanes next to each other have four columns each of a chunk, the
+// workgroup's 1,024 / LANES such rows share the chunks; a wavefront's rows are joined by swaps and rotations, the wavefronts over LDS.
 struct Joined { const float *from[G_VECTORS]; float *to[G_VECTORS]; uint64_t count[G_VECTORS]; uint32_t n; uint64_t gate_chunks, gate_out_st; };
-template <int COLS> __global__ __launch_bounds__(1024) void k_norm_join(Joined J, uint32_t width, uint32_t tiles) {
-    constexpr uint32_t SHARE = 1024 / COLS;
-    __shared__ float lds[SHARE][COLS];
-    const uint32_t lane = threadIdx.x % COLS, part = threadIdx.x / COLS;
+template <int LANES> __global__ __launch_bounds__(1024) void k_norm_join(Joined J, uint32_t width, uint32_t tiles) {
+    static_assert(LANES == 16 || LANES == 4, "");
+    constexpr uint32_t SHARE = 1024 / LANES, COLS = 4 * LANES;
+    typedef Vec<float, 4> Any __attribute__((aligned(4)));
+    __shared__ float4 lds[16][LANES];
+    const uint32_t part = threadIdx.x / LANES;
     const uint64_t job = blockIdx.x / tiles;
-    const uint32_t col = blockIdx.x % tiles * COLS + lane;
+    const uint32_t col0 = blockIdx.x % tiles * COLS, col = col0 + threadIdx.x % LANES * 4;
     // the vectors first, then the gates one by one (J.gate_chunks each)
     const uint32_t v = job < J.n ? (uint32_t)job : J.n;
     const float *from = J.from[v];
     float *to = J.to[v];
     uint64_t count = J.count[v];
     if (job >= J.n) { from += (job - J.n) * J.gate_chunks * width; to += (job - J.n) * J.gate_out_st; count = J.gate_chunks; }
-    float s = 0.f;
-    if (col < width) {
+    Vec<float, 4> s = {0.f, 0.f, 0.f, 0.f};
+    if (col + 4 <= width) {
         uint64_t c = part;
-        for (; c + 7 * SHARE < count; c += 8 * SHARE) {         // eight under way at once
-            float x[8];
+        for (; c + 3 * SHARE < count; c += 4 * SHARE) {         // four under way at once
+            Vec<float, 4> x[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = from[(c + SHARE * i) * width + col];
+            for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const Any *>(from + (c + SHARE * i) * width + col);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s += x[i];
+            for (int i = 0; i < 4; ++i) s += x[i];
         }
-        for (; c < count; c += SHARE) s += from[c * width + col];
+        for (; c < count; c += SHARE) s += *reinterpret_cast<const Any *>(from + c * width + col);
+    } else if (col < width) {                                   // the vector that the width cuts
+        for (uint64_t c = part; c < count; c += SHARE)
+#pragma unroll
+            for (int i = 0; i < 3; ++i) if (col + i < width) s[i] += from[c * width + col + i];
     }
-    lds[part][lane] = s;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float o;
+        s[i] = swap32(s[i], o) + o;
+        s[i] = swap16(s[i], o) + o;
+        if constexpr (LANES == 4) { s[i] += dpp_of<0x128>(s[i]); s[i] += dpp_of<0x124>(s[i]); }      // row_ror:8, 4
+    }
+    if ((threadIdx.x & 63u) < (uint32_t)LANES) lds[threadIdx.x >> 6][threadIdx.x % LANES] = make_float4(s[0], s[1], s[2], s[3]);
     __syncthreads();
-    if (threadIdx.x >= COLS) return;
-#pragma unroll 16
-    for (uint32_t w = 1; w < SHARE; ++w) s += lds[w][lane];
-    if (col < width) to[col] = s;
+    if (threadIdx.x >= COLS || col0 + threadIdx.x >= width) return;
+    float sum = 0.f;
+#pragma unroll
+    for (uint32_t w = 0; w < 16; ++w) sum += reinterpret_cast<const float *>(lds[w])[threadIdx.x];
+    to[col0 + threadIdx.x] = sum;
 }
 
 // ---- host
@@ -877,11 +892,11 @@ extern "C" int32_t rk_norm_backward(rk_ctx *ctx, const rk_norm_block *block, uin
         }
     }
     if (join_jobs) {
-        // 64 columns a workgroup, or 16 where that would leave compute units without one
-        const bool narrow = join_jobs * ((width + 63) / 64) < 256;
+        // 64 columns a workgroup, or 16 where that would leave half of the compute units without one
+        const bool narrow = join_jobs * ((width + 63) / 64) < 128;
         const uint32_t tiles = narrow ? (width + 15) / 16 : (width + 63) / 64;
-        if (narrow) k_norm_join<16><<<(uint32_t)(join_jobs * tiles), 1024, 0, ctx->stream>>>(J, width, tiles);
-        else k_norm_join<64><<<(uint32_t)(join_jobs * tiles), 1024, 0, ctx->stream>>>(J, width, tiles);
+        if (narrow) k_norm_join<4><<<(uint32_t)(join_jobs * tiles), 1024, 0, ctx->stream>>>(J, width, tiles);
+        else k_norm_join<16><<<(uint32_t)(join_jobs * tiles), 1024, 0, ctx->stream>>>(J, width, tiles);
         RK_CHECK_LAUNCH(ctx, "k_norm_join");
     }
     return RK_OK;
