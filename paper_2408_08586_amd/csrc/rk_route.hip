@@ -61,21 +61,25 @@ template <int CTRL> __device__ __forceinline__ double dpp_d(double v) {
     return __longlong_as_double((long long)((unsigned long long)dpp_u<CTRL>((uint32_t)(u >> 32)) << 32 | dpp_u<CTRL>((uint32_t)u)));
 }
 
-// four logits from `first` on; behind the last expert -inf
-template <typename T, bool CUTS> __device__ __forceinline__ void load4(const T *row, uint32_t first, uint32_t n, bool live, float (&v)[4]) {
+// four logits from `first` on, as they lie in memory; behind the last expert -inf
+template <typename T, bool CUTS> __device__ __forceinline__ Words<T, 4> fetch4(const T *row, uint32_t first, uint32_t n, bool live) {
     typedef Words<T, 4> Any __attribute__((aligned(sizeof(T))));
+    constexpr uint32_t NONE = sizeof(T) == 4 ? 0xFF800000u : __is_same(T, __bf16) ? 0xFF80FF80u : 0xFC00FC00u;
+    Words<T, 4> w;
     if (live && first + 4 <= n) {
-        const Words<T, 4> w = *reinterpret_cast<const Any *>(row + first);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = element<T>(w, i);
+        w = *reinterpret_cast<const Any *>(row + first);
     } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = -INFINITY;
+        w = NONE;
         if constexpr (CUTS)
             if (live)
 #pragma unroll
-                for (int i = 0; i < 3; ++i) if (first + i < n) v[i] = (float)row[first + i];
+                for (int i = 0; i < 3; ++i)
+                    if (first + i < n) {
+                        if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(row[first + i]);
+                        else w[i / 2] = (w[i / 2] & (i & 1 ? 0xFFFFu : 0xFFFF0000u)) | (uint32_t)__builtin_bit_cast(uint16_t, row[first + i]) << (i & 1 ? 16 : 0);
+                    }
     }
+    return w;
 }
 template <typename T, bool CUTS> __device__ __forceinline__ void store4(T *row, uint32_t first, uint32_t n, const float (&v)[4]) {
     typedef Words<T, 4> Any __attribute__((aligned(sizeof(T))));
@@ -180,10 +184,9 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_forward(RouteArgs A) {
         float l[V], m = -INFINITY;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            float x[4];
-            load4<T, CUTS>(row, (j + L * i) * 4, E, live, x);
+            const Words<T, 4> x = fetch4<T, CUTS>(row, (j + L * i) * 4, E, live);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) { l[4 * i + q] = x[q]; m = fmaxf(m, x[q]); }
+            for (int q = 0; q < 4; ++q) { l[4 * i + q] = element<T>(x, q); m = fmaxf(m, l[4 * i + q]); }
         }
         bool there = live;
         if (A.mask && live) there = A.mask[t] != 0;
@@ -216,12 +219,15 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_forward(RouteArgs A) {
         float w[KEPT], ws = 0.f;
 #pragma unroll
         for (int h = 0; h < KEPT; ++h) {
+            w[h] = 0.f;
+            if (h && h * L >= K) continue;                      // (the same for all: few ask for more than a row's lanes hold)
             w[h] = Keys<T>::expert(mine[h]) >= 0 ? exp_f32(Keys<T>::value(mine[h]) - lse) : 0.f;
             ws += w[h];
         }
         const float scale = A.renorm && there ? 1.f / lanes_sum<L>(ws) : 1.f;
 #pragma unroll
         for (int h = 0; h < KEPT; ++h) {
+            if (h && h * L >= K) continue;
             const uint32_t k = h * L + j;
             const int32_t e = Keys<T>::expert(mine[h]);
             if (live && k < K) {
@@ -354,6 +360,32 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_backward(RouteArgs A) {
     const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < NV; ++i) ((float4 *)y)[j + L * i] = zero;
+    const uint64_t t0 = (uint64_t)blockIdx.x * A.chunk;
+    const uint64_t t1 = t0 + A.chunk < A.n_tokens ? t0 + A.chunk : A.n_tokens;
+    // the next token's data are on their way while one is worked on, the first's while the groups are counted (not of so many
+    // experts that registers for it would cost wavefronts)
+    constexpr bool AHEAD = NV <= 4;
+    Words<T, 4> next_l[NV];
+    int32_t next_e[KEPT];
+    float next_dw[KEPT], next_lse;
+    auto fetch = [&](uint64_t t) {
+        const bool live = t < t1;
+        const T *const row = (const T *)A.logits + t * A.st;
+#pragma unroll
+        for (int h = 0; h < KEPT; ++h) {
+            next_e[h] = -1; next_dw[h] = 0.f;
+            if (h && h * L >= K) continue;                      // (the same for all)
+            const uint32_t k = h * L + j;
+            if (live && k < K) {
+                next_e[h] = A.expert[t * K + k];
+                if (A.d_weight) next_dw[h] = A.d_weight[t * K + k];
+            }
+        }
+        next_lse = live ? A.lse[t] : 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) next_l[i] = fetch4<T, CUTS>(row, (j + L * i) * 4, E, live);
+    };
+    if constexpr (AHEAD) fetch(t0 + wave * SLOTS + slot);
     float n = 0.f, some = 0.f;
     for (uint64_t g = threadIdx.x; g < A.n_groups; g += RT_THREADS) {
         const uint32_t c = A.tokens[g];
@@ -367,8 +399,6 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_backward(RouteArgs A) {
     for (int w = 0; w < RT_WAVES; ++w) { n += red[w][0]; some += red[w][1]; }
     const float bal = some > 0.f ? A.d_loss[0] * (float)E / ((float)K * some) : 0.f;
     const float dz = n > 0.f ? A.d_loss[1] * 2.f / n : 0.f;
-    const uint64_t t0 = (uint64_t)blockIdx.x * A.chunk;
-    const uint64_t t1 = t0 + A.chunk < A.n_tokens ? t0 + A.chunk : A.n_tokens;
     uint64_t g_end = 0;                                     // first token behind the group that `a` is of
     float a[4 * NV] = {};
     for (uint64_t base = t0 + wave * SLOTS; base < t1; base += RT_WAVES * SLOTS) {
@@ -386,37 +416,30 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_backward(RouteArgs A) {
         }
         const T *const row = (const T *)A.logits + t * A.st;
         T *const out = (T *)A.d_logits + t * A.d_st;
+        if constexpr (!AHEAD) fetch(t);
         int32_t e[KEPT];
-        float dw[KEPT];
+        float dw[KEPT], p[4 * NV];
 #pragma unroll
-        for (int h = 0; h < KEPT; ++h) {
-            const uint32_t k = h * L + j;
-            const bool on = live && k < K;
-            e[h] = on ? A.expert[t * K + k] : -1;
-            e[h] = (uint32_t)e[h] < E ? e[h] : -1;
-            dw[h] = on && A.d_weight ? A.d_weight[t * K + k] : 0.f;
-        }
-        float p[4 * NV];
+        for (int h = 0; h < KEPT; ++h) { e[h] = (uint32_t)next_e[h] < E ? next_e[h] : -1; dw[h] = next_dw[h]; }
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            float x[4];
-            load4<T, CUTS>(row, (j + L * i) * 4, E, live, x);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) p[4 * i + q] = x[q];
-        }
-        const float lse = live ? A.lse[t] : 0.f;
+        for (int i = 0; i < 4 * NV; ++i) p[i] = element<T>(next_l[i / 4], i % 4);
+        const float lse = next_lse;
+        if constexpr (AHEAD) fetch(t + RT_WAVES * SLOTS);
         // a token that counts has its first choice, unless all its logits are -inf and NaN
         const bool there = __shfl(e[0], lane & ~(L - 1), 64) >= 0 || lse != lse;
         float yk[KEPT], ws = 0.f, wd = 0.f;
         if (A.d_weight) {
 #pragma unroll
             for (int h = 0; h < KEPT; ++h) {
+                yk[h] = 0.f;
+                if (h && h * L >= K) continue;
                 yk[h] = e[h] >= 0 ? exp_f32((float)row[e[h]] - lse) : 0.f;
                 ws += yk[h]; wd += e[h] >= 0 ? yk[h] * dw[h] : 0.f;
             }
             ws = lanes_sum<L>(ws); wd = lanes_sum<L>(wd);
 #pragma unroll
             for (int h = 0; h < KEPT; ++h) {
+                if (h && h * L >= K) continue;
                 yk[h] = A.renorm ? yk[h] / ws * (dw[h] - wd / ws) : yk[h] * dw[h];
                 if (e[h] >= 0) y[e[h]] = yk[h];
             }
@@ -568,9 +591,10 @@ extern "C" int32_t rk_route_backward(rk_ctx *ctx, const rk_router *router, uint6
     A.expert = const_cast<int32_t *>(expert); A.lse = const_cast<float *>(lse); A.counts = const_cast<uint32_t *>(counts);
     A.tokens = const_cast<uint32_t *>(tokens);
     A.d_loss = d_loss; A.d_weight = d_weight; A.d_logits = d_logits->data; A.d_st = d_logits->stride;
-    // four workgroups a compute unit, each at least as many tokens as its wavefronts hold at once
+    // two workgroups a compute unit, as many as fit at once, each at least as many tokens as its wavefronts hold at once (131072 x 160 in 32
+    // bits 42.9 us, with twice as many 44.0; 60000 x 250 23.9 and 28.4)
     const uint64_t at_once = RT_WAVES * 64 / lanes_of(A.n_experts);
-    A.chunk = (n_tokens + 1023) / 1024;
+    A.chunk = (n_tokens + 511) / 512;
     A.chunk = (A.chunk + at_once - 1) / at_once * at_once;
     const uint64_t blocks = (n_tokens + A.chunk - 1) / A.chunk;
     with_lanes(logits->type, A.n_experts, [&](auto t, auto l, auto v, auto c) {
