@@ -124,6 +124,44 @@ __device__ __forceinline__ RowOf row_of(uint64_t n_rows, bool per_wave, RowGroup
     return RowOf{row, per_wave ? G.lane : t, per_wave ? 64u : blockDim.x, row < n_rows};
 }
 
+// What is behind the row's fetching, of rows of few whole vectors a lane: what the norms multiply and add is asked for before the sums are taken, all of
+// it at once.  (Longer rows would pay for the registers with wavefronts: 8192 x 12288 149 us without, 187 with; 4096 x 2048 14.6 and 13.8.)
+template <typename T, typename R, int CH, int NC>
+__device__ __forceinline__ void forward_early(const NormArgs &A, const RowOf &P, RowGroup &G, const Place (&at)[NC], const Words<R, CH> (&wx)[NC], const Words<T, CH> (&wy)[NC]) {
+    Words<T, CH> w[NC], b[NC], g[NC];
+    auto ask = [&](int which, uint64_t row, uint64_t stride, Words<T, CH> (&v)[NC]) {
+        const Row<T> of(A.vec[which], row, stride, A.width);                    // (zeros, if there is none)
+#pragma unroll
+        for (int k = 0; k < NC; ++k) v[k] = fetch_at<T, CH>(of, at[k].whole);
+    };
+    ask(G_POST_W, 0, 0, w); ask(G_GATE, A.gate_rows ? P.row / A.gate_rows : 0, A.gate_st, g); ask(G_POST_B, 0, 0, b);
+    float my, ry, mx, rx;
+    row_stats<CH, NC>(G, [&](int k, int i) { return element<T>(wy[k], i); }, A.width, at, A.post, A.post_eps, my, ry);
+    const bool has_w1 = A.vec[G_POST_W] != nullptr, has_gate = A.vec[G_GATE] != nullptr, has_w2 = A.vec[G_PRE_W] != nullptr;
+    float x[NC][CH];
+    const Row<R> xo(A.xo, P.row, A.xo_st, A.width);
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const float n = (element<T>(wy[k], i) - my) * ry * (has_w1 ? element<T>(w[k], i) : 1.f) + element<T>(b[k], i);
+            x[k][i] = i < at[k].valid ? A.scale * element<R>(wx[k], i) + (has_gate ? element<T>(g[k], i) : 1.f) * n : 0.f;
+        }
+        store_at<R, CH, STREAM>(xo, at[k].whole, words_of<R, CH>(x[k]));
+    }
+    ask(G_PRE_W, 0, 0, w); ask(G_PRE_B, 0, 0, b);
+    row_stats<CH, NC>(G, [&](int k, int i) { return x[k][i]; }, A.width, at, A.pre, A.pre_eps, mx, rx);
+    if (P.tid == 0) reinterpret_cast<float4 *>(A.stats)[P.row] = make_float4(my, ry, mx, rx);
+    if (A.pre == RK_NORM_NONE) return;
+    const Row<T> u(A.u, P.row, A.u_st, A.width);
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) x[k][i] = (x[k][i] - mx) * rx * (has_w2 ? element<T>(w[k], i) : 1.f) + element<T>(b[k], i);
+        store_at<T, CH, STREAM>(u, at[k].whole, words_of<T, CH>(x[k]));
+    }
+}
+
 template <bool CUTS, typename T, typename R, int CH, int NC, int MAXT>
 __global__ __launch_bounds__(MAXT) void k_norm_forward(NormArgs A, bool per_wave) {
     __shared__ float lds[96];
@@ -142,6 +180,11 @@ __global__ __launch_bounds__(MAXT) void k_norm_forward(NormArgs A, bool per_wave
 #pragma unroll
         for (int k = 0; k < NC; ++k) wx[k] = fetch_row<CUTS, R, CH>(rx, at[k]);
     }
+    if constexpr (!CUTS && MAXT <= 512)
+        if (sizeof(T) == 4 || !A.p32) {                     // (32-bit vectors beside narrow rows take too many registers: 4096 x 4096 26 us, early 28)
+            forward_early<T, R, CH, NC>(A, P, G, at, wx, wy);
+            return;
+        }
     float my, ry, mx, rx;
     row_stats<CH, NC>(G, [&](int k, int i) { return element<T>(wy[k], i); }, A.width, at, A.post, A.post_eps, my, ry);
     float x[NC][CH];
@@ -357,6 +400,9 @@ constexpr uint32_t sums_lds_of(int ch, int nc) { return (uint32_t)(3 * nc * ch /
 template <bool CUTS, typename T, typename R, int CH, int NC, int MAXT, bool BIAS>
 __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool per_wave, bool alone) {
     constexpr bool LEAN = MAXT == 768 && (BIAS || CUTS || sizeof(R) == 4);
+    // The pieces of a cut vector stay apart until they are wanted, where there are registers for it: 4096 x 5003 104 -> 69 us, 8192 x 777
+    // with biases 43 -> 35; but 4096 x 7777 in 32 bits 194 -> 262, 8192 x 777 52 -> 61, 4096 x 9999 149 -> 185.
+    constexpr bool HOLD = CUTS && sizeof(T) == 2 && (MAXT <= 512 || (MAXT == 1024 && sizeof(R) == 2));
     extern __shared__ float4 param_lds[];
     __shared__ float lds[96];
     const NormArgs &A = S.A;
@@ -370,8 +416,8 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
     const uint64_t stride = shared ? blockDim.x >> 6 : 1, begin = r0 + (shared ? G.wave : 0u);
     Place at[NC];
     places<CH, NC>(at, P.tid, P.threads, A.width);
-    Words<R, CH> rx[NC], rd[NC];
-    Words<T, CH> ru[NC], ry[NC];
+    Held<HOLD, R, CH> rx[NC], rd[NC];
+    Held<HOLD, T, CH> ru[NC], ry[NC];
     float4 st_next = make_float4(0.f, 1.f, 0.f, 1.f);
     auto fetch_first = [&](uint64_t r) {
         const bool there = r < r1;                              // (behind the chunk: a row of no elements)
@@ -380,8 +426,8 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
         const Row<T> u(there ? A.du : nullptr, r, A.du_st, A.width);
 #pragma unroll
         for (int k = 0; k < NC; ++k) {
-            rx[k] = fetch_row<CUTS, R, CH, STREAM>(x, at[k]);
-            ru[k] = fetch_row<CUTS, T, CH, STREAM>(u, at[k]);
+            rx[k] = held<HOLD, CUTS, R, CH, STREAM>(x, at[k]);
+            ru[k] = held<HOLD, CUTS, T, CH, STREAM>(u, at[k]);
         }
     };
     auto fetch_second = [&](uint64_t r) {
@@ -390,8 +436,8 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
         const Row<T> y(there ? A.y : nullptr, r, A.y_st, A.width);
 #pragma unroll
         for (int k = 0; k < NC; ++k) {
-            rd[k] = fetch_row<CUTS, R, CH, STREAM>(dxo, at[k]);
-            ry[k] = fetch_row<CUTS, T, CH, STREAM>(y, at[k]);
+            rd[k] = held<HOLD, CUTS, R, CH, STREAM>(dxo, at[k]);
+            ry[k] = held<HOLD, CUTS, T, CH, STREAM>(y, at[k]);
         }
     };
     fetch_first(begin);
@@ -414,13 +460,13 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
     // the vectors' parts, all under way before the first is waited for
     auto vectors = [&](auto p) {
         typedef decltype(p) V;
-        Words<V, CH> w[3][NC];
+        Held<HOLD, V, CH> w[3][NC];
         const Row<V> w1(A.vec[G_POST_W], 0, 0, A.width), w2(A.vec[G_PRE_W], 0, 0, A.width), g(begin < r1 ? A.vec[G_GATE] : nullptr, gate, A.gate_st, A.width);
 #pragma unroll
         for (int k = 0; k < NC; ++k) {
-            w[L_W1][k] = fetch_row<CUTS, V, CH>(w1, at[k]);
-            w[L_W2][k] = fetch_row<CUTS, V, CH>(w2, at[k]);
-            w[L_GATE][k] = fetch_row<CUTS, V, CH>(g, at[k]);
+            w[L_W1][k] = held<HOLD, CUTS, V, CH>(w1, at[k]);
+            w[L_W2][k] = held<HOLD, CUTS, V, CH>(w2, at[k]);
+            w[L_GATE][k] = held<HOLD, CUTS, V, CH>(g, at[k]);
         }
         const bool have[3] = {A.vec[G_POST_W] != nullptr, A.vec[G_PRE_W] != nullptr, A.vec[G_GATE] != nullptr};
 #pragma unroll
@@ -428,8 +474,9 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
 #pragma unroll
             for (int k = 0; k < NC; ++k) {
                 float x[CH];
+                const Words<V, CH> own = whole_of<V, CH>(w[v][k], at[k]);
 #pragma unroll
-                for (int i = 0; i < CH; ++i) x[i] = have[v] ? element<V>(w[v][k], i) : 1.f;
+                for (int i = 0; i < CH; ++i) x[i] = have[v] ? element<V>(own, i) : 1.f;
                 put(v, k, x);
             }
     };
@@ -469,10 +516,12 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
         for (int k = 0; k < NC; ++k) {
             float w2[CH];
             get(L_W2, k, w2);
+            const Words<T, CH> wu = whole_of<T, CH>(ru[k], at[k]);
+            const Words<R, CH> wx = whole_of<R, CH>(rx[k], at[k]);
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
-                const float u = element<T>(ru[k], i);
-                hat[k][i] = (element<R>(rx[k], i) - st.z) * st.w;
+                const float u = element<T>(wu, i);
+                hat[k][i] = (element<R>(wx, i) - st.z) * st.w;
                 acc_w2[k][i] += u * hat[k][i];
                 if constexpr (BIAS) acc_b2[k][i] += u;
                 d[k][i] = u * w2[i];
@@ -485,9 +534,11 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
         c *= inv;
         m = A.pre == RK_NORM_LAYER ? m * inv : 0.f;
 #pragma unroll
-        for (int k = 0; k < NC; ++k)
+        for (int k = 0; k < NC; ++k) {
+            const Words<R, CH> wd = whole_of<R, CH>(rd[k], at[k]);
 #pragma unroll
-            for (int i = 0; i < CH; ++i) d[k][i] = st.w * (d[k][i] - m - hat[k][i] * c) + element<R>(rd[k], i);
+            for (int i = 0; i < CH; ++i) d[k][i] = st.w * (d[k][i] - m - hat[k][i] * c) + element<R>(wd, i);
+        }
         c = 0.f; m = 0.f;
         const Row<R> dx(A.xo, r, A.xo_st, A.width);
 #pragma unroll
@@ -500,9 +551,10 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
                 t[i] = A.scale * d[k][i];
             }
             store_row<CUTS, R, CH, STREAM>(dx, at[k], t);
+            const Words<T, CH> wy = whole_of<T, CH>(ry[k], at[k]);
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
-                const float y = (element<T>(ry[k], i) - st.x) * st.y;
+                const float y = (element<T>(wy, i) - st.x) * st.y;
                 sum_dy[k][i] += d[k][i] * y;
                 if constexpr (BIAS) sum_d[k][i] += d[k][i];
                 hat[k][i] = y;

@@ -50,48 +50,69 @@ template <typename T, int N, int HINT = KEEP> __device__ __forceinline__ Words<T
     }
     return w;
 }
-template <bool CUTS, typename T, int N, int HINT = KEEP> __device__ __forceinline__ Words<T, N> fetch_row(const Row<T> &row, const Place &p) {
-    Words<T, N> w = fetch_at<T, N, HINT>(row, p.whole);
-    if (CUTS && p.cut_here) {
-        const uint32_t from = p.cut * (uint32_t)sizeof(T);
-        if constexpr (sizeof(T) == 4) {
-            static_assert(N == 4 || N == 8, "");
-            constexpr uint32_t HALF = N / 2;
-            uint32_t at = 0;
-            if (N == 8 && (p.tail & 4u)) {
-                const Vec<uint32_t, 4> x = __builtin_amdgcn_raw_buffer_load_b128(row.buf, from, 0, 0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] |= x[i];
-                at = HALF;
-            }
-            if (p.tail & 2u) {
-                const Vec<uint32_t, 2> x = __builtin_amdgcn_raw_buffer_load_b64(row.buf, from + 4u * at, 0, 0);
-#pragma unroll
-                for (uint32_t i = 0; i < 2; ++i) { if (at) w[(HALF + i) % N] |= x[i]; else w[i] |= x[i]; }
-            }
-            if (p.tail & 1u) {
-                const uint32_t x = __builtin_amdgcn_raw_buffer_load_b32(row.buf, from + 4u * (p.tail & 6u), 0, 0);
-#pragma unroll
-                for (uint32_t i = 0; i < N; i += 2) w[i] |= (p.tail & 6u) == i ? x : 0u;
-            }
-        } else {
-            static_assert(N == 8, "");
-            if (p.tail & 4u) {
-                const Vec<uint32_t, 2> x = __builtin_amdgcn_raw_buffer_load_b64(row.buf, from, 0, 0);
-                w[0] |= x[0]; w[1] |= x[1];
-            }
-            if (p.tail & 2u) {
-                const uint32_t x = __builtin_amdgcn_raw_buffer_load_b32(row.buf, from + 2u * (p.tail & 4u), 0, 0);
-                w[0] |= p.tail & 4u ? 0u : x; w[2] |= p.tail & 4u ? x : 0u;
-            }
-            if (p.tail & 1u) {
-                const uint32_t x = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(row.buf, from + 2u * (p.tail & 6u), 0, 0);
-#pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) w[i] |= (p.tail & 6u) == 2u * i ? x : 0u;
-            }
+// A vector under way: what is whole, and the pieces of one that is cut, four, two and one element of it.  They become one vector where
+// they are wanted (`whole_of`), so that a wavefront with a cut vector does not wait for each as it asks for it.
+template <bool CUTS, typename T, int N> struct Held { Words<T, N> w; };
+template <typename T, int N> struct Held<true, T, N> {
+    Words<T, N> w;
+    Vec<uint32_t, 4> four;              // (of narrow elements two words)
+    Vec<uint32_t, 2> two;               // (of narrow elements one word)
+    uint32_t one;
+};
+template <typename T, int N, int HINT = KEEP> __device__ __forceinline__ Held<true, T, N> hold_row(const Row<T> &row, const Place &p) {
+    Held<true, T, N> h;
+    h.w = fetch_at<T, N, HINT>(row, p.whole);
+    h.four = 0u; h.two = 0u; h.one = 0u;
+    if (!p.cut_here) return h;
+    const uint32_t from = p.cut * (uint32_t)sizeof(T);
+    if constexpr (sizeof(T) == 4) {
+        static_assert(N == 4 || N == 8, "");
+        if (N == 8 && (p.tail & 4u)) h.four = __builtin_amdgcn_raw_buffer_load_b128(row.buf, from, 0, 0);
+        if (p.tail & 2u) h.two = __builtin_amdgcn_raw_buffer_load_b64(row.buf, from + 4u * (N == 8 ? p.tail & 4u : 0u), 0, 0);
+        if (p.tail & 1u) h.one = __builtin_amdgcn_raw_buffer_load_b32(row.buf, from + 4u * (p.tail & 6u), 0, 0);
+    } else {
+        static_assert(N == 8, "");
+        if (p.tail & 4u) {
+            const Vec<uint32_t, 2> x = __builtin_amdgcn_raw_buffer_load_b64(row.buf, from, 0, 0);
+            h.four[0] = x[0]; h.four[1] = x[1];
         }
+        if (p.tail & 2u) h.two[0] = __builtin_amdgcn_raw_buffer_load_b32(row.buf, from + 2u * (p.tail & 4u), 0, 0);
+        if (p.tail & 1u) h.one = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(row.buf, from + 2u * (p.tail & 6u), 0, 0);
+    }
+    return h;
+}
+template <typename T, int N> __device__ __forceinline__ Words<T, N> whole_of(const Held<false, T, N> &h, const Place &) { return h.w; }
+template <typename T, int N> __device__ __forceinline__ Words<T, N> whole_of(const Held<true, T, N> &h, const Place &p) {
+    Words<T, N> w = h.w;
+    if (!p.cut_here) return w;
+    if constexpr (sizeof(T) == 4) {
+        const bool behind = N == 8 && (p.tail & 4u);
+        if constexpr (N == 8)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] |= h.four[i];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (N == 8) w[(4 + i) % N] |= behind ? h.two[i] : 0u;
+            w[i] |= behind ? 0u : h.two[i];
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < N; i += 2) w[i] |= (p.tail & 6u) == i ? h.one : 0u;
+    } else {
+        w[0] |= h.four[0]; w[1] |= h.four[1];
+        w[0] |= p.tail & 4u ? 0u : h.two[0]; w[2] |= p.tail & 4u ? h.two[0] : 0u;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) w[i] |= (p.tail & 6u) == 2u * i ? h.one : 0u;
     }
     return w;
+}
+template <bool CUTS, typename T, int N, int HINT = KEEP> __device__ __forceinline__ Words<T, N> fetch_row(const Row<T> &row, const Place &p) {
+    if constexpr (CUTS) return whole_of<T, N>(hold_row<T, N, HINT>(row, p), p);
+    else return fetch_at<T, N, HINT>(row, p.whole);
+}
+// HOLD: pieces stay apart; otherwise the vector is put together at once
+template <bool HOLD, bool CUTS, typename T, int N, int HINT = KEEP> __device__ __forceinline__ Held<HOLD, T, N> held(const Row<T> &row, const Place &p) {
+    if constexpr (HOLD) return hold_row<T, N, HINT>(row, p);
+    else return Held<false, T, N>{fetch_row<CUTS, T, N, HINT>(row, p)};
 }
 template <typename T, int W> __device__ __forceinline__ float element(const Vec<uint32_t, W> &w, int i) {
     if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
