@@ -804,7 +804,9 @@ int32_t rk_schedule_round_nodes(rk_ctx *ctx, const rk_jobs *jobs, const rk_plan_
  * sums over all rows or tokens in fixed order, so that equal calls return equal
  * bits.  A matrix without rows is no error: sums over its rows are zero.  With
  * the same shapes a call allocates nothing after the first, waits for nothing
- * and can be captured into a graph. */
+ * and can be captured into a graph.  A graph holds addresses of the context's
+ * working buffers: after a call of larger shapes on the same context, which
+ * moves them, it has to be captured anew. */
 #define RK_F32   0u
 #define RK_BF16  1u
 #define RK_F16   2u

@@ -335,12 +335,14 @@ __device__ __forceinline__ void keep_row(const DistillArgs &A, uint64_t r, const
 
 // A workgroup a row: its sums, its loss and, if there is a d_student, its gradient.  Of what a thread reads, its first NR vectors stay in
 // registers and its next NL in LDS until then; only what is beyond them is read again.
+// Short rows, of which several fit a compute unit, have registers for eight vectors at five wavefronts a SIMD (at eight: 4096 x 32000 losses
+// 74 us, now 51).
 template <bool CUTS, int THREADS, int NR, int NL, int MOST, typename T, int CH, int SUMS>
-__global__ __launch_bounds__(THREADS, 8) void k_distill_rows(DistillArgs A) {
+__global__ __launch_bounds__(THREADS, NL > 0 ? 8 : 5) void k_distill_rows(DistillArgs A) {
     extern __shared__ float4 kept_lds[];
     __shared__ float4 red[16];
     __shared__ Shares<MOST> lds;
-    constexpr uint32_t STEP = THREADS * CH;
+    constexpr uint32_t STEP = THREADS * CH, MORE = 4;              // vectors under way at once of what is beyond
     const uint64_t r = blockIdx.x;
     const Row<T> from(A.student, r, A.st, A.vocab), to(A.d_student, r, A.d_st, A.vocab);
     const float weight = A.row_weight ? A.row_weight[r] : 1.f;
@@ -398,13 +400,13 @@ __global__ __launch_bounds__(THREADS, 8) void k_distill_rows(DistillArgs A) {
             if (A.d_student) kept_lds[k * THREADS + threadIdx.x] = __builtin_bit_cast(float4, x[k]);
             take(NR + k, x[k]);
         }
-        for (uint32_t k = NR + NL; k <= whole; k += 4) {
-            Words<T, CH> y[4];
+        for (uint32_t k = NR + NL; k <= whole; k += MORE) {
+            Words<T, CH> y[MORE];
 #pragma unroll
-            for (uint32_t u = 0; u < 4; ++u)
+            for (uint32_t u = 0; u < MORE; ++u)
                 if (k + u <= whole) y[u] = fetch(k + u, keep);
 #pragma unroll
-            for (uint32_t u = 0; u < 4; ++u)
+            for (uint32_t u = 0; u < MORE; ++u)
                 if (k + u <= whole) take(k + u, y[u]);
         }
     }
@@ -438,13 +440,13 @@ __global__ __launch_bounds__(THREADS, 8) void k_distill_rows(DistillArgs A) {
             else store_row<CUTS, T, CH, STREAM>(to, last, g);
         };
         if constexpr (NL > 0)
-            for (uint32_t k = NR + NL; k <= whole; k += 4) {
-                Words<T, CH> y[4];
+            for (uint32_t k = NR + NL; k <= whole; k += MORE) {
+                Words<T, CH> y[MORE];
 #pragma unroll
-                for (uint32_t u = 0; u < 4; ++u)
+                for (uint32_t u = 0; u < MORE; ++u)
                     if (k + u <= whole) y[u] = fetch(k + u, stream);
 #pragma unroll
-                for (uint32_t u = 0; u < 4; ++u)
+                for (uint32_t u = 0; u < MORE; ++u)
                     if (k + u <= whole) give(k + u, y[u]);
             }
 #pragma unroll
@@ -558,29 +560,36 @@ __global__ __launch_bounds__(THREADS) void k_distill_gradient(DistillArgs A) {
 }
 
 // the rows' losses added up, in one order
-__global__ __launch_bounds__(256) void k_distill_total(DistillArgs A) {
-    __shared__ double lds[4];
+constexpr int TOTAL_THREADS = 1024;
+__global__ __launch_bounds__(TOTAL_THREADS) void k_distill_total(DistillArgs A) {
+    __shared__ double lds[TOTAL_THREADS / 64];
     double s = 0.0;
-    for (uint64_t r = threadIdx.x; r < A.n_rows; r += 1024) {
+    for (uint64_t r = threadIdx.x; r < A.n_rows; r += 4 * TOTAL_THREADS) {
         float w[4], l[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {                           // four under way at once
-            const uint64_t q = r + 256 * i < A.n_rows ? r + 256 * i : r;
+            const uint64_t q = r + TOTAL_THREADS * i < A.n_rows ? r + TOTAL_THREADS * i : r;
             w[i] = A.row_weight ? A.row_weight[q] : 1.f;
             l[i] = A.loss[q];
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s += r + 256 * i < A.n_rows && w[i] != 0.f ? (double)w[i] * (double)l[i] : 0.0;
+        for (int i = 0; i < 4; ++i) s += r + TOTAL_THREADS * i < A.n_rows && w[i] != 0.f ? (double)w[i] * (double)l[i] : 0.0;
     }
 #pragma unroll
     for (int off = 32; off; off >>= 1) s += __shfl_xor(s, off, 64);
     if ((threadIdx.x & 63u) == 0) lds[threadIdx.x >> 6] = s;
     __syncthreads();
-    if (threadIdx.x == 0) A.total[0] = (float)((lds[0] + lds[1]) + (lds[2] + lds[3]));
+    if (threadIdx.x) return;
+    s = 0.0;
+#pragma unroll
+    for (int w = 0; w < TOTAL_THREADS / 64; ++w) s += lds[w];
+    A.total[0] = (float)s;
 }
 
 // ---- host
-constexpr int DS_REGISTERS = 4, DS_LDS = 4;                     // vectors a thread of a long row keeps in LDS: 64 KB a workgroup, two of which fit a compute unit
+// Vectors that a thread of a long row keeps in registers and in LDS: 64 KB a workgroup, two of which fit a compute unit, at 64 registers
+// a lane.  A fourth in registers goes to scratch memory instead: 2048 x 128000 both at once 211 us with three, 219 with four, 512 x 64000 31 and 35.
+constexpr int DS_REGISTERS = 3, DS_LDS = 4;
 constexpr uint64_t DS_FEW = 256;                // rows
 constexpr uint32_t DS_SMALL = 16384;           // elements up to which 256 threads take a row or slice
 
@@ -693,7 +702,7 @@ int32_t run(rk_ctx *ctx, uint32_t type, DistillArgs &A, bool want_loss, bool wan
         if ((rc = send(ctx, type, A, STEP_GRADIENT)) != RK_OK) return rc;
     }
     if (want_loss) {
-        k_distill_total<<<1, 256, 0, ctx->stream>>>(A);
+        k_distill_total<<<1, TOTAL_THREADS, 0, ctx->stream>>>(A);
         RK_CHECK_LAUNCH(ctx, "k_distill_total");
     }
     return RK_OK;
