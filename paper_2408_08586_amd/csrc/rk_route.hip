@@ -159,7 +159,8 @@ __device__ __forceinline__ float balance_of(uint32_t n_experts, uint32_t top_k, 
     return n > 0.f ? (float)n_experts / ((float)top_k * n) * (cp / n) : 0.f;
 }
 
-// A workgroup's tokens belong to one group.  The only workgroup of a call ends it; otherwise k_route_join follows.
+// A workgroup's tokens belong to one group.  The only workgroup of a call ends it; otherwise k_route_join follows.  Bound by the chain of
+// top_k largest keys of a row and, of few tokens, by latency: 8192 x 256 bfloat16, k = 8, 7.6 us (4 MB of logits), 16 x 64 5.4 us.
 template <typename T, int L, int NV, bool CUTS>
 __global__ __launch_bounds__(RT_THREADS) void k_route_forward(RouteArgs A) {
     constexpr int SLOTS = 64 / L, V = 4 * NV, KEPT = (int)RK_MAX_TOP_K / L;
@@ -274,6 +275,7 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_forward(RouteArgs A) {
 }
 
 // The workgroups' parts of a group added up in their order: a workgroup has 16 experts, and 64 threads of it share an expert's parts.
+// Bound by latency, its launch and three trips to the device's scope one after the other: 6.6 us for 8192 x 256 in four groups.
 constexpr uint32_t RT_COLS = 16, RT_SHARE = 64;
 __global__ __launch_bounds__(RT_COLS * RT_SHARE) void k_route_join(RouteArgs A) {
     __shared__ float lds_p[RT_SHARE][RT_COLS], lds_n[16], lds_z[16];
@@ -349,7 +351,8 @@ __global__ __launch_bounds__(256) void k_route_nothing(RouteArgs A) {
 
 // d l = p (A - sum A p - sum y + d_z 2 lse / n) + y at the chosen experts, where y = p d weight, or, of renormalised weights,
 // w (d weight - sum w d weight), and then not in the sum.  y reaches its experts' lanes over LDS: zeros but for what a
-// token's lanes put there and take away again; the tokens of a wavefront use places of their own, in program order.
+// token's lanes put there and take away again; the tokens of a wavefront use places of their own, in program order.  131072 x 160 float32,
+// k = 6, 41.5 us, 174 MB, 4.2 TB/s: bound by HBM and, behind it, by the exponentials (about 350 instructions of a wavefront for four tokens).
 template <typename T, int L, int NV, bool CUTS>
 __global__ __launch_bounds__(RT_THREADS) void k_route_backward(RouteArgs A) {
     constexpr int SLOTS = 64 / L, KEPT = (int)RK_MAX_TOP_K / L;
