@@ -409,7 +409,8 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
     constexpr bool LEAN = MAXT == 768 && (BIAS || CUTS || sizeof(R) == 4);
     // The pieces of a cut vector stay apart until they are wanted, where there are registers for it: 4096 x 5003 104 -> 69 us, 8192 x 777
     // with biases 43 -> 35; but 4096 x 7777 in 32 bits 194 -> 262, 8192 x 777 52 -> 61, 4096 x 9999 149 -> 185.
-    constexpr bool HOLD = CUTS && sizeof(T) == 2 && (MAXT <= 512 || (MAXT == 1024 && sizeof(R) == 2));
+    // Elsewhere they are asked for where they are wanted: 4096 x 9999 with biases 254 -> 212 us, in 32 bits 358 -> 277.
+    constexpr bool HOLD = CUTS && sizeof(T) == 2 && (MAXT <= 512 || (MAXT == 1024 && sizeof(R) == 2)), LATE = CUTS && !HOLD;
     extern __shared__ float4 param_lds[];
     __shared__ float lds[96];
     const NormArgs &A = S.A;
@@ -433,8 +434,8 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
         const Row<T> u(there ? A.du : nullptr, r, A.du_st, A.width);
 #pragma unroll
         for (int k = 0; k < NC; ++k) {
-            rx[k] = held<HOLD, CUTS, R, CH, STREAM>(x, at[k]);
-            ru[k] = held<HOLD, CUTS, T, CH, STREAM>(u, at[k]);
+            rx[k] = held<HOLD, R, CH, STREAM>(x, at[k]);
+            ru[k] = held<HOLD, T, CH, STREAM>(u, at[k]);
         }
     };
     auto fetch_second = [&](uint64_t r) {
@@ -443,8 +444,8 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
         const Row<T> y(there ? A.y : nullptr, r, A.y_st, A.width);
 #pragma unroll
         for (int k = 0; k < NC; ++k) {
-            rd[k] = held<HOLD, CUTS, R, CH, STREAM>(dxo, at[k]);
-            ry[k] = held<HOLD, CUTS, T, CH, STREAM>(y, at[k]);
+            rd[k] = held<HOLD, R, CH, STREAM>(dxo, at[k]);
+            ry[k] = held<HOLD, T, CH, STREAM>(y, at[k]);
         }
     };
     fetch_first(begin);
@@ -468,12 +469,15 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
     auto vectors = [&](auto p) {
         typedef decltype(p) V;
         Held<HOLD, V, CH> w[3][NC];
+        auto hold_vector = [&](const Row<V> &of, const Place &p) {
+            if constexpr (HOLD) return hold_row<V, CH>(of, p); else return Held<false, V, CH>{fetch_row<CUTS, V, CH>(of, p)};
+        };
         const Row<V> w1(A.vec[G_POST_W], 0, 0, A.width), w2(A.vec[G_PRE_W], 0, 0, A.width), g(begin < r1 ? A.vec[G_GATE] : nullptr, gate, A.gate_st, A.width);
 #pragma unroll
         for (int k = 0; k < NC; ++k) {
-            w[L_W1][k] = held<HOLD, CUTS, V, CH>(w1, at[k]);
-            w[L_W2][k] = held<HOLD, CUTS, V, CH>(w2, at[k]);
-            w[L_GATE][k] = held<HOLD, CUTS, V, CH>(g, at[k]);
+            w[L_W1][k] = hold_vector(w1, at[k]);
+            w[L_W2][k] = hold_vector(w2, at[k]);
+            w[L_GATE][k] = hold_vector(g, at[k]);
         }
         const bool have[3] = {A.vec[G_POST_W] != nullptr, A.vec[G_PRE_W] != nullptr, A.vec[G_GATE] != nullptr};
 #pragma unroll
@@ -523,8 +527,15 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
         for (int k = 0; k < NC; ++k) {
             float w2[CH];
             get(L_W2, k, w2);
-            const Words<T, CH> wu = whole_of<T, CH>(ru[k], at[k]);
-            const Words<R, CH> wx = whole_of<R, CH>(rx[k], at[k]);
+            Words<T, CH> wu;
+            Words<R, CH> wx;
+            if constexpr (LATE) {
+                const Held<true, T, CH> hu = with_pieces<T, CH>(Row<T>(A.du, r, A.du_st, A.width), at[k], ru[k].w);
+                const Held<true, R, CH> hx = with_pieces<R, CH>(Row<R>(A.x, r, A.x_st, A.width), at[k], rx[k].w);
+                wu = whole_of<T, CH>(hu, at[k]); wx = whole_of<R, CH>(hx, at[k]);
+            } else {
+                wu = whole_of<T, CH>(ru[k], at[k]); wx = whole_of<R, CH>(rx[k], at[k]);
+            }
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
                 const float u = element<T>(wu, i);
@@ -542,7 +553,9 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
         m = A.pre == RK_NORM_LAYER ? m * inv : 0.f;
 #pragma unroll
         for (int k = 0; k < NC; ++k) {
-            const Words<R, CH> wd = whole_of<R, CH>(rd[k], at[k]);
+            Words<R, CH> wd;
+            if constexpr (LATE) wd = whole_of<R, CH>(with_pieces<R, CH>(Row<R>(A.dxo, r, A.dxo_st, A.width), at[k], rd[k].w), at[k]);
+            else wd = whole_of<R, CH>(rd[k], at[k]);
 #pragma unroll
             for (int i = 0; i < CH; ++i) d[k][i] = st.w * (d[k][i] - m - hat[k][i] * c) + element<R>(wd, i);
         }
@@ -558,7 +571,9 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
                 t[i] = A.scale * d[k][i];
             }
             store_row<CUTS, R, CH, STREAM>(dx, at[k], t);
-            const Words<T, CH> wy = whole_of<T, CH>(ry[k], at[k]);
+            Words<T, CH> wy;
+            if constexpr (LATE) wy = whole_of<T, CH>(with_pieces<T, CH>(Row<T>(A.y, r, A.y_st, A.width), at[k], ry[k].w), at[k]);
+            else wy = whole_of<T, CH>(ry[k], at[k]);
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
                 const float y = (element<T>(wy, i) - st.x) * st.y;

@@ -59,9 +59,10 @@ template <typename T, int N> struct Held<true, T, N> {
     Vec<uint32_t, 2> two;               // (of narrow elements one word)
     uint32_t one;
 };
-template <typename T, int N, int HINT = KEEP> __device__ __forceinline__ Held<true, T, N> hold_row(const Row<T> &row, const Place &p) {
+// the pieces beside a vector `w` that has been asked for
+template <typename T, int N> __device__ __forceinline__ Held<true, T, N> with_pieces(const Row<T> &row, const Place &p, const Words<T, N> &w) {
     Held<true, T, N> h;
-    h.w = fetch_at<T, N, HINT>(row, p.whole);
+    h.w = w;
     h.four = 0u; h.two = 0u; h.one = 0u;
     if (!p.cut_here) return h;
     const uint32_t from = p.cut * (uint32_t)sizeof(T);
@@ -80,6 +81,9 @@ template <typename T, int N, int HINT = KEEP> __device__ __forceinline__ Held<tr
         if (p.tail & 1u) h.one = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(row.buf, from + 2u * (p.tail & 6u), 0, 0);
     }
     return h;
+}
+template <typename T, int N, int HINT = KEEP> __device__ __forceinline__ Held<true, T, N> hold_row(const Row<T> &row, const Place &p) {
+    return with_pieces<T, N>(row, p, fetch_at<T, N, HINT>(row, p.whole));
 }
 template <typename T, int N> __device__ __forceinline__ Words<T, N> whole_of(const Held<false, T, N> &h, const Place &) { return h.w; }
 template <typename T, int N> __device__ __forceinline__ Words<T, N> whole_of(const Held<true, T, N> &h, const Place &p) {
@@ -109,10 +113,10 @@ template <bool CUTS, typename T, int N, int HINT = KEEP> __device__ __forceinlin
     if constexpr (CUTS) return whole_of<T, N>(hold_row<T, N, HINT>(row, p), p);
     else return fetch_at<T, N, HINT>(row, p.whole);
 }
-// HOLD: pieces stay apart; otherwise the vector is put together at once
-template <bool HOLD, bool CUTS, typename T, int N, int HINT = KEEP> __device__ __forceinline__ Held<HOLD, T, N> held(const Row<T> &row, const Place &p) {
+// HOLD: the pieces are asked for along with the vector; otherwise where it is wanted (with_pieces)
+template <bool HOLD, typename T, int N, int HINT = KEEP> __device__ __forceinline__ Held<HOLD, T, N> held(const Row<T> &row, const Place &p) {
     if constexpr (HOLD) return hold_row<T, N, HINT>(row, p);
-    else return Held<false, T, N>{fetch_row<CUTS, T, N, HINT>(row, p)};
+    else return Held<false, T, N>{fetch_at<T, N, HINT>(row, p.whole)};
 }
 template <typename T, int W> __device__ __forceinline__ float element(const Vec<uint32_t, W> &w, int i) {
     if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
