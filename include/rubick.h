@@ -840,10 +840,14 @@ typedef struct {
 } rk_norm_block;
 
 /* Gradients of a block's vectors, float32 [device]; those not wanted, or whose
- * vector is null, are null.  Gates' gradients lie gate_stride elements apart. */
+ * vector is null, are null.  Gates' gradients lie gate_stride elements apart.
+ * gates: how many gates there are where the block has gate_rows; those behind
+ * the last row's have a gradient of zero.  0: as many as the rows need, and no
+ * other is written.  Fewer than the rows need are refused. */
 typedef struct {
     float *post_weight, *post_bias, *pre_weight, *pre_bias, *gate;
     uint64_t gate_stride;
+    uint64_t gates;
 } rk_norm_grads;
 
 /* x, x_out share a type: that of y and u, or RK_F32.  y null: x_out = res_scale * x (the

@@ -626,7 +626,8 @@ class rk_norm_block(C.Structure):
 
 
 class rk_norm_grads(C.Structure):
-    _fields_ = [(n, C.c_void_p) for n in ("post_weight", "post_bias", "pre_weight", "pre_bias", "gate")] + [("gate_stride", C.c_uint64)]
+    _fields_ = [(n, C.c_void_p) for n in ("post_weight", "post_bias", "pre_weight", "pre_bias", "gate")] + \
+               [("gate_stride", C.c_uint64), ("gates", C.c_uint64)]
 
 
 class rk_router(C.Structure):
@@ -761,7 +762,8 @@ class NormBlock:
 
 
 class NormGrads:
-    """Room for the gradients of a block's vectors, float32; `tensors` by name (all that the block has, or those named)."""
+    """Room for the gradients of a block's vectors, float32; `tensors` by name (all that the block has, or those named).  Of gates that
+    no row of a call uses, the gradients are zero."""
 
     def __init__(self, block: NormBlock, names=None):
         import torch
@@ -771,7 +773,7 @@ class NormGrads:
                         if t is not None and (names is None or n in names)}
         ptr = {n: t.data_ptr() for n, t in self.tensors.items()}
         self.c = rk_norm_grads(*[ptr.get(n) for n in ("post_weight", "post_bias", "pre_weight", "pre_bias", "gate")],
-                               block.width or 0)
+                               block.width or 0, block.gate.shape[0] if block.gate is not None and block.c.gate_rows else 0)
 
 
 def rk_norm_forward(ctx, block: NormBlock, x, y, x_out, u, stats):

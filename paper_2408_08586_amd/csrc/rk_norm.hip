@@ -719,6 +719,11 @@ template <int LANES> __global__ __launch_bounds__(1024) void k_norm_join(Joined 
     to[col0 + threadIdx.x] = sum;
 }
 
+// gates that no row has: their gradients are sums over nothing
+__global__ __launch_bounds__(256) void k_norm_no_rows(float *to, uint64_t stride, uint64_t gates, uint32_t width) {
+    for (uint64_t i = blockIdx.x * 256ull + threadIdx.x; i < gates * width; i += gridDim.x * 256ull) to[i / width * stride + i % width] = 0.f;
+}
+
 // ---- host
 struct Shape { int nc; uint32_t threads, rows_per_wg; bool per_wave; };
 
@@ -894,10 +899,13 @@ extern "C" int32_t rk_norm_backward(rk_ctx *ctx, const rk_norm_block *block, uin
     for (int s = 0; s < G_VECTORS; ++s) {
         if (out[s] && (!have[s] || ((uintptr_t)out[s] & 3u))) return rk_fail(ctx, RK_ERR_INVALID_ARG, "gradient of a vector that is not there, or misaligned");
     }
-    if (n_rows == 0 && block->gate_rows) out[G_GATE] = nullptr;         // no row, no gate
+    // the gates that rows use, and those behind them whose gradients are asked for
+    const uint64_t needed = !out[G_GATE] || !block->gate_rows ? 0 : n_rows / block->gate_rows + (n_rows % block->gate_rows != 0);
+    const uint64_t all_gates = out[G_GATE] && block->gate_rows && grads->gates ? grads->gates : needed;
+    if (all_gates < needed || all_gates > 0x7FFFFFFFull) return rk_fail(ctx, RK_ERR_INVALID_ARG, "fewer gates than the rows need, or more than 2^31 - 1");
+    if (all_gates > 1 && grads->gate_stride < width) return rk_fail(ctx, RK_ERR_INVALID_ARG, "gate_stride of the gradients below the width");
+    if (block->gate_rows && !all_gates) out[G_GATE] = nullptr;              // no row, no gate
     for (float *o : out) any = any || o;
-    if (out[G_GATE] && block->gate_rows && n_rows > block->gate_rows && grads->gate_stride < width)
-        return rk_fail(ctx, RK_ERR_INVALID_ARG, "gate_stride of the gradients below the width");
     if (n_rows == 0 && !any) return RK_OK;
     RK_HIP(ctx, hipSetDevice(ctx->device));
     NormArgs A{};
@@ -973,6 +981,12 @@ extern "C" int32_t rk_norm_backward(rk_ctx *ctx, const rk_norm_block *block, uin
         if (narrow) k_norm_join<4><<<(uint32_t)(join_jobs * tiles), 1024, 0, ctx->stream>>>(J, width, tiles);
         else k_norm_join<16><<<(uint32_t)(join_jobs * tiles), 1024, 0, ctx->stream>>>(J, width, tiles);
         RK_CHECK_LAUNCH(ctx, "k_norm_join");
+    }
+    const uint64_t written = needed ? needed : 1;               // (without a row the join has the first)
+    if (all_gates > written) {
+        const uint64_t blocks = ((all_gates - written) * width + 255) / 256;
+        k_norm_no_rows<<<(uint32_t)(blocks < 2048 ? blocks : 2048), 256, 0, ctx->stream>>>(out[G_GATE] + written * grads->gate_stride, grads->gate_stride, all_gates - written, width);
+        RK_CHECK_LAUNCH(ctx, "k_norm_no_rows");
     }
     return RK_OK;
 }

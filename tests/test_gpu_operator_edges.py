@@ -1,0 +1,77 @@
+"""The training-step operators at the edges of what their header promises, each held against the definition in 64 bits or against a call
+that needs no edge.  Tolerances are those of the operators' own tests, or derived where they are used.
+"""
+import pytest
+
+from oracle import training
+from test_gpu_distill import TERMS, U32, Student
+from test_gpu_norm import ALL, Case
+from test_gpu_route import Route, logits_of
+
+pytestmark = pytest.mark.gpu
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module")
+def gpu():
+    import torch
+    assert torch.cuda.is_available(), "these tests need the GPU"
+    import paper_2408_08586_amd as rk
+    ctx = rk.rk_create(0)
+    yield torch, rk, ctx
+    rk.rk_sync(ctx)
+    rk.rk_destroy(ctx)
+
+
+@pytest.mark.parametrize("rows,gate_rows,gates", [(15, 10, 5), (8, 10, 2), (10, 10, 3), (300, 7, 60), (3000, 2, 1600), (1, 1, 2), (0, 4, 3)])
+@pytest.mark.parametrize("width", [40, 521, 2056, 13000])
+def test_gates_without_rows_have_zero_gradients(gpu, rows, gate_rows, gates, width):
+    """As in a shorter last batch: the gates behind the last row's are there, and no row uses them."""
+    torch, rk, ctx = gpu
+    if width > 3000 and rows > 300:
+        rows, gates = 40, 33
+    c = Case(torch, rows, width, gate=gates, gate_rows=gate_rows, vectors=ALL, seed=3)
+    x_out, u, stats = c.forward(rk, ctx)
+    dx, dy, grads = c.backward(rk, ctx, x_out, stats)
+    used = (rows + gate_rows - 1) // gate_rows
+    assert grads["gate"].shape[0] == gates and bool((grads["gate"][used:] == 0).all())
+    c.vec["gate"] = c.vec["gate"][:max(used, 1)]
+    ex, ey, exact = c.backward(rk, ctx, x_out, stats)
+    assert torch.equal(dx, ex) and torch.equal(dy, ey)
+    for name, v in exact.items():
+        assert torch.equal(grads[name][:used] if name == "gate" else grads[name], v[:used] if name == "gate" else v), name
+    # the gates' gradient alone, and in a call that follows one with more rows
+    block = rk.NormBlock(post=c.post, pre=c.pre, gate_rows=gate_rows, **dict(c.vec, gate=torch.ones(gates, width, dtype=c.p, device="cuda")))
+    alone = rk.NormGrads(block, ("gate",))
+    alone.tensors["gate"].fill_(7.0)
+    rk.rk_norm_backward(ctx, block, x_out, c.y, stats, c.dxo, c.du, dx, dy, alone)
+    assert bool((alone.tensors["gate"][used:] == 0).all()) and bool(torch.isfinite(alone.tensors["gate"]).all())
+
+
+def test_gates_without_rows_in_a_graph(gpu):
+    torch, rk, _ = gpu
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        ctx = rk.rk_create(0)
+        c = Case(torch, 50, 300, gate=9, gate_rows=20, vectors=ALL)
+        block = c.block(rk)
+        grads = rk.NormGrads(block)
+        x_out, u, stats = c.forward(rk, ctx)
+        dx, dy = c.rows_of(None, c.r), c.rows_of(None, c.t)
+        step = lambda: rk.rk_norm_backward(ctx, block, x_out, c.y, stats, c.dxo, c.du, dx, dy, grads)
+        step()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            step()
+        for turn in range(3):
+            c.du.mul_(1.25)
+            for v in grads.tensors.values():
+                v.fill_(NAN)
+            graph.replay()
+            replayed = [t.clone() for t in (dx, dy, *grads.tensors.values())]
+            step()
+            for a, b in zip(replayed, (dx, dy, *grads.tensors.values())):
+                assert torch.equal(a, b), turn
+            assert bool((grads.tensors["gate"][3:] == 0).all())
+        rk.rk_sync(ctx)
+        rk.rk_destroy(ctx)

@@ -1,0 +1,19 @@
+"""Host-side: what the training-step operators refuse beside test_operators_abi.py, and that their binding leaves the library as it is."""
+import ctypes as C
+
+import pytest
+
+from test_operators_abi import call, rk  # noqa: F401  (fixtures)
+
+
+def test_gates_of_the_gradients(call, rk):
+    """Fewer gates than the rows need, a stride that lets gates overlap, more than are counted."""
+    P, m = call.P, call.matrix
+
+    def backward(rows, gate_rows, gates, stride):
+        b = rk.rk_norm_block(1, 1, 1e-6, 1e-6, 1.0, 1, P, None, P, None, P, gate_rows, 64)
+        g = rk.rk_norm_grads(P, None, P, None, P, stride, gates)
+        return call.lib.rk_norm_backward(call.ctx, C.byref(b), C.c_uint64(rows), C.c_uint32(64), m(), m(), C.c_void_p(P), m(), m(), m(), m(), C.byref(g))
+
+    for rows, gate_rows, gates, stride in ((9, 4, 2, 64), (8, 4, 1, 64), (3, 4, 2, 63), (0, 4, 3, 63), (9, 4, 3, 63), (9, 4, 1 << 31, 64)):
+        assert backward(rows, gate_rows, gates, stride) == rk.RK_ERR_INVALID_ARG and call.text(), (rows, gate_rows, gates, stride)
