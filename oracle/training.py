@@ -118,7 +118,7 @@ def route(logits, mask, top_k, renormalise, group_tokens, d_loss=None, d_weight=
         expert[t, :len(order)] = torch.tensor(order)
         weight[t, :len(order)] = p[t, order]
         if renormalise:
-            weight[t] = weight[t] / weight[t].sum()
+            weight[t, :len(order)] = weight[t, :len(order)] / weight[t].sum()
         g = t // per
         counts[g, order] += 1
         prob_sum[g] += p[t]

@@ -233,7 +233,7 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_forward(RouteArgs A) {
             const int32_t e = Keys<T>::expert(mine[h]);
             if (live && k < K) {
                 A.expert[t * K + k] = e;
-                A.weight[t * K + k] = w[h] * scale;
+                A.weight[t * K + k] = e >= 0 ? w[h] * scale : 0.f;     // (scale is NaN beside a NaN)
                 if (e >= 0) atomicAdd(&hist[e], 1u);
             }
         }

@@ -75,3 +75,28 @@ def test_gates_without_rows_in_a_graph(gpu):
             assert bool((grads.tensors["gate"][3:] == 0).all())
         rk.rk_sync(ctx)
         rk.rk_destroy(ctx)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("renorm", [False, True])
+@pytest.mark.parametrize("n", [12, 1500])
+def test_choices_that_are_not_there_have_weight_zero(gpu, dtype, renorm, n):
+    """Also those of a token with a NaN, whose chosen ones have weight NaN."""
+    torch = gpu[0]
+    l = logits_of(torch, n, 48, dtype)
+    l[1], l[2], l[3], l[4], l[5] = NAN, -INF, -INF, NAN, -INF
+    l[2, 7] = NAN                                        # beside nothing but -inf
+    l[3, 5], l[3, 9] = NAN, 1.0                          # two of them chosen
+    l[3, 20] = 2.0
+    l[4, 30] = 0.5                                       # one chosen
+    l[6, 3] = NAN                                        # all chosen
+    l[7] = -INF
+    l[7, [4, 8]] = 1.0                                   # no NaN: two chosen, their weights as they are
+    got = {k: v.cpu() for k, v in Route(gpu, l, None, 4, renorm).forward().items()}
+    none = got["expert"] < 0
+    assert none[[1, 2, 5]].all() and none[3].tolist() == none[7].tolist() == [False, False, True, True] and none[4].tolist() == [False, True, True, True]
+    assert bool((got["weight"][none] == 0).all())
+    assert bool(torch.isnan(got["weight"][[3, 4, 6]][~none[[3, 4, 6]]]).all()) \
+        and bool(((got["weight"][7, :2] - 0.5).abs() <= 4 * U32).all())
+    ref = training.route(l[:8].double(), None, 4, renorm, 0)
+    assert torch.equal(ref["weight"].isnan(), got["weight"][:8].isnan()) and bool((ref["weight"][none[:8]] == 0).all())
