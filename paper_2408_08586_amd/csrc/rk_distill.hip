@@ -29,6 +29,12 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 
+// a product that is rounded by itself, not fused with what is added to it
+__device__ __forceinline__ float times(float a, float b) {
+#pragma clang fp contract(off)
+    return a * b;
+}
+
 // The exponentials of a row: one stream where the two terms of the loss share it (T = 1) or one of them is all there is, two
 // streams otherwise, of which the second is the first's square if T = 2.
 enum { ONE, TWO, SQUARE };
@@ -211,24 +217,43 @@ template <int WAVES, bool MAX> __device__ __forceinline__ void block_all(float4 
     v = make_float4(row(o.x), row(o.y), row(o.z), row(o.w));
 }
 
-// d s of a logit: the streams' exponentials are e^(k (s - top) - l), in the streams' units
-template <typename T, int SUMS> struct Slope {
-    float ka, kb, top, la, lb, ba, bb, ca, cb;
+// d s of a logit.  The streams' exponentials are e^(k (s - top) - l) in the streams' units, top the row's largest logit and l the
+// logarithms of the sums relative to it; or, from the log sums (LSE), e^(s / T - lse_T) and e^(s - lse_1): each stream from its own, since what
+// lse_T T has beyond the largest logit grows with T and would take the second stream's digits.
+template <typename T, int SUMS, bool LSE> struct Slope {
+    float ka, kb, inv, a, b, la, lb, ba, bb, ca, cb;
     float ft, f1;                       // of a kept logit's share, of the label
-    __device__ __forceinline__ Slope(const DistillArgs &A, const Streams &S, float top_, float la_, float lb_, float weight, bool kept, bool labelled)
-        : ka(S.ka), kb(S.kb), top(top_), la(la_), lb(lb_), ba(top_ * S.ka + la_), bb(top_ * S.kb + lb_) {
+    bool apart;                         // a 16-bit student's exponents are too large for one fused product
+    __device__ __forceinline__ Slope(const DistillArgs &A, const Streams &S, float weight, bool kept, bool labelled) : ka(S.ka), kb(S.kb), inv(S.inv_a) {
         const float scale = weight * (A.d_total ? A.d_total[0] : 1.f);
         ft = kept ? scale * A.kd * A.temperature : 0.f;
         f1 = labelled ? scale * A.ce : 0.f;
         // (a stream that both terms share, or that is the only term's)
         ca = SUMS == ONE ? ft + f1 : ft;
-        cb = SUMS == SQUARE ? f1 * Exp<T>::of(la + la - lb) : f1;
+    }
+    static __device__ __forceinline__ Slope of_sums(const DistillArgs &A, const Streams &S, float top, float la, float lb, float weight, bool kept, bool labelled) {
+        Slope s(A, S, weight, kept, labelled);
+        s.a = s.b = top; s.la = la; s.lb = lb;
+        s.ba = top * S.ka + la; s.bb = top * S.kb + lb;
+        s.cb = SUMS == SQUARE ? s.f1 * Exp<T>::of(la + la - lb) : s.f1;
+        s.apart = is_huge(top);
+        return s;
+    }
+    static __device__ __forceinline__ Slope of_lse(const DistillArgs &A, const Streams &S, float lse_a, float lse_b, float weight, bool kept, bool labelled) {
+        const float U = Exp<T>::unit();
+        Slope s(A, S, weight, kept, labelled);
+        s.a = lse_a; s.b = lse_b;
+        s.ba = lse_a * U; s.bb = lse_b * U;
+        s.cb = SUMS == SQUARE ? s.f1 * Exp<T>::of((lse_a + lse_a - lse_b) * U) : s.f1;
+        s.apart = is_huge(lse_a) || is_huge(lse_b);
+        return s;
     }
     template <bool APART> __device__ __forceinline__ float of(float x) const {
-        const float v = x - top;
-        const float e = Exp<T>::of(APART ? __builtin_fmaf(v, ka, -la) : __builtin_fmaf(x, ka, -ba));
+        const float U = Exp<T>::unit();
+        // (a largest logit's product is rounded as in its log sum, so that no probability is beyond one)
+        const float e = Exp<T>::of(!APART ? __builtin_fmaf(x, ka, -ba) : LSE ? (times(x, inv) - a) * U : __builtin_fmaf(x - a, ka, -la));
         if constexpr (SUMS == ONE) return ca * e;
-        if constexpr (SUMS == TWO) return ca * e + cb * Exp<T>::of(APART ? __builtin_fmaf(v, kb, -lb) : __builtin_fmaf(x, kb, -bb));
+        if constexpr (SUMS == TWO) return ca * e + cb * Exp<T>::of(!APART ? __builtin_fmaf(x, kb, -bb) : LSE ? (x - b) * U : __builtin_fmaf(x - b, kb, -lb));
         return e * (ca + cb * e);
     }
     __device__ __forceinline__ float operator()(float x) const { return of<Exp<T>::EXACT>(x); }
@@ -264,19 +289,19 @@ template <int THREADS, int MOST> __device__ __forceinline__ float share_wanted(c
     return threadIdx.x == THREADS - 1 && W.label >= 0 ? together(W.label) : 0.f;
 }
 // where teacher or label have something in [begin, end): the whole value, once more (equal indices get equal values)
-template <int THREADS, int MOST, typename T, int SUMS>
-__device__ __forceinline__ void write_wanted(const Wanted<THREADS, MOST> &W, const Slope<T, SUMS> &slope, T *out, uint32_t begin, uint32_t end, float label_q) {
+template <int THREADS, int MOST, typename T, int SUMS, bool LSE>
+__device__ __forceinline__ void write_wanted(const Wanted<THREADS, MOST> &W, const Slope<T, SUMS, LSE> &slope, T *out, uint32_t begin, uint32_t end, float label_q) {
     auto again = [&](int32_t i, float s, float mass) {
         if ((uint32_t)i < begin || (uint32_t)i >= end) return;
-        out[i] = (T)((is_huge(slope.top) ? slope.template of<true>(s) : slope(s)) - slope.ft * mass - (i == W.label ? slope.f1 : 0.f));
+        out[i] = (T)((slope.apart ? slope.template of<true>(s) : slope(s)) - slope.ft * mass - (i == W.label ? slope.f1 : 0.f));
     };
 #pragma unroll
     for (int n = 0; n < Wanted<THREADS, MOST>::N; ++n)
         if (W.at[n] >= 0) again(W.at[n], W.s[n], W.t[n]);
     if (threadIdx.x == THREADS - 1 && W.label >= 0) again(W.label, W.label_s, label_q);
 }
-template <bool CUTS, int THREADS, typename T, int CH, int SUMS>
-__device__ __forceinline__ void write_huge(const Row<T> &from, const Row<T> &to, uint32_t begin, uint32_t end, const Slope<T, SUMS> &slope) {
+template <bool CUTS, int THREADS, typename T, int CH, int SUMS, bool LSE>
+__device__ __forceinline__ void write_huge(const Row<T> &from, const Row<T> &to, uint32_t begin, uint32_t end, const Slope<T, SUMS, LSE> &slope) {
     for (uint32_t c = begin + threadIdx.x * CH; c < end; c += THREADS * CH) {
         const Place p(c, end, CH);
         float v[CH];
@@ -287,10 +312,10 @@ __device__ __forceinline__ void write_huge(const Row<T> &from, const Row<T> &to,
     }
 }
 template <bool CUTS, int THREADS, typename T, int CH, int SUMS>
-__device__ __forceinline__ void write_gradient(const DistillArgs &A, const Row<T> &from, const Row<T> &to, T *out, uint32_t begin, uint32_t end, const Slope<T, SUMS> &slope,
+__device__ __forceinline__ void write_gradient(const DistillArgs &A, const Row<T> &from, const Row<T> &to, T *out, uint32_t begin, uint32_t end, const Slope<T, SUMS, true> &slope,
                                                Wanted<THREADS> &W, float t_sum, Shares<(int)RK_MAX_TEACHER_LOGITS> &lds) {
     const float label_q = share_wanted(A, W, t_sum, lds);
-    if (is_huge(slope.top)) write_huge<CUTS, THREADS, T, CH, SUMS>(from, to, begin, end, slope);
+    if (slope.apart) write_huge<CUTS, THREADS, T, CH>(from, to, begin, end, slope);
     else stream_row<CUTS, THREADS, T, CH, STREAM>(from, begin, end,
         [&](uint32_t first, const Words<T, CH> &w) {
             float v[CH];
@@ -320,7 +345,7 @@ template <typename T, int SUMS> __device__ __forceinline__ RowLoss row_loss(cons
     L.left = false;
     L.la = Exp<T>::log(sa);
     L.lb = SUMS == ONE ? L.la : Exp<T>::log(sb);
-    L.lse_a = top * S.inv_a + Exp<T>::natural(L.la);
+    L.lse_a = times(top, S.inv_a) + Exp<T>::natural(L.la);
     L.lse_b = SUMS == ONE ? L.lse_a : top + Exp<T>::natural(L.lb);
     L.loss = 0.f;
     if (A.kd > 0.f && cross.y != 0.f) L.loss = A.kd * A.temperature * A.temperature * (cross.x / cross.y - logf(cross.y) + L.lse_a);
@@ -428,10 +453,10 @@ __global__ __launch_bounds__(THREADS, NL > 0 ? 8 : 5) void k_distill_rows(Distil
         write_zeros<CUTS, THREADS, T, CH>(to, 0, A.vocab);
         return;
     }
-    const Slope<T, SUMS> slope(A, S, top, L.la, L.lb, weight, v.z != 0.f, W.label >= 0);
+    const auto slope = Slope<T, SUMS, false>::of_sums(A, S, top, L.la, L.lb, weight, v.z != 0.f, W.label >= 0);
     const float label_q = share_wanted(A, W, v.z, lds);
-    if (is_huge(top)) {
-        write_huge<CUTS, THREADS, T, CH, SUMS>(from, to, 0, A.vocab, slope);
+    if (slope.apart) {
+        write_huge<CUTS, THREADS, T, CH>(from, to, 0, A.vocab, slope);
     } else {
         auto give = [&](uint32_t k, const Words<T, CH> &x) {
             float g[CH];
@@ -554,11 +579,8 @@ __global__ __launch_bounds__(THREADS) void k_distill_gradient(DistillArgs A) {
         write_zeros<CUTS, THREADS, T, CH>(to, begin, end);
         return;
     }
-    // relative to where the first stream's exponential is one
-    const Streams S = streams_of<T>(A);
-    const float top = SUMS == ONE && A.kd == 0.f ? la : la * A.temperature;
     write_gradient<CUTS, THREADS, T, CH, SUMS>(A, from, to, (T *)A.d_student + r * A.d_st, begin, end,
-                                               Slope<T, SUMS>(A, S, top, 0.f, (lb - top) * S.kb, weight, sum != 0.f, W.label >= 0), W, sum, lds);
+                                               Slope<T, SUMS, true>::of_lse(A, streams_of<T>(A), la, lb, weight, sum != 0.f, W.label >= 0), W, sum, lds);
 }
 
 // the rows' losses added up, in one order

@@ -100,3 +100,12 @@ def test_choices_that_are_not_there_have_weight_zero(gpu, dtype, renorm, n):
         and bool(((got["weight"][7, :2] - 0.5).abs() <= 4 * U32).all())
     ref = training.route(l[:8].double(), None, 4, renorm, 0)
     assert torch.equal(ref["weight"].isnan(), got["weight"][:8].isnan()) and bool((ref["weight"][none[:8]] == 0).all())
+
+
+@pytest.mark.parametrize("tau", [20.0, 100.0, 1e3, 1e5])
+@pytest.mark.parametrize("rows,vocab", [(5, 1000), (5, 20001), (300, 1000)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_high_temperatures_leave_the_labels_loss_alone(gpu, tau, rows, vocab, dtype):
+    """The label's probability is no less exact the higher the temperature of the other term, whether the gradient is taken by itself, of
+    rows in slices or along with the loss.  (kd_weight 1 / T^2: both terms of the loss are of size one.)"""
+    Student(gpu, rows, vocab, 8, dtype, tau=tau, kd=1 / tau ** 2, ce=0.5).check()
