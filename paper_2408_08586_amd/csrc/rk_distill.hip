@@ -20,7 +20,7 @@ struct DistillArgs {
     float temperature, kd, ce;
     uint32_t slices, slice;             // of a row, where several workgroups share it, and their elements
     float4 *part;                       // [row][slice]: largest logit, sums of the exponentials relative to it
-    float4 *cross;                      // [row]: what teacher and label add to the loss
+    float4 *cross;                      // [row]: what teacher and label add to the loss; then the row's largest logit and its sums' logarithms
 };
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -39,10 +39,11 @@ __device__ __forceinline__ float times(float a, float b) {
 // streams otherwise, of which the second is the first's square if T = 2.
 enum { ONE, TWO, SQUARE };
 
-// A 16-bit student's are taken to base 2, e^(x/T - r) = 2^(x log2(e)/T - r'): one fused product and one instruction, whose exponent's
-// rounding, 2^-24 of it, is far below a step of the logits.  Rows whose largest logit is beyond HUGE_LOGIT (all of them masked by the
-// type's lowest value) would overflow there, and a 32-bit student wants its exponents closer: these take differences of logits first.
-constexpr float HUGE_LOGIT = 1e30f;
+// A 16-bit student's are taken to base 2, e^(x/T - r) = 2^(x log2(e)/T - r'): one fused product and one instruction.  r' is rounded by up to
+// 2^-24 of itself, and the exponent with it: below 2^11 that is 2^-14 at most, an eighth of a float16's half step.  Rows whose largest logit is
+// further from zero (all of them masked by a large value, say) and a 32-bit student take differences of logits first, which lose nothing
+// (and which the largest of 32-bit logits, beyond HUGE_LOGIT, would overflow while the largest of the row is not known).
+constexpr float FUSED_EXPONENT = 2048.f, HUGE_LOGIT = 1e30f;
 template <typename T> struct Exp {
     static constexpr bool EXACT = sizeof(T) == 4;
     static __device__ __forceinline__ float of(float x) { return EXACT ? exp_f32(x) : __builtin_amdgcn_exp2f(x); }
@@ -50,18 +51,21 @@ template <typename T> struct Exp {
     static __device__ __forceinline__ float unit() { return EXACT ? 1.f : 1.4426950408889634f; }
     static __device__ __forceinline__ float natural(float x) { return EXACT ? x : x * 0.6931471805599453f; }
 };
-struct Streams { float ka, kb, inv_a; };        // what a logit is multiplied by; the first without the base
-template <typename T> __device__ __forceinline__ Streams streams_of(const DistillArgs &A) {
-    const float inv = A.kd > 0.f ? 1.f / A.temperature : 1.f;
-    return Streams{inv * Exp<T>::unit(), Exp<T>::unit(), inv};
+// what a logit is multiplied by, the first also without the base; the largest that goes the short way
+struct Streams {
+    float ka, kb, inv_a, most;
+    __device__ __forceinline__ bool huge(float top) const { return fabsf(top) > most && top != -INFINITY; }
+};
+template <typename T, int SUMS> __device__ __forceinline__ Streams streams_of(const DistillArgs &A) {
+    const float inv = A.kd > 0.f ? 1.f / A.temperature : 1.f, ka = inv * Exp<T>::unit(), kb = Exp<T>::unit();
+    return Streams{ka, kb, inv, Exp<T>::EXACT ? HUGE_LOGIT : FUSED_EXPONENT / (SUMS == ONE ? ka : fmaxf(ka, kb))};
 }
-__device__ __forceinline__ bool is_huge(float top) { return fabsf(top) > HUGE_LOGIT && top != -INFINITY; }
 
 // the sums of a stretch of logits, relative to the largest of them seen so far
 template <typename T, int SUMS> struct Running {
     float m = -INFINITY, ref = 0.f, ra = 0.f, rb = 0.f, sa = 0.f, sb = 0.f;     // (nothing above -inf yet: relative to 0)
     __device__ __forceinline__ void rebase(const Streams &S, float top) {
-        const float r = fminf(fmaxf(top, -HUGE_LOGIT), HUGE_LOGIT);             // (of a row that is not huge, one of its huge parts: its sums are zero)
+        const float r = fminf(fmaxf(top, -S.most), S.most);     // (a part that is huge: of a row that is not, its sums count from -most; a row that is takes sum_huge)
         if (m != -INFINITY) {
             const float f = Exp<T>::of((ref - r) * S.ka);
             sa *= f;
@@ -218,43 +222,41 @@ template <int WAVES, bool MAX> __device__ __forceinline__ void block_all(float4 
 }
 
 // d s of a logit.  The streams' exponentials are e^(k (s - top) - l) in the streams' units, top the row's largest logit and l the
-// logarithms of the sums relative to it; or, from the log sums (LSE), e^(s / T - lse_T) and e^(s - lse_1): each stream from its own, since what
-// lse_T T has beyond the largest logit grows with T and would take the second stream's digits.
-template <typename T, int SUMS, bool LSE> struct Slope {
-    float ka, kb, inv, a, b, la, lb, ba, bb, ca, cb;
+// logarithms of the sums relative to it; or, from the log sums, e^(s / T - lse_T) and e^(s - lse_1): each stream from its own, since what
+// lse_T T has beyond the largest logit grows with T and would take the second stream's digits.  EITHER: which of them is known at the call.
+template <typename T, int SUMS, bool EITHER> struct Slope {
+    float ka, kb, ba, bb, ca, cb;       // fused: e^(ka s - ba), e^(kb s - bb)
+    float pre, pa, a, la, b, lb;        // from differences: e^(pa (pre s - a) - la), e^(kb (s - b) - lb)
     float ft, f1;                       // of a kept logit's share, of the label
     bool apart;                         // a 16-bit student's exponents are too large for one fused product
-    __device__ __forceinline__ Slope(const DistillArgs &A, const Streams &S, float weight, bool kept, bool labelled) : ka(S.ka), kb(S.kb), inv(S.inv_a) {
+    __device__ __forceinline__ Slope(const DistillArgs &A, const Streams &S, float weight, bool kept, bool labelled) : ka(S.ka), kb(S.kb) {
         const float scale = weight * (A.d_total ? A.d_total[0] : 1.f);
         ft = kept ? scale * A.kd * A.temperature : 0.f;
         f1 = labelled ? scale * A.ce : 0.f;
         // (a stream that both terms share, or that is the only term's)
         ca = SUMS == ONE ? ft + f1 : ft;
     }
-    static __device__ __forceinline__ Slope of_sums(const DistillArgs &A, const Streams &S, float top, float la, float lb, float weight, bool kept, bool labelled) {
-        Slope s(A, S, weight, kept, labelled);
-        s.a = s.b = top; s.la = la; s.lb = lb;
-        s.ba = top * S.ka + la; s.bb = top * S.kb + lb;
-        s.cb = SUMS == SQUARE ? s.f1 * Exp<T>::of(la + la - lb) : s.f1;
-        s.apart = is_huge(top);
-        return s;
+    __device__ __forceinline__ void from_sums(const Streams &S, float top, float la_, float lb_) {
+        pre = 1.f; pa = ka;
+        a = b = top; la = la_; lb = lb_;
+        ba = top * ka + la; bb = top * kb + lb;
+        cb = SUMS == SQUARE ? f1 * Exp<T>::of(la + la - lb) : f1;
+        apart = S.huge(top);
     }
-    static __device__ __forceinline__ Slope of_lse(const DistillArgs &A, const Streams &S, float lse_a, float lse_b, float weight, bool kept, bool labelled) {
-        const float U = Exp<T>::unit();
-        Slope s(A, S, weight, kept, labelled);
-        s.a = lse_a; s.b = lse_b;
-        s.ba = lse_a * U; s.bb = lse_b * U;
-        s.cb = SUMS == SQUARE ? s.f1 * Exp<T>::of((lse_a + lse_a - lse_b) * U) : s.f1;
-        s.apart = is_huge(lse_a) || is_huge(lse_b);
-        return s;
+    __device__ __forceinline__ void from_lse(const Streams &S, float lse_a, float lse_b) {
+        static_assert(EITHER, "");
+        pre = S.inv_a; pa = kb;
+        a = lse_a; b = lse_b; la = lb = 0.f;
+        ba = lse_a * kb; bb = lse_b * kb;
+        cb = SUMS == SQUARE ? f1 * Exp<T>::of((lse_a + lse_a - lse_b) * kb) : f1;
+        apart = !Exp<T>::EXACT && fmaxf(fabsf(ba), SUMS == ONE ? 0.f : fabsf(bb)) > FUSED_EXPONENT;
     }
     template <bool APART> __device__ __forceinline__ float of(float x) const {
-        const float U = Exp<T>::unit();
-        // (a largest logit's product is rounded as in its log sum, so that no probability is beyond one)
-        const float e = Exp<T>::of(!APART ? __builtin_fmaf(x, ka, -ba) : LSE ? (times(x, inv) - a) * U : __builtin_fmaf(x - a, ka, -la));
+        // (the product with 1 / T is rounded as that of the largest logit in its log sum: no probability is beyond one)
+        const float e = Exp<T>::of(!APART ? __builtin_fmaf(x, ka, -ba) : __builtin_fmaf((EITHER ? times(x, pre) : x) - a, EITHER ? pa : ka, -la));
         if constexpr (SUMS == ONE) return ca * e;
-        if constexpr (SUMS == TWO) return ca * e + cb * Exp<T>::of(!APART ? __builtin_fmaf(x, kb, -bb) : LSE ? (x - b) * U : __builtin_fmaf(x - b, kb, -lb));
-        return e * (ca + cb * e);
+        if constexpr (SUMS == SQUARE && !APART) return e * (ca + cb * e);
+        return ft * e + f1 * Exp<T>::of(!APART ? __builtin_fmaf(x, kb, -bb) : __builtin_fmaf(x - b, kb, -lb));
     }
     __device__ __forceinline__ float operator()(float x) const { return of<Exp<T>::EXACT>(x); }
 };
@@ -289,8 +291,8 @@ template <int THREADS, int MOST> __device__ __forceinline__ float share_wanted(c
     return threadIdx.x == THREADS - 1 && W.label >= 0 ? together(W.label) : 0.f;
 }
 // where teacher or label have something in [begin, end): the whole value, once more (equal indices get equal values)
-template <int THREADS, int MOST, typename T, int SUMS, bool LSE>
-__device__ __forceinline__ void write_wanted(const Wanted<THREADS, MOST> &W, const Slope<T, SUMS, LSE> &slope, T *out, uint32_t begin, uint32_t end, float label_q) {
+template <int THREADS, int MOST, typename T, int SUMS, bool EITHER>
+__device__ __forceinline__ void write_wanted(const Wanted<THREADS, MOST> &W, const Slope<T, SUMS, EITHER> &slope, T *out, uint32_t begin, uint32_t end, float label_q) {
     auto again = [&](int32_t i, float s, float mass) {
         if ((uint32_t)i < begin || (uint32_t)i >= end) return;
         out[i] = (T)((slope.apart ? slope.template of<true>(s) : slope(s)) - slope.ft * mass - (i == W.label ? slope.f1 : 0.f));
@@ -300,8 +302,8 @@ __device__ __forceinline__ void write_wanted(const Wanted<THREADS, MOST> &W, con
         if (W.at[n] >= 0) again(W.at[n], W.s[n], W.t[n]);
     if (threadIdx.x == THREADS - 1 && W.label >= 0) again(W.label, W.label_s, label_q);
 }
-template <bool CUTS, int THREADS, typename T, int CH, int SUMS, bool LSE>
-__device__ __forceinline__ void write_huge(const Row<T> &from, const Row<T> &to, uint32_t begin, uint32_t end, const Slope<T, SUMS, LSE> &slope) {
+template <bool CUTS, int THREADS, typename T, int CH, int SUMS, bool EITHER>
+__device__ __forceinline__ void write_huge(const Row<T> &from, const Row<T> &to, uint32_t begin, uint32_t end, const Slope<T, SUMS, EITHER> &slope) {
     for (uint32_t c = begin + threadIdx.x * CH; c < end; c += THREADS * CH) {
         const Place p(c, end, CH);
         float v[CH];
@@ -397,7 +399,7 @@ __global__ __launch_bounds__(THREADS, NL > 0 ? 8 : 5) void k_distill_rows(Distil
     }
     if (NL > 0) begin();
     W.template look<T>(A, r);
-    const Streams S = streams_of<T>(A);
+    const Streams S = streams_of<T, SUMS>(A);
     Running<T, SUMS> R;
     auto take = [&](uint32_t k, const Words<T, CH> &x) {
         float v[CH];
@@ -440,7 +442,7 @@ __global__ __launch_bounds__(THREADS, NL > 0 ? 8 : 5) void k_distill_rows(Distil
     block_all<THREADS / 64, true>(v, red);
     const float top = v.x;
     R.move(S, top);
-    if (is_huge(top)) sum_huge<CUTS, THREADS, T, CH, SUMS>(from, 0, A.vocab, S, top, R);
+    if (S.huge(top)) sum_huge<CUTS, THREADS, T, CH, SUMS>(from, 0, A.vocab, S, top, R);
     float sum, cross;
     W.weigh(A, v.y, sum, cross);
     v = make_float4(R.sa, R.sb, sum, cross);
@@ -453,7 +455,8 @@ __global__ __launch_bounds__(THREADS, NL > 0 ? 8 : 5) void k_distill_rows(Distil
         write_zeros<CUTS, THREADS, T, CH>(to, 0, A.vocab);
         return;
     }
-    const auto slope = Slope<T, SUMS, false>::of_sums(A, S, top, L.la, L.lb, weight, v.z != 0.f, W.label >= 0);
+    Slope<T, SUMS, false> slope(A, S, weight, v.z != 0.f, W.label >= 0);
+    slope.from_sums(S, top, L.la, L.lb);
     const float label_q = share_wanted(A, W, v.z, lds);
     if (slope.apart) {
         write_huge<CUTS, THREADS, T, CH>(from, to, 0, A.vocab, slope);
@@ -500,14 +503,14 @@ __global__ __launch_bounds__(THREADS) void k_distill_part(DistillArgs A) {
     Wanted<THREADS> W;
     W.at[0] = -1; W.t[0] = -INFINITY;
     if (slice == 0) { W.ask(A, r); W.template look<T>(A, r); }
-    const Streams S = streams_of<T>(A);
+    const Streams S = streams_of<T, SUMS>(A);
     Running<T, SUMS> R;
     sum_row<CUTS, THREADS, T, CH, SUMS>(from, begin, end, S, R);
     float4 v = make_float4(R.m, slice == 0 ? W.top() : -INFINITY, -INFINITY, -INFINITY);
     block_all<THREADS / 64, true>(v, red);
     const float top = v.x;
     R.move(S, top);
-    if (is_huge(top)) sum_huge<CUTS, THREADS, T, CH, SUMS>(from, begin, end, S, top, R);
+    if (S.huge(top)) sum_huge<CUTS, THREADS, T, CH, SUMS>(from, begin, end, S, top, R);
     float sum = 0.f, cross = 0.f;
     if (slice == 0) W.weigh(A, v.y, sum, cross);
     v = make_float4(R.sa, R.sb, sum, cross);
@@ -522,7 +525,7 @@ constexpr int JOIN_WAVES = 16;
 template <typename T, int SUMS> __global__ __launch_bounds__(64 * JOIN_WAVES) void k_distill_join(DistillArgs A) {
     __shared__ double lds[JOIN_WAVES];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    const Streams S = streams_of<T>(A);
+    const Streams S = streams_of<T, SUMS>(A);
     double total = 0.0;
     for (uint64_t r = (uint64_t)blockIdx.x * JOIN_WAVES + wave; r < A.n_rows; r += (uint64_t)gridDim.x * JOIN_WAVES) {
         const float weight = A.row_weight ? A.row_weight[r] : 1.f;
@@ -537,7 +540,10 @@ template <typename T, int SUMS> __global__ __launch_bounds__(64 * JOIN_WAVES) vo
         const float d = p.x - top, f = Exp<T>::of(d * S.ka);
         const float sa = some ? p.y * f : p.y, sb = some ? p.z * (SUMS == SQUARE ? f * f : Exp<T>::of(d * S.kb)) : p.z;
         const RowLoss L = row_loss<T, SUMS>(A, S, top, wave_sum(sa), wave_sum(sb), cross);
-        if (lane == 0) keep_row(A, r, L);
+        if (lane == 0) {
+            keep_row(A, r, L);
+            if (A.d_student) A.cross[r] = make_float4(top, L.la, L.lb, 0.f);    // (the gradient of these very sums follows)
+        }
         total += (double)weight * (double)L.loss;
     }
     if (gridDim.x > 1) return;
@@ -579,8 +585,11 @@ __global__ __launch_bounds__(THREADS) void k_distill_gradient(DistillArgs A) {
         write_zeros<CUTS, THREADS, T, CH>(to, begin, end);
         return;
     }
-    write_gradient<CUTS, THREADS, T, CH, SUMS>(A, from, to, (T *)A.d_student + r * A.d_st, begin, end,
-                                               Slope<T, SUMS, true>::of_lse(A, streams_of<T>(A), la, lb, weight, sum != 0.f, W.label >= 0), W, sum, lds);
+    const Streams S = streams_of<T, SUMS>(A);
+    Slope<T, SUMS, true> slope(A, S, weight, sum != 0.f, W.label >= 0);
+    if (A.cross) slope.from_sums(S, A.cross[r].x, A.cross[r].y, A.cross[r].z);
+    else slope.from_lse(S, la, lb);
+    write_gradient<CUTS, THREADS, T, CH, SUMS>(A, from, to, (T *)A.d_student + r * A.d_st, begin, end, slope, W, sum, lds);
 }
 
 // the rows' losses added up, in one order

@@ -109,3 +109,36 @@ def test_high_temperatures_leave_the_labels_loss_alone(gpu, tau, rows, vocab, dt
     """The label's probability is no less exact the higher the temperature of the other term, whether the gradient is taken by itself, of
     rows in slices or along with the loss.  (kd_weight 1 / T^2: both terms of the loss are of size one.)"""
     Student(gpu, rows, vocab, 8, dtype, tau=tau, kd=1 / tau ** 2, ce=0.5).check()
+
+
+# steps of the type at the size: float16 2 and 16 and 32, bfloat16 2 and 512 and 2^23
+@pytest.mark.parametrize("dtype,size,step", [("float16", -3000.0, 2.0), ("float16", 20000.0, 16.0), ("float16", -65504.0, 0.0), ("bfloat16", -300.0, 2.0),
+                                             ("bfloat16", 1e5, 512.0), ("bfloat16", -1e9, 0.0), ("bfloat16", -1e28, 0.0), ("float32", -1e9, 0.0), ("float32", 70000.0, 0.25)])
+@pytest.mark.parametrize("tau", [1.0, 2.0, 3.0])
+@pytest.mark.parametrize("rows,vocab", [(4, 700), (260, 900), (4, 20001)])
+def test_logits_far_from_zero(gpu, dtype, size, step, tau, rows, vocab):
+    """Rows masked by a large value that is not the type's lowest, or shifted as a whole: loss and gradient in one call are those of the same
+    logits less the row's largest.  A 16-bit student's exponents below 2^11 are rounded to 2^-14 twice, larger ones are taken from
+    differences."""
+    torch = gpu[0]
+    s = Student(gpu, rows, vocab, 6, dtype, kd=0.5, ce=0.5, tau=tau, weights=False)
+    g = torch.Generator().manual_seed(vocab)
+    base = float(torch.tensor(size).to(s.s.dtype))
+    near = step * torch.randint(-2, 3, (rows, vocab), generator=g)
+    far = near.to(torch.float64) + base
+    assert torch.equal(far.to(s.s.dtype).double(), far)
+    s.s[1:4] = far[1:4].to(s.s.dtype).cuda()
+    shifted = s.s.double().cpu()
+    shifted = shifted - shifted.max(1, keepdim=True).values
+    d = lambda t: t.double().cpu()
+    ref = training.distill(shifted, d(s.tl), s.ti.cpu(), s.label.cpu(), None, tau, 0.5, 0.5, 0.75)
+    _, d1, both, d2 = s.run()
+    rounding = torch.finfo(s.s.dtype).eps / 2 if dtype != "float32" else 0.0
+    tiny = 2.0 ** -25 if dtype == "float16" else 1e-37
+    exponents = 2 * 2.0 ** -14 if dtype != "float32" else 0.0
+    tol = rounding * (1 + 2.0 ** -8) * ref["d_student"].abs() + ((TERMS + vocab / 64) * U32 + exponents) * ref["big"] + tiny
+    s.near(d2, ref["d_student"], tol, "d_student")
+    # from the log sums, which are rounded to 32 bits: no probability beyond one
+    most = (0.5 * tau + 0.5) * 0.75 * (1 + 2.0 ** -7)
+    assert bool((d1.double().cpu().abs() <= most).all())
+    assert bool(torch.isfinite(both["lse"]).all()) and bool(torch.isfinite(both["loss"]).all())
