@@ -934,12 +934,13 @@ int32_t rk_distill_loss(rk_ctx *ctx, const rk_distill *distill, uint64_t n_rows,
                         const rk_matrix *student, const rk_teacher *teacher, float *loss, float *lse, float *total);
 
 /* The gradient of the student's logits from that of total (d_total [device] one
- * float, NULL: one) and the forward pass's lse; 0 for rows that are left out. d_student has the student's type. */
+ * float, NULL: one) and the forward pass's lse; 0 for rows that are left out.
+ * d_student has the student's type and may be the student (same data and stride). */
 int32_t rk_distill_backward(rk_ctx *ctx, const rk_distill *distill, uint64_t n_rows, uint32_t vocab,
                             const rk_matrix *student, const rk_teacher *teacher, const float *lse,
                             const float *d_total_or_null, const rk_matrix *d_student);
 
-/* Both at once, where the gradient of total is known beforehand. */
+/* Both at once, where the gradient of total is known beforehand; d_student may be the student here too. */
 int32_t rk_distill_loss_backward(rk_ctx *ctx, const rk_distill *distill, uint64_t n_rows, uint32_t vocab,
                                  const rk_matrix *student, const rk_teacher *teacher, const float *d_total_or_null,
                                  float *loss, float *lse, float *total, const rk_matrix *d_student);

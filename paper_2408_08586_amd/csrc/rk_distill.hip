@@ -176,15 +176,17 @@ template <int THREADS, int MOST = (int)RK_MAX_TEACHER_LOGITS> struct Wanted {
             }
         }
     }
-    template <typename T> __device__ __forceinline__ void look(const DistillArgs &A, uint64_t r) {
+    // Logits are looked up in [begin, end) only, where they are wanted for what is written there: others may be gradients by now.
+    template <typename T> __device__ __forceinline__ void look(const DistillArgs &A, uint64_t r, uint32_t begin, uint32_t end) {
         const T *const row = (const T *)A.student + r * A.st;
         if ((uint32_t)label >= A.vocab) label = -1;
-        label_s = label >= 0 ? (float)row[label] : 0.f;
+        auto logit = [&](int32_t i) { return (uint32_t)i >= begin && (uint32_t)i < end ? (float)row[i] : 0.f; };
+        label_s = logit(label);
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             at[n] = (uint32_t)at[n] < A.vocab && t[n] != -INFINITY ? at[n] : -1;
             if (at[n] < 0) t[n] = -INFINITY;
-            s[n] = at[n] >= 0 ? (float)row[at[n]] : 0.f;
+            s[n] = logit(at[n]);
         }
     }
     __device__ __forceinline__ float top() const {
@@ -398,7 +400,7 @@ __global__ __launch_bounds__(THREADS, NL > 0 ? 8 : 5) void k_distill_rows(Distil
         return;
     }
     if (NL > 0) begin();
-    W.template look<T>(A, r);
+    W.template look<T>(A, r, 0, A.vocab);
     const Streams S = streams_of<T, SUMS>(A);
     Running<T, SUMS> R;
     auto take = [&](uint32_t k, const Words<T, CH> &x) {
@@ -502,7 +504,7 @@ __global__ __launch_bounds__(THREADS) void k_distill_part(DistillArgs A) {
     const Row<T> from(A.student, r, A.st, A.vocab);
     Wanted<THREADS> W;
     W.at[0] = -1; W.t[0] = -INFINITY;
-    if (slice == 0) { W.ask(A, r); W.template look<T>(A, r); }
+    if (slice == 0) { W.ask(A, r); W.template look<T>(A, r, 0, A.vocab); }
     const Streams S = streams_of<T, SUMS>(A);
     Running<T, SUMS> R;
     sum_row<CUTS, THREADS, T, CH, SUMS>(from, begin, end, S, R);
@@ -571,7 +573,7 @@ __global__ __launch_bounds__(THREADS) void k_distill_gradient(DistillArgs A) {
     }
     Wanted<THREADS> W;
     W.ask(A, r);
-    W.template look<T>(A, r);
+    W.template look<T>(A, r, begin, end);
     float4 v = make_float4(W.top(), -INFINITY, -INFINITY, -INFINITY);
     float sum = 0.f, cross = 0.f;
     if (A.kd > 0.f) {

@@ -142,3 +142,23 @@ def test_logits_far_from_zero(gpu, dtype, size, step, tau, rows, vocab):
     most = (0.5 * tau + 0.5) * 0.75 * (1 + 2.0 ** -7)
     assert bool((d1.double().cpu().abs() <= most).all())
     assert bool(torch.isfinite(both["lse"]).all()) and bool(torch.isfinite(both["loss"]).all())
+
+
+@pytest.mark.parametrize("rows,vocab", [(3, 40000), (700, 20000), (260, 70001)])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_distill_in_place_by_slices(gpu, rows, vocab, dtype):
+    """d_student may be student, also where several workgroups share a row and what the teacher wants lies in all of their parts."""
+    torch = gpu[0]
+    s = Student(gpu, rows, vocab, 200, dtype, kd=0.5, ce=0.5, tau=2.0)
+    _, _, both, d2 = s.run()
+    copy, d1 = s.s.clone(), torch.empty_like(s.s)
+    s.rk.rk_distill_backward(*s.given(), both["lse"], s.d_total, d1)
+    f = lambda *n: torch.empty(n, device="cuda")
+    out = dict(loss=f(rows), lse=f(rows, 2), total=f(1))
+    s.rk.rk_distill_loss_backward(*s.given(), s.d_total, *out.values(), s.s)
+    assert torch.equal(s.s, d2)
+    for k in out:
+        assert torch.equal(out[k], both[k])
+    s.s.copy_(copy)
+    s.rk.rk_distill_backward(*s.given(), both["lse"], s.d_total, s.s)
+    assert torch.equal(s.s, d1)
