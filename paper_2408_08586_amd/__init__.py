@@ -713,13 +713,19 @@ _OPERATORS = {
 }
 
 
+_functions = {}
+
+
 def _operator(name):
-    """The library's function, its argument types known (which spares wrapping every number of every call)."""
-    f = getattr(load_library(), name)
-    if f.argtypes is None:
+    """The library's function, its argument types known (which spares wrapping every number of every call): an object of the binding's
+    own, so that whoever calls the library's attribute of that name finds it as it was."""
+    f = _functions.get(name)
+    if f is None:
         kinds = {"c": C.c_void_p, "q": C.c_uint64, "u": C.c_uint32, "p": C.c_void_p, "b": C.POINTER(rk_norm_block), "g": C.POINTER(rk_norm_grads),
                  "m": C.POINTER(rk_matrix), "r": C.POINTER(rk_router), "d": C.POINTER(rk_distill), "t": C.POINTER(rk_teacher)}
-        f.argtypes = [kinds[k] for k in _OPERATORS[name]]
+        f = load_library()[name]
+        f.restype, f.argtypes = C.c_int32, [kinds[k] for k in _OPERATORS[name]]
+        _functions[name] = f
     return f
 
 

@@ -17,3 +17,13 @@ def test_gates_of_the_gradients(call, rk):
 
     for rows, gate_rows, gates, stride in ((9, 4, 2, 64), (8, 4, 1, 64), (3, 4, 2, 63), (0, 4, 3, 63), (9, 4, 3, 63), (9, 4, 1 << 31, 64)):
         assert backward(rows, gate_rows, gates, stride) == rk.RK_ERR_INVALID_ARG and call.text(), (rows, gate_rows, gates, stride)
+
+
+def test_the_binding_leaves_the_librarys_functions_alone(rk):
+    """Argument types that the binding sets are its own: a caller of the C functions finds them as they were, whoever called first."""
+    lib = rk.load_library()
+    for name in rk._OPERATORS:
+        own = rk._operator(name)
+        assert own is rk._operator(name) and own.argtypes and own.restype is C.c_int32
+        assert getattr(lib, name).argtypes is None
+        assert getattr(lib, name)(*[C.c_void_p(0)] * 13) == rk.RK_ERR_INVALID_ARG
