@@ -855,7 +855,7 @@ typedef struct {
  * exactly if pre_kind is RK_NORM_NONE.  x_out may be x, u may be y (same data and stride).
  *   stats  [device] n_rows x 4 floats: mean and 1/sqrt(..) of y, the same of
  *          x_out (mean 0 for RK_NORM_RMS; 0 and 1 for RK_NORM_NONE); for the backward pass
- * Rows of 1 to RK_NORM_MAX_WIDTH elements. */
+ * Rows of 1 to RK_NORM_MAX_WIDTH elements, up to 2^31 - 1 of them. */
 int32_t rk_norm_forward(rk_ctx *ctx, const rk_norm_block *block, uint64_t n_rows, uint32_t width,
                         const rk_matrix *x, const rk_matrix *y_or_null, const rk_matrix *x_out_or_null,
                         const rk_matrix *u_or_null, float *stats);
@@ -873,7 +873,8 @@ int32_t rk_norm_backward(rk_ctx *ctx, const rk_norm_block *block, uint64_t n_row
 #define RK_MAX_TOP_K    32u
 
 /* A router over n_experts logits a token.  group_tokens: the tokens that one
- * balance is taken over (a sequence), 0: all; the last group may have fewer. */
+ * balance is taken over (a sequence), 0: all; the last group may have fewer.  Up
+ * to 2^24 - 1 tokens; groups times experts (rounded up to 16) below 2^26. */
 typedef struct {
     uint32_t n_experts, top_k;
     uint32_t renormalise;       /* 1: a token's weights sum to one */
@@ -917,7 +918,8 @@ typedef struct {
 
 /* What the rows are compared with.  An index outside the vocabulary is no kept
  * logit (nor is a logit of -inf), a label outside it no label; indices that repeat add up.  A
- * row without a kept logit has no first term, one without a label no second. */
+ * row without a kept logit has no first term, one without a label no second.  Up to
+ * 2^31 - 1 rows of up to 2^28 words. */
 typedef struct {
     const rk_matrix *logits;    /* n_rows x top_k, any type; null exactly if kd_weight is 0 */
     const int32_t *index;       /* [device] n_rows * top_k */

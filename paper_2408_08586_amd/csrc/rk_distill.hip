@@ -10,7 +10,7 @@ namespace {
 struct DistillArgs {
     const void *student;
     void *d_student;
-    uint64_t st, d_st, n_rows;
+    uint64_t st, d_st, n_rows, first;   // first: the launch's first row
     uint32_t vocab, top_k, t_type;
     const void *teacher;
     uint64_t t_st;
@@ -373,7 +373,7 @@ __global__ __launch_bounds__(THREADS, NL > 0 ? 8 : 5) void k_distill_rows(Distil
     __shared__ float4 red[16];
     __shared__ Shares<MOST> lds;
     constexpr uint32_t STEP = THREADS * CH, MORE = 4;              // vectors under way at once of what is beyond
-    const uint64_t r = blockIdx.x;
+    const uint64_t r = A.first + blockIdx.x;
     const Row<T> from(A.student, r, A.st, A.vocab), to(A.d_student, r, A.d_st, A.vocab);
     const float weight = A.row_weight ? A.row_weight[r] : 1.f;
     Wanted<THREADS, MOST> W;
@@ -561,8 +561,8 @@ template <bool CUTS, int THREADS, typename T, int CH, int SUMS>
 __global__ __launch_bounds__(THREADS) void k_distill_gradient(DistillArgs A) {
     __shared__ float4 red[16];
     __shared__ Shares<(int)RK_MAX_TEACHER_LOGITS> lds;
-    const uint64_t r = blockIdx.x / A.slices;
-    const uint32_t slice = blockIdx.x - (uint32_t)r * A.slices, begin = slice * A.slice;
+    const uint64_t r = A.first + blockIdx.x / A.slices;
+    const uint32_t slice = blockIdx.x % A.slices, begin = slice * A.slice;
     const uint32_t end = slice + 1 == A.slices ? A.vocab : begin + A.slice;
     const Row<T> from(A.student, r, A.st, A.vocab), to(A.d_student, r, A.d_st, A.vocab);
     const float weight = A.row_weight ? A.row_weight[r] : 1.f;
@@ -651,31 +651,35 @@ int32_t check_distill(rk_ctx *ctx, const rk_distill *d, uint64_t n_rows, uint32_
     return RK_OK;
 }
 enum Step { STEP_ROWS, STEP_PART, STEP_JOIN, STEP_GRADIENT };
-template <typename T, int SUMS> hipError_t launch(hipStream_t st, const DistillArgs &A, Step step) {
+template <typename T, int SUMS> hipError_t launch(hipStream_t st, DistillArgs A, Step step) {
     constexpr int CH = sizeof(T) == 4 ? 4 : 8;
     if (step == STEP_JOIN) {
         k_distill_join<T, SUMS><<<A.n_rows < DS_FEW ? 1 : (uint32_t)((A.n_rows + JOIN_WAVES - 1) / JOIN_WAVES), 64 * JOIN_WAVES, 0, st>>>(A);
         return hipSuccess;
     }
+    // f(workgroups) for as many rows as a launch holds, `each` workgroups a row
+    auto by_rows = [&](uint64_t threads, uint64_t each, auto f) {
+        const uint64_t most = RK_LAUNCH_THREADS / (threads * each);
+        for (A.first = 0; A.first < A.n_rows; A.first += most) f((uint32_t)((A.n_rows - A.first < most ? A.n_rows - A.first : most) * each));
+    };
     auto go = [&](auto cuts, auto threads) {
         constexpr bool CUTS = decltype(cuts)::value;
         constexpr int N = decltype(threads)::value;
-        const uint32_t blocks = (uint32_t)(A.n_rows * A.slices);
-        if (step == STEP_PART) k_distill_part<CUTS, N, T, CH, SUMS><<<blocks, N, 0, st>>>(A);
-        else k_distill_gradient<CUTS, N, T, CH, SUMS><<<blocks, N, 0, st>>>(A);
+        if (step == STEP_PART) k_distill_part<CUTS, N, T, CH, SUMS><<<(uint32_t)(A.n_rows * A.slices), N, 0, st>>>(A);
+        else by_rows(N, A.slices, [&](uint32_t blocks) { k_distill_gradient<CUTS, N, T, CH, SUMS><<<blocks, N, 0, st>>>(A); });
     };
     auto rows = [&](auto cuts) {
         constexpr bool CUTS = decltype(cuts)::value;
-        const uint32_t vectors = (A.vocab + CH - 1) / CH, n = (uint32_t)A.n_rows;
+        const uint32_t vectors = (A.vocab + CH - 1) / CH;
         constexpr int MOST = (int)RK_MAX_TEACHER_LOGITS;
-        if (vectors <= 128 * 4 && A.top_k <= 256) k_distill_rows<CUTS, 128, 4, 0, 256, T, CH, SUMS><<<n, 128, 0, st>>>(A);
-        else if (vectors <= 256 * 8) k_distill_rows<CUTS, 256, 8, 0, MOST, T, CH, SUMS><<<n, 256, 0, st>>>(A);
-        else if (vectors <= 512 * 8) k_distill_rows<CUTS, 512, 8, 0, MOST, T, CH, SUMS><<<n, 512, 0, st>>>(A);
+        if (vectors <= 128 * 4 && A.top_k <= 256) by_rows(128, 1, [&](uint32_t n) { k_distill_rows<CUTS, 128, 4, 0, 256, T, CH, SUMS><<<n, 128, 0, st>>>(A); });
+        else if (vectors <= 256 * 8) by_rows(256, 1, [&](uint32_t n) { k_distill_rows<CUTS, 256, 8, 0, MOST, T, CH, SUMS><<<n, 256, 0, st>>>(A); });
+        else if (vectors <= 512 * 8) by_rows(512, 1, [&](uint32_t n) { k_distill_rows<CUTS, 512, 8, 0, MOST, T, CH, SUMS><<<n, 512, 0, st>>>(A); });
         else {
             const auto kernel = k_distill_rows<CUTS, 1024, DS_REGISTERS, DS_LDS, MOST, T, CH, SUMS>;
             const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, DS_LDS * 1024 * 16);
             if (e != hipSuccess) return e;
-            kernel<<<n, 1024, DS_LDS * 1024 * 16, st>>>(A);
+            by_rows(1024, 1, [&](uint32_t n) { kernel<<<n, 1024, DS_LDS * 1024 * 16, st>>>(A); });
         }
         return hipSuccess;
     };

@@ -16,7 +16,7 @@ struct NormArgs {
     float *stats;
     const void *vec[G_VECTORS];
     uint64_t gate_rows, gate_st;
-    uint64_t n_rows;
+    uint64_t n_rows, first;             // first: the launch's first row
     uint32_t width;
     uint32_t post, pre, p32;            // p32: the vectors are float32
     float post_eps, pre_eps, scale;
@@ -116,11 +116,11 @@ template <int CH, int NC> __device__ __forceinline__ void places(Place (&at)[NC]
 
 // The rows of a workgroup: one (its wavefronts share it), or one per wavefront for rows that a wavefront holds.
 struct RowOf { uint64_t row; uint32_t tid, threads; bool there; };
-__device__ __forceinline__ RowOf row_of(uint64_t n_rows, bool per_wave, RowGroup &G, float *lds) {
+__device__ __forceinline__ RowOf row_of(uint64_t first, uint64_t n_rows, bool per_wave, RowGroup &G, float *lds) {
     const uint32_t t = threadIdx.x, waves = blockDim.x >> 6;
     G.lane = t & 63u; G.wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(t >> 6)); G.turn = 0; G.lds = lds;
     G.nw = per_wave ? 1u : waves;
-    const uint64_t row = per_wave ? (uint64_t)blockIdx.x * waves + G.wave : blockIdx.x;
+    const uint64_t row = first + (per_wave ? (uint64_t)blockIdx.x * waves + G.wave : blockIdx.x);
     return RowOf{row, per_wave ? G.lane : t, per_wave ? 64u : blockDim.x, row < n_rows};
 }
 
@@ -169,7 +169,7 @@ template <bool CUTS, typename T, typename R, int CH, int NC, int MAXT>
 __global__ __launch_bounds__(MAXT) void k_norm_forward(NormArgs A, bool per_wave) {
     __shared__ float lds[96];
     RowGroup G;
-    const RowOf P = row_of(A.n_rows, per_wave, G, lds);
+    const RowOf P = row_of(A.first, A.n_rows, per_wave, G, lds);
     if (!P.there) return;                                   // (per_wave only: whole wavefronts, no barrier follows)
     Place at[NC];
     places<CH, NC>(at, P.tid, P.threads, A.width);
@@ -228,7 +228,7 @@ template <bool CUTS, typename T, typename R, int CH, int NC, int MAXT>
 __global__ __launch_bounds__(MAXT) void k_norm_backward(NormArgs A, bool per_wave) {
     __shared__ float lds[96];
     RowGroup G;
-    const RowOf P = row_of(A.n_rows, per_wave, G, lds);
+    const RowOf P = row_of(A.first, A.n_rows, per_wave, G, lds);
     if (!P.there) return;
     Place at[NC];
     places<CH, NC>(at, P.tid, P.threads, A.width);
@@ -415,7 +415,7 @@ __global__ __launch_bounds__(MAXT) void k_norm_backward_sums(NormSums S, bool pe
     __shared__ float lds[96];
     const NormArgs &A = S.A;
     RowGroup G;
-    const RowOf P = row_of(S.C.n, per_wave, G, lds);            // (its "row" is the chunk of one that is alone)
+    const RowOf P = row_of(0, S.C.n, per_wave, G, lds);            // (its "row" is the chunk of one that is alone)
     if (!P.there && alone) return;
     const bool shared = per_wave && !alone;
     const uint64_t chunk = shared ? blockIdx.x : P.row;
@@ -740,13 +740,17 @@ Shape shape_of(uint32_t width, int ch) {
 }
 
 template <typename T, typename R, int NC, int MAXT>
-void launch_nc(hipStream_t st, const NormArgs &A, const Shape &S, bool back) {
+void launch_nc(hipStream_t st, NormArgs A, const Shape &S, bool back) {
     constexpr int CH = chunk_of<T, R>();
-    const uint32_t blocks = (uint32_t)((A.n_rows + S.rows_per_wg - 1) / S.rows_per_wg);
+    const uint64_t all = (A.n_rows + S.rows_per_wg - 1) / S.rows_per_wg, most = RK_LAUNCH_THREADS / S.threads;
     auto go = [&](auto cuts) {
         constexpr bool CUTS = decltype(cuts)::value;
-        if (back) k_norm_backward<CUTS, T, R, CH, NC, MAXT><<<blocks, S.threads, 0, st>>>(A, S.per_wave);
-        else k_norm_forward<CUTS, T, R, CH, NC, MAXT><<<blocks, S.threads, 0, st>>>(A, S.per_wave);
+        for (uint64_t at = 0; at < all; at += most) {
+            const uint32_t blocks = (uint32_t)(all - at < most ? all - at : most);
+            A.first = at * S.rows_per_wg;
+            if (back) k_norm_backward<CUTS, T, R, CH, NC, MAXT><<<blocks, S.threads, 0, st>>>(A, S.per_wave);
+            else k_norm_forward<CUTS, T, R, CH, NC, MAXT><<<blocks, S.threads, 0, st>>>(A, S.per_wave);
+        }
     };
     if (A.width % CH) go(std::true_type()); else go(std::false_type());
 }

@@ -535,6 +535,8 @@ extern "C" int32_t rk_route_forward(rk_ctx *ctx, const rk_router *router, uint64
     if ((n_tokens && (!expert || !weight || !lse)) || (A.n_groups && (!counts || !prob_sum || !tokens)) || !loss ||
         misaligned4({expert, weight, lse, counts, prob_sum, tokens, loss}))
         return rk_fail(ctx, RK_ERR_INVALID_ARG, "an output is null or misaligned");
+    A.tiles = (A.n_experts + RT_COLS - 1) / RT_COLS;
+    if (A.n_groups * A.tiles * RT_COLS * RT_SHARE > 0xFFFFFFFFull) return rk_fail(ctx, RK_ERR_UNSUPPORTED, "2^26 groups times experts or more");
     RK_HIP(ctx, hipSetDevice(ctx->device));
     A.mask = mask; A.expert = expert; A.weight = weight; A.lse = lse; A.counts = counts; A.prob_sum = prob_sum; A.tokens = tokens; A.loss = loss;
     // up to four workgroups a compute unit share the tokens, each in rounds of as many as its wavefronts hold; few tokens are one's
@@ -542,7 +544,6 @@ extern "C" int32_t rk_route_forward(rk_ctx *ctx, const rk_router *router, uint64
     A.chunk = (n_tokens + 1024 * at_once - 1) / (1024 * at_once) * at_once;
     if (A.n_groups == 1 && n_tokens <= 4 * at_once) A.chunk = 4 * at_once;      // (then there is nothing to join)
     A.per_group = n_tokens ? (A.group_tokens + A.chunk - 1) / A.chunk : 0;
-    A.tiles = (A.n_experts + RT_COLS - 1) / RT_COLS;
     const uint64_t blocks = A.per_group * (n_tokens ? A.n_groups : 0);
     if (blocks == 0) {
         k_route_nothing<<<1, 256, 0, ctx->stream>>>(A);

@@ -237,7 +237,9 @@ __device__ __forceinline__ float exp_f32(float x) {
     return x < -87.4f ? 0.f : __builtin_fmaf(e, low * LN2, e);
 }
 
-// host side: a matrix of the operators
+// host side: threads of one launch (it has fewer than 2^32); what needs more goes in several
+constexpr uint64_t RK_LAUNCH_THREADS = 1ull << 31;
+// a matrix of the operators
 static inline bool rk_matrix_ok(const rk_matrix *m, uint64_t n_rows, uint64_t width) {
     if (!m || m->type > RK_F16) return false;
     if (n_rows == 0) return true;

@@ -162,3 +162,53 @@ def test_distill_in_place_by_slices(gpu, rows, vocab, dtype):
     s.s.copy_(copy)
     s.rk.rk_distill_backward(*s.given(), both["lse"], s.d_total, s.s)
     assert torch.equal(s.s, d1)
+
+
+def test_more_norm_rows_than_one_launch_has(gpu):
+    """A launch has fewer than 2^32 threads, 64 of them a row: rows beyond 2^26, of one element."""
+    torch, rk, ctx = gpu
+    rows = (1 << 26) + 70
+    x = ((torch.arange(rows, device="cuda") % 251) - 125).to(torch.bfloat16)[:, None]
+    y = ((torch.arange(rows, device="cuda") % 127) + 1).to(torch.bfloat16)[:, None]
+    gate = torch.tensor([[0.5], [2.0]], dtype=torch.bfloat16, device="cuda")
+    first = 1 << 25
+    gate = torch.cat((gate, torch.tensor([[4.0]], dtype=torch.bfloat16, device="cuda")))
+    block = rk.NormBlock(post="none", pre="none", gate=gate, gate_rows=first)
+    x_out, stats = torch.full_like(x, NAN), torch.full((rows, 4), NAN, device="cuda")
+    rk.rk_norm_forward(ctx, block, x, y, x_out, None, stats)
+    g = gate.float()[torch.arange(rows, device="cuda") // first]
+    assert torch.equal(x_out, (x.float() + g * y.float()).to(torch.bfloat16))
+    assert bool((stats == torch.tensor([0.0, 1.0, 0.0, 1.0], device="cuda")).all())
+    dx, dy = torch.full_like(x, NAN), torch.full_like(x, NAN)
+    rk.rk_norm_backward(ctx, block, x_out, y, stats, x, None, dx, dy)
+    assert torch.equal(dx, x) and torch.equal(dy, (g * x.float()).to(torch.bfloat16))
+
+
+def test_more_distilled_rows_than_one_launch_has(gpu):
+    """Rows of two words, 128 threads each: beyond 2^25 of them."""
+    torch, rk, ctx = gpu
+    rows = (1 << 25) + 70
+    s = (torch.arange(2 * rows, device="cuda") % 13).float().view(rows, 2) / 4
+    label = (torch.arange(rows, device="cuda") % 2).to(torch.int32)
+    distill = rk.make_distill(kd_weight=0.0, ce_weight=1.0)
+    w = torch.full((rows,), 1.0 / rows, device="cuda")
+    f = lambda *n: torch.full(n, NAN, device="cuda")
+    loss, lse, total, d = f(rows), f(rows, 2), f(1), f(rows, 2)
+    # 2 x 2^-24 a term, of numbers up to 4
+    x = s.double()
+    want = torch.logsumexp(x, 1)
+    right = x.gather(1, label.long()[:, None])[:, 0]
+    p = torch.softmax(x, 1)
+    p.scatter_add_(1, label.long()[:, None], torch.full_like(p[:, :1], -1.0))
+    for both in (True, False):
+        loss.fill_(NAN), d.fill_(NAN), total.fill_(NAN)
+        if both:
+            rk.rk_distill_loss_backward(ctx, distill, s, None, None, label, w, None, loss, lse, total, d)
+        else:
+            rk.rk_distill_loss(ctx, distill, s, None, None, label, w, loss, lse, total)
+            rk.rk_distill_backward(ctx, distill, s, None, None, label, w, lse, None, d)
+        assert bool(((lse[:, 1].double() - want).abs() <= 16 * U32 * 4).all())
+        assert bool(((loss.double() - (want - right)).abs() <= 32 * U32 * 4).all())
+        assert bool(((d.double() * rows - p).abs() <= 32 * U32).all())
+        assert abs(float(total) - float((want - right).mean())) <= 64 * U32 * 4
+

@@ -27,3 +27,10 @@ def test_the_binding_leaves_the_librarys_functions_alone(rk):
         assert own is rk._operator(name) and own.argtypes and own.restype is C.c_int32
         assert getattr(lib, name).argtypes is None
         assert getattr(lib, name)(*[C.c_void_p(0)] * 13) == rk.RK_ERR_INVALID_ARG
+
+
+def test_groups_that_one_launch_cannot_join(call, rk):
+    """300,000 groups of 16 tiles of experts, 1,024 threads each."""
+    wide = call.matrix(stride=256)
+    assert call.route(n=300000, e=256, group=1, logits=wide) == rk.RK_ERR_UNSUPPORTED and "2^26" in call.text()
+    assert call.route(n=(1 << 24) - 1, e=33, group=8, logits=wide) == rk.RK_ERR_UNSUPPORTED
