@@ -5,7 +5,9 @@ steps take and keep becomes the t_fwd_sample, k_bwd and mem_act that a schedulin
 
 The products are torch's; what lies between them are the library's operators: the join of each block with the residual stream
 (rk_norm_forward / rk_norm_backward), the router (rk_route_forward / rk_route_backward) and the student's loss
-(rk_distill_loss_backward).  Data and weights are random, of the job's sizes.
+(rk_distill_loss_backward).  Data and weights are random.  A layer is a dense block and a block of experts, without attention, and the
+job that is scheduled is this very student: its width follows from --params, its parameters are counted, and what its layers take is scaled to
+all of them, while the first norm, the output's product and the loss count once.
 """
 from __future__ import annotations
 
@@ -106,9 +108,13 @@ class Student:
                 vector(f"pre{b}{i}", 1.0, hidden)
                 vector(f"gate{b}{i}", 0.5, 1, hidden)
         product("head", hidden, vocab)
+        count = {n: p.numel() for n, p in self.params.items()}
+        self.params_rest = count["first"] + count["head"]
+        self.params_layers = sum(count.values()) - self.params_rest
 
     def experts(self, i, u, weight, expert):
-        """Every expert's product on the tokens that chose it, a copy a choice, put back in the tokens' order."""
+        """Every expert's product on the tokens that chose it, a copy a choice, put back in the tokens' order.  (How many chose it comes to
+        the host, a wait in every layer that is part of what this student takes.)"""
         k = expert.shape[1]
         order = torch.argsort(expert.reshape(-1), stable=True)
         sizes = torch.bincount(expert.reshape(-1), minlength=self.router.n_experts).tolist()
@@ -120,20 +126,24 @@ class Student:
         back[order] = torch.arange(len(order), device=DEV)
         return (torch.cat(parts)[back].view(-1, k, u.shape[1]) * weight[:, :, None]).sum(1).to(torch.bfloat16)
 
-    def forward(self, ctx, x):
+    def forward(self, ctx, x, mark=lambda where, u: None):
+        """mark is called with the input of the first layer and the output of the last."""
         p, losses = self.params, []
         x, u = Join.apply(ctx, x, None, None, p["first"], None)
+        mark("layers", u)
         for i in range(self.layers):
             y = u @ p[f"dense{i}"]
             x, u = Join.apply(ctx, x, y, p[f"posta{i}"], p[f"prea{i}"], p[f"gatea{i}"])
             weight, expert, loss = Route.apply(ctx, self.router, u @ p[f"router{i}"])
             losses.append(loss)
             x, u = Join.apply(ctx, x, self.experts(i, u, weight, expert), p[f"postb{i}"], p[f"preb{i}"], p[f"gateb{i}"])
+        mark("head", u)
         return u @ p["head"], losses
 
 
 def measure(hidden, seq, micro_batch, layers=2, experts=8, top_k=2, vocab=32000, kept=64, steps=8, rate=1e-3, seed=0):
-    """Trains for `steps` steps; seconds forward and backward of one, bytes that the forward keeps, and the losses by step."""
+    """Trains for `steps` steps; seconds forward and backward of one, bytes that the forward keeps, each also of the layers alone, the
+    student's parameters, and the losses by step."""
     ctx = rk.rk_create(0)
     student = Student(hidden, layers, experts, top_k, vocab, seq, seed)
     g = torch.Generator(DEV).manual_seed(seed + 1)
@@ -147,40 +157,55 @@ def measure(hidden, seq, micro_batch, layers=2, experts=8, top_k=2, vocab=32000,
     row_weight = torch.full((tokens,), 1.0 / tokens, device=DEV)
     loss, lse, total = f32(tokens), f32(tokens, 2), f32(1)
     d_losses = torch.tensor([BALANCE, ROUTER_Z], device=DEV)
-    times, history, bytes_kept = [], [], 0
+    times, history, kept_at = [], [], {}
     for step in range(steps):
         torch.cuda.synchronize()
+        ev = {n: torch.cuda.Event(enable_timing=True) for n in ("start", "layers", "head", "forward", "back_head", "back_layers", "backward")}
+
+        def mark(where, u):
+            ev[where].record()
+            kept_at[where] = torch.cuda.memory_allocated()
+            # (the gradient of what a layer gets is there when all behind it has gone back)
+            u.register_hook(lambda _: ev["back_head" if where == "head" else "back_layers"].record())
+
         before = torch.cuda.memory_allocated()
-        ev = [torch.cuda.Event(enable_timing=True) for _ in range(3)]
-        ev[0].record()
-        logits, losses = student.forward(ctx, x)
-        ev[1].record()
-        bytes_kept = torch.cuda.memory_allocated() - before
+        ev["start"].record()
+        logits, losses = student.forward(ctx, x, mark)
+        ev["forward"].record()
+        kept_at["forward"] = torch.cuda.memory_allocated()
         d_logits = torch.empty_like(logits)
         rk.rk_distill_loss_backward(ctx, distill, logits.detach(), teacher, index, label, row_weight, None, loss, lse, total, d_logits)
         torch.autograd.backward([logits] + losses, [d_logits] + [d_losses] * len(losses))
-        ev[2].record()
+        ev["backward"].record()
         with torch.no_grad():
             for p in student.params.values():
                 p -= rate * torch.sign(p.grad)
                 p.grad = None
         torch.cuda.synchronize()
-        times.append((ev[0].elapsed_time(ev[1]) * 1e-3, ev[1].elapsed_time(ev[2]) * 1e-3))
+        took = lambda a, b: ev[a].elapsed_time(ev[b]) * 1e-3
+        times.append((took("start", "forward"), took("layers", "head"), took("forward", "backward"), took("back_head", "back_layers")))
         history.append((float(total), sum(float(l.detach()[0]) for l in losses) / len(losses)))
     rk.rk_sync(ctx)
     rk.rk_destroy(ctx)
-    forward, backward = np.median(np.array(times[1:] or times), axis=0)
-    return dict(forward=float(forward), backward=float(backward), bytes_kept=int(bytes_kept), history=history)
+    forward, forward_layers, backward, backward_layers = (float(t) for t in np.median(np.array(times[1:] or times), axis=0))
+    return dict(forward=forward, forward_layers=forward_layers, backward=backward, backward_layers=backward_layers,
+                bytes_kept=int(kept_at["forward"] - before), bytes_layers=int(kept_at["head"] - kept_at["layers"]),
+                params_layers=student.params_layers, params_rest=student.params_rest, history=history)
 
 
 def descriptor(workload, job, m, layers, seq, micro_batch):
-    """The workload's job with what was measured in place of its drawn coefficients, scaled to all of its layers."""
+    """The workload's job with what was measured in place of its drawn coefficients: what the layers take, keep and are is scaled to all
+    of the job's layers, what is outside them counts once (what it keeps, at the measured micro-batch, is part of the constant)."""
     coef, ints = workload.coef.copy(), workload.ints.copy()
     col = {n: i for i, n in enumerate(workloads.COEF_FIELDS)}
-    all_layers, hidden = float(ints[job, 0]), float(coef[job, col["hidden"]])
-    coef[job, col["t_fwd_sample"]] = m["forward"] * all_layers / layers / micro_batch
-    coef[job, col["k_bwd"]] = max(1.0, m["backward"] / m["forward"])
-    coef[job, col["mem_act"]] = m["bytes_kept"] / (seq * micro_batch * hidden * layers)
+    times, hidden = float(ints[job, 0]) / layers, float(coef[job, col["hidden"]])
+    forward = m["forward"] + m["forward_layers"] * (times - 1)
+    backward = m["backward"] + m["backward_layers"] * (times - 1)
+    coef[job, col["P_bytes"]] = 2 * (m["params_layers"] * times + m["params_rest"])
+    coef[job, col["t_fwd_sample"]] = forward / micro_batch
+    coef[job, col["k_bwd"]] = max(1.0, backward / forward)
+    coef[job, col["mem_act"]] = m["bytes_layers"] / (seq * micro_batch * hidden * layers)
+    coef[job, col["mem_const"]] += m["bytes_kept"] - m["bytes_layers"]
     return coef, ints
 
 
@@ -194,20 +219,22 @@ def main(argv=None):
     a.add_argument("--vocab", type=int, default=32000)
     a.add_argument("--steps", type=int, default=8)
     a = a.parse_args(argv)
-    # the workloads' size relation N ~ 12 l h^2
-    hidden = 128 * max(1, round((a.params / (12 * a.layers)) ** 0.5 / 128))
+    # params ~ layers (1 + 2 experts) h^2 + vocab h
+    per = a.layers * (1 + 2 * a.experts)
+    hidden = 128 * max(1, round(((a.vocab ** 2 + 4 * per * a.params) ** 0.5 - a.vocab) / (2 * per) / 128))
     m = measure(hidden, a.seq, 1, a.measured_layers, a.experts, vocab=a.vocab, steps=a.steps)
     for step, (total, balance) in enumerate(m["history"]):
         print(f"step {step}: loss {total:.4f}, balance {balance:.4f}")
     print(f"{a.measured_layers} layers of {hidden}: forward {m['forward'] * 1e3:.2f} ms, backward {m['backward'] * 1e3:.2f} ms, "
-          f"{m['bytes_kept'] / 2 ** 20:.0f} MiB kept")
+          f"{m['bytes_kept'] / 2 ** 20:.0f} MiB kept; of the layers alone {m['forward_layers'] * 1e3:.2f} and {m['backward_layers'] * 1e3:.2f} ms, "
+          f"{m['bytes_layers'] / 2 ** 20:.0f} MiB")
     wl = workloads.tiny()
     col = {n: i for i, n in enumerate(workloads.COEF_FIELDS)}
-    wl.coef[0, [col["P_bytes"], col["hidden"], col["seq"]]] = 2 * a.params, hidden, a.seq
+    wl.coef[0, [col["hidden"], col["seq"]]] = hidden, a.seq
     wl.ints[0] = (a.layers, 32, 1)
     coef, ints = descriptor(wl, 0, m, a.measured_layers, a.seq, 1)
     coef, ints = coef[:1], ints[:1]                     # the job alone on one node
-    print(f"t_fwd_sample {coef[0, col['t_fwd_sample']]:.4f} s, k_bwd {coef[0, col['k_bwd']]:.2f}, mem_act {coef[0, col['mem_act']]:.1f}")
+    print(f"{coef[0, col['P_bytes']] / 2e9:.2f} billion parameters, t_fwd_sample {coef[0, col['t_fwd_sample']]:.4f} s, k_bwd {coef[0, col['k_bwd']]:.2f}, mem_act {coef[0, col['mem_act']]:.1f}")
     ctx = rk.rk_create(0)
     jobs = rk.Jobs(coef, ints)
     assign, total = rk.new_assign(1), torch.zeros(1, device=DEV)
