@@ -185,6 +185,7 @@ def measure(hidden, seq, micro_batch, layers=2, experts=8, top_k=2, vocab=32000,
         took = lambda a, b: ev[a].elapsed_time(ev[b]) * 1e-3
         times.append((took("start", "forward"), took("layers", "head"), took("forward", "backward"), took("back_head", "back_layers")))
         history.append((float(total), sum(float(l.detach()[0]) for l in losses) / len(losses)))
+        del logits, losses, d_logits                    # (the next step's forward is not to find them where it counts what it keeps)
     rk.rk_sync(ctx)
     rk.rk_destroy(ctx)
     forward, forward_layers, backward, backward_layers = (float(t) for t in np.median(np.array(times[1:] or times), axis=0))

@@ -31,3 +31,13 @@ def test_only_the_layers_are_scaled(example):
     assert got["P_bytes"] == 2 * (700 * 12 + 100)
     assert (ints == wl.ints).all() and (coef[1:] == wl.coef[1:]).all()
 
+
+@pytest.mark.gpu
+def test_a_larger_output_changes_nothing_of_the_layers(example):
+    # (two steps: the first product of all takes room for the library that runs it; a rate of 0: the same choices in both)
+    small, large = (example.measure(256, 64, 2, layers=2, experts=4, top_k=2, vocab=v, kept=16, steps=2, rate=0.0) for v in (512, 4096))
+    assert small["bytes_layers"] == large["bytes_layers"] > 0 and small["params_layers"] == large["params_layers"]
+    assert large["bytes_kept"] - small["bytes_kept"] == 2 * 128 * (4096 - 512)
+    assert large["params_rest"] - small["params_rest"] == 256 * (4096 - 512)
+    for m in (small, large):
+        assert 0 < m["forward_layers"] < m["forward"] and 0 < m["backward_layers"] < m["backward"] and 0 < m["bytes_layers"] < m["bytes_kept"]
