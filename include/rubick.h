@@ -798,7 +798,8 @@ int32_t rk_schedule_round_nodes(rk_ctx *ctx, const rk_jobs *jobs, const rk_plan_
  *
  * Matrices (rk_matrix) have rows of consecutive elements; row i begins
  * i * stride elements behind data.  Unlike the other [device] pointers of this
- * header, those of the operators need only their element's alignment.  Strides are
+ * header, those of the operators need only their element's alignment (stats: 16
+ * bytes).  Strides are
  * not smaller than the width; outputs may not overlap inputs except where
  * stated, nor each other.  Every sum, statistic and softmax is held in 32 bits,
  * sums over all rows or tokens in fixed order, so that equal calls return equal
@@ -853,7 +854,7 @@ typedef struct {
 /* x, x_out share a type: that of y and u, or RK_F32.  y null: x_out = res_scale * x (the
  * stream's first norm; post_kind RK_NORM_NONE, no gate).  x_out null: not kept.  u null
  * exactly if pre_kind is RK_NORM_NONE.  x_out may be x, u may be y (same data and stride).
- *   stats  [device] n_rows x 4 floats: mean and 1/sqrt(..) of y, the same of
+ *   stats  [device] n_rows x 4 floats, 16-byte aligned: mean and 1/sqrt(..) of y, the same of
  *          x_out (mean 0 for RK_NORM_RMS; 0 and 1 for RK_NORM_NONE); for the backward pass
  * Rows of 1 to RK_NORM_MAX_WIDTH elements, up to 2^31 - 1 of them. */
 int32_t rk_norm_forward(rk_ctx *ctx, const rk_norm_block *block, uint64_t n_rows, uint32_t width,

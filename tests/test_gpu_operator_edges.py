@@ -212,3 +212,34 @@ def test_more_distilled_rows_than_one_launch_has(gpu):
         assert bool(((d.double() * rows - p).abs() <= 32 * U32).all())
         assert abs(float(total) - float((want - right).mean())) <= 64 * U32 * 4
 
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("e,k", [(8, 4), (64, 6), (200, 8), (1024, 32)])
+@pytest.mark.parametrize("n", [9, 1200])
+def test_the_largest_finite_logits(gpu, dtype, e, k, n):
+    """Tokens of the type's largest finite value, alone, beside its neighbour below and beside +inf: which are chosen, and in what order."""
+    torch = gpu[0]
+    l = logits_of(torch, n, e, dtype)
+    top = torch.finfo(l.dtype).max
+    below = torch.nextafter(torch.tensor(top, dtype=l.dtype), torch.tensor(0.0, dtype=l.dtype)) if dtype == "float32" else \
+        torch.tensor([torch.tensor(top, dtype=l.dtype).view(torch.int16).item() - 1], dtype=torch.int16).view(l.dtype)[0]
+    l[0] = top
+    l[1] = below
+    l[1, ::3] = top
+    l[2, e // 2], l[2, e - 1] = top, top
+    l[3] = -top
+    l[3, 1::2] = top
+    l[4] = top
+    l[4, [1, e - 2]] = INF
+    got = {name: v.cpu() for name, v in Route(gpu, l, None, k, True).forward().items()}
+    for t in range(5):
+        x = l[t].double()
+        order = sorted(range(e), key=lambda i: (-float(x[i]), i))[:k]
+        assert got["expert"][t].tolist() == order, t
+    for t in range(4):                                   # (the fifth's softmax is not a number)
+        x = l[t].double()
+        w = torch.exp(x[got["expert"][t].long()] - x.max())
+        assert float((got["weight"][t].double() - w / w.sum()).abs().max()) <= 64 * U32, t
+        assert abs(float(got["lse"][t]) - float(torch.logsumexp(x, 0))) <= 2 * U32 * top
+    assert bool(torch.isnan(got["lse"][4]))
