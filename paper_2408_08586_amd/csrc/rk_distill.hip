@@ -364,7 +364,7 @@ __device__ __forceinline__ void keep_row(const DistillArgs &A, uint64_t r, const
 
 // A workgroup a row: its sums, its loss and, if there is a d_student, its gradient.  Of what a thread reads, its first NR vectors stay in
 // registers and its next NL in LDS until then; only what is beyond them is read again.  Bound by HBM: 2048 x 128000 bfloat16, T = 2, both terms, 207 us,
-// 1.05 GB in and out, 5.0 TB/s (nine of sixteen vectors a thread of such a row are read twice); 1024 x 32000 float32 52 us, 262 MB, 5.0 TB/s.
+// 1.0 GB that has to move (a tenth of the rows has no weight and is only written), 1.2 GB that does (nine of sixteen vectors a thread are read twice), 5.9 TB/s; 1024 x 32000 float32 52 us, 262 MB, 5.0 TB/s.
 // Short rows, of which several fit a compute unit, have registers for eight vectors at five wavefronts a SIMD (at eight: 4096 x 32000 losses
 // 74 us, now 51).
 template <bool CUTS, int THREADS, int NR, int NL, int MOST, typename T, int CH, int SUMS>
@@ -556,7 +556,8 @@ template <typename T, int SUMS> __global__ __launch_bounds__(64 * JOIN_WAVES) vo
     A.total[0] = (float)total;
 }
 
-// The gradient of a slice of a row (or of all of it) from the row's log sums.  Bound by HBM: 777 x 50021 float16 31 us, 155 MB, 5.0 TB/s.
+// The gradient of a slice of a row (or of all of it) from the row's log sums.  Bound by HBM: 777 x 50021 float16 31 us, 141 MB (a quarter
+// of the rows has no weight and is only written), 4.6 TB/s.
 template <bool CUTS, int THREADS, typename T, int CH, int SUMS>
 __global__ __launch_bounds__(THREADS) void k_distill_gradient(DistillArgs A) {
     __shared__ float4 red[16];
@@ -625,8 +626,13 @@ __global__ __launch_bounds__(TOTAL_THREADS) void k_distill_total(DistillArgs A) 
 // Vectors that a thread of a long row keeps in registers and in LDS: 64 KB a workgroup, two of which fit a compute unit, at 64 registers
 // a lane.  A fourth in registers goes to scratch memory instead: 2048 x 128000 both at once 211 us with three, 219 with four, 512 x 64000 31 and 35.
 constexpr int DS_REGISTERS = 3, DS_LDS = 4;
-constexpr uint64_t DS_FEW = 256;                // rows
-constexpr uint32_t DS_SMALL = 16384;           // elements up to which 256 threads take a row or slice
+// Rows that are cut into slices where there are fewer.  Losses (four times as many): 300 x 20000 13.0 us, 500 x 32000 16.6 (cut below 2,048 rows 26.6
+// and 44.4; only below 512, 900 x 128000 55 instead of 69).  With the gradient: 5 x 128000 13 us; but above half as many a workgroup a row is faster, 200 x 128000 56 us
+// in slices and 30 in rows, 150 x 10000 23 and 9.
+constexpr uint64_t DS_FEW = 256;
+// Elements up to which 256 threads take a row or slice, beyond 1,024: gradient of 300 x 50000 16.5 us, with half as many elements
+// 26, with twice as many the same, but losses of 900 x 128000 57 instead of 69.
+constexpr uint32_t DS_SMALL = 16384;
 
 int32_t check_distill(rk_ctx *ctx, const rk_distill *d, uint64_t n_rows, uint32_t vocab, const rk_matrix *student, const rk_teacher *t, DistillArgs &A) {
     if (!d || !t) return rk_fail(ctx, RK_ERR_INVALID_ARG, "distill or teacher is null");
@@ -721,7 +727,9 @@ int32_t run(rk_ctx *ctx, uint32_t type, DistillArgs &A, bool want_loss, bool wan
     bool gradient = want_grad && !want_loss;
     if (want_loss && A.n_rows) {
         // Rows that would leave compute units without one are cut into slices: fewer than DS_FEW of them, or, where the loss is all and
-        // the slices need no second reading, up to four times as many.
+        // the slices need no second reading, up to four times as many.  512 workgroups with the gradient: 60 x 32000 17.8 us, 200 x 32000 33.3; 1,024
+        // 17.8 and 32.3.  4,096 without: 900 x 128000 69 us, 2,048 59, 8,192 55, others the same.  Slices of at least 4,096 elements with it: 60 x 32000
+        // 17.8 us, 2,048 18.5, 8,192 16.5; of 8,192 without: 500 x 32000 16.6 us, 4,096 19.4, 16,384 14.0, but 5 x 128000 6.8, 7.0 and 7.7.
         cut_rows(A, want_grad ? 512 : 4096, want_grad ? 4096 : 8192);
         if (A.slices > 1 && A.n_rows < (want_grad ? DS_FEW : 4 * DS_FEW)) {
             const size_t parts = (size_t)(A.n_rows * A.slices);
@@ -737,6 +745,8 @@ int32_t run(rk_ctx *ctx, uint32_t type, DistillArgs &A, bool want_loss, bool wan
         }
     }
     if (gradient && A.n_rows) {
+        // (300 x 50000 16.5 us, of 4,096 elements at least 19.4, of 16,384 18.4; 777 x 50000 with 8,192 workgroups 36 instead of 38, 1500 x 32000
+        // with 2,048 41 instead of 43)
         cut_rows(A, 4096, 8192);
         if ((rc = send(ctx, type, A, STEP_GRADIENT)) != RK_OK) return rc;
     }

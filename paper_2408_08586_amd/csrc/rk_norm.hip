@@ -927,7 +927,9 @@ extern "C" int32_t rk_norm_backward(rk_ctx *ctx, const rk_norm_block *block, uin
     const Shape H = sums_shape_of(width, type == RK_F32 ? 4 : 8);
     if (any) {
         // a chunk for every workgroup (of rows with gates that a wavefront holds: every wavefront) that fits the chip at once, but of
-        // several rows, where there are enough: chunks cost a start and sums that have to be joined
+        // several rows, where there are enough: chunks cost a start and sums that have to be joined.  Half as many chunks: 8192 x 8576 178 -> 206 us, 4096 x
+        // 5248 in 32 bits 94 -> 121, but 1000 x 2048 22.8 -> 17.9; twice as many: 184, 97 and 22.8, 1024 x 8576 39 -> 48.  Half the least rows: 2048 x 896
+        // 14.3 -> 17.2 us, 300 x 2048 12.3 -> 16.1; twice: 15.4 and 12.9, 1000 x 2048 17.8.  (In graphs of 4 to 16 calls.)
         const uint64_t at_once = H.per_wave && A.gate_rows ? 2048 : H.nc && H.threads <= 512 ? 512 : 256;
         const uint64_t least = n_rows <= 256 ? (H.per_wave && !A.gate_rows ? 4 : 1) : H.per_wave && !A.gate_rows ? 8 : 2;
         uint64_t rows = (n_rows + at_once - 1) / at_once;
