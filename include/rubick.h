@@ -948,6 +948,94 @@ int32_t rk_distill_loss_backward(rk_ctx *ctx, const rk_distill *distill, uint64_
                                  const rk_matrix *student, const rk_teacher *teacher, const float *d_total_or_null,
                                  float *loss, float *lse, float *total, const rk_matrix *d_student);
 
+#define RK_RECUR_MAX_WIDTH 1048576u
+
+/* A gated linear recurrence over the rows of sequences that lie one behind the other, every column by itself:
+ *     f_t = sigmoid(z_t + bias)
+ *     h_t = f_t h_{t-1} + (1 - f_t) x_t      (coupled)
+ *     h_t = f_t h_{t-1} + x_t                (otherwise)
+ * h before a sequence's first row is its row of state_in, or zero.  Sequence i has rows offsets[i] to
+ * offsets[i + 1] - 1 (offsets [device] n_seqs + 1, ascending, none below 0 or above the rows; equal ones: a
+ * sequence without rows); rows that no sequence has are neither read nor written.  offsets null:
+ * every seq_rows rows are a sequence, the last may have fewer; seq_rows 0: all rows are one. */
+typedef struct {
+    uint32_t coupled;
+    uint32_t param_type;
+    const void *bias;           /* [device] width elements of param_type, or null: zeros */
+    const int32_t *offsets;
+    uint32_t n_seqs;            /* with offsets */
+    uint64_t seq_rows;          /* without */
+} rk_recur;
+
+/* x, z and h share a type; states are RK_F32 matrices, a row a sequence.  state_in null: zeros; state_out null: not kept;
+ * that of a sequence without rows is its state_in.  h may be x or z, state_out may be state_in (same data and
+ * stride).  A NaN stays in its sequence.  Up to 2^31 - 1 rows. */
+int32_t rk_recur_forward(rk_ctx *ctx, const rk_recur *recur, uint64_t n_rows, uint32_t width, const rk_matrix *x,
+                         const rk_matrix *z, const rk_matrix *state_in_or_null, const rk_matrix *h,
+                         const rk_matrix *state_out_or_null);
+
+/* From the gradients of h (dh) and state_out (d_state_out, null: zero) and what the forward pass had and
+ * gave, those of x, z, state_in and the bias (the last two null: not wanted):
+ *     e_t = dh_t + f_{t+1} e_{t+1}           (behind a sequence's last row stands d_state_out)
+ *     dx_t = (1 - f_t) e_t,  dz_t = e_t (h_{t-1} - x_t) f_t (1 - f_t)       (coupled)
+ *     dx_t = e_t,            dz_t = e_t h_{t-1} f_t (1 - f_t)               (otherwise; x may be null then)
+ *     d_state_in = f e of the first row,  d_bias = sum of dz over the rows
+ * h is taken as it was stored.  dx may be dh, d_state_in may be d_state_out.  d_bias [device] width floats. */
+int32_t rk_recur_backward(rk_ctx *ctx, const rk_recur *recur, uint64_t n_rows, uint32_t width, const rk_matrix *x_or_null,
+                          const rk_matrix *z, const rk_matrix *h, const rk_matrix *state_in_or_null, const rk_matrix *dh,
+                          const rk_matrix *d_state_out_or_null, const rk_matrix *dx, const rk_matrix *dz,
+                          const rk_matrix *d_state_in_or_null, float *d_bias_or_null);
+
+/* Dropout whose mask is made where it is needed and never stored: Philox4x32-10 (Salmon, Moraes, Dror and Shaw, 2011) under the key
+ * `seed` turns the counter (column / 8, row, offset's low and high word) into eight 16-bit numbers, one for each of
+ * eight columns, the first in the low half of the first word.  An element stays if its number is not below D = floor(65536 p + 1/2), and
+ * is then multiplied by 65536 / (65536 - D).  What is dropped counts as zero whatever it was. */
+typedef struct {
+    float p;                    /* 0 to 1: the share that is dropped, in steps of 2^-16 */
+    const uint64_t *rng;        /* [device] two words: seed, offset; read when the kernel runs */
+} rk_dropout;
+
+/* out = residual + dropped x (residual null: dropped x).  out has the residual's type: that of x, or RK_F32.  out may be x or the
+ * residual (same type, data and stride).  Up to 2^31 - 1 rows of up to 2^28 elements. */
+int32_t rk_dropout_forward(rk_ctx *ctx, const rk_dropout *dropout, uint64_t n_rows, uint32_t width, const rk_matrix *x,
+                           const rk_matrix *residual_or_null, const rk_matrix *out);
+
+/* dx from the gradient of out, with the same rng (the residual's gradient is that of out); dx may be d_out. */
+int32_t rk_dropout_backward(rk_ctx *ctx, const rk_dropout *dropout, uint64_t n_rows, uint32_t width, const rk_matrix *d_out,
+                            const rk_matrix *dx);
+
+#define RK_HEAD_MAX_WIDTH 65536u
+
+/* The loss of rows x under a vocabulary's weights, without keeping their logits:
+ *     l = logit_scale x weight^T     lse = log sum exp l     loss = lse - l[label] + z_weight lse^2
+ * A row whose label lies outside the vocabulary or whose weight is 0 is left out, whatever it holds: loss, lse
+ * and gradients 0. */
+typedef struct {
+    float logit_scale;          /* finite, not 0 */
+    float z_weight;             /* finite, >= 0 */
+} rk_head;
+
+/* x n_rows x width, weight vocab x width, of one type; label [device] n_rows; row_weight [device] n_rows or null: ones;
+ * loss, lse [device] n_rows (loss unweighted); total [device] one float: sum of row_weight * loss.  Up to 2^20 rows,
+ * of up to RK_HEAD_MAX_WIDTH elements, and 2^28 words. */
+int32_t rk_head_loss(rk_ctx *ctx, const rk_head *head, uint64_t n_rows, uint32_t width, uint32_t vocab, const rk_matrix *x,
+                     const rk_matrix *weight, const int32_t *label, const float *row_weight_or_null, float *loss, float *lse,
+                     float *total);
+
+/* The gradients of x and weight (either null: not wanted; not both) from that of total (d_total [device] one float, null:
+ * one) and the forward pass's lse.  They have x's type; neither may overlap an input.  The logits' gradients are
+ * made in pieces of the vocabulary and rounded to x's type on their way into the products, relative to their row's weight for dx and
+ * to the largest row's weight for d_weight. */
+int32_t rk_head_backward(rk_ctx *ctx, const rk_head *head, uint64_t n_rows, uint32_t width, uint32_t vocab, const rk_matrix *x,
+                         const rk_matrix *weight, const int32_t *label, const float *row_weight_or_null, const float *lse,
+                         const float *d_total_or_null, const rk_matrix *dx_or_null, const rk_matrix *d_weight_or_null);
+
+/* Both at once, where the gradient of total is known beforehand. */
+int32_t rk_head_loss_backward(rk_ctx *ctx, const rk_head *head, uint64_t n_rows, uint32_t width, uint32_t vocab,
+                              const rk_matrix *x, const rk_matrix *weight, const int32_t *label, const float *row_weight_or_null,
+                              const float *d_total_or_null, float *loss, float *lse, float *total, const rk_matrix *dx_or_null,
+                              const rk_matrix *d_weight_or_null);
+
 /* ---- measurement helper (no part of the method) --------------------------- */
 
 /* Streams a buffer and nothing else, for the benchmark's roofline context:

@@ -194,3 +194,102 @@ def distill(student, t_logits, index, label, row_weight, tau, kd, ce, d_total=1.
     total = torch.where(wv != 0, wv * loss, 0.0).sum().reshape(1)
     big = torch.nan_to_num(big, nan=0.0)
     return dict(loss=loss, lse=lse, total=total, d_student=d, big_loss=big_loss, big=big)
+
+
+# ---------------------------------------------------------------------- gated recurrence
+def recurrence(x, z, bias, at, coupled, state_in, dh=None, d_state_out=None, h_given=None):
+    """Rows of sequences at[i] .. at[i + 1] - 1, one after the other.  Sizes: what an error of one unit of each row's own magnitude adds up
+    to on its way through the rows behind it.  With dh, the gradients too, from h as given; rows that no sequence has are NaN."""
+    n, width = len(at) - 1, z.shape[1]
+    v = z if bias is None else z + bias
+    f, nf = torch.sigmoid(v), torch.sigmoid(-v)
+    share = nf if coupled else torch.ones_like(nf)
+    start = torch.zeros(n, width, dtype=torch.float64) if state_in is None else state_in.clone()
+    nan = lambda *s: torch.full(s, float("nan"), dtype=torch.float64)
+    out, size = {"h": nan(*z.shape), "state_out": start.clone()}, {"h": nan(*z.shape), "state_out": start.abs()}
+    for s in range(n):
+        h, big, err = start[s], start[s].abs(), start[s].abs()
+        for t in range(at[s], at[s + 1]):
+            h = f[t] * h + share[t] * x[t]
+            big = f[t] * big + share[t] * x[t].abs()
+            err = f[t] * err + big
+            out["h"][t], size["h"][t] = h, err
+        out["state_out"][s], size["state_out"][s] = h, err
+    if dh is None:
+        return out, size
+    before = nan(*z.shape)
+    back = torch.zeros(n, width, dtype=torch.float64) if d_state_out is None else d_state_out
+    names = ("dx", "dz")
+    for k in names:
+        out[k], size[k] = nan(*z.shape), nan(*z.shape)
+    out["d_state_in"], size["d_state_in"] = back.clone(), back.abs()
+    out["d_bias"], size["d_bias"] = torch.zeros(width, dtype=torch.float64), torch.zeros(width, dtype=torch.float64)
+    for s in range(n):
+        carry, big, err = back[s], back[s].abs(), back[s].abs()
+        for t in reversed(range(at[s], at[s + 1])):
+            before[t] = h_given[t - 1] if t > at[s] else start[s]
+            e, big = dh[t] + carry, dh[t].abs() + big
+            err = err + big
+            of = before[t] - x[t] if coupled else before[t]
+            most = before[t].abs() + (x[t].abs() if coupled else 0.0)
+            out["dx"][t], size["dx"][t] = share[t] * e, share[t] * err
+            out["dz"][t], size["dz"][t] = e * of * f[t] * nf[t], err * most * f[t] * nf[t]
+            out["d_bias"] += out["dz"][t]
+            size["d_bias"] += size["dz"][t]
+            carry, big, err = f[t] * e, f[t] * big, f[t] * err
+        out["d_state_in"][s], size["d_state_in"][s] = carry, err
+    return out, size
+
+
+# ---------------------------------------------------------------------- dropout
+def philox(counter, key):
+    """Philox4x32-10 (Salmon, Moraes, Dror and Shaw, 2011) of one counter, in whole numbers."""
+    c, k, low = list(counter), list(key), 0xFFFFFFFF
+    for _ in range(10):
+        p, q = c[0] * 0xD2511F53, c[2] * 0xCD9E8D57
+        c = [(q >> 32) ^ c[1] ^ k[0], q & low, (p >> 32) ^ c[3] ^ k[1], p & low]
+        k = [(k[0] + 0x9E3779B9) & low, (k[1] + 0xBB67AE85) & low]
+    return c
+
+
+def dropout_numbers(rows, width, seed, offset):
+    """The 16-bit number of every element: rows is a list of row numbers."""
+    low = 0xFFFFFFFF
+    out = torch.empty(len(rows), (width + 7) // 8 * 8, dtype=torch.int32)
+    for i, r in enumerate(rows):
+        for g in range((width + 7) // 8):
+            words = philox((g, r, offset & low, offset >> 32), (seed & low, seed >> 32))
+            out[i, 8 * g:8 * g + 8] = torch.tensor([w >> s & 0xFFFF for w in words for s in (0, 16)], dtype=torch.int32)
+    return out[:, :width]
+
+
+# ---------------------------------------------------------------------- vocabulary head
+def head(x, weight, label, row_weight, scale, z_weight, d_total, lse_given=None):
+    """Loss, lse, total and gradients; sizes: of the logits (loss, lse), and the magnitudes that the gradients' sums take in: g |W| and g |x|."""
+    rows, vocab = x.shape[0], weight.shape[0]
+    w = torch.ones(rows, dtype=torch.float64) if row_weight is None else row_weight
+    there = (w != 0) & (label >= 0) & (label < vocab)
+    kept = torch.nonzero(there)[:, 0]
+    zeros = lambda *s: torch.zeros(*s, dtype=torch.float64)
+    out = {"loss": zeros(rows), "lse": zeros(rows), "dx": zeros(*x.shape), "d_weight": zeros(*weight.shape)}
+    size = {k: v.clone() for k, v in out.items()}
+    if len(kept):
+        xs, l = x[kept], scale * x[kept] @ weight.t()
+        big = (abs(scale) * xs.abs() @ weight.abs().t()).amax(1)
+        lse = torch.logsumexp(l, 1)
+        at = torch.arange(len(kept))
+        out["loss"][kept] = lse - l[at, label[kept].long()] + z_weight * lse ** 2
+        out["lse"][kept] = lse
+        size["loss"][kept], size["lse"][kept] = big * (2 + 2 * z_weight * lse.abs()), big
+        use = lse if lse_given is None else lse_given[kept]
+        p = torch.exp(l - use[:, None])
+        g = p * (1 + 2 * z_weight * use[:, None])
+        g[at, label[kept].long()] -= 1
+        f = (w[kept] * d_total * scale)[:, None]
+        out["dx"][kept], out["d_weight"] = f * (g @ weight), (f * g).t() @ xs
+        most = g.abs() + p * (1 + 2 * z_weight * use[:, None].abs())
+        size["dx"][kept], size["d_weight"] = f.abs() * (most @ weight.abs()), (f.abs() * most).t() @ xs.abs()
+        size["big"] = big
+    out["total"] = (w[kept] * out["loss"][kept]).sum().reshape(1)
+    size["total"] = (w[kept].abs() * (size["loss"][kept] + out["loss"][kept].abs())).sum().reshape(1)
+    return out, size

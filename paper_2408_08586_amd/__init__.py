@@ -28,7 +28,9 @@ EXPORTS = ("rk_create", "rk_destroy", "rk_sync", "rk_last_error", "rk_enumerate_
            "rk_eval_points", "rk_min_res", "rk_allocate_sla", "rk_schedule_round_sla", "rk_fit_models", "rk_simulate", "rk_schedule_rounds_shared", "rk_place", "rk_allocate_static", "rk_place_plans",
            "rk_schedule_round_placed", "rk_reschedule", "rk_probe_stream", "rk_eval_best_plan", "rk_reschedule_nodes", "rk_best_plan_placed", "rk_reschedule_rounds", "rk_schedule_round_nodes", "rk_privileged", "rk_curve_slopes",
            "rk_norm_forward", "rk_norm_backward", "rk_route_forward", "rk_route_backward", "rk_distill_loss",
-           "rk_distill_backward", "rk_distill_loss_backward")
+           "rk_distill_backward", "rk_distill_loss_backward",
+           "rk_recur_forward", "rk_recur_backward", "rk_dropout_forward", "rk_dropout_backward", "rk_head_loss", "rk_head_backward",
+           "rk_head_loss_backward")
 
 _JOB_F32 = ("P_bytes", "seq", "hidden", "elem_bytes", "t_fwd_sample", "k_bwd", "k_sync", "k_opt", "k_opt_off",
             "k_off", "k_swap", "k_const", "mem_state", "mem_act", "mem_act_gc", "mem_const", "ref_thr")
@@ -612,6 +614,7 @@ def u32(t) -> np.ndarray:
 RK_F32, RK_BF16, RK_F16 = 0, 1, 2
 RK_NORM_KINDS = {"none": 0, "rms": 1, "layer": 2}
 RK_NORM_MAX_WIDTH, RK_MAX_EXPERTS, RK_MAX_TOP_K, RK_MAX_TEACHER_LOGITS = 32768, 1024, 32, 1024
+RK_RECUR_MAX_WIDTH, RK_HEAD_MAX_WIDTH = 1048576, 65536
 
 
 class rk_matrix(C.Structure):
@@ -643,6 +646,19 @@ class rk_teacher(C.Structure):
                 ("row_weight", C.c_void_p)]
 
 
+class rk_recur(C.Structure):
+    _fields_ = [("coupled", C.c_uint32), ("param_type", C.c_uint32), ("bias", C.c_void_p), ("offsets", C.c_void_p),
+                ("n_seqs", C.c_uint32), ("seq_rows", C.c_uint64)]
+
+
+class rk_dropout(C.Structure):
+    _fields_ = [("p", C.c_float), ("rng", C.c_void_p)]
+
+
+class rk_head(C.Structure):
+    _fields_ = [("logit_scale", C.c_float), ("z_weight", C.c_float)]
+
+
 def _refuse(what):
     raise RkError(RK_ERR_INVALID_ARG, what)
 
@@ -654,7 +670,7 @@ def _types():
     if not _TYPES:
         import torch
         _TYPES.update({torch.float32: RK_F32, torch.bfloat16: RK_BF16, torch.float16: RK_F16, "float32": torch.float32,
-                       "int32": torch.int32, "uint8": torch.uint8, "bool": torch.bool})
+                       "int32": torch.int32, "int64": torch.int64, "uint8": torch.uint8, "bool": torch.bool})
     return _TYPES
 
 
@@ -710,6 +726,9 @@ _OPERATORS = {
     "rk_norm_forward": "cbqu" + "m" * 4 + "p", "rk_norm_backward": "cbqu" + "mmp" + "m" * 4 + "g",
     "rk_route_forward": "crqm" + "p" * 8, "rk_route_backward": "crqm" + "p" * 6 + "m",
     "rk_distill_loss": "cdqumt" + "ppp", "rk_distill_backward": "cdqumt" + "ppm", "rk_distill_loss_backward": "cdqumt" + "ppppm",
+    "rk_recur_forward": "csqu" + "m" * 5, "rk_recur_backward": "csqu" + "m" * 9 + "p",
+    "rk_dropout_forward": "coqu" + "mmm", "rk_dropout_backward": "coqu" + "mm",
+    "rk_head_loss": "chquu" + "mmpp" + "ppp", "rk_head_backward": "chquu" + "mmpp" + "ppmm", "rk_head_loss_backward": "chquu" + "mmpp" + "ppppmm",
 }
 
 
@@ -722,7 +741,8 @@ def _operator(name):
     f = _functions.get(name)
     if f is None:
         kinds = {"c": C.c_void_p, "q": C.c_uint64, "u": C.c_uint32, "p": C.c_void_p, "b": C.POINTER(rk_norm_block), "g": C.POINTER(rk_norm_grads),
-                 "m": C.POINTER(rk_matrix), "r": C.POINTER(rk_router), "d": C.POINTER(rk_distill), "t": C.POINTER(rk_teacher)}
+                 "m": C.POINTER(rk_matrix), "r": C.POINTER(rk_router), "d": C.POINTER(rk_distill), "t": C.POINTER(rk_teacher),
+                 "s": C.POINTER(rk_recur), "o": C.POINTER(rk_dropout), "h": C.POINTER(rk_head)}
         f = load_library()[name]
         f.restype, f.argtypes = C.c_int32, [kinds[k] for k in _OPERATORS[name]]
         _functions[name] = f
@@ -880,3 +900,108 @@ def rk_distill_loss_backward(ctx, distill: rk_distill, student, teacher_logits, 
                   _plain(d_total, "d_total", (1,), _F32), _plain(loss, "loss", (rows,), _F32),
                   _plain(lse, "lse", (rows, 2), _F32), _plain(total, "total", (1,), _F32),
                   _ref(_matrix(d_student, "d_student", student.shape)))
+
+
+class Recur:
+    """A gated linear recurrence (rk_recur).  bias [width] or None; offsets int32 [sequences + 1] on the GPU, or None: every seq_rows rows
+    are a sequence (0: all of them are one)."""
+
+    def __init__(self, coupled=True, bias=None, offsets=None, seq_rows=0):
+        if bias is not None and (bias.dim() != 1 or not bias.is_contiguous()):
+            _refuse("bias is no contiguous vector")
+        if offsets is not None and (offsets.dim() != 1 or len(offsets) < 1 or seq_rows):
+            _refuse("offsets are a vector of the sequences' number and one, or there are seq_rows")
+        self.bias, self.offsets = bias, offsets
+        self.n_seqs = None if offsets is None else len(offsets) - 1
+        at = None if offsets is None else _plain(offsets, "offsets", offsets.shape, _I32)
+        self.c = rk_recur(int(bool(coupled)), RK_F32 if bias is None else _type_of(bias), None if bias is None else bias.data_ptr(), at,
+                          self.n_seqs or 0, int(seq_rows))
+
+    def _sizes(self, z):
+        """The shapes of the rows and of the states that a call is about."""
+        size = z.shape
+        if len(size) != 2 or (self.bias is not None and len(self.bias) != size[1]):
+            _refuse("z has no rows of the bias's width")
+        per = self.c.seq_rows
+        seqs = self.n_seqs if self.offsets is not None else (size[0] + per - 1) // per if per else 1
+        return size, size[:0] + (seqs, size[1])
+
+
+def rk_recur_forward(ctx, recur: Recur, x, z, state_in, h, state_out):
+    """x, z, h [rows, width]; state_in and state_out float32 [sequences, width] or None."""
+    size, states = recur._sizes(z)
+    _same_device(z, x, state_in, h, state_out, recur.bias, recur.offsets)
+    _check(ctx, _operator("rk_recur_forward")(
+        ctx, C.byref(recur.c), size[0], size[1], _ref(_matrix(x, "x", size)), C.byref(_matrix(z, "z")), _ref(_matrix(state_in, "state_in", states)),
+        _ref(_matrix(h, "h", size)), _ref(_matrix(state_out, "state_out", states))))
+
+
+def rk_recur_backward(ctx, recur: Recur, x, z, h, state_in, dh, d_state_out, dx, dz, d_state_in, d_bias):
+    """d_bias float32 [width] or None; x may be None if the recurrence is not coupled."""
+    size, states = recur._sizes(z)
+    _same_device(z, x, h, state_in, dh, d_state_out, dx, dz, d_state_in, d_bias, recur.bias, recur.offsets)
+    _check(ctx, _operator("rk_recur_backward")(
+        ctx, C.byref(recur.c), size[0], size[1], _ref(_matrix(x, "x", size)), C.byref(_matrix(z, "z")), _ref(_matrix(h, "h", size)),
+        _ref(_matrix(state_in, "state_in", states)), _ref(_matrix(dh, "dh", size)), _ref(_matrix(d_state_out, "d_state_out", states)),
+        _ref(_matrix(dx, "dx", size)), _ref(_matrix(dz, "dz", size)), _ref(_matrix(d_state_in, "d_state_in", states)),
+        _plain(d_bias, "d_bias", size[1:], _F32)))
+
+
+class Dropout:
+    """Dropout of a share p (rk_dropout) under rng: int64 [2] on the GPU, the seed and the offset, which the kernels read when they run."""
+
+    def __init__(self, p, rng):
+        self.rng = rng
+        self.c = rk_dropout(float(p), _plain(rng, "rng", (2,), ("int64",)))
+
+
+def rk_dropout_forward(ctx, dropout: Dropout, x, residual, out):
+    """out [rows, width] has the residual's type (None: that of x): x's or float32."""
+    size = x.shape
+    _same_device(x, residual, out, dropout.rng)
+    _check(ctx, _operator("rk_dropout_forward")(
+        ctx, C.byref(dropout.c), size[0], size[-1], C.byref(_matrix(x, "x")), _ref(_matrix(residual, "residual", size)), _ref(_matrix(out, "out", size))))
+
+
+def rk_dropout_backward(ctx, dropout: Dropout, d_out, dx):
+    size = d_out.shape
+    _same_device(d_out, dx, dropout.rng)
+    _check(ctx, _operator("rk_dropout_backward")(
+        ctx, C.byref(dropout.c), size[0], size[-1], C.byref(_matrix(d_out, "d_out")), _ref(_matrix(dx, "dx", size))))
+
+
+def make_head(logit_scale=1.0, z_weight=0.0) -> rk_head:
+    return rk_head(float(logit_scale), float(z_weight))
+
+
+def _head_call(ctx, name, head, x, weight, label, row_weight, *rest):
+    size = x.shape
+    if len(size) != 2 or weight.dim() != 2 or weight.shape[1] != size[1]:
+        _refuse("x and weight are not [rows, width] and [vocab, width]")
+    _check(ctx, _operator(name)(
+        ctx, C.byref(head), size[0], size[1], weight.shape[0], C.byref(_matrix(x, "x")), C.byref(_matrix(weight, "weight")),
+        _plain(label, "label", size[:1], _I32), _plain(row_weight, "row_weight", size[:1], _F32), *rest))
+
+
+def rk_head_loss(ctx, head: rk_head, x, weight, label, row_weight, loss, lse, total):
+    """x [rows, width], weight [vocab, width]; label int32 [rows], row_weight float32 [rows] or None; loss [rows], lse [rows], total [1], all
+    float32."""
+    _same_device(x, weight, label, row_weight, loss, lse, total)
+    rows = x.shape[:1]
+    _head_call(ctx, "rk_head_loss", head, x, weight, label, row_weight, _plain(loss, "loss", rows, _F32), _plain(lse, "lse", rows, _F32),
+               _plain(total, "total", (1,), _F32))
+
+
+def rk_head_backward(ctx, head: rk_head, x, weight, label, row_weight, lse, d_total, dx, d_weight):
+    """dx or d_weight may be None."""
+    _same_device(x, weight, label, row_weight, lse, d_total, dx, d_weight)
+    _head_call(ctx, "rk_head_backward", head, x, weight, label, row_weight, _plain(lse, "lse", x.shape[:1], _F32),
+               _plain(d_total, "d_total", (1,), _F32), _ref(_matrix(dx, "dx", x.shape)), _ref(_matrix(d_weight, "d_weight", weight.shape)))
+
+
+def rk_head_loss_backward(ctx, head: rk_head, x, weight, label, row_weight, d_total, loss, lse, total, dx, d_weight):
+    _same_device(x, weight, label, row_weight, d_total, loss, lse, total, dx, d_weight)
+    rows = x.shape[:1]
+    _head_call(ctx, "rk_head_loss_backward", head, x, weight, label, row_weight, _plain(d_total, "d_total", (1,), _F32),
+               _plain(loss, "loss", rows, _F32), _plain(lse, "lse", rows, _F32), _plain(total, "total", (1,), _F32),
+               _ref(_matrix(dx, "dx", x.shape)), _ref(_matrix(d_weight, "d_weight", weight.shape)))

@@ -1,0 +1,590 @@
+// The loss of rows under a vocabulary's weights and its gradients, without keeping the logits (rk_head in rubick.h).
+//
+// Rows that count are gathered first, so that products take no others, and padded with zeros to whole steps of k.  The loss
+// takes the logits' tiles out of the product's registers: of every row the largest and the sum of exponentials over a wavefront's
+// words, joined in fixed order.  The gradients go through the vocabulary in pieces: a piece's logits are made again and become
+// g = p (1 + 2 z lse) - onehot, written both ways round, rounded to the rows' type with a power of two for each row that keeps float16 in its range;
+// dx adds up g W over the pieces in float32, and the piece's rows of d_weight are g^T x.  Every product has k along both sides' rows:
+// x and the piece of W are turned around once for that.
+#include "rk_gemm.h"
+
+namespace {
+
+constexpr uint32_t HD_THREADS = 1024;
+constexpr uint64_t HD_BUDGET = 1ull << 30;                  // bytes of a piece's gradients and weights
+constexpr uint64_t HD_PARTS = 1ull << 28;                   // ... of the sums of the loss's tiles
+
+struct RowInfo { float lse, factor, up, share; };           // g = (p factor - onehot) times up for dx, times share for d_weight
+
+// what the device keeps of the rows that count
+struct Rows {
+    uint32_t *count;            // [0] how many, [1] bits of the largest weight's power of two
+    int32_t *row, *place;       // a kept row's place in the matrix; a row's place among the kept, or -1
+    int32_t *label;
+    float *weight, *label_logit, *top, *sum;
+    RowInfo *info;
+};
+
+struct RowsArgs {
+    Rows R;
+    const int32_t *label;
+    const float *row_weight;
+    float *loss, *lse;          // zeros for rows that are left out, or null
+    uint64_t n_rows;
+    uint32_t vocab;
+};
+
+__global__ __launch_bounds__(HD_THREADS) void k_head_rows(const RowsArgs A) {
+    __shared__ uint32_t in_wave[HD_THREADS / 64];
+    constexpr uint32_t EACH = 4;
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    uint32_t before = 0;
+    for (uint64_t begin = 0; begin < A.n_rows; begin += HD_THREADS * EACH) {
+        int32_t label[EACH];
+        float weight[EACH];
+        uint32_t n = 0;
+#pragma unroll
+        for (uint32_t e = 0; e < EACH; ++e) {
+            const uint64_t r = begin + threadIdx.x * EACH + e;
+            label[e] = r < A.n_rows ? A.label[r] : -1;
+            weight[e] = r < A.n_rows ? A.row_weight ? A.row_weight[r] : 1.f : 0.f;
+            if (label[e] < 0 || (uint32_t)label[e] >= A.vocab || weight[e] == 0.f) label[e] = -1;
+            n += label[e] >= 0;
+        }
+        uint32_t upto = n;                                  // inclusive over the wavefront
+#pragma unroll
+        for (uint32_t d = 1; d < 64; d *= 2) {
+            const uint32_t o = __shfl_up(upto, d, 64);
+            upto += lane >= d ? o : 0u;
+        }
+        if (lane == 63) in_wave[wave] = upto;
+        __syncthreads();
+        uint32_t at = before + upto - n, all = 0;
+#pragma unroll
+        for (uint32_t w = 0; w < HD_THREADS / 64; ++w) {
+            at += w < wave ? in_wave[w] : 0u;
+            all += in_wave[w];
+        }
+        before += all;
+#pragma unroll
+        for (uint32_t e = 0; e < EACH; ++e) {
+            const uint64_t r = begin + threadIdx.x * EACH + e;
+            if (r >= A.n_rows) continue;
+            const bool there = label[e] >= 0;
+            A.R.place[r] = there ? (int32_t)at : -1;
+            if (there) {
+                A.R.row[at] = (int32_t)r;
+                A.R.label[at] = label[e];
+                A.R.weight[at] = weight[e];
+                A.R.top[at] = -INFINITY;
+                A.R.sum[at] = 0.f;
+                ++at;
+            } else if (A.loss) {
+                A.loss[r] = 0.f;
+                A.lse[r] = 0.f;
+            }
+        }
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) A.R.count[0] = before;
+}
+
+// the kept rows of x one behind the other, each padded with zeros; a workgroup a row
+template <typename T> __global__ __launch_bounds__(256) void k_head_gather(const Rows R, const T *x, uint64_t stride, uint32_t width, T *out, uint32_t out_width) {
+    for (uint32_t i = blockIdx.x; i < R.count[0]; i += gridDim.x) {
+        const T *const from = x + (uint64_t)R.row[i] * stride;
+        T *const to = out + (uint64_t)i * out_width;
+        for (uint32_t c = threadIdx.x; c < out_width; c += 256) to[c] = c < width ? from[c] : (T)0.f;
+    }
+}
+// rows of any alignment as rows padded with zeros
+template <typename T> __global__ __launch_bounds__(256) void k_head_pad(const T *x, uint64_t stride, uint32_t n_rows, uint32_t width, T *out, uint32_t out_width) {
+    for (uint32_t i = blockIdx.x; i < n_rows; i += gridDim.x) {
+        const T *const from = x + (uint64_t)i * stride;
+        T *const to = out + (uint64_t)i * out_width;
+        for (uint32_t c = threadIdx.x; c < out_width; c += 256) to[c] = c < width ? from[c] : (T)0.f;
+    }
+}
+// out[c][r] = x[r][c]; zeros up to out_width.  rows on the device (count) or given
+template <typename T> __global__ __launch_bounds__(256) void k_head_turn(const T *x, uint64_t stride, const uint32_t *count, uint32_t n_rows, uint32_t width, T *out, uint64_t out_stride, uint32_t tiles_c) {
+    __shared__ T tile[64][65];
+    const uint32_t rows = count ? *count : n_rows;
+    const uint32_t r0 = blockIdx.x / tiles_c * 64u, c0 = blockIdx.x % tiles_c * 64u;
+    constexpr uint32_t STEP = GM_ROW / sizeof(T);           // (whole steps of k are zeros, no more are read)
+    if (r0 >= (rows + STEP - 1) / STEP * STEP) return;
+    const uint32_t lane = threadIdx.x & 63u, w = threadIdx.x >> 6;
+#pragma unroll
+    for (uint32_t i = 0; i < 16; ++i) {
+        const uint32_t r = r0 + w * 16 + i, c = c0 + lane;
+        tile[w * 16 + i][lane] = r < rows && c < width ? x[(uint64_t)r * stride + c] : (T)0.f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (uint32_t i = 0; i < 16; ++i) {
+        const uint32_t c = c0 + w * 16 + i;
+        if (c < width) out[(uint64_t)c * out_stride + r0 + lane] = tile[lane][w * 16 + i];
+    }
+}
+
+struct LogitsArgs {
+    Rows R;
+    Side W, X;                  // of this piece; the kept rows
+    uint32_t bytes_k, tiles_b;
+    uint32_t first, words;      // the piece's first word, how many it has
+    float scale;
+    float2 *parts;              // loss: [words / (TA / WA)][kept rows]
+    uint64_t parts_stride;
+    void *g, *gt;               // gradient: [kept rows][g_stride], [words][gt_stride]; null: not wanted
+    uint64_t g_stride, gt_stride;
+};
+template <typename T> __device__ __forceinline__ float exp_of(float x) {
+    if constexpr (sizeof(T) == 4) return exp_f32(x);
+    else return __builtin_amdgcn_exp2f(x * 1.4426950408889634f);
+}
+
+// LOSS: a wavefront's largest logit and sum of exponentials of every row, and its label's logit; otherwise the gradients of the logits
+template <typename T, int TA, int TB, int WA, bool LOSS> __global__ __launch_bounds__(GM_THREADS) void k_head_logits(const LogitsArgs A) {
+    typedef Tile<T, TA, TB, WA> Tl;
+    const uint32_t n = A.R.count[0];
+    const uint32_t a0 = blockIdx.x / A.tiles_b * TA, b0 = blockIdx.x % A.tiles_b * TB;
+    if (b0 >= n) return;
+    Side X = A.X;
+    X.rows = n;
+    Tl t;
+    t.run(A.W, X, a0, b0, 0, A.bytes_k);
+    const uint32_t lane = threadIdx.x & 63u, a_of = a0 + Tl::wave_a() + 4 * (lane >> 4), b_of = b0 + Tl::wave_b() + (lane & 15u);
+#pragma unroll
+    for (int j = 0; j < Tl::MB; ++j) {
+        const uint32_t b = b_of + 16 * j;
+        const bool there = b < n;
+        const int64_t label = there ? (int64_t)A.R.label[b] - (int64_t)A.first : -1;
+        if constexpr (LOSS) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < Tl::MA; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t a = a_of + 16 * i + q;
+                    float l = t.acc[i][j][q] * A.scale;
+                    l = a < A.words ? l : -INFINITY;
+                    t.acc[i][j][q] = l;
+                    top = fmaxf(top, l);
+                    if (label == (int64_t)a) A.R.label_logit[b] = l;
+                }
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            float sum = 0.f;
+            const float from = top == -INFINITY ? 0.f : top;
+#pragma unroll
+            for (int i = 0; i < Tl::MA; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) sum += exp_of<T>(t.acc[i][j][q] - from);
+            sum += __shfl_xor(sum, 16, 64);
+            sum += __shfl_xor(sum, 32, 64);
+            if (there && lane < 16) A.parts[(uint64_t)((a0 + Tl::wave_a()) / (TA / WA)) * A.parts_stride + b] = make_float2(top, sum);
+        } else {
+            const RowInfo info = there ? A.R.info[b] : RowInfo{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < Tl::MA; ++i) {
+                const uint32_t a = a_of + 16 * i;
+                float g[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float p = exp_of<T>(t.acc[i][j][q] * A.scale - info.lse) * info.factor;
+                    g[q] = there && a + q < A.words ? label == (int64_t)(a + q) ? p - 1.f : p : 0.f;
+                }
+                if (A.g) {
+                    Vec<T, 4> v;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[q] = (T)(g[q] * info.up);
+                    if (there) *(Vec<T, 4> *)((T *)A.g + (uint64_t)b * A.g_stride + a) = v;
+                }
+                if (A.gt)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (a + q < A.words) ((T *)A.gt)[(uint64_t)(a + q) * A.gt_stride + b] = (T)(g[q] * info.share);
+            }
+        }
+    }
+}
+
+struct JoinArgs {
+    Rows R;
+    const float2 *parts;
+    uint64_t parts_stride;
+    uint32_t n_parts;
+    bool last;
+    float z_weight;
+    float *loss, *lse, *total;
+    uint64_t n_rows;
+};
+// sixteen lanes a row: a row's parts in sixteen runs, joined in fixed order
+__global__ __launch_bounds__(256) void k_head_join(const JoinArgs A) {
+    __shared__ float2 runs[16][16];
+    const uint32_t n = A.R.count[0];
+    const uint32_t x = threadIdx.x & 15u, y = threadIdx.x >> 4;
+    const uint32_t i = blockIdx.x * 16u + x;
+    auto add = [](float &m, float &s, float2 o) {
+        const float top = fmaxf(m, o.x), from = top == -INFINITY ? 0.f : top;
+        s = s * exp_f32(m - from) + o.y * exp_f32(o.x - from);
+        m = top;
+    };
+    if (blockIdx.x * 16u >= n) return;
+    float m = -INFINITY, s = 0.f;
+    if (i < n) {
+        const uint32_t each = (A.n_parts + 15) / 16, end = min(A.n_parts, (y + 1) * each);
+        for (uint32_t p = y * each; p < end; ++p) add(m, s, A.parts[(uint64_t)p * A.parts_stride + i]);
+    }
+    runs[y][x] = make_float2(m, s);
+    __syncthreads();
+    if (y || i >= n) return;
+    m = A.R.top[i]; s = A.R.sum[i];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) add(m, s, runs[k][x]);
+    A.R.top[i] = m; A.R.sum[i] = s;
+    if (!A.last) return;
+    const float lse = m + logf(s), loss = lse - A.R.label_logit[i] + A.z_weight * lse * lse;
+    A.loss[A.R.row[i]] = loss;
+    A.lse[A.R.row[i]] = lse;
+}
+// sums over one workgroup, every thread's part in fixed order
+__device__ __forceinline__ double block_sum(double v, double *lds) {
+    lds[threadIdx.x] = v;
+    __syncthreads();
+    for (uint32_t d = HD_THREADS / 2; d; d /= 2) {
+        if (threadIdx.x < d) lds[threadIdx.x] += lds[threadIdx.x + d];
+        __syncthreads();
+    }
+    return lds[0];
+}
+__global__ __launch_bounds__(HD_THREADS) void k_head_total(const JoinArgs A) {
+    __shared__ double lds[HD_THREADS];
+    double v = 0.0;
+    for (uint32_t i = threadIdx.x; i < A.R.count[0]; i += HD_THREADS) v += (double)A.R.weight[i] * (double)A.loss[A.R.row[i]];
+    v = block_sum(v, lds);
+    if (threadIdx.x == 0) *A.total = (float)v;
+}
+
+// 2^n with 2^n >= v (1 for what is no positive finite number)
+__device__ __forceinline__ float power_above(float v) {
+    if (!(v > 0.f) || !(v < 1e38f)) return 1.f;
+    int e;
+    const float m = frexpf(v, &e);
+    return ldexpf(1.f, m == 0.5f ? e - 1 : e);
+}
+// The numbers that g is made with.  room: what g's largest element may be (a power of two).
+__global__ __launch_bounds__(HD_THREADS) void k_head_info(const Rows R, const float *lse_of, float z_weight, float room) {
+    __shared__ float lds[HD_THREADS];
+    const uint32_t n = R.count[0];
+    float most = 0.f;
+    for (uint32_t i = threadIdx.x; i < n; i += HD_THREADS) {
+        const float factor = 1.f + 2.f * z_weight * lse_of[R.row[i]], v = fabsf(R.weight[i]) * fmaxf(1.f, fabsf(factor));
+        if (v < 1e38f) most = fmaxf(most, v);
+    }
+    lds[threadIdx.x] = most;
+    __syncthreads();
+    for (uint32_t d = HD_THREADS / 2; d; d /= 2) {
+        if (threadIdx.x < d) lds[threadIdx.x] = fmaxf(lds[threadIdx.x], lds[threadIdx.x + d]);
+        __syncthreads();
+    }
+    const float unit = power_above(lds[0]);
+    if (threadIdx.x == 0) R.count[1] = __float_as_uint(unit);
+    for (uint32_t i = threadIdx.x; i < n; i += HD_THREADS) {
+        const float lse = lse_of[R.row[i]], factor = 1.f + 2.f * z_weight * lse;
+        R.info[i] = RowInfo{lse, factor, room / power_above(fmaxf(1.f, fabsf(factor))), R.weight[i] / unit * room};
+    }
+}
+
+struct OutArgs {
+    Rows R;
+    Side A, B;
+    uint32_t tiles_b, bytes_k;
+    uint32_t splits;
+    float *sums;                // dx: [splits][rows][stride]
+    uint64_t stride, split_stride;
+    bool first;
+    void *out;                  // d_weight
+    uint32_t width, words;
+    const float *d_total;
+    float scale;
+};
+// dx: sums over the piece's words, one share of them a split, added to those of the pieces before
+template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_THREADS) void k_head_dx(const OutArgs A) {
+    typedef Tile<T, TA, TB, WA> Tl;
+    const uint32_t n = A.R.count[0];
+    const uint32_t split = blockIdx.x % A.splits, tile = blockIdx.x / A.splits;
+    const uint32_t a0 = tile / A.tiles_b * TA, b0 = tile % A.tiles_b * TB;
+    if (b0 >= n) return;
+    Side B = A.B;
+    B.rows = n;
+    const uint32_t steps = (A.bytes_k + GM_ROW - 1) / GM_ROW;
+    const uint32_t from = (uint32_t)((uint64_t)steps * split / A.splits), to = (uint32_t)((uint64_t)steps * (split + 1) / A.splits);
+    Tl t;
+    t.run(A.A, B, a0, b0, (uint64_t)from * GM_ROW, (to - from) * GM_ROW);
+    const uint32_t lane = threadIdx.x & 63u, a_of = a0 + Tl::wave_a() + 4 * (lane >> 4), b_of = b0 + Tl::wave_b() + (lane & 15u);
+#pragma unroll
+    for (int j = 0; j < Tl::MB; ++j)
+#pragma unroll
+        for (int i = 0; i < Tl::MA; ++i) {
+            const uint32_t a = a_of + 16 * i, b = b_of + 16 * j;
+            if (b >= n || a >= A.stride) continue;
+            Vec<float, 4> *const at = (Vec<float, 4> *)(A.sums + split * A.split_stride + (uint64_t)b * A.stride + a);
+            *at = A.first ? t.acc[i][j] : *at + t.acc[i][j];
+        }
+}
+template <typename T> __global__ __launch_bounds__(256) void k_head_dx_out(const OutArgs A, T *dx, uint64_t dx_st, uint64_t n_rows) {
+    for (uint64_t r = blockIdx.x; r < n_rows; r += gridDim.x) {
+        const int32_t i = A.R.place[r];
+        const float f = i < 0 ? 0.f : (A.d_total ? *A.d_total : 1.f) * A.scale * A.R.weight[i] / A.R.info[i].up;
+        for (uint32_t c = threadIdx.x; c < A.width; c += 256) {
+            float v = 0.f;
+            if (i >= 0)
+                for (uint32_t s = 0; s < A.splits; ++s) v += A.sums[s * A.split_stride + (uint64_t)i * A.stride + c];
+            dx[r * dx_st + c] = (T)(i < 0 ? 0.f : v * f);
+        }
+    }
+}
+template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_THREADS) void k_head_dw(const OutArgs A, float room) {
+    typedef Tile<T, TA, TB, WA> Tl;
+    constexpr uint32_t STEP = GM_ROW / sizeof(T);
+    const uint32_t n = A.R.count[0];
+    const uint32_t a0 = blockIdx.x / A.tiles_b * TA, b0 = blockIdx.x % A.tiles_b * TB;
+    Tl t;
+    t.run(A.A, A.B, a0, b0, 0, (n + STEP - 1) / STEP * GM_ROW);
+    const float f = n ? (A.d_total ? *A.d_total : 1.f) * A.scale * (__uint_as_float(A.R.count[1]) / room) : 0.f;
+    const uint32_t lane = threadIdx.x & 63u, a_of = a0 + Tl::wave_a() + 4 * (lane >> 4), b_of = b0 + Tl::wave_b() + (lane & 15u);
+#pragma unroll
+    for (int j = 0; j < Tl::MB; ++j)
+#pragma unroll
+        for (int i = 0; i < Tl::MA; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t a = a_of + 16 * i + q, b = b_of + 16 * j;
+                if (a < A.width && b < A.words) ((T *)A.out)[(uint64_t)b * A.stride + a] = (T)(n ? t.acc[i][j][q] * f : 0.f);
+            }
+}
+
+// ---- host
+struct Call {
+    const rk_head *head;
+    uint64_t n_rows;
+    uint32_t width, vocab;
+    const rk_matrix *x, *weight;
+    const int32_t *label;
+    const float *row_weight, *d_total;
+    float *loss, *lse, *total;
+    const rk_matrix *dx, *d_weight;
+    const float *given_lse;
+};
+uint64_t up_to(uint64_t v, uint64_t m) { return (v + m - 1) / m * m; }
+uint32_t blocks_of(uint64_t n) { return (uint32_t)(n < (1u << 20) ? n : 1u << 20); }
+
+template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
+    constexpr uint32_t ES = sizeof(T), STEP = GM_ROW / ES;
+    const hipStream_t stream = ctx->stream;
+    const uint32_t wide = (uint32_t)up_to(C.width, STEP);
+    const uint64_t rows_pad = up_to(C.n_rows, 256);
+    int32_t rc;
+    Rows R{};
+    {
+        char *p;
+        if ((rc = rk_scratch(ctx, SL_HEAD_ROWS, 256 + rows_pad * (7 * 4 + sizeof(RowInfo)), (void **)&p)) != RK_OK) return rc;
+        R.count = (uint32_t *)p; p += 256;
+        R.info = (RowInfo *)p; p += rows_pad * sizeof(RowInfo);
+        R.row = (int32_t *)p; p += rows_pad * 4;
+        R.place = (int32_t *)p; p += rows_pad * 4;
+        R.label = (int32_t *)p; p += rows_pad * 4;
+        R.weight = (float *)p; p += rows_pad * 4;
+        R.label_logit = (float *)p; p += rows_pad * 4;
+        R.top = (float *)p; p += rows_pad * 4;
+        R.sum = (float *)p;
+    }
+    T *xc;
+    if ((rc = rk_scratch(ctx, SL_HEAD_X, C.n_rows * wide * ES, (void **)&xc)) != RK_OK) return rc;
+    k_head_rows<<<1, HD_THREADS, 0, stream>>>(RowsArgs{R, C.label, C.row_weight, C.loss, C.lse, C.n_rows, C.vocab});
+    RK_CHECK_LAUNCH(ctx, "k_head_rows");
+    if (C.n_rows) {
+        k_head_gather<T><<<blocks_of(C.n_rows), 256, 0, stream>>>(R, (const T *)C.x->data, C.x->stride, C.width, xc, wide);
+        RK_CHECK_LAUNCH(ctx, "k_head_gather");
+    }
+    const Side X = {(const char *)xc, (uint64_t)wide * ES, 0};
+    const T *const w = (const T *)C.weight->data;
+    const uint64_t w_st = C.weight->stride;
+    // rows of W go into the product as they lie where their vectors do not straddle; others are padded first, piece by piece
+    const bool direct = ((uintptr_t)w % 16 == 0 && w_st * ES % 16 == 0 && (uint64_t)C.width * ES % 16 == 0 && w_st * ES * 256 < GM_NOWHERE);
+    const uint32_t tiles_b = (uint32_t)(rows_pad / 256);
+    const uint64_t most_tiles = (1u << 22) / (tiles_b ? tiles_b : 1);
+    const bool back = C.dx || C.d_weight;
+    // words of a piece: what the budget holds of both g, W turned around and W padded
+    uint64_t words = up_to(C.vocab, 256);
+    if (back || !direct) {
+        const uint64_t each = (back ? 2 * rows_pad * ES + (uint64_t)up_to(C.width, 256) * ES : 0) + (direct ? 0 : (uint64_t)wide * ES);
+        words = HD_BUDGET / each / 256 * 256;
+    }
+    if (words > most_tiles * 256) words = most_tiles * 256;
+    if (words < 256) words = 256;
+    if (words > up_to(C.vocab, 256)) words = up_to(C.vocab, 256);
+    T *padded = nullptr;
+    if (!direct && (rc = rk_scratch(ctx, SL_HEAD_W, words * wide * ES, (void **)&padded)) != RK_OK) return rc;
+
+    auto side_of = [&](uint32_t first, uint32_t n, Side &S) -> int32_t {
+        if (direct) {
+            S = Side{(const char *)(w + first * w_st), w_st * ES, n};
+            return RK_OK;
+        }
+        k_head_pad<T><<<blocks_of(n), 256, 0, stream>>>(w + first * w_st, w_st, n, C.width, padded, wide);
+        RK_CHECK_LAUNCH(ctx, "k_head_pad");
+        S = Side{(const char *)padded, (uint64_t)wide * ES, n};
+        return RK_OK;
+    };
+    LogitsArgs L{};
+    L.R = R; L.X = X;
+    L.bytes_k = (uint32_t)(direct ? C.width * ES : wide * ES);
+    L.tiles_b = tiles_b;
+    L.scale = C.head->logit_scale;
+
+    if (C.total) {
+        uint64_t loss_words = words;
+        const uint64_t per = rows_pad * 8;                  // a part of 128 words
+        if (loss_words / 128 * per > HD_PARTS) loss_words = HD_PARTS / per * 128 / 256 * 256;
+        if (loss_words < 256) loss_words = 256;
+        if ((rc = rk_scratch(ctx, SL_HEAD_PARTS, loss_words / 128 * per, (void **)&L.parts)) != RK_OK) return rc;
+        L.parts_stride = rows_pad;
+        JoinArgs J{R, L.parts, rows_pad, 0, false, C.head->z_weight, C.loss, C.lse, C.total, C.n_rows};
+        for (uint64_t first = 0; first < C.vocab && C.n_rows; first += loss_words) {
+            const uint32_t n = (uint32_t)(C.vocab - first < loss_words ? C.vocab - first : loss_words);
+            if ((rc = side_of((uint32_t)first, n, L.W)) != RK_OK) return rc;
+            L.first = (uint32_t)first; L.words = n;
+            const uint32_t tiles_a = (n + 255) / 256;
+            k_head_logits<T, 256, 256, 2, true><<<tiles_a * tiles_b, GM_THREADS, 0, stream>>>(L);
+            RK_CHECK_LAUNCH(ctx, "k_head_logits");
+            J.n_parts = tiles_a * 2;
+            J.last = first + n == C.vocab;
+            k_head_join<<<(uint32_t)((C.n_rows + 15) / 16), 256, 0, stream>>>(J);
+            RK_CHECK_LAUNCH(ctx, "k_head_join");
+        }
+        k_head_total<<<1, HD_THREADS, 0, stream>>>(J);
+        RK_CHECK_LAUNCH(ctx, "k_head_total");
+    }
+    if (!back) return RK_OK;
+
+    // float16 has 30 powers of two between one and its smallest: g, at most one, is moved up by fourteen
+    const float room = __is_same(T, _Float16) ? 16384.f : 1.f;
+    k_head_info<<<1, HD_THREADS, 0, stream>>>(R, C.given_lse ? C.given_lse : C.lse, C.head->z_weight, room);
+    RK_CHECK_LAUNCH(ctx, "k_head_info");
+    const uint64_t width_pad = up_to(C.width, 256);
+    T *xt = nullptr, *wt = nullptr;
+    float *sums = nullptr;
+    OutArgs O{};
+    O.R = R; O.d_total = C.d_total; O.scale = C.head->logit_scale; O.width = C.width;
+    const uint32_t tiles_w = (uint32_t)(width_pad / 256);
+    if (C.dx) {
+        if ((rc = rk_scratch(ctx, SL_HEAD_G, rows_pad * words * ES, (void **)&L.g)) != RK_OK) return rc;
+        if ((rc = rk_scratch(ctx, SL_HEAD_WT, width_pad * words * ES, (void **)&wt)) != RK_OK) return rc;
+        L.g_stride = words;
+        // as many shares of the words as fill the compute units
+        const uint64_t tiles = (uint64_t)tiles_w * (tiles_b ? tiles_b : 1);
+        O.splits = (uint32_t)(tiles >= 256 ? 1 : (256 + tiles - 1) / tiles);
+        if (O.splits > words / 1024 + 1) O.splits = (uint32_t)(words / 1024 + 1);
+        O.stride = up_to(C.width, 4);
+        O.split_stride = C.n_rows * O.stride;
+        if ((rc = rk_scratch(ctx, SL_HEAD_DX, O.splits * O.split_stride * 4, (void **)&sums)) != RK_OK) return rc;
+        O.sums = sums;
+    }
+    if (C.d_weight) {
+        if ((rc = rk_scratch(ctx, SL_HEAD_GT, rows_pad * words * ES, (void **)&L.gt)) != RK_OK) return rc;
+        if ((rc = rk_scratch(ctx, SL_HEAD_XT, rows_pad * C.width * ES, (void **)&xt)) != RK_OK) return rc;
+        L.gt_stride = rows_pad;
+        if (C.n_rows) {
+            const uint32_t tiles_c = (C.width + 63) / 64;
+            k_head_turn<T><<<(uint32_t)(rows_pad / 64 * tiles_c), 256, 0, stream>>>(xc, wide, R.count, 0, C.width, xt, rows_pad, tiles_c);
+            RK_CHECK_LAUNCH(ctx, "k_head_turn");
+        }
+    }
+    for (uint64_t first = 0; first < C.vocab; first += words) {
+        const uint32_t n = (uint32_t)(C.vocab - first < words ? C.vocab - first : words);
+        const uint32_t tiles_a = (n + 255) / 256;
+        if (C.n_rows) {
+            if ((rc = side_of((uint32_t)first, n, L.W)) != RK_OK) return rc;
+            L.first = (uint32_t)first; L.words = n;
+            k_head_logits<T, 256, 256, 2, false><<<tiles_a * tiles_b, GM_THREADS, 0, stream>>>(L);
+            RK_CHECK_LAUNCH(ctx, "k_head_logits");
+        }
+        if (C.dx && C.n_rows) {
+            const uint32_t tiles_c = (C.width + 63) / 64;
+            k_head_turn<T><<<(uint32_t)((n + 63) / 64 * tiles_c), 256, 0, stream>>>(w + first * w_st, w_st, nullptr, n, C.width, wt, words, tiles_c);
+            RK_CHECK_LAUNCH(ctx, "k_head_turn");
+            O.A = Side{(const char *)wt, words * ES, C.width};
+            O.B = Side{(const char *)L.g, words * ES, 0};
+            O.bytes_k = (uint32_t)(up_to(n, STEP) * ES);
+            O.tiles_b = tiles_b; O.first = first == 0;
+            k_head_dx<T, 256, 256, 2><<<tiles_w * tiles_b * O.splits, GM_THREADS, 0, stream>>>(O);
+            RK_CHECK_LAUNCH(ctx, "k_head_dx");
+        }
+        if (C.d_weight) {
+            OutArgs D = O;
+            D.A = Side{(const char *)xt, rows_pad * ES, C.width};
+            D.B = Side{(const char *)L.gt, rows_pad * ES, n};
+            D.tiles_b = tiles_a; D.words = n;
+            D.out = (T *)C.d_weight->data + first * C.d_weight->stride; D.stride = C.d_weight->stride;
+            k_head_dw<T, 256, 256, 2><<<tiles_w * tiles_a, GM_THREADS, 0, stream>>>(D, room);
+            RK_CHECK_LAUNCH(ctx, "k_head_dw");
+        }
+    }
+    if (C.dx && C.n_rows) {
+        k_head_dx_out<T><<<blocks_of(C.n_rows), 256, 0, stream>>>(O, (T *)C.dx->data, C.dx->stride, C.n_rows);
+        RK_CHECK_LAUNCH(ctx, "k_head_dx_out");
+    }
+    return RK_OK;
+}
+
+bool misaligned4(std::initializer_list<const void *> ps) {
+    for (const void *p : ps) if (((uintptr_t)p & 3u)) return true;
+    return false;
+}
+
+int32_t run_head(rk_ctx *ctx, const Call &C, bool loss, bool back) {
+    if (!ctx) return RK_ERR_INVALID_ARG;
+    if (!C.head || !(C.head->z_weight >= 0.f) || !(C.head->z_weight < INFINITY) || !(fabsf(C.head->logit_scale) < INFINITY) || C.head->logit_scale == 0.f)
+        return rk_fail(ctx, RK_ERR_INVALID_ARG, "head is null, its z_weight negative or not finite, or its logit_scale 0 or not finite");
+    if (C.width < 1 || C.vocab < 1) return rk_fail(ctx, RK_ERR_INVALID_ARG, "rows or the vocabulary are empty");
+    if (C.width > RK_HEAD_MAX_WIDTH || C.vocab > (1u << 28) || C.n_rows > (1ull << 20))
+        return rk_fail(ctx, RK_ERR_UNSUPPORTED, "more than 2^20 rows, 2^28 words or %u columns", RK_HEAD_MAX_WIDTH);
+    if (!rk_matrix_ok(C.x, C.n_rows, C.width) || !rk_matrix_ok(C.weight, C.vocab, C.width))
+        return rk_fail(ctx, RK_ERR_INVALID_ARG, "x or weight null, misaligned or of a stride below the width");
+    if (C.x->type != C.weight->type) return rk_fail(ctx, RK_ERR_INVALID_ARG, "weight has another type than x");
+    if ((C.n_rows && !C.label) || misaligned4({C.label, C.row_weight})) return rk_fail(ctx, RK_ERR_INVALID_ARG, "label null, or it or row_weight misaligned");
+    if (loss && ((C.n_rows && (!C.loss || !C.lse)) || !C.total || misaligned4({C.loss, C.lse, C.total})))
+        return rk_fail(ctx, RK_ERR_INVALID_ARG, "loss, lse or total null or misaligned");
+    if (back) {
+        if (!C.dx && !C.d_weight) return rk_fail(ctx, RK_ERR_INVALID_ARG, "no gradient is wanted");
+        if ((C.dx && (!rk_matrix_ok(C.dx, C.n_rows, C.width) || C.dx->type != C.x->type)) ||
+            (C.d_weight && (!rk_matrix_ok(C.d_weight, C.vocab, C.width) || C.d_weight->type != C.x->type)))
+            return rk_fail(ctx, RK_ERR_INVALID_ARG, "dx or d_weight misaligned, of a stride below the width or of another type than x");
+        if ((!loss && C.n_rows && !C.given_lse) || misaligned4({C.given_lse, C.d_total})) return rk_fail(ctx, RK_ERR_INVALID_ARG, "lse null, or it or d_total misaligned");
+    }
+    RK_HIP(ctx, hipSetDevice(ctx->device));
+    if (C.x->type == RK_F32) return run_typed<float>(ctx, C);
+    if (C.x->type == RK_BF16) return run_typed<__bf16>(ctx, C);
+    return run_typed<_Float16>(ctx, C);
+}
+
+}  // namespace
+
+extern "C" int32_t rk_head_loss(rk_ctx *ctx, const rk_head *head, uint64_t n_rows, uint32_t width, uint32_t vocab, const rk_matrix *x,
+                                const rk_matrix *weight, const int32_t *label, const float *row_weight, float *loss, float *lse,
+                                float *total) {
+    return run_head(ctx, Call{head, n_rows, width, vocab, x, weight, label, row_weight, nullptr, loss, lse, total, nullptr, nullptr, nullptr}, true, false);
+}
+
+extern "C" int32_t rk_head_backward(rk_ctx *ctx, const rk_head *head, uint64_t n_rows, uint32_t width, uint32_t vocab, const rk_matrix *x,
+                                    const rk_matrix *weight, const int32_t *label, const float *row_weight, const float *lse,
+                                    const float *d_total, const rk_matrix *dx, const rk_matrix *d_weight) {
+    return run_head(ctx, Call{head, n_rows, width, vocab, x, weight, label, row_weight, d_total, nullptr, nullptr, nullptr, dx, d_weight, lse}, false, true);
+}
+
+extern "C" int32_t rk_head_loss_backward(rk_ctx *ctx, const rk_head *head, uint64_t n_rows, uint32_t width, uint32_t vocab, const rk_matrix *x,
+                                         const rk_matrix *weight, const int32_t *label, const float *row_weight, const float *d_total,
+                                         float *loss, float *lse, float *total, const rk_matrix *dx, const rk_matrix *d_weight) {
+    return run_head(ctx, Call{head, n_rows, width, vocab, x, weight, label, row_weight, d_total, loss, lse, total, dx, d_weight, nullptr}, true, true);
+}

@@ -75,3 +75,56 @@ def test_distill_gradient():
             total = total - w[r] * 0.4 * torch.log_softmax(s[r], 0)[label[r]]
     assert torch.allclose(total, out["total"])
     assert torch.allclose(torch.autograd.grad(0.9 * total, s)[0], out["d_student"])
+
+
+@pytest.mark.parametrize("coupled", [False, True])
+def test_recurrence_gradient(coupled):
+    torch.manual_seed(3)
+    at, width = [0, 3, 3, 4, 9], 5
+    x, z = (torch.randn(9, width).double().requires_grad_() for _ in range(2))
+    bias, state = torch.randn(width).double().requires_grad_(), torch.randn(4, width).double().requires_grad_()
+    f = torch.sigmoid(z + bias)
+    rows, last = [], []
+    for s in range(4):
+        h = state[s]
+        for t in range(at[s], at[s + 1]):
+            h = f[t] * h + ((1 - f[t]) * x[t] if coupled else x[t])
+            rows.append(h)
+        last.append(h)
+    h, last = torch.stack(rows), torch.stack(last)
+    a, b = torch.randn(9, width).double(), torch.randn(4, width).double()
+    grads = torch.autograd.grad((a * h).sum() + (b * last).sum(), [x, z, bias, state])
+    out, _ = training.recurrence(*(t.detach() for t in (x, z, bias)), at, coupled, state.detach(), a, b, h.detach())
+    assert torch.allclose(out["h"], h) and torch.allclose(out["state_out"], last)
+    for name, g in zip(("dx", "dz", "d_bias", "d_state_in"), grads):
+        assert torch.allclose(out[name], g), name
+
+
+def test_recurrence_by_hand():
+    x, z = torch.tensor([[2.0], [4.0], [8.0]]).double(), torch.zeros(3, 1).double()
+    out, _ = training.recurrence(x, z, None, [0, 2, 3], True, torch.tensor([[2.0], [0.0]]).double())
+    assert out["h"][:, 0].tolist() == [2.0, 3.0, 4.0] and out["state_out"][:, 0].tolist() == [3.0, 4.0]
+    out, _ = training.recurrence(x, z, None, [0, 3], False, None)
+    assert out["h"][:, 0].tolist() == [2.0, 5.0, 10.5]
+
+
+def test_philox_of_the_published_vectors():
+    """The known answers that the authors published beside their paper: counters and keys of zeros and of ones."""
+    assert training.philox((0, 0, 0, 0), (0, 0)) == [0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8]
+    ones = 0xFFFFFFFF
+    assert training.philox((ones,) * 4, (ones,) * 2) == [0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD]
+
+
+def test_head_gradient():
+    torch.manual_seed(4)
+    x, w = torch.randn(6, 5).double().requires_grad_(), torch.randn(9, 5).double().requires_grad_()
+    label, rw = torch.tensor([0, 8, -1, 9, 4, 3]), torch.tensor([1.0, 0.5, 2.0, 1.0, 0.0, -0.7]).double()
+    out, _ = training.head(x.detach(), w.detach(), label, rw, 0.7, 0.03, 1.3)
+    total = 0.0
+    for r in (0, 1, 5):
+        l = 0.7 * w @ x[r]
+        lse = torch.logsumexp(l, 0)
+        total = total + rw[r] * (lse - l[label[r]] + 0.03 * lse ** 2)
+    assert torch.allclose(total, out["total"][0])
+    dx, dw = torch.autograd.grad(1.3 * total, [x, w])
+    assert torch.allclose(dx, out["dx"]) and torch.allclose(dw, out["d_weight"])
