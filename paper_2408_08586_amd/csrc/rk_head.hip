@@ -152,14 +152,15 @@ template <typename T, int TA, int TB, int WA, bool LOSS> __global__ __launch_bou
     X.rows = n;
     Tl t;
     t.run(A.W, X, a0, b0, 0, A.bytes_k);
-    const uint32_t lane = threadIdx.x & 63u, a_of = a0 + Tl::wave_a() + 4 * (lane >> 4), b_of = b0 + Tl::wave_b() + (lane & 15u);
+    const typename Tl::At at = Tl::place();
+    const uint32_t a_of = a0 + at.a, b_of = b0 + at.b;
+    if constexpr (LOSS) {
 #pragma unroll
-    for (int j = 0; j < Tl::MB; ++j) {
-        const uint32_t b = b_of + 16 * j;
-        const bool there = b < n;
-        const int64_t label = there ? (int64_t)A.R.label[b] - (int64_t)A.first : -1;
-        if constexpr (LOSS) {
-            float top = -INFINITY;
+        for (int j = 0; j < Tl::MB; ++j) {
+            const uint32_t b = b_of + 16 * j;
+            const bool there = b < n;
+            const int64_t label = there ? (int64_t)A.R.label[b] - (int64_t)A.first : -1;
+            float top = -INFINITY, own = 0.f;
 #pragma unroll
             for (int i = 0; i < Tl::MA; ++i)
 #pragma unroll
@@ -169,8 +170,10 @@ template <typename T, int TA, int TB, int WA, bool LOSS> __global__ __launch_bou
                     l = a < A.words ? l : -INFINITY;
                     t.acc[i][j][q] = l;
                     top = fmaxf(top, l);
-                    if (label == (int64_t)a) A.R.label_logit[b] = l;
+                    own = label == (int64_t)a ? l : own;
                 }
+            const uint32_t d = (uint32_t)(label - (int64_t)a_of);
+            if (label >= 0 && d < 16 * Tl::MA && (d & 15u) < 4) A.R.label_logit[b] = own;
             top = fmaxf(top, __shfl_xor(top, 16, 64));
             top = fmaxf(top, __shfl_xor(top, 32, 64));
             float sum = 0.f;
@@ -181,30 +184,39 @@ template <typename T, int TA, int TB, int WA, bool LOSS> __global__ __launch_bou
                 for (int q = 0; q < 4; ++q) sum += exp_of<T>(t.acc[i][j][q] - from);
             sum += __shfl_xor(sum, 16, 64);
             sum += __shfl_xor(sum, 32, 64);
-            if (there && lane < 16) A.parts[(uint64_t)((a0 + Tl::wave_a()) / (TA / WA)) * A.parts_stride + b] = make_float2(top, sum);
-        } else {
-            const RowInfo info = there ? A.R.info[b] : RowInfo{0.f, 0.f, 0.f, 0.f};
+            if (there && at.lane < 16) A.parts[(uint64_t)(a_of / (TA / WA)) * A.parts_stride + b] = make_float2(top, sum);
+        }
+    }
+    if constexpr (!LOSS) {
+        // g in place of the logits, then out in both orders, each with its own scale
+        RowInfo info[Tl::MB];
 #pragma unroll
-            for (int i = 0; i < Tl::MA; ++i) {
-                const uint32_t a = a_of + 16 * i;
-                float g[4];
+        for (int j = 0; j < Tl::MB; ++j) {
+            const uint32_t b = b_of + 16 * j;
+            const bool there = b < n;
+            const int64_t label = there ? (int64_t)A.R.label[b] - (int64_t)A.first : -1;
+            info[j] = there ? A.R.info[b] : RowInfo{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < Tl::MA; ++i)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const float p = exp_of<T>(t.acc[i][j][q] * A.scale - info.lse) * info.factor;
-                    g[q] = there && a + q < A.words ? label == (int64_t)(a + q) ? p - 1.f : p : 0.f;
+                    const uint32_t a = a_of + 16 * i + q;
+                    const float p = exp_of<T>(t.acc[i][j][q] * A.scale - info[j].lse) * info[j].factor;
+                    t.acc[i][j][q] = there && a < A.words ? label == (int64_t)a ? p - 1.f : p : 0.f;
                 }
-                if (A.g) {
-                    Vec<T, 4> v;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) v[q] = (T)(g[q] * info.up);
-                    if (there) *(Vec<T, 4> *)((T *)A.g + (uint64_t)b * A.g_stride + a) = v;
-                }
-                if (A.gt)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        if (a + q < A.words) ((T *)A.gt)[(uint64_t)(a + q) * A.gt_stride + b] = (T)(g[q] * info.share);
-            }
+            __builtin_amdgcn_sched_barrier(0);
         }
+        constexpr uint32_t EACH = 16 / sizeof(T);
+        if (A.g)
+            t.rows([&](int i, int j) { return t.acc[i][j] * info[j].up; },
+                   [&](uint32_t a, uint32_t b, const Vec<uint32_t, 4> &w) {
+                       if (b0 + b < n) *(Vec<uint32_t, 4> *)((T *)A.g + (uint64_t)(b0 + b) * A.g_stride + a0 + a) = w;
+                   });
+        if (A.gt)
+            t.columns([&](int i, int j) { return t.acc[i][j] * info[j].share; },
+                      [&](uint32_t a, uint32_t b, const Vec<uint32_t, 4> &w) {
+                          if (a0 + a < A.words) *(Vec<uint32_t, 4> *)((T *)A.gt + (uint64_t)(a0 + a) * A.gt_stride + b0 + b) = w;
+                      });
     }
 }
 
@@ -304,6 +316,7 @@ struct OutArgs {
     uint64_t stride, split_stride;
     bool first;
     void *out;                  // d_weight
+    bool aligned;               // its rows take whole vectors
     uint32_t width, words;
     const float *d_total;
     float scale;
@@ -321,15 +334,16 @@ template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_TH
     const uint32_t from = (uint32_t)((uint64_t)steps * split / A.splits), to = (uint32_t)((uint64_t)steps * (split + 1) / A.splits);
     Tl t;
     t.run(A.A, B, a0, b0, (uint64_t)from * GM_ROW, (to - from) * GM_ROW);
-    const uint32_t lane = threadIdx.x & 63u, a_of = a0 + Tl::wave_a() + 4 * (lane >> 4), b_of = b0 + Tl::wave_b() + (lane & 15u);
+    const typename Tl::At at = Tl::place();
+    const uint32_t a_of = a0 + at.a, b_of = b0 + at.b;
 #pragma unroll
     for (int j = 0; j < Tl::MB; ++j)
 #pragma unroll
         for (int i = 0; i < Tl::MA; ++i) {
             const uint32_t a = a_of + 16 * i, b = b_of + 16 * j;
             if (b >= n || a >= A.stride) continue;
-            Vec<float, 4> *const at = (Vec<float, 4> *)(A.sums + split * A.split_stride + (uint64_t)b * A.stride + a);
-            *at = A.first ? t.acc[i][j] : *at + t.acc[i][j];
+            Vec<float, 4> *const to = (Vec<float, 4> *)(A.sums + split * A.split_stride + (uint64_t)b * A.stride + a);
+            *to = A.first ? t.acc[i][j] : *to + t.acc[i][j];
         }
 }
 template <typename T> __global__ __launch_bounds__(256) void k_head_dx_out(const OutArgs A, T *dx, uint64_t dx_st, uint64_t n_rows) {
@@ -352,16 +366,21 @@ template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_TH
     Tl t;
     t.run(A.A, A.B, a0, b0, 0, (n + STEP - 1) / STEP * GM_ROW);
     const float f = n ? (A.d_total ? *A.d_total : 1.f) * A.scale * (__uint_as_float(A.R.count[1]) / room) : 0.f;
-    const uint32_t lane = threadIdx.x & 63u, a_of = a0 + Tl::wave_a() + 4 * (lane >> 4), b_of = b0 + Tl::wave_b() + (lane & 15u);
+    constexpr uint32_t EACH = 16 / sizeof(T);
+    T *const out = (T *)A.out;
+    const bool whole = A.aligned && a0 + TA <= A.width;
+    t.rows([&](int i, int j) { return n ? t.acc[i][j] * f : Vec<float, 4>(0.f); },
+           [&](uint32_t a, uint32_t b, const Vec<uint32_t, 4> &w) {
+               if (b0 + b >= A.words) return;
+               T *const to = out + (uint64_t)(b0 + b) * A.stride + a0 + a;
+               if (whole) {
+                   __builtin_nontemporal_store(w, (Vec<uint32_t, 4> *)to);
+               } else {
+                   const Vec<T, EACH> v = __builtin_bit_cast(Vec<T, EACH>, w);
 #pragma unroll
-    for (int j = 0; j < Tl::MB; ++j)
-#pragma unroll
-        for (int i = 0; i < Tl::MA; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint32_t a = a_of + 16 * i + q, b = b_of + 16 * j;
-                if (a < A.width && b < A.words) ((T *)A.out)[(uint64_t)b * A.stride + a] = (T)(n ? t.acc[i][j][q] * f : 0.f);
-            }
+                   for (uint32_t e = 0; e < EACH; ++e) if (a0 + a + e < A.width) to[e] = v[e];
+               }
+           });
 }
 
 // ---- host
@@ -526,6 +545,7 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
             D.A = Side{(const char *)xt, rows_pad * ES, C.width};
             D.B = Side{(const char *)L.gt, rows_pad * ES, n};
             D.tiles_b = tiles_a; D.words = n;
+            D.aligned = (uintptr_t)C.d_weight->data % 16 == 0 && C.d_weight->stride * ES % 16 == 0;
             D.out = (T *)C.d_weight->data + first * C.d_weight->stride; D.stride = C.d_weight->stride;
             k_head_dw<T, 256, 256, 2><<<tiles_w * tiles_a, GM_THREADS, 0, stream>>>(D, room);
             RK_CHECK_LAUNCH(ctx, "k_head_dw");
