@@ -79,6 +79,7 @@ enum {
     SL_DISTILL_PARTS,                                    // distillation: the sums of the rows' slices
     SL_HEAD_ROWS, SL_HEAD_X, SL_HEAD_XT, SL_HEAD_W, SL_HEAD_WT, SL_HEAD_PARTS, SL_HEAD_G, SL_HEAD_GT, SL_HEAD_DX,   // head: the rows that count; they and a
                                                          // piece of the weights, padded or turned around; sums of tiles; the logits' gradients; sums of dx
+    SL_RECUR_CHAIN, SL_RECUR_BIAS,                       // recurrence: what its tiles tell each other; their sums of the bias's gradient
     SL_COUNT
 };
 static_assert(SL_COUNT <= RK_SCRATCH_SLOTS, "more scratch slots than the context holds");

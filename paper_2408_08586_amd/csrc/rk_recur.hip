@@ -1,11 +1,22 @@
 // Gated linear recurrence over packed sequences, and its gradient (rk_recur in rubick.h).
 //
-// The simplest form: a lane has a column and goes through all rows of it, one after the other.
+// Both directions are chains v <- p v + q, forward over h, backward over what a row hands to the one before it.  The rows are cut into tiles of
+// RC_WAVES x L rows and 128 columns, a workgroup each: a wavefront has L rows, a lane two columns, and reads them once.  It takes
+// its rows as one step (the product of their p, and q from nothing), the workgroup joins its wavefronts' steps, tells the tiles behind
+// it what it makes of a value that comes in, finds the value that comes in to itself from the tiles before it, and goes through its rows again,
+// in registers, for the results.
+//
+// What a tile says is one 64-bit word a column (p and q), readable as soon as it is no longer all ones, so that words need no flags or fences beside them.
+// A tile joins the words of at most RC_BLOCK - 1 tiles before it, in order, with the value behind the last block of RC_BLOCK tiles, which that block's
+// last tile writes: always the same sums in the same order.  Tiles are handed out by a counter, earlier ones first: who
+// waits, waits for workgroups that run already.  A tile whose first row begins a sequence waits for nobody, and nobody
+// looks behind the beginning of a sequence, so that nothing of one sequence comes near another.
 #include "rk_vec.h"
 
 namespace {
 
-constexpr uint32_t RC_THREADS = 64;
+constexpr uint32_t RC_WAVES = 8, RC_THREADS = 64 * RC_WAVES, RC_COLS = 128, RC_BLOCK = 16;
+constexpr uint32_t RC_FORWARD_ROWS = 16, RC_BACK_ROWS = 8;      // of a wavefront
 
 struct RecurArgs {
     const void *x, *z, *h, *dh, *bias;
@@ -15,74 +26,370 @@ struct RecurArgs {
     float *state_out, *d_state_in, *d_bias;
     uint64_t si_st, so_st, dso_st, dsi_st;
     const int32_t *offsets;
-    uint64_t seq_rows, n_rows;
+    uint32_t seq_rows, n_rows;
     uint32_t n_seqs, width, coupled, bias_type;
+    uint32_t n_tiles, n_cols;       // tiles of rows; of columns
+    uint32_t *ticket;               // null: there is one tile of rows
+    uint64_t *steps;                // [n_tiles][width]: p and q
+    uint32_t *behind;               // [n_tiles / RC_BLOCK][width]: the value behind a block of tiles
+    float *bias_parts;              // [n_tiles][width]
+    uint32_t idle;                  // workgroups that look for sequences without rows
 };
 
+// ---- a lane's two columns
+template <typename T> using Two = Words<T, 2>;
+template <typename T> using LooseTwo = Two<T> __attribute__((aligned(sizeof(T))));
+struct Columns {
+    uint32_t at;                    // where it reads: both elements are inside the row
+    bool two, one, cut_here;        // writes both; the first alone, which it has read as the second; some lane of the wavefront does
+    bool single;                    // rows have one element
+    __device__ __forceinline__ Columns(uint32_t c, uint32_t width) {
+        two = c + 1 < width; one = c + 1 == width; single = width == 1;
+        at = two ? c : one && !single ? width - 2 : 0;
+        cut_here = width % 2 && __builtin_amdgcn_ballot_w64(one) != 0;
+    }
+};
+template <typename T> __device__ __forceinline__ Two<T> read_two(const T *row, const Columns &c) {
+    if (c.single) {
+        Vec<T, 2> v = (T)0.f;
+        v[0] = row[0];
+        return __builtin_bit_cast(Two<T>, v);
+    }
+    return __builtin_nontemporal_load((const LooseTwo<T> *)(row + c.at));
+}
+template <typename T> __device__ __forceinline__ Vec<float, 2> floats(Two<T> w, const Columns &c) {
+    Vec<float, 2> v;
+    v[0] = element<T>(w, 0); v[1] = element<T>(w, 1);
+    if (c.cut_here) v[0] = c.one && !c.single ? v[1] : v[0];
+    return v;
+}
+template <typename T> __device__ __forceinline__ void write_two(T *row, const Columns &c, uint32_t first, Vec<float, 2> f) {
+    Vec<T, 2> v;
+    v[0] = (T)f[0]; v[1] = (T)f[1];
+    if (c.two) __builtin_nontemporal_store(__builtin_bit_cast(Two<T>, v), (LooseTwo<T> *)(row + first));
+    if (c.cut_here) { if (c.one) row[first] = v[0]; }
+}
+__device__ __forceinline__ Vec<float, 2> read_state(const float *states, uint64_t stride, uint32_t seq, const Columns &c) {
+    return floats<float>(read_two<float>(states + seq * stride, c), c);
+}
 __device__ __forceinline__ float bias_at(const RecurArgs &A, uint32_t c) {
-    if (!A.bias) return 0.f;
+    if (!A.bias || c >= A.width) return 0.f;
     if (A.bias_type == RK_F32) return ((const float *)A.bias)[c];
     return A.bias_type == RK_BF16 ? (float)((const __bf16 *)A.bias)[c] : (float)((const _Float16 *)A.bias)[c];
 }
+
 // f = sigmoid(v) and 1 - f, neither as a difference from one
 struct Gate { float f, not_f; };
-__device__ __forceinline__ Gate gate_of(float v) {
-    const float e = exp_f32(-fabsf(v)), near = 1.f / (1.f + e), far = e * near;
-    return v >= 0.f ? Gate{near, far} : Gate{v != v ? v : far, v != v ? v : near};
+template <typename T> __device__ __forceinline__ Gate gate_of(float v) {
+    const float a = fabsf(v), e = sizeof(T) == 4 ? exp_f32(-a) : __builtin_amdgcn_exp2f(a * -1.4426950408889634f);
+    const float near = __builtin_amdgcn_rcpf(1.f + e), far = e * near;
+    const bool up = v >= 0.f;
+    return Gate{up ? near : far, up ? far : near};
 }
-__device__ __forceinline__ void seq_range(const RecurArgs &A, uint32_t s, uint64_t &first, uint64_t &end) {
+
+// ---- which rows of a wavefront begin and end sequences
+struct Marks {
+    uint32_t live, first, last;     // a bit a row
+    int32_t seq, begin, end;        // of lane i: of row i
+};
+// L rows from row0 on; rows that no sequence has are not live.  Offsets that are no offsets lead nowhere outside the rows.
+template <int L> __device__ __forceinline__ Marks marks_of(const RecurArgs &A, uint32_t row0) {
+    const uint32_t lane = threadIdx.x & 63u, row = row0 + lane;
+    Marks m{0, 0, 0, 0, 0, 0};
+    bool live = lane < L && row < A.n_rows;
     if (A.offsets) {
-        const int64_t a = A.offsets[s], b = A.offsets[s + 1];
-        first = a < 0 ? 0 : (uint64_t)a;
-        end = b < 0 ? 0 : (uint64_t)b < A.n_rows ? (uint64_t)b : A.n_rows;
-    } else {
-        first = s * A.seq_rows;
-        end = first + A.seq_rows < A.n_rows ? first + A.seq_rows : A.n_rows;
-    }
-}
-
-template <typename T> __global__ __launch_bounds__(RC_THREADS) void k_recur_forward(const RecurArgs A) {
-    const uint32_t c = blockIdx.x * RC_THREADS + threadIdx.x;
-    if (c >= A.width) return;
-    const float bias = bias_at(A, c);
-    for (uint32_t s = 0; s < A.n_seqs; ++s) {
-        uint64_t first, end;
-        seq_range(A, s, first, end);
-        float h = A.state_in ? A.state_in[s * A.si_st + c] : 0.f;
-        for (uint64_t t = first; t < end; ++t) {
-            const Gate g = gate_of((float)((const T *)A.z)[t * A.z_st + c] + bias);
-            const float x = (float)((const T *)A.x)[t * A.x_st + c];
-            h = g.f * h + (A.coupled ? g.not_f * x : x);
-            ((T *)A.out)[t * A.o_st + c] = (T)h;
+        if (live) {
+            // the last sequence that begins at this row or before it
+            int32_t lo = -1, hi = (int32_t)A.n_seqs + 1;
+            while (hi - lo > 1) {
+                const int32_t mid = lo + (hi - lo) / 2;
+                if (A.offsets[mid] <= (int32_t)row) lo = mid; else hi = mid;
+            }
+            live = lo >= 0 && lo < (int32_t)A.n_seqs;
+            if (live) {
+                m.seq = lo;
+                m.begin = max(A.offsets[lo], 0);
+                m.end = min(A.offsets[lo + 1], (int32_t)A.n_rows);
+            }
         }
-        if (A.state_out) A.state_out[s * A.so_st + c] = h;
+    } else if (live) {
+        m.seq = (int32_t)(row / A.seq_rows);
+        m.begin = m.seq * (int32_t)A.seq_rows;
+        m.end = (int32_t)(A.n_rows - (uint32_t)m.begin < A.seq_rows ? A.n_rows : (uint32_t)m.begin + A.seq_rows);
     }
+    m.live = (uint32_t)__builtin_amdgcn_ballot_w64(live);
+    m.first = (uint32_t)__builtin_amdgcn_ballot_w64(live && (int32_t)row == m.begin);
+    m.last = (uint32_t)__builtin_amdgcn_ballot_w64(live && (int32_t)row + 1 == m.end);
+    return m;
+}
+__device__ __forceinline__ uint32_t of_row(int32_t v, int i) { return (uint32_t)__builtin_amdgcn_readlane(v, i); }
+
+// ---- chains
+struct Link { Vec<float, 2> p, q; };            // v -> p v + q
+__device__ __forceinline__ uint32_t not_all_ones(float v) {
+    const uint32_t w = __float_as_uint(v);
+    return w == 0xFFFFFFFFu ? 0x7FC00000u : w;  // (one NaN for another)
+}
+struct Lds {
+    Vec<float, 2> p[RC_WAVES][64], q[RC_WAVES][64];
+    uint32_t cuts;                              // wavefronts in which a chain begins
+    uint32_t ticket;
+};
+// The value that comes in to this wavefront's rows.  order: its place in the direction of the chain; cut: a chain begins in its rows; needs: its
+// tile's first row goes on with a chain that began in tile `from` (tiles counted in the direction of the chain).
+__device__ __forceinline__ Vec<float, 2> join(const RecurArgs &A, Lds &lds, uint32_t order, const Link &own, bool cut, uint32_t tile, uint32_t column, bool needs, uint32_t from) {
+    const uint32_t lane = threadIdx.x & 63u;
+    lds.p[order][lane] = own.p;
+    lds.q[order][lane] = own.q;
+    if (lane == 0 && cut) atomicOr(&lds.cuts, 1u << order);
+    __syncthreads();
+    const uint32_t cuts = lds.cuts;
+    Vec<float, 2> p = 1.f, q = 0.f;
+    for (uint32_t w = 0; w < order; ++w) {
+        const Vec<float, 2> pw = lds.p[w][lane], qw = lds.q[w][lane];
+        if (cuts >> w & 1u) { p = 0.f; q = qw; }
+        else { q = pw * q + qw; p = p * pw; }
+    }
+    if (!A.ticket) return q;                    // (nothing comes in to the only tile)
+    if (order == RC_WAVES - 1) {                // what the tile makes of a value
+        const Vec<float, 2> to_p = cuts ? Vec<float, 2>(0.f) : p * own.p, to_q = cut ? own.q : own.p * q + own.q;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (column + i < A.width)
+                __hip_atomic_store(A.steps + (uint64_t)tile * A.width + column + i, (uint64_t)not_all_ones(to_q[i]) << 32 | not_all_ones(to_p[i]),
+                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    Vec<float, 2> in = 0.f;
+    if (needs) {
+        const uint32_t block = tile / RC_BLOCK * RC_BLOCK, begin = from > block ? from : block, n = tile - begin;
+        // the tiles before this one, a run of them a wavefront, and the value behind the block before
+        const uint32_t a = begin + n * order / RC_WAVES, b = begin + n * (order + 1) / RC_WAVES;
+        Vec<float, 2> jp = 1.f, jq = 0.f, before = 0.f;
+        for (uint32_t t = a; t < b; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                if (column + i >= A.width) continue;
+                uint64_t word;
+                while ((word = __hip_atomic_load(A.steps + (uint64_t)t * A.width + column + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) == ~0ull)
+                    __builtin_amdgcn_s_sleep(1);
+                const float tp = __uint_as_float((uint32_t)word), tq = __uint_as_float((uint32_t)(word >> 32));
+                jq[i] = tp * jq[i] + tq;
+                jp[i] *= tp;
+            }
+        if (from < block)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                if (column + i >= A.width) continue;
+                uint32_t word;
+                while ((word = __hip_atomic_load(A.behind + (uint64_t)(tile / RC_BLOCK - 1) * A.width + column + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) == ~0u)
+                    __builtin_amdgcn_s_sleep(1);
+                before[i] = __uint_as_float(word);
+            }
+        in = before;
+        __syncthreads();                        // (needs is the same for the whole workgroup)
+        lds.p[order][lane] = jp;
+        lds.q[order][lane] = jq;
+        __syncthreads();
+#pragma unroll
+        for (uint32_t w = 0; w < RC_WAVES; ++w) in = lds.p[w][lane] * in + lds.q[w][lane];
+    }
+    return cuts & ((1u << order) - 1u) ? q : p * in + q;
+}
+// the value behind the tile, if it is a block's last
+__device__ __forceinline__ void tell(const RecurArgs &A, uint32_t order, uint32_t tile, uint32_t column, const Vec<float, 2> &v) {
+    if (!A.ticket || order != RC_WAVES - 1 || tile % RC_BLOCK != RC_BLOCK - 1) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (column + i < A.width)
+            __hip_atomic_store(A.behind + (uint64_t)(tile / RC_BLOCK) * A.width + column + i, not_all_ones(v[i]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// Which tile a workgroup has; false: none, it looked for sequences without rows instead, whose state goes from one end to the other.
+__device__ __forceinline__ bool take(const RecurArgs &A, Lds &lds, const float *from, uint64_t from_st, float *to, uint64_t to_st, uint32_t &tile, uint32_t &column_tile) {
+    if (threadIdx.x == 0) {
+        lds.cuts = 0;
+        lds.ticket = A.ticket ? atomicAdd(A.ticket, 1u) : blockIdx.x;
+    }
+    __syncthreads();
+    const uint32_t t = lds.ticket, tiles = A.n_tiles * A.n_cols;
+    if (t < tiles) {
+        tile = t / A.n_cols;
+        column_tile = t % A.n_cols;
+        return true;
+    }
+    for (uint32_t s = (t - tiles) * RC_WAVES + (threadIdx.x >> 6); s < A.n_seqs; s += A.idle * RC_WAVES) {
+        const bool none = A.offsets ? A.offsets[s + 1] <= A.offsets[s] : A.n_rows == 0;
+        if (none)
+            for (uint32_t c = threadIdx.x & 63u; c < A.width; c += 64) to[s * to_st + c] = from ? from[s * from_st + c] : 0.f;
+    }
+    return false;
 }
 
-template <typename T> __global__ __launch_bounds__(RC_THREADS) void k_recur_backward(const RecurArgs A) {
-    const uint32_t c = blockIdx.x * RC_THREADS + threadIdx.x;
-    if (c >= A.width) return;
-    const float bias = bias_at(A, c);
-    float sum = 0.f;
-    for (uint32_t s = 0; s < A.n_seqs; ++s) {
-        uint64_t first, end;
-        seq_range(A, s, first, end);
-        const float before = A.state_in ? A.state_in[s * A.si_st + c] : 0.f;
-        float carry = A.d_state_out ? A.d_state_out[s * A.dso_st + c] : 0.f;
-        for (uint64_t t = end; t-- > first;) {
-            const Gate g = gate_of((float)((const T *)A.z)[t * A.z_st + c] + bias);
-            const float x = A.coupled ? (float)((const T *)A.x)[t * A.x_st + c] : 0.f;
-            const float h = t > first ? (float)((const T *)A.h)[(t - 1) * A.h_st + c] : before;
-            const float e = (float)((const T *)A.dh)[t * A.dh_st + c] + carry;
-            const float dz = e * (h - x) * (g.f * g.not_f);
-            carry = g.f * e;
+template <typename T> __global__ __launch_bounds__(RC_THREADS, 4) void k_recur_forward(const RecurArgs A) {
+    __shared__ Lds lds;
+    constexpr int L = RC_FORWARD_ROWS;
+    uint32_t tile, column_tile;
+    if (!take(A, lds, A.state_in, A.si_st, A.state_out, A.so_st, tile, column_tile)) return;
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t column = column_tile * RC_COLS + 2 * lane, tile0 = tile * RC_WAVES * L, row0 = tile0 + wave * L;
+    const Columns c(column, A.width);
+    Two<T> z[L], x[L];
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+        z[i] = 0u; x[i] = 0u;
+        if (row0 + i < A.n_rows) {
+            z[i] = read_two<T>((const T *)A.z + (uint64_t)(row0 + i) * A.z_st, c);
+            x[i] = read_two<T>((const T *)A.x + (uint64_t)(row0 + i) * A.x_st, c);
+        }
+    }
+    const Marks m = marks_of<L>(A, row0);
+    Vec<float, 2> bias;
+    bias[0] = bias_at(A, column); bias[1] = bias_at(A, column + 1);
+    Vec<float, 2> f[L], q[L], state[L];
+    if (m.first && A.state_in)
+#pragma unroll
+        for (int i = 0; i < L; ++i) if (m.first >> i & 1u) state[i] = read_state(A.state_in, A.si_st, of_row(m.seq, i), c);
+    Link own;
+    own.p = 1.f; own.q = 0.f;
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+        const Vec<float, 2> zi = floats<T>(z[i], c) + bias, xi = floats<T>(x[i], c);
+        const bool live = m.live >> i & 1u, first = m.first >> i & 1u;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const Gate g = gate_of<T>(zi[k]);
+            f[i][k] = live ? g.f : 1.f;
+            q[i][k] = live ? A.coupled ? g.not_f * xi[k] : xi[k] : 0.f;
+        }
+        if (first) {
+            if (A.state_in) q[i] += f[i] * state[i];
+            own.p = 0.f; own.q = q[i];
+        } else {
+            own.p *= f[i];
+            own.q = f[i] * own.q + q[i];
+        }
+    }
+    // how the tile's first row goes on
+    const bool needs = wave == 0 && (m.live & 1u) && !(m.first & 1u);
+    __shared__ uint32_t from;
+    if (threadIdx.x == 0) from = needs ? of_row(m.begin, 0) / (RC_WAVES * L) : ~0u;
+    __syncthreads();
+    Vec<float, 2> h = join(A, lds, wave, own, m.first != 0, tile, column, from != ~0u, from);
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+        const bool first = m.first >> i & 1u;
+        h = first ? q[i] : f[i] * h + q[i];
+        if (m.live >> i & 1u) {
+            write_two<T>((T *)A.out + (uint64_t)(row0 + i) * A.o_st, c, column, h);
+            if (A.state_out && (m.last >> i & 1u)) write_two<float>(A.state_out + of_row(m.seq, i) * A.so_st, c, column, h);
+        }
+    }
+    tell(A, wave, tile, column, h);
+}
+
+template <typename T> __global__ __launch_bounds__(RC_THREADS, 4) void k_recur_backward(const RecurArgs A) {
+    __shared__ Lds lds;
+    constexpr int L = RC_BACK_ROWS;
+    uint32_t tile, column_tile;                     // (counted from the last rows)
+    if (!take(A, lds, A.d_state_out, A.dso_st, A.d_state_in, A.dsi_st, tile, column_tile)) return;
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t column = column_tile * RC_COLS + 2 * lane, row_tile = A.n_tiles - 1 - tile, row0 = (row_tile * RC_WAVES + wave) * L;
+    const Columns c(column, A.width);
+    Two<T> z[L], x[L], h[L], dh[L];
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+        z[i] = 0u; x[i] = 0u; h[i] = 0u; dh[i] = 0u;
+        if (row0 + i < A.n_rows) {
+            z[i] = read_two<T>((const T *)A.z + (uint64_t)(row0 + i) * A.z_st, c);
+            dh[i] = read_two<T>((const T *)A.dh + (uint64_t)(row0 + i) * A.dh_st, c);
+            if (A.coupled) x[i] = read_two<T>((const T *)A.x + (uint64_t)(row0 + i) * A.x_st, c);
+            if (row0 + i) h[i] = read_two<T>((const T *)A.h + (uint64_t)(row0 + i - 1) * A.h_st, c);
+        }
+    }
+    const Marks m = marks_of<L>(A, row0);
+    Vec<float, 2> bias;
+    bias[0] = bias_at(A, column); bias[1] = bias_at(A, column + 1);
+    Vec<float, 2> state[L], d_state[L];
+    if (m.first && A.state_in)
+#pragma unroll
+        for (int i = 0; i < L; ++i) if (m.first >> i & 1u) state[i] = read_state(A.state_in, A.si_st, of_row(m.seq, i), c);
+    if (m.last && A.d_state_out)
+#pragma unroll
+        for (int i = 0; i < L; ++i) if (m.last >> i & 1u) d_state[i] = read_state(A.d_state_out, A.dso_st, of_row(m.seq, i), c);
+    Vec<float, 2> f[L], not_f[L], of[L], e[L];
+    Link own;
+    own.p = 1.f; own.q = 0.f;
+#pragma unroll
+    for (int i = L - 1; i >= 0; --i) {
+        const bool live = m.live >> i & 1u, last = m.last >> i & 1u;
+        const Vec<float, 2> zi = floats<T>(z[i], c) + bias;
+        of[i] = floats<T>(h[i], c);
+        if (m.first >> i & 1u) of[i] = A.state_in ? state[i] : Vec<float, 2>(0.f);
+        of[i] -= floats<T>(x[i], c);
+        e[i] = floats<T>(dh[i], c);
+        if (last && A.d_state_out) e[i] += d_state[i];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const Gate g = gate_of<T>(zi[k]);
+            f[i][k] = live ? g.f : 1.f;
+            not_f[i][k] = g.not_f;
+            e[i][k] = live ? e[i][k] : 0.f;
+        }
+        if (last) { own.p = 0.f; own.q = f[i] * e[i]; }
+        else { own.p *= f[i]; own.q = f[i] * (e[i] + own.q); }
+    }
+    const uint32_t order = RC_WAVES - 1 - wave;
+    __shared__ uint32_t from;
+    // how the tile's last row goes on; a tile of the matrix's end is cut short there, and nothing comes in to it
+    if (threadIdx.x == RC_THREADS - 64) {
+        const bool needs = (m.live >> (L - 1) & 1u) && !(m.last >> (L - 1) & 1u);
+        from = needs ? A.n_tiles - 1 - (of_row(m.end, L - 1) - 1) / (RC_WAVES * L) : ~0u;
+    }
+    __syncthreads();
+    Vec<float, 2> carry = join(A, lds, order, own, m.last != 0, tile, column, from != ~0u, from), sum = 0.f;
+#pragma unroll
+    for (int i = L - 1; i >= 0; --i) {
+        const bool last = m.last >> i & 1u, live = m.live >> i & 1u;
+        const Vec<float, 2> now = last ? e[i] : e[i] + carry, dz = now * of[i] * (f[i] * not_f[i]);
+        carry = f[i] * now;
+        if (live) {
             sum += dz;
-            ((T *)A.dx)[t * A.dx_st + c] = (T)(A.coupled ? g.not_f * e : e);
-            ((T *)A.dz)[t * A.dz_st + c] = (T)dz;
+            write_two<T>((T *)A.dx + (uint64_t)(row0 + i) * A.dx_st, c, column, A.coupled ? not_f[i] * now : now);
+            write_two<T>((T *)A.dz + (uint64_t)(row0 + i) * A.dz_st, c, column, dz);
+            if (A.d_state_in && (m.first >> i & 1u)) write_two<float>(A.d_state_in + of_row(m.seq, i) * A.dsi_st, c, column, carry);
         }
-        if (A.d_state_in) A.d_state_in[s * A.dsi_st + c] = carry;
     }
-    if (A.d_bias) A.d_bias[c] = sum;
+    tell(A, order, tile, column, carry);
+    if (!A.d_bias) return;
+    __syncthreads();
+    lds.p[wave][lane] = sum;
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (uint32_t w = 1; w < RC_WAVES; ++w) sum += lds.p[w][lane];
+    float *const to = A.ticket ? A.bias_parts + (uint64_t)tile * A.width : A.d_bias;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) if (column + k < A.width) to[column + k] = sum[k];
+}
+
+// sixteen runs of tiles a column, joined in fixed order
+__global__ __launch_bounds__(1024) void k_recur_bias(const float *parts, uint32_t n_tiles, uint32_t width, float *d_bias) {
+    __shared__ float lds[16][64];
+    const uint32_t lane = threadIdx.x & 63u, run = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+    float sum = 0.f;
+    if (c < width) {
+        const uint32_t end = (uint32_t)((uint64_t)n_tiles * (run + 1) / 16);
+        for (uint32_t t = (uint32_t)((uint64_t)n_tiles * run / 16); t < end; ++t) sum += parts[(uint64_t)t * width + c];
+    }
+    lds[run][lane] = sum;
+    __syncthreads();
+    if (run || c >= width) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) sum += lds[i][lane];
+    d_bias[c] = sum;
+}
+__global__ __launch_bounds__(256) void k_recur_clear(uint64_t *words, uint64_t n, uint32_t *ticket) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) words[i] = ~0ull;
 }
 
 template <typename F> void with_type(uint32_t type, F f) {
@@ -108,8 +415,28 @@ void fill_recur(RecurArgs &A, const rk_recur *r, uint64_t n_rows, uint32_t width
     A.z = z->data; A.z_st = z->stride;
     A.bias = r->bias; A.bias_type = r->param_type;
     A.offsets = r->offsets;
-    A.seq_rows = r->seq_rows && r->seq_rows < n_rows ? r->seq_rows : n_rows;
-    A.n_rows = n_rows; A.n_seqs = (uint32_t)n_seqs; A.width = width; A.coupled = r->coupled;
+    A.seq_rows = (uint32_t)(r->seq_rows && r->seq_rows < n_rows ? r->seq_rows : n_rows);
+    A.n_rows = (uint32_t)n_rows; A.n_seqs = (uint32_t)n_seqs; A.width = width; A.coupled = r->coupled;
+}
+// tiles of tile_rows rows, and what their chains need; the number of workgroups
+int32_t tiles_of(rk_ctx *ctx, RecurArgs &A, uint32_t tile_rows, bool states, uint64_t &blocks) {
+    A.n_tiles = (uint32_t)(((uint64_t)A.n_rows + tile_rows - 1) / tile_rows);
+    A.n_cols = (A.width + RC_COLS - 1) / RC_COLS;
+    // (of sequences without rows there is only the state to be taken along)
+    A.idle = states && (A.offsets || A.n_rows == 0) ? (A.n_seqs / RC_WAVES < 1024 ? A.n_seqs / RC_WAVES + 1 : 1024) : 0;
+    blocks = (uint64_t)A.n_tiles * A.n_cols + A.idle;
+    if (blocks > RK_LAUNCH_THREADS / RC_THREADS) return rk_fail(ctx, RK_ERR_UNSUPPORTED, "2^22 tiles of %u rows and %u columns or more", tile_rows, RC_COLS);
+    if (A.n_tiles < 2) return RK_OK;
+    const uint64_t words = (uint64_t)A.n_tiles * A.width, after = ((uint64_t)(A.n_tiles / RC_BLOCK) * A.width + 1) / 2;
+    int32_t rc = rk_scratch(ctx, SL_RECUR_CHAIN, (words + after + 1) * 8, (void **)&A.steps);
+    if (rc != RK_OK) return rc;
+    A.behind = (uint32_t *)(A.steps + words);
+    A.ticket = (uint32_t *)(A.steps + words + after);
+    if (A.d_bias && (rc = rk_scratch(ctx, SL_RECUR_BIAS, words * 4, (void **)&A.bias_parts)) != RK_OK) return rc;
+    const uint64_t clear = (words + after + 1023) / 1024;
+    k_recur_clear<<<(uint32_t)(clear < 2048 ? clear : 2048), 256, 0, ctx->stream>>>(A.steps, words + after, A.ticket);
+    RK_CHECK_LAUNCH(ctx, "k_recur_clear");
+    return RK_OK;
 }
 
 }  // namespace
@@ -132,9 +459,9 @@ extern "C" int32_t rk_recur_forward(rk_ctx *ctx, const rk_recur *recur, uint64_t
     A.out = h->data; A.o_st = h->stride;
     if (state_in) { A.state_in = (const float *)state_in->data; A.si_st = state_in->stride; }
     if (state_out) { A.state_out = (float *)state_out->data; A.so_st = state_out->stride; }
-    with_type(z->type, [&](auto t) {
-        k_recur_forward<decltype(t)><<<(width + RC_THREADS - 1) / RC_THREADS, RC_THREADS, 0, ctx->stream>>>(A);
-    });
+    uint64_t blocks;
+    if ((rc = tiles_of(ctx, A, RC_WAVES * RC_FORWARD_ROWS, state_out != nullptr, blocks)) != RK_OK) return rc;
+    with_type(z->type, [&](auto t) { k_recur_forward<decltype(t)><<<(uint32_t)blocks, RC_THREADS, 0, ctx->stream>>>(A); });
     RK_CHECK_LAUNCH(ctx, "k_recur_forward");
     return RK_OK;
 }
@@ -166,9 +493,15 @@ extern "C" int32_t rk_recur_backward(rk_ctx *ctx, const rk_recur *recur, uint64_
     if (d_state_out) { A.d_state_out = (const float *)d_state_out->data; A.dso_st = d_state_out->stride; }
     if (d_state_in) { A.d_state_in = (float *)d_state_in->data; A.dsi_st = d_state_in->stride; }
     A.d_bias = d_bias;
-    with_type(z->type, [&](auto t) {
-        k_recur_backward<decltype(t)><<<(width + RC_THREADS - 1) / RC_THREADS, RC_THREADS, 0, ctx->stream>>>(A);
-    });
-    RK_CHECK_LAUNCH(ctx, "k_recur_backward");
+    uint64_t blocks;
+    if ((rc = tiles_of(ctx, A, RC_WAVES * RC_BACK_ROWS, d_state_in != nullptr, blocks)) != RK_OK) return rc;
+    if (blocks) {
+        with_type(z->type, [&](auto t) { k_recur_backward<decltype(t)><<<(uint32_t)blocks, RC_THREADS, 0, ctx->stream>>>(A); });
+        RK_CHECK_LAUNCH(ctx, "k_recur_backward");
+    }
+    if (d_bias && A.n_tiles != 1) {
+        k_recur_bias<<<(width + 63) / 64, 1024, 0, ctx->stream>>>(A.bias_parts, A.n_tiles, width, d_bias);
+        RK_CHECK_LAUNCH(ctx, "k_recur_bias");
+    }
     return RK_OK;
 }
