@@ -2,19 +2,20 @@
 //
 // Rows that count are gathered first, so that products take no others, and padded with zeros to whole steps of k.  The loss
 // takes the logits' tiles out of the product's registers: of every row the largest and the sum of exponentials over a wavefront's
-// words, joined in fixed order.  The gradients go through the vocabulary in pieces: a piece's logits are made again and become
-// g = p (1 + 2 z lse) - onehot, written both ways round, rounded to the rows' type with a power of two for each row that keeps float16 in its range;
-// dx adds up g W over the pieces in float32, and the piece's rows of d_weight are g^T x.  Every product has k along both sides' rows:
-// x and the piece of W are turned around once for that.
+// words, joined in fixed order.  The gradients go through the vocabulary in pieces, from the last to the first: a piece's logits are made again and become
+// g = row_weight (p (1 + 2 z lse) - onehot), rounded to the rows' type and scaled by a power of two that keeps float16 in its range;
+// dx adds up g W over the pieces in float32, and the piece's rows of d_weight are g^T x.  Where the loss is made along with
+// them, it leaves the exponentials of the piece that it ends with, which then only have to be scaled.
 #include "rk_gemm.h"
 
 namespace {
 
 constexpr uint32_t HD_THREADS = 1024;
-constexpr uint64_t HD_BUDGET = 1ull << 30;                  // bytes of a piece's gradients and weights
+constexpr uint64_t HD_BUDGET = 1ull << 30;                  // bytes of a piece's gradients, and weights where they are padded
 constexpr uint64_t HD_PARTS = 1ull << 28;                   // ... of the sums of the loss's tiles
+constexpr uint32_t HD_PART = 128;                           // words of a wavefront of the logits' tiles
 
-struct RowInfo { float lse, factor, up, share; };           // g = (p factor - onehot) times up for dx, times share for d_weight
+struct RowInfo { float lse, factor, share; uint32_t unused; };     // g = (p factor - onehot) share
 
 // what the device keeps of the rows that count
 struct Rows {
@@ -105,53 +106,33 @@ template <typename T> __global__ __launch_bounds__(256) void k_head_pad(const T 
         for (uint32_t c = threadIdx.x; c < out_width; c += 256) to[c] = c < width ? from[c] : (T)0.f;
     }
 }
-// out[c][r] = x[r][c]; zeros up to out_width.  rows on the device (count) or given
-template <typename T> __global__ __launch_bounds__(256) void k_head_turn(const T *x, uint64_t stride, const uint32_t *count, uint32_t n_rows, uint32_t width, T *out, uint64_t out_stride, uint32_t tiles_c) {
-    __shared__ T tile[64][65];
-    const uint32_t rows = count ? *count : n_rows;
-    const uint32_t r0 = blockIdx.x / tiles_c * 64u, c0 = blockIdx.x % tiles_c * 64u;
-    constexpr uint32_t STEP = GM_ROW / sizeof(T);           // (whole steps of k are zeros, no more are read)
-    if (r0 >= (rows + STEP - 1) / STEP * STEP) return;
-    const uint32_t lane = threadIdx.x & 63u, w = threadIdx.x >> 6;
-#pragma unroll
-    for (uint32_t i = 0; i < 16; ++i) {
-        const uint32_t r = r0 + w * 16 + i, c = c0 + lane;
-        tile[w * 16 + i][lane] = r < rows && c < width ? x[(uint64_t)r * stride + c] : (T)0.f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (uint32_t i = 0; i < 16; ++i) {
-        const uint32_t c = c0 + w * 16 + i;
-        if (c < width) out[(uint64_t)c * out_stride + r0 + lane] = tile[lane][w * 16 + i];
-    }
-}
-
 struct LogitsArgs {
     Rows R;
     Side W, X;                  // of this piece; the kept rows
-    uint32_t bytes_k, tiles_b;
+    uint32_t width, tiles_b;
     uint32_t first, words;      // the piece's first word, how many it has
-    float scale;
+    float scale, room;
     float2 *parts;              // loss: [words / (TA / WA)][kept rows]
     uint64_t parts_stride;
-    void *g, *gt;               // gradient: [kept rows][g_stride], [words][gt_stride]; null: not wanted
-    uint64_t g_stride, gt_stride;
+    void *g;                    // [kept rows][g_stride]: gradients, or what the loss leaves of them (null: nothing)
+    uint64_t g_stride;
 };
 template <typename T> __device__ __forceinline__ float exp_of(float x) {
     if constexpr (sizeof(T) == 4) return exp_f32(x);
     else return __builtin_amdgcn_exp2f(x * 1.4426950408889634f);
 }
 
-// LOSS: a wavefront's largest logit and sum of exponentials of every row, and its label's logit; otherwise the gradients of the logits
+// LOSS: a wavefront's largest logit and sum of exponentials of every row, and its label's logit (and, with g, the exponentials themselves, `room` times as
+// large); otherwise the gradients of the logits
 template <typename T, int TA, int TB, int WA, bool LOSS> __global__ __launch_bounds__(GM_THREADS) void k_head_logits(const LogitsArgs A) {
-    typedef Tile<T, TA, TB, WA> Tl;
+    typedef Tile<T, TA, TB, WA, ALONG, ALONG> Tl;
     const uint32_t n = A.R.count[0];
     const uint32_t a0 = blockIdx.x / A.tiles_b * TA, b0 = blockIdx.x % A.tiles_b * TB;
     if (b0 >= n) return;
     Side X = A.X;
-    X.rows = n;
+    X.count = n;
     Tl t;
-    t.run(A.W, X, a0, b0, 0, A.bytes_k);
+    t.run(A.W, X, a0, b0, 0, A.width);
     const typename Tl::At at = Tl::place();
     const uint32_t a_of = a0 + at.a, b_of = b0 + at.b;
     if constexpr (LOSS) {
@@ -181,42 +162,68 @@ template <typename T, int TA, int TB, int WA, bool LOSS> __global__ __launch_bou
 #pragma unroll
             for (int i = 0; i < Tl::MA; ++i)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) sum += exp_of<T>(t.acc[i][j][q] - from);
+                for (int q = 0; q < 4; ++q) {
+                    const float e = exp_of<T>(t.acc[i][j][q] - from);
+                    t.acc[i][j][q] = e;
+                    sum += e;
+                }
             sum += __shfl_xor(sum, 16, 64);
             sum += __shfl_xor(sum, 32, 64);
             if (there && at.lane < 16) A.parts[(uint64_t)(a_of / (TA / WA)) * A.parts_stride + b] = make_float2(top, sum);
         }
     }
     if constexpr (!LOSS) {
-        // g in place of the logits, then out in both orders, each with its own scale
-        RowInfo info[Tl::MB];
 #pragma unroll
         for (int j = 0; j < Tl::MB; ++j) {
             const uint32_t b = b_of + 16 * j;
             const bool there = b < n;
             const int64_t label = there ? (int64_t)A.R.label[b] - (int64_t)A.first : -1;
-            info[j] = there ? A.R.info[b] : RowInfo{0.f, 0.f, 0.f, 0.f};
+            const RowInfo info = there ? A.R.info[b] : RowInfo{0.f, 0.f, 0.f, 0u};
 #pragma unroll
             for (int i = 0; i < Tl::MA; ++i)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const uint32_t a = a_of + 16 * i + q;
-                    const float p = exp_of<T>(t.acc[i][j][q] * A.scale - info[j].lse) * info[j].factor;
-                    t.acc[i][j][q] = there && a < A.words ? label == (int64_t)a ? p - 1.f : p : 0.f;
+                    const float p = exp_of<T>(t.acc[i][j][q] * A.scale - info.lse) * info.factor;
+                    t.acc[i][j][q] = there && a < A.words ? (label == (int64_t)a ? p - 1.f : p) * info.share : 0.f;
                 }
             __builtin_amdgcn_sched_barrier(0);
         }
-        constexpr uint32_t EACH = 16 / sizeof(T);
-        if (A.g)
-            t.rows([&](int i, int j) { return t.acc[i][j] * info[j].up; },
-                   [&](uint32_t a, uint32_t b, const Vec<uint32_t, 4> &w) {
-                       if (b0 + b < n) *(Vec<uint32_t, 4> *)((T *)A.g + (uint64_t)(b0 + b) * A.g_stride + a0 + a) = w;
-                   });
-        if (A.gt)
-            t.columns([&](int i, int j) { return t.acc[i][j] * info[j].share; },
-                      [&](uint32_t a, uint32_t b, const Vec<uint32_t, 4> &w) {
-                          if (a0 + a < A.words) *(Vec<uint32_t, 4> *)((T *)A.gt + (uint64_t)(a0 + a) * A.gt_stride + b0 + b) = w;
-                      });
+    }
+    if (A.g)
+        t.rows([&](int i, int j) { return LOSS ? t.acc[i][j] * A.room : t.acc[i][j]; },
+               [&](uint32_t a, uint32_t b, const Vec<uint32_t, 4> &w) {
+                   if (b0 + b < n) *(Vec<uint32_t, 4> *)((T *)A.g + (uint64_t)(b0 + b) * A.g_stride + a0 + a) = w;
+               });
+}
+
+// What the loss left of a piece becomes its gradients: each wavefront's words had their own largest logit.  A workgroup takes rows of 2,048 words.
+struct ScaleArgs {
+    Rows R;
+    const float2 *parts;
+    uint64_t parts_stride, g_stride;
+    void *g;
+    uint32_t first, words, part;
+    float room;
+};
+template <typename T> __global__ __launch_bounds__(256) void k_head_scale(const ScaleArgs A) {
+    constexpr uint32_t EACH = 16 / sizeof(T);
+    const uint32_t n = A.R.count[0], a = (blockIdx.x * 256u + threadIdx.x) * EACH;
+    if (a >= A.words) return;                               // (words behind the piece's last are zeros already)
+    for (uint32_t b = blockIdx.y; b < n; b += gridDim.y) {
+        const RowInfo info = A.R.info[b];
+        const int64_t label = (int64_t)A.R.label[b] - (int64_t)A.first - (int64_t)a;
+        const float top = A.parts[(uint64_t)(a / A.part) * A.parts_stride + b].x;
+        const float f = exp_f32((top == -INFINITY ? 0.f : top) - info.lse) * info.factor * (1.f / A.room);
+        Vec<uint32_t, 4> *const at = (Vec<uint32_t, 4> *)((T *)A.g + (uint64_t)b * A.g_stride + a);
+        const Vec<uint32_t, 4> w = *at;
+        Vec<T, EACH> v;
+#pragma unroll
+        for (uint32_t e = 0; e < EACH; ++e) {
+            const float p = element<T>(w, e) * f;
+            v[e] = (T)((label == (int64_t)e ? p - 1.f : p) * info.share);
+        }
+        *at = __builtin_bit_cast(Vec<uint32_t, 4>, v);
     }
 }
 
@@ -303,14 +310,14 @@ __global__ __launch_bounds__(HD_THREADS) void k_head_info(const Rows R, const fl
     if (threadIdx.x == 0) R.count[1] = __float_as_uint(unit);
     for (uint32_t i = threadIdx.x; i < n; i += HD_THREADS) {
         const float lse = lse_of[R.row[i]], factor = 1.f + 2.f * z_weight * lse;
-        R.info[i] = RowInfo{lse, factor, room / power_above(fmaxf(1.f, fabsf(factor))), R.weight[i] / unit * room};
+        R.info[i] = RowInfo{lse, factor, R.weight[i] / unit * room, 0u};
     }
 }
 
 struct OutArgs {
     Rows R;
     Side A, B;
-    uint32_t tiles_b, bytes_k;
+    uint32_t tiles_b, ks;
     uint32_t splits;
     float *sums;                // dx: [splits][rows][stride]
     uint64_t stride, split_stride;
@@ -319,21 +326,21 @@ struct OutArgs {
     bool aligned;               // its rows take whole vectors
     uint32_t width, words;
     const float *d_total;
-    float scale;
+    float scale, room;
 };
 // dx: sums over the piece's words, one share of them a split, added to those of the pieces before
 template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_THREADS) void k_head_dx(const OutArgs A) {
-    typedef Tile<T, TA, TB, WA> Tl;
+    typedef Tile<T, TA, TB, WA, ACROSS, ALONG> Tl;
     const uint32_t n = A.R.count[0];
     const uint32_t split = blockIdx.x % A.splits, tile = blockIdx.x / A.splits;
     const uint32_t a0 = tile / A.tiles_b * TA, b0 = tile % A.tiles_b * TB;
     if (b0 >= n) return;
     Side B = A.B;
-    B.rows = n;
-    const uint32_t steps = (A.bytes_k + GM_ROW - 1) / GM_ROW;
-    const uint32_t from = (uint32_t)((uint64_t)steps * split / A.splits), to = (uint32_t)((uint64_t)steps * (split + 1) / A.splits);
+    B.count = n;
+    const uint32_t steps = (A.ks + Tl::KS - 1) / Tl::KS;
+    const uint32_t from = (uint32_t)((uint64_t)steps * split / A.splits) * Tl::KS, to = (uint32_t)((uint64_t)steps * (split + 1) / A.splits) * Tl::KS;
     Tl t;
-    t.run(A.A, B, a0, b0, (uint64_t)from * GM_ROW, (to - from) * GM_ROW);
+    t.run(A.A, B, a0, b0, from, (to < A.ks ? to : A.ks) - from);
     const typename Tl::At at = Tl::place();
     const uint32_t a_of = a0 + at.a, b_of = b0 + at.b;
 #pragma unroll
@@ -349,7 +356,7 @@ template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_TH
 template <typename T> __global__ __launch_bounds__(256) void k_head_dx_out(const OutArgs A, T *dx, uint64_t dx_st, uint64_t n_rows) {
     for (uint64_t r = blockIdx.x; r < n_rows; r += gridDim.x) {
         const int32_t i = A.R.place[r];
-        const float f = i < 0 ? 0.f : (A.d_total ? *A.d_total : 1.f) * A.scale * A.R.weight[i] / A.R.info[i].up;
+        const float f = i < 0 ? 0.f : (A.d_total ? *A.d_total : 1.f) * A.scale * (__uint_as_float(A.R.count[1]) / A.room);
         for (uint32_t c = threadIdx.x; c < A.width; c += 256) {
             float v = 0.f;
             if (i >= 0)
@@ -358,14 +365,13 @@ template <typename T> __global__ __launch_bounds__(256) void k_head_dx_out(const
         }
     }
 }
-template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_THREADS) void k_head_dw(const OutArgs A, float room) {
-    typedef Tile<T, TA, TB, WA> Tl;
-    constexpr uint32_t STEP = GM_ROW / sizeof(T);
+template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_THREADS) void k_head_dw(const OutArgs A) {
+    typedef Tile<T, TA, TB, WA, ACROSS, ACROSS> Tl;
     const uint32_t n = A.R.count[0];
     const uint32_t a0 = blockIdx.x / A.tiles_b * TA, b0 = blockIdx.x % A.tiles_b * TB;
     Tl t;
-    t.run(A.A, A.B, a0, b0, 0, (n + STEP - 1) / STEP * GM_ROW);
-    const float f = n ? (A.d_total ? *A.d_total : 1.f) * A.scale * (__uint_as_float(A.R.count[1]) / room) : 0.f;
+    t.run(A.A, A.B, a0, b0, 0, n);
+    const float f = n ? (A.d_total ? *A.d_total : 1.f) * A.scale * (__uint_as_float(A.R.count[1]) / A.room) : 0.f;
     constexpr uint32_t EACH = 16 / sizeof(T);
     T *const out = (T *)A.out;
     const bool whole = A.aligned && a0 + TA <= A.width;
@@ -434,51 +440,52 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
     const uint32_t tiles_b = (uint32_t)(rows_pad / 256);
     const uint64_t most_tiles = (1u << 22) / (tiles_b ? tiles_b : 1);
     const bool back = C.dx || C.d_weight;
-    // words of a piece: what the budget holds of both g, W turned around and W padded
+    // words of a piece: what the budget holds of their gradients, of W padded, and of the sums of tiles
     uint64_t words = up_to(C.vocab, 256);
-    if (back || !direct) {
-        const uint64_t each = (back ? 2 * rows_pad * ES + (uint64_t)up_to(C.width, 256) * ES : 0) + (direct ? 0 : (uint64_t)wide * ES);
-        words = HD_BUDGET / each / 256 * 256;
-    }
+    const uint64_t each = (back ? rows_pad * ES : 0) + (direct ? 0 : (uint64_t)wide * ES), sums_each = C.total ? rows_pad * 8 / HD_PART : 0;
+    if (each && HD_BUDGET / each < words) words = HD_BUDGET / each / 256 * 256;
+    if (sums_each && HD_PARTS / sums_each < words) words = HD_PARTS / sums_each / 256 * 256;
     if (words > most_tiles * 256) words = most_tiles * 256;
     if (words < 256) words = 256;
-    if (words > up_to(C.vocab, 256)) words = up_to(C.vocab, 256);
     T *padded = nullptr;
     if (!direct && (rc = rk_scratch(ctx, SL_HEAD_W, words * wide * ES, (void **)&padded)) != RK_OK) return rc;
-
-    auto side_of = [&](uint32_t first, uint32_t n, Side &S) -> int32_t {
+    // the piece from word `first` on
+    uint32_t n_words = 0;
+    Side W{};
+    auto piece = [&](uint64_t first) -> int32_t {
+        n_words = (uint32_t)(C.vocab - first < words ? C.vocab - first : words);
         if (direct) {
-            S = Side{(const char *)(w + first * w_st), w_st * ES, n};
+            W = Side{(const char *)(w + first * w_st), w_st * ES, 0};
             return RK_OK;
         }
-        k_head_pad<T><<<blocks_of(n), 256, 0, stream>>>(w + first * w_st, w_st, n, C.width, padded, wide);
+        k_head_pad<T><<<blocks_of(n_words), 256, 0, stream>>>(w + first * w_st, w_st, n_words, C.width, padded, wide);
         RK_CHECK_LAUNCH(ctx, "k_head_pad");
-        S = Side{(const char *)padded, (uint64_t)wide * ES, n};
+        W = Side{(const char *)padded, (uint64_t)wide * ES, 0};
         return RK_OK;
     };
+    // float16 has 30 powers of two between one and its smallest: what is at most one is moved up by fourteen
+    const float room = __is_same(T, _Float16) ? 16384.f : 1.f;
     LogitsArgs L{};
-    L.R = R; L.X = X;
-    L.bytes_k = (uint32_t)(direct ? C.width * ES : wide * ES);
-    L.tiles_b = tiles_b;
-    L.scale = C.head->logit_scale;
+    L.R = R; L.X = X; L.width = C.width; L.tiles_b = tiles_b; L.scale = C.head->logit_scale; L.room = room;
+    if (back && (rc = rk_scratch(ctx, SL_HEAD_G, rows_pad * words * ES, (void **)&L.g)) != RK_OK) return rc;
+    L.g_stride = words;
+    void *const g = L.g;
+    const uint64_t last_piece = (C.vocab - 1) / words * words;
 
     if (C.total) {
-        uint64_t loss_words = words;
-        const uint64_t per = rows_pad * 8;                  // a part of 128 words
-        if (loss_words / 128 * per > HD_PARTS) loss_words = HD_PARTS / per * 128 / 256 * 256;
-        if (loss_words < 256) loss_words = 256;
-        if ((rc = rk_scratch(ctx, SL_HEAD_PARTS, loss_words / 128 * per, (void **)&L.parts)) != RK_OK) return rc;
+        if ((rc = rk_scratch(ctx, SL_HEAD_PARTS, words * sums_each, (void **)&L.parts)) != RK_OK) return rc;
         L.parts_stride = rows_pad;
         JoinArgs J{R, L.parts, rows_pad, 0, false, C.head->z_weight, C.loss, C.lse, C.total, C.n_rows};
-        for (uint64_t first = 0; first < C.vocab && C.n_rows; first += loss_words) {
-            const uint32_t n = (uint32_t)(C.vocab - first < loss_words ? C.vocab - first : loss_words);
-            if ((rc = side_of((uint32_t)first, n, L.W)) != RK_OK) return rc;
-            L.first = (uint32_t)first; L.words = n;
-            const uint32_t tiles_a = (n + 255) / 256;
+        for (uint64_t first = 0; first < C.vocab && C.n_rows; first += words) {
+            if ((rc = piece(first)) != RK_OK) return rc;
+            L.first = (uint32_t)first; L.words = n_words;
+            L.W = W; L.W.count = n_words;
+            L.g = first == last_piece ? g : nullptr;
+            const uint32_t tiles_a = (n_words + 255) / 256;
             k_head_logits<T, 256, 256, 2, true><<<tiles_a * tiles_b, GM_THREADS, 0, stream>>>(L);
             RK_CHECK_LAUNCH(ctx, "k_head_logits");
             J.n_parts = tiles_a * 2;
-            J.last = first + n == C.vocab;
+            J.last = first == last_piece;
             k_head_join<<<(uint32_t)((C.n_rows + 15) / 16), 256, 0, stream>>>(J);
             RK_CHECK_LAUNCH(ctx, "k_head_join");
         }
@@ -487,69 +494,54 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
     }
     if (!back) return RK_OK;
 
-    // float16 has 30 powers of two between one and its smallest: g, at most one, is moved up by fourteen
-    const float room = __is_same(T, _Float16) ? 16384.f : 1.f;
     k_head_info<<<1, HD_THREADS, 0, stream>>>(R, C.given_lse ? C.given_lse : C.lse, C.head->z_weight, room);
     RK_CHECK_LAUNCH(ctx, "k_head_info");
-    const uint64_t width_pad = up_to(C.width, 256);
-    T *xt = nullptr, *wt = nullptr;
-    float *sums = nullptr;
+    const uint32_t tiles_w = (uint32_t)((C.width + 255) / 256);
     OutArgs O{};
-    O.R = R; O.d_total = C.d_total; O.scale = C.head->logit_scale; O.width = C.width;
-    const uint32_t tiles_w = (uint32_t)(width_pad / 256);
+    O.R = R; O.d_total = C.d_total; O.scale = C.head->logit_scale; O.room = room; O.width = C.width;
     if (C.dx) {
-        if ((rc = rk_scratch(ctx, SL_HEAD_G, rows_pad * words * ES, (void **)&L.g)) != RK_OK) return rc;
-        if ((rc = rk_scratch(ctx, SL_HEAD_WT, width_pad * words * ES, (void **)&wt)) != RK_OK) return rc;
-        L.g_stride = words;
         // as many shares of the words as fill the compute units
         const uint64_t tiles = (uint64_t)tiles_w * (tiles_b ? tiles_b : 1);
         O.splits = (uint32_t)(tiles >= 256 ? 1 : (256 + tiles - 1) / tiles);
         if (O.splits > words / 1024 + 1) O.splits = (uint32_t)(words / 1024 + 1);
         O.stride = up_to(C.width, 4);
         O.split_stride = C.n_rows * O.stride;
-        if ((rc = rk_scratch(ctx, SL_HEAD_DX, O.splits * O.split_stride * 4, (void **)&sums)) != RK_OK) return rc;
-        O.sums = sums;
+        if ((rc = rk_scratch(ctx, SL_HEAD_DX, O.splits * O.split_stride * 4, (void **)&O.sums)) != RK_OK) return rc;
     }
-    if (C.d_weight) {
-        if ((rc = rk_scratch(ctx, SL_HEAD_GT, rows_pad * words * ES, (void **)&L.gt)) != RK_OK) return rc;
-        if ((rc = rk_scratch(ctx, SL_HEAD_XT, rows_pad * C.width * ES, (void **)&xt)) != RK_OK) return rc;
-        L.gt_stride = rows_pad;
-        if (C.n_rows) {
-            const uint32_t tiles_c = (C.width + 63) / 64;
-            k_head_turn<T><<<(uint32_t)(rows_pad / 64 * tiles_c), 256, 0, stream>>>(xc, wide, R.count, 0, C.width, xt, rows_pad, tiles_c);
-            RK_CHECK_LAUNCH(ctx, "k_head_turn");
-        }
-    }
-    for (uint64_t first = 0; first < C.vocab; first += words) {
-        const uint32_t n = (uint32_t)(C.vocab - first < words ? C.vocab - first : words);
-        const uint32_t tiles_a = (n + 255) / 256;
-        if (C.n_rows) {
-            if ((rc = side_of((uint32_t)first, n, L.W)) != RK_OK) return rc;
-            L.first = (uint32_t)first; L.words = n;
+    const uint64_t row_bytes = direct ? (uint64_t)C.width * ES : (uint64_t)wide * ES;
+    L.g = g;
+    for (uint64_t first = last_piece;; first -= words) {
+        if ((rc = piece(first)) != RK_OK) return rc;        // (padded once more where the loss has been through all pieces)
+        const uint32_t tiles_a = (n_words + 255) / 256;
+        if (C.n_rows && C.total && first == last_piece) {
+            const uint32_t across = (n_words + 256 * 16 / ES - 1) / (256 * 16 / ES);
+            k_head_scale<T><<<dim3(across, (uint32_t)(C.n_rows < 4096 ? C.n_rows : 4096)), 256, 0, stream>>>(
+                ScaleArgs{R, L.parts, rows_pad, words, g, (uint32_t)first, n_words, HD_PART, room});
+            RK_CHECK_LAUNCH(ctx, "k_head_scale");
+        } else if (C.n_rows) {
+            L.first = (uint32_t)first; L.words = n_words;
+            L.W = W; L.W.count = n_words;
             k_head_logits<T, 256, 256, 2, false><<<tiles_a * tiles_b, GM_THREADS, 0, stream>>>(L);
             RK_CHECK_LAUNCH(ctx, "k_head_logits");
         }
         if (C.dx && C.n_rows) {
-            const uint32_t tiles_c = (C.width + 63) / 64;
-            k_head_turn<T><<<(uint32_t)((n + 63) / 64 * tiles_c), 256, 0, stream>>>(w + first * w_st, w_st, nullptr, n, C.width, wt, words, tiles_c);
-            RK_CHECK_LAUNCH(ctx, "k_head_turn");
-            O.A = Side{(const char *)wt, words * ES, C.width};
-            O.B = Side{(const char *)L.g, words * ES, 0};
-            O.bytes_k = (uint32_t)(up_to(n, STEP) * ES);
-            O.tiles_b = tiles_b; O.first = first == 0;
+            O.A = W; O.A.count = row_bytes;
+            O.B = Side{(const char *)g, words * ES, 0};
+            O.ks = n_words; O.tiles_b = tiles_b; O.first = first == last_piece;
             k_head_dx<T, 256, 256, 2><<<tiles_w * tiles_b * O.splits, GM_THREADS, 0, stream>>>(O);
             RK_CHECK_LAUNCH(ctx, "k_head_dx");
         }
         if (C.d_weight) {
             OutArgs D = O;
-            D.A = Side{(const char *)xt, rows_pad * ES, C.width};
-            D.B = Side{(const char *)L.gt, rows_pad * ES, n};
-            D.tiles_b = tiles_a; D.words = n;
+            D.A = X; D.A.count = (uint64_t)wide * ES;
+            D.B = Side{(const char *)g, words * ES, words * ES};
+            D.tiles_b = tiles_a; D.words = n_words;
             D.aligned = (uintptr_t)C.d_weight->data % 16 == 0 && C.d_weight->stride * ES % 16 == 0;
             D.out = (T *)C.d_weight->data + first * C.d_weight->stride; D.stride = C.d_weight->stride;
-            k_head_dw<T, 256, 256, 2><<<tiles_w * tiles_a, GM_THREADS, 0, stream>>>(D, room);
+            k_head_dw<T, 256, 256, 2><<<tiles_w * tiles_a, GM_THREADS, 0, stream>>>(D);
             RK_CHECK_LAUNCH(ctx, "k_head_dw");
         }
+        if (first == 0) break;
     }
     if (C.dx && C.n_rows) {
         k_head_dx_out<T><<<blocks_of(C.n_rows), 256, 0, stream>>>(O, (T *)C.dx->data, C.dx->stride, C.n_rows);
