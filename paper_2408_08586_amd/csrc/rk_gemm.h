@@ -1,9 +1,12 @@
 // Matrix products of the operators: out[b][a] = sum over k of A(a, k) B(b, k), held in float32.
 //
-// A workgroup of eight wavefronts makes a tile of TA x TB, 128 bytes of k at a time: both tiles go from memory straight into LDS
-// while the ones before them are multiplied.  A side lies with k along its rows (ALONG) or with k from row to row (ACROSS), and so it
-// comes into LDS; nothing is turned around beforehand:
-//   ALONG   128 bytes a row.  A lane's part of a fragment is a 16-byte piece of its row; pieces lie in the order piece ^ (row % 8), so that the
+// A workgroup of four wavefronts makes a tile of TA x TB.  64 bytes of k at a time, both tiles go from memory straight into one of
+// four places in LDS; fragments are read from there one step ahead of the products that take them, so that the matrix units, the reads of LDS and the loads
+// from memory of the three steps that follow run side by side, with one barrier a step.  A wavefront has 128 x 128 sums of the largest tile: a
+// byte that it reads from LDS is used 128 times, which keeps LDS at half the matrix units' time (of wavefronts of
+// 128 x 64, eight to a workgroup, the products waited for LDS at every step).
+// A side lies with k along its rows (ALONG) or with k from row to row (ACROSS), and so it comes into LDS; nothing is turned around beforehand:
+//   ALONG   64 bytes a row.  A lane's part of a fragment is a 16-byte piece of its row; pieces lie in the order piece ^ (row / 4 % 4), so that the
 //           sixteen rows of a fragment do not meet in the banks.
 //   ACROSS  a row of TA (TB) elements for every k.  Of narrow elements, sixteen lanes read four k of sixteen elements and get them
 //           turned around by the LDS unit; of 32-bit ones, a lane reads its element of each k.  Pieces lie in the order piece ^ something that
@@ -11,11 +14,13 @@
 // Memory gives pieces in that order, as LDS is written in the order of the lanes.  The matrix units take sixteen elements of 32 narrow k at once, or of four
 // 32-bit ones: there, each of four products takes one k of every lane's four, the same of both sides.
 #pragma once
+#include <type_traits>
+
 #include "rk_vec.h"
 
 namespace {
 
-constexpr uint32_t GM_THREADS = 512, GM_ROW = 128;          // threads; bytes of k in LDS
+constexpr uint32_t GM_THREADS = 256, GM_STEP = 64;          // threads; bytes of k of a step
 constexpr uint32_t GM_NOWHERE = 0x80000000u;                // a lane's place behind every buffer: zeros
 
 // (builtins of this GPU alone: the host's pass over the source does not know them)
@@ -45,6 +50,15 @@ __device__ __forceinline__ Vec<uint32_t, 2> turned(const char *lds) {
     return Vec<uint32_t, 2>{0u, 0u};
 #endif
 }
+// Until no more than N of the wavefront's loads are under way, then until all wavefronts are here.
+template <int N> __device__ __forceinline__ void landed() {
+    asm volatile("" ::: "memory");
+#ifdef __HIP_DEVICE_COMPILE__
+    __builtin_amdgcn_s_waitcnt(0xC07F & ~0xC00F | (N & 0xF) | (N >> 4 << 14));     // vmcnt(N) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+#endif
+    asm volatile("" ::: "memory");
+}
 
 enum { ALONG = 0, ACROSS = 1 };
 // One side of a product, its first byte and stride multiples of 16.
@@ -53,28 +67,36 @@ struct Side {
     uint64_t stride;            // bytes from row to row
     uint64_t count;             // ALONG: rows; ACROSS: bytes of a row
 };
-// order of the pieces of a row of LDS for one k
-template <typename T> __device__ __forceinline__ uint32_t order_of(uint32_t k) {
-    if constexpr (sizeof(T) == 4) return (k >> 2 & 3u) * 4u;
-    else return ((k & 3u) | (k >> 3 & 3u) << 2) * 2u;
-}
-// What a wavefront asks for of a tile of R elements: R / 64 instructions of 1,024 bytes.
+// ACROSS: where a piece of k's row lies among the row's PIECES (place), and which one lies there (piece): pairs of pieces move
+// (of 32-bit elements fours), by a step for every k that is read together
+template <typename T, uint32_t PIECES> struct Order {
+    static constexpr bool POWER = (PIECES & (PIECES - 1)) == 0;
+    static __device__ __forceinline__ uint32_t by(uint32_t k) {
+        if constexpr (sizeof(T) == 4) return (k >> 2 & 3u) * 4u % PIECES;
+        else return ((k & 3u) | (k >> 3 & 3u) << 2) * 2u % PIECES;
+    }
+    static __device__ __forceinline__ uint32_t place(uint32_t piece, uint32_t k) { return POWER ? piece ^ by(k) : (piece + by(k)) % PIECES; }
+    static __device__ __forceinline__ uint32_t piece(uint32_t place, uint32_t k) { return POWER ? place ^ by(k) : (place + PIECES - by(k)) % PIECES; }
+};
+// What a wavefront asks for of a tile of R elements: R / 64 instructions of 1,024 bytes, of small tiles one, some of them twice, so that
+// every wavefront has as many under way.
 template <typename T, int R, int WAY> struct Fetch {
     static constexpr int N = R >= 64 ? R / 64 : 1;
-    static constexpr uint32_t KS = GM_ROW / sizeof(T), PIECES = R * sizeof(T) / 16;     // k of a step; ACROSS: pieces of a row of LDS
+    static constexpr uint32_t KS = GM_STEP / sizeof(T), PIECES = R * sizeof(T) / 16;    // k of a step; ACROSS: pieces of a row of LDS
     const char *base;
     uint64_t hop;               // bytes from step to step
     uint32_t at[N], tail[N];    // of a lane, and in the last step
+    static __device__ __forceinline__ uint32_t part(int i) { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * N % (R / 16) + i; }
     __device__ __forceinline__ Fetch(const Side &s, uint64_t first, uint64_t k0, uint32_t ks) {
-        const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, left = ks % KS ? ks % KS : KS;
+        const uint32_t lane = threadIdx.x & 63u, left = ks % KS ? ks % KS : KS;
         if constexpr (WAY == ALONG) {
             base = s.data + first * s.stride + k0 * sizeof(T);
-            hop = GM_ROW;
+            hop = GM_STEP;
             const uint64_t rows = s.count - first;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                uint32_t r = (wave * N + i) * 8 + (lane >> 3);
-                const uint32_t piece = (lane & 7u) ^ (r & 7u);
+                uint32_t r = part(i) * 16 + (lane >> 2);
+                const uint32_t piece = (lane & 3u) ^ (r >> 2 & 3u);
                 r = r < rows ? r : (uint32_t)(rows - 1);    // (rows behind the last repeat it: their results go nowhere)
                 at[i] = r * (uint32_t)s.stride + piece * 16;
                 tail[i] = piece * (16 / sizeof(T)) < left ? at[i] : GM_NOWHERE;
@@ -84,54 +106,50 @@ template <typename T, int R, int WAY> struct Fetch {
             hop = KS * s.stride;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const uint32_t x = (wave * N + i) * 64 + lane, k = x / PIECES, piece = (x % PIECES) ^ (order_of<T>(k) % PIECES);
+                const uint32_t x = part(i) * 64 + lane, k = x / PIECES, piece = Order<T, PIECES>::piece(x % PIECES, k);
                 at[i] = first * sizeof(T) + piece * 16 < s.count ? k * (uint32_t)s.stride + piece * 16 : GM_NOWHERE;
                 tail[i] = k < left ? at[i] : GM_NOWHERE;
             }
         }
     }
-    // step s into LDS; `last`: the rest of k alone, zeros behind it
-    __device__ __forceinline__ void into(char *lds, uint32_t s, bool last) const {
-        const uint32_t wave = threadIdx.x >> 6;
-        if (R < 64 && wave * 8 >= R) return;
-        const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base) + s * hop, 0, (int)GM_NOWHERE, 0x00027000);
+    // step s of `steps` into LDS; LAST: of the last one what is left of k, zeros behind it and of steps that there are not
+    template <bool LAST> __device__ __forceinline__ void into(char *lds, uint32_t s, uint32_t steps) const {
+        const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base) + (!LAST || s < steps ? s : 0) * hop, 0, (int)GM_NOWHERE, 0x00027000);
 #pragma unroll
-        for (int i = 0; i < N; ++i) into_lds(buf, lds + (wave * N + i) * 1024, last ? tail[i] : at[i]);
+        for (int i = 0; i < N; ++i) into_lds(buf, lds + part(i) * 1024, !LAST || s + 1 < steps ? at[i] : s < steps ? tail[i] : GM_NOWHERE);
     }
 };
 // A wavefront's fragments of M times sixteen elements, from element `first` of the tile on
 template <typename T, int R, int WAY, int M> struct Reader {
     static constexpr uint32_t PITCH = R * sizeof(T), PIECES = PITCH / 16;
-    uint32_t at[WAY == ALONG ? 2 : M];
+    uint32_t at[WAY == ALONG ? 1 : M];
     __device__ __forceinline__ Reader(uint32_t first) {
         const uint32_t lane = threadIdx.x & 63u, j = lane & 15u, g = lane >> 4;
         if constexpr (WAY == ALONG) {
-#pragma unroll
-            for (uint32_t h = 0; h < 2; ++h) at[h] = (first + j) * GM_ROW + ((h * 4 + g) ^ (j & 7u)) * 16;
+            at[0] = (first + j) * GM_STEP + (g ^ (j >> 2)) * 16;
         } else {
 #pragma unroll
             for (int i = 0; i < M; ++i) {
                 if constexpr (sizeof(T) == 4) {
                     const uint32_t k = 4 * g, piece = (first + 16 * i) / 4 + (j >> 2);
-                    at[i] = k * PITCH + (piece ^ (order_of<T>(k) % PIECES)) * 16 + (j & 3u) * 4;
+                    at[i] = k * PITCH + Order<T, PIECES>::place(piece, k) * 16 + (j & 3u) * 4;
                 } else {
                     const uint32_t k = 8 * g + (j >> 2), piece = (first + 16 * i) / 8 + (j >> 1 & 1u);
-                    at[i] = k * PITCH + (piece ^ (order_of<T>(k) % PIECES)) * 16 + (j & 1u) * 8;
+                    at[i] = k * PITCH + Order<T, PIECES>::place(piece, k) * 16 + (j & 1u) * 8;
                 }
             }
         }
     }
-    // half h of the step's k
-    __device__ __forceinline__ Vec<uint32_t, 4> read(const char *lds, int i, uint32_t h) const {
+    __device__ __forceinline__ Vec<uint32_t, 4> read(const char *lds, int i) const {
         if constexpr (WAY == ALONG) {
-            return *(const Vec<uint32_t, 4> *)(lds + at[h] + i * 16 * GM_ROW);
+            return *(const Vec<uint32_t, 4> *)(lds + at[0] + i * 16 * GM_STEP);
         } else if constexpr (sizeof(T) == 4) {
             Vec<uint32_t, 4> w;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) w[q] = *(const uint32_t *)(lds + at[i] + (16 * h + q) * PITCH);
+            for (int q = 0; q < 4; ++q) w[q] = *(const uint32_t *)(lds + at[i] + q * PITCH);
             return w;
         } else {
-            const Vec<uint32_t, 2> lo = turned(lds + at[i] + 32 * h * PITCH), hi = turned(lds + at[i] + (32 * h + 4) * PITCH);
+            const Vec<uint32_t, 2> lo = turned(lds + at[i]), hi = turned(lds + at[i] + 4 * PITCH);
             return Vec<uint32_t, 4>{lo[0], lo[1], hi[0], hi[1]};
         }
     }
@@ -140,11 +158,15 @@ template <typename T, int R, int WAY, int M> struct Reader {
 // The tile at (a0, b0) over ks of k from k0 on; WA x WB wavefronts share it.  acc[i][j]: lane l holds the elements
 // a = a0 + wa TA/WA + 16 i + 4 (l / 16) + 0..3,  b = b0 + wb TB/WB + 16 j + l % 16.
 template <typename T, int TA, int TB, int WA, int WAY_A, int WAY_B> struct Tile {
-    static constexpr int WB = 8 / WA, MA = TA / WA / 16, MB = TB / WB / 16;
-    static constexpr uint32_t KS = GM_ROW / sizeof(T);
+    static constexpr int WB = 4 / WA, MA = TA / WA / 16, MB = TB / WB / 16;
+    static constexpr uint32_t KS = GM_STEP / sizeof(T), GRAIN = 4 * KS;         // k of a step; of a turn of the loop, which is done whole
+    typedef Fetch<T, TA, WAY_A> FetchA;
+    typedef Fetch<T, TB, WAY_B> FetchB;
     typedef Reader<T, TA, WAY_A, MA> ReadA;
     typedef Reader<T, TB, WAY_B, MB> ReadB;
+    static constexpr int EACH = FetchA::N + FetchB::N;                          // a wavefront's loads of a step
     Vec<float, 4> acc[MA][MB];
+    struct Fragments { Vec<uint32_t, 4> a[MA], b[MB]; };
     // The lane's place in the tile for what is made of the sums: taken anew behind the loop, which has no registers for it.
     struct At { uint32_t a, b, lane; };
     static __device__ __forceinline__ At place() {
@@ -156,73 +178,89 @@ template <typename T, int TA, int TB, int WA, int WAY_A, int WAY_B> struct Tile 
     static __device__ __forceinline__ uint32_t wave_a() { return (threadIdx.x >> 6) / WB * (TA / WA); }
     static __device__ __forceinline__ uint32_t wave_b() { return (threadIdx.x >> 6) % WB * (TB / WB); }
 
-    __device__ __forceinline__ void step(const char *a, const char *b, const ReadA &ra, const ReadB &rb) {
+    static __device__ __forceinline__ void read(Fragments &f, const char *a, const char *b, const ReadA &ra, const ReadB &rb) {
 #pragma unroll
-        for (uint32_t h = 0; h < 2; ++h) {
-            Vec<uint32_t, 4> fa[MA], fb[MB];
+        for (int j = 0; j < MB; ++j) f.b[j] = rb.read(b, j);
 #pragma unroll
-            for (int j = 0; j < MB; ++j) fb[j] = rb.read(b, j, h);
-#pragma unroll
-            for (int i = 0; i < MA; ++i) fa[i] = ra.read(a, i, h);
-#pragma unroll
-            for (int i = 0; i < MA; ++i)
-#pragma unroll
-                for (int j = 0; j < MB; ++j) acc[i][j] = products<T>(fa[i], fb[j], acc[i][j]);
-        }
+        for (int i = 0; i < MA; ++i) f.a[i] = ra.read(a, i);
     }
-    char *room[2];              // two runs of TA * GM_ROW bytes of LDS, free behind the loop
+    __device__ __forceinline__ void multiply(const Fragments &f) {
+#pragma unroll
+        for (int i = 0; i < MA; ++i)
+#pragma unroll
+            for (int j = 0; j < MB; ++j) acc[i][j] = products<T>(f.a[i], f.b[j], acc[i][j]);
+    }
+    // loads and reads among the products, not before them
+    static __device__ __forceinline__ void interleave() {
+#ifdef __HIP_DEVICE_COMPILE__
+        constexpr int PRODUCTS = MA * MB * (sizeof(T) == 4 ? 4 : 1), READS_A = WAY_A == ALONG ? 1 : sizeof(T) == 4 ? 4 : 2, READS_B = WAY_B == ALONG ? 1 : sizeof(T) == 4 ? 4 : 2;
+        constexpr int READS = MA * READS_A + MB * READS_B, GROUPS = MA + MB, AT = PRODUCTS / GROUPS;
+        if constexpr (AT >= 1) {
+#pragma unroll
+            for (int i = 0; i < GROUPS; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x100, (READS + GROUPS - 1) / GROUPS, 0);
+                if (i < EACH) __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, AT, 0);
+            }
+        }
+#endif
+    }
+    char *room[4];              // four runs of TA * GM_STEP bytes of LDS, free behind the loop
 
     __device__ __forceinline__ void run(const Side &A, const Side &B, uint64_t a0, uint64_t b0, uint64_t k0, uint32_t ks) {
-        __shared__ __attribute__((aligned(128))) char a_even[TA * GM_ROW], b_even[TB * GM_ROW];
-        __shared__ __attribute__((aligned(128))) char a_odd[TA * GM_ROW], b_odd[TB * GM_ROW];
+        __shared__ __attribute__((aligned(128))) char a_0[TA * GM_STEP], a_1[TA * GM_STEP], a_2[TA * GM_STEP], a_3[TA * GM_STEP];
+        __shared__ __attribute__((aligned(128))) char b_0[TB * GM_STEP], b_1[TB * GM_STEP], b_2[TB * GM_STEP], b_3[TB * GM_STEP];
 #pragma unroll
         for (int i = 0; i < MA; ++i)
 #pragma unroll
             for (int j = 0; j < MB; ++j) acc[i][j] = 0.f;
-        room[0] = a_even; room[1] = a_odd;
+        room[0] = a_0; room[1] = a_1; room[2] = a_2; room[3] = a_3;
         const uint32_t steps = (ks + KS - 1) / KS;
         if (steps == 0) return;
-        const Fetch<T, TA, WAY_A> fa(A, a0, k0, ks);
-        const Fetch<T, TB, WAY_B> fb(B, b0, k0, ks);
+        const FetchA fa(A, a0, k0, ks);
+        const FetchB fb(B, b0, k0, ks);
         const ReadA ra(wave_a());
         const ReadB rb(wave_b());
-        // an odd step goes first, and there is one way out of the loop: the sums stay in their registers
+        Fragments even, odd;
+        auto fetch = [&](auto last, char *a, char *b, uint32_t s) {
+            fa.template into<decltype(last)::value>(a, s, steps);
+            fb.template into<decltype(last)::value>(b, s, steps);
+        };
+        constexpr std::true_type LAST{};
+        constexpr std::false_type NOT_LAST{};
+        fetch(LAST, a_0, b_0, 0);
+        fetch(LAST, a_1, b_1, 1);
+        fetch(LAST, a_2, b_2, 2);
+        fetch(LAST, a_3, b_3, 3);
+        landed<3 * EACH>();
+        read(even, a_0, b_0, ra, rb);
+        // Step s: its fragments are in registers; the next one's have landed, and no wavefront reads this one's place any more.
+        auto turn = [&](auto last, Fragments &now, Fragments &next, char *a, char *b, const char *next_a, const char *next_b, uint32_t s) {
+            landed<2 * EACH>();
+            fetch(last, a, b, s + 4);
+            read(next, next_a, next_b, ra, rb);
+            multiply(now);
+            interleave();
+        };
+        auto four = [&](auto last, uint32_t s) {
+            turn(last, even, odd, a_0, b_0, a_1, b_1, s);
+            turn(last, odd, even, a_1, b_1, a_2, b_2, s + 1);
+            turn(last, even, odd, a_2, b_2, a_3, b_3, s + 2);
+            turn(last, odd, even, a_3, b_3, a_0, b_0, s + 3);
+        };
         uint32_t s = 0;
-        if (steps & 1u) {
-            fa.into(a_odd, 0, steps == 1);
-            fb.into(b_odd, 0, steps == 1);
-            __syncthreads();
-            if (steps > 1) {
-                fa.into(a_even, 1, false);
-                fb.into(b_even, 1, false);
-            }
-            step(a_odd, b_odd, ra, rb);
-            s = 1;
-        } else {
-            fa.into(a_even, 0, false);
-            fb.into(b_even, 0, false);
-        }
-        __syncthreads();
-        for (; s < steps; s += 2) {
-            fa.into(a_odd, s + 1, s + 2 == steps);
-            fb.into(b_odd, s + 1, s + 2 == steps);
-            step(a_even, b_even, ra, rb);
-            __syncthreads();
-            if (s + 2 < steps) {
-                fa.into(a_even, s + 2, false);
-                fb.into(b_even, s + 2, false);
-            }
-            step(a_odd, b_odd, ra, rb);
-            __syncthreads();
-        }
+        for (; s + 8 < steps; s += 4) four(NOT_LAST, s);        // (nothing that is asked for there is the last)
+        for (; s < steps; s += 4) four(LAST, s);
+        landed<0>();            // (places of steps that there are not are being filled with zeros)
     }
 
-    // A wavefront's part of LDS behind the loop: 16 rows of TA / WA elements, or TA / WA rows of 16
+    // A wavefront's part of LDS behind the loop: 16 rows of TA / WA elements
     static constexpr int PART = TA / WA * 16 * (int)sizeof(T);
     __device__ __forceinline__ char *part() const {
-        constexpr uint32_t HERE = TA * GM_ROW / PART;       // wavefronts whose parts the first run holds
+        constexpr uint32_t HERE = TA * GM_STEP / PART;      // wavefronts whose parts a run holds
         const uint32_t wave = threadIdx.x >> 6;
-        return HERE >= 8 || wave < HERE ? room[0] + wave * PART : room[1] + (wave - HERE) * PART;
+        if constexpr (HERE >= 4) return room[0] + wave * PART;
+        else return (wave < HERE ? room[0] : room[1]) + wave % HERE * PART;
     }
     static __device__ __forceinline__ void wave_sync() {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

@@ -13,6 +13,7 @@ namespace {
 constexpr uint32_t HD_THREADS = 1024;
 constexpr uint64_t HD_BUDGET = 1ull << 30;                  // bytes of a piece's gradients, and weights where they are padded
 constexpr uint64_t HD_PARTS = 1ull << 28;                   // ... of the sums of the loss's tiles
+constexpr int HD_TA = 256, HD_TB = 192;                     // a tile of sums
 constexpr uint32_t HD_PART = 128;                           // words of a wavefront of the logits' tiles
 
 struct RowInfo { float lse, factor, share; uint32_t unused; };     // g = (p factor - onehot) share
@@ -124,7 +125,7 @@ template <typename T> __device__ __forceinline__ float exp_of(float x) {
 
 // LOSS: a wavefront's largest logit and sum of exponentials of every row, and its label's logit (and, with g, the exponentials themselves, `room` times as
 // large); otherwise the gradients of the logits
-template <typename T, int TA, int TB, int WA, bool LOSS> __global__ __launch_bounds__(GM_THREADS) void k_head_logits(const LogitsArgs A) {
+template <typename T, int TA, int TB, int WA, bool LOSS> __global__ __launch_bounds__(GM_THREADS, 1) void k_head_logits(const LogitsArgs A) {
     typedef Tile<T, TA, TB, WA, ALONG, ALONG> Tl;
     const uint32_t n = A.R.count[0];
     const uint32_t a0 = blockIdx.x / A.tiles_b * TA, b0 = blockIdx.x % A.tiles_b * TB;
@@ -329,7 +330,7 @@ struct OutArgs {
     float scale, room;
 };
 // dx: sums over the piece's words, one share of them a split, added to those of the pieces before
-template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_THREADS) void k_head_dx(const OutArgs A) {
+template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_THREADS, 1) void k_head_dx(const OutArgs A) {
     typedef Tile<T, TA, TB, WA, ACROSS, ALONG> Tl;
     const uint32_t n = A.R.count[0];
     const uint32_t split = blockIdx.x % A.splits, tile = blockIdx.x / A.splits;
@@ -337,8 +338,8 @@ template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_TH
     if (b0 >= n) return;
     Side B = A.B;
     B.count = n;
-    const uint32_t steps = (A.ks + Tl::KS - 1) / Tl::KS;
-    const uint32_t from = (uint32_t)((uint64_t)steps * split / A.splits) * Tl::KS, to = (uint32_t)((uint64_t)steps * (split + 1) / A.splits) * Tl::KS;
+    const uint32_t turns = (A.ks + Tl::GRAIN - 1) / Tl::GRAIN;
+    const uint32_t from = (uint32_t)((uint64_t)turns * split / A.splits) * Tl::GRAIN, to = (uint32_t)((uint64_t)turns * (split + 1) / A.splits) * Tl::GRAIN;
     Tl t;
     t.run(A.A, B, a0, b0, from, (to < A.ks ? to : A.ks) - from);
     const typename Tl::At at = Tl::place();
@@ -365,7 +366,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_head_dx_out(const
         }
     }
 }
-template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_THREADS) void k_head_dw(const OutArgs A) {
+template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_THREADS, 1) void k_head_dw(const OutArgs A) {
     typedef Tile<T, TA, TB, WA, ACROSS, ACROSS> Tl;
     const uint32_t n = A.R.count[0];
     const uint32_t a0 = blockIdx.x / A.tiles_b * TA, b0 = blockIdx.x % A.tiles_b * TB;
@@ -405,7 +406,7 @@ uint64_t up_to(uint64_t v, uint64_t m) { return (v + m - 1) / m * m; }
 uint32_t blocks_of(uint64_t n) { return (uint32_t)(n < (1u << 20) ? n : 1u << 20); }
 
 template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
-    constexpr uint32_t ES = sizeof(T), STEP = GM_ROW / ES;
+    constexpr uint32_t ES = sizeof(T), STEP = 128 / ES;
     const hipStream_t stream = ctx->stream;
     const uint32_t wide = (uint32_t)up_to(C.width, STEP);
     const uint64_t rows_pad = up_to(C.n_rows, 256);
@@ -437,7 +438,7 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
     const uint64_t w_st = C.weight->stride;
     // rows of W go into the product as they lie where their vectors do not straddle; others are padded first, piece by piece
     const bool direct = ((uintptr_t)w % 16 == 0 && w_st * ES % 16 == 0 && (uint64_t)C.width * ES % 16 == 0 && w_st * ES * 256 < GM_NOWHERE);
-    const uint32_t tiles_b = (uint32_t)(rows_pad / 256);
+    const uint32_t tiles_b = (uint32_t)((C.n_rows + HD_TB - 1) / HD_TB);
     const uint64_t most_tiles = (1u << 22) / (tiles_b ? tiles_b : 1);
     const bool back = C.dx || C.d_weight;
     // words of a piece: what the budget holds of their gradients, of W padded, and of the sums of tiles
@@ -482,7 +483,7 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
             L.W = W; L.W.count = n_words;
             L.g = first == last_piece ? g : nullptr;
             const uint32_t tiles_a = (n_words + 255) / 256;
-            k_head_logits<T, 256, 256, 2, true><<<tiles_a * tiles_b, GM_THREADS, 0, stream>>>(L);
+            k_head_logits<T, HD_TA, HD_TB, 2, true><<<tiles_a * tiles_b, GM_THREADS, 0, stream>>>(L);
             RK_CHECK_LAUNCH(ctx, "k_head_logits");
             J.n_parts = tiles_a * 2;
             J.last = first == last_piece;
@@ -500,10 +501,14 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
     OutArgs O{};
     O.R = R; O.d_total = C.d_total; O.scale = C.head->logit_scale; O.room = room; O.width = C.width;
     if (C.dx) {
-        // as many shares of the words as fill the compute units
+        // the words in as many shares as leave the fewest compute units idle in the last turn; none shorter than 1,024 words
         const uint64_t tiles = (uint64_t)tiles_w * (tiles_b ? tiles_b : 1);
-        O.splits = (uint32_t)(tiles >= 256 ? 1 : (256 + tiles - 1) / tiles);
-        if (O.splits > words / 1024 + 1) O.splits = (uint32_t)(words / 1024 + 1);
+        double best = 0.0;
+        for (uint32_t n = 1; n <= 16 && n <= words / 1024 + 1; ++n) {
+            const uint64_t turns = (tiles * n + 255) / 256;
+            const double filled = (double)(tiles * n) / (double)(turns * 256) * (1.0 - 0.01 * n);
+            if (filled > best) { best = filled; O.splits = n; }
+        }
         O.stride = up_to(C.width, 4);
         O.split_stride = C.n_rows * O.stride;
         if ((rc = rk_scratch(ctx, SL_HEAD_DX, O.splits * O.split_stride * 4, (void **)&O.sums)) != RK_OK) return rc;
@@ -521,24 +526,24 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
         } else if (C.n_rows) {
             L.first = (uint32_t)first; L.words = n_words;
             L.W = W; L.W.count = n_words;
-            k_head_logits<T, 256, 256, 2, false><<<tiles_a * tiles_b, GM_THREADS, 0, stream>>>(L);
+            k_head_logits<T, HD_TA, HD_TB, 2, false><<<tiles_a * tiles_b, GM_THREADS, 0, stream>>>(L);
             RK_CHECK_LAUNCH(ctx, "k_head_logits");
         }
         if (C.dx && C.n_rows) {
             O.A = W; O.A.count = row_bytes;
             O.B = Side{(const char *)g, words * ES, 0};
             O.ks = n_words; O.tiles_b = tiles_b; O.first = first == last_piece;
-            k_head_dx<T, 256, 256, 2><<<tiles_w * tiles_b * O.splits, GM_THREADS, 0, stream>>>(O);
+            k_head_dx<T, HD_TA, HD_TB, 2><<<tiles_w * tiles_b * O.splits, GM_THREADS, 0, stream>>>(O);
             RK_CHECK_LAUNCH(ctx, "k_head_dx");
         }
         if (C.d_weight) {
             OutArgs D = O;
             D.A = X; D.A.count = (uint64_t)wide * ES;
             D.B = Side{(const char *)g, words * ES, words * ES};
-            D.tiles_b = tiles_a; D.words = n_words;
+            D.tiles_b = (n_words + HD_TB - 1) / HD_TB; D.words = n_words;
             D.aligned = (uintptr_t)C.d_weight->data % 16 == 0 && C.d_weight->stride * ES % 16 == 0;
             D.out = (T *)C.d_weight->data + first * C.d_weight->stride; D.stride = C.d_weight->stride;
-            k_head_dw<T, 256, 256, 2><<<tiles_w * tiles_a, GM_THREADS, 0, stream>>>(D);
+            k_head_dw<T, HD_TA, HD_TB, 2><<<tiles_w * D.tiles_b, GM_THREADS, 0, stream>>>(D);
             RK_CHECK_LAUNCH(ctx, "k_head_dw");
         }
         if (first == 0) break;
