@@ -20,22 +20,19 @@
 
 namespace {
 
-constexpr uint32_t GM_THREADS = 256, GM_STEP = 64;          // threads; bytes of k of a step
+constexpr uint32_t GM_WAVES = 8, GM_THREADS = 64 * GM_WAVES, GM_STEP = 64;          // threads; bytes of k of a step
 constexpr uint32_t GM_NOWHERE = 0x80000000u;                // a lane's place behind every buffer: zeros
 
-// (builtins of this GPU alone: the host's pass over the source does not know them)
-template <typename T> __device__ __forceinline__ Vec<float, 4> products(const Vec<uint32_t, 4> &a, const Vec<uint32_t, 4> &b, Vec<float, 4> c) {
+// c += a b, the sums staying in their registers (as a builtin, whose result may go anywhere, they wander from step to step, and what does not
+// fit then is spilled).  The instruction's hazards are the caller's: sums are taken again three products later at the earliest, and read
+// by others behind settle().
+// (instructions and builtins of this GPU alone: the host's pass over the source does not know them)
+template <typename T> __device__ __forceinline__ void product(const Vec<uint32_t, 4> &a, const Vec<uint32_t, 4> &b, int q, Vec<float, 4> &c) {
 #ifdef __HIP_DEVICE_COMPILE__
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0, 0, 0);
-    } else if constexpr (__is_same(T, __bf16)) {
-        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Vec<__bf16, 8>, a), __builtin_bit_cast(Vec<__bf16, 8>, b), c, 0, 0, 0);
-    } else {
-        c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(Vec<_Float16, 8>, a), __builtin_bit_cast(Vec<_Float16, 8>, b), c, 0, 0, 0);
-    }
+    if constexpr (sizeof(T) == 4) asm volatile("v_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+v"(c) : "v"(a[q]), "v"(b[q]));
+    else if constexpr (__is_same(T, __bf16)) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
+    else asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
 #endif
-    return c;
 }
 __device__ __forceinline__ void into_lds(__amdgpu_buffer_rsrc_t buf, char *lds, uint32_t at) {
 #ifdef __HIP_DEVICE_COMPILE__
@@ -67,21 +64,17 @@ struct Side {
     uint64_t stride;            // bytes from row to row
     uint64_t count;             // ALONG: rows; ACROSS: bytes of a row
 };
-// ACROSS: where a piece of k's row lies among the row's PIECES (place), and which one lies there (piece): pairs of pieces move
-// (of 32-bit elements fours), by a step for every k that is read together
-template <typename T, uint32_t PIECES> struct Order {
-    static constexpr bool POWER = (PIECES & (PIECES - 1)) == 0;
-    static __device__ __forceinline__ uint32_t by(uint32_t k) {
-        if constexpr (sizeof(T) == 4) return (k >> 2 & 3u) * 4u % PIECES;
-        else return ((k & 3u) | (k >> 3 & 3u) << 2) * 2u % PIECES;
-    }
-    static __device__ __forceinline__ uint32_t place(uint32_t piece, uint32_t k) { return POWER ? piece ^ by(k) : (piece + by(k)) % PIECES; }
-    static __device__ __forceinline__ uint32_t piece(uint32_t place, uint32_t k) { return POWER ? place ^ by(k) : (place + PIECES - by(k)) % PIECES; }
-};
+// ACROSS: a piece of k's row lies at piece ^ order_of(k): pairs of pieces change places (of 32-bit elements fours), differently for all k that
+// are read together
+template <typename T, uint32_t PIECES> __device__ __forceinline__ uint32_t order_of(uint32_t k) {
+    static_assert((PIECES & (PIECES - 1)) == 0, "");
+    if constexpr (sizeof(T) == 4) return (k >> 2 & 3u) * 4u % PIECES;
+    else return ((k & 3u) | (k >> 3 & 3u) << 2) * 2u % PIECES;
+}
 // What a wavefront asks for of a tile of R elements: R / 64 instructions of 1,024 bytes, of small tiles one, some of them twice, so that
 // every wavefront has as many under way.
 template <typename T, int R, int WAY> struct Fetch {
-    static constexpr int N = R >= 64 ? R / 64 : 1;
+    static constexpr int N = (R / 16 + (int)GM_WAVES - 1) / (int)GM_WAVES;
     static constexpr uint32_t KS = GM_STEP / sizeof(T), PIECES = R * sizeof(T) / 16;    // k of a step; ACROSS: pieces of a row of LDS
     const char *base;
     uint64_t hop;               // bytes from step to step
@@ -106,7 +99,7 @@ template <typename T, int R, int WAY> struct Fetch {
             hop = KS * s.stride;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const uint32_t x = part(i) * 64 + lane, k = x / PIECES, piece = Order<T, PIECES>::piece(x % PIECES, k);
+                const uint32_t x = part(i) * 64 + lane, k = x / PIECES, piece = (x % PIECES) ^ order_of<T, PIECES>(k);
                 at[i] = first * sizeof(T) + piece * 16 < s.count ? k * (uint32_t)s.stride + piece * 16 : GM_NOWHERE;
                 tail[i] = k < left ? at[i] : GM_NOWHERE;
             }
@@ -119,38 +112,37 @@ template <typename T, int R, int WAY> struct Fetch {
         for (int i = 0; i < N; ++i) into_lds(buf, lds + part(i) * 1024, !LAST || s + 1 < steps ? at[i] : s < steps ? tail[i] : GM_NOWHERE);
     }
 };
-// A wavefront's fragments of M times sixteen elements, from element `first` of the tile on
-template <typename T, int R, int WAY, int M> struct Reader {
+// A wavefront's fragments, sixteen elements each, from element `first` of the tile on (a multiple of what the wavefront has)
+template <typename T, int R, int WAY> struct Reader {
     static constexpr uint32_t PITCH = R * sizeof(T), PIECES = PITCH / 16;
-    uint32_t at[WAY == ALONG ? 1 : M];
+    uint32_t at;
     __device__ __forceinline__ Reader(uint32_t first) {
         const uint32_t lane = threadIdx.x & 63u, j = lane & 15u, g = lane >> 4;
         if constexpr (WAY == ALONG) {
-            at[0] = (first + j) * GM_STEP + (g ^ (j >> 2)) * 16;
+            at = (first + j) * GM_STEP + (g ^ (j >> 2)) * 16;
+        } else if constexpr (sizeof(T) == 4) {
+            const uint32_t k = 4 * g, piece = first / 4 + (j >> 2);
+            at = k * PITCH + (piece ^ order_of<T, PIECES>(k)) * 16 + (j & 3u) * 4;
         } else {
-#pragma unroll
-            for (int i = 0; i < M; ++i) {
-                if constexpr (sizeof(T) == 4) {
-                    const uint32_t k = 4 * g, piece = (first + 16 * i) / 4 + (j >> 2);
-                    at[i] = k * PITCH + Order<T, PIECES>::place(piece, k) * 16 + (j & 3u) * 4;
-                } else {
-                    const uint32_t k = 8 * g + (j >> 2), piece = (first + 16 * i) / 8 + (j >> 1 & 1u);
-                    at[i] = k * PITCH + Order<T, PIECES>::place(piece, k) * 16 + (j & 1u) * 8;
-                }
-            }
+            const uint32_t k = 8 * g + (j >> 2), piece = first / 8 + (j >> 1 & 1u);
+            at = k * PITCH + (piece ^ order_of<T, PIECES>(k)) * 16 + (j & 1u) * 8;
         }
     }
+    // fragment i (ACROSS: its pieces' numbers differ from the first one's in bits that these do not have, and so do their places)
     __device__ __forceinline__ Vec<uint32_t, 4> read(const char *lds, int i) const {
         if constexpr (WAY == ALONG) {
-            return *(const Vec<uint32_t, 4> *)(lds + at[0] + i * 16 * GM_STEP);
-        } else if constexpr (sizeof(T) == 4) {
-            Vec<uint32_t, 4> w;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) w[q] = *(const uint32_t *)(lds + at[i] + q * PITCH);
-            return w;
+            return *(const Vec<uint32_t, 4> *)(lds + at + i * 16 * GM_STEP);
         } else {
-            const Vec<uint32_t, 2> lo = turned(lds + at[i]), hi = turned(lds + at[i] + 4 * PITCH);
-            return Vec<uint32_t, 4>{lo[0], lo[1], hi[0], hi[1]};
+            const char *const p = lds + (at ^ (uint32_t)(i * 16 * sizeof(T)));
+            if constexpr (sizeof(T) == 4) {
+                Vec<uint32_t, 4> w;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) w[q] = *(const uint32_t *)(p + q * PITCH);
+                return w;
+            } else {
+                const Vec<uint32_t, 2> lo = turned(p), hi = turned(p + 4 * PITCH);
+                return Vec<uint32_t, 4>{lo[0], lo[1], hi[0], hi[1]};
+            }
         }
     }
 };
@@ -158,12 +150,12 @@ template <typename T, int R, int WAY, int M> struct Reader {
 // The tile at (a0, b0) over ks of k from k0 on; WA x WB wavefronts share it.  acc[i][j]: lane l holds the elements
 // a = a0 + wa TA/WA + 16 i + 4 (l / 16) + 0..3,  b = b0 + wb TB/WB + 16 j + l % 16.
 template <typename T, int TA, int TB, int WA, int WAY_A, int WAY_B> struct Tile {
-    static constexpr int WB = 4 / WA, MA = TA / WA / 16, MB = TB / WB / 16;
+    static constexpr int WB = (int)GM_WAVES / WA, MA = TA / WA / 16, MB = TB / WB / 16;
     static constexpr uint32_t KS = GM_STEP / sizeof(T), GRAIN = 4 * KS;         // k of a step; of a turn of the loop, which is done whole
     typedef Fetch<T, TA, WAY_A> FetchA;
     typedef Fetch<T, TB, WAY_B> FetchB;
-    typedef Reader<T, TA, WAY_A, MA> ReadA;
-    typedef Reader<T, TB, WAY_B, MB> ReadB;
+    typedef Reader<T, TA, WAY_A> ReadA;
+    typedef Reader<T, TB, WAY_B> ReadB;
     static constexpr int EACH = FetchA::N + FetchB::N;                          // a wavefront's loads of a step
     Vec<float, 4> acc[MA][MB];
     struct Fragments { Vec<uint32_t, 4> a[MA], b[MB]; };
@@ -184,28 +176,36 @@ template <typename T, int TA, int TB, int WA, int WAY_A, int WAY_B> struct Tile 
 #pragma unroll
         for (int i = 0; i < MA; ++i) f.a[i] = ra.read(a, i);
     }
-    __device__ __forceinline__ void multiply(const Fragments &f) {
+    // The products of `now`, with the next step's reads among them, in the first three quarters: what stands between two lines of products stays there.
+    __device__ __forceinline__ void multiply(const Fragments &now, Fragments &next, const char *a, const char *b, const ReadA &ra, const ReadB &rb) {
+        constexpr int READS = MA + MB, LINES = MA * 3 / 4 > 0 ? MA * 3 / 4 : 1;
+#pragma unroll
+        for (int i = 0; i < MA; ++i) {
+#pragma unroll
+            for (int r = 0; r < READS; ++r)
+                if (r * LINES / READS == i) {
+                    if (r < MB) next.b[r] = rb.read(b, r); else next.a[r - MB] = ra.read(a, r - MB);
+                }
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int q = 0; q < (sizeof(T) == 4 ? 4 : 1); ++q)
+#pragma unroll
+                for (int j = 0; j < MB; ++j) product<T>(now.a[i], now.b[j], q, acc[i][j]);
+        }
+    }
+    // the sums as others may read them: the last products have been through the matrix units
+    __device__ __forceinline__ void settle() {
+#ifdef __HIP_DEVICE_COMPILE__
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
         for (int i = 0; i < MA; ++i)
 #pragma unroll
-            for (int j = 0; j < MB; ++j) acc[i][j] = products<T>(f.a[i], f.b[j], acc[i][j]);
-    }
-    // loads and reads among the products, not before them
-    static __device__ __forceinline__ void interleave() {
-#ifdef __HIP_DEVICE_COMPILE__
-        constexpr int PRODUCTS = MA * MB * (sizeof(T) == 4 ? 4 : 1), READS_A = WAY_A == ALONG ? 1 : sizeof(T) == 4 ? 4 : 2, READS_B = WAY_B == ALONG ? 1 : sizeof(T) == 4 ? 4 : 2;
-        constexpr int READS = MA * READS_A + MB * READS_B, GROUPS = MA + MB, AT = PRODUCTS / GROUPS;
-        if constexpr (AT >= 1) {
-#pragma unroll
-            for (int i = 0; i < GROUPS; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x100, (READS + GROUPS - 1) / GROUPS, 0);
-                if (i < EACH) __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x8, AT, 0);
-            }
-        }
+            for (int j = 0; j < MB; ++j) asm volatile("" : "+v"(acc[i][j]));
 #endif
     }
-    char *room[4];              // four runs of TA * GM_STEP bytes of LDS, free behind the loop
+    // a wavefront's part of LDS behind the loop: 16 rows of TA / WA elements
+    static constexpr int PART = TA / WA * 16 * (int)sizeof(T);
+    char *part;
 
     __device__ __forceinline__ void run(const Side &A, const Side &B, uint64_t a0, uint64_t b0, uint64_t k0, uint32_t ks) {
         __shared__ __attribute__((aligned(128))) char a_0[TA * GM_STEP], a_1[TA * GM_STEP], a_2[TA * GM_STEP], a_3[TA * GM_STEP];
@@ -214,7 +214,11 @@ template <typename T, int TA, int TB, int WA, int WAY_A, int WAY_B> struct Tile 
         for (int i = 0; i < MA; ++i)
 #pragma unroll
             for (int j = 0; j < MB; ++j) acc[i][j] = 0.f;
-        room[0] = a_0; room[1] = a_1; room[2] = a_2; room[3] = a_3;
+        {
+            constexpr uint32_t HERE = TA * GM_STEP / PART;  // wavefronts whose parts one of the places holds
+            const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), run = wave / HERE;
+            part = (run == 0 ? a_0 : run == 1 ? a_1 : run == 2 ? a_2 : a_3) + wave % HERE * PART;
+        }
         const uint32_t steps = (ks + KS - 1) / KS;
         if (steps == 0) return;
         const FetchA fa(A, a0, k0, ks);
@@ -238,9 +242,7 @@ template <typename T, int TA, int TB, int WA, int WAY_A, int WAY_B> struct Tile 
         auto turn = [&](auto last, Fragments &now, Fragments &next, char *a, char *b, const char *next_a, const char *next_b, uint32_t s) {
             landed<2 * EACH>();
             fetch(last, a, b, s + 4);
-            read(next, next_a, next_b, ra, rb);
-            multiply(now);
-            interleave();
+            multiply(now, next, next_a, next_b, ra, rb);
         };
         auto four = [&](auto last, uint32_t s) {
             turn(last, even, odd, a_0, b_0, a_1, b_1, s);
@@ -251,17 +253,10 @@ template <typename T, int TA, int TB, int WA, int WAY_A, int WAY_B> struct Tile 
         uint32_t s = 0;
         for (; s + 8 < steps; s += 4) four(NOT_LAST, s);        // (nothing that is asked for there is the last)
         for (; s < steps; s += 4) four(LAST, s);
+        settle();
         landed<0>();            // (places of steps that there are not are being filled with zeros)
     }
 
-    // A wavefront's part of LDS behind the loop: 16 rows of TA / WA elements
-    static constexpr int PART = TA / WA * 16 * (int)sizeof(T);
-    __device__ __forceinline__ char *part() const {
-        constexpr uint32_t HERE = TA * GM_STEP / PART;      // wavefronts whose parts a run holds
-        const uint32_t wave = threadIdx.x >> 6;
-        if constexpr (HERE >= 4) return room[0] + wave * PART;
-        else return (wave < HERE ? room[0] : room[1]) + wave % HERE * PART;
-    }
     static __device__ __forceinline__ void wave_sync() {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -271,7 +266,7 @@ template <typename T, int TA, int TB, int WA, int WAY_A, int WAY_B> struct Tile 
     // in the tile).  A row's pieces lie in the order piece ^ row.
     template <typename Value, typename Sink> __device__ __forceinline__ void rows(Value value, Sink sink) {
         constexpr uint32_t PIECES = TA / WA * sizeof(T) / 16, AT_ONCE = 64 / PIECES, EACH = 16 / sizeof(T);
-        char *const lds = part();
+        char *const lds = part;
         const At at = place();
         const uint32_t first_a = at.a - 4 * (at.lane >> 4), first_b = at.b - (at.lane & 15u);
 #pragma unroll

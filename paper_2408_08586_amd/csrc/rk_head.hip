@@ -13,7 +13,7 @@ namespace {
 constexpr uint32_t HD_THREADS = 1024;
 constexpr uint64_t HD_BUDGET = 1ull << 30;                  // bytes of a piece's gradients, and weights where they are padded
 constexpr uint64_t HD_PARTS = 1ull << 28;                   // ... of the sums of the loss's tiles
-constexpr int HD_TA = 256, HD_TB = 192;                     // a tile of sums
+constexpr int HD_TA = 256, HD_TB = 256;                     // a tile of sums
 constexpr uint32_t HD_PART = 128;                           // words of a wavefront of the logits' tiles
 
 struct RowInfo { float lse, factor, share; uint32_t unused; };     // g = (p factor - onehot) share
@@ -125,7 +125,7 @@ template <typename T> __device__ __forceinline__ float exp_of(float x) {
 
 // LOSS: a wavefront's largest logit and sum of exponentials of every row, and its label's logit (and, with g, the exponentials themselves, `room` times as
 // large); otherwise the gradients of the logits
-template <typename T, int TA, int TB, int WA, bool LOSS> __global__ __launch_bounds__(GM_THREADS, 1) void k_head_logits(const LogitsArgs A) {
+template <typename T, int TA, int TB, int WA, bool LOSS> __global__ __launch_bounds__(GM_THREADS) void k_head_logits(const LogitsArgs A) {
     typedef Tile<T, TA, TB, WA, ALONG, ALONG> Tl;
     const uint32_t n = A.R.count[0];
     const uint32_t a0 = blockIdx.x / A.tiles_b * TA, b0 = blockIdx.x % A.tiles_b * TB;
@@ -330,7 +330,7 @@ struct OutArgs {
     float scale, room;
 };
 // dx: sums over the piece's words, one share of them a split, added to those of the pieces before
-template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_THREADS, 1) void k_head_dx(const OutArgs A) {
+template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_THREADS) void k_head_dx(const OutArgs A) {
     typedef Tile<T, TA, TB, WA, ACROSS, ALONG> Tl;
     const uint32_t n = A.R.count[0];
     const uint32_t split = blockIdx.x % A.splits, tile = blockIdx.x / A.splits;
@@ -366,7 +366,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_head_dx_out(const
         }
     }
 }
-template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_THREADS, 1) void k_head_dw(const OutArgs A) {
+template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_THREADS) void k_head_dw(const OutArgs A) {
     typedef Tile<T, TA, TB, WA, ACROSS, ACROSS> Tl;
     const uint32_t n = A.R.count[0];
     const uint32_t a0 = blockIdx.x / A.tiles_b * TA, b0 = blockIdx.x % A.tiles_b * TB;
