@@ -292,4 +292,18 @@ template <typename T, int TA, int TB, int WA, int WAY_A, int WAY_B> struct Tile 
     }
 };
 
+// Which tile a workgroup has.  Workgroups go to the eight dies in turn, each with its own L2: a die gets a run of the tiles, and in a
+// run eight tiles of b are done for one of a before the next, so that what works at the same time shares both sides.
+constexpr uint32_t GM_DIES = 8, GM_GROUP = 8;
+struct Turn { uint32_t a, b; };
+__device__ __forceinline__ uint32_t in_runs(uint32_t block, uint32_t blocks) {
+    const uint32_t die = block % GM_DIES, each = blocks / GM_DIES, more = blocks % GM_DIES;
+    return die * each + (die < more ? die : more) + block / GM_DIES;
+}
+__device__ __forceinline__ Turn turn_of(uint32_t i, uint32_t tiles_a, uint32_t tiles_b) {
+    const uint32_t group = i / (tiles_a * GM_GROUP), rest = i - group * tiles_a * GM_GROUP;
+    const uint32_t wide = tiles_b - group * GM_GROUP < GM_GROUP ? tiles_b - group * GM_GROUP : GM_GROUP;
+    return Turn{rest / wide, group * GM_GROUP + rest % wide};
+}
+
 }  // namespace

@@ -128,7 +128,8 @@ template <typename T> __device__ __forceinline__ float exp_of(float x) {
 template <typename T, int TA, int TB, int WA, bool LOSS> __global__ __launch_bounds__(GM_THREADS) void k_head_logits(const LogitsArgs A) {
     typedef Tile<T, TA, TB, WA, ALONG, ALONG> Tl;
     const uint32_t n = A.R.count[0];
-    const uint32_t a0 = blockIdx.x / A.tiles_b * TA, b0 = blockIdx.x % A.tiles_b * TB;
+    const Turn at_turn = turn_of(in_runs(blockIdx.x, gridDim.x), gridDim.x / A.tiles_b, A.tiles_b);
+    const uint32_t a0 = at_turn.a * TA, b0 = at_turn.b * TB;
     if (b0 >= n) return;
     Side X = A.X;
     X.count = n;
@@ -333,8 +334,9 @@ struct OutArgs {
 template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_THREADS) void k_head_dx(const OutArgs A) {
     typedef Tile<T, TA, TB, WA, ACROSS, ALONG> Tl;
     const uint32_t n = A.R.count[0];
-    const uint32_t split = blockIdx.x % A.splits, tile = blockIdx.x / A.splits;
-    const uint32_t a0 = tile / A.tiles_b * TA, b0 = tile % A.tiles_b * TB;
+    const uint32_t i = in_runs(blockIdx.x, gridDim.x), tiles = gridDim.x / A.splits, split = i / tiles;
+    const Turn at_turn = turn_of(i - split * tiles, tiles / A.tiles_b, A.tiles_b);
+    const uint32_t a0 = at_turn.a * TA, b0 = at_turn.b * TB;
     if (b0 >= n) return;
     Side B = A.B;
     B.count = n;
@@ -369,7 +371,8 @@ template <typename T> __global__ __launch_bounds__(256) void k_head_dx_out(const
 template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_THREADS) void k_head_dw(const OutArgs A) {
     typedef Tile<T, TA, TB, WA, ACROSS, ACROSS> Tl;
     const uint32_t n = A.R.count[0];
-    const uint32_t a0 = blockIdx.x / A.tiles_b * TA, b0 = blockIdx.x % A.tiles_b * TB;
+    const Turn at_turn = turn_of(in_runs(blockIdx.x, gridDim.x), gridDim.x / A.tiles_b, A.tiles_b);
+    const uint32_t a0 = at_turn.a * TA, b0 = at_turn.b * TB;
     Tl t;
     t.run(A.A, A.B, a0, b0, 0, n);
     const float f = n ? (A.d_total ? *A.d_total : 1.f) * A.scale * (__uint_as_float(A.R.count[1]) / A.room) : 0.f;
