@@ -178,19 +178,33 @@ template <typename T, int TA, int TB, int WA, int WAY_A, int WAY_B> struct Tile 
     }
     // The products of `now`, with the next step's reads among them, in the first three quarters: what stands between two lines of products stays there.
     __device__ __forceinline__ void multiply(const Fragments &now, Fragments &next, const char *a, const char *b, const ReadA &ra, const ReadB &rb) {
-        constexpr int READS = MA + MB, LINES = MA * 3 / 4 > 0 ? MA * 3 / 4 : 1;
-#pragma unroll
-        for (int i = 0; i < MA; ++i) {
+        constexpr int READS = MA + MB, LINES = MB >= 4 && MA * 3 / 4 > 0 ? MA * 3 / 4 : 1, PARTS = sizeof(T) == 4 ? 4 : 1;
+        auto reads = [&](int line) {
 #pragma unroll
             for (int r = 0; r < READS; ++r)
-                if (r * LINES / READS == i) {
+                if (r * LINES / READS == line) {
                     if (r < MB) next.b[r] = rb.read(b, r); else next.a[r - MB] = ra.read(a, r - MB);
                 }
             asm volatile("" ::: "memory");
+        };
+        if constexpr (MB >= 4) {
 #pragma unroll
-            for (int q = 0; q < (sizeof(T) == 4 ? 4 : 1); ++q)
+            for (int i = 0; i < MA; ++i) {
+                reads(i);
 #pragma unroll
-                for (int j = 0; j < MB; ++j) product<T>(now.a[i], now.b[j], q, acc[i][j]);
+                for (int q = 0; q < PARTS; ++q)
+#pragma unroll
+                    for (int j = 0; j < MB; ++j) product<T>(now.a[i], now.b[j], q, acc[i][j]);
+            }
+        } else {
+            static_assert(MA * MB >= 4, "");                // (three others between two products for the same sums)
+            reads(0);
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q)
+#pragma unroll
+                for (int i = 0; i < MA; ++i)
+#pragma unroll
+                    for (int j = 0; j < MB; ++j) product<T>(now.a[i], now.b[j], q, acc[i][j]);
         }
     }
     // the sums as others may read them: the last products have been through the matrix units
@@ -206,6 +220,7 @@ template <typename T, int TA, int TB, int WA, int WAY_A, int WAY_B> struct Tile 
     // a wavefront's part of LDS behind the loop: 16 rows of TA / WA elements
     static constexpr int PART = TA / WA * 16 * (int)sizeof(T);
     char *part;
+    char *shared;               // ... and one of all wavefronts, 8 bytes for every WA and TB
 
     __device__ __forceinline__ void run(const Side &A, const Side &B, uint64_t a0, uint64_t b0, uint64_t k0, uint32_t ks) {
         __shared__ __attribute__((aligned(128))) char a_0[TA * GM_STEP], a_1[TA * GM_STEP], a_2[TA * GM_STEP], a_3[TA * GM_STEP];
@@ -217,6 +232,8 @@ template <typename T, int TA, int TB, int WA, int WAY_A, int WAY_B> struct Tile 
         {
             constexpr uint32_t HERE = TA * GM_STEP / PART;  // wavefronts whose parts one of the places holds
             const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), run = wave / HERE;
+            static_assert(WA * TB * 8 <= TB * GM_STEP, "");
+            shared = b_0;
             part = (run == 0 ? a_0 : run == 1 ? a_1 : run == 2 ? a_2 : a_3) + wave % HERE * PART;
         }
         const uint32_t steps = (ks + KS - 1) / KS;

@@ -1,7 +1,7 @@
 // The loss of rows under a vocabulary's weights and its gradients, without keeping the logits (rk_head in rubick.h).
 //
 // Rows that count are gathered first, so that products take no others, and padded with zeros to whole steps of k.  The loss
-// takes the logits' tiles out of the product's registers: of every row the largest and the sum of exponentials over a wavefront's
+// takes the logits' tiles out of the product's registers: of every row the largest and the sum of exponentials over a tile's
 // words, joined in fixed order.  The gradients go through the vocabulary in pieces, from the last to the first: a piece's logits are made again and become
 // g = row_weight (p (1 + 2 z lse) - onehot), rounded to the rows' type and scaled by a power of two that keeps float16 in its range;
 // dx adds up g W over the pieces in float32, and the piece's rows of d_weight are g^T x.  Where the loss is made along with
@@ -13,8 +13,7 @@ namespace {
 constexpr uint32_t HD_THREADS = 1024;
 constexpr uint64_t HD_BUDGET = 1ull << 30;                  // bytes of a piece's gradients, and weights where they are padded
 constexpr uint64_t HD_PARTS = 1ull << 28;                   // ... of the sums of the loss's tiles
-constexpr int HD_TA = 256, HD_TB = 256;                     // a tile of sums
-constexpr uint32_t HD_PART = 128;                           // words of a wavefront of the logits' tiles
+constexpr int HD_TA = 256;                                  // words, or columns, of a tile
 
 struct RowInfo { float lse, factor, share; uint32_t unused; };     // g = (p factor - onehot) share
 
@@ -78,8 +77,6 @@ __global__ __launch_bounds__(HD_THREADS) void k_head_rows(const RowsArgs A) {
                 A.R.row[at] = (int32_t)r;
                 A.R.label[at] = label[e];
                 A.R.weight[at] = weight[e];
-                A.R.top[at] = -INFINITY;
-                A.R.sum[at] = 0.f;
                 ++at;
             } else if (A.loss) {
                 A.loss[r] = 0.f;
@@ -113,7 +110,7 @@ struct LogitsArgs {
     uint32_t width, tiles_b;
     uint32_t first, words;      // the piece's first word, how many it has
     float scale, room;
-    float2 *parts;              // loss: [words / (TA / WA)][kept rows]
+    float2 *parts;              // loss: [words / TA][kept rows]
     uint64_t parts_stride;
     void *g;                    // [kept rows][g_stride]: gradients, or what the loss leaves of them (null: nothing)
     uint64_t g_stride;
@@ -123,7 +120,7 @@ template <typename T> __device__ __forceinline__ float exp_of(float x) {
     else return __builtin_amdgcn_exp2f(x * 1.4426950408889634f);
 }
 
-// LOSS: a wavefront's largest logit and sum of exponentials of every row, and its label's logit (and, with g, the exponentials themselves, `room` times as
+// LOSS: a tile's largest logit and sum of exponentials of every row, and its label's logit (and, with g, the exponentials themselves, `room` times as
 // large); otherwise the gradients of the logits
 template <typename T, int TA, int TB, int WA, bool LOSS> __global__ __launch_bounds__(GM_THREADS) void k_head_logits(const LogitsArgs A) {
     typedef Tile<T, TA, TB, WA, ALONG, ALONG> Tl;
@@ -138,12 +135,15 @@ template <typename T, int TA, int TB, int WA, bool LOSS> __global__ __launch_bou
     const typename Tl::At at = Tl::place();
     const uint32_t a_of = a0 + at.a, b_of = b0 + at.b;
     if constexpr (LOSS) {
+        float *const tops = (float *)t.shared, *const sums = tops + WA * TB;
+        const uint32_t wa = at.a / (TA / WA), in_tile = at.b;           // (the wavefront's place, and its rows' in the tile)
+        float top[Tl::MB];
 #pragma unroll
         for (int j = 0; j < Tl::MB; ++j) {
             const uint32_t b = b_of + 16 * j;
-            const bool there = b < n;
-            const int64_t label = there ? (int64_t)A.R.label[b] - (int64_t)A.first : -1;
-            float top = -INFINITY, own = 0.f;
+            const int64_t label = b < n ? (int64_t)A.R.label[b] - (int64_t)A.first : -1;
+            float own = 0.f;
+            top[j] = -INFINITY;
 #pragma unroll
             for (int i = 0; i < Tl::MA; ++i)
 #pragma unroll
@@ -152,15 +152,22 @@ template <typename T, int TA, int TB, int WA, bool LOSS> __global__ __launch_bou
                     float l = t.acc[i][j][q] * A.scale;
                     l = a < A.words ? l : -INFINITY;
                     t.acc[i][j][q] = l;
-                    top = fmaxf(top, l);
+                    top[j] = fmaxf(top[j], l);
                     own = label == (int64_t)a ? l : own;
                 }
             const uint32_t d = (uint32_t)(label - (int64_t)a_of);
             if (label >= 0 && d < 16 * Tl::MA && (d & 15u) < 4) A.R.label_logit[b] = own;
-            top = fmaxf(top, __shfl_xor(top, 16, 64));
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            top[j] = fmaxf(top[j], __shfl_xor(top[j], 16, 64));
+            top[j] = fmaxf(top[j], __shfl_xor(top[j], 32, 64));
+            if (at.lane < 16) tops[wa * TB + in_tile + 16 * j] = top[j];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < Tl::MB; ++j) {
+#pragma unroll
+            for (uint32_t w = 0; w < WA; ++w) top[j] = fmaxf(top[j], tops[w * TB + in_tile + 16 * j]);
+            const float from = top[j] == -INFINITY ? 0.f : top[j];
             float sum = 0.f;
-            const float from = top == -INFINITY ? 0.f : top;
 #pragma unroll
             for (int i = 0; i < Tl::MA; ++i)
 #pragma unroll
@@ -171,7 +178,14 @@ template <typename T, int TA, int TB, int WA, bool LOSS> __global__ __launch_bou
                 }
             sum += __shfl_xor(sum, 16, 64);
             sum += __shfl_xor(sum, 32, 64);
-            if (there && at.lane < 16) A.parts[(uint64_t)(a_of / (TA / WA)) * A.parts_stride + b] = make_float2(top, sum);
+            if (at.lane < 16) sums[wa * TB + in_tile + 16 * j] = sum;
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __syncthreads();
+        for (uint32_t b = threadIdx.x; b < TB && b0 + b < n; b += GM_THREADS) {
+            float m = tops[b], s = sums[b];
+            for (uint32_t w = 1; w < WA; ++w) { m = fmaxf(m, tops[w * TB + b]); s += sums[w * TB + b]; }
+            A.parts[(uint64_t)at_turn.a * A.parts_stride + b0 + b] = make_float2(m, s);
         }
     }
     if constexpr (!LOSS) {
@@ -199,7 +213,7 @@ template <typename T, int TA, int TB, int WA, bool LOSS> __global__ __launch_bou
                });
 }
 
-// What the loss left of a piece becomes its gradients: each wavefront's words had their own largest logit.  A workgroup takes rows of 2,048 words.
+// What the loss left of a piece becomes its gradients: each tile's words had their own largest logit.  A workgroup takes rows of 2,048 words.
 struct ScaleArgs {
     Rows R;
     const float2 *parts;
@@ -234,14 +248,15 @@ struct JoinArgs {
     const float2 *parts;
     uint64_t parts_stride;
     uint32_t n_parts;
-    bool last;
+    bool first, last;           // of the pieces
     float z_weight;
     float *loss, *lse, *total;
     uint64_t n_rows;
 };
-// sixteen lanes a row: a row's parts in sixteen runs, joined in fixed order
-__global__ __launch_bounds__(256) void k_head_join(const JoinArgs A) {
-    __shared__ float2 runs[16][16];
+// 64 lanes a row: a row's parts in as many runs, joined in fixed order
+constexpr uint32_t HD_RUNS = 64;
+__global__ __launch_bounds__(16 * HD_RUNS) void k_head_join(const JoinArgs A) {
+    __shared__ float2 runs[HD_RUNS][16];
     const uint32_t n = A.R.count[0];
     const uint32_t x = threadIdx.x & 15u, y = threadIdx.x >> 4;
     const uint32_t i = blockIdx.x * 16u + x;
@@ -253,15 +268,19 @@ __global__ __launch_bounds__(256) void k_head_join(const JoinArgs A) {
     if (blockIdx.x * 16u >= n) return;
     float m = -INFINITY, s = 0.f;
     if (i < n) {
-        const uint32_t each = (A.n_parts + 15) / 16, end = min(A.n_parts, (y + 1) * each);
+        const uint32_t each = (A.n_parts + HD_RUNS - 1) / HD_RUNS, end = min(A.n_parts, (y + 1) * each);
         for (uint32_t p = y * each; p < end; ++p) add(m, s, A.parts[(uint64_t)p * A.parts_stride + i]);
     }
     runs[y][x] = make_float2(m, s);
-    __syncthreads();
+    for (uint32_t d = HD_RUNS / 2; d; d /= 2) {
+        __syncthreads();
+        if (y < d) {
+            add(m, s, runs[y + d][x]);
+            runs[y][x] = make_float2(m, s);
+        }
+    }
     if (y || i >= n) return;
-    m = A.R.top[i]; s = A.R.sum[i];
-#pragma unroll
-    for (int k = 0; k < 16; ++k) add(m, s, runs[k][x]);
+    if (!A.first) add(m, s, make_float2(A.R.top[i], A.R.sum[i]));
     A.R.top[i] = m; A.R.sum[i] = s;
     if (!A.last) return;
     const float lse = m + logf(s), loss = lse - A.R.label_logit[i] + A.z_weight * lse * lse;
@@ -405,6 +424,13 @@ struct Call {
     const rk_matrix *dx, *d_weight;
     const float *given_lse;
 };
+// f(rows of a tile, wavefronts along its words): few rows take small tiles, which leave LDS for two workgroups a compute unit
+template <typename F> void with_rows(uint32_t tile, F f) {
+    if (tile == 32) f(std::integral_constant<int, 32>(), std::integral_constant<int, 8>());
+    else if (tile == 64) f(std::integral_constant<int, 64>(), std::integral_constant<int, 8>());
+    else if (tile == 128) f(std::integral_constant<int, 128>(), std::integral_constant<int, 4>());
+    else f(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
+}
 uint64_t up_to(uint64_t v, uint64_t m) { return (v + m - 1) / m * m; }
 uint32_t blocks_of(uint64_t n) { return (uint32_t)(n < (1u << 20) ? n : 1u << 20); }
 
@@ -441,12 +467,13 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
     const uint64_t w_st = C.weight->stride;
     // rows of W go into the product as they lie where their vectors do not straddle; others are padded first, piece by piece
     const bool direct = ((uintptr_t)w % 16 == 0 && w_st * ES % 16 == 0 && (uint64_t)C.width * ES % 16 == 0 && w_st * ES * 256 < GM_NOWHERE);
-    const uint32_t tiles_b = (uint32_t)((C.n_rows + HD_TB - 1) / HD_TB);
+    const uint32_t tile_b = C.n_rows <= 32 ? 32 : C.n_rows <= 64 ? 64 : C.n_rows <= 128 ? 128 : 256;
+    const uint32_t tiles_b = (uint32_t)((C.n_rows + tile_b - 1) / tile_b);
     const uint64_t most_tiles = (1u << 22) / (tiles_b ? tiles_b : 1);
     const bool back = C.dx || C.d_weight;
     // words of a piece: what the budget holds of their gradients, of W padded, and of the sums of tiles
     uint64_t words = up_to(C.vocab, 256);
-    const uint64_t each = (back ? rows_pad * ES : 0) + (direct ? 0 : (uint64_t)wide * ES), sums_each = C.total ? rows_pad * 8 / HD_PART : 0;
+    const uint64_t each = (back ? rows_pad * ES : 0) + (direct ? 0 : (uint64_t)wide * ES), sums_each = C.total ? rows_pad * 8 / HD_TA : 0;
     if (each && HD_BUDGET / each < words) words = HD_BUDGET / each / 256 * 256;
     if (sums_each && HD_PARTS / sums_each < words) words = HD_PARTS / sums_each / 256 * 256;
     if (words > most_tiles * 256) words = most_tiles * 256;
@@ -479,18 +506,20 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
     if (C.total) {
         if ((rc = rk_scratch(ctx, SL_HEAD_PARTS, words * sums_each, (void **)&L.parts)) != RK_OK) return rc;
         L.parts_stride = rows_pad;
-        JoinArgs J{R, L.parts, rows_pad, 0, false, C.head->z_weight, C.loss, C.lse, C.total, C.n_rows};
+        JoinArgs J{R, L.parts, rows_pad, 0, false, false, C.head->z_weight, C.loss, C.lse, C.total, C.n_rows};
         for (uint64_t first = 0; first < C.vocab && C.n_rows; first += words) {
             if ((rc = piece(first)) != RK_OK) return rc;
             L.first = (uint32_t)first; L.words = n_words;
             L.W = W; L.W.count = n_words;
             L.g = first == last_piece ? g : nullptr;
             const uint32_t tiles_a = (n_words + 255) / 256;
-            k_head_logits<T, HD_TA, HD_TB, 2, true><<<tiles_a * tiles_b, GM_THREADS, 0, stream>>>(L);
+            with_rows(tile_b, [&](auto tb, auto wa) {
+                k_head_logits<T, HD_TA, decltype(tb)::value, decltype(wa)::value, true><<<tiles_a * tiles_b, GM_THREADS, 0, stream>>>(L);
+            });
             RK_CHECK_LAUNCH(ctx, "k_head_logits");
-            J.n_parts = tiles_a * 2;
-            J.last = first == last_piece;
-            k_head_join<<<(uint32_t)((C.n_rows + 15) / 16), 256, 0, stream>>>(J);
+            J.n_parts = tiles_a;
+            J.first = first == 0; J.last = first == last_piece;
+            k_head_join<<<(uint32_t)((C.n_rows + 15) / 16), 16 * HD_RUNS, 0, stream>>>(J);
             RK_CHECK_LAUNCH(ctx, "k_head_join");
         }
         k_head_total<<<1, HD_THREADS, 0, stream>>>(J);
@@ -507,9 +536,9 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
         // the words in as many shares as leave the fewest compute units idle in the last turn; none shorter than 1,024 words
         const uint64_t tiles = (uint64_t)tiles_w * (tiles_b ? tiles_b : 1);
         double best = 0.0;
-        for (uint32_t n = 1; n <= 16 && n <= words / 1024 + 1; ++n) {
+        for (uint32_t n = 1; n <= 64 && n <= words / 1024 + 1; ++n) {
             const uint64_t turns = (tiles * n + 255) / 256;
-            const double filled = (double)(tiles * n) / (double)(turns * 256) * (1.0 - 0.01 * n);
+            const double filled = (double)(tiles * n) / (double)(turns * 256) * (1.0 - 0.002 * n);
             if (filled > best) { best = filled; O.splits = n; }
         }
         O.stride = up_to(C.width, 4);
@@ -524,29 +553,33 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
         if (C.n_rows && C.total && first == last_piece) {
             const uint32_t across = (n_words + 256 * 16 / ES - 1) / (256 * 16 / ES);
             k_head_scale<T><<<dim3(across, (uint32_t)(C.n_rows < 4096 ? C.n_rows : 4096)), 256, 0, stream>>>(
-                ScaleArgs{R, L.parts, rows_pad, words, g, (uint32_t)first, n_words, HD_PART, room});
+                ScaleArgs{R, L.parts, rows_pad, words, g, (uint32_t)first, n_words, HD_TA, room});
             RK_CHECK_LAUNCH(ctx, "k_head_scale");
         } else if (C.n_rows) {
             L.first = (uint32_t)first; L.words = n_words;
             L.W = W; L.W.count = n_words;
-            k_head_logits<T, HD_TA, HD_TB, 2, false><<<tiles_a * tiles_b, GM_THREADS, 0, stream>>>(L);
+            with_rows(tile_b, [&](auto tb, auto wa) {
+                k_head_logits<T, HD_TA, decltype(tb)::value, decltype(wa)::value, false><<<tiles_a * tiles_b, GM_THREADS, 0, stream>>>(L);
+            });
             RK_CHECK_LAUNCH(ctx, "k_head_logits");
         }
         if (C.dx && C.n_rows) {
             O.A = W; O.A.count = row_bytes;
             O.B = Side{(const char *)g, words * ES, 0};
             O.ks = n_words; O.tiles_b = tiles_b; O.first = first == last_piece;
-            k_head_dx<T, HD_TA, HD_TB, 2><<<tiles_w * tiles_b * O.splits, GM_THREADS, 0, stream>>>(O);
+            with_rows(tile_b, [&](auto tb, auto wa) {
+                k_head_dx<T, HD_TA, decltype(tb)::value, decltype(wa)::value><<<tiles_w * tiles_b * O.splits, GM_THREADS, 0, stream>>>(O);
+            });
             RK_CHECK_LAUNCH(ctx, "k_head_dx");
         }
         if (C.d_weight) {
             OutArgs D = O;
             D.A = X; D.A.count = (uint64_t)wide * ES;
             D.B = Side{(const char *)g, words * ES, words * ES};
-            D.tiles_b = (n_words + HD_TB - 1) / HD_TB; D.words = n_words;
+            D.tiles_b = (n_words + 255) / 256; D.words = n_words;
             D.aligned = (uintptr_t)C.d_weight->data % 16 == 0 && C.d_weight->stride * ES % 16 == 0;
             D.out = (T *)C.d_weight->data + first * C.d_weight->stride; D.stride = C.d_weight->stride;
-            k_head_dw<T, HD_TA, HD_TB, 2><<<tiles_w * D.tiles_b, GM_THREADS, 0, stream>>>(D);
+            k_head_dw<T, HD_TA, 256, 2><<<tiles_w * D.tiles_b, GM_THREADS, 0, stream>>>(D);
             RK_CHECK_LAUNCH(ctx, "k_head_dw");
         }
         if (first == 0) break;
