@@ -980,7 +980,7 @@ int32_t rk_recur_forward(rk_ctx *ctx, const rk_recur *recur, uint64_t n_rows, ui
  *     dx_t = (1 - f_t) e_t,  dz_t = e_t (h_{t-1} - x_t) f_t (1 - f_t)       (coupled)
  *     dx_t = e_t,            dz_t = e_t h_{t-1} f_t (1 - f_t)               (otherwise; x may be null then)
  *     d_state_in = f e of the first row,  d_bias = sum of dz over the rows
- * h is taken as it was stored.  dx may be dh, d_state_in may be d_state_out.  d_bias [device] width floats. */
+ * h is taken as it was stored.  dx may be dh.  d_bias [device] width floats. */
 int32_t rk_recur_backward(rk_ctx *ctx, const rk_recur *recur, uint64_t n_rows, uint32_t width, const rk_matrix *x_or_null,
                           const rk_matrix *z, const rk_matrix *h, const rk_matrix *state_in_or_null, const rk_matrix *dh,
                           const rk_matrix *d_state_out_or_null, const rk_matrix *dx, const rk_matrix *dz,

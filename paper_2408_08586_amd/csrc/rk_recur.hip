@@ -8,15 +8,15 @@
 //
 // What a tile says is one 64-bit word a column (p and q), readable as soon as it is no longer all ones, so that words need no flags or fences beside them.
 // A tile joins the words of at most RC_BLOCK - 1 tiles before it, in order, with the value behind the last block of RC_BLOCK tiles, which that block's
-// last tile writes: always the same sums in the same order.  Tiles are handed out by a counter, earlier ones first: who
+// last tile writes: always the same sums in the same order.  The tiles of a column are handed out by a counter of its own, earlier ones first: who
 // waits, waits for workgroups that run already.  A tile whose first row begins a sequence waits for nobody, and nobody
 // looks behind the beginning of a sequence, so that nothing of one sequence comes near another.
 #include "rk_vec.h"
 
 namespace {
 
-constexpr uint32_t RC_WAVES = 8, RC_THREADS = 64 * RC_WAVES, RC_COLS = 128, RC_BLOCK = 16;
-constexpr uint32_t RC_FORWARD_ROWS = 16, RC_BACK_ROWS = 8;      // of a wavefront
+constexpr uint32_t RC_WAVES = 8, RC_THREADS = 64 * RC_WAVES, RC_COLS = 128, RC_BLOCK = 16, RC_TICKET = 16;
+constexpr uint32_t RC_FORWARD_ROWS = 16, RC_BACK_ROWS = 16;     // of a wavefront (back in 32 bits half as many)
 
 struct RecurArgs {
     const void *x, *z, *h, *dh, *bias;
@@ -29,7 +29,7 @@ struct RecurArgs {
     uint32_t seq_rows, n_rows;
     uint32_t n_seqs, width, coupled, bias_type;
     uint32_t n_tiles, n_cols;       // tiles of rows; of columns
-    uint32_t *ticket;               // null: there is one tile of rows
+    uint32_t *ticket;               // [n_cols] counters, RC_TICKET words apart; null: there is one tile of rows
     uint64_t *steps;                // [n_tiles][width]: p and q
     uint32_t *behind;               // [n_tiles / RC_BLOCK][width]: the value behind a block of tiles
     float *bias_parts;              // [n_tiles][width]
@@ -55,7 +55,7 @@ template <typename T> __device__ __forceinline__ Two<T> read_two(const T *row, c
         v[0] = row[0];
         return __builtin_bit_cast(Two<T>, v);
     }
-    return __builtin_nontemporal_load((const LooseTwo<T> *)(row + c.at));
+    return *(const LooseTwo<T> *)(row + c.at);
 }
 template <typename T> __device__ __forceinline__ Vec<float, 2> floats(Two<T> w, const Columns &c) {
     Vec<float, 2> v;
@@ -151,20 +151,20 @@ __device__ __forceinline__ Vec<float, 2> join(const RecurArgs &A, Lds &lds, uint
         else { q = pw * q + qw; p = p * pw; }
     }
     if (!A.ticket) return q;                    // (nothing comes in to the only tile)
-    if (order == RC_WAVES - 1) {                // what the tile makes of a value
-        const Vec<float, 2> to_p = cuts ? Vec<float, 2>(0.f) : p * own.p, to_q = cut ? own.q : own.p * q + own.q;
+    // what the tile makes of a value
+    const Vec<float, 2> all_p = cuts ? Vec<float, 2>(0.f) : p * own.p, all_q = cut ? own.q : own.p * q + own.q;
+    if (order == RC_WAVES - 1)
 #pragma unroll
         for (int i = 0; i < 2; ++i)
             if (column + i < A.width)
-                __hip_atomic_store(A.steps + (uint64_t)tile * A.width + column + i, (uint64_t)not_all_ones(to_q[i]) << 32 | not_all_ones(to_p[i]),
+                __hip_atomic_store(A.steps + (uint64_t)tile * A.width + column + i, (uint64_t)not_all_ones(all_q[i]) << 32 | not_all_ones(all_p[i]),
                                    __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
     Vec<float, 2> in = 0.f;
     if (needs) {
         const uint32_t block = tile / RC_BLOCK * RC_BLOCK, begin = from > block ? from : block, n = tile - begin;
         // the tiles before this one, a run of them a wavefront, and the value behind the block before
         const uint32_t a = begin + n * order / RC_WAVES, b = begin + n * (order + 1) / RC_WAVES;
-        Vec<float, 2> jp = 1.f, jq = 0.f, before = 0.f;
+        Vec<float, 2> jp = 1.f, jq = 0.f;
         for (uint32_t t = a; t < b; ++t)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -176,6 +176,16 @@ __device__ __forceinline__ Vec<float, 2> join(const RecurArgs &A, Lds &lds, uint
                 jq[i] = tp * jq[i] + tq;
                 jp[i] *= tp;
             }
+        __syncthreads();                        // (needs is the same for the whole workgroup)
+        lds.p[order][lane] = jp;
+        lds.q[order][lane] = jq;
+        __syncthreads();
+        jp = lds.p[0][lane]; jq = lds.q[0][lane];
+#pragma unroll
+        for (uint32_t w = 1; w < RC_WAVES; ++w) {
+            jq = lds.p[w][lane] * jq + lds.q[w][lane];
+            jp *= lds.p[w][lane];
+        }
         if (from < block)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -183,40 +193,34 @@ __device__ __forceinline__ Vec<float, 2> join(const RecurArgs &A, Lds &lds, uint
                 uint32_t word;
                 while ((word = __hip_atomic_load(A.behind + (uint64_t)(tile / RC_BLOCK - 1) * A.width + column + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) == ~0u)
                     __builtin_amdgcn_s_sleep(1);
-                before[i] = __uint_as_float(word);
+                in[i] = __uint_as_float(word);
             }
-        in = before;
-        __syncthreads();                        // (needs is the same for the whole workgroup)
-        lds.p[order][lane] = jp;
-        lds.q[order][lane] = jq;
-        __syncthreads();
+        in = jp * in + jq;
+    }
+    // the value behind the tile, if it is a block's last: the next block is waiting for it
+    if (order == RC_WAVES - 1 && tile % RC_BLOCK == RC_BLOCK - 1) {
+        const Vec<float, 2> behind = cuts ? all_q : all_p * in + all_q;
 #pragma unroll
-        for (uint32_t w = 0; w < RC_WAVES; ++w) in = lds.p[w][lane] * in + lds.q[w][lane];
+        for (int i = 0; i < 2; ++i)
+            if (column + i < A.width)
+                __hip_atomic_store(A.behind + (uint64_t)(tile / RC_BLOCK) * A.width + column + i, not_all_ones(behind[i]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     return cuts & ((1u << order) - 1u) ? q : p * in + q;
 }
-// the value behind the tile, if it is a block's last
-__device__ __forceinline__ void tell(const RecurArgs &A, uint32_t order, uint32_t tile, uint32_t column, const Vec<float, 2> &v) {
-    if (!A.ticket || order != RC_WAVES - 1 || tile % RC_BLOCK != RC_BLOCK - 1) return;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-        if (column + i < A.width)
-            __hip_atomic_store(A.behind + (uint64_t)(tile / RC_BLOCK) * A.width + column + i, not_all_ones(v[i]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
 // Which tile a workgroup has; false: none, it looked for sequences without rows instead, whose state goes from one end to the other.
 __device__ __forceinline__ bool take(const RecurArgs &A, Lds &lds, const float *from, uint64_t from_st, float *to, uint64_t to_st, uint32_t &tile, uint32_t &column_tile) {
+    const uint32_t tiles = A.n_tiles * A.n_cols;
     if (threadIdx.x == 0) {
         lds.cuts = 0;
-        lds.ticket = A.ticket ? atomicAdd(A.ticket, 1u) : blockIdx.x;
+        lds.ticket = A.ticket && blockIdx.x < tiles ? atomicAdd(A.ticket + blockIdx.x % A.n_cols * RC_TICKET, 1u) : 0u;
     }
     __syncthreads();
-    const uint32_t t = lds.ticket, tiles = A.n_tiles * A.n_cols;
-    if (t < tiles) {
-        tile = t / A.n_cols;
-        column_tile = t % A.n_cols;
+    if (blockIdx.x < tiles) {
+        tile = lds.ticket;
+        column_tile = blockIdx.x % A.n_cols;
         return true;
     }
-    for (uint32_t s = (t - tiles) * RC_WAVES + (threadIdx.x >> 6); s < A.n_seqs; s += A.idle * RC_WAVES) {
+    for (uint32_t s = (blockIdx.x - tiles) * RC_WAVES + (threadIdx.x >> 6); s < A.n_seqs; s += A.idle * RC_WAVES) {
         const bool none = A.offsets ? A.offsets[s + 1] <= A.offsets[s] : A.n_rows == 0;
         if (none)
             for (uint32_t c = threadIdx.x & 63u; c < A.width; c += 64) to[s * to_st + c] = from ? from[s * from_st + c] : 0.f;
@@ -283,12 +287,14 @@ template <typename T> __global__ __launch_bounds__(RC_THREADS, 4) void k_recur_f
             if (A.state_out && (m.last >> i & 1u)) write_two<float>(A.state_out + of_row(m.seq, i) * A.so_st, c, column, h);
         }
     }
-    tell(A, wave, tile, column, h);
 }
 
+// The rows wait for what comes in to them as they were read, and their gates are made a second time behind it (16-bit rows take twice as many
+// rows a wavefront that way).
+template <typename T> constexpr int back_rows() { return sizeof(T) == 4 ? RC_BACK_ROWS / 2 : RC_BACK_ROWS; }
 template <typename T> __global__ __launch_bounds__(RC_THREADS, 4) void k_recur_backward(const RecurArgs A) {
     __shared__ Lds lds;
-    constexpr int L = RC_BACK_ROWS;
+    constexpr int L = back_rows<T>();
     uint32_t tile, column_tile;                     // (counted from the last rows)
     if (!take(A, lds, A.d_state_out, A.dso_st, A.d_state_in, A.dsi_st, tile, column_tile)) return;
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -308,35 +314,37 @@ template <typename T> __global__ __launch_bounds__(RC_THREADS, 4) void k_recur_b
     const Marks m = marks_of<L>(A, row0);
     Vec<float, 2> bias;
     bias[0] = bias_at(A, column); bias[1] = bias_at(A, column + 1);
-    Vec<float, 2> state[L], d_state[L];
-    if (m.first && A.state_in)
+    // rows 4 g .. 4 g + 3, the last first: row(i, e, d_state), with what behind the last row of a sequence comes in to it
+    auto four = [&](int g, auto row) {
+        Vec<float, 2> d_state[4];
+        if (A.d_state_out && (m.last >> 4 * g & 15u))
 #pragma unroll
-        for (int i = 0; i < L; ++i) if (m.first >> i & 1u) state[i] = read_state(A.state_in, A.si_st, of_row(m.seq, i), c);
-    if (m.last && A.d_state_out)
+            for (int k = 0; k < 4; ++k) if (m.last >> (4 * g + k) & 1u) d_state[k] = read_state(A.d_state_out, A.dso_st, of_row(m.seq, 4 * g + k), c);
 #pragma unroll
-        for (int i = 0; i < L; ++i) if (m.last >> i & 1u) d_state[i] = read_state(A.d_state_out, A.dso_st, of_row(m.seq, i), c);
-    Vec<float, 2> f[L], not_f[L], of[L], e[L];
+        for (int k = 3; k >= 0; --k) {
+            const int i = 4 * g + k;
+            const bool live = m.live >> i & 1u, last = m.last >> i & 1u;
+            const Vec<float, 2> zi = floats<T>(z[i], c) + bias;
+            Vec<float, 2> e = floats<T>(dh[i], c), f, not_f;
+            if (last && A.d_state_out) e += d_state[k];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const Gate gate = gate_of<T>(zi[n]);
+                f[n] = live ? gate.f : 1.f;
+                not_f[n] = gate.not_f;
+                e[n] = live ? e[n] : 0.f;
+            }
+            row(i, live, last, e, f, not_f);
+        }
+    };
     Link own;
     own.p = 1.f; own.q = 0.f;
 #pragma unroll
-    for (int i = L - 1; i >= 0; --i) {
-        const bool live = m.live >> i & 1u, last = m.last >> i & 1u;
-        const Vec<float, 2> zi = floats<T>(z[i], c) + bias;
-        of[i] = floats<T>(h[i], c);
-        if (m.first >> i & 1u) of[i] = A.state_in ? state[i] : Vec<float, 2>(0.f);
-        of[i] -= floats<T>(x[i], c);
-        e[i] = floats<T>(dh[i], c);
-        if (last && A.d_state_out) e[i] += d_state[i];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const Gate g = gate_of<T>(zi[k]);
-            f[i][k] = live ? g.f : 1.f;
-            not_f[i][k] = g.not_f;
-            e[i][k] = live ? e[i][k] : 0.f;
-        }
-        if (last) { own.p = 0.f; own.q = f[i] * e[i]; }
-        else { own.p *= f[i]; own.q = f[i] * (e[i] + own.q); }
-    }
+    for (int g = L / 4 - 1; g >= 0; --g)
+        four(g, [&](int, bool, bool last, const Vec<float, 2> &e, const Vec<float, 2> &f, const Vec<float, 2> &) {
+            if (last) { own.p = 0.f; own.q = f * e; }
+            else { own.p *= f; own.q = f * (e + own.q); }
+        });
     const uint32_t order = RC_WAVES - 1 - wave;
     __shared__ uint32_t from;
     // how the tile's last row goes on; a tile of the matrix's end is cut short there, and nothing comes in to it
@@ -346,19 +354,35 @@ template <typename T> __global__ __launch_bounds__(RC_THREADS, 4) void k_recur_b
     }
     __syncthreads();
     Vec<float, 2> carry = join(A, lds, order, own, m.last != 0, tile, column, from != ~0u, from), sum = 0.f;
+    // (nothing that is made of the rows is to be kept for here, or made ahead)
 #pragma unroll
-    for (int i = L - 1; i >= 0; --i) {
-        const bool last = m.last >> i & 1u, live = m.live >> i & 1u;
-        const Vec<float, 2> now = last ? e[i] : e[i] + carry, dz = now * of[i] * (f[i] * not_f[i]);
-        carry = f[i] * now;
-        if (live) {
-            sum += dz;
-            write_two<T>((T *)A.dx + (uint64_t)(row0 + i) * A.dx_st, c, column, A.coupled ? not_f[i] * now : now);
-            write_two<T>((T *)A.dz + (uint64_t)(row0 + i) * A.dz_st, c, column, dz);
-            if (A.d_state_in && (m.first >> i & 1u)) write_two<float>(A.d_state_in + of_row(m.seq, i) * A.dsi_st, c, column, carry);
+    for (int i = 0; i < L; ++i)
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
+            uint32_t v[4] = {z[i][k], dh[i][k], x[i][k], h[i][k]};
+            asm volatile("" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]));
+            z[i][k] = v[0]; dh[i][k] = v[1]; x[i][k] = v[2]; h[i][k] = v[3];
         }
+#pragma unroll
+    for (int g = L / 4 - 1; g >= 0; --g) {
+        Vec<float, 2> state[4];
+        if (A.state_in && (m.first >> 4 * g & 15u))
+#pragma unroll
+            for (int k = 0; k < 4; ++k) if (m.first >> (4 * g + k) & 1u) state[k] = read_state(A.state_in, A.si_st, of_row(m.seq, 4 * g + k), c);
+        four(g, [&](int i, bool live, bool last, const Vec<float, 2> &e, const Vec<float, 2> &f, const Vec<float, 2> &not_f) {
+            const Vec<float, 2> now = last ? e : e + carry;
+            carry = f * now;
+            if (!live) return;
+            const bool first = m.first >> i & 1u;
+            Vec<float, 2> of = floats<T>(h[i], c);
+            if (first) of = A.state_in ? state[i % 4] : Vec<float, 2>(0.f);
+            const Vec<float, 2> dz = now * (of - floats<T>(x[i], c)) * (f * not_f);
+            sum += dz;
+            write_two<T>((T *)A.dx + (uint64_t)(row0 + i) * A.dx_st, c, column, A.coupled ? not_f * now : now);
+            write_two<T>((T *)A.dz + (uint64_t)(row0 + i) * A.dz_st, c, column, dz);
+            if (A.d_state_in && first) write_two<float>(A.d_state_in + of_row(m.seq, i) * A.dsi_st, c, column, carry);
+        });
     }
-    tell(A, order, tile, column, carry);
     if (!A.d_bias) return;
     __syncthreads();
     lds.p[wave][lane] = sum;
@@ -387,8 +411,8 @@ __global__ __launch_bounds__(1024) void k_recur_bias(const float *parts, uint32_
     for (int i = 1; i < 16; ++i) sum += lds[i][lane];
     d_bias[c] = sum;
 }
-__global__ __launch_bounds__(256) void k_recur_clear(uint64_t *words, uint64_t n, uint32_t *ticket) {
-    if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;
+__global__ __launch_bounds__(256) void k_recur_clear(uint64_t *words, uint64_t n, uint32_t *ticket, uint32_t n_tickets) {
+    for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < n_tickets; i += gridDim.x * 256) ticket[i] = 0;
     for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) words[i] = ~0ull;
 }
 
@@ -428,13 +452,13 @@ int32_t tiles_of(rk_ctx *ctx, RecurArgs &A, uint32_t tile_rows, bool states, uin
     if (blocks > RK_LAUNCH_THREADS / RC_THREADS) return rk_fail(ctx, RK_ERR_UNSUPPORTED, "2^22 tiles of %u rows and %u columns or more", tile_rows, RC_COLS);
     if (A.n_tiles < 2) return RK_OK;
     const uint64_t words = (uint64_t)A.n_tiles * A.width, after = ((uint64_t)(A.n_tiles / RC_BLOCK) * A.width + 1) / 2;
-    int32_t rc = rk_scratch(ctx, SL_RECUR_CHAIN, (words + after + 1) * 8, (void **)&A.steps);
+    int32_t rc = rk_scratch(ctx, SL_RECUR_CHAIN, (words + after) * 8 + (uint64_t)A.n_cols * RC_TICKET * 4, (void **)&A.steps);
     if (rc != RK_OK) return rc;
     A.behind = (uint32_t *)(A.steps + words);
     A.ticket = (uint32_t *)(A.steps + words + after);
     if (A.d_bias && (rc = rk_scratch(ctx, SL_RECUR_BIAS, words * 4, (void **)&A.bias_parts)) != RK_OK) return rc;
     const uint64_t clear = (words + after + 1023) / 1024;
-    k_recur_clear<<<(uint32_t)(clear < 2048 ? clear : 2048), 256, 0, ctx->stream>>>(A.steps, words + after, A.ticket);
+    k_recur_clear<<<(uint32_t)(clear < 2048 ? clear : 2048), 256, 0, ctx->stream>>>(A.steps, words + after, A.ticket, A.n_cols * RC_TICKET);
     RK_CHECK_LAUNCH(ctx, "k_recur_clear");
     return RK_OK;
 }
@@ -494,7 +518,7 @@ extern "C" int32_t rk_recur_backward(rk_ctx *ctx, const rk_recur *recur, uint64_
     if (d_state_in) { A.d_state_in = (float *)d_state_in->data; A.dsi_st = d_state_in->stride; }
     A.d_bias = d_bias;
     uint64_t blocks;
-    if ((rc = tiles_of(ctx, A, RC_WAVES * RC_BACK_ROWS, d_state_in != nullptr, blocks)) != RK_OK) return rc;
+    if ((rc = tiles_of(ctx, A, RC_WAVES * (z->type == RK_F32 ? back_rows<float>() : back_rows<__bf16>()), d_state_in != nullptr, blocks)) != RK_OK) return rc;
     if (blocks) {
         with_type(z->type, [&](auto t) { k_recur_backward<decltype(t)><<<(uint32_t)blocks, RC_THREADS, 0, ctx->stream>>>(A); });
         RK_CHECK_LAUNCH(ctx, "k_recur_backward");

@@ -171,9 +171,9 @@ def test_in_place(gpu):
             rk.rk_recur_forward(ctx, d.recur(rk), d.x, d.z, d.state_in, getattr(d, into), d.state_in)
             assert torch.equal(getattr(d, into), h) and torch.equal(d.state_in, state)
         d = Case(torch, at, 200, seed=11)
-        dz2, db2 = d.matrix(), torch.empty_like(db)
-        rk.rk_recur_backward(ctx, d.recur(rk), d.x, d.z, h, d.state_in, d.dh, d.d_state_out, d.dh, dz2, d.d_state_out, db2)
-        assert torch.equal(d.dh, dx) and torch.equal(dz2, dz) and torch.equal(d.d_state_out, dsi) and torch.equal(db2, db)
+        dz2, dsi2, db2 = d.matrix(), d.state(), torch.empty_like(db)
+        rk.rk_recur_backward(ctx, d.recur(rk), d.x, d.z, h, d.state_in, d.dh, d.d_state_out, d.dh, dz2, dsi2, db2)
+        assert torch.equal(d.dh, dx) and torch.equal(dz2, dz) and torch.equal(dsi2, dsi) and torch.equal(db2, db)
 
 
 def test_step_by_step_is_the_whole(gpu):
