@@ -11,6 +11,8 @@
 // last tile writes: always the same sums in the same order.  The tiles of a column are handed out by a counter of its own, earlier ones first: who
 // waits, waits for workgroups that run already.  A tile whose first row begins a sequence waits for nobody, and nobody
 // looks behind the beginning of a sequence, so that nothing of one sequence comes near another.
+#include <type_traits>
+
 #include "rk_vec.h"
 
 namespace {
@@ -41,36 +43,51 @@ template <typename T> using Two = Words<T, 2>;
 template <typename T> using LooseTwo = Two<T> __attribute__((aligned(sizeof(T))));
 struct Columns {
     uint32_t at;                    // where it reads: both elements are inside the row
-    bool two, one, cut_here;        // writes both; the first alone, which it has read as the second; some lane of the wavefront does
-    bool single;                    // rows have one element
+    bool two, one;                  // writes both; the first alone, which it has read as the second
     __device__ __forceinline__ Columns(uint32_t c, uint32_t width) {
-        two = c + 1 < width; one = c + 1 == width; single = width == 1;
-        at = two ? c : one && !single ? width - 2 : 0;
-        cut_here = width % 2 && __builtin_amdgcn_ballot_w64(one) != 0;
+        two = c + 1 < width; one = c + 1 == width;
+        at = two ? c : one && width > 1 ? width - 2 : 0;
     }
 };
-template <typename T> __device__ __forceinline__ Two<T> read_two(const T *row, const Columns &c) {
-    if (c.single) {
+// CUT: rows have an odd number of elements
+template <bool CUT, typename T> __device__ __forceinline__ Two<T> read_two(const T *row, const Columns &c, uint32_t width) {
+    if (CUT && width == 1) {
         Vec<T, 2> v = (T)0.f;
-        v[0] = row[0];
+        v[1] = row[0];
         return __builtin_bit_cast(Two<T>, v);
     }
-    return *(const LooseTwo<T> *)(row + c.at);
+    return *(const LooseTwo<T> *)((const char *)row + c.at * (uint32_t)sizeof(T));     // (a place of 32 bits beside a row that all lanes share)
 }
-template <typename T> __device__ __forceinline__ Vec<float, 2> floats(Two<T> w, const Columns &c) {
+template <bool CUT, typename T> __device__ __forceinline__ Vec<float, 2> floats(Two<T> w, const Columns &c) {
     Vec<float, 2> v;
     v[0] = element<T>(w, 0); v[1] = element<T>(w, 1);
-    if (c.cut_here) v[0] = c.one && !c.single ? v[1] : v[0];
+    if (CUT) v[0] = c.one ? v[1] : v[0];
     return v;
 }
-template <typename T> __device__ __forceinline__ void write_two(T *row, const Columns &c, uint32_t first, Vec<float, 2> f) {
+// ONE: of a lane that has one column
+template <bool ONE, typename T> __device__ __forceinline__ void write_two(T *row, uint32_t column, Vec<float, 2> f) {
+    T *const at = (T *)((char *)row + column * (uint32_t)sizeof(T));
     Vec<T, 2> v;
     v[0] = (T)f[0]; v[1] = (T)f[1];
-    if (c.two) __builtin_nontemporal_store(__builtin_bit_cast(Two<T>, v), (LooseTwo<T> *)(row + first));
-    if (c.cut_here) { if (c.one) row[first] = v[0]; }
+    if (ONE) *at = v[0];
+    else __builtin_nontemporal_store(__builtin_bit_cast(Two<T>, v), (LooseTwo<T> *)at);
 }
-__device__ __forceinline__ Vec<float, 2> read_state(const float *states, uint64_t stride, uint32_t seq, const Columns &c) {
-    return floats<float>(read_two<float>(states + seq * stride, c), c);
+// f(false) for lanes of two columns, f(true) for one of a single column: what they do is done under one mask
+template <bool CUT, typename F> __device__ __forceinline__ void where_columns(const Columns &c, F f) {
+    if (c.two) f(std::false_type());
+    if constexpr (CUT) { if (c.one) f(std::true_type()); }
+}
+template <bool CUT> __device__ __forceinline__ Vec<float, 2> read_state(const float *states, uint64_t stride, uint32_t seq, const Columns &c, uint32_t width) {
+    return floats<CUT, float>(read_two<CUT, float>(states + seq * stride, c, width), c);
+}
+// L rows as they lie, from row0 on; behind the last of n_rows that one again
+template <bool CUT, int L, typename T> __device__ __forceinline__ void read_rows(Two<T> (&w)[L], const void *data, uint64_t stride, uint32_t row0, uint32_t n_rows, const Columns &c, uint32_t width) {
+    const T *p = (const T *)data + (uint64_t)(row0 < n_rows ? row0 : n_rows - 1) * stride;
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+        w[i] = read_two<CUT, T>(p, c, width);
+        p += row0 + i + 1 < n_rows ? stride : 0;
+    }
 }
 __device__ __forceinline__ float bias_at(const RecurArgs &A, uint32_t c) {
     if (!A.bias || c >= A.width) return 0.f;
@@ -78,25 +95,29 @@ __device__ __forceinline__ float bias_at(const RecurArgs &A, uint32_t c) {
     return A.bias_type == RK_BF16 ? (float)((const __bf16 *)A.bias)[c] : (float)((const _Float16 *)A.bias)[c];
 }
 
-// f = sigmoid(v) and 1 - f, neither as a difference from one
+// f = sigmoid(v) and 1 - f, which is a difference from one only where f is below a half
 struct Gate { float f, not_f; };
 template <typename T> __device__ __forceinline__ Gate gate_of(float v) {
-    const float a = fabsf(v), e = sizeof(T) == 4 ? exp_f32(-a) : __builtin_amdgcn_exp2f(a * -1.4426950408889634f);
-    const float near = __builtin_amdgcn_rcpf(1.f + e), far = e * near;
-    const bool up = v >= 0.f;
-    return Gate{up ? near : far, up ? far : near};
+    if constexpr (sizeof(T) == 4) {
+        const float e = exp_f32(-fabsf(v)), near = __builtin_amdgcn_rcpf(1.f + e), far = e * near;
+        return v >= 0.f ? Gate{near, far} : Gate{far, near};
+    } else {
+        const float e = __builtin_amdgcn_exp2f(v * -1.4426950408889634f), f = __builtin_amdgcn_rcpf(1.f + e);
+        return Gate{f, e > 1.f ? 1.f - f : e * f};
+    }
 }
 
 // ---- which rows of a wavefront begin and end sequences
 struct Marks {
     uint32_t live, first, last;     // a bit a row
-    int32_t seq, begin, end;        // of lane i: of row i
+    int32_t seq, begin, end;        // of lane i: of row i; of lane L: of the tile's first row
+    bool plain;                     // no sequence begins or ends in the tile, and all its rows are one's
 };
 // L rows from row0 on; rows that no sequence has are not live.  Offsets that are no offsets lead nowhere outside the rows.
-template <int L> __device__ __forceinline__ Marks marks_of(const RecurArgs &A, uint32_t row0) {
-    const uint32_t lane = threadIdx.x & 63u, row = row0 + lane;
-    Marks m{0, 0, 0, 0, 0, 0};
-    bool live = lane < L && row < A.n_rows;
+template <int L> __device__ __forceinline__ Marks marks_of(const RecurArgs &A, uint32_t tile0, uint32_t row0) {
+    const uint32_t lane = threadIdx.x & 63u, row = lane == L ? tile0 : row0 + lane;
+    Marks m{0, 0, 0, 0, 0, 0, false};
+    bool live = lane <= L && row < A.n_rows;
     if (A.offsets) {
         if (live) {
             // the last sequence that begins at this row or before it
@@ -117,12 +138,15 @@ template <int L> __device__ __forceinline__ Marks marks_of(const RecurArgs &A, u
         m.begin = m.seq * (int32_t)A.seq_rows;
         m.end = (int32_t)(A.n_rows - (uint32_t)m.begin < A.seq_rows ? A.n_rows : (uint32_t)m.begin + A.seq_rows);
     }
-    m.live = (uint32_t)__builtin_amdgcn_ballot_w64(live);
-    m.first = (uint32_t)__builtin_amdgcn_ballot_w64(live && (int32_t)row == m.begin);
-    m.last = (uint32_t)__builtin_amdgcn_ballot_w64(live && (int32_t)row + 1 == m.end);
+    // (lanes' registers are read here alone, where all lanes are at work: elsewhere one may have been brought back from memory for some of them)
+    constexpr uint32_t ROWS = (1u << L) - 1u;
+    const uint32_t lives = (uint32_t)__builtin_amdgcn_ballot_w64(live);
+    m.live = lives & ROWS;
+    m.first = (uint32_t)__builtin_amdgcn_ballot_w64(live && (int32_t)row == m.begin) & ROWS;
+    m.last = (uint32_t)__builtin_amdgcn_ballot_w64(live && (int32_t)row + 1 == m.end) & ROWS;
+    m.plain = (lives >> L & 1u) && (uint32_t)__builtin_amdgcn_readlane(m.begin, L) < tile0 && (uint32_t)__builtin_amdgcn_readlane(m.end, L) > tile0 + RC_WAVES * L;
     return m;
 }
-__device__ __forceinline__ uint32_t of_row(int32_t v, int i) { return (uint32_t)__builtin_amdgcn_readlane(v, i); }
 
 // ---- chains
 struct Link { Vec<float, 2> p, q; };            // v -> p v + q
@@ -134,6 +158,13 @@ struct Lds {
     Vec<float, 2> p[RC_WAVES][64], q[RC_WAVES][64];
     uint32_t cuts;                              // wavefronts in which a chain begins
     uint32_t ticket;
+    int32_t seq[RC_WAVES][64];                  // a row's sequence, for code that not all lanes are in
+    __device__ __forceinline__ void keep(uint32_t wave, int32_t of_lane) {
+        seq[wave][threadIdx.x & 63u] = of_lane;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+    __device__ __forceinline__ uint32_t seq_of(uint32_t wave, int i) const { return (uint32_t)__builtin_amdgcn_readfirstlane(seq[wave][i]); }
 };
 // The value that comes in to this wavefront's rows.  order: its place in the direction of the chain; cut: a chain begins in its rows; needs: its
 // tile's first row goes on with a chain that began in tile `from` (tiles counted in the direction of the chain).
@@ -228,161 +259,190 @@ __device__ __forceinline__ bool take(const RecurArgs &A, Lds &lds, const float *
     return false;
 }
 
-template <typename T> __global__ __launch_bounds__(RC_THREADS, 4) void k_recur_forward(const RecurArgs A) {
+// The rows' steps stay in registers until what comes in to them is known.
+template <typename T, bool COUPLED, bool CUT> __global__ __launch_bounds__(RC_THREADS, 4) void k_recur_forward(const RecurArgs A) {
     __shared__ Lds lds;
     constexpr int L = RC_FORWARD_ROWS;
     uint32_t tile, column_tile;
     if (!take(A, lds, A.state_in, A.si_st, A.state_out, A.so_st, tile, column_tile)) return;
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t column = column_tile * RC_COLS + 2 * lane, tile0 = tile * RC_WAVES * L, row0 = tile0 + wave * L;
+    const uint32_t column = column_tile * RC_COLS + 2 * lane, tile0 = tile * RC_WAVES * L, row0 = __builtin_amdgcn_readfirstlane(tile0 + wave * L);
     const Columns c(column, A.width);
     Two<T> z[L], x[L];
-#pragma unroll
-    for (int i = 0; i < L; ++i) {
-        z[i] = 0u; x[i] = 0u;
-        if (row0 + i < A.n_rows) {
-            z[i] = read_two<T>((const T *)A.z + (uint64_t)(row0 + i) * A.z_st, c);
-            x[i] = read_two<T>((const T *)A.x + (uint64_t)(row0 + i) * A.x_st, c);
-        }
-    }
-    const Marks m = marks_of<L>(A, row0);
+    read_rows<CUT, L, T>(z, A.z, A.z_st, row0, A.n_rows, c, A.width);
+    read_rows<CUT, L, T>(x, A.x, A.x_st, row0, A.n_rows, c, A.width);
+    const Marks m = marks_of<L>(A, tile0, row0);
+    lds.keep(wave, m.seq);
     Vec<float, 2> bias;
     bias[0] = bias_at(A, column); bias[1] = bias_at(A, column + 1);
-    Vec<float, 2> f[L], q[L], state[L];
-    if (m.first && A.state_in)
+    auto rows = [&](auto plain) {
+        constexpr bool PLAIN = decltype(plain)::value;
+        Vec<float, 2> f[L], q[L];
+        Link own;
+        own.p = 1.f; own.q = 0.f;
 #pragma unroll
-        for (int i = 0; i < L; ++i) if (m.first >> i & 1u) state[i] = read_state(A.state_in, A.si_st, of_row(m.seq, i), c);
-    Link own;
-    own.p = 1.f; own.q = 0.f;
+        for (int g = 0; g < L / 4; ++g) {
+            Vec<float, 2> state[4];
+            if (!PLAIN && A.state_in && (m.first >> 4 * g & 15u))
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-        const Vec<float, 2> zi = floats<T>(z[i], c) + bias, xi = floats<T>(x[i], c);
-        const bool live = m.live >> i & 1u, first = m.first >> i & 1u;
+                for (int k = 0; k < 4; ++k)
+                    if (m.first >> (4 * g + k) & 1u) state[k] = read_state<CUT>(A.state_in, A.si_st, lds.seq_of(wave, 4 * g + k), c, A.width);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const Gate g = gate_of<T>(zi[k]);
-            f[i][k] = live ? g.f : 1.f;
-            q[i][k] = live ? A.coupled ? g.not_f * xi[k] : xi[k] : 0.f;
+            for (int i = 4 * g; i < 4 * g + 4; ++i) {
+                const Vec<float, 2> zi = floats<CUT, T>(z[i], c) + bias, xi = floats<CUT, T>(x[i], c);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const Gate gate = gate_of<T>(zi[k]);
+                    f[i][k] = gate.f;
+                    q[i][k] = COUPLED ? gate.not_f * xi[k] : xi[k];
+                }
+                if (!PLAIN) {
+                    if (!(m.live >> i & 1u)) { f[i] = 1.f; q[i] = 0.f; }
+                    if (m.first >> i & 1u) {
+                        if (A.state_in) q[i] += f[i] * state[i % 4];
+                        own.p = 0.f; own.q = 0.f;
+                    }
+                }
+                own.p *= f[i];
+                own.q = f[i] * own.q + q[i];
+            }
+            __builtin_amdgcn_sched_barrier(0);              // (four rows at a time: more under way would not fit the registers)
         }
-        if (first) {
-            if (A.state_in) q[i] += f[i] * state[i];
-            own.p = 0.f; own.q = q[i];
-        } else {
-            own.p *= f[i];
-            own.q = f[i] * own.q + q[i];
-        }
-    }
-    // how the tile's first row goes on
-    const bool needs = wave == 0 && (m.live & 1u) && !(m.first & 1u);
-    __shared__ uint32_t from;
-    if (threadIdx.x == 0) from = needs ? of_row(m.begin, 0) / (RC_WAVES * L) : ~0u;
-    __syncthreads();
-    Vec<float, 2> h = join(A, lds, wave, own, m.first != 0, tile, column, from != ~0u, from);
+        // how the tile's first row goes on
+        __shared__ uint32_t from;
+        if (threadIdx.x == 0) from = PLAIN || ((m.live & 1u) && !(m.first & 1u)) ? (uint32_t)m.begin / (RC_WAVES * L) : ~0u;     // (its lane's row)
+        __syncthreads();
+        const Vec<float, 2> in = join(A, lds, wave, own, !PLAIN && m.first != 0, tile, column, from != ~0u, from);
+        where_columns<CUT>(c, [&](auto one) {
+            constexpr bool ONE = decltype(one)::value;
+            T *to = (T *)A.out + (uint64_t)row0 * A.o_st;
+            Vec<float, 2> h = in;
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-        const bool first = m.first >> i & 1u;
-        h = first ? q[i] : f[i] * h + q[i];
-        if (m.live >> i & 1u) {
-            write_two<T>((T *)A.out + (uint64_t)(row0 + i) * A.o_st, c, column, h);
-            if (A.state_out && (m.last >> i & 1u)) write_two<float>(A.state_out + of_row(m.seq, i) * A.so_st, c, column, h);
-        }
-    }
+            for (int i = 0; i < L; ++i) {
+                if (!PLAIN && (m.first >> i & 1u)) h = 0.f;
+                h = f[i] * h + q[i];
+                if (PLAIN || (m.live >> i & 1u)) write_two<ONE>(to, column, h);
+                if (!PLAIN && A.state_out && (m.last >> i & 1u)) write_two<ONE>(A.state_out + lds.seq_of(wave, i) * A.so_st, column, h);
+                to += A.o_st;
+            }
+        });
+    };
+    if (m.plain) rows(std::true_type()); else rows(std::false_type());
 }
 
-// The rows wait for what comes in to them as they were read, and their gates are made a second time behind it (16-bit rows take twice as many
-// rows a wavefront that way).
+// The rows wait for what comes in to them as they were read, and their gates are made a second time behind it: so a wavefront holds
+// twice as many of 16 bits.
 template <typename T> constexpr int back_rows() { return sizeof(T) == 4 ? RC_BACK_ROWS / 2 : RC_BACK_ROWS; }
-template <typename T> __global__ __launch_bounds__(RC_THREADS, 4) void k_recur_backward(const RecurArgs A) {
+template <typename T, bool COUPLED, bool CUT> __global__ __launch_bounds__(RC_THREADS, 4) void k_recur_backward(const RecurArgs A) {
     __shared__ Lds lds;
     constexpr int L = back_rows<T>();
     uint32_t tile, column_tile;                     // (counted from the last rows)
     if (!take(A, lds, A.d_state_out, A.dso_st, A.d_state_in, A.dsi_st, tile, column_tile)) return;
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t column = column_tile * RC_COLS + 2 * lane, row_tile = A.n_tiles - 1 - tile, row0 = (row_tile * RC_WAVES + wave) * L;
+    const uint32_t column = column_tile * RC_COLS + 2 * lane, tile0 = (A.n_tiles - 1 - tile) * RC_WAVES * L, row0 = __builtin_amdgcn_readfirstlane(tile0 + wave * L);
     const Columns c(column, A.width);
     Two<T> z[L], x[L], h[L], dh[L];
+    read_rows<CUT, L, T>(z, A.z, A.z_st, row0, A.n_rows, c, A.width);
+    read_rows<CUT, L, T>(dh, A.dh, A.dh_st, row0, A.n_rows, c, A.width);
+    if constexpr (COUPLED) read_rows<CUT, L, T>(x, A.x, A.x_st, row0, A.n_rows, c, A.width);
+    // (the rows before; before the matrix's first stands that one, which is not used)
+    {
+        const T *p = (const T *)A.h + (uint64_t)(row0 == 0 ? 0 : row0 <= A.n_rows ? row0 - 1 : A.n_rows - 1) * A.h_st;
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-        z[i] = 0u; x[i] = 0u; h[i] = 0u; dh[i] = 0u;
-        if (row0 + i < A.n_rows) {
-            z[i] = read_two<T>((const T *)A.z + (uint64_t)(row0 + i) * A.z_st, c);
-            dh[i] = read_two<T>((const T *)A.dh + (uint64_t)(row0 + i) * A.dh_st, c);
-            if (A.coupled) x[i] = read_two<T>((const T *)A.x + (uint64_t)(row0 + i) * A.x_st, c);
-            if (row0 + i) h[i] = read_two<T>((const T *)A.h + (uint64_t)(row0 + i - 1) * A.h_st, c);
+        for (int i = 0; i < L; ++i) {
+            h[i] = read_two<CUT, T>(p, c, A.width);
+            p += row0 + i > 0 && row0 + i < A.n_rows ? A.h_st : 0;
         }
     }
-    const Marks m = marks_of<L>(A, row0);
-    Vec<float, 2> bias;
+    const Marks m = marks_of<L>(A, tile0, row0);
+    lds.keep(wave, m.seq);
+    Vec<float, 2> bias, sum = 0.f;
     bias[0] = bias_at(A, column); bias[1] = bias_at(A, column + 1);
-    // rows 4 g .. 4 g + 3, the last first: row(i, e, d_state), with what behind the last row of a sequence comes in to it
-    auto four = [&](int g, auto row) {
-        Vec<float, 2> d_state[4];
-        if (A.d_state_out && (m.last >> 4 * g & 15u))
-#pragma unroll
-            for (int k = 0; k < 4; ++k) if (m.last >> (4 * g + k) & 1u) d_state[k] = read_state(A.d_state_out, A.dso_st, of_row(m.seq, 4 * g + k), c);
-#pragma unroll
-        for (int k = 3; k >= 0; --k) {
-            const int i = 4 * g + k;
-            const bool live = m.live >> i & 1u, last = m.last >> i & 1u;
-            const Vec<float, 2> zi = floats<T>(z[i], c) + bias;
-            Vec<float, 2> e = floats<T>(dh[i], c), f, not_f;
-            if (last && A.d_state_out) e += d_state[k];
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                const Gate gate = gate_of<T>(zi[n]);
-                f[n] = live ? gate.f : 1.f;
-                not_f[n] = gate.not_f;
-                e[n] = live ? e[n] : 0.f;
-            }
-            row(i, live, last, e, f, not_f);
-        }
-    };
-    Link own;
-    own.p = 1.f; own.q = 0.f;
-#pragma unroll
-    for (int g = L / 4 - 1; g >= 0; --g)
-        four(g, [&](int, bool, bool last, const Vec<float, 2> &e, const Vec<float, 2> &f, const Vec<float, 2> &) {
-            if (last) { own.p = 0.f; own.q = f * e; }
-            else { own.p *= f; own.q = f * (e + own.q); }
-        });
     const uint32_t order = RC_WAVES - 1 - wave;
-    __shared__ uint32_t from;
-    // how the tile's last row goes on; a tile of the matrix's end is cut short there, and nothing comes in to it
-    if (threadIdx.x == RC_THREADS - 64) {
-        const bool needs = (m.live >> (L - 1) & 1u) && !(m.last >> (L - 1) & 1u);
-        from = needs ? A.n_tiles - 1 - (of_row(m.end, L - 1) - 1) / (RC_WAVES * L) : ~0u;
-    }
-    __syncthreads();
-    Vec<float, 2> carry = join(A, lds, order, own, m.last != 0, tile, column, from != ~0u, from), sum = 0.f;
-    // (nothing that is made of the rows is to be kept for here, or made ahead)
+    auto rows = [&](auto plain) {
+        constexpr bool PLAIN = decltype(plain)::value;
+        // rows 4 g .. 4 g + 3, the last first: row(i, ..), with what behind the last row of a sequence comes in to it, and cut() before that one
+        auto four = [&](int g, auto cut, auto row) {
+            Vec<float, 2> d_state[4];
+            if (!PLAIN && A.d_state_out && (m.last >> 4 * g & 15u))
 #pragma unroll
-    for (int i = 0; i < L; ++i)
+                for (int k = 0; k < 4; ++k)
+                    if (m.last >> (4 * g + k) & 1u) d_state[k] = read_state<CUT>(A.d_state_out, A.dso_st, lds.seq_of(wave, 4 * g + k), c, A.width);
 #pragma unroll
-        for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
-            uint32_t v[4] = {z[i][k], dh[i][k], x[i][k], h[i][k]};
-            asm volatile("" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]));
-            z[i][k] = v[0]; dh[i][k] = v[1]; x[i][k] = v[2]; h[i][k] = v[3];
-        }
+            for (int k = 3; k >= 0; --k) {
+                const int i = 4 * g + k;
+                const Vec<float, 2> zi = floats<CUT, T>(z[i], c) + bias;
+                Vec<float, 2> e = floats<CUT, T>(dh[i], c), f, not_f;
 #pragma unroll
-    for (int g = L / 4 - 1; g >= 0; --g) {
-        Vec<float, 2> state[4];
-        if (A.state_in && (m.first >> 4 * g & 15u))
+                for (int n = 0; n < 2; ++n) {
+                    const Gate gate = gate_of<T>(zi[n]);
+                    f[n] = gate.f; not_f[n] = gate.not_f;
+                }
+                if (!PLAIN) {
+                    if (!(m.live >> i & 1u)) { f = 1.f; e = 0.f; }
+                    if (m.last >> i & 1u) {
+                        if (A.d_state_out) e += d_state[k];
+                        cut();
+                    }
+                }
+                row(i, e, f, not_f);
+            }
+            __builtin_amdgcn_sched_barrier(0);              // (four rows at a time: more under way would not fit the registers)
+        };
+        Link own;
+        own.p = 1.f; own.q = 0.f;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) if (m.first >> (4 * g + k) & 1u) state[k] = read_state(A.state_in, A.si_st, of_row(m.seq, 4 * g + k), c);
-        four(g, [&](int i, bool live, bool last, const Vec<float, 2> &e, const Vec<float, 2> &f, const Vec<float, 2> &not_f) {
-            const Vec<float, 2> now = last ? e : e + carry;
-            carry = f * now;
-            if (!live) return;
-            const bool first = m.first >> i & 1u;
-            Vec<float, 2> of = floats<T>(h[i], c);
-            if (first) of = A.state_in ? state[i % 4] : Vec<float, 2>(0.f);
-            const Vec<float, 2> dz = now * (of - floats<T>(x[i], c)) * (f * not_f);
-            sum += dz;
-            write_two<T>((T *)A.dx + (uint64_t)(row0 + i) * A.dx_st, c, column, A.coupled ? not_f * now : now);
-            write_two<T>((T *)A.dz + (uint64_t)(row0 + i) * A.dz_st, c, column, dz);
-            if (A.d_state_in && first) write_two<float>(A.d_state_in + of_row(m.seq, i) * A.dsi_st, c, column, carry);
+        for (int g = L / 4 - 1; g >= 0; --g)
+            four(g, [&]() { own.p = 0.f; own.q = 0.f; }, [&](int, const Vec<float, 2> &e, const Vec<float, 2> &f, const Vec<float, 2> &) {
+                own.p *= f;
+                own.q = f * (e + own.q);
+            });
+        __shared__ uint32_t from;
+        // how the tile's last row goes on; a tile of the matrix's end is cut short there, and nothing comes in to it
+        if (threadIdx.x == RC_THREADS - 64 + L - 1)         // (its lane's row)
+            from = PLAIN || ((m.live >> (L - 1) & 1u) && !(m.last >> (L - 1) & 1u)) ? A.n_tiles - 1 - (uint32_t)(m.end - 1) / (RC_WAVES * L) : ~0u;
+        __syncthreads();
+        const Vec<float, 2> in = join(A, lds, order, own, !PLAIN && m.last != 0, tile, column, from != ~0u, from);
+        // (nothing that is made of the rows is to be kept for here, or made ahead)
+#pragma unroll
+        for (int i = 0; i < L; ++i)
+#pragma unroll
+            for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
+                uint32_t v[4] = {z[i][k], dh[i][k], COUPLED ? x[i][k] : 0u, h[i][k]};
+                asm volatile("" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]));
+                z[i][k] = v[0]; dh[i][k] = v[1]; x[i][k] = v[2]; h[i][k] = v[3];
+            }
+        where_columns<CUT>(c, [&](auto one) {
+            constexpr bool ONE = decltype(one)::value;
+            T *to_x = (T *)A.dx + (uint64_t)(row0 + L - 1) * A.dx_st, *to_z = (T *)A.dz + (uint64_t)(row0 + L - 1) * A.dz_st;
+            Vec<float, 2> carry = in;
+#pragma unroll
+            for (int g = L / 4 - 1; g >= 0; --g) {
+                Vec<float, 2> state[4];
+                if (!PLAIN && A.state_in && (m.first >> 4 * g & 15u))
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (m.first >> (4 * g + k) & 1u) state[k] = read_state<CUT>(A.state_in, A.si_st, lds.seq_of(wave, 4 * g + k), c, A.width);
+                four(g, [&]() { carry = 0.f; }, [&](int i, const Vec<float, 2> &e, const Vec<float, 2> &f, const Vec<float, 2> &not_f) {
+                    const Vec<float, 2> now = e + carry;
+                    carry = f * now;
+                    if (PLAIN || (m.live >> i & 1u)) {
+                        const bool first = !PLAIN && (m.first >> i & 1u);
+                        Vec<float, 2> of = floats<CUT, T>(h[i], c);
+                        if (first) of = A.state_in ? state[i % 4] : Vec<float, 2>(0.f);
+                        if (COUPLED) of -= floats<CUT, T>(x[i], c);
+                        const Vec<float, 2> dz = now * of * (f * not_f);
+                        sum += dz;
+                        write_two<ONE>(to_x, column, COUPLED ? not_f * now : now);
+                        write_two<ONE>(to_z, column, dz);
+                        if (A.d_state_in && first) write_two<ONE>(A.d_state_in + lds.seq_of(wave, i) * A.dsi_st, column, carry);
+                    }
+                    to_x -= A.dx_st; to_z -= A.dz_st;
+                });
+            }
         });
-    }
+    };
+    if (m.plain) rows(std::true_type()); else rows(std::false_type());
     if (!A.d_bias) return;
     __syncthreads();
     lds.p[wave][lane] = sum;
@@ -416,8 +476,11 @@ __global__ __launch_bounds__(256) void k_recur_clear(uint64_t *words, uint64_t n
     for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) words[i] = ~0ull;
 }
 
-template <typename F> void with_type(uint32_t type, F f) {
-    if (type == RK_F32) f(float()); else if (type == RK_BF16) f(__bf16()); else f(_Float16());
+// f(type, coupled, whether rows have an odd number of elements)
+template <typename F> void with_kernel(const RecurArgs &A, uint32_t type, F f) {
+    auto cut = [&](auto t, auto coupled) { if (A.width % 2) f(t, coupled, std::true_type()); else f(t, coupled, std::false_type()); };
+    auto typed = [&](auto t) { if (A.coupled) cut(t, std::true_type()); else cut(t, std::false_type()); };
+    if (type == RK_F32) typed(float()); else if (type == RK_BF16) typed(__bf16()); else typed(_Float16());
 }
 // what both directions check alike; how many sequences there are
 int32_t check_recur(rk_ctx *ctx, const rk_recur *r, uint64_t n_rows, uint32_t width, const rk_matrix *z, uint64_t &n_seqs) {
@@ -485,7 +548,9 @@ extern "C" int32_t rk_recur_forward(rk_ctx *ctx, const rk_recur *recur, uint64_t
     if (state_out) { A.state_out = (float *)state_out->data; A.so_st = state_out->stride; }
     uint64_t blocks;
     if ((rc = tiles_of(ctx, A, RC_WAVES * RC_FORWARD_ROWS, state_out != nullptr, blocks)) != RK_OK) return rc;
-    with_type(z->type, [&](auto t) { k_recur_forward<decltype(t)><<<(uint32_t)blocks, RC_THREADS, 0, ctx->stream>>>(A); });
+    with_kernel(A, z->type, [&](auto t, auto coupled, auto cut) {
+        k_recur_forward<decltype(t), decltype(coupled)::value, decltype(cut)::value><<<(uint32_t)blocks, RC_THREADS, 0, ctx->stream>>>(A);
+    });
     RK_CHECK_LAUNCH(ctx, "k_recur_forward");
     return RK_OK;
 }
@@ -520,7 +585,9 @@ extern "C" int32_t rk_recur_backward(rk_ctx *ctx, const rk_recur *recur, uint64_
     uint64_t blocks;
     if ((rc = tiles_of(ctx, A, RC_WAVES * (z->type == RK_F32 ? back_rows<float>() : back_rows<__bf16>()), d_state_in != nullptr, blocks)) != RK_OK) return rc;
     if (blocks) {
-        with_type(z->type, [&](auto t) { k_recur_backward<decltype(t)><<<(uint32_t)blocks, RC_THREADS, 0, ctx->stream>>>(A); });
+        with_kernel(A, z->type, [&](auto t, auto coupled, auto cut) {
+            k_recur_backward<decltype(t), decltype(coupled)::value, decltype(cut)::value><<<(uint32_t)blocks, RC_THREADS, 0, ctx->stream>>>(A);
+        });
         RK_CHECK_LAUNCH(ctx, "k_recur_backward");
     }
     if (d_bias && A.n_tiles != 1) {
