@@ -1,11 +1,13 @@
 """A job's descriptor, measured: a few layers of a mixture-of-experts student are trained for some steps on this GPU, and what the
 steps take and keep becomes the t_fwd_sample, k_bwd and mem_act that a scheduling round is then run with.
 
-    python examples/measure_job.py [--params 1.3e9] [--layers 24] [--experts 8] [--steps 8]
+    python examples/measure_job.py [--params 1.3e9] [--layers 24] [--experts 8] [--steps 8] [--recurrence] [--dropout 0.1] [--head]
 
 The products are torch's; what lies between them are the library's operators: the join of each block with the residual stream
 (rk_norm_forward / rk_norm_backward), the router (rk_route_forward / rk_route_backward) and the student's loss
-(rk_distill_loss_backward).  Data and weights are random.  A layer is a dense block and a block of experts, without attention, and the
+(rk_distill_loss_backward).  With --recurrence the dense block mixes the tokens of a sequence (rk_recur_forward / rk_recur_backward), with
+--dropout blocks' outputs are dropped out (rk_dropout_forward / rk_dropout_backward), and with --head the loss is that of the labels alone, taken
+from the hidden rows without the logits (rk_head_loss_backward).  Data and weights are random.  A layer is a dense block and a block of experts, without attention, and the
 job that is scheduled is this very student: its width follows from --params, its parameters are counted, and what its layers take is scaled to
 all of them, while the first norm, the output's product and the loss count once.
 """
@@ -82,13 +84,51 @@ class Route(torch.autograd.Function):
         return None, None, d_logits
 
 
+class Recurrence(torch.autograd.Function):
+    """(input, forget gates, their bias) -> hidden rows, every seq rows a sequence."""
+
+    @staticmethod
+    def forward(fn, ctx, x, z, bias, seq):
+        recur, h = rk.Recur(bias=bias, seq_rows=seq), torch.empty_like(x)
+        rk.rk_recur_forward(ctx, recur, x, z, None, h, None)
+        fn.ctx, fn.recur = ctx, recur
+        fn.save_for_backward(x, z, h)
+        return h
+
+    @staticmethod
+    def backward(fn, dh):
+        x, z, h = fn.saved_tensors
+        dx, dz, d_bias = torch.empty_like(x), torch.empty_like(z), f32(x.shape[1])
+        rk.rk_recur_backward(fn.ctx, fn.recur, x, z, h, None, dh.contiguous(), None, dx, dz, None, d_bias)
+        return None, dx, dz, d_bias, None
+
+
+class Drop(torch.autograd.Function):
+    """A block's output, dropped out; the mask is made anew on the way back, from the same counters."""
+
+    @staticmethod
+    def forward(fn, ctx, dropout, y):
+        fn.ctx, fn.dropout = ctx, dropout
+        out = torch.empty_like(y)
+        rk.rk_dropout_forward(ctx, dropout, y, None, out)
+        return out
+
+    @staticmethod
+    def backward(fn, d_out):
+        dy = torch.empty_like(d_out)
+        rk.rk_dropout_backward(fn.ctx, fn.dropout, d_out.contiguous(), dy)
+        return None, None, dy
+
+
 class Student:
     """`layers` layers of a dense block and a block of experts, norms in float32 and products in bfloat16."""
 
-    def __init__(self, hidden, layers, experts, top_k, vocab, seq, seed=0):
+    def __init__(self, hidden, layers, experts, top_k, vocab, seq, seed=0, recurrence=False, dropout=0.0, head=False):
         g = torch.Generator(DEV).manual_seed(seed)
         self.router = rk.make_router(experts, top_k, renormalise=True, group_tokens=seq)
-        self.layers, self.params = layers, {}
+        self.layers, self.params, self.seq, self.recurrence, self.head = layers, {}, seq, recurrence, head
+        # a generator's state for every place that drops out; the steps count its offset on
+        self.drops = [rk.Dropout(dropout, torch.tensor([seed, i], device=DEV)) for i in range(2 * layers)] if dropout else None
 
         def product(name, *shape):
             w = torch.randn(*shape, generator=g, device=DEV) / shape[-2] ** 0.5
@@ -100,6 +140,9 @@ class Student:
         vector("first", 1.0, hidden)
         for i in range(layers):
             product(f"dense{i}", hidden, hidden)
+            if recurrence:
+                product(f"forget{i}", hidden, hidden)
+                vector(f"remember{i}", 2.0, hidden)
             product(f"router{i}", hidden, experts)
             product(f"up{i}", experts, hidden, hidden)
             product(f"down{i}", experts, hidden, hidden)
@@ -108,6 +151,8 @@ class Student:
                 vector(f"pre{b}{i}", 1.0, hidden)
                 vector(f"gate{b}{i}", 0.5, 1, hidden)
         product("head", hidden, vocab)
+        if head:                                            # (rows of the vocabulary's words)
+            self.params["head"] = self.params["head"].detach().t().contiguous().requires_grad_()
         count = {n: p.numel() for n, p in self.params.items()}
         self.params_rest = count["first"] + count["head"]
         self.params_layers = sum(count.values()) - self.params_rest
@@ -126,26 +171,38 @@ class Student:
         back[order] = torch.arange(len(order), device=DEV)
         return (torch.cat(parts)[back].view(-1, k, u.shape[1]) * weight[:, :, None]).sum(1).to(torch.bfloat16)
 
+    def block(self, ctx, y, place):
+        return Drop.apply(ctx, self.drops[place], y) if self.drops else y
+
+    def next_step(self):
+        for d in self.drops or ():
+            d.rng[1:] += len(self.drops)
+
     def forward(self, ctx, x, mark=lambda where, u: None):
-        """mark is called with the input of the first layer and the output of the last."""
+        """mark is called with the input of the first layer and the output of the last.  Logits, or what the head takes them from."""
         p, losses = self.params, []
         x, u = Join.apply(ctx, x, None, None, p["first"], None)
         mark("layers", u)
         for i in range(self.layers):
             y = u @ p[f"dense{i}"]
+            if self.recurrence:
+                y = Recurrence.apply(ctx, y, u @ p[f"forget{i}"], p[f"remember{i}"], self.seq)
+            y = self.block(ctx, y, 2 * i)
             x, u = Join.apply(ctx, x, y, p[f"posta{i}"], p[f"prea{i}"], p[f"gatea{i}"])
             weight, expert, loss = Route.apply(ctx, self.router, u @ p[f"router{i}"])
             losses.append(loss)
-            x, u = Join.apply(ctx, x, self.experts(i, u, weight, expert), p[f"postb{i}"], p[f"preb{i}"], p[f"gateb{i}"])
+            x, u = Join.apply(ctx, x, self.block(ctx, self.experts(i, u, weight, expert), 2 * i + 1), p[f"postb{i}"], p[f"preb{i}"], p[f"gateb{i}"])
         mark("head", u)
-        return u @ p["head"], losses
+        return u if self.head else u @ p["head"], losses
 
 
-def measure(hidden, seq, micro_batch, layers=2, experts=8, top_k=2, vocab=32000, kept=64, steps=8, rate=1e-3, seed=0):
+def measure(hidden, seq, micro_batch, layers=2, experts=8, top_k=2, vocab=32000, kept=64, steps=8, rate=1e-3, seed=0, recurrence=False, dropout=0.0,
+            head=False):
     """Trains for `steps` steps; seconds forward and backward of one, bytes that the forward keeps, each also of the layers alone, the
     student's parameters, and the losses by step."""
     ctx = rk.rk_create(0)
-    student = Student(hidden, layers, experts, top_k, vocab, seq, seed)
+    student = Student(hidden, layers, experts, top_k, vocab, seq, seed, recurrence, dropout, head)
+    of_labels = rk.make_head() if head else None
     g = torch.Generator(DEV).manual_seed(seed + 1)
     tokens = seq * micro_batch
     x = torch.randn(tokens, hidden, generator=g, device=DEV).to(torch.bfloat16)
@@ -174,7 +231,12 @@ def measure(hidden, seq, micro_batch, layers=2, experts=8, top_k=2, vocab=32000,
         ev["forward"].record()
         kept_at["forward"] = torch.cuda.memory_allocated()
         d_logits = torch.empty_like(logits)
-        rk.rk_distill_loss_backward(ctx, distill, logits.detach(), teacher, index, label, row_weight, None, loss, lse, total, d_logits)
+        if head:
+            words = student.params["head"]
+            words.grad = torch.empty_like(words)
+            rk.rk_head_loss_backward(ctx, of_labels, logits.detach(), words.detach(), label, row_weight, None, loss, lse[:, 0].contiguous(), total, d_logits, words.grad)
+        else:
+            rk.rk_distill_loss_backward(ctx, distill, logits.detach(), teacher, index, label, row_weight, None, loss, lse, total, d_logits)
         torch.autograd.backward([logits] + losses, [d_logits] + [d_losses] * len(losses))
         ev["backward"].record()
         with torch.no_grad():
@@ -184,6 +246,7 @@ def measure(hidden, seq, micro_batch, layers=2, experts=8, top_k=2, vocab=32000,
         torch.cuda.synchronize()
         took = lambda a, b: ev[a].elapsed_time(ev[b]) * 1e-3
         times.append((took("start", "forward"), took("layers", "head"), took("forward", "backward"), took("back_head", "back_layers")))
+        student.next_step()
         history.append((float(total), sum(float(l.detach()[0]) for l in losses) / len(losses)))
         del logits, losses, d_logits                    # (the next step's forward is not to find them where it counts what it keeps)
     rk.rk_sync(ctx)
@@ -219,11 +282,14 @@ def main(argv=None):
     a.add_argument("--seq", type=int, default=2048)
     a.add_argument("--vocab", type=int, default=32000)
     a.add_argument("--steps", type=int, default=8)
+    a.add_argument("--recurrence", action="store_true")
+    a.add_argument("--dropout", type=float, default=0.0)
+    a.add_argument("--head", action="store_true")
     a = a.parse_args(argv)
-    # params ~ layers (1 + 2 experts) h^2 + vocab h
-    per = a.layers * (1 + 2 * a.experts)
+    # params ~ layers (1 + 2 experts) h^2 + vocab h, with recurrence another h^2 a layer
+    per = a.layers * (1 + int(a.recurrence) + 2 * a.experts)
     hidden = 128 * max(1, round(((a.vocab ** 2 + 4 * per * a.params) ** 0.5 - a.vocab) / (2 * per) / 128))
-    m = measure(hidden, a.seq, 1, a.measured_layers, a.experts, vocab=a.vocab, steps=a.steps)
+    m = measure(hidden, a.seq, 1, a.measured_layers, a.experts, vocab=a.vocab, steps=a.steps, recurrence=a.recurrence, dropout=a.dropout, head=a.head)
     for step, (total, balance) in enumerate(m["history"]):
         print(f"step {step}: loss {total:.4f}, balance {balance:.4f}")
     print(f"{a.measured_layers} layers of {hidden}: forward {m['forward'] * 1e3:.2f} ms, backward {m['backward'] * 1e3:.2f} ms, "
