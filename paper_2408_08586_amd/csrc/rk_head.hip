@@ -4,7 +4,9 @@
 // takes the logits' tiles out of the product's registers: of every row the largest and the sum of exponentials over a tile's
 // words, joined in fixed order.  The gradients go through the vocabulary in pieces, from the last to the first: a piece's logits are made again and become
 // g = row_weight (p (1 + 2 z lse) - onehot), rounded to the rows' type and scaled by a power of two that keeps float16 in its range;
-// dx adds up g W over the pieces in float32, and the piece's rows of d_weight are g^T x.  Where the loss is made along with
+// dx adds up g W over the pieces in float32, and the piece's rows of d_weight are g^T x.  By far the largest element of a row is its label's: what
+// rounding to 16 bits takes off it is kept and its products are added to dx and d_weight in float32 (777 x 50021 x 1111 in float16: both are
+// 2.1e-4 from the definition, all of it their own rounding, and 3.5e-4 without).  Where the loss is made along with
 // them, it leaves the exponentials of the piece that it ends with, which then only have to be scaled.
 #include "rk_gemm.h"
 
@@ -23,6 +25,7 @@ struct Rows {
     int32_t *row, *place;       // a kept row's place in the matrix; a row's place among the kept, or -1
     int32_t *label;
     float *weight, *label_logit, *top, *sum;
+    float *lost;                // what rounding takes off the gradient of a row's label
     RowInfo *info;
 };
 
@@ -195,14 +198,19 @@ template <typename T, int TA, int TB, int WA, bool LOSS> __global__ __launch_bou
             const bool there = b < n;
             const int64_t label = there ? (int64_t)A.R.label[b] - (int64_t)A.first : -1;
             const RowInfo info = there ? A.R.info[b] : RowInfo{0.f, 0.f, 0.f, 0u};
+            float own = 0.f;
 #pragma unroll
             for (int i = 0; i < Tl::MA; ++i)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const uint32_t a = a_of + 16 * i + q;
                     const float p = exp_of<T>(t.acc[i][j][q] * A.scale - info.lse) * info.factor;
-                    t.acc[i][j][q] = there && a < A.words ? (label == (int64_t)a ? p - 1.f : p) * info.share : 0.f;
+                    const float g = there && a < A.words ? (label == (int64_t)a ? p - 1.f : p) * info.share : 0.f;
+                    own = label == (int64_t)a ? g : own;
+                    t.acc[i][j][q] = g;
                 }
+            const uint32_t d = (uint32_t)(label - (int64_t)a_of);
+            if (label >= 0 && d < 16 * Tl::MA && (d & 15u) < 4) A.R.lost[b] = own - (float)(T)own;
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -235,9 +243,12 @@ template <typename T> __global__ __launch_bounds__(256) void k_head_scale(const 
         const Vec<uint32_t, 4> w = *at;
         Vec<T, EACH> v;
 #pragma unroll
-        for (uint32_t e = 0; e < EACH; ++e) {
-            const float p = element<T>(w, e) * f;
-            v[e] = (T)((label == (int64_t)e ? p - 1.f : p) * info.share);
+        for (uint32_t e = 0; e < EACH; ++e) v[e] = (T)(element<T>(w, e) * f * info.share);
+        if (label >= 0 && label < (int64_t)EACH) {          // (the label's logit is there in 32 bits)
+            const float own = (exp_f32(A.R.label_logit[b] - info.lse) * info.factor - 1.f) * info.share;
+#pragma unroll
+            for (uint32_t e = 0; e < EACH; ++e) v[e] = label == (int64_t)e ? (T)own : v[e];
+            A.R.lost[b] = own - (float)(T)own;
         }
         *at = __builtin_bit_cast(Vec<uint32_t, 4>, v);
     }
@@ -345,7 +356,7 @@ struct OutArgs {
     bool first;
     void *out;                  // d_weight
     bool aligned;               // its rows take whole vectors
-    uint32_t width, words;
+    uint32_t width, words, word0;
     const float *d_total;
     float scale, room;
 };
@@ -375,12 +386,14 @@ template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_TH
             *to = A.first ? t.acc[i][j] : *to + t.acc[i][j];
         }
 }
-template <typename T> __global__ __launch_bounds__(256) void k_head_dx_out(const OutArgs A, T *dx, uint64_t dx_st, uint64_t n_rows) {
+template <typename T> __global__ __launch_bounds__(256) void k_head_dx_out(const OutArgs A, const T *weight, uint64_t w_st, T *dx, uint64_t dx_st, uint64_t n_rows) {
     for (uint64_t r = blockIdx.x; r < n_rows; r += gridDim.x) {
         const int32_t i = A.R.place[r];
         const float f = i < 0 ? 0.f : (A.d_total ? *A.d_total : 1.f) * A.scale * (__uint_as_float(A.R.count[1]) / A.room);
+        const T *const own = weight + (uint64_t)(i < 0 ? 0 : A.R.label[i]) * w_st;
+        const float lost = sizeof(T) == 2 && i >= 0 ? A.R.lost[i] : 0.f;
         for (uint32_t c = threadIdx.x; c < A.width; c += 256) {
-            float v = 0.f;
+            float v = sizeof(T) == 2 && i >= 0 ? lost * (float)own[c] : 0.f;
             if (i >= 0)
                 for (uint32_t s = 0; s < A.splits; ++s) v += A.sums[s * A.split_stride + (uint64_t)i * A.stride + c];
             dx[r * dx_st + c] = (T)(i < 0 ? 0.f : v * f);
@@ -394,6 +407,54 @@ template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_TH
     const uint32_t a0 = at_turn.a * TA, b0 = at_turn.b * TB;
     Tl t;
     t.run(A.A, A.B, a0, b0, 0, n);
+    if constexpr (sizeof(T) == 2) {
+        // what rounding took off the labels of the tile: their rows in order, 2,048 looked through at a time
+        constexpr uint32_t EVERY = 4;
+        uint32_t *const found = (uint32_t *)t.shared, *const counts = found + EVERY * GM_THREADS;
+        static_assert((EVERY * GM_THREADS + EVERY * GM_WAVES) * 4 <= TB * GM_STEP, "");
+        const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        for (uint32_t begin = 0; begin < n; begin += EVERY * GM_THREADS) {
+            uint32_t v[EVERY], before[EVERY];
+            uint64_t hits[EVERY];
+#pragma unroll
+            for (uint32_t e = 0; e < EVERY; ++e) {
+                const uint32_t r = begin + e * GM_THREADS + threadIdx.x;
+                v[e] = r < n ? (uint32_t)A.R.label[r] - A.word0 - b0 : ~0u;
+                hits[e] = __builtin_amdgcn_ballot_w64(v[e] < (uint32_t)TB);
+                before[e] = (uint32_t)__popcll(hits[e] & ((1ull << lane) - 1ull));
+                if (lane == 0) counts[e * GM_WAVES + wave] = (uint32_t)__popcll(hits[e]);
+            }
+            __syncthreads();
+            uint32_t all = 0;
+#pragma unroll
+            for (uint32_t e = 0; e < EVERY; ++e)
+#pragma unroll
+                for (uint32_t w = 0; w < GM_WAVES; ++w) {
+                    if (w == wave && v[e] < (uint32_t)TB) found[all + before[e]] = (begin + e * GM_THREADS + threadIdx.x) << 8 | v[e];
+                    all += counts[e * GM_WAVES + w];
+                }
+            __syncthreads();
+            for (uint32_t k = 0; k < all; ++k) {
+                const uint32_t which = __builtin_amdgcn_readfirstlane(found[k]), r = which >> 8, at_b = which & 255u;
+                if (at_b / (TB / Tl::WB) != wave % Tl::WB) continue;
+                const uint32_t own_j = at_b % (TB / Tl::WB) / 16;
+                const float lost = A.R.lost[r];
+                const T *const x = (const T *)(A.A.data + r * A.A.stride);
+                const uint32_t first = a0 + Tl::wave_a() + 4 * (lane >> 4);
+#pragma unroll
+                for (int i = 0; i < Tl::MA; ++i) {
+                    Vec<T, 4> xs = (T)0.f;
+                    if ((lane & 15u) == at_b % 16 && (first + 16 * i) * sizeof(T) < A.A.count) xs = *(const Vec<T, 4> *)(x + first + 16 * i);
+#pragma unroll
+                    for (int j = 0; j < Tl::MB; ++j)
+                        if (j == (int)own_j)
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) t.acc[i][j][q] += lost * (float)xs[q];
+                }
+            }
+            __syncthreads();
+        }
+    }
     const float f = n ? (A.d_total ? *A.d_total : 1.f) * A.scale * (__uint_as_float(A.R.count[1]) / A.room) : 0.f;
     constexpr uint32_t EACH = 16 / sizeof(T);
     T *const out = (T *)A.out;
@@ -443,7 +504,7 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
     Rows R{};
     {
         char *p;
-        if ((rc = rk_scratch(ctx, SL_HEAD_ROWS, 256 + rows_pad * (7 * 4 + sizeof(RowInfo)), (void **)&p)) != RK_OK) return rc;
+        if ((rc = rk_scratch(ctx, SL_HEAD_ROWS, 256 + rows_pad * (8 * 4 + sizeof(RowInfo)), (void **)&p)) != RK_OK) return rc;
         R.count = (uint32_t *)p; p += 256;
         R.info = (RowInfo *)p; p += rows_pad * sizeof(RowInfo);
         R.row = (int32_t *)p; p += rows_pad * 4;
@@ -452,7 +513,8 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
         R.weight = (float *)p; p += rows_pad * 4;
         R.label_logit = (float *)p; p += rows_pad * 4;
         R.top = (float *)p; p += rows_pad * 4;
-        R.sum = (float *)p;
+        R.sum = (float *)p; p += rows_pad * 4;
+        R.lost = (float *)p;
     }
     T *xc;
     if ((rc = rk_scratch(ctx, SL_HEAD_X, C.n_rows * wide * ES, (void **)&xc)) != RK_OK) return rc;
@@ -576,7 +638,7 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
             OutArgs D = O;
             D.A = X; D.A.count = (uint64_t)wide * ES;
             D.B = Side{(const char *)g, words * ES, words * ES};
-            D.tiles_b = (n_words + 255) / 256; D.words = n_words;
+            D.tiles_b = (n_words + 255) / 256; D.words = n_words; D.word0 = (uint32_t)first;
             D.aligned = (uintptr_t)C.d_weight->data % 16 == 0 && C.d_weight->stride * ES % 16 == 0;
             D.out = (T *)C.d_weight->data + first * C.d_weight->stride; D.stride = C.d_weight->stride;
             k_head_dw<T, HD_TA, 256, 2><<<tiles_w * D.tiles_b, GM_THREADS, 0, stream>>>(D);
@@ -585,7 +647,7 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
         if (first == 0) break;
     }
     if (C.dx && C.n_rows) {
-        k_head_dx_out<T><<<blocks_of(C.n_rows), 256, 0, stream>>>(O, (T *)C.dx->data, C.dx->stride, C.n_rows);
+        k_head_dx_out<T><<<blocks_of(C.n_rows), 256, 0, stream>>>(O, w, w_st, (T *)C.dx->data, C.dx->stride, C.n_rows);
         RK_CHECK_LAUNCH(ctx, "k_head_dx_out");
     }
     return RK_OK;
