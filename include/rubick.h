@@ -969,7 +969,7 @@ typedef struct {
 
 /* x, z and h share a type; states are RK_F32 matrices, a row a sequence.  state_in null: zeros; state_out null: not kept;
  * that of a sequence without rows is its state_in.  h may be x or z, state_out may be state_in (same data and
- * stride).  A NaN stays in its sequence.  Up to 2^31 - 1 rows. */
+ * stride).  A NaN stays in its sequence; a row of h that is infinite may be followed by NaN there.  Up to 2^31 - 1 rows. */
 int32_t rk_recur_forward(rk_ctx *ctx, const rk_recur *recur, uint64_t n_rows, uint32_t width, const rk_matrix *x,
                          const rk_matrix *z, const rk_matrix *state_in_or_null, const rk_matrix *h,
                          const rk_matrix *state_out_or_null);
@@ -1024,8 +1024,8 @@ int32_t rk_head_loss(rk_ctx *ctx, const rk_head *head, uint64_t n_rows, uint32_t
 
 /* The gradients of x and weight (either null: not wanted; not both) from that of total (d_total [device] one float, null:
  * one) and the forward pass's lse.  They have x's type; neither may overlap an input.  The logits' gradients are
- * made in pieces of the vocabulary and rounded to x's type on their way into the products, relative to their row's weight for dx and
- * to the largest row's weight for d_weight. */
+ * made in pieces of the vocabulary and rounded to x's type on their way into the products (their labels' in 32 bits); float16 keeps
+ * them down to 2^-38 of the largest row's weight. */
 int32_t rk_head_backward(rk_ctx *ctx, const rk_head *head, uint64_t n_rows, uint32_t width, uint32_t vocab, const rk_matrix *x,
                          const rk_matrix *weight, const int32_t *label, const float *row_weight_or_null, const float *lse,
                          const float *d_total_or_null, const rk_matrix *dx_or_null, const rk_matrix *d_weight_or_null);

@@ -91,22 +91,28 @@ __global__ __launch_bounds__(HD_THREADS) void k_head_rows(const RowsArgs A) {
     if (threadIdx.x == 0) A.R.count[0] = before;
 }
 
-// the kept rows of x one behind the other, each padded with zeros; a workgroup a row
-template <typename T> __global__ __launch_bounds__(256) void k_head_gather(const Rows R, const T *x, uint64_t stride, uint32_t width, T *out, uint32_t out_width) {
-    for (uint32_t i = blockIdx.x; i < R.count[0]; i += gridDim.x) {
-        const T *const from = x + (uint64_t)R.row[i] * stride;
-        T *const to = out + (uint64_t)i * out_width;
-        for (uint32_t c = threadIdx.x; c < out_width; c += 256) to[c] = c < width ? from[c] : (T)0.f;
+// Rows one behind the other, each padded with zeros to out_width (a multiple of 16 bytes): the kept ones of x (count rows of R), or n_rows as they lie
+// (count null).  A lane takes 16 bytes of the result, whatever the alignment of what it reads.
+template <typename T> using Loose = Vec<uint32_t, 4> __attribute__((aligned(sizeof(T))));
+template <typename T> __global__ __launch_bounds__(256) void k_head_pad(const int32_t *row, const uint32_t *count, uint32_t n_rows, const T *x, uint64_t stride, uint32_t width, T *out, uint32_t out_width) {
+    constexpr uint32_t EACH = 16 / sizeof(T);
+    const uint32_t per_row = out_width / EACH, rows = count ? *count : n_rows;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < (uint64_t)rows * per_row; i += (uint64_t)gridDim.x * 256) {
+        const uint32_t r = (uint32_t)(i / per_row), c = (uint32_t)(i - (uint64_t)r * per_row) * EACH;
+        const T *const from = x + (uint64_t)(row ? (uint32_t)row[r] : r) * stride + c;
+        Vec<uint32_t, 4> w;
+        if (c + EACH <= width) {
+            w = *(const Loose<T> *)from;
+        } else {
+            Vec<T, EACH> v = (T)0.f;
+#pragma unroll
+            for (uint32_t e = 0; e < EACH; ++e) if (c + e < width) v[e] = from[e];
+            w = __builtin_bit_cast(Vec<uint32_t, 4>, v);
+        }
+        *(Vec<uint32_t, 4> *)(out + (uint64_t)r * out_width + c) = w;
     }
 }
-// rows of any alignment as rows padded with zeros
-template <typename T> __global__ __launch_bounds__(256) void k_head_pad(const T *x, uint64_t stride, uint32_t n_rows, uint32_t width, T *out, uint32_t out_width) {
-    for (uint32_t i = blockIdx.x; i < n_rows; i += gridDim.x) {
-        const T *const from = x + (uint64_t)i * stride;
-        T *const to = out + (uint64_t)i * out_width;
-        for (uint32_t c = threadIdx.x; c < out_width; c += 256) to[c] = c < width ? from[c] : (T)0.f;
-    }
-}
+
 struct LogitsArgs {
     Rows R;
     Side W, X;                  // of this piece; the kept rows
@@ -308,14 +314,6 @@ __device__ __forceinline__ double block_sum(double v, double *lds) {
     }
     return lds[0];
 }
-__global__ __launch_bounds__(HD_THREADS) void k_head_total(const JoinArgs A) {
-    __shared__ double lds[HD_THREADS];
-    double v = 0.0;
-    for (uint32_t i = threadIdx.x; i < A.R.count[0]; i += HD_THREADS) v += (double)A.R.weight[i] * (double)A.loss[A.R.row[i]];
-    v = block_sum(v, lds);
-    if (threadIdx.x == 0) *A.total = (float)v;
-}
-
 // 2^n with 2^n >= v (1 for what is no positive finite number)
 __device__ __forceinline__ float power_above(float v) {
     if (!(v > 0.f) || !(v < 1e38f)) return 1.f;
@@ -323,26 +321,42 @@ __device__ __forceinline__ float power_above(float v) {
     const float m = frexpf(v, &e);
     return ldexpf(1.f, m == 0.5f ? e - 1 : e);
 }
-// The numbers that g is made with.  room: what g's largest element may be (a power of two).
-__global__ __launch_bounds__(HD_THREADS) void k_head_info(const Rows R, const float *lse_of, float z_weight, float room) {
-    __shared__ float lds[HD_THREADS];
-    const uint32_t n = R.count[0];
+// What one workgroup does behind the loss: the total (null: there was none), and, with room > 0, the numbers that g is made with; room: what g's
+// largest element may be (a power of two).
+struct EndArgs {
+    Rows R;
+    const float *loss, *lse;
+    float *total;
+    float z_weight, room;
+};
+__global__ __launch_bounds__(HD_THREADS) void k_head_end(const EndArgs A) {
+    __shared__ double lds[HD_THREADS];
+    const uint32_t n = A.R.count[0];
+    if (A.total) {
+        double v = 0.0;
+        for (uint32_t i = threadIdx.x; i < n; i += HD_THREADS) v += (double)A.R.weight[i] * (double)A.loss[A.R.row[i]];
+        v = block_sum(v, lds);
+        if (threadIdx.x == 0) *A.total = (float)v;
+    }
+    if (!(A.room > 0.f)) return;
     float most = 0.f;
     for (uint32_t i = threadIdx.x; i < n; i += HD_THREADS) {
-        const float factor = 1.f + 2.f * z_weight * lse_of[R.row[i]], v = fabsf(R.weight[i]) * fmaxf(1.f, fabsf(factor));
+        const float factor = 1.f + 2.f * A.z_weight * A.lse[A.R.row[i]], v = fabsf(A.R.weight[i]) * fmaxf(1.f, fabsf(factor));
         if (v < 1e38f) most = fmaxf(most, v);
     }
-    lds[threadIdx.x] = most;
+    __syncthreads();
+    float *const tops = (float *)lds;
+    tops[threadIdx.x] = most;
     __syncthreads();
     for (uint32_t d = HD_THREADS / 2; d; d /= 2) {
-        if (threadIdx.x < d) lds[threadIdx.x] = fmaxf(lds[threadIdx.x], lds[threadIdx.x + d]);
+        if (threadIdx.x < d) tops[threadIdx.x] = fmaxf(tops[threadIdx.x], tops[threadIdx.x + d]);
         __syncthreads();
     }
-    const float unit = power_above(lds[0]);
-    if (threadIdx.x == 0) R.count[1] = __float_as_uint(unit);
+    const float unit = power_above(tops[0]);
+    if (threadIdx.x == 0) A.R.count[1] = __float_as_uint(unit);
     for (uint32_t i = threadIdx.x; i < n; i += HD_THREADS) {
-        const float lse = lse_of[R.row[i]], factor = 1.f + 2.f * z_weight * lse;
-        R.info[i] = RowInfo{lse, factor, R.weight[i] / unit * room, 0u};
+        const float lse = A.lse[A.R.row[i]], factor = 1.f + 2.f * A.z_weight * lse;
+        A.R.info[i] = RowInfo{lse, factor, A.R.weight[i] / unit * A.room, 0u};
     }
 }
 
@@ -386,18 +400,27 @@ template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_TH
             *to = A.first ? t.acc[i][j] : *to + t.acc[i][j];
         }
 }
+// a lane four columns of a row, a workgroup's first index its columns
 template <typename T> __global__ __launch_bounds__(256) void k_head_dx_out(const OutArgs A, const T *weight, uint64_t w_st, T *dx, uint64_t dx_st, uint64_t n_rows) {
-    for (uint64_t r = blockIdx.x; r < n_rows; r += gridDim.x) {
+    const uint32_t c = (blockIdx.x * 256u + threadIdx.x) * 4u;
+    if (c >= A.width) return;
+    for (uint64_t r = blockIdx.y; r < n_rows; r += gridDim.y) {
         const int32_t i = A.R.place[r];
-        const float f = i < 0 ? 0.f : (A.d_total ? *A.d_total : 1.f) * A.scale * (__uint_as_float(A.R.count[1]) / A.room);
-        const T *const own = weight + (uint64_t)(i < 0 ? 0 : A.R.label[i]) * w_st;
-        const float lost = sizeof(T) == 2 && i >= 0 ? A.R.lost[i] : 0.f;
-        for (uint32_t c = threadIdx.x; c < A.width; c += 256) {
-            float v = sizeof(T) == 2 && i >= 0 ? lost * (float)own[c] : 0.f;
-            if (i >= 0)
-                for (uint32_t s = 0; s < A.splits; ++s) v += A.sums[s * A.split_stride + (uint64_t)i * A.stride + c];
-            dx[r * dx_st + c] = (T)(i < 0 ? 0.f : v * f);
+        Vec<float, 4> v = 0.f;
+        if (i >= 0) {
+            if constexpr (sizeof(T) == 2) {
+                const T *const own = weight + (uint64_t)A.R.label[i] * w_st + c;
+                const float lost = A.R.lost[i];
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e) v[e] = c + e < A.width ? lost * (float)own[e] : 0.f;
+            }
+            const float *const from = A.sums + (uint64_t)i * A.stride + c;
+#pragma unroll 8
+            for (uint32_t s = 0; s < A.splits; ++s) v += *(const Vec<float, 4> *)(from + s * A.split_stride);
+            v *= (A.d_total ? *A.d_total : 1.f) * A.scale * (__uint_as_float(A.R.count[1]) / A.room);
         }
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) if (c + e < A.width) dx[r * dx_st + c + e] = (T)v[e];
     }
 }
 template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_THREADS) void k_head_dw(const OutArgs A) {
@@ -485,12 +508,25 @@ struct Call {
     const rk_matrix *dx, *d_weight;
     const float *given_lse;
 };
-// f(rows of a tile, wavefronts along its words): few rows take small tiles, which leave LDS for two workgroups a compute unit
-template <typename F> void with_rows(uint32_t tile, F f) {
+// f(rows of a tile, wavefronts along its words)
+template <typename T, typename F> void with_rows(uint32_t tile, F f) {
     if (tile == 32) f(std::integral_constant<int, 32>(), std::integral_constant<int, 8>());
     else if (tile == 64) f(std::integral_constant<int, 64>(), std::integral_constant<int, 8>());
     else if (tile == 128) f(std::integral_constant<int, 128>(), std::integral_constant<int, 4>());
-    else f(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
+    else if (tile == 256) f(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
+    else if constexpr (sizeof(T) == 4) f(std::integral_constant<int, 192>(), std::integral_constant<int, 2>());
+}
+// Rows of a tile.  Few take small tiles, which leave LDS for two workgroups a compute unit (5 x 128000 x 5248: 258 us, with tiles of 256 rows 368).
+// More of 16 bits take the largest, even where it is half empty (300 x 64000 x 4096: 238 us, of 192 rows 244, of 128 rows 263); of 32 bits, where only
+// the matrix units' time counts, the one that has the fewest rows in all turns of the compute units (300 x 64000 x 4096: 1,867, 1,451 and 1,420 us).
+template <typename T> uint32_t rows_of_tile(uint64_t n_rows, uint64_t tiles_a) {
+    if (n_rows <= 128) return n_rows <= 32 ? 32 : n_rows <= 64 ? 64 : 128;
+    uint32_t best = 256;
+    if (sizeof(T) == 4) {
+        auto cost = [&](uint64_t tile) { return (tiles_a * ((n_rows + tile - 1) / tile) + 255) / 256 * tile; };
+        for (uint32_t tile : {192u, 128u}) if (cost(tile) < cost(best)) best = tile;
+    }
+    return best;
 }
 uint64_t up_to(uint64_t v, uint64_t m) { return (v + m - 1) / m * m; }
 uint32_t blocks_of(uint64_t n) { return (uint32_t)(n < (1u << 20) ? n : 1u << 20); }
@@ -521,15 +557,15 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
     k_head_rows<<<1, HD_THREADS, 0, stream>>>(RowsArgs{R, C.label, C.row_weight, C.loss, C.lse, C.n_rows, C.vocab});
     RK_CHECK_LAUNCH(ctx, "k_head_rows");
     if (C.n_rows) {
-        k_head_gather<T><<<blocks_of(C.n_rows), 256, 0, stream>>>(R, (const T *)C.x->data, C.x->stride, C.width, xc, wide);
-        RK_CHECK_LAUNCH(ctx, "k_head_gather");
+        k_head_pad<T><<<blocks_of((C.n_rows * wide * ES / 16 + 255) / 256), 256, 0, stream>>>(R.row, R.count, 0, (const T *)C.x->data, C.x->stride, C.width, xc, wide);
+        RK_CHECK_LAUNCH(ctx, "k_head_pad");
     }
     const Side X = {(const char *)xc, (uint64_t)wide * ES, 0};
     const T *const w = (const T *)C.weight->data;
     const uint64_t w_st = C.weight->stride;
     // rows of W go into the product as they lie where their vectors do not straddle; others are padded first, piece by piece
     const bool direct = ((uintptr_t)w % 16 == 0 && w_st * ES % 16 == 0 && (uint64_t)C.width * ES % 16 == 0 && w_st * ES * 256 < GM_NOWHERE);
-    const uint32_t tile_b = C.n_rows <= 32 ? 32 : C.n_rows <= 64 ? 64 : C.n_rows <= 128 ? 128 : 256;
+    const uint32_t tile_b = rows_of_tile<T>(C.n_rows, (C.vocab + 255) / 256);
     const uint32_t tiles_b = (uint32_t)((C.n_rows + tile_b - 1) / tile_b);
     const uint64_t most_tiles = (1u << 22) / (tiles_b ? tiles_b : 1);
     const bool back = C.dx || C.d_weight;
@@ -551,7 +587,7 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
             W = Side{(const char *)(w + first * w_st), w_st * ES, 0};
             return RK_OK;
         }
-        k_head_pad<T><<<blocks_of(n_words), 256, 0, stream>>>(w + first * w_st, w_st, n_words, C.width, padded, wide);
+        k_head_pad<T><<<blocks_of(((uint64_t)n_words * wide * ES / 16 + 255) / 256), 256, 0, stream>>>(nullptr, nullptr, n_words, w + first * w_st, w_st, C.width, padded, wide);
         RK_CHECK_LAUNCH(ctx, "k_head_pad");
         W = Side{(const char *)padded, (uint64_t)wide * ES, 0};
         return RK_OK;
@@ -575,7 +611,7 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
             L.W = W; L.W.count = n_words;
             L.g = first == last_piece ? g : nullptr;
             const uint32_t tiles_a = (n_words + 255) / 256;
-            with_rows(tile_b, [&](auto tb, auto wa) {
+            with_rows<T>(tile_b, [&](auto tb, auto wa) {
                 k_head_logits<T, HD_TA, decltype(tb)::value, decltype(wa)::value, true><<<tiles_a * tiles_b, GM_THREADS, 0, stream>>>(L);
             });
             RK_CHECK_LAUNCH(ctx, "k_head_logits");
@@ -584,13 +620,10 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
             k_head_join<<<(uint32_t)((C.n_rows + 15) / 16), 16 * HD_RUNS, 0, stream>>>(J);
             RK_CHECK_LAUNCH(ctx, "k_head_join");
         }
-        k_head_total<<<1, HD_THREADS, 0, stream>>>(J);
-        RK_CHECK_LAUNCH(ctx, "k_head_total");
     }
+    k_head_end<<<1, HD_THREADS, 0, stream>>>(EndArgs{R, C.loss, C.given_lse ? C.given_lse : C.lse, C.total, C.head->z_weight, back ? room : 0.f});
+    RK_CHECK_LAUNCH(ctx, "k_head_end");
     if (!back) return RK_OK;
-
-    k_head_info<<<1, HD_THREADS, 0, stream>>>(R, C.given_lse ? C.given_lse : C.lse, C.head->z_weight, room);
-    RK_CHECK_LAUNCH(ctx, "k_head_info");
     const uint32_t tiles_w = (uint32_t)((C.width + 255) / 256);
     OutArgs O{};
     O.R = R; O.d_total = C.d_total; O.scale = C.head->logit_scale; O.room = room; O.width = C.width;
@@ -620,7 +653,7 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
         } else if (C.n_rows) {
             L.first = (uint32_t)first; L.words = n_words;
             L.W = W; L.W.count = n_words;
-            with_rows(tile_b, [&](auto tb, auto wa) {
+            with_rows<T>(tile_b, [&](auto tb, auto wa) {
                 k_head_logits<T, HD_TA, decltype(tb)::value, decltype(wa)::value, false><<<tiles_a * tiles_b, GM_THREADS, 0, stream>>>(L);
             });
             RK_CHECK_LAUNCH(ctx, "k_head_logits");
@@ -629,7 +662,7 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
             O.A = W; O.A.count = row_bytes;
             O.B = Side{(const char *)g, words * ES, 0};
             O.ks = n_words; O.tiles_b = tiles_b; O.first = first == last_piece;
-            with_rows(tile_b, [&](auto tb, auto wa) {
+            with_rows<T>(tile_b, [&](auto tb, auto wa) {
                 k_head_dx<T, HD_TA, decltype(tb)::value, decltype(wa)::value><<<tiles_w * tiles_b * O.splits, GM_THREADS, 0, stream>>>(O);
             });
             RK_CHECK_LAUNCH(ctx, "k_head_dx");
@@ -638,16 +671,17 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
             OutArgs D = O;
             D.A = X; D.A.count = (uint64_t)wide * ES;
             D.B = Side{(const char *)g, words * ES, words * ES};
-            D.tiles_b = (n_words + 255) / 256; D.words = n_words; D.word0 = (uint32_t)first;
+            D.tiles_b = tiles_a; D.words = n_words; D.word0 = (uint32_t)first;
             D.aligned = (uintptr_t)C.d_weight->data % 16 == 0 && C.d_weight->stride * ES % 16 == 0;
             D.out = (T *)C.d_weight->data + first * C.d_weight->stride; D.stride = C.d_weight->stride;
-            k_head_dw<T, HD_TA, 256, 2><<<tiles_w * D.tiles_b, GM_THREADS, 0, stream>>>(D);
+            // (tiles of 64 words, two workgroups a compute unit, were slower for few rows too: 5 x 128000 x 5248 566 instead of 436 us)
+            k_head_dw<T, HD_TA, 256, 2><<<tiles_w * tiles_a, GM_THREADS, 0, stream>>>(D);
             RK_CHECK_LAUNCH(ctx, "k_head_dw");
         }
         if (first == 0) break;
     }
     if (C.dx && C.n_rows) {
-        k_head_dx_out<T><<<blocks_of(C.n_rows), 256, 0, stream>>>(O, w, w_st, (T *)C.dx->data, C.dx->stride, C.n_rows);
+        k_head_dx_out<T><<<dim3((C.width + 1023) / 1024, (uint32_t)(C.n_rows < 32768 ? C.n_rows : 32768)), 256, 0, stream>>>(O, w, w_st, (T *)C.dx->data, C.dx->stride, C.n_rows);
         RK_CHECK_LAUNCH(ctx, "k_head_dx_out");
     }
     return RK_OK;

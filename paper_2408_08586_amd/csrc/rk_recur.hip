@@ -31,7 +31,7 @@ struct RecurArgs {
     uint32_t seq_rows, n_rows;
     uint32_t n_seqs, width, coupled, bias_type;
     uint32_t n_tiles, n_cols;       // tiles of rows; of columns
-    uint32_t *ticket;               // [n_cols] counters, RC_TICKET words apart; null: there is one tile of rows
+    uint32_t *ticket;               // [n_cols] counters, RC_TICKET words apart; null: no tile goes on with another's sequence
     uint64_t *steps;                // [n_tiles][width]: p and q
     uint32_t *behind;               // [n_tiles / RC_BLOCK][width]: the value behind a block of tiles
     float *bias_parts;              // [n_tiles][width]
@@ -181,7 +181,7 @@ __device__ __forceinline__ Vec<float, 2> join(const RecurArgs &A, Lds &lds, uint
         if (cuts >> w & 1u) { p = 0.f; q = qw; }
         else { q = pw * q + qw; p = p * pw; }
     }
-    if (!A.ticket) return q;                    // (nothing comes in to the only tile)
+    if (!A.ticket) return q;                    // (nothing comes in to any tile)
     // what the tile makes of a value
     const Vec<float, 2> all_p = cuts ? Vec<float, 2>(0.f) : p * own.p, all_q = cut ? own.q : own.p * q + own.q;
     if (order == RC_WAVES - 1)
@@ -247,7 +247,7 @@ __device__ __forceinline__ bool take(const RecurArgs &A, Lds &lds, const float *
     }
     __syncthreads();
     if (blockIdx.x < tiles) {
-        tile = lds.ticket;
+        tile = A.ticket ? lds.ticket : blockIdx.x / A.n_cols;
         column_tile = blockIdx.x % A.n_cols;
         return true;
     }
@@ -450,7 +450,7 @@ template <typename T, bool COUPLED, bool CUT> __global__ __launch_bounds__(RC_TH
     if (wave) return;
 #pragma unroll
     for (uint32_t w = 1; w < RC_WAVES; ++w) sum += lds.p[w][lane];
-    float *const to = A.ticket ? A.bias_parts + (uint64_t)tile * A.width : A.d_bias;
+    float *const to = A.n_tiles > 1 ? A.bias_parts + (uint64_t)tile * A.width : A.d_bias;
 #pragma unroll
     for (int k = 0; k < 2; ++k) if (column + k < A.width) to[column + k] = sum[k];
 }
@@ -493,7 +493,7 @@ int32_t check_recur(rk_ctx *ctx, const rk_recur *r, uint64_t n_rows, uint32_t wi
     if (width > RK_RECUR_MAX_WIDTH || n_rows > 0x7FFFFFFFull || r->n_seqs > 0x7FFFFFFEu)
         return rk_fail(ctx, RK_ERR_UNSUPPORTED, "more than 2^31 - 1 rows or sequences, or more than %u columns", RK_RECUR_MAX_WIDTH);
     if (!rk_matrix_ok(z, n_rows, width)) return rk_fail(ctx, RK_ERR_INVALID_ARG, "z null, misaligned or of a stride below the width");
-    n_seqs = r->offsets ? r->n_seqs : r->seq_rows ? (n_rows + r->seq_rows - 1) / r->seq_rows : 1;
+    n_seqs = r->offsets ? r->n_seqs : r->seq_rows ? n_rows / r->seq_rows + (n_rows % r->seq_rows != 0) : 1;
     return RK_OK;
 }
 bool alike(const rk_matrix *m, const rk_matrix *z, uint64_t n_rows, uint32_t width) { return rk_matrix_ok(m, n_rows, width) && m->type == z->type; }
@@ -514,12 +514,15 @@ int32_t tiles_of(rk_ctx *ctx, RecurArgs &A, uint32_t tile_rows, bool states, uin
     blocks = (uint64_t)A.n_tiles * A.n_cols + A.idle;
     if (blocks > RK_LAUNCH_THREADS / RC_THREADS) return rk_fail(ctx, RK_ERR_UNSUPPORTED, "2^22 tiles of %u rows and %u columns or more", tile_rows, RC_COLS);
     if (A.n_tiles < 2) return RK_OK;
+    int32_t rc;
+    if (A.d_bias && (rc = rk_scratch(ctx, SL_RECUR_BIAS, (uint64_t)A.n_tiles * A.width * 4, (void **)&A.bias_parts)) != RK_OK) return rc;
+    // whole sequences in every tile, as in a step of serving, have nothing to tell (1,024 x 2,048, one row each: 14.6 us, with a chain 17.9)
+    if (!A.offsets && tile_rows % A.seq_rows == 0) return RK_OK;
     const uint64_t words = (uint64_t)A.n_tiles * A.width, after = ((uint64_t)(A.n_tiles / RC_BLOCK) * A.width + 1) / 2;
-    int32_t rc = rk_scratch(ctx, SL_RECUR_CHAIN, (words + after) * 8 + (uint64_t)A.n_cols * RC_TICKET * 4, (void **)&A.steps);
+    rc = rk_scratch(ctx, SL_RECUR_CHAIN, (words + after) * 8 + (uint64_t)A.n_cols * RC_TICKET * 4, (void **)&A.steps);
     if (rc != RK_OK) return rc;
     A.behind = (uint32_t *)(A.steps + words);
     A.ticket = (uint32_t *)(A.steps + words + after);
-    if (A.d_bias && (rc = rk_scratch(ctx, SL_RECUR_BIAS, words * 4, (void **)&A.bias_parts)) != RK_OK) return rc;
     const uint64_t clear = (words + after + 1023) / 1024;
     k_recur_clear<<<(uint32_t)(clear < 2048 ? clear : 2048), 256, 0, ctx->stream>>>(A.steps, words + after, A.ticket, A.n_cols * RC_TICKET);
     RK_CHECK_LAUNCH(ctx, "k_recur_clear");

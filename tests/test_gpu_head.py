@@ -230,3 +230,57 @@ def test_gradients_are_differences(gpu):
         slope, want = (up - down) / (2 * eps), float((grad.double() * way.double()).sum())
         scale = float((grad.double() * way.double()).abs().sum())
         assert abs(slope - want) <= 100 * eps ** 2 * scale + 12 * 2.0 ** -21 / eps, (slope, want)
+
+
+def test_several_pieces_of_the_vocabulary(gpu):
+    """More gradients than the working buffer holds at once, labels in every piece; rows that need padding and rows that do not.  Against
+    64 bits on the GPU, a norm of each result: 16-bit results are off by half a step each, the gradients' rounding by as much again."""
+    torch, rk, ctx = gpu
+    rows, vocab, half = 4200, 140001, torch.finfo(torch.bfloat16).eps / 2
+    for width in (40, 33):
+        g = torch.Generator("cuda").manual_seed(width)
+        n = lambda *s: torch.randn(*s, generator=g, device="cuda").to(torch.bfloat16)
+        x, words = n(rows, width), n(vocab, width) * 0.5
+        label = torch.randint(0, vocab, (rows,), generator=g, device="cuda").int()
+        label[:3] = torch.tensor([0, vocab - 1, -1])
+        f = lambda *s: torch.full(s, float("nan"), device="cuda")
+        loss, lse, total, dx, dw = f(rows), f(rows), f(1), n(rows, width), n(vocab, width)
+        given = (ctx, rk.make_head(), x, words, label, None)
+        rk.rk_head_loss_backward(*given, None, loss, lse, total, dx, dw)
+        dx2, dw2 = torch.empty_like(dx), torch.empty_like(dw)
+        rk.rk_head_backward(*given, lse, None, dx2, dw2)
+        want_dw, want_dx, want_lse = torch.zeros(vocab, width, dtype=torch.float64, device="cuda"), [], []
+        w64 = words.double()
+        for a in range(0, rows, 700):
+            x64 = x[a:a + 700].double()
+            l = x64 @ w64.t()
+            want_lse.append(torch.logsumexp(l, 1))
+            p = torch.softmax(l, 1)
+            keep = label[a:a + 700] >= 0
+            p[torch.arange(len(p), device="cuda")[keep], label[a:a + 700][keep].long()] -= 1
+            p[~keep] = 0
+            want_dx.append(p @ w64)
+            want_dw += p.t() @ x64
+        want_dx, want_lse = torch.cat(want_dx), torch.cat(want_lse)
+        assert float((lse.double() - want_lse)[3:].abs().max()) <= 64 * U32 * float(want_lse.max())
+        for got, want in ((dx, want_dx), (dx2, want_dx), (dw, want_dw), (dw2, want_dw)):
+            assert float((got.double() - want).norm()) <= 2 * half * float(want.norm())
+            assert float((got.double() - want).abs().max()) <= 4 * half * float(want.abs().max())
+
+
+def test_more_rows_than_the_sums_of_all_tiles_have_room_for(gpu):
+    torch, rk, ctx = gpu
+    rows, vocab, width = 1 << 18, 33001, 8
+    g = torch.Generator("cuda").manual_seed(1)
+    x, words = (torch.randn(n, width, generator=g, device="cuda").to(torch.bfloat16) for n in (rows, vocab))
+    label = torch.randint(0, vocab, (rows,), generator=g, device="cuda").int()
+    f = lambda *s: torch.full(s, float("nan"), device="cuda")
+    loss, lse, total = f(rows), f(rows), f(1)
+    rk.rk_head_loss(ctx, rk.make_head(), x, words, label, None, loss, lse, total)
+    for a in (0, 100000, rows - 500):
+        l = x[a:a + 500].double() @ words.double().t()
+        want = torch.logsumexp(l, 1)
+        assert float((lse[a:a + 500].double() - want).abs().max()) <= 64 * U32 * float(want.max())
+        own = want - l[torch.arange(500, device="cuda"), label[a:a + 500].long()]
+        assert float((loss[a:a + 500].double() - own).abs().max()) <= 128 * U32 * float(want.max())
+    assert abs(float(total) - float(loss.double().sum())) <= U32 * float(total)

@@ -261,3 +261,43 @@ def test_gradients_are_differences(gpu):
         # the differences' third-order term, and the loss's rounding over the step
         scale = float((grad.double() * way.double()).abs().sum())
         assert abs(slope - want) <= 4 * eps ** 2 * scale + 1e-5 / eps * 0.1, (slope, want)
+
+
+def test_no_sequences(gpu):
+    """Offsets that hold no sequence, and rows without any: nothing is written but the bias's gradient of zero."""
+    torch, rk, ctx = gpu
+    for rows in (0, 5):
+        f = lambda *s: torch.full(s, float("nan"), device="cuda")
+        x, recur = torch.randn(rows, 33, device="cuda"), rk.Recur(bias=torch.zeros(33, device="cuda"), offsets=torch.zeros(1, dtype=torch.int32, device="cuda"))
+        h, state, dx, dz, db = f(rows, 33), f(0, 33), f(rows, 33), f(rows, 33), f(33)
+        rk.rk_recur_forward(ctx, recur, x, x, state, h, state)
+        rk.rk_recur_backward(ctx, recur, x, x, h, None, x, None, dx, dz, None, db)
+        assert bool(torch.isnan(h).all()) and bool(torch.isnan(dx).all()) and bool((db == 0).all())
+    # rows without a sequence length end are one sequence, also of no rows: its state goes through
+    state, out = torch.randn(1, 33, device="cuda"), f(1, 33)
+    e = torch.empty(0, 33, device="cuda")
+    rk.rk_recur_forward(ctx, rk.Recur(), e, e, state, e, out)
+    assert torch.equal(out, state)
+    # a length beyond any number of rows is one sequence
+    x = torch.randn(200, 34, device="cuda")
+    a, b = f(200, 34), f(200, 34)
+    rk.rk_recur_forward(ctx, rk.Recur(seq_rows=2 ** 64 - 1), x, x, None, a, None)
+    rk.rk_recur_forward(ctx, rk.Recur(), x, x, None, b, None)
+    assert torch.equal(a, b)
+
+
+def test_offsets_that_are_none_lead_nowhere(gpu):
+    """Descending, negative and far offsets: the results are nobody's business, but the call ends and writes no other rows' memory."""
+    torch, rk, ctx = gpu
+    rows, width = 400, 66
+    room = torch.zeros(rows + 2, width, device="cuda")
+    x = torch.randn(rows, width, device="cuda")
+    for at in ([300, 100, 200, 50, 400], [-7, 30, 1000000, 60], [2 ** 31 - 1, -2 ** 31, 0, 400], [5, 5, 4, 5, 399]):
+        recur = rk.Recur(offsets=torch.tensor(at, dtype=torch.int32, device="cuda"))
+        n = len(at) - 1
+        states = torch.zeros(n + 2, width, device="cuda")
+        h, d = room[1:rows + 1], torch.empty(rows, width, device="cuda")
+        rk.rk_recur_forward(ctx, recur, x, x, torch.zeros(n, width, device="cuda"), h, states[1:n + 1])
+        rk.rk_recur_backward(ctx, recur, x, x, h, None, x, torch.zeros(n, width, device="cuda"), torch.empty_like(d), d, torch.zeros(n, width, device="cuda"), None)
+        rk.rk_sync(ctx)
+        assert bool((room[0] == 0).all()) and bool((room[-1] == 0).all()) and bool((states[0] == 0).all()) and bool((states[-1] == 0).all())
