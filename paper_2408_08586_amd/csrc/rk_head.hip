@@ -369,7 +369,6 @@ struct OutArgs {
     uint64_t stride, split_stride;
     bool first;
     void *out;                  // d_weight
-    bool aligned;               // its rows take whole vectors
     uint32_t width, words, word0;
     const float *d_total;
     float scale, room;
@@ -419,8 +418,13 @@ template <typename T> __global__ __launch_bounds__(256) void k_head_dx_out(const
             for (uint32_t s = 0; s < A.splits; ++s) v += *(const Vec<float, 4> *)(from + s * A.split_stride);
             v *= (A.d_total ? *A.d_total : 1.f) * A.scale * (__uint_as_float(A.R.count[1]) / A.room);
         }
+        T *const to = dx + r * dx_st + c;
+        if (c + 4 <= A.width) {
+            *(Vec<uint32_t, (int)sizeof(T)> __attribute__((aligned(sizeof(T)))) *)to = words_of<T, 4>({v[0], v[1], v[2], v[3]});
+        } else {
 #pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) if (c + e < A.width) dx[r * dx_st + c + e] = (T)v[e];
+            for (uint32_t e = 0; e < 3; ++e) if (c + e < A.width) to[e] = (T)v[e];
+        }
     }
 }
 template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_THREADS) void k_head_dw(const OutArgs A) {
@@ -481,13 +485,12 @@ template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_TH
     const float f = n ? (A.d_total ? *A.d_total : 1.f) * A.scale * (__uint_as_float(A.R.count[1]) / A.room) : 0.f;
     constexpr uint32_t EACH = 16 / sizeof(T);
     T *const out = (T *)A.out;
-    const bool whole = A.aligned && a0 + TA <= A.width;
     t.rows([&](int i, int j) { return n ? t.acc[i][j] * f : Vec<float, 4>(0.f); },
            [&](uint32_t a, uint32_t b, const Vec<uint32_t, 4> &w) {
                if (b0 + b >= A.words) return;
                T *const to = out + (uint64_t)(b0 + b) * A.stride + a0 + a;
-               if (whole) {
-                   __builtin_nontemporal_store(w, (Vec<uint32_t, 4> *)to);
+               if (a0 + a + EACH <= A.width) {
+                   __builtin_nontemporal_store(w, (Loose<T> *)to);
                } else {
                    const Vec<T, EACH> v = __builtin_bit_cast(Vec<T, EACH>, w);
 #pragma unroll
@@ -672,7 +675,6 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
             D.A = X; D.A.count = (uint64_t)wide * ES;
             D.B = Side{(const char *)g, words * ES, words * ES};
             D.tiles_b = tiles_a; D.words = n_words; D.word0 = (uint32_t)first;
-            D.aligned = (uintptr_t)C.d_weight->data % 16 == 0 && C.d_weight->stride * ES % 16 == 0;
             D.out = (T *)C.d_weight->data + first * C.d_weight->stride; D.stride = C.d_weight->stride;
             // (tiles of 64 words, two workgroups a compute unit, were slower for few rows too: 5 x 128000 x 5248 566 instead of 436 us)
             k_head_dw<T, HD_TA, 256, 2><<<tiles_w * tiles_a, GM_THREADS, 0, stream>>>(D);
