@@ -158,7 +158,8 @@ __device__ __forceinline__ uint32_t not_all_ones(float v) {
     return w == 0xFFFFFFFFu ? 0x7FC00000u : w;  // (one NaN for another)
 }
 struct Lds {
-    Vec<float, 2> p[RC_WAVES][64], q[RC_WAVES][64];
+    Vec<float, 2> p[RC_WAVES][64], q[RC_WAVES][64];         // the wavefronts' links; those of the tiles before, a run a wavefront
+    Vec<float, 2> jp[RC_WAVES][64], jq[RC_WAVES][64];
     uint32_t cuts;                              // wavefronts in which a chain begins
     uint32_t ticket;
     int32_t seq[RC_WAVES][64];                  // a row's sequence, for code that not all lanes are in
@@ -169,30 +170,37 @@ struct Lds {
     }
     __device__ __forceinline__ uint32_t seq_of(uint32_t wave, int i) const { return (uint32_t)__builtin_amdgcn_readfirstlane(seq[wave][i]); }
 };
+// what the first n wavefronts make of a value, in the direction of the chain
+__device__ __forceinline__ Link link_of(const Lds &lds, uint32_t n, uint32_t cuts) {
+    const uint32_t lane = threadIdx.x & 63u;
+    Link l;
+    l.p = 1.f; l.q = 0.f;
+    for (uint32_t w = 0; w < n; ++w) {
+        const Vec<float, 2> p = lds.p[w][lane], q = lds.q[w][lane];
+        if (cuts >> w & 1u) { l.p = 0.f; l.q = q; }
+        else { l.q = p * l.q + q; l.p = l.p * p; }
+    }
+    return l;
+}
 // The value that comes in to this wavefront's rows.  order: its place in the direction of the chain; cut: a chain begins in its rows; needs: its
-// tile's first row goes on with a chain that began in tile `from` (tiles counted in the direction of the chain).
+// tile's first row goes on with a chain that began in tile `from` (tiles counted in the direction of the chain).  (Links are folded anew where they are
+// wanted: the rows leave no registers to keep them in.)
 __device__ __forceinline__ Vec<float, 2> join(const RecurArgs &A, Lds &lds, uint32_t order, const Link &own, bool cut, uint32_t tile, uint32_t column, bool needs, uint32_t from) {
     const uint32_t lane = threadIdx.x & 63u;
     lds.p[order][lane] = own.p;
     lds.q[order][lane] = own.q;
     if (lane == 0 && cut) atomicOr(&lds.cuts, 1u << order);
     __syncthreads();
-    const uint32_t cuts = lds.cuts;
-    Vec<float, 2> p = 1.f, q = 0.f;
-    for (uint32_t w = 0; w < order; ++w) {
-        const Vec<float, 2> pw = lds.p[w][lane], qw = lds.q[w][lane];
-        if (cuts >> w & 1u) { p = 0.f; q = qw; }
-        else { q = pw * q + qw; p = p * pw; }
-    }
-    if (!A.ticket) return q;                    // (nothing comes in to any tile)
-    // what the tile makes of a value
-    const Vec<float, 2> all_p = cuts ? Vec<float, 2>(0.f) : p * own.p, all_q = cut ? own.q : own.p * q + own.q;
-    if (order == RC_WAVES - 1)
+    const uint32_t cuts = __builtin_amdgcn_readfirstlane(lds.cuts);
+    if (!A.ticket) return link_of(lds, order, cuts).q;      // (nothing comes in to any tile)
+    if (order == RC_WAVES - 1) {
+        const Link all = link_of(lds, RC_WAVES, cuts);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
             if (column + i < A.width)
-                __hip_atomic_store(A.steps + (uint64_t)tile * A.width + column + i, (uint64_t)not_all_ones(all_q[i]) << 32 | not_all_ones(all_p[i]),
+                __hip_atomic_store(A.steps + (uint64_t)tile * A.width + column + i, (uint64_t)not_all_ones(all.q[i]) << 32 | not_all_ones(cuts ? 0.f : all.p[i]),
                                    __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
     Vec<float, 2> in = 0.f;
     if (needs) {
         const uint32_t block = tile / RC_BLOCK * RC_BLOCK, begin = from > block ? from : block, n = tile - begin;
@@ -210,16 +218,8 @@ __device__ __forceinline__ Vec<float, 2> join(const RecurArgs &A, Lds &lds, uint
                 jq[i] = tp * jq[i] + tq;
                 jp[i] *= tp;
             }
-        __syncthreads();                        // (needs is the same for the whole workgroup)
-        lds.p[order][lane] = jp;
-        lds.q[order][lane] = jq;
-        __syncthreads();
-        jp = lds.p[0][lane]; jq = lds.q[0][lane];
-#pragma unroll
-        for (uint32_t w = 1; w < RC_WAVES; ++w) {
-            jq = lds.p[w][lane] * jq + lds.q[w][lane];
-            jp *= lds.p[w][lane];
-        }
+        lds.jp[order][lane] = jp;
+        lds.jq[order][lane] = jq;
         if (from < block)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -229,17 +229,21 @@ __device__ __forceinline__ Vec<float, 2> join(const RecurArgs &A, Lds &lds, uint
                     __builtin_amdgcn_s_sleep(1);
                 in[i] = __uint_as_float(word);
             }
-        in = jp * in + jq;
+        __syncthreads();                        // (needs is the same for the whole workgroup)
+#pragma unroll
+        for (uint32_t w = 0; w < RC_WAVES; ++w) in = lds.jp[w][lane] * in + lds.jq[w][lane];
     }
     // the value behind the tile, if it is a block's last: the next block is waiting for it
     if (order == RC_WAVES - 1 && tile % RC_BLOCK == RC_BLOCK - 1) {
-        const Vec<float, 2> behind = cuts ? all_q : all_p * in + all_q;
+        const Link all = link_of(lds, RC_WAVES, cuts);
+        const Vec<float, 2> behind = cuts ? all.q : all.p * in + all.q;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
             if (column + i < A.width)
                 __hip_atomic_store(A.behind + (uint64_t)(tile / RC_BLOCK) * A.width + column + i, not_all_ones(behind[i]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    return cuts & ((1u << order) - 1u) ? q : p * in + q;
+    const Link before = link_of(lds, order, cuts);
+    return cuts & ((1u << order) - 1u) ? before.q : before.p * in + before.q;
 }
 // Which tile a workgroup has; false: none, it looked for sequences without rows instead, whose state goes from one end to the other.
 __device__ __forceinline__ bool take(const RecurArgs &A, Lds &lds, const float *from, uint64_t from_st, float *to, uint64_t to_st, uint32_t &tile, uint32_t &column_tile) {
