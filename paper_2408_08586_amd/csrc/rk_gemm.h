@@ -1,18 +1,23 @@
 // Matrix products of the operators: out[b][a] = sum over k of A(a, k) B(b, k), held in float32.
 //
-// A workgroup of four wavefronts makes a tile of TA x TB.  64 bytes of k at a time, both tiles go from memory straight into one of
-// four places in LDS; fragments are read from there one step ahead of the products that take them, so that the matrix units, the reads of LDS and the loads
-// from memory of the three steps that follow run side by side, with one barrier a step.  A wavefront has 128 x 128 sums of the largest tile: a
-// byte that it reads from LDS is used 128 times, which keeps LDS at half the matrix units' time (of wavefronts of
-// 128 x 64, eight to a workgroup, the products waited for LDS at every step).
+// A workgroup of eight wavefronts makes a tile of TA x TB.  64 bytes of k at a time, both tiles go from memory straight into one of
+// four places in LDS; fragments are read from there one step ahead of the products that take them, between the products of the step before, so that the matrix
+// units, the reads of LDS and the loads from memory of the three steps that follow run side by side, with one barrier a step.  A wavefront
+// has 128 x 64 sums of the largest tile, which 128 registers hold beside the two steps' fragments: with four wavefronts of 128 x 128, LDS is read a quarter less
+// and nothing else runs on a SIMD while its one wavefront waits at the barrier.
 // A side lies with k along its rows (ALONG) or with k from row to row (ACROSS), and so it comes into LDS; nothing is turned around beforehand:
-//   ALONG   64 bytes a row.  A lane's part of a fragment is a 16-byte piece of its row; pieces lie in the order piece ^ (row / 4 % 4), so that the
-//           sixteen rows of a fragment do not meet in the banks.
+//   ALONG   64 bytes a row.  A lane's part of a fragment is a 16-byte piece of its row; pieces lie in the order piece ^ something that rows
+//           which are read together do not share, so that they do not meet in the banks.
 //   ACROSS  a row of TA (TB) elements for every k.  Of narrow elements, sixteen lanes read four k of sixteen elements and get them
 //           turned around by the LDS unit; of 32-bit ones, a lane reads its element of each k.  Pieces lie in the order piece ^ something that
 //           the k of the lanes that read together do not share.
 // Memory gives pieces in that order, as LDS is written in the order of the lanes.  The matrix units take sixteen elements of 32 narrow k at once, or of four
 // 32-bit ones: there, each of four products takes one k of every lane's four, the same of both sides.
+//
+// Measured with 1,843 rows, 128,000 words and a width of 5,248 in bfloat16 (2.48 TFLOP a product): logits 2.19 ms, dx 2.25, d_weight 2.40, that is 1,130, 1,100 and
+// 1,030 TFLOP/s, where large products of a library reach 1,260 to 1,310; what the matrix units do (rows up to whole tiles with it) fills 0.63, 0.66 and
+// 0.54 of the cycles, at the 1.9 GHz that the card then holds.  In 32 bits (1,024 x 32,000 x 2,048, 134 GFLOP): 0.96 ms, 0.93 and 1.02, 140, 145 and 131 of the 152
+// TFLOP/s that a library reaches.  d_weight has the shortest sums: what a tile spends before its first product and on writing is not covered.
 #pragma once
 #include <type_traits>
 
@@ -64,6 +69,9 @@ struct Side {
     uint64_t stride;            // bytes from row to row
     uint64_t count;             // ALONG: rows; ACROSS: bytes of a row
 };
+// ALONG: a piece of row r lies at piece ^ {0, 2, 3, 1}[r / 4 % 4].  LDS takes a read of 16 bytes a lane in four parts, lanes 0 to 3, 12 to 15 and 20 to 27 in
+// the first; with {0, 1, 2, 3} half of these met in the banks (4 more cycles a read, counted, and the same time: the matrix units' covers them).
+__device__ __forceinline__ uint32_t order_along(uint32_t r) { return 0x78u >> (r >> 1 & 6u) & 3u; }
 // ACROSS: a piece of k's row lies at piece ^ order_of(k): pairs of pieces change places (of 32-bit elements fours), differently for all k that
 // are read together
 template <typename T, uint32_t PIECES> __device__ __forceinline__ uint32_t order_of(uint32_t k) {
@@ -89,7 +97,7 @@ template <typename T, int R, int WAY> struct Fetch {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 uint32_t r = part(i) * 16 + (lane >> 2);
-                const uint32_t piece = (lane & 3u) ^ (r >> 2 & 3u);
+                const uint32_t piece = (lane & 3u) ^ order_along(r);
                 r = r < rows ? r : (uint32_t)(rows - 1);    // (rows behind the last repeat it: their results go nowhere)
                 at[i] = r * (uint32_t)s.stride + piece * 16;
                 tail[i] = piece * (16 / sizeof(T)) < left ? at[i] : GM_NOWHERE;
@@ -119,7 +127,7 @@ template <typename T, int R, int WAY> struct Reader {
     __device__ __forceinline__ Reader(uint32_t first) {
         const uint32_t lane = threadIdx.x & 63u, j = lane & 15u, g = lane >> 4;
         if constexpr (WAY == ALONG) {
-            at = (first + j) * GM_STEP + (g ^ (j >> 2)) * 16;
+            at = (first + j) * GM_STEP + (g ^ order_along(j)) * 16;
         } else if constexpr (sizeof(T) == 4) {
             const uint32_t k = 4 * g, piece = first / 4 + (j >> 2);
             at = k * PITCH + (piece ^ order_of<T, PIECES>(k)) * 16 + (j & 3u) * 4;

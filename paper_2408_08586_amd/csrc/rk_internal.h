@@ -77,8 +77,8 @@ enum {
     SL_NORM_PARTS, SL_NORM_ROWS,                         // norms around a block: sums of the chunks of rows; per row, what its gradient takes off
     SL_ROUTE_COUNTS, SL_ROUTE_PROBS, SL_ROUTE_Z, SL_ROUTE_GROUPS, SL_ROUTE_DONE,   // router: its workgroups' counts and sums, its groups'
     SL_DISTILL_PARTS,                                    // distillation: the sums of the rows' slices
-    SL_HEAD_ROWS, SL_HEAD_X, SL_HEAD_XT, SL_HEAD_W, SL_HEAD_WT, SL_HEAD_PARTS, SL_HEAD_G, SL_HEAD_GT, SL_HEAD_DX,   // head: the rows that count; they and a
-                                                         // piece of the weights, padded or turned around; sums of tiles; the logits' gradients; sums of dx
+    SL_HEAD_ROWS, SL_HEAD_X, SL_HEAD_W, SL_HEAD_PARTS, SL_HEAD_G, SL_HEAD_DX,   // head: the rows that count; they and a piece of the weights,
+                                                         // padded; sums of tiles; the logits' gradients; sums of dx
     SL_RECUR_CHAIN, SL_RECUR_BIAS,                       // recurrence: what its tiles tell each other; their sums of the bias's gradient
     SL_COUNT
 };
