@@ -228,7 +228,8 @@ template <typename T, int TA, int TB, int WA, int WAY_A, int WAY_B> struct Tile 
     // a wavefront's part of LDS behind the loop: 16 rows of TA / WA elements
     static constexpr int PART = TA / WA * 16 * (int)sizeof(T);
     char *part;
-    char *shared;               // ... and one of all wavefronts, 8 bytes for every WA and TB
+    char *shared;               // ... one of all wavefronts, 8 bytes for every WA and TB (two kilobytes and more)
+    char *step_a, *step_b;      // ... and a step's place in the sides' order (step_a lies among the wavefronts' parts)
 
     __device__ __forceinline__ void run(const Side &A, const Side &B, uint64_t a0, uint64_t b0, uint64_t k0, uint32_t ks) {
         __shared__ __attribute__((aligned(128))) char a_0[TA * GM_STEP], a_1[TA * GM_STEP], a_2[TA * GM_STEP], a_3[TA * GM_STEP];
@@ -241,7 +242,7 @@ template <typename T, int TA, int TB, int WA, int WAY_A, int WAY_B> struct Tile 
             constexpr uint32_t HERE = TA * GM_STEP / PART;  // wavefronts whose parts one of the places holds
             const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), run = wave / HERE;
             static_assert(WA * TB * 8 <= TB * GM_STEP, "");
-            shared = b_0;
+            shared = b_1; step_a = a_0; step_b = b_0;
             part = (run == 0 ? a_0 : run == 1 ? a_1 : run == 2 ? a_2 : a_3) + wave % HERE * PART;
         }
         const uint32_t steps = (ks + KS - 1) / KS;
@@ -280,6 +281,29 @@ template <typename T, int TA, int TB, int WA, int WAY_A, int WAY_B> struct Tile 
         for (; s < steps; s += 4) four(LAST, s);
         settle();
         landed<0>();            // (places of steps that there are not are being filled with zeros)
+    }
+
+    // One step more, which lies in step_a and step_b, by itself.
+    __device__ __forceinline__ void step_alone() {
+        Fragments f;
+        read(f, step_a, step_b, ReadA(wave_a()), ReadB(wave_b()));
+        // (what vector instructions wrote is there two cycles later at the earliest)
+#pragma unroll
+        for (int i = 0; i < MA; ++i) asm volatile("" : "+v"(f.a[i]));
+#pragma unroll
+        for (int j = 0; j < MB; ++j) asm volatile("" : "+v"(f.b[j]));
+#pragma unroll
+        for (int i = 0; i < MA; ++i)
+#pragma unroll
+            for (int j = 0; j < MB; ++j) asm volatile("" : "+v"(acc[i][j]));
+        asm volatile("s_nop 7" ::: "memory");
+#pragma unroll
+        for (int q = 0; q < (sizeof(T) == 4 ? 4 : 1); ++q)
+#pragma unroll
+            for (int i = 0; i < MA; ++i)
+#pragma unroll
+                for (int j = 0; j < MB; ++j) product<T>(f.a[i], f.b[j], q, acc[i][j]);
+        settle();
     }
 
     static __device__ __forceinline__ void wave_sync() {

@@ -441,8 +441,10 @@ template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_TH
     Tl t;
     t.run(A.A, A.B, a0, b0, 0, n);
     if constexpr (sizeof(T) == 2) {
-        // what rounding took off the labels of the tile: their rows in order, 2,048 looked through at a time
-        constexpr uint32_t EVERY = 4;
+        // What rounding took off the labels of the tile: rows are looked through in order, 2,048 at a time, and those whose label lies in the tile make
+        // further steps, 32 of them each, as their x and a side that has one element of each k: what was lost, rounded to the rows' type itself (the
+        // label's gradient then has a 512th of its rounding, of float16 a 4,096th).  A tile takes as many steps as its labels are, however they lie.
+        constexpr uint32_t EVERY = 4, KS = GM_STEP / sizeof(T), EL = 16 / sizeof(T), PA = TA / EL, PB = TB / EL;
         uint32_t *const found = (uint32_t *)t.shared, *const counts = found + EVERY * GM_THREADS;
         static_assert((EVERY * GM_THREADS + EVERY * GM_WAVES) * 4 <= TB * GM_STEP, "");
         const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -467,25 +469,28 @@ template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_TH
                     all += counts[e * GM_WAVES + w];
                 }
             __syncthreads();
-            for (uint32_t k = 0; k < all; ++k) {
-                const uint32_t which = __builtin_amdgcn_readfirstlane(found[k]), r = which >> 8, at_b = which & 255u;
-                if (at_b / (TB / Tl::WB) != wave % Tl::WB) continue;
-                const uint32_t own_j = at_b % (TB / Tl::WB) / 16;
-                const float lost = A.R.lost[r];
-                const T *const x = (const T *)(A.A.data + r * A.A.stride);
-                const uint32_t first = a0 + Tl::wave_a() + 4 * (lane >> 4);
-#pragma unroll
-                for (int i = 0; i < Tl::MA; ++i) {
-                    Vec<T, 4> xs = (T)0.f;
-                    if ((lane & 15u) == at_b % 16 && (first + 16 * i) * sizeof(T) < A.A.count) xs = *(const Vec<T, 4> *)(x + first + 16 * i);
-#pragma unroll
-                    for (int j = 0; j < Tl::MB; ++j)
-                        if (j == (int)own_j)
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) t.acc[i][j][q] += lost * (float)xs[q];
+            for (uint32_t step = 0; step < all; step += KS) {
+                for (uint32_t i = threadIdx.x; i < KS * PA; i += GM_THREADS) {
+                    const uint32_t k = i / PA, piece = i % PA;
+                    Vec<uint32_t, 4> w = 0u;
+                    if (step + k < all && a0 * sizeof(T) + piece * 16 < A.A.count)
+                        w = *(const Vec<uint32_t, 4> *)(A.A.data + (uint64_t)(found[step + k] >> 8) * A.A.stride + a0 * sizeof(T) + piece * 16);
+                    *(Vec<uint32_t, 4> *)(t.step_a + k * (TA * sizeof(T)) + (piece ^ order_of<T, PA>(k)) * 16) = w;
                 }
+                for (uint32_t i = threadIdx.x; i < KS * PB; i += GM_THREADS) {
+                    const uint32_t k = i / PB, piece = i % PB, of = step + k < all ? found[step + k] : 0u;
+                    Vec<T, EL> w = (T)0.f;
+                    if (step + k < all && (of & 255u) / EL == piece) {
+                        const T lost = (T)A.R.lost[of >> 8];
+#pragma unroll
+                        for (uint32_t e = 0; e < EL; ++e) w[e] = (of & 255u) % EL == e ? lost : (T)0.f;
+                    }
+                    *(Vec<T, EL> *)(t.step_b + k * (TB * sizeof(T)) + (piece ^ order_of<T, PB>(k)) * 16) = w;
+                }
+                __syncthreads();
+                t.step_alone();
+                __syncthreads();
             }
-            __syncthreads();
         }
     }
     const float f = n ? (A.d_total ? *A.d_total : 1.f) * A.scale * (__uint_as_float(A.R.count[1]) / A.room) : 0.f;

@@ -284,3 +284,32 @@ def test_more_rows_than_the_sums_of_all_tiles_have_room_for(gpu):
         own = want - l[torch.arange(500, device="cuda"), label[a:a + 500].long()]
         assert float((loss[a:a + 500].double() - own).abs().max()) <= 128 * U32 * float(want.max())
     assert abs(float(total) - float(loss.double().sum())) <= U32 * float(total)
+
+
+@pytest.mark.parametrize("type", ("bfloat16", "float16"))
+@pytest.mark.parametrize("rows, vocab, width", [(4500, 600, 264), (2100, 40, 33), (33, 300, 520)])
+def test_labels_that_meet_in_a_tile(gpu, type, rows, vocab, width):
+    """What rounding takes off the labels' gradients is there, of however many rows have one label: what d_weight is off by are other words'
+    roundings and its own, and of its labels' rows the rounding of a rounding."""
+    torch, rk, ctx = gpu
+    c = Case(torch, rows, vocab, width, type)
+    words = torch.tensor([vocab - 1, 0, min(255, vocab - 1), min(256, vocab - 1)], dtype=torch.int32).cuda()
+    few = torch.arange(rows, device="cuda") % 50 < 4
+    c.label[~few] = 7
+    c.label[few] = words[torch.arange(rows, device="cuda")[few] % 4]
+    c.check(rk, ctx)
+    x, w, label, weight = c.x.double().cpu(), c.weight.double().cpu(), c.label.long().cpu(), c.row_weight.double().cpu()
+    g = torch.softmax(x @ w.T, 1)
+    g[torch.arange(rows), label] -= 1.0
+    g *= weight[:, None]
+    own = torch.zeros_like(g)
+    own[torch.arange(rows), label] = g[torch.arange(rows), label]
+    others = g - own
+    exact, half = g.T @ x, torch.finfo(c.t).eps / 2
+    logit = (width / 4 + 32) * U32 * float((x.abs() @ w.abs().T).max())
+    # (at once, the others are rounded twice; what was lost is at most half of the label's gradient, and its rounding half of that)
+    tol = half * (1 + 2.0 ** -8) * exact.abs() + 2.02 * half * (others.abs().T @ x.abs()) + (half * half + 2 * logit + (rows / 4 + 64) * U32) * (g.abs().T @ x.abs()) \
+        + TINY[type] + 2.0 ** (-39 if type == "float16" else -126) * 4 * float(weight.max()) * x.abs().sum(0)[None]
+    for out in c.run(rk, ctx):
+        bad = (out["d_weight"].double().cpu() - exact).abs() > tol
+        assert not bool(bad.any()), (int(bad.sum()), bad.nonzero()[0].tolist())
