@@ -212,29 +212,33 @@ __device__ __forceinline__ Vec<float, 2> join(const RecurArgs &A, Lds &lds, uint
         const uint32_t block = tile / RC_BLOCK * RC_BLOCK, begin = from > block ? from : block, n = tile - begin;
         // the tiles before this one, a run of them a wavefront, and the value behind the block before
         const uint32_t a = begin + n * order / RC_WAVES, b = begin + n * (order + 1) / RC_WAVES;
+        // (lanes wait together, those behind the last column with it: were some of them to go on alone, what does not fit the registers might be written down for
+        // them alone)
+        const uint32_t c0 = column < A.width ? column : A.width - 1, c1 = column + 1 < A.width ? column + 1 : A.width - 1;
         Vec<float, 2> jp = 1.f, jq = 0.f;
-        for (uint32_t t = a; t < b; ++t)
+        for (uint32_t t = a; t < b; ++t) {
+            const uint64_t *const at = A.steps + (uint64_t)t * A.width;
+            uint64_t word[2];
+            while (word[0] = __hip_atomic_load(at + c0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), word[1] = __hip_atomic_load(at + c1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
+                   __builtin_amdgcn_ballot_w64(word[0] == ~0ull || word[1] == ~0ull))
+                __builtin_amdgcn_s_sleep(1);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                if (column + i >= A.width) continue;
-                uint64_t word;
-                while ((word = __hip_atomic_load(A.steps + (uint64_t)t * A.width + column + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) == ~0ull)
-                    __builtin_amdgcn_s_sleep(1);
-                const float tp = __uint_as_float((uint32_t)word), tq = __uint_as_float((uint32_t)(word >> 32));
+                const float tp = __uint_as_float((uint32_t)word[i]), tq = __uint_as_float((uint32_t)(word[i] >> 32));
                 jq[i] = tp * jq[i] + tq;
                 jp[i] *= tp;
             }
+        }
         lds.jp[order][lane] = jp;
         lds.jq[order][lane] = jq;
-        if (from < block)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                if (column + i >= A.width) continue;
-                uint32_t word;
-                while ((word = __hip_atomic_load(A.behind + (uint64_t)(tile / RC_BLOCK - 1) * A.width + column + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) == ~0u)
-                    __builtin_amdgcn_s_sleep(1);
-                in[i] = __uint_as_float(word);
-            }
+        if (from < block) {
+            const uint32_t *const at = A.behind + (uint64_t)(tile / RC_BLOCK - 1) * A.width;
+            uint32_t word[2];
+            while (word[0] = __hip_atomic_load(at + c0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), word[1] = __hip_atomic_load(at + c1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
+                   __builtin_amdgcn_ballot_w64(word[0] == ~0u || word[1] == ~0u))
+                __builtin_amdgcn_s_sleep(1);
+            in[0] = __uint_as_float(word[0]); in[1] = __uint_as_float(word[1]);
+        }
         __syncthreads();                        // (needs is the same for the whole workgroup)
 #pragma unroll
         for (uint32_t w = 0; w < RC_WAVES; ++w) in = lds.jp[w][lane] * in + lds.jq[w][lane];
