@@ -24,6 +24,7 @@
 namespace {
 
 constexpr uint32_t RC_WAVES = 8, RC_THREADS = 64 * RC_WAVES, RC_COLS = 128, RC_BLOCK = 16, RC_TICKET = 16;
+constexpr int RC_NAP = 8;                                       // of who waits, in 64 clocks
 constexpr uint32_t RC_ROWS = 16;                               // of a wavefront, the most
 
 struct RecurArgs {
@@ -221,7 +222,7 @@ __device__ __forceinline__ Vec<float, 2> join(const RecurArgs &A, Lds &lds, uint
             uint64_t word[2];
             while (word[0] = __hip_atomic_load(at + c0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), word[1] = __hip_atomic_load(at + c1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
                    __builtin_amdgcn_ballot_w64(word[0] == ~0ull || word[1] == ~0ull))
-                __builtin_amdgcn_s_sleep(1);
+                __builtin_amdgcn_s_sleep(RC_NAP);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const float tp = __uint_as_float((uint32_t)word[i]), tq = __uint_as_float((uint32_t)(word[i] >> 32));
@@ -229,16 +230,18 @@ __device__ __forceinline__ Vec<float, 2> join(const RecurArgs &A, Lds &lds, uint
                 jp[i] *= tp;
             }
         }
-        lds.jp[order][lane] = jp;
-        lds.jq[order][lane] = jq;
-        if (from < block) {
+        if (order == 0 && from < block) {       // (the first of the runs goes on from there)
             const uint32_t *const at = A.behind + (uint64_t)(tile / RC_BLOCK - 1) * A.width;
             uint32_t word[2];
             while (word[0] = __hip_atomic_load(at + c0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), word[1] = __hip_atomic_load(at + c1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
                    __builtin_amdgcn_ballot_w64(word[0] == ~0u || word[1] == ~0u))
-                __builtin_amdgcn_s_sleep(1);
+                __builtin_amdgcn_s_sleep(RC_NAP);
             in[0] = __uint_as_float(word[0]); in[1] = __uint_as_float(word[1]);
+            jq = jp * in + jq;
+            in = 0.f;
         }
+        lds.jp[order][lane] = jp;
+        lds.jq[order][lane] = jq;
         __syncthreads();                        // (needs is the same for the whole workgroup)
 #pragma unroll
         for (uint32_t w = 0; w < RC_WAVES; ++w) in = lds.jp[w][lane] * in + lds.jq[w][lane];
