@@ -14,9 +14,9 @@
 //
 // The gates' exponentials and divisions, the chain and the two ways through the rows are about 20 vector instructions an element forward and 44 backward, two fifths of the
 // kernels' cycles; the rest is the rows' trip from memory and then the wait for the tiles before, under which two workgroups a compute unit have too little else to do.
-// Measured in bfloat16, coupled, kernels alone: forward 8,192 x 8,576 of equal sequences 94 to 100 us (421 MB, 4.3 TB/s); backward 8,192 x 5,248 118 to 122 us
-// (516 MB, 4.3 TB/s), k_recur_bias 4 to 5, k_recur_clear 3 to 6.  One sequence of 65,536 x 1,024, not coupled: 122 to 128 us (403 MB, 3.2 TB/s): its 32 blocks
-// of tiles wait for each other, about 2 us a block beyond what memory takes.  Blocks of 8 tiles or of 32, wavefronts of 8 rows or four to a workgroup were slower in most.
+// Measured in bfloat16, coupled, kernels alone: forward 8,192 x 8,576 of equal sequences 92 to 95 us (421 MB, 4.5 TB/s); backward 8,192 x 5,248 118 to 122 us
+// (516 MB, 4.3 TB/s), k_recur_bias 4 to 5, k_recur_clear 3 to 6.  One sequence of 65,536 x 1,024, not coupled: 102 to 106 us (403 MB, 3.9 TB/s): its 32 blocks
+// of tiles wait for each other, about 1 us a block beyond what memory takes.  Blocks of 8 tiles or of 32, wavefronts of 8 rows or four to a workgroup were slower in most.
 #include <type_traits>
 
 #include "rk_vec.h"
@@ -24,7 +24,9 @@
 namespace {
 
 constexpr uint32_t RC_WAVES = 8, RC_THREADS = 64 * RC_WAVES, RC_COLS = 128, RC_BLOCK = 16, RC_TICKET = 16;
-constexpr int RC_NAP = 8;                                       // of who waits, in 64 clocks
+// How long who waits sleeps before it looks again, in 64 clocks: looking takes the memory's time from those that are waited for (one sequence of 65536 x 1024 forward, of 1,
+// 4, 8, 16 and 30: 136, 114, 111, 110 and 107 us; ragged 9001 x 1111 backward 73, 70, 70, 70 and 71; 8192 x 8576 the same)
+constexpr int RC_NAP = 16;
 constexpr uint32_t RC_ROWS = 16;                               // of a wavefront, the most
 
 struct RecurArgs {
