@@ -970,7 +970,7 @@ typedef struct {
 /* x, z and h share a type; states are RK_F32 matrices, a row a sequence.  state_in null: zeros; state_out null: not kept;
  * that of a sequence without rows is its state_in.  h may be x or z, state_out may be state_in (same data and
  * stride).  A NaN stays in its sequence; a row of h that is infinite may be followed by NaN there.  Up to 2^31 - 1 rows,
- * and fewer than 2^22 tiles of 128 rows (RK_F32: 64) by 128 columns. */
+ * 2^31 - 2 sequences, and fewer than 2^22 tiles of 128 rows (RK_F32: 64) by 128 columns. */
 int32_t rk_recur_forward(rk_ctx *ctx, const rk_recur *recur, uint64_t n_rows, uint32_t width, const rk_matrix *x,
                          const rk_matrix *z, const rk_matrix *state_in_or_null, const rk_matrix *h,
                          const rk_matrix *state_out_or_null);

@@ -132,10 +132,10 @@ template <int L> __device__ __forceinline__ Marks marks_of(const RecurArgs &A, u
     bool live = lane <= L && row < A.n_rows;
     if (A.offsets) {
         if (live) {
-            // the last sequence that begins at this row or before it
-            int32_t lo = -1, hi = (int32_t)A.n_seqs + 1;
-            while (hi - lo > 1) {
-                const int32_t mid = lo + (hi - lo) / 2;
+            // the last sequence that begins at this row or before it (of the most sequences there are 2^31 numbers from lo to hi)
+            int32_t lo = -1, hi = (int32_t)(A.n_seqs + 1u);
+            while ((uint32_t)hi - (uint32_t)lo > 1u) {
+                const int32_t mid = lo + (int32_t)(((uint32_t)hi - (uint32_t)lo) / 2u);
                 if (A.offsets[mid] <= (int32_t)row) lo = mid; else hi = mid;
             }
             live = lo >= 0 && lo < (int32_t)A.n_seqs;
@@ -514,7 +514,7 @@ int32_t check_recur(rk_ctx *ctx, const rk_recur *r, uint64_t n_rows, uint32_t wi
     if (!r->offsets && r->n_seqs) return rk_fail(ctx, RK_ERR_INVALID_ARG, "n_seqs without offsets");
     if (width < 1) return rk_fail(ctx, RK_ERR_INVALID_ARG, "rows have no elements");
     if (width > RK_RECUR_MAX_WIDTH || n_rows > 0x7FFFFFFFull || r->n_seqs > 0x7FFFFFFEu)
-        return rk_fail(ctx, RK_ERR_UNSUPPORTED, "more than 2^31 - 1 rows or sequences, or more than %u columns", RK_RECUR_MAX_WIDTH);
+        return rk_fail(ctx, RK_ERR_UNSUPPORTED, "more than 2^31 - 1 rows, 2^31 - 2 sequences or %u columns", RK_RECUR_MAX_WIDTH);
     if (!rk_matrix_ok(z, n_rows, width)) return rk_fail(ctx, RK_ERR_INVALID_ARG, "z null, misaligned or of a stride below the width");
     n_seqs = r->offsets ? r->n_seqs : r->seq_rows ? n_rows / r->seq_rows + (n_rows % r->seq_rows != 0) : 1;
     return RK_OK;
