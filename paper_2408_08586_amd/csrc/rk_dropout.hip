@@ -39,14 +39,13 @@ __device__ __forceinline__ Philox philox(uint32_t c0, uint32_t c1, uint64_t offs
 }
 
 // eight elements, `n` of them in the row, of any alignment; what passes once is streamed
-template <typename T> using Loose = Vec<uint32_t, 4> __attribute__((aligned(sizeof(T))));
 template <typename T> __device__ __forceinline__ Words<T, 8> load8(const T *p, uint32_t n) {
     constexpr int PARTS = (int)sizeof(T) / 2;
     Words<T, 8> w = 0u;
     if (n >= 8) {
 #pragma unroll
         for (int h = 0; h < PARTS; ++h) {
-            const Vec<uint32_t, 4> x = __builtin_nontemporal_load((const Loose<T> *)p + h);
+            const Vec<uint32_t, 4> x = __builtin_nontemporal_load((const Loose<Vec<uint32_t, 4>, T> *)p + h);
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[4 * h + i] = x[i];
         }
@@ -67,7 +66,7 @@ template <typename T> __device__ __forceinline__ void store8(T *p, uint32_t n, c
             Vec<uint32_t, 4> y;
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[i] = w[4 * h + i];
-            __builtin_nontemporal_store(y, (Loose<T> *)p + h);
+            __builtin_nontemporal_store(y, (Loose<Vec<uint32_t, 4>, T> *)p + h);
         }
     } else {
 #pragma unroll

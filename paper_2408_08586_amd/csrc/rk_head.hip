@@ -97,7 +97,6 @@ __global__ __launch_bounds__(HD_THREADS) void k_head_rows(const RowsArgs A) {
 
 // Rows one behind the other, each padded with zeros to out_width (a multiple of 16 bytes): the kept ones of x (count rows of R), or n_rows as they lie
 // (count null).  A lane takes 16 bytes of the result, whatever the alignment of what it reads.
-template <typename T> using Loose = Vec<uint32_t, 4> __attribute__((aligned(sizeof(T))));
 template <typename T> __global__ __launch_bounds__(256) void k_head_pad(const int32_t *row, const uint32_t *count, uint32_t n_rows, const T *x, uint64_t stride, uint32_t width, T *out, uint32_t out_width) {
     constexpr uint32_t EACH = 16 / sizeof(T);
     const uint32_t per_row = out_width / EACH, rows = count ? *count : n_rows;
@@ -106,7 +105,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_head_pad(const in
         const T *const from = x + (uint64_t)(row ? (uint32_t)row[r] : r) * stride + c;
         Vec<uint32_t, 4> w;
         if (c + EACH <= width) {
-            w = *(const Loose<T> *)from;
+            w = *(const Loose<Vec<uint32_t, 4>, T> *)from;
         } else {
             Vec<T, EACH> v = (T)0.f;
 #pragma unroll
@@ -426,7 +425,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_head_dx_out(const
         }
         T *const to = dx + r * dx_st + c;
         if (c + 4 <= A.width) {
-            *(Vec<uint32_t, (int)sizeof(T)> __attribute__((aligned(sizeof(T)))) *)to = words_of<T, 4>({v[0], v[1], v[2], v[3]});
+            *(Loose<Words<T, 4>, T> *)to = words_of<T, 4>({v[0], v[1], v[2], v[3]});
         } else {
 #pragma unroll
             for (uint32_t e = 0; e < 3; ++e) if (c + e < A.width) to[e] = (T)v[e];
@@ -501,7 +500,7 @@ template <typename T, int TA, int TB, int WA> __global__ __launch_bounds__(GM_TH
                if (b0 + b >= A.words) return;
                T *const to = out + (uint64_t)(b0 + b) * A.stride + a0 + a;
                if (a0 + a + EACH <= A.width) {
-                   __builtin_nontemporal_store(w, (Loose<T> *)to);
+                   __builtin_nontemporal_store(w, (Loose<Vec<uint32_t, 4>, T> *)to);
                } else {
                    const Vec<T, EACH> v = __builtin_bit_cast(Vec<T, EACH>, w);
 #pragma unroll

@@ -49,7 +49,7 @@ struct RecurArgs {
 
 // ---- a lane's two columns
 template <typename T> using Two = Words<T, 2>;
-template <typename T> using LooseTwo = Two<T> __attribute__((aligned(sizeof(T))));
+template <typename T> using LooseTwo = Loose<Two<T>, T>;
 struct Columns {
     uint32_t at;                    // where it reads: both elements are inside the row
     bool two, one;                  // writes both; the first alone, which it has read as the second

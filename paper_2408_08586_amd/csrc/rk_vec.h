@@ -10,6 +10,11 @@ template <typename T, int N> using Vec = T __attribute__((ext_vector_type(N)));
 // taken apart where paths meet, a register an element)
 template <typename T, int N> using Words = Vec<uint32_t, N * (int)sizeof(T) / 4>;
 
+// V where it begins at any element of T.  (As a class's member: an alias template would drop the attribute, which depends on T, and say nothing.)
+template <typename V, typename T> struct LooseAs { typedef V type __attribute__((aligned(sizeof(T)))); };
+template <typename V, typename T> using Loose = typename LooseAs<V, T>::type;
+static_assert(alignof(Loose<Vec<uint32_t, 4>, __bf16>) == 2 && alignof(Loose<Vec<uint32_t, 2>, float>) == 4, "what begins at any element is declared so");
+
 // A row as a buffer that ends with it: what is loaded from behind its end is zero and what is stored there is dropped, by the memory
 // system, so that rows of any width take the same instructions; a matrix that is not there is one whose rows have no elements; and a
 // lane's place in a row is one register, whatever the matrix.
