@@ -1025,8 +1025,9 @@ int32_t rk_head_loss(rk_ctx *ctx, const rk_head *head, uint64_t n_rows, uint32_t
 
 /* The gradients of x and weight (either null: not wanted; not both) from that of total (d_total [device] one float, null:
  * one) and the forward pass's lse.  They have x's type; neither may overlap an input.  The logits' gradients are
- * made in pieces of the vocabulary and rounded to x's type on their way into the products (their labels' in 32 bits); float16 keeps
- * them down to 2^-38 of the largest row's weight. */
+ * made in pieces of the vocabulary and rounded to x's type on their way into the products; what that takes off a row's label in 16 bits
+ * is added to dx in 32 bits and goes into d_weight as another number of the type.  float16 keeps the others of a row down to 2^-32 u for dx
+ * and down to 2^-38 of the largest row's u for d_weight, where u is a power of two, at or above |row_weight| max(1, |1 + 2 z_weight lse|). */
 int32_t rk_head_backward(rk_ctx *ctx, const rk_head *head, uint64_t n_rows, uint32_t width, uint32_t vocab, const rk_matrix *x,
                          const rk_matrix *weight, const int32_t *label, const float *row_weight_or_null, const float *lse,
                          const float *d_total_or_null, const rk_matrix *dx_or_null, const rk_matrix *d_weight_or_null);

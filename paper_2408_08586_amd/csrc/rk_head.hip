@@ -3,7 +3,8 @@
 // Rows that count are gathered first, so that products take no others, and padded with zeros to whole steps of k.  The loss
 // takes the logits' tiles out of the product's registers: of every row the largest and the sum of exponentials over a tile's
 // words, joined in fixed order.  The gradients go through the vocabulary in pieces, from the last to the first: a piece's logits are made again and become
-// g = row_weight (p (1 + 2 z lse) - onehot), rounded to the rows' type and scaled by a power of two that keeps float16 in its range;
+// g = row_weight (p (1 + 2 z lse) - onehot), rounded to the rows' type and scaled by a power of two that keeps float16 in its range (rows far below the
+// largest one by their own, for dx; d_weight takes them under the largest one's again);
 // dx adds up g W over the pieces in float32, and the piece's rows of d_weight are g^T x.  By far the largest element of a row is its label's: what
 // rounding to 16 bits takes off it is kept and its products are added to dx and d_weight in float32 (777 x 50021 x 1111 in float16: both are
 // 2.1e-4 from the definition, all of it their own rounding, and 3.5e-4 without).  Where the loss is made along with
@@ -21,15 +22,15 @@ constexpr uint64_t HD_BUDGET = 1ull << 30;                  // bytes of a piece'
 constexpr uint64_t HD_PARTS = 1ull << 28;                   // ... of the sums of the loss's tiles
 constexpr int HD_TA = 256;                                  // words, or columns, of a tile
 
-struct RowInfo { float lse, factor, share; uint32_t unused; };     // g = (p factor - onehot) share
+struct RowInfo { float lse, factor, share, unit; };         // g = (p factor - onehot) share, which stands for room / unit times the gradient
 
 // what the device keeps of the rows that count
 struct Rows {
-    uint32_t *count;            // [0] how many, [1] bits of the largest weight's power of two
+    uint32_t *count;            // [0] how many, [1] bits of the largest unit of a row
     int32_t *row, *place;       // a kept row's place in the matrix; a row's place among the kept, or -1
     int32_t *label;
     float *weight, *label_logit, *top, *sum;
-    float *lost;                // what rounding takes off the gradient of a row's label
+    float *lost, *lost_dw;      // what rounding takes off the gradient of a row's label; float16: for d_weight, under the largest unit
     RowInfo *info;
 };
 
@@ -327,12 +328,14 @@ __device__ __forceinline__ float power_above(float v) {
     return ldexpf(1.f, m == 0.5f ? e - 1 : e);
 }
 // What one workgroup does behind the loss: the total (null: there was none), and, with room > 0, the numbers that g is made with; room: what g's
-// largest element may be (a power of two).
+// largest element may be (a power of two).  own_units: rows whose gradients are below a 64th of the largest row's are made under a unit of their own, so that
+// float16 keeps them for dx whatever other rows weigh; others share the largest, and need no k_head_shared.
 struct EndArgs {
     Rows R;
     const float *loss, *lse;
     float *total;
     float z_weight, room;
+    bool own_units;
 };
 __global__ __launch_bounds__(HD_THREADS) void k_head_end(const EndArgs A) {
     __shared__ double lds[HD_THREADS];
@@ -360,8 +363,38 @@ __global__ __launch_bounds__(HD_THREADS) void k_head_end(const EndArgs A) {
     const float unit = power_above(tops[0]);
     if (threadIdx.x == 0) A.R.count[1] = __float_as_uint(unit);
     for (uint32_t i = threadIdx.x; i < n; i += HD_THREADS) {
-        const float lse = A.lse[A.R.row[i]], factor = 1.f + 2.f * A.z_weight * lse;
-        A.R.info[i] = RowInfo{lse, factor, A.R.weight[i] / unit * A.room, 0u};
+        const float lse = A.lse[A.R.row[i]], factor = 1.f + 2.f * A.z_weight * lse, own = power_above(fabsf(A.R.weight[i]) * fmaxf(1.f, fabsf(factor)));
+        const float of = A.own_units && own < unit * 0.015625f ? own : unit;
+        A.R.info[i] = RowInfo{lse, factor, A.R.weight[i] / of * A.room, of};
+    }
+}
+
+// d_weight sums over rows, under one unit: those that had their own are brought to the largest (exactly, but for what is then below float16's smallest).  A
+// workgroup's second index is its row; most have nothing to do but the label's.
+template <typename T> __global__ __launch_bounds__(256) void k_head_shared(Rows R, T *g, uint64_t g_stride, uint32_t first, uint32_t words) {
+    constexpr uint32_t EACH = 16 / sizeof(T);
+    const uint32_t n = R.count[0];
+    const float largest = __uint_as_float(R.count[1]);
+    for (uint32_t b = blockIdx.y; b < n; b += gridDim.y) {
+        const float down = R.info[b].unit / largest;
+        const int64_t label = (int64_t)R.label[b] - (int64_t)first;
+        if (down == 1.f) {
+            if (blockIdx.x == 0 && threadIdx.x == 0) R.lost_dw[b] = R.lost[b];
+            continue;
+        }
+        for (uint32_t a = (blockIdx.x * 256u + threadIdx.x) * EACH; a < words; a += gridDim.x * 256u * EACH) {
+            Vec<uint32_t, 4> *const at = (Vec<uint32_t, 4> *)(g + (uint64_t)b * g_stride + a);
+            const Vec<uint32_t, 4> w = *at;
+            Vec<T, EACH> v;
+#pragma unroll
+            for (uint32_t e = 0; e < EACH; ++e) {
+                const bool own = label == (int64_t)(a + e);
+                const float x = (element<T>(w, e) + (own ? R.lost[b] : 0.f)) * down;
+                v[e] = (T)x;
+                if (own) R.lost_dw[b] = x - (float)v[e];
+            }
+            *at = __builtin_bit_cast(Vec<uint32_t, 4>, v);
+        }
     }
 }
 
@@ -421,7 +454,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_head_dx_out(const
             const float *const from = A.sums + (uint64_t)i * A.stride + c;
 #pragma unroll 8
             for (uint32_t s = 0; s < A.splits; ++s) v += *(const Vec<float, 4> *)(from + s * A.split_stride);
-            v *= (A.d_total ? *A.d_total : 1.f) * A.scale * (__uint_as_float(A.R.count[1]) / A.room);
+            v *= (A.d_total ? *A.d_total : 1.f) * A.scale * (A.R.info[i].unit / A.room);
         }
         T *const to = dx + r * dx_st + c;
         if (c + 4 <= A.width) {
@@ -553,7 +586,7 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
     Rows R{};
     {
         char *p;
-        if ((rc = rk_scratch(ctx, SL_HEAD_ROWS, 256 + rows_pad * (8 * 4 + sizeof(RowInfo)), (void **)&p)) != RK_OK) return rc;
+        if ((rc = rk_scratch(ctx, SL_HEAD_ROWS, 256 + rows_pad * (9 * 4 + sizeof(RowInfo)), (void **)&p)) != RK_OK) return rc;
         R.count = (uint32_t *)p; p += 256;
         R.info = (RowInfo *)p; p += rows_pad * sizeof(RowInfo);
         R.row = (int32_t *)p; p += rows_pad * 4;
@@ -563,7 +596,8 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
         R.label_logit = (float *)p; p += rows_pad * 4;
         R.top = (float *)p; p += rows_pad * 4;
         R.sum = (float *)p; p += rows_pad * 4;
-        R.lost = (float *)p;
+        R.lost = (float *)p; p += rows_pad * 4;
+        R.lost_dw = (float *)p;
     }
     T *xc;
     if ((rc = rk_scratch(ctx, SL_HEAD_X, C.n_rows * wide * ES, (void **)&xc)) != RK_OK) return rc;
@@ -607,6 +641,7 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
     };
     // float16 has 30 powers of two between one and its smallest: what is at most one is moved up by fourteen
     const float room = __is_same(T, _Float16) ? 16384.f : 1.f;
+    const bool own_units = __is_same(T, _Float16) && C.dx;
     LogitsArgs L{};
     L.R = R; L.X = X; L.width = C.width; L.tiles_b = tiles_b; L.scale = C.head->logit_scale; L.room = room;
     if (back && (rc = rk_scratch(ctx, SL_HEAD_G, rows_pad * words * ES, (void **)&L.g)) != RK_OK) return rc;
@@ -634,7 +669,7 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
             RK_CHECK_LAUNCH(ctx, "k_head_join");
         }
     }
-    k_head_end<<<1, HD_THREADS, 0, stream>>>(EndArgs{R, C.loss, C.given_lse ? C.given_lse : C.lse, C.total, C.head->z_weight, back ? room : 0.f});
+    k_head_end<<<1, HD_THREADS, 0, stream>>>(EndArgs{R, C.loss, C.given_lse ? C.given_lse : C.lse, C.total, C.head->z_weight, back ? room : 0.f, own_units});
     RK_CHECK_LAUNCH(ctx, "k_head_end");
     if (!back) return RK_OK;
     const uint32_t tiles_w = (uint32_t)((C.width + 255) / 256);
@@ -682,6 +717,14 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
         }
         if (C.d_weight) {
             OutArgs D = O;
+            if constexpr (__is_same(T, _Float16)) {
+                if (own_units && C.n_rows) {
+                    const uint32_t across = (n_words + 2047) / 2048;
+                    k_head_shared<T><<<dim3(across < 4 ? across : 4, (uint32_t)(C.n_rows < 4096 ? C.n_rows : 4096)), 256, 0, stream>>>(R, (T *)g, words, (uint32_t)first, n_words);
+                    RK_CHECK_LAUNCH(ctx, "k_head_shared");
+                    D.R.lost = R.lost_dw;
+                }
+            }
             D.A = X; D.A.count = (uint64_t)wide * ES;
             D.B = Side{(const char *)g, words * ES, words * ES};
             D.tiles_b = tiles_a; D.words = n_words; D.word0 = (uint32_t)first;

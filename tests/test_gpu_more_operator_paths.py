@@ -16,11 +16,11 @@ def test_large_tiles_in_32_bits(gpu, rows, vocab, width, ignored):
     Head(torch, rows, vocab, width, "float32", z=1e-3, ignored=ignored, seed=3).check(rk, ctx)
 
 
-@pytest.mark.parametrize("type", ["float16", "float32"])
+@pytest.mark.parametrize("type, weights", [("float16", False), ("float16", True), ("float32", False), ("float32", True)])
 @pytest.mark.parametrize("width", [40, 33])
-def test_several_pieces_in_every_type(gpu, type, width):
+def test_several_pieces_in_every_type(gpu, type, weights, width):
     """More gradients than a piece holds, labels in every piece, the last word's and the first's among them: every element against 64 bits on the GPU.
-    (At once, the last piece's elements in 16 bits are rounded twice.)"""
+    (At once, the last piece's elements in 16 bits are rounded twice, and for d_weight those of small weight.)"""
     torch, rk, ctx = gpu
     rows, vocab, t = 4200, 140001, getattr(torch, type)
     g = torch.Generator("cuda").manual_seed(width)
@@ -30,7 +30,8 @@ def test_several_pieces_in_every_type(gpu, type, width):
     label[:3] = torch.tensor([0, vocab - 1, -1])
     f = lambda *s: torch.full(s, float("nan"), device="cuda")
     loss, lse, total, dx, dw = f(rows), f(rows), f(1), n(rows, width), n(vocab, width)
-    given = (ctx, rk.make_head(), x, words, label, None)
+    row_weight = torch.exp2(torch.randint(-20, 1, (rows,), generator=g, device="cuda").float()) if weights else torch.ones(rows, device="cuda")
+    given = (ctx, rk.make_head(), x, words, label, row_weight if weights else None)
     rk.rk_head_loss_backward(*given, None, loss, lse, total, dx, dw)
     dx2, dw2 = torch.empty_like(dx), torch.empty_like(dw)
     rk.rk_head_backward(*given, lse, None, dx2, dw2)
@@ -50,6 +51,7 @@ def test_several_pieces_in_every_type(gpu, type, width):
         d = p.clone()
         d[at[keep], own[keep]] -= 1
         d[~keep], p[~keep] = 0, 0
+        d, p = d * row_weight[part, None], p * row_weight[part, None]
         most = d.abs() + p
         exact["dx"][part], size["dx"][part] = d @ w64, most @ w64.abs()
         exact["dw"] += d.t() @ x64
@@ -60,10 +62,12 @@ def test_several_pieces_in_every_type(gpu, type, width):
     for got, want in ((lse, exact["lse"]), (loss, exact["loss"])):
         assert bool(((got.double() - want).abs() <= 2 * logit + 64 * U32 * (want.abs() + 1)).all())
     half = torch.finfo(t).eps / 2 if type != "float32" else 0.0
-    for times, which, name in ((2, dx, "dx"), (1, dx2, "dx"), (2, dw, "dw"), (1, dw2, "dw")):
+    # half of the smallest step of float16: of a 2^38th of the largest weight, of rows below a 64th of it of their own
+    least = torch.where(row_weight >= 2.0 ** -6, 1.0, row_weight.double())[:, None]
+    for times, which, name in ((2, dx, "dx"), (1, dx2, "dx"), (2, dw, "dw"), (2 if weights else 1, dw2, "dw")):
         other = (w64 if name == "dx" else x.double()).abs().sum(0)[None]
         steps = (vocab if name == "dx" else rows) / 4 + 64
-        tol = (times * half + p + steps * U32) * size[name] + half * (1 + 2.0 ** -8) * exact[name].abs() + TINY[type] + 2.0 ** (-39 if type == "float16" else -126) * 4 * other
+        tol = (times * half + p + steps * U32) * size[name] + half * (1 + 2.0 ** -8) * exact[name].abs() + TINY[type] + 2.0 ** (-39 if type == "float16" else -126) * 4 * other * (least if name == "dx" else 1.0)
         bad = ~((which.double() - exact[name]).abs() <= tol)
         assert not bool(bad.any()), (name, times, int(bad.sum()), bad.nonzero()[0].tolist())
 
