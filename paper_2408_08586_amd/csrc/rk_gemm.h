@@ -56,7 +56,7 @@ __device__ __forceinline__ Vec<uint32_t, 2> turned(const char *lds) {
 template <int N> __device__ __forceinline__ void landed() {
     asm volatile("" ::: "memory");
 #ifdef __HIP_DEVICE_COMPILE__
-    __builtin_amdgcn_s_waitcnt(0xC07F & ~0xC00F | (N & 0xF) | (N >> 4 << 14));     // vmcnt(N) lgkmcnt(0)
+    __builtin_amdgcn_s_waitcnt((0xC07F & ~0xC00F) | (N & 0xF) | (N >> 4 << 14));   // vmcnt(N) lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
 #endif
     asm volatile("" ::: "memory");

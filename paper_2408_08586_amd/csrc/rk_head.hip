@@ -273,8 +273,7 @@ struct JoinArgs {
     uint32_t n_parts;
     bool first, last;           // of the pieces
     float z_weight;
-    float *loss, *lse, *total;
-    uint64_t n_rows;
+    float *loss, *lse;
 };
 // 64 lanes a row: a row's parts in as many runs, joined in fixed order
 constexpr uint32_t HD_RUNS = 64;
@@ -652,7 +651,7 @@ template <typename T> int32_t run_typed(rk_ctx *ctx, const Call &C) {
     if (C.total) {
         if ((rc = rk_scratch(ctx, SL_HEAD_PARTS, words * sums_each, (void **)&L.parts)) != RK_OK) return rc;
         L.parts_stride = rows_pad;
-        JoinArgs J{R, L.parts, rows_pad, 0, false, false, C.head->z_weight, C.loss, C.lse, C.total, C.n_rows};
+        JoinArgs J{R, L.parts, rows_pad, 0, false, false, C.head->z_weight, C.loss, C.lse};
         for (uint64_t first = 0; first < C.vocab && C.n_rows; first += words) {
             if ((rc = piece(first)) != RK_OK) return rc;
             L.first = (uint32_t)first; L.words = n_words;
