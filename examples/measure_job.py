@@ -198,8 +198,8 @@ class Student:
 
 def measure(hidden, seq, micro_batch, layers=2, experts=8, top_k=2, vocab=32000, kept=64, steps=8, rate=1e-3, seed=0, recurrence=False, dropout=0.0,
             head=False):
-    """Trains for `steps` steps; seconds forward and backward of one, bytes that the forward keeps, each also of the layers alone, the
-    student's parameters, and the losses by step."""
+    """Trains for `steps` steps; seconds forward and backward of one, bytes that the forward keeps, each also of the layers alone, the bytes of
+    the library's own working buffers, the student's parameters, and the losses by step."""
     ctx = rk.rk_create(0)
     student = Student(hidden, layers, experts, top_k, vocab, seq, seed, recurrence, dropout, head)
     of_labels = rk.make_head() if head else None
@@ -250,16 +250,18 @@ def measure(hidden, seq, micro_batch, layers=2, experts=8, top_k=2, vocab=32000,
         history.append((float(total), sum(float(l.detach()[0]) for l in losses) / len(losses)))
         del logits, losses, d_logits                    # (the next step's forward is not to find them where it counts what it keeps)
     rk.rk_sync(ctx)
+    bytes_library = rk.rk_workspace_bytes(ctx)              # (torch's count has not seen them)
     rk.rk_destroy(ctx)
     forward, forward_layers, backward, backward_layers = (float(t) for t in np.median(np.array(times[1:] or times), axis=0))
     return dict(forward=forward, forward_layers=forward_layers, backward=backward, backward_layers=backward_layers,
-                bytes_kept=int(kept_at["forward"] - before), bytes_layers=int(kept_at["head"] - kept_at["layers"]),
+                bytes_kept=int(kept_at["forward"] - before), bytes_layers=int(kept_at["head"] - kept_at["layers"]), bytes_library=bytes_library,
                 params_layers=student.params_layers, params_rest=student.params_rest, history=history)
 
 
 def descriptor(workload, job, m, layers, seq, micro_batch):
     """The workload's job with what was measured in place of its drawn coefficients: what the layers take, keep and are is scaled to all
-    of the job's layers, what is outside them counts once (what it keeps, at the measured micro-batch, is part of the constant)."""
+    of the job's layers, what is outside them counts once (what it keeps, at the measured micro-batch, is part of the constant, and so are
+    the library's working buffers, which all layers share)."""
     coef, ints = workload.coef.copy(), workload.ints.copy()
     col = {n: i for i, n in enumerate(workloads.COEF_FIELDS)}
     times, hidden = float(ints[job, 0]) / layers, float(coef[job, col["hidden"]])
@@ -269,7 +271,7 @@ def descriptor(workload, job, m, layers, seq, micro_batch):
     coef[job, col["t_fwd_sample"]] = forward / micro_batch
     coef[job, col["k_bwd"]] = max(1.0, backward / forward)
     coef[job, col["mem_act"]] = m["bytes_layers"] / (seq * micro_batch * hidden * layers)
-    coef[job, col["mem_const"]] += m["bytes_kept"] - m["bytes_layers"]
+    coef[job, col["mem_const"]] += m["bytes_kept"] - m["bytes_layers"] + m.get("bytes_library", 0)
     return coef, ints
 
 
@@ -294,7 +296,7 @@ def main(argv=None):
         print(f"step {step}: loss {total:.4f}, balance {balance:.4f}")
     print(f"{a.measured_layers} layers of {hidden}: forward {m['forward'] * 1e3:.2f} ms, backward {m['backward'] * 1e3:.2f} ms, "
           f"{m['bytes_kept'] / 2 ** 20:.0f} MiB kept; of the layers alone {m['forward_layers'] * 1e3:.2f} and {m['backward_layers'] * 1e3:.2f} ms, "
-          f"{m['bytes_layers'] / 2 ** 20:.0f} MiB")
+          f"{m['bytes_layers'] / 2 ** 20:.0f} MiB; working buffers of the library {m['bytes_library'] / 2 ** 20:.0f} MiB")
     wl = workloads.tiny()
     col = {n: i for i, n in enumerate(workloads.COEF_FIELDS)}
     wl.coef[0, [col["hidden"], col["seq"]]] = hidden, a.seq

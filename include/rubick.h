@@ -164,6 +164,9 @@ typedef struct {
 int32_t rk_create(rk_ctx **ctx, int32_t device_id, void *hip_stream);
 int32_t rk_destroy(rk_ctx *ctx);
 int32_t rk_sync(rk_ctx *ctx);
+/* How much device memory the context's working buffers take by now: they grow with the largest calls, by a quarter more than these
+ * need, and are kept until rk_destroy. */
+int32_t rk_workspace_bytes(const rk_ctx *ctx, uint64_t *bytes);
 const char *rk_last_error(const rk_ctx *ctx);
 
 /* Plan enumeration (Sec. 3 "execution plans", Table 1: d*t*p = g; Fig. 6:

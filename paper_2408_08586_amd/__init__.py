@@ -23,7 +23,7 @@ RK_MAX_TENANTS = 256
 RK_FIT_PARAMS, RK_FIT_MAX_STARTS, RK_FIT_MAX_SAMPLES, RK_FIT_K_MAX = 7, 8, 64, 32.0
 FIT_FIELDS = ("k_bwd", "k_sync", "k_opt", "k_opt_off", "k_off", "k_swap", "k_const")
 
-EXPORTS = ("rk_create", "rk_destroy", "rk_sync", "rk_last_error", "rk_enumerate_plans", "rk_eval_candidates",
+EXPORTS = ("rk_create", "rk_destroy", "rk_sync", "rk_workspace_bytes", "rk_last_error", "rk_enumerate_plans", "rk_eval_candidates",
            "rk_best_plan", "rk_curves", "rk_job_curves", "rk_allocate", "rk_schedule_round", "rk_schedule_rounds",
            "rk_eval_points", "rk_min_res", "rk_allocate_sla", "rk_schedule_round_sla", "rk_fit_models", "rk_simulate", "rk_schedule_rounds_shared", "rk_place", "rk_allocate_static", "rk_place_plans",
            "rk_schedule_round_placed", "rk_reschedule", "rk_probe_stream", "rk_eval_best_plan", "rk_reschedule_nodes", "rk_best_plan_placed", "rk_reschedule_rounds", "rk_schedule_round_nodes", "rk_privileged", "rk_curve_slopes",
@@ -247,6 +247,15 @@ def rk_destroy(ctx):
 
 def rk_sync(ctx):
     _check(ctx, load_library().rk_sync(ctx))
+
+
+def rk_workspace_bytes(ctx) -> int:
+    """Bytes of device memory in the context's working buffers."""
+    bytes_ = C.c_uint64()
+    rc = load_library().rk_workspace_bytes(ctx, C.byref(bytes_))
+    if rc != RK_OK:
+        raise RkError(rc, "rk_workspace_bytes failed")
+    return bytes_.value
 
 
 def rk_last_error(ctx) -> str:

@@ -140,6 +140,13 @@ int32_t rk_sync(rk_ctx *ctx) {
     return RK_OK;
 }
 
+int32_t rk_workspace_bytes(const rk_ctx *ctx, uint64_t *bytes) {
+    if (!ctx || !bytes) return RK_ERR_INVALID_ARG;
+    *bytes = 0;
+    for (int i = 0; i < RK_SCRATCH_SLOTS; ++i) *bytes += ctx->scratch_bytes[i];
+    return RK_OK;
+}
+
 int32_t rk_ctx_ways(const rk_ctx *ctx, uint32_t *ways) {
     if (!ctx || !ways) return 0;
     for (int i = 0; i < WAY_COUNT; ++i) ways[i] = ctx->ways[i];
