@@ -920,6 +920,8 @@ class Recur:
             _refuse("bias is no contiguous vector")
         if offsets is not None and (offsets.dim() != 1 or len(offsets) < 1 or seq_rows):
             _refuse("offsets are a vector of the sequences' number and one, or there are seq_rows")
+        if not 0 <= int(seq_rows) < 1 << 64:
+            _refuse(f"sequences of {seq_rows} rows")
         self.bias, self.offsets = bias, offsets
         self.n_seqs = None if offsets is None else len(offsets) - 1
         at = None if offsets is None else _plain(offsets, "offsets", offsets.shape, _I32)
