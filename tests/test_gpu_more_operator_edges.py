@@ -51,3 +51,47 @@ def test_float16_weights_of_very_different_rows(gpu, z, d_total):
             assert bool(torch.isfinite(out[k]).all())
             bad = ~((d(out[k]) - exact[k]).abs() <= tol)
             assert not bool(bad.any()), (which, k, int(bad.sum()), bad.nonzero()[0].tolist())
+
+
+class Far:
+    """Matrices side by side in rows that lie `stride` elements apart."""
+
+    def __init__(self, torch, rows, stride, t):
+        self.room, self.at = torch.empty(rows * stride, dtype=t, device="cuda").view(rows, stride), 0
+
+    def __call__(self, v):
+        self.at += 128
+        return self.room[:v.shape[0], self.at - 128:self.at - 128 + v.shape[1]].copy_(v)
+
+
+@pytest.mark.parametrize("type", ["bfloat16", "float32"])
+def test_rows_beyond_2_to_32_elements(gpu, type):
+    """Rows so far apart that the last begin beyond 2^32 elements: bit for bit what rows side by side give."""
+    torch, rk, ctx = gpu
+    t, rows, width = getattr(torch, type), 560, 72
+    g = torch.Generator().manual_seed(3)
+    n = lambda *s: torch.randn(*s, generator=g).to(t).cuda()
+    near = lambda v: v.clone()
+    x, z, dh = n(rows, width), n(rows, width), n(rows, width)
+    recur = rk.Recur(bias=n(width), offsets=torch.tensor([0, 300, 300, rows], dtype=torch.int32, device="cuda"))
+    got = []
+    for at in (near, Far(torch, rows, 1 << 23, t)):
+        h, dx, dz, db = at(x * 0), at(x * 0), at(x * 0), torch.empty(width, device="cuda")
+        rk.rk_recur_forward(ctx, recur, at(x), at(z), None, h, None)
+        rk.rk_recur_backward(ctx, recur, at(x), at(z), h, None, at(dh), None, dx, dz, None, db)
+        got.append((h.clone(), dx.clone(), dz.clone(), db))
+        rk.rk_sync(ctx)
+    del at, h, dx, dz
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    # words of the head: so far apart that they are padded first, and less far
+    for vocab, stride in ((560, 1 << 23), (1 << 14, 1 << 19)):
+        words, label, got = n(vocab, width), torch.randint(0, vocab, (90,), generator=g).int().cuda(), []
+        for at in (near, Far(torch, vocab, stride, t)):
+            f = lambda *s: torch.full(s, float("nan"), device="cuda")
+            dx, dw, loss, lse, total = at(x[:90] * 0), at(words * 0), f(90), f(90), f(1)
+            rk.rk_head_loss_backward(ctx, rk.make_head(), at(x[:90]), at(words), label, None, None, loss, lse, total, dx, dw)
+            got.append((dx.clone(), dw.clone(), loss, lse, total))
+            rk.rk_sync(ctx)
+        del at, dx, dw
+        assert all(torch.equal(a, b) and bool(torch.isfinite(a).all()) for a, b in zip(*got))
+    torch.cuda.empty_cache()
