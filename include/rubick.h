@@ -959,7 +959,7 @@ int32_t rk_distill_loss_backward(rk_ctx *ctx, const rk_distill *distill, uint64_
  *     h_t = f_t h_{t-1} + x_t                (otherwise)
  * h before a sequence's first row is its row of state_in, or zero.  Sequence i has rows offsets[i] to
  * offsets[i + 1] - 1 (offsets [device] n_seqs + 1, ascending, none below 0 or above the rows; equal ones: a
- * sequence without rows); rows that no sequence has are neither read nor written.  offsets null:
+ * sequence without rows); rows that no sequence has count for nothing and are not written.  offsets null:
  * every seq_rows rows are a sequence, the last may have fewer; seq_rows 0: all rows are one. */
 typedef struct {
     uint32_t coupled;
@@ -1010,7 +1010,7 @@ int32_t rk_dropout_backward(rk_ctx *ctx, const rk_dropout *dropout, uint64_t n_r
 
 #define RK_HEAD_MAX_WIDTH 65536u
 
-/* The loss of rows x under a vocabulary's weights, without keeping their logits:
+/* The loss of rows x under a vocabulary's weights, without handing out their logits:
  *     l = logit_scale x weight^T     lse = log sum exp l     loss = lse - l[label] + z_weight lse^2
  * A row whose label lies outside the vocabulary or whose weight is 0 is left out, whatever it holds: loss, lse
  * and gradients 0. */
@@ -1035,7 +1035,13 @@ int32_t rk_head_backward(rk_ctx *ctx, const rk_head *head, uint64_t n_rows, uint
                          const rk_matrix *weight, const int32_t *label, const float *row_weight_or_null, const float *lse,
                          const float *d_total_or_null, const rk_matrix *dx_or_null, const rk_matrix *d_weight_or_null);
 
-/* Both at once, where the gradient of total is known beforehand. */
+/* Both at once, where the gradient of total is known beforehand.  The loss leaves its exponentials of the last piece, rounded, for the gradients, so that a
+ * vocabulary of one piece takes three products and not four; of 16-bit types these gradients are rounded twice and may differ by that from
+ * those of the two calls.
+ *
+ * Working buffers: the rows that count; with gradients a piece's, which are as many as 2^30 bytes hold (together with the piece's weights where these
+ * have to be copied, because their rows do not begin and end at 16 bytes; 256 words at least), and dx in 32 bits once for every share of the words that is
+ * summed by itself (up to 64, fewer the more rows there are); for the loss 8 bytes for every row and 256 words, up to 2^28. */
 int32_t rk_head_loss_backward(rk_ctx *ctx, const rk_head *head, uint64_t n_rows, uint32_t width, uint32_t vocab,
                               const rk_matrix *x, const rk_matrix *weight, const int32_t *label, const float *row_weight_or_null,
                               const float *d_total_or_null, float *loss, float *lse, float *total, const rk_matrix *dx_or_null,

@@ -79,8 +79,8 @@ template <typename T, uint32_t PIECES> __device__ __forceinline__ uint32_t order
     if constexpr (sizeof(T) == 4) return (k >> 2 & 3u) * 4u % PIECES;
     else return ((k & 3u) | (k >> 3 & 3u) << 2) * 2u % PIECES;
 }
-// What a wavefront asks for of a tile of R elements: R / 64 instructions of 1,024 bytes, of small tiles one, some of them twice, so that
-// every wavefront has as many under way.
+// What a wavefront asks for of a tile of R elements, which is R / 16 instructions of 1,024 bytes: an eighth of these, rounded up, some of them twice, so
+// that every wavefront has as many under way.
 template <typename T, int R, int WAY> struct Fetch {
     static constexpr int N = (R / 16 + (int)GM_WAVES - 1) / (int)GM_WAVES;
     static constexpr uint32_t KS = GM_STEP / sizeof(T), PIECES = R * sizeof(T) / 16;    // k of a step; ACROSS: pieces of a row of LDS

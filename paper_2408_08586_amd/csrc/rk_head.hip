@@ -8,7 +8,8 @@
 // dx adds up g W over the pieces in float32, and the piece's rows of d_weight are g^T x.  By far the largest element of a row is its label's: what
 // rounding to 16 bits takes off it is kept and its products are added to dx and d_weight in float32 (777 x 50021 x 1111 in float16: both are
 // 2.1e-4 from the definition, all of it their own rounding, and 3.5e-4 without).  Where the loss is made along with
-// them, it leaves the exponentials of the piece that it ends with, which then only have to be scaled.
+// them, it leaves the exponentials of the piece that it ends with, which then only have to be scaled: of a vocabulary of one piece all of them, of a longer one
+// what is left for the last piece.
 //
 // The products' kernels are bound by the matrix units (figures in rk_gemm.h), what stands around them by memory: for 2,048 x 128,000 x 5,248 in bfloat16 the rows'
 // gathering takes 10 us, k_head_join 9, k_head_scale 147 (0.94 GB, 6.4 TB/s) instead of the 2.2 ms of another product, k_head_dx_out 40.
@@ -563,7 +564,8 @@ template <typename T, typename F> void with_rows(uint32_t tile, F f) {
 }
 // Rows of a tile.  Few take small tiles, which leave LDS for two workgroups a compute unit (5 x 128000 x 5248: 258 us, with tiles of 256 rows 368).
 // More of 16 bits take the largest, even where it is half empty (300 x 64000 x 4096: 238 us, of 192 rows 244, of 128 rows 263); of 32 bits, where only
-// the matrix units' time counts, the one that has the fewest rows in all turns of the compute units (300 x 64000 x 4096: 1,867, 1,451 and 1,420 us).
+// the matrix units' time counts, the one that has the fewest rows in all turns of the compute units (300 x 64000 x 4096: 1,867, 1,451 and 1,420 us).  Neither is
+// made for vocabularies of fewer tiles than compute units, which leave many of these without work (1000 x 1000 x 1000 in 16 bits, loss and gradients: 128 us).
 template <typename T> uint32_t rows_of_tile(uint64_t n_rows, uint64_t tiles_a) {
     if (n_rows <= 128) return n_rows <= 32 ? 32 : n_rows <= 64 ? 64 : 128;
     uint32_t best = 256;

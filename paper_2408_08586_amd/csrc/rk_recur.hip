@@ -13,10 +13,13 @@
 // looks behind the beginning of a sequence, so that nothing of one sequence comes near another.
 //
 // The gates' exponentials and divisions, the chain and the two ways through the rows are about 20 vector instructions an element forward and 44 backward, two fifths of the
-// kernels' cycles; the rest is the rows' trip from memory and then the wait for the tiles before, under which two workgroups a compute unit have too little else to do.
+// kernels' cycles; the rest is the rows' trip from memory and then the wait for the tiles before, under which two workgroups a compute unit have too little else to do
+// (forward's gates and inflows take 64 of a lane's 128 registers through the wait; backward spills up to 204 bytes a lane).  Finding rows' sequences by their offsets is
+// log2 of their number loads, each behind the one before: 64 x 5,248 of one row each 7.8 us, by seq_rows 7.1; 20,000 x 1,000 of 2 or of 1,000 sequences 48.
 // Measured in bfloat16, coupled, kernels alone: forward 8,192 x 8,576 of equal sequences 92 to 95 us (421 MB, 4.5 TB/s); backward 8,192 x 5,248 118 to 122 us
 // (516 MB, 4.3 TB/s), k_recur_bias 4 to 5, k_recur_clear 3 to 6.  One sequence of 65,536 x 1,024, not coupled: 102 to 106 us (403 MB, 3.9 TB/s): its 32 blocks
-// of tiles wait for each other, about 1 us a block beyond what memory takes.  Blocks of 8 tiles or of 32, wavefronts of 8 rows or four to a workgroup were slower in most.
+// of tiles wait for each other, about 1 us a block beyond what memory takes.  Blocks of 8 tiles or of 32, wavefronts of 8 rows or four to a workgroup were slower in most
+// (timed with sequences of 2,048 rows, which a block holds whole, ragged ones and one of all rows; as it is, 8,192 x 8,576 takes 90 to 94 us for sequences of 1,000 to 8,192 rows).
 #include <type_traits>
 
 #include "rk_vec.h"
